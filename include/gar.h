@@ -361,6 +361,147 @@ GAR_API int gar_optimal_steps(int P, double m_bytes, double alpha, double beta, 
 #define GAR_NOALLOC_MAX_P 64
 GAR_API int gar_allreduce_noalloc(gar_plan *plan, void *const *rank_buffers, gar_stream_t stream);
 
+/* ---------------------------------------------------------------------------------------
+ * Decoding operators: what a model split over P virtual ranks runs between its
+ * Allreduces when it produces one token at a time.  Rotary positions, a paged key-value
+ * cache that may be quantised as it is written, and attention of one new token over that
+ * cache.  The paper has no counterpart of any of them; what ties them to the Allreduce is
+ * that attention over a share of a sequence gives a partial result (output, log of the sum
+ * of weights), and the ranks' partial results are joined by a max- and a sum-Allreduce.
+ *
+ * The conventions above hold: GAR_OK or a negative code, work enqueued on `stream`, no
+ * allocation and no wait in the calls that take a stream except where stated (so they can
+ * be captured into a CUDA graph), buffers owned by the caller.  Strides count elements;
+ * the channels of one head are contiguous. */
+
+/* Element types beyond the Allreduce's: 16-bit IEEE floats, and the 8-bit cache types
+ * (signed integers in [-127, 127]; floats with 4 exponent and 3 mantissa bits, at most
+ * 448).  Allreduce plans refuse them. */
+enum { GAR_F16 = 3, GAR_I8 = 4, GAR_E4M3 = 5 };
+
+#define GAR_MAX_HEAD_DIM 256 /* largest number of channels of one head */
+
+/* Which channels form a pair of the first `rot` channels: c and c + rot/2, or 2c and 2c+1. */
+enum { GAR_ROPE_HALF = 0, GAR_ROPE_INTERLEAVED = 1 };
+
+/* How the rotary frequencies base^(-2i/rot) are changed for contexts longer than those a
+ * model was trained on.  LINEAR: divided by `factor`.  BASE: the base grows by
+ * factor^(rot/(rot-2)), which leaves the fastest pair and divides the slowest by factor.
+ * PARTS: pairs that turn fewer than 1 time over the `original` positions are divided by
+ * factor, those that turn more than 32 times are kept, a linear ramp between; the rotation
+ * is also multiplied by 0.1 ln(factor) + 1 ("NTK-by-parts" and attention temperature of
+ * arXiv 2309.00071, Secs. 3.2 and 3.4). */
+enum { GAR_ROPE_PLAIN = 0, GAR_ROPE_LINEAR = 1, GAR_ROPE_BASE = 2, GAR_ROPE_PARTS = 3 };
+
+/* Fills rot/2 frequencies (radians per position) and the magnitude of the rotation.
+ * rot: even, 2..GAR_MAX_HEAD_DIM (BASE: at least 4).  factor >= 1, original > 0 (PARTS).  Host-only. */
+GAR_API int gar_rope_frequencies(int rot, double base, int scaling, double factor, double original,
+                                 double *frequencies, double *magnitude);
+
+/* Fills the device table [count][rot/2][2] with magnitude * (cos, sin) of (first + row) *
+ * frequencies[pair], angles and functions in 64 bits, entries rounded once to 32 bits: at
+ * position 10^6 an angle in 32 bits would be off by 0.03 radians.  frequencies: host array. */
+GAR_API int gar_rope_table(float *table, int64_t first, int64_t count, int rot,
+                           const double *frequencies, double magnitude, gar_stream_t stream);
+
+/* out = x with the first `rot` of its `dim` channels rotated by the table row of the
+ * token's position, the rest copied.  x, out: [tokens][heads][dim] of dtype GAR_F32,
+ * GAR_BF16 or GAR_F16, any token and head strides; out may equal x with equal strides,
+ * other overlaps are undefined.  inverse: rotates back by the same angles (and multiplies
+ * by the same magnitude), which is the gradient: grad_x = gar_rope(grad_out, inverse).
+ * positions: `tokens` integers of position_bytes (4 or 8) bytes.  A position outside
+ * [0, table_rows) makes the row's rotated channels NaN.  Products and sums round to 32
+ * bits one by one; the result rounds once to dtype. */
+GAR_API int gar_rope(const void *x, int64_t x_token_stride, int64_t x_head_stride, void *out,
+                     int64_t out_token_stride, int64_t out_head_stride, int dtype, int64_t tokens,
+                     int heads, int dim, int rot, const void *positions, int position_bytes,
+                     const float *table, int64_t table_rows, int layout, int inverse,
+                     gar_stream_t stream);
+
+/* A paged cache: k and v hold [pages][heads][page_size][dim] elements in any order that
+ * leaves the channels contiguous (the strides are those of both).  dtype GAR_F32, GAR_BF16,
+ * GAR_F16, or GAR_I8 / GAR_E4M3 with one 32-bit scale for each key and value row in
+ * k_scale and v_scale ([pages][heads][page_size], strides of their own); NULL otherwise.
+ * A row that stands for values x holds codes round(x / scale) (to nearest, ties to even),
+ * scale = max|x| * (1/127) or max|x| * (1/448), each operation rounded to 32 bits, and reads
+ * back as code * scale.  A row with an infinity or a NaN reads
+ * back as NaN throughout.
+ * status: a device word that the kernels set when an index is out of range (such an index
+ * never reads or writes outside the cache); zero it once.  May be NULL. */
+typedef struct {
+  void *k, *v;
+  float *k_scale, *v_scale;
+  uint32_t *status;
+  int64_t pages;
+  int64_t page_stride, head_stride, token_stride;
+  int64_t scale_page_stride, scale_head_stride, scale_token_stride;
+  int32_t dtype, heads, dim, page_size;
+} gar_kv_cache;
+
+/* Bits of the status word. */
+enum { GAR_KV_BAD_SLOT = 1, GAR_KV_BAD_PAGE = 2, GAR_KV_BAD_POSITION = 4, GAR_KV_BAD_LENGTH = 8 };
+
+/* Writes the keys and values of `tokens` tokens ([tokens][heads][dim] of dtype GAR_F32,
+ * GAR_BF16 or GAR_F16; a cache of float type takes its own type) to the cache slots
+ * slots[t] = page * page_size + row (64-bit, distinct).  A negative slot skips the token; one past the
+ * cache is skipped and sets GAR_KV_BAD_SLOT.  With positions (else NULL) the keys'
+ * first rot channels are rotated as by gar_rope, in 32 bits, before they are quantised or
+ * rounded; a bad position sets GAR_KV_BAD_POSITION and writes NaN. */
+GAR_API int gar_kv_write(const gar_kv_cache *cache, const void *k, int64_t k_token_stride,
+                         int64_t k_head_stride, const void *v, int64_t v_token_stride,
+                         int64_t v_head_stride, int dtype, int64_t tokens, const int64_t *slots,
+                         const void *positions, int position_bytes, const float *table,
+                         int64_t table_rows, int rot, int layout, gar_stream_t stream);
+
+/* Reads the slots' keys and values back into contiguous [tokens][heads][dim] arrays of
+ * dtype GAR_F32, GAR_BF16 or GAR_F16, rounded once.  Rows of negative slots (and of
+ * slots past the cache, which set GAR_KV_BAD_SLOT) are zero. */
+GAR_API int gar_kv_read(const gar_kv_cache *cache, const int64_t *slots, int64_t tokens, void *k,
+                        void *v, int dtype, gar_stream_t stream);
+
+/* Waits for `stream`, then returns GAR_OK if no kernel has set the cache's status word
+ * since it was last cleared; else clears it and returns GAR_EINVAL with the bits in *bits
+ * (may be NULL) and their meaning in gar_last_error(). */
+GAR_API int gar_kv_status(const gar_kv_cache *cache, uint32_t *bits, gar_stream_t stream);
+
+typedef struct gar_attn_plan gar_attn_plan;
+
+/* Attention of one new token per sequence: q_heads queries over kv_heads cached heads of
+ * dim channels, q_heads a multiple of kv_heads; query head h reads cached head
+ * h / (q_heads / kv_heads).  Host-only. */
+GAR_API int gar_attn_plan_create(gar_attn_plan **out, int q_heads, int kv_heads, int dim);
+/* NULL is a no-op.  No work using the plan may still be running. */
+GAR_API void gar_attn_plan_destroy(gar_attn_plan *plan);
+/* Bytes of device workspace a plan needs (whatever the batch and the lengths).  Host-only. */
+GAR_API int gar_attn_plan_bytes(const gar_attn_plan *plan, size_t *workspace_bytes);
+/* Attaches the caller's workspace (16-byte aligned) and clears its counters, waiting until
+ * that is done; call it outside stream captures.  The workspace holds the partial results
+ * of one call at a time: order the calls of one plan on one stream, or use a plan for
+ * each stream. */
+GAR_API int gar_attn_plan_set_workspace(gar_attn_plan *plan, void *dev_ptr, size_t bytes);
+
+/* For each sequence b and query head h, over the cached rows n in [lengths[b] - window,
+ * lengths[b]) (all below lengths[b] when window is 0):
+ *   out = sum_n softmax_n(scale q.k_n) v_n,   lse = ln sum_n exp(scale q.k_n).
+ * A head without rows (length 0) gives out 0 and lse -infinity.  What the cache holds in
+ * other rows, NaN or infinities too, has no effect.
+ * q: [batch][q_heads][dim] of dtype GAR_BF16, GAR_F16 or GAR_F32 with strides; the cache
+ * is of the same type or of an 8-bit type.  out: the same shape, of q's type or GAR_F32 (for joining
+ * ranks' shares).  lse: contiguous [batch][q_heads], or NULL.
+ * page_table: [batch][table_width] page numbers with a row stride; row n of sequence b is
+ * row n % page_size of page page_table[b][n / page_size].  A page number outside the cache
+ * sets GAR_KV_BAD_PAGE and its rows count as zeros; a length that is negative or past table_width *
+ * page_size sets GAR_KV_BAD_LENGTH and counts as the nearest that is not.
+ * Scores, the running maximum and sum, and outputs are held in 32 bits until the one
+ * rounding of out; weights enter the products as two 16-bit parts, about 2^-17 relative.  Results do not depend on timing: partial results
+ * are joined in the order of the rows. */
+GAR_API int gar_decode_attention(gar_attn_plan *plan, const gar_kv_cache *cache, const void *q,
+                                 int64_t q_batch_stride, int64_t q_head_stride, int q_dtype,
+                                 void *out, int64_t out_batch_stride, int64_t out_head_stride,
+                                 int out_dtype, float *lse, const int32_t *page_table,
+                                 int64_t table_stride, int table_width, const int32_t *lengths,
+                                 int batch, float scale, int window, gar_stream_t stream);
+
 /* Library self-test for build checks: generates and compiles (host-only, no GPU) the
  * fused kernels of a few plans.  Returns GAR_OK or GAR_EJIT. */
 GAR_API int gar_selftest_compile(void);

@@ -23,8 +23,9 @@ INCLUDE = os.path.join(ROOT, "include")
 OUT = os.path.join(PKG, "libgar.so")
 BUILD = os.path.join(ROOT, "_build")
 
-SOURCES = ["api.cpp", "plan.cpp", "codegen.cpp", "jit.cpp", "step_kernels.cu"]
-HEADERS = ["gar_internal.hpp"]
+SOURCES = ["api.cpp", "plan.cpp", "codegen.cpp", "jit.cpp", "step_kernels.cu", "rope.cu", "cache.cu",
+           "decode_api.cu", "decode_general.cu"]
+HEADERS = ["gar_internal.hpp", "gar_device.cuh", "decode.cuh"]
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 
 

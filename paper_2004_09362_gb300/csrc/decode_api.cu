@@ -1,0 +1,136 @@
+// Decode attention: plans, workspaces, checks of arguments, choice of the kernel.
+#include <algorithm>
+#include <cmath>
+#include <new>
+
+#include "decode.cuh"
+
+struct gar_attn_plan {
+  int q_heads, kv_heads, dim;
+  int device = -1, sms = 0;
+  void *ws = nullptr;
+};
+
+namespace gar {
+namespace {
+
+constexpr size_t kCounterBytes = (kMaxCtas * sizeof(unsigned) + 255) / 256 * 256;
+
+int dim_pad(int dim) { return (dim + 31) / 32 * 32; }
+
+size_t workspace_bytes(const gar_attn_plan &p) {
+  const size_t rows = (size_t)kMaxCtas * 2 * kMaxGroup;
+  return kCounterBytes + rows * (2 + dim_pad(p.dim)) * sizeof(float);
+}
+
+// Round-up reciprocal: n / d = (umulhi(mul, n) + n) >> shift for n < 2^31.
+Divide divide_by(uint32_t d) {
+  uint32_t shift = 0;
+  while ((1ull << shift) < d) ++shift;
+  return {(uint32_t)(((1ull << 32) * ((1ull << shift) - d)) / d + 1), shift};
+}
+
+}  // namespace
+}  // namespace gar
+
+using namespace gar;
+
+extern "C" {
+
+int gar_attn_plan_create(gar_attn_plan **out, int q_heads, int kv_heads, int dim) {
+  if (out == nullptr) return refuse("null output");
+  if (kv_heads < 1 || q_heads < 1 || q_heads % kv_heads) return refuse("q_heads must be a multiple of kv_heads");
+  if (dim < 1 || dim > GAR_MAX_HEAD_DIM) return refuse("dim must be 1..256");
+  gar_attn_plan *p = new (std::nothrow) gar_attn_plan{q_heads, kv_heads, dim};
+  if (p == nullptr) {
+    set_error("no memory for a plan");
+    return GAR_ENOMEM;
+  }
+  *out = p;
+  return GAR_OK;
+}
+
+void gar_attn_plan_destroy(gar_attn_plan *plan) { delete plan; }
+
+int gar_attn_plan_bytes(const gar_attn_plan *plan, size_t *bytes) {
+  if (plan == nullptr || bytes == nullptr) return refuse("null plan or output");
+  *bytes = workspace_bytes(*plan);
+  return GAR_OK;
+}
+
+int gar_attn_plan_set_workspace(gar_attn_plan *plan, void *dev_ptr, size_t bytes) {
+  if (plan == nullptr) return refuse("null plan");
+  if (dev_ptr == nullptr) {
+    plan->ws = nullptr;
+    return GAR_OK;
+  }
+  if ((uintptr_t)dev_ptr % 16) {
+    set_error("the workspace must be 16-byte aligned");
+    return GAR_EALIGN;
+  }
+  if (bytes < workspace_bytes(*plan)) {
+    set_error("the workspace is smaller than gar_attn_plan_bytes");
+    return GAR_ENOWS;
+  }
+  int dev = -1, sms = 0;
+  cudaError_t e = cudaGetDevice(&dev);
+  if (e == cudaSuccess) e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);
+  if (e == cudaSuccess) e = cudaMemset(dev_ptr, 0, kCounterBytes);
+  if (e == cudaSuccess) e = cudaStreamSynchronize(nullptr);
+  if (e != cudaSuccess) return cuda_fail(e, "gar_attn_plan_set_workspace");
+  plan->ws = dev_ptr, plan->device = dev, plan->sms = std::min(sms, 152);
+  return GAR_OK;
+}
+
+int gar_decode_attention(gar_attn_plan *plan, const gar_kv_cache *cache, const void *q, int64_t q_batch_stride,
+                         int64_t q_head_stride, int q_dtype, void *out, int64_t out_batch_stride,
+                         int64_t out_head_stride, int out_dtype, float *lse, const int32_t *page_table,
+                         int64_t table_stride, int table_width, const int32_t *lengths, int batch, float scale,
+                         int window, gar_stream_t stream) {
+  if (plan == nullptr) return refuse("null plan");
+  if (int rc = check_cache(cache)) return rc;
+  if (cache->heads != plan->kv_heads || cache->dim != plan->dim) return refuse("the cache's heads or dim are not the plan's");
+  if (!float_type(q_dtype)) return refuse("q is GAR_F32, GAR_BF16 or GAR_F16");
+  if (float_type(cache->dtype) && cache->dtype != q_dtype) return refuse("a cache of float type goes with queries of its type");
+  if (out_dtype != q_dtype && out_dtype != GAR_F32) return refuse("out is of q's type or GAR_F32");
+  if (batch < 0 || table_width < 0 || window < 0) return refuse("negative batch, table_width or window");
+  if (!std::isfinite(scale)) return refuse("scale must be finite");
+  if (batch == 0) return GAR_OK;
+  if (q == nullptr || out == nullptr || lengths == nullptr || (page_table == nullptr && table_width > 0))
+    return refuse("null pointer");
+  if ((uintptr_t)q % element_size(q_dtype) || (uintptr_t)out % element_size(out_dtype) || (uintptr_t)lse % 4 ||
+      (uintptr_t)page_table % 4 || (uintptr_t)lengths % 4) {
+    set_error("a buffer is not aligned to its elements");
+    return GAR_EALIGN;
+  }
+  if (plan->ws == nullptr) {
+    set_error("gar_attn_plan_set_workspace has not been called");
+    return GAR_ENOWS;
+  }
+  int dev = -1;
+  const cudaError_t e = cudaGetDevice(&dev);
+  if (e != cudaSuccess) return cuda_fail(e, "cudaGetDevice");
+  if (dev != plan->device) {
+    set_error("the plan's workspace is on another device");
+    return GAR_ESTATE;
+  }
+  DecodeArgs a{};
+  a.c = *cache;
+  a.q = q, a.out = out, a.lse = lse;
+  a.qb = q_batch_stride, a.qh = q_head_stride, a.ob = out_batch_stride, a.oh = out_head_stride;
+  a.table = page_table, a.table_stride = table_stride, a.lengths = lengths;
+  a.page = divide_by((uint32_t)cache->page_size);
+  // Row numbers stay below 2^31 with room for a tile past the end.
+  a.most_rows = std::min<int64_t>((int64_t)table_width * cache->page_size, 0x7fffffff - 4096);
+  a.batch = batch, a.q_heads = plan->q_heads, a.group = plan->q_heads / plan->kv_heads;
+  a.q_dtype = q_dtype, a.out_dtype = out_dtype, a.window = window;
+  a.scale_log2 = (float)((double)scale * 1.4426950408889634);
+  char *ws = static_cast<char *>(plan->ws);
+  a.count = reinterpret_cast<unsigned *>(ws);
+  a.part_ml = reinterpret_cast<float *>(ws + kCounterBytes);
+  a.part_o = a.part_ml + (size_t)kMaxCtas * 2 * kMaxGroup * 2;
+  a.dim_pad = dim_pad(plan->dim);
+  return decode_general(a, plan->sms, (cudaStream_t)stream);
+}
+
+}  // extern "C"

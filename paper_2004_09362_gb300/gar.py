@@ -21,6 +21,11 @@ GAR_SUM, GAR_MAX, GAR_MIN = 0, 1, 2
 GAR_STEP_FAITHFUL, GAR_FUSED, GAR_STEP_PERSISTENT = 0, 1, 2
 GAR_STEPS_BO, GAR_STEPS_LO, GAR_STEPS_RING = -1, -2, -3
 GAR_GROUP_CYCLIC, GAR_GROUP_XOR = 0, 1
+GAR_F16, GAR_I8, GAR_E4M3 = 3, 4, 5          # decoding operators only
+GAR_ROPE_HALF, GAR_ROPE_INTERLEAVED = 0, 1
+GAR_ROPE_PLAIN, GAR_ROPE_LINEAR, GAR_ROPE_BASE, GAR_ROPE_PARTS = 0, 1, 2, 3
+GAR_KV_BAD_SLOT, GAR_KV_BAD_PAGE, GAR_KV_BAD_POSITION, GAR_KV_BAD_LENGTH = 1, 2, 4, 8
+GAR_MAX_HEAD_DIM = 256
 GAR_FORM_SINGLE, GAR_FORM_BREADTH, GAR_FORM_SPLIT = 0, 1, 2
 GROUPS = {"cyclic": GAR_GROUP_CYCLIC, "xor": GAR_GROUP_XOR}
 GAR_MAX_P = 1024
@@ -31,6 +36,9 @@ DTYPES = {"f32": GAR_F32, "bf16": GAR_BF16, "i32": GAR_I32}
 OPS = {"sum": GAR_SUM, "max": GAR_MAX, "min": GAR_MIN}
 MODES = {"step": GAR_STEP_FAITHFUL, "step_faithful": GAR_STEP_FAITHFUL, "fused": GAR_FUSED,
          "persistent": GAR_STEP_PERSISTENT}
+ROPE_LAYOUTS = {"half": GAR_ROPE_HALF, "interleaved": GAR_ROPE_INTERLEAVED}
+ROPE_SCALINGS = {"plain": GAR_ROPE_PLAIN, "linear": GAR_ROPE_LINEAR, "base": GAR_ROPE_BASE,
+                 "parts": GAR_ROPE_PARTS}
 ELEM_SIZE = {GAR_F32: 4, GAR_BF16: 2, GAR_I32: 4}
 
 # Every symbol include/gar.h declares (checked by the CPU tests).
@@ -41,7 +49,9 @@ EXPORTS = (
     "gar_allreduce_host", "gar_allreduce_batched", "gar_last_step_bytes", "gar_strerror",
     "gar_last_error", "gar_selftest_compile", "gar_allreduce_noalloc", "gar_plan_fused_source",
     "gar_cost_model", "gar_optimal_steps", "gar_plan_status", "gar_plan_debug_barrier",
-    "gar_plan_create_group",
+    "gar_plan_create_group", "gar_rope_frequencies", "gar_rope_table", "gar_rope", "gar_kv_write",
+    "gar_kv_read", "gar_kv_status", "gar_attn_plan_create", "gar_attn_plan_destroy",
+    "gar_attn_plan_bytes", "gar_attn_plan_set_workspace", "gar_decode_attention",
 )
 
 
@@ -60,11 +70,20 @@ class gar_plan_info(ctypes.Structure):
                 ("group", ctypes.c_int32), ("ring", ctypes.c_int32), ("fused_form", ctypes.c_int32)]
 
 
+class gar_kv_cache(ctypes.Structure):
+    _fields_ = ([(f, ctypes.c_void_p) for f in ("k", "v", "k_scale", "v_scale", "status")] +
+                [(f, ctypes.c_int64) for f in ("pages", "page_stride", "head_stride", "token_stride",
+                                               "scale_page_stride", "scale_head_stride",
+                                               "scale_token_stride")] +
+                [(f, ctypes.c_int32) for f in ("dtype", "heads", "dim", "page_size")])
+
+
 def _load():
     if not os.path.exists(_LIB_PATH):
         raise ImportError(f"libgar.so not built at {_LIB_PATH}; run __graft_entry__.build()")
     lib = ctypes.CDLL(_LIB_PATH)
     vp, i32, u64, sz = ctypes.c_void_p, ctypes.c_int, ctypes.c_uint64, ctypes.c_size_t
+    i64, f32, f64 = ctypes.c_int64, ctypes.c_float, ctypes.c_double
     P_ = ctypes.POINTER
     sig = {
         "gar_plan_create": (i32, [P_(vp), i32, u64, i32, i32, i32]),
@@ -94,6 +113,20 @@ def _load():
                                     ctypes.c_double, P_(i32)]),
         "gar_plan_status": (i32, [vp]),
         "gar_plan_debug_barrier": (i32, [vp, ctypes.c_uint, ctypes.c_uint]),
+        "gar_rope_frequencies": (i32, [i32, f64, i32, f64, f64, P_(f64), P_(f64)]),
+        "gar_rope_table": (i32, [vp, i64, i64, i32, P_(f64), f64, vp]),
+        "gar_rope": (i32, [vp, i64, i64, vp, i64, i64, i32, i64, i32, i32, i32, vp, i32, vp, i64, i32,
+                           i32, vp]),
+        "gar_kv_write": (i32, [P_(gar_kv_cache), vp, i64, i64, vp, i64, i64, i32, i64, vp, vp, i32, vp,
+                               i64, i32, i32, vp]),
+        "gar_kv_read": (i32, [P_(gar_kv_cache), vp, i64, vp, vp, i32, vp]),
+        "gar_kv_status": (i32, [P_(gar_kv_cache), P_(ctypes.c_uint32), vp]),
+        "gar_attn_plan_create": (i32, [P_(vp), i32, i32, i32]),
+        "gar_attn_plan_destroy": (None, [vp]),
+        "gar_attn_plan_bytes": (i32, [vp, P_(sz)]),
+        "gar_attn_plan_set_workspace": (i32, [vp, vp, sz]),
+        "gar_decode_attention": (i32, [vp, P_(gar_kv_cache), vp, i64, i64, i32, vp, i64, i64, i32, vp, vp,
+                                       i64, i32, vp, i32, f32, i32, vp]),
     }
     for name, (res, args) in sig.items():
         fn = getattr(lib, name)
@@ -258,10 +291,21 @@ def gar_plan_prepare(plan: Plan, mode="fused") -> None:
     _check(_lib.gar_plan_prepare(plan.handle, _code(mode, MODES, "mode")), "gar_plan_prepare")
 
 
+_current_raw_stream = None
+
+
 def _stream_handle(stream) -> ctypes.c_void_p:
+    """`stream` (None: torch's current one) as a handle.  The current stream's handle is asked
+    for without making a torch.cuda.Stream of it, which takes 3 us."""
+    global _current_raw_stream
     if stream is None:
-        import torch
-        stream = torch.cuda.current_stream()
+        if _current_raw_stream is None:
+            import torch
+            raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+            torch.cuda.current_stream()     # initialises CUDA
+            _current_raw_stream = ((lambda: raw(torch._C._cuda_getDevice())) if raw else
+                                   (lambda: torch.cuda.current_stream().cuda_stream))
+        return ctypes.c_void_p(_current_raw_stream() or None)
     if hasattr(stream, "cuda_stream"):
         stream = stream.cuda_stream
     return ctypes.c_void_p(int(stream) or None)
@@ -406,3 +450,299 @@ def gar_optimal_steps(P: int, m_bytes: float, alpha: float, beta: float, gamma: 
 
 def gar_selftest_compile() -> None:
     _check(_lib.gar_selftest_compile(), "gar_selftest_compile")
+
+
+# ---------------------------------------------------------------------------------------
+# Decoding operators: rotary positions, a paged (quantised) key-value cache, and attention of
+# one new token over it.  Tensors are CUDA tensors; head and token strides are free, the
+# channels of one head contiguous.
+# ---------------------------------------------------------------------------------------
+
+_TENSOR_DTYPES = None
+
+
+def _dtypes():
+    """GAR_* code of each torch dtype (torch is imported on first use)."""
+    global _TENSOR_DTYPES
+    if _TENSOR_DTYPES is None:
+        import torch
+        _TENSOR_DTYPES = {torch.float32: GAR_F32, torch.bfloat16: GAR_BF16, torch.float16: GAR_F16,
+                          torch.int8: GAR_I8, torch.float8_e4m3fn: GAR_E4M3}
+    return _TENSOR_DTYPES
+
+
+def _dtype_of(t, what: str) -> int:
+    code = _dtypes().get(t.dtype)
+    if code is None:
+        raise ValueError(f"{what}: dtype {t.dtype} is not supported")
+    return code
+
+
+def _rows(t, what: str):
+    """Checks [tokens, heads, dim] with contiguous channels; returns its shape and strides."""
+    if t.dim() != 3:
+        raise ValueError(f"{what} must be [tokens, heads, dim]")
+    shape, stride = t.shape, t.stride()
+    if stride[2] != 1 and shape[2] > 1:
+        raise ValueError(f"{what}: the channels of a head must be contiguous")
+    if not t.is_cuda:
+        raise ValueError(f"{what} must be a CUDA tensor")
+    return shape, stride
+
+
+def _integers(t, n: int, what: str, sizes=(4, 8)) -> int:
+    """Checks n contiguous integers on the GPU; returns their width in bytes."""
+    if t.dim() != 1 or t.shape[0] != n or not t.is_cuda or (n > 1 and t.stride(0) != 1):
+        raise ValueError(f"{what} must be {n} contiguous integers on the GPU")
+    size = t.element_size()
+    if size not in sizes or t.is_floating_point() or t.is_complex():
+        raise ValueError(f"{what}: dtype {t.dtype} is not supported")
+    return size
+
+
+def _check_table(table, dim: int):
+    shape = table.shape
+    if len(shape) != 3 or shape[2] != 2 or table.element_size() != 4 or not table.is_floating_point() \
+            or not table.is_cuda or not table.is_contiguous():
+        raise ValueError("the table must be a contiguous float32 CUDA tensor [positions, rot / 2, 2]")
+    if not 0 < 2 * shape[1] <= dim:
+        raise ValueError(f"the table rotates {2 * shape[1]} channels, the heads have {dim}")
+    return shape
+
+
+def _empty(shape, dtype, device, stream):
+    """An output that the call on `stream` (None, a torch stream or a raw handle) fills: allocated
+    under that stream, so that its memory is not given away while that stream uses it."""
+    import torch
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    if not hasattr(stream, "cuda_stream"):
+        stream = torch.cuda.ExternalStream(int(stream))
+    with torch.cuda.stream(stream):
+        return torch.empty(shape, dtype=dtype, device=device)
+
+
+def gar_rope_frequencies(rot: int, base: float = 10000.0, scaling="plain", factor: float = 1.0,
+                         original: float = 1.0):
+    """(rot/2 frequencies in radians per position, magnitude of the rotation)."""
+    f = (ctypes.c_double * max(1, min(int(rot), GAR_MAX_HEAD_DIM) // 2))()
+    m = ctypes.c_double()
+    _check(_lib.gar_rope_frequencies(int(rot), float(base), _code(scaling, ROPE_SCALINGS, "scaling"),
+                                     float(factor), float(original), f, ctypes.byref(m)),
+           "gar_rope_frequencies")
+    return list(f), m.value
+
+
+def gar_rope_table(count: int, frequencies, magnitude: float = 1.0, first: int = 0, stream=None):
+    """The [count, rot/2, 2] float32 table of magnitude * (cos, sin) at positions first, first + 1, ..."""
+    import torch
+    n = len(frequencies)
+    f = (ctypes.c_double * max(1, n))(*frequencies)
+    table = _empty((int(count), n, 2), torch.float32, "cuda", stream)
+    _check(_lib.gar_rope_table(table.data_ptr(), int(first), int(count), 2 * n, f, float(magnitude),
+                               _stream_handle(stream)), "gar_rope_table")
+    return table
+
+
+def gar_rope(x, positions, table, layout="half", inverse: bool = False, out=None, stream=None):
+    """x [tokens, heads, dim] with its first rot channels rotated by the table's rows at
+    `positions`; out may be x.  With inverse, the gradient: x is grad_out, the result grad_x."""
+    shape, xs = _rows(x, "x")
+    tshape = _check_table(table, shape[2])
+    width = _integers(positions, shape[0], "positions")
+    if out is None:
+        out = _empty(shape, x.dtype, x.device, stream)
+    elif out.dtype != x.dtype or out.shape != shape:
+        raise ValueError("out must have x's shape and dtype")
+    _, os_ = _rows(out, "out")
+    _check(_lib.gar_rope(x.data_ptr(), xs[0], xs[1], out.data_ptr(), os_[0], os_[1], _dtype_of(x, "x"),
+                         shape[0], shape[1], shape[2], 2 * tshape[1], positions.data_ptr(), width,
+                         table.data_ptr(), tshape[0], _code(layout, ROPE_LAYOUTS, "layout"),
+                         1 if inverse else 0, _stream_handle(stream)), "gar_rope")
+    return out
+
+
+class KVCache:
+    """A paged cache over the caller's tensors (which it keeps alive).
+
+    k, v: [pages, heads, page_size, dim] views with equal strides and contiguous channels, of
+    dtype float32, bfloat16, float16, int8 or float8_e4m3fn; permute a [pages, page_size,
+    heads, dim] tensor to get the view.  k_scale, v_scale: [pages, heads, page_size] float32
+    views with equal strides, for the 8-bit types."""
+
+    def __init__(self, k, v, k_scale=None, v_scale=None):
+        import torch
+        if k.dim() != 4 or k.shape != v.shape or k.dtype != v.dtype or k.stride() != v.stride():
+            raise ValueError("k and v must be [pages, heads, page_size, dim], alike in shape, dtype and strides")
+        pages, heads, page_size, dim = k.shape
+        if k.stride(3) != 1 and dim > 1:
+            raise ValueError("the channels of a head must be contiguous")
+        dtype = _dtype_of(k, "cache")
+        scaled = dtype in (GAR_I8, GAR_E4M3)
+        if scaled != (k_scale is not None) or scaled != (v_scale is not None):
+            raise ValueError("scales go with the 8-bit types, and only with them")
+        c = gar_kv_cache(k=k.data_ptr(), v=v.data_ptr(), pages=pages, page_stride=k.stride(0),
+                         head_stride=k.stride(1), token_stride=k.stride(2), dtype=dtype, heads=heads,
+                         dim=dim, page_size=page_size)
+        tensors = [k, v]
+        if scaled:
+            if (k_scale.shape != k.shape[:3] or v_scale.shape != k.shape[:3] or k_scale.stride() != v_scale.stride()
+                    or k_scale.dtype != torch.float32 or v_scale.dtype != torch.float32):
+                raise ValueError("scales must be float32 [pages, heads, page_size], alike in strides")
+            c.k_scale, c.v_scale = k_scale.data_ptr(), v_scale.data_ptr()
+            c.scale_page_stride, c.scale_head_stride, c.scale_token_stride = k_scale.stride()
+            tensors += [k_scale, v_scale]
+        if not all(t.is_cuda for t in tensors):
+            raise ValueError("a cache is of CUDA tensors")
+        self.status = torch.zeros(1, dtype=torch.int32, device=k.device)
+        c.status = self.status.data_ptr()
+        self.k, self.v, self.k_scale, self.v_scale = k, v, k_scale, v_scale
+        self.heads, self.dim, self.page_size, self.pages, self.dtype = heads, dim, page_size, pages, dtype
+        self._c = c
+        self._ref = ctypes.byref(c)
+
+
+def gar_kv_write(cache: KVCache, k, v, slots, positions=None, table=None, layout="half", stream=None) -> None:
+    """Writes k, v [tokens, heads, dim] to the cache's slots (int64; negative: skipped),
+    quantised where the cache is; with positions and table, the keys rotated first."""
+    shape, ks = _rows(k, "k")
+    vshape, vs = _rows(v, "v")
+    if shape != vshape or k.dtype != v.dtype or shape[1] != cache.heads or shape[2] != cache.dim:
+        raise ValueError("k and v must be [tokens, heads, dim] of the cache's heads and dim, alike in dtype")
+    _integers(slots, shape[0], "slots", (8,))
+    if (positions is None) != (table is None):
+        raise ValueError("positions and table go together")
+    pos, width, tab, trows, rot = None, 8, None, 0, 0
+    if positions is not None:
+        tshape = _check_table(table, shape[2])
+        width = _integers(positions, shape[0], "positions")
+        pos, tab, trows, rot = positions.data_ptr(), table.data_ptr(), tshape[0], 2 * tshape[1]
+    _check(_lib.gar_kv_write(cache._ref, k.data_ptr(), ks[0], ks[1], v.data_ptr(), vs[0], vs[1],
+                             _dtype_of(k, "k"), shape[0], slots.data_ptr(), pos, width, tab, trows, rot,
+                             _code(layout, ROPE_LAYOUTS, "layout"), _stream_handle(stream)), "gar_kv_write")
+
+
+def gar_kv_read(cache: KVCache, slots, dtype=None, out=None, stream=None):
+    """(k, v), each [tokens, heads, dim], of the cache's slots; rows of negative slots are 0.
+    dtype: "f32", "bf16" or "f16" (default: the cache's, bf16 for an 8-bit one); out: a pair of
+    contiguous tensors to fill instead."""
+    import torch
+    n = slots.shape[0] if slots.dim() == 1 else -1
+    _integers(slots, n, "slots", (8,))
+    if out is None:
+        kinds = {"f32": torch.float32, "bf16": torch.bfloat16, "f16": torch.float16}
+        if dtype is None:
+            kind = torch.bfloat16 if cache.dtype in (GAR_I8, GAR_E4M3) else cache.k.dtype
+        elif dtype in kinds:
+            kind = kinds[dtype]
+        else:
+            raise ValueError(f"unknown dtype {dtype!r}")
+        both = _empty((2, n, cache.heads, cache.dim), kind, slots.device, stream)
+        k, v = both[0], both[1]
+    else:
+        k, v = out
+        want = (n, cache.heads, cache.dim)
+        if tuple(k.shape) != want or tuple(v.shape) != want or k.dtype != v.dtype \
+                or not (k.is_cuda and v.is_cuda and k.is_contiguous() and v.is_contiguous()):
+            raise ValueError("out must be two contiguous CUDA tensors [tokens, heads, dim] of one dtype")
+    _check(_lib.gar_kv_read(cache._ref, slots.data_ptr(), n, k.data_ptr(), v.data_ptr(), _dtype_of(k, "out"),
+                            _stream_handle(stream)), "gar_kv_read")
+    return k, v
+
+
+def gar_kv_status(cache: KVCache, stream=None) -> None:
+    """Waits for the stream; raises GarError if a kernel met an index out of range since the last call."""
+    _check(_lib.gar_kv_status(cache._ref, None, _stream_handle(stream)), "gar_kv_status")
+
+
+class AttnPlan:
+    """Owns a gar_attn_plan* and the torch tensor that backs its workspace.  The workspace holds
+    one call's partial results: keep a plan's calls on one stream, or use a plan for each."""
+
+    def __init__(self, handle: int, q_heads: int, kv_heads: int, dim: int):
+        self._h = ctypes.c_void_p(handle)
+        self.q_heads, self.kv_heads, self.dim = q_heads, kv_heads, dim
+        self.default_scale = dim ** -0.5
+        self.workspace = None
+
+    @property
+    def handle(self) -> ctypes.c_void_p:
+        if not self._h:
+            raise ValueError("plan destroyed")
+        return self._h
+
+    def __del__(self):
+        try:
+            gar_attn_plan_destroy(self)
+        except Exception:
+            pass
+
+
+def gar_attn_plan_create(q_heads: int, kv_heads: int, dim: int) -> AttnPlan:
+    h = ctypes.c_void_p()
+    _check(_lib.gar_attn_plan_create(ctypes.byref(h), int(q_heads), int(kv_heads), int(dim)),
+           "gar_attn_plan_create")
+    return AttnPlan(h.value, int(q_heads), int(kv_heads), int(dim))
+
+
+def gar_attn_plan_destroy(plan: AttnPlan) -> None:
+    if plan._h:
+        _lib.gar_attn_plan_destroy(plan._h)
+        plan._h = ctypes.c_void_p(None)
+
+
+def gar_attn_plan_bytes(plan: AttnPlan) -> int:
+    n = ctypes.c_size_t()
+    _check(_lib.gar_attn_plan_bytes(plan.handle, ctypes.byref(n)), "gar_attn_plan_bytes")
+    return n.value
+
+
+def gar_attn_plan_set_workspace(plan: AttnPlan, ptr: int, nbytes: int) -> None:
+    _check(_lib.gar_attn_plan_set_workspace(plan.handle, ctypes.c_void_p(int(ptr) or None), int(nbytes)),
+           "gar_attn_plan_set_workspace")
+
+
+def gar_decode_attention(plan: AttnPlan, q, cache: KVCache, page_table, lengths, scale=None, window: int = 0,
+                         out=None, lse=None, stream=None):
+    """Attention of q [batch, q_heads, dim] over each sequence's cached rows.
+
+    page_table: int32 [batch, width]; lengths: int32 [batch], the new token's row included.
+    scale: dim**-0.5 by default.  window: only the last `window` rows (0: all).  out: q's shape, of
+    q's dtype or float32.  lse: True, or a contiguous float32 [batch, q_heads] tensor, returns
+    (out, log of the sum of weights); else returns out.  The plan's workspace is allocated on its
+    first call; make one before capturing calls into a CUDA graph."""
+    import torch
+    shape, qs = _rows(q, "q")
+    batch, q_heads, dim = shape
+    if q_heads != plan.q_heads or dim != plan.dim:
+        raise ValueError(f"q must be [batch, {plan.q_heads}, {plan.dim}]")
+    if lengths.dtype != torch.int32 or page_table.dtype != torch.int32:
+        raise ValueError("page_table and lengths must be int32")
+    _integers(lengths, batch, "lengths", (4,))
+    tshape, ts = page_table.shape, page_table.stride()
+    if len(tshape) != 2 or tshape[0] != batch or not page_table.is_cuda or (ts[1] != 1 and tshape[1] > 1):
+        raise ValueError(f"page_table must be [{batch}, width] on the GPU with contiguous rows")
+    handle = _stream_handle(stream)
+    if plan.workspace is None:
+        n = gar_attn_plan_bytes(plan)
+        plan.workspace = _empty((n,), torch.uint8, q.device, stream)
+        torch.cuda.synchronize()            # what held this memory before is done
+        gar_attn_plan_set_workspace(plan, plan.workspace.data_ptr(), n)
+    if out is None:
+        out = _empty(shape, q.dtype, q.device, stream)
+    if lse is True:
+        lse = _empty((batch, q_heads), torch.float32, q.device, stream)
+    if out.shape != shape:
+        raise ValueError("out must have q's shape")
+    lse_ptr = None
+    if lse is not None and lse is not False:
+        if lse.dtype != torch.float32 or lse.shape != shape[:2] or not lse.is_contiguous() or not lse.is_cuda:
+            raise ValueError("lse must be a contiguous float32 CUDA tensor [batch, q_heads]")
+        lse_ptr = lse.data_ptr()
+    _, os_ = _rows(out, "out")
+    _check(_lib.gar_decode_attention(plan._h, cache._ref, q.data_ptr(), qs[0], qs[1], _dtype_of(q, "q"),
+                                     out.data_ptr(), os_[0], os_[1], _dtype_of(out, "out"), lse_ptr,
+                                     page_table.data_ptr(), ts[0], tshape[1], lengths.data_ptr(), batch,
+                                     plan.default_scale if scale is None else float(scale), int(window), handle),
+           "gar_decode_attention")
+    return out if lse_ptr is None else (out, lse)
