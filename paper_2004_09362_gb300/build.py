@@ -24,8 +24,9 @@ OUT = os.path.join(PKG, "libgar.so")
 BUILD = os.path.join(ROOT, "_build")
 
 SOURCES = ["api.cpp", "plan.cpp", "codegen.cpp", "jit.cpp", "step_kernels.cu", "rope.cu", "cache.cu",
-           "decode_api.cu", "decode_general.cu"]
-HEADERS = ["gar_internal.hpp", "gar_device.cuh", "decode.cuh"]
+           "decode_api.cu", "decode_general.cu", "decode_mma_bf16.cu", "decode_mma_f16.cu", "decode_mma_i8.cu",
+           "decode_mma_e4m3.cu"]
+HEADERS = ["gar_internal.hpp", "gar_device.cuh", "decode.cuh", "decode_mma.cuh"]
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 
 

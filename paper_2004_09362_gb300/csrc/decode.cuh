@@ -248,5 +248,9 @@ __device__ __forceinline__ void finish(const DecodeArgs &a, const Walk &walk, co
 }
 
 int decode_general(const DecodeArgs &a, int sms, cudaStream_t stream);
+int decode_mma_bf16(const DecodeArgs &a, int sms, cudaStream_t stream);
+int decode_mma_f16(const DecodeArgs &a, int sms, cudaStream_t stream);
+int decode_mma_i8(const DecodeArgs &a, int sms, cudaStream_t stream);
+int decode_mma_e4m3(const DecodeArgs &a, int sms, cudaStream_t stream);
 
 }  // namespace gar

@@ -30,6 +30,13 @@ Divide divide_by(uint32_t d) {
   return {(uint32_t)(((1ull << 32) * ((1ull << shift) - d)) / d + 1), shift};
 }
 
+// The tensor-core kernels copy 16-byte chunks and take 16-bit queries.
+bool takes_mma(const gar_kv_cache &c, int q_dtype) {
+  const int64_t n = 16 / element_size(c.dtype);
+  return c.dtype != GAR_F32 && q_dtype != GAR_F32 && (uintptr_t)c.k % 16 == 0 && (uintptr_t)c.v % 16 == 0 &&
+         c.dim % n == 0 && c.page_stride % n == 0 && c.head_stride % n == 0 && c.token_stride % n == 0;
+}
+
 }  // namespace
 }  // namespace gar
 
@@ -130,7 +137,14 @@ int gar_decode_attention(gar_attn_plan *plan, const gar_kv_cache *cache, const v
   a.part_ml = reinterpret_cast<float *>(ws + kCounterBytes);
   a.part_o = a.part_ml + (size_t)kMaxCtas * 2 * kMaxGroup * 2;
   a.dim_pad = dim_pad(plan->dim);
-  return decode_general(a, plan->sms, (cudaStream_t)stream);
+  const cudaStream_t s = (cudaStream_t)stream;
+  if (!takes_mma(*cache, q_dtype)) return decode_general(a, plan->sms, s);
+  switch (cache->dtype) {
+    case GAR_BF16: return decode_mma_bf16(a, plan->sms, s);
+    case GAR_F16: return decode_mma_f16(a, plan->sms, s);
+    case GAR_I8: return decode_mma_i8(a, plan->sms, s);
+    default: return decode_mma_e4m3(a, plan->sms, s);
+  }
 }
 
 }  // extern "C"

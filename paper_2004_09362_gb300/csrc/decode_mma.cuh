@@ -1,0 +1,448 @@
+// Decode attention on tensor cores, for 16-bit queries over a 16- or 8-bit cache whose rows are
+// 16-byte aligned.
+//
+// Bound by memory: each cached row is read once for up to 8 NG query heads.  Per 16 rows of 128
+// channels the products take 40 (NG = 1) warp-wide m16n8k16 instructions, a small part of
+// the time those rows' 8 KB need from memory, so the plain warp-level instruction does and the
+// layouts are chosen to keep the rows out of everything but registers:
+//
+//  * Scores are computed transposed, S^T = K Q^T, rows of the cache as the 16-row operand and
+//    the (at most 8, else zero) query heads as the 8 columns.  Which channel sits at which place of the
+//    summed dimension is free as long as K and Q agree, so a lane's part of a K row is whole 16-byte chunks.
+//  * O^T = V^T P^T, channels as the 16 rows.  Which channel is which row is free too, so a lane's part of a
+//    V row is whole chunks as well; the pairs of neighbouring rows that the instruction wants are
+//    made with byte permutes.  P^T comes out of the scores' layout by one 8x8 transpose.
+//  * So every lane copies its own chunks to shared memory (cp.async, zeros for rows outside
+//    the segment) and reads back only those: no barrier, no bank conflicts, and a warp keeps
+//    kStages - 1 tiles in flight on its own.  Warps take every fourth tile of the CTA's segment and
+//    join at its end.
+//
+// 8-bit codes become f16, exactly; a row's key scale multiplies its scores, its value scale
+// its weight, taken relative to the largest value scale so far so that the weights stay in f16's
+// range.  Weights are split into a high and a low 16-bit part, one product each.
+#pragma once
+
+#include "decode.cuh"
+
+namespace gar {
+
+template <typename C> struct operand {  // the tensor cores' type
+  using type = __half;
+};
+template <> struct operand<__nv_bfloat16> {
+  using type = __nv_bfloat16;
+};
+
+template <typename T>
+__device__ __forceinline__ void mma(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0,
+                                    uint32_t b1);
+template <>
+__device__ __forceinline__ void mma<__half>(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3,
+                                            uint32_t b0, uint32_t b1) {
+  asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+      : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+      : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+template <>
+__device__ __forceinline__ void mma<__nv_bfloat16>(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3,
+                                                   uint32_t b0, uint32_t b1) {
+  asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+      : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+      : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+
+__device__ __forceinline__ uint32_t bits(__half2 x) { return *reinterpret_cast<uint32_t *>(&x); }
+__device__ __forceinline__ uint32_t bits(__nv_bfloat162 x) { return *reinterpret_cast<uint32_t *>(&x); }
+
+// Two weights as a high and a low part.
+template <typename T> __device__ __forceinline__ void split(float x, float y, uint32_t *hi, uint32_t *lo);
+template <> __device__ __forceinline__ void split<__half>(float x, float y, uint32_t *hi, uint32_t *lo) {
+  const __half2 h = __floats2half2_rn(x, y);
+  const float2 b = __half22float2(h);
+  *hi = bits(h), *lo = bits(__floats2half2_rn(x - b.x, y - b.y));
+}
+template <> __device__ __forceinline__ void split<__nv_bfloat16>(float x, float y, uint32_t *hi, uint32_t *lo) {
+  const __nv_bfloat162 h = __floats2bfloat162_rn(x, y);
+  const float2 b = __bfloat1622float2(h);
+  *hi = bits(h), *lo = bits(__floats2bfloat162_rn(x - b.x, y - b.y));
+}
+
+// Four 8-bit codes to two pairs of f16.
+template <typename C> __device__ __forceinline__ void expand(uint32_t x, uint32_t *a, uint32_t *b);
+template <> __device__ __forceinline__ void expand<e4m3>(uint32_t x, uint32_t *a, uint32_t *b) {
+  asm("{.reg .b16 l, h; mov.b32 {l, h}, %2; cvt.rn.f16x2.e4m3x2 %0, l; cvt.rn.f16x2.e4m3x2 %1, h;}"
+      : "=r"(*a), "=r"(*b)
+      : "r"(x));
+}
+template <> __device__ __forceinline__ void expand<i8>(uint32_t x, uint32_t *a, uint32_t *b) {
+  // 0x6400 + u is 1024 + u in f16: with u = x + 128, taking away 1152 leaves x exactly.
+  const uint32_t u = x ^ 0x80808080u;
+  const __half2 off = __floats2half2_rn(1152.f, 1152.f);
+  uint32_t p = __byte_perm(u, 0x64646464u, 0x4140), q = __byte_perm(u, 0x64646464u, 0x4342);
+  *a = bits(__hsub2(*reinterpret_cast<__half2 *>(&p), off));
+  *b = bits(__hsub2(*reinterpret_cast<__half2 *>(&q), off));
+}
+
+__device__ __forceinline__ uint32_t transpose8x8(uint32_t x) {
+  uint32_t y;
+  asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
+  return y;
+}
+
+template <int BYTES> __device__ __forceinline__ void copy_async(uint32_t to, const char *from, bool there) {
+  if (BYTES == 16)
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(to), "l"(from), "r"(there ? 16 : 0) : "memory");
+  else if (BYTES == 8)
+    asm volatile("cp.async.ca.shared.global [%0], [%1], 8, %2;" ::"r"(to), "l"(from), "r"(there ? 8 : 0) : "memory");
+  else
+    asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(to), "l"(from), "r"(there ? 4 : 0) : "memory");
+}
+
+template <int N> struct words;
+template <> struct words<16> {
+  using type = uint4;
+};
+template <> struct words<8> {
+  using type = uint2;
+};
+
+// DP: the head's channels rounded up to 64, 128 or 256; NG: groups of 8 query heads.
+template <typename C, int DP, int NG> struct MmaShape {
+  static constexpr int EL = sizeof(C);
+  static constexpr bool Q8 = quantised<C>::value;
+  static constexpr int KC = DP * EL / 64;                          // 16-byte chunks of a key row in a lane
+  static constexpr int VB = DP * EL / 8 < 16 ? DP * EL / 8 : 16;   // bytes of a value chunk
+  static constexpr int VC = DP * EL / 8 / VB;                      // value chunks of a row in a lane
+  static constexpr int KT = DP * EL <= 128 ? 32 : 16;              // rows of a tile
+  static constexpr int kStage = 2 * KT * DP * EL + (Q8 ? 2 * KT * 4 : 0);
+  static constexpr int kStages = kStage > 8192 + 256 ? 3 : kStage > 4096 + 256 ? 3 : 6;
+  static constexpr int kCtas = kStage > 8192 + 256 ? 1 : 2;        // per SM
+  static constexpr int kRow = DP + 4;                              // floats of an o row in shared memory
+  static constexpr int kJoin = kDecodeWarps * 8 * NG * kRow * 4;
+  static constexpr int kShared = kDecodeWarps * kStages * kStage > kJoin ? kDecodeWarps * kStages * kStage : kJoin;
+};
+
+template <typename C, int DP, int NG>
+__global__ void __launch_bounds__(kDecodeThreads, MmaShape<C, DP, NG>::kCtas) mma_kernel(const DecodeArgs a) {
+  using S = MmaShape<C, DP, NG>;
+  using T = typename operand<C>::type;
+  constexpr int EL = S::EL, KC = S::KC, VB = S::VB, VC = S::VC, KT = S::KT, SUBS = KT / 16;
+  constexpr bool Q8 = S::Q8;
+  constexpr int MT = DP / 16;  // tiles of 16 channels of the output
+  extern __shared__ __align__(16) char shared[];
+  __shared__ float ml[kDecodeWarps * kMaxGroup * 2];
+  const gar_kv_cache &c = a.c;
+  const int warp = threadIdx.x / 32, lane = threadIdx.x & 31, g = lane / 4, t = lane & 3;
+  char *const mine = shared + warp * (S::kStages * S::kStage);
+  const uint32_t mine_at = (uint32_t)__cvta_generic_to_shared(mine);
+  const int row_bytes = c.dim * EL;
+
+  Walk walk;
+  walk.start(a);
+  Segment seg;
+  while (walk.next(a, &seg)) {
+    const int lo = max(walk.s.lo, seg.from), to = seg.to;
+    const int32_t *table = a.table + seg.b * a.table_stride;
+    const char *kp = static_cast<const char *>(c.k) + seg.kv_head * c.head_stride * EL;
+    const char *vp = static_cast<const char *>(c.v) + seg.kv_head * c.head_stride * EL;
+
+    // Queries: head g (+ 8 ng), the channels of this lane's chunks.
+    uint32_t qf[NG][DP / 8];
+    float q_scale[NG][2];
+#pragma unroll
+    for (int ng = 0; ng < NG; ++ng) {
+      constexpr int CE = 16 / EL;  // channels of a chunk
+      float q[DP / 4], most = 0.f;
+      const bool there = g + 8 * ng < seg.heads;
+      const int64_t at = seg.b * a.qb + (seg.head + g + 8 * ng) * a.qh;
+#pragma unroll
+      for (int i = 0; i < DP / 4; ++i) {
+        const int d = (t + 4 * (i / CE)) * CE + i % CE;
+        q[i] = there && d < c.dim ? load_q(a, at + d) : 0.f;
+        most = fmaxf(most, fabsf(q[i]));
+      }
+      // bf16 queries become f16 relative to the power of two at their largest
+      float up = 1.f, down = 1.f;
+      if (Q8 && a.q_dtype == GAR_BF16) {
+        most = fmaxf(most, __shfl_xor_sync(~0u, most, 1));
+        most = fmaxf(most, __shfl_xor_sync(~0u, most, 2));
+        const int e = (__float_as_int(most) >> 23) & 0xff;
+        if (e > 0 && e < 0xfe) up = __int_as_float(e << 23), down = __int_as_float((254 - e) << 23);
+      }
+#pragma unroll
+      for (int i = 0; i < DP / 8; ++i) {
+        if constexpr (sizeof(C) == 2 && !std::is_same<T, __half>::value)
+          qf[ng][i] = bits(__floats2bfloat162_rn(q[2 * i], q[2 * i + 1]));
+        else
+          qf[ng][i] = bits(__floats2half2_rn(q[2 * i] * down, q[2 * i + 1] * down));
+      }
+      up *= a.scale_log2;
+      q_scale[ng][0] = __shfl_sync(~0u, up, 8 * t);      // lane 4 (2t) holds head 2t's
+      q_scale[ng][1] = __shfl_sync(~0u, up, 8 * t + 4);
+    }
+
+    float o[MT][NG][4] = {};
+    float m[NG][2], l[NG][2] = {};
+    float v_ref = 1e-30f;  // Q8: the value scale that o is relative to
+#pragma unroll
+    for (int ng = 0; ng < NG; ++ng) m[ng][0] = m[ng][1] = -INFINITY;
+
+    const int tiles = (to - seg.from + KT - 1) / KT;
+    // The page of this lane's row of a tile, fetched one tile before it is needed.
+    const auto page_of = [&](int tile) {
+      const int n = seg.from + tile * KT + (lane & (KT - 1));
+      return tile < tiles && n >= lo && n < to ? table[a.page(n)] : -1;
+    };
+    const auto issue = [&](int tile, int stage, int page) {
+      const int n = seg.from + tile * KT + (lane & (KT - 1));
+      int64_t at = -1, at_scale = 0;
+      if (n >= lo && n < to) {
+        const int r = n - (int)a.page(n) * c.page_size;
+        if ((unsigned)page < (uint64_t)c.pages) {
+          at = (page * c.page_stride + r * c.token_stride) * EL;
+          if (Q8) at_scale = page * c.scale_page_stride + r * c.scale_token_stride + seg.kv_head * c.scale_head_stride;
+        } else if (c.status) {
+          atomicOr(c.status, GAR_KV_BAD_PAGE);
+        }
+      }
+      uint32_t dst = mine_at + stage * S::kStage + lane * 16;
+#pragma unroll
+      for (int s = 0; s < SUBS; ++s)
+#pragma unroll
+        for (int r = 0; r < 2; ++r) {
+          const int64_t x = __shfl_sync(~0u, at, s * 16 + g + 8 * r);
+#pragma unroll
+          for (int k = 0; k < KC; ++k) {
+            const int off = (t + 4 * k) * 16;
+            const bool there = x >= 0 && off < row_bytes;
+            copy_async<16>(dst, there ? kp + x + off : kp, there);
+            dst += 512;
+          }
+        }
+      dst = mine_at + stage * S::kStage + KT * DP * EL + lane * VB;
+#pragma unroll
+      for (int s = 0; s < SUBS; ++s)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          const int64_t x = __shfl_sync(~0u, at, s * 16 + 2 * t + (r & 1) + 8 * (r / 2));
+#pragma unroll
+          for (int k = 0; k < VC; ++k) {
+            const int off = (g + 8 * k) * VB;
+            const bool there = x >= 0 && off < row_bytes;
+            copy_async<VB>(dst, there ? vp + x + off : vp, there);
+            dst += 32 * VB;
+          }
+        }
+      if (Q8 && lane < KT) {
+        const uint32_t to_scale = mine_at + stage * S::kStage + 2 * KT * DP * EL + lane * 4;
+        copy_async<4>(to_scale, reinterpret_cast<const char *>(c.k_scale + at_scale), at >= 0);
+        copy_async<4>(to_scale + KT * 4, reinterpret_cast<const char *>(c.v_scale + at_scale), at >= 0);
+      }
+    };
+
+    int page = page_of(warp);
+    int next = warp;
+#pragma unroll
+    for (int s = 0; s < S::kStages - 1; ++s) {
+      if (next < tiles) {
+        const int p = page;
+        page = page_of(next + kDecodeWarps);
+        issue(next, s, p);
+      }
+      asm volatile("cp.async.commit_group;" ::: "memory");
+      next += kDecodeWarps;
+    }
+    int stage = 0;
+    for (int tile = warp; tile < tiles; tile += kDecodeWarps) {
+      asm volatile("cp.async.wait_group %0;" ::"n"(S::kStages - 2) : "memory");
+      __syncwarp();
+      if (next < tiles) {
+        const int p = page;
+        page = page_of(next + kDecodeWarps);
+        issue(next, stage == 0 ? S::kStages - 1 : stage - 1, p);
+      }
+      asm volatile("cp.async.commit_group;" ::: "memory");
+      next += kDecodeWarps;
+      const char *at = mine + stage * S::kStage;
+      stage = stage == S::kStages - 1 ? 0 : stage + 1;
+      const float *k_scale = reinterpret_cast<const float *>(at + 2 * KT * DP * EL), *v_scale = k_scale + KT;
+
+      // Scores.
+      float s[SUBS][NG][4] = {};
+#pragma unroll
+      for (int sub = 0; sub < SUBS; ++sub)
+#pragma unroll
+        for (int k = 0; k < KC; ++k) {
+          const uint4 x = *reinterpret_cast<const uint4 *>(at + ((sub * 2 * KC + k) * 32 + lane) * 16);
+          const uint4 y = *reinterpret_cast<const uint4 *>(at + ((sub * 2 * KC + KC + k) * 32 + lane) * 16);
+          const uint32_t xs[4] = {x.x, x.y, x.z, x.w}, ys[4] = {y.x, y.y, y.z, y.w};
+          if constexpr (!Q8) {
+#pragma unroll
+            for (int i = 0; i < 4; i += 2)
+#pragma unroll
+              for (int ng = 0; ng < NG; ++ng)
+                mma<T>(s[sub][ng], xs[i], ys[i], xs[i + 1], ys[i + 1], qf[ng][k * 4 + i], qf[ng][k * 4 + i + 1]);
+          } else {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              uint32_t a0, a1, a2, a3;
+              expand<C>(xs[i], &a0, &a2);
+              expand<C>(ys[i], &a1, &a3);
+#pragma unroll
+              for (int ng = 0; ng < NG; ++ng)
+                mma<T>(s[sub][ng], a0, a1, a2, a3, qf[ng][k * 8 + 2 * i], qf[ng][k * 8 + 2 * i + 1]);
+            }
+          }
+        }
+      const int n0 = seg.from + tile * KT;
+      const bool ragged = n0 < lo || n0 + KT > to;
+      float top[NG][2];
+#pragma unroll
+      for (int ng = 0; ng < NG; ++ng) top[ng][0] = m[ng][0], top[ng][1] = m[ng][1];
+#pragma unroll
+      for (int sub = 0; sub < SUBS; ++sub)
+#pragma unroll
+        for (int r = 0; r < 2; ++r) {
+          const int n = n0 + sub * 16 + g + 8 * r;
+          const bool seen = !ragged || (n >= lo && n < to);
+          const float f = Q8 ? k_scale[sub * 16 + g + 8 * r] : 1.f;
+#pragma unroll
+          for (int ng = 0; ng < NG; ++ng)
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+              float &x = s[sub][ng][2 * r + h];
+              x = seen ? x * (Q8 ? f * q_scale[ng][h] : q_scale[ng][h]) : -INFINITY;
+              top[ng][h] = fmaxf(top[ng][h], x);
+            }
+        }
+      bool grown = false;
+#pragma unroll
+      for (int ng = 0; ng < NG; ++ng)
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+#pragma unroll
+          for (int d = 4; d < 32; d *= 2) top[ng][h] = fmaxf(top[ng][h], __shfl_xor_sync(~0u, top[ng][h], d));
+          grown |= top[ng][h] > m[ng][h];
+        }
+      float v_inverse = 1.f, v_shrink = 1.f;
+      if (Q8) {
+        const float most = __uint_as_float(__reduce_max_sync(~0u, __float_as_uint(v_scale[lane & (KT - 1)]) & 0x7fffffffu));
+        if (most > v_ref) v_shrink = v_ref / most, v_ref = most, grown = true;
+        v_inverse = 1.f / v_ref;
+      }
+      if (__any_sync(~0u, grown)) {
+#pragma unroll
+        for (int ng = 0; ng < NG; ++ng)
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+            const float f = exp2_fast(m[ng][h] - offset_of(top[ng][h]));
+            m[ng][h] = top[ng][h];
+            l[ng][h] *= f;
+#pragma unroll
+            for (int i = 0; i < MT; ++i) o[i][ng][h] *= f * v_shrink, o[i][ng][2 + h] *= f * v_shrink;
+          }
+      }
+      // Weights, in the layout of the second product's right operand.
+      uint32_t hi[SUBS][NG][2], low[SUBS][NG][2];
+#pragma unroll
+      for (int sub = 0; sub < SUBS; ++sub)
+#pragma unroll
+        for (int r = 0; r < 2; ++r) {
+          const float f = Q8 ? v_scale[sub * 16 + g + 8 * r] * v_inverse : 1.f;
+#pragma unroll
+          for (int ng = 0; ng < NG; ++ng) {
+            float p[2];
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+              p[h] = exp2_fast(s[sub][ng][2 * r + h] - offset_of(m[ng][h]));
+              l[ng][h] += p[h];
+              if (Q8) p[h] *= f;
+            }
+            split<T>(p[0], p[1], &hi[sub][ng][r], &low[sub][ng][r]);
+            hi[sub][ng][r] = transpose8x8(hi[sub][ng][r]);
+            low[sub][ng][r] = transpose8x8(low[sub][ng][r]);
+          }
+        }
+      // Values.
+      const char *const v_at = at + KT * DP * EL + lane * VB;
+#pragma unroll
+      for (int sub = 0; sub < SUBS; ++sub)
+#pragma unroll
+        for (int k = 0; k < VC; ++k) {
+          using W = typename words<VB>::type;
+          union {
+            W w;
+            uint32_t u[VB / 4];
+          } x[4];
+#pragma unroll
+          for (int r = 0; r < 4; ++r) x[r].w = *reinterpret_cast<const W *>(v_at + ((sub * 4 + r) * VC + k) * 32 * VB);
+#pragma unroll
+          for (int i = 0; i < VB / 4; ++i) {
+            if constexpr (!Q8) {
+              const uint32_t a0 = __byte_perm(x[0].u[i], x[1].u[i], 0x5410), a1 = __byte_perm(x[0].u[i], x[1].u[i], 0x7632);
+              const uint32_t a2 = __byte_perm(x[2].u[i], x[3].u[i], 0x5410), a3 = __byte_perm(x[2].u[i], x[3].u[i], 0x7632);
+#pragma unroll
+              for (int ng = 0; ng < NG; ++ng) {
+                mma<T>(o[k * 4 + i][ng], a0, a1, a2, a3, hi[sub][ng][0], hi[sub][ng][1]);
+                mma<T>(o[k * 4 + i][ng], a0, a1, a2, a3, low[sub][ng][0], low[sub][ng][1]);
+              }
+            } else {
+#pragma unroll
+              for (int j = 0; j < 2; ++j) {
+                uint32_t a0, a1, a2, a3;
+                expand<C>(__byte_perm(x[0].u[i], x[1].u[i], j ? 0x7362 : 0x5140), &a0, &a1);
+                expand<C>(__byte_perm(x[2].u[i], x[3].u[i], j ? 0x7362 : 0x5140), &a2, &a3);
+#pragma unroll
+                for (int ng = 0; ng < NG; ++ng) {
+                  float(&d)[4] = o[(k * (VB / 4) + i) * 2 + j][ng];
+                  mma<T>(d, a0, a1, a2, a3, hi[sub][ng][0], hi[sub][ng][1]);
+                  mma<T>(d, a0, a1, a2, a3, low[sub][ng][0], low[sub][ng][1]);
+                }
+              }
+            }
+          }
+        }
+    }
+    asm volatile("cp.async.wait_all;" ::: "memory");
+    __syncthreads();  // the tiles' memory becomes the join's
+    float *const o_shared = reinterpret_cast<float *>(shared);
+#pragma unroll
+    for (int ng = 0; ng < NG; ++ng)
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const int head = 8 * ng + 2 * t + h;
+#pragma unroll
+        for (int d = 4; d < 32; d *= 2) l[ng][h] += __shfl_xor_sync(~0u, l[ng][h], d);
+        if (g == 0) ml[(warp * kMaxGroup + head) * 2] = m[ng][h], ml[(warp * kMaxGroup + head) * 2 + 1] = l[ng][h];
+        float *const row = o_shared + (warp * 8 * NG + head) * S::kRow;
+#pragma unroll
+        for (int i = 0; i < MT; ++i) {
+          constexpr int CE = VB / EL;  // channels of a chunk, two of them in a tile of 16
+          const int k = i / (CE / 2), d = (g + 8 * k) * CE + i % (CE / 2) * 2;
+          *reinterpret_cast<float2 *>(row + d) =
+              Q8 ? make_float2(o[i][ng][h] * v_ref, o[i][ng][2 + h] * v_ref) : make_float2(o[i][ng][h], o[i][ng][2 + h]);
+        }
+      }
+    finish(a, walk, seg, ml, o_shared, 8 * NG, S::kRow);
+  }
+}
+
+template <typename C, int DP, int NG> int launch_mma(DecodeArgs a, int sms, cudaStream_t stream) {
+  using S = MmaShape<C, DP, NG>;
+  a.item_heads = std::min(a.group, 8 * NG);
+  a.item_groups = (a.group + 8 * NG - 1) / (8 * NG);
+  const cudaError_t e =
+      cudaFuncSetAttribute(mma_kernel<C, DP, NG>, cudaFuncAttributeMaxDynamicSharedMemorySize, S::kShared);
+  if (e != cudaSuccess) return cuda_fail(e, "cudaFuncSetAttribute");
+  mma_kernel<C, DP, NG><<<sms * S::kCtas, kDecodeThreads, S::kShared, stream>>>(a);
+  return launched("mma_kernel");
+}
+
+template <typename C> int decode_mma(const DecodeArgs &a, int sms, cudaStream_t stream) {
+  const bool two = a.group > 8;
+  if (a.c.dim <= 64) return two ? launch_mma<C, 64, 2>(a, sms, stream) : launch_mma<C, 64, 1>(a, sms, stream);
+  if (a.c.dim <= 128) return two ? launch_mma<C, 128, 2>(a, sms, stream) : launch_mma<C, 128, 1>(a, sms, stream);
+  return launch_mma<C, 256, 1>(a, sms, stream);
+}
+
+}  // namespace gar
