@@ -31,10 +31,10 @@ Divide divide_by(uint32_t d) {
 }
 
 // The tensor-core kernels copy 16-byte chunks and take 16-bit queries.
-bool takes_mma(const gar_kv_cache &c, int q_dtype) {
+bool takes_mma(const gar_kv_cache &c, const void *q, int64_t q_batch_stride, int64_t q_head_stride, int q_dtype) {
   const int64_t n = 16 / element_size(c.dtype);
-  return c.dtype != GAR_F32 && q_dtype != GAR_F32 && (uintptr_t)c.k % 16 == 0 && (uintptr_t)c.v % 16 == 0 &&
-         c.dim % n == 0 && c.page_stride % n == 0 && c.head_stride % n == 0 && c.token_stride % n == 0;
+  return c.dtype != GAR_F32 && q_dtype != GAR_F32 && (uintptr_t)q % 16 == 0 && q_batch_stride % 8 == 0 &&
+         q_head_stride % 8 == 0 && (uintptr_t)c.k % 16 == 0 && (uintptr_t)c.v % 16 == 0 && c.dim % n == 0 && c.page_stride % n == 0 && c.head_stride % n == 0 && c.token_stride % n == 0;
 }
 
 }  // namespace
@@ -128,17 +128,25 @@ int gar_decode_attention(gar_attn_plan *plan, const gar_kv_cache *cache, const v
   a.table = page_table, a.table_stride = table_stride, a.lengths = lengths;
   a.page = divide_by((uint32_t)cache->page_size);
   // Row numbers stay below 2^31 with room for a tile past the end.
-  a.most_rows = std::min<int64_t>((int64_t)table_width * cache->page_size, 0x7fffffff - 4096);
+  a.most_rows = (int)std::min<int64_t>((int64_t)table_width * cache->page_size, 0x7fffffff - 65536);
   a.batch = batch, a.q_heads = plan->q_heads, a.group = plan->q_heads / plan->kv_heads;
   a.q_dtype = q_dtype, a.out_dtype = out_dtype, a.window = window;
   a.scale_log2 = (float)((double)scale * 1.4426950408889634);
   char *ws = static_cast<char *>(plan->ws);
   a.count = reinterpret_cast<unsigned *>(ws);
-  a.part_ml = reinterpret_cast<float *>(ws + kCounterBytes);
-  a.part_o = a.part_ml + (size_t)kMaxCtas * 2 * kMaxGroup * 2;
+  a.part_ml = reinterpret_cast<float2 *>(ws + kCounterBytes);
+  a.part_o = reinterpret_cast<float *>(a.part_ml + (size_t)kMaxCtas * 2 * kMaxGroup);
   a.dim_pad = dim_pad(plan->dim);
+  a.out_wide = (uintptr_t)out % (4 * element_size(out_dtype)) == 0 && plan->dim % 4 == 0 && out_batch_stride % 4 == 0 &&
+               out_head_stride % 4 == 0;
+  // Units as large as it takes for the whole line to stay below 2^30 of them.
+  const int64_t items = (int64_t)batch * plan->kv_heads * ((a.group + 7) / 8);
+  if (items >= 1 << 28) return refuse("too many sequences and heads");
+  a.unit_shift = 6;
+  while (items * ((a.most_rows >> a.unit_shift) + 3) >= 1 << 30) ++a.unit_shift;
+  if (a.unit_shift > 15) return refuse("too many sequences and heads for tables this wide");
   const cudaStream_t s = (cudaStream_t)stream;
-  if (!takes_mma(*cache, q_dtype)) return decode_general(a, plan->sms, s);
+  if (!takes_mma(*cache, q, q_batch_stride, q_head_stride, q_dtype)) return decode_general(a, plan->sms, s);
   switch (cache->dtype) {
     case GAR_BF16: return decode_mma_bf16(a, plan->sms, s);
     case GAR_F16: return decode_mma_f16(a, plan->sms, s);

@@ -8,21 +8,23 @@ namespace {
 
 constexpr int kHeads = 8;   // query heads of an item
 constexpr int kRows = 4;    // rows a warp takes at once
+constexpr int kWarps = 4, kThreads = 32 * kWarps;
 
 // A warp takes kRows rows at a time; its lanes hold every 32nd channel (J each) of the rows, the
 // queries and the outputs.  The 4 x 8 products of rows and heads are summed over the lanes by an
 // exchange that halves the values with each step, so that 31 shuffles do them all and lane
 // 8 r + h is left with the score of row r and head h.  Bound by memory for a few heads a cached
 // head; the rows' loads (8 J of 128 bytes a warp) are in flight together.
-template <typename T, int J> __global__ void __launch_bounds__(kDecodeThreads) general_kernel(const DecodeArgs a) {
-  __shared__ float ml[kDecodeWarps * kMaxGroup * 2];
-  extern __shared__ float o_shared[];
+template <typename T, int J> __global__ void __launch_bounds__(kThreads) general_kernel(const DecodeArgs a) {
+  __shared__ JoinShared<kWarps> join;
+  extern __shared__ __align__(16) float o_shared[];
   const gar_kv_cache &c = a.c;
   const int warp = threadIdx.x / 32, lane = threadIdx.x & 31;
   const int row = lane / 8, head = lane & 7;
   const int o_row = J * 32;
   Walk walk;
-  walk.start(a);
+  walk.start<kThreads>(a);
+  if (lane == 0) join.at[warp] = warp * kHeads * o_row;
   Segment g;
   while (walk.next(a, &g)) {
     float q[kHeads][J], o[kHeads][J], m = -INFINITY, l = 0.f;
@@ -34,8 +36,8 @@ template <typename T, int J> __global__ void __launch_bounds__(kDecodeThreads) g
         q[h][j] = h < g.heads && d < c.dim ? load_q(a, g.b * a.qb + (g.head + h) * a.qh + d) : 0.f;
         o[h][j] = 0.f;
       }
-    const int lo = max(walk.s.lo, g.from);
-    for (int n0 = g.from + warp * kRows; n0 < g.to; n0 += kDecodeWarps * kRows) {
+    const int lo = g.lo;
+    for (int n0 = g.from + warp * kRows; n0 < g.to; n0 += kWarps * kRows) {
       // Lane r < kRows finds row r.
       const int n = n0 + (lane & (kRows - 1));
       int64_t at = -1, at_scale = 0;
@@ -108,20 +110,21 @@ template <typename T, int J> __global__ void __launch_bounds__(kDecodeThreads) g
     }
     l += __shfl_xor_sync(~0u, l, 8);
     l += __shfl_xor_sync(~0u, l, 16);
-    if (row == 0) ml[(warp * kMaxGroup + head) * 2] = m, ml[(warp * kMaxGroup + head) * 2 + 1] = l;
+    if (row == 0) join.ml[warp][head] = make_float2(m, l);
 #pragma unroll
     for (int h = 0; h < kHeads; ++h)
 #pragma unroll
       for (int j = 0; j < J; ++j) o_shared[(warp * kHeads + h) * o_row + lane + 32 * j] = o[h][j];
-    finish(a, walk, g, ml, o_shared, kHeads, o_row);
+    join_warps(a, g, join, o_shared, o_row, 0, kWarps, threadIdx.x, kThreads, [] { __syncthreads(); });
+    if (!g.whole) join_parts(a, g, join);
   }
 }
 
 template <typename T, int J> int launch(DecodeArgs a, int sms, cudaStream_t stream) {
-  const size_t shared = sizeof(float) * kDecodeWarps * kHeads * J * 32;
+  const size_t shared = sizeof(float) * kWarps * kHeads * J * 32;
   a.item_heads = std::min(a.group, kHeads);
   a.item_groups = (a.group + kHeads - 1) / kHeads;
-  general_kernel<T, J><<<sms * (J <= 4 ? 4 : 2), kDecodeThreads, shared, stream>>>(a);
+  general_kernel<T, J><<<sms * (J <= 4 ? 4 : 2), kThreads, shared, stream>>>(a);
   return launched("general_kernel");
 }
 

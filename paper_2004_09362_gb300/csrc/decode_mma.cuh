@@ -12,10 +12,12 @@
 //  * O^T = V^T P^T, channels as the 16 rows.  Which channel is which row is free too, so a lane's part of a
 //    V row is whole chunks as well; the pairs of neighbouring rows that the instruction wants are
 //    made with byte permutes.  P^T comes out of the scores' layout by one 8x8 transpose.
-//  * So every lane copies its own chunks to shared memory (cp.async, zeros for rows outside
-//    the segment) and reads back only those: no barrier, no bank conflicts, and a warp keeps
-//    kStages - 1 tiles in flight on its own.  Warps take every fourth tile of the CTA's segment and
-//    join at its end.
+//  * A warp copies its tiles to its own part of shared memory (cp.async, zeros for rows outside the
+//    segment), whole 128-byte lines an instruction, and is the only one to read them: it waits for
+//    its own copies, never for another warp.  It keeps kStages - 1 tiles in flight, and goes on to the
+//    next segment's while the CTA still joins the last one's results.
+//  * The warps of a CTA take a segment's tiles in turn and join at its end; an item of at most
+//    kSolo tiles goes to one warp whole, so that short sequences need no barrier at all.
 //
 // 8-bit codes become f16, exactly; a row's key scale multiplies its scores, its value scale
 // its weight, taken relative to the largest value scale so far so that the weights stay in f16's
@@ -106,6 +108,8 @@ template <> struct words<8> {
   using type = uint2;
 };
 
+constexpr int kSolo = 4;
+
 // DP: the head's channels rounded up to 64, 128 or 256; NG: groups of 8 query heads.
 template <typename C, int DP, int NG> struct MmaShape {
   static constexpr int EL = sizeof(C);
@@ -115,111 +119,101 @@ template <typename C, int DP, int NG> struct MmaShape {
   static constexpr int VC = DP * EL / 8 / VB;                      // value chunks of a row in a lane
   static constexpr int KT = DP * EL <= 128 ? 32 : 16;              // rows of a tile
   static constexpr int kStage = 2 * KT * DP * EL + (Q8 ? 2 * KT * 4 : 0);
-  static constexpr int kStages = kStage > 8192 + 256 ? 3 : kStage > 4096 + 256 ? 3 : 6;
-  static constexpr int kCtas = kStage > 8192 + 256 ? 1 : 2;        // per SM
-  static constexpr int kRow = DP + 4;                              // floats of an o row in shared memory
-  static constexpr int kJoin = kDecodeWarps * 8 * NG * kRow * 4;
-  static constexpr int kShared = kDecodeWarps * kStages * kStage > kJoin ? kDecodeWarps * kStages * kStage : kJoin;
+  static constexpr int kStages = kStage > 4096 + 256 ? 3 : 6;
+  static constexpr int kWarps = kStage > 8192 + 256 ? 4 : 8;       // one CTA per SM
+  // Floats of an o row; a row of o for each head fits a stage.  A few floats more than DP spread
+  // the rows over the banks.
+  static constexpr int kRow = 8 * NG * (DP + 4) * 4 <= kStage ? DP + 4 : DP;
+  static_assert(8 * NG * kRow * 4 <= kStage, "o must fit a stage");
+  static constexpr int kShared = kWarps * kStages * kStage;
+};
+
+// One warp's way through its CTA's segments, tile by tile.
+template <typename S> struct Tiles {
+  Walk walk;
+  Segment seg;
+  int ordinal, tile, step, tiles;
+  bool alone, mine;  // alone: the segment is one warp's; mine: this warp has to do with it
+
+  __device__ __forceinline__ bool next(const DecodeArgs &a, int warp) {
+    if (!walk.next(a, &seg)) return false;
+    tiles = (max(0, seg.to - seg.from) + S::KT - 1) / S::KT;
+    alone = seg.whole && tiles <= kSolo;
+    mine = !alone || ordinal % S::kWarps == warp;
+    if (!mine) tiles = 0;
+    tile = alone ? 0 : warp, step = alone ? 1 : S::kWarps;
+    ++ordinal;
+    return true;
+  }
 };
 
 template <typename C, int DP, int NG>
-__global__ void __launch_bounds__(kDecodeThreads, MmaShape<C, DP, NG>::kCtas) mma_kernel(const DecodeArgs a) {
+__global__ void __launch_bounds__(32 * MmaShape<C, DP, NG>::kWarps, 1) mma_kernel(const DecodeArgs a) {
   using S = MmaShape<C, DP, NG>;
   using T = typename operand<C>::type;
-  constexpr int EL = S::EL, KC = S::KC, VB = S::VB, VC = S::VC, KT = S::KT, SUBS = KT / 16;
+  constexpr int EL = S::EL, KC = S::KC, VB = S::VB, VC = S::VC, KT = S::KT, SUBS = KT / 16, W = S::kWarps;
   constexpr bool Q8 = S::Q8;
-  constexpr int MT = DP / 16;  // tiles of 16 channels of the output
+  constexpr int MT = DP / 16;          // tiles of 16 channels of the output
+  constexpr int LINE = DP * EL < 128 ? DP * EL : 128;   // bytes of a row copied by neighbouring lanes
+  constexpr int LANES = LINE / 16, PARTS = DP * EL / LINE;
   extern __shared__ __align__(16) char shared[];
-  __shared__ float ml[kDecodeWarps * kMaxGroup * 2];
+  __shared__ JoinShared<W> join;
   const gar_kv_cache &c = a.c;
   const int warp = threadIdx.x / 32, lane = threadIdx.x & 31, g = lane / 4, t = lane & 3;
   char *const mine = shared + warp * (S::kStages * S::kStage);
   const uint32_t mine_at = (uint32_t)__cvta_generic_to_shared(mine);
   const int row_bytes = c.dim * EL;
 
-  Walk walk;
-  walk.start(a);
-  Segment seg;
-  while (walk.next(a, &seg)) {
-    const int lo = max(walk.s.lo, seg.from), to = seg.to;
-    const int32_t *table = a.table + seg.b * a.table_stride;
-    const char *kp = static_cast<const char *>(c.k) + seg.kv_head * c.head_stride * EL;
-    const char *vp = static_cast<const char *>(c.v) + seg.kv_head * c.head_stride * EL;
+  Tiles<S> get;   // copies, kStages - 1 tiles ahead of
+  get.walk.template start<32 * W>(a);
+  get.ordinal = get.tile = get.tiles = 0;
+  Tiles<S> use = get;
+  bool more = get.next(a, warp);
+  int page = -1;  // of this lane's row of get's tile, fetched one tile before it is needed
 
-    // Queries: head g (+ 8 ng), the channels of this lane's chunks.
-    uint32_t qf[NG][DP / 8];
-    float q_scale[NG][2];
-#pragma unroll
-    for (int ng = 0; ng < NG; ++ng) {
-      constexpr int CE = 16 / EL;  // channels of a chunk
-      float q[DP / 4], most = 0.f;
-      const bool there = g + 8 * ng < seg.heads;
-      const int64_t at = seg.b * a.qb + (seg.head + g + 8 * ng) * a.qh;
-#pragma unroll
-      for (int i = 0; i < DP / 4; ++i) {
-        const int d = (t + 4 * (i / CE)) * CE + i % CE;
-        q[i] = there && d < c.dim ? load_q(a, at + d) : 0.f;
-        most = fmaxf(most, fabsf(q[i]));
-      }
-      // bf16 queries become f16 relative to the power of two at their largest
-      float up = 1.f, down = 1.f;
-      if (Q8 && a.q_dtype == GAR_BF16) {
-        most = fmaxf(most, __shfl_xor_sync(~0u, most, 1));
-        most = fmaxf(most, __shfl_xor_sync(~0u, most, 2));
-        const int e = (__float_as_int(most) >> 23) & 0xff;
-        if (e > 0 && e < 0xfe) up = __int_as_float(e << 23), down = __int_as_float((254 - e) << 23);
-      }
-#pragma unroll
-      for (int i = 0; i < DP / 8; ++i) {
-        if constexpr (sizeof(C) == 2 && !std::is_same<T, __half>::value)
-          qf[ng][i] = bits(__floats2bfloat162_rn(q[2 * i], q[2 * i + 1]));
-        else
-          qf[ng][i] = bits(__floats2half2_rn(q[2 * i] * down, q[2 * i + 1] * down));
-      }
-      up *= a.scale_log2;
-      q_scale[ng][0] = __shfl_sync(~0u, up, 8 * t);      // lane 4 (2t) holds head 2t's
-      q_scale[ng][1] = __shfl_sync(~0u, up, 8 * t + 4);
+  const auto fetch_page = [&] {
+    while (more && get.tile >= get.tiles) more = get.next(a, warp);
+    page = -1;
+    if (more) {
+      const int n = get.seg.from + get.tile * KT + (lane & (KT - 1));
+      if (n >= get.seg.lo && n < get.seg.to) page = a.table[get.seg.b * a.table_stride + a.page(n)];
     }
-
-    float o[MT][NG][4] = {};
-    float m[NG][2], l[NG][2] = {};
-    float v_ref = 1e-30f;  // Q8: the value scale that o is relative to
-#pragma unroll
-    for (int ng = 0; ng < NG; ++ng) m[ng][0] = m[ng][1] = -INFINITY;
-
-    const int tiles = (to - seg.from + KT - 1) / KT;
-    // The page of this lane's row of a tile, fetched one tile before it is needed.
-    const auto page_of = [&](int tile) {
-      const int n = seg.from + tile * KT + (lane & (KT - 1));
-      return tile < tiles && n >= lo && n < to ? table[a.page(n)] : -1;
-    };
-    const auto issue = [&](int tile, int stage, int page) {
-      const int n = seg.from + tile * KT + (lane & (KT - 1));
-      int64_t at = -1, at_scale = 0;
-      if (n >= lo && n < to) {
+  };
+  const auto issue = [&](int stage) {
+    if (more) {
+      const int n = get.seg.from + get.tile * KT + (lane & (KT - 1));
+      int64_t at = -1, at_scale = 0;  // bytes; elements
+      if (n >= get.seg.lo && n < get.seg.to) {
         const int r = n - (int)a.page(n) * c.page_size;
         if ((unsigned)page < (uint64_t)c.pages) {
-          at = (page * c.page_stride + r * c.token_stride) * EL;
-          if (Q8) at_scale = page * c.scale_page_stride + r * c.scale_token_stride + seg.kv_head * c.scale_head_stride;
+          at = (page * c.page_stride + get.seg.kv_head * c.head_stride + r * c.token_stride) * EL;
+          if (Q8) at_scale = page * c.scale_page_stride + r * c.scale_token_stride + get.seg.kv_head * c.scale_head_stride;
         } else if (c.status) {
           atomicOr(c.status, GAR_KV_BAD_PAGE);
         }
       }
-      uint32_t dst = mine_at + stage * S::kStage + lane * 16;
+      get.tile += get.step;
+      fetch_page();
+      const char *const kp = static_cast<const char *>(c.k), *const vp = static_cast<const char *>(c.v);
+      // Keys: LANES lanes a line.  Odd rows swap the halves of a 128-byte line, so that
+      // the 8 lanes that read 4 chunks of two rows at once meet 32 different banks.
+      {
+        constexpr int ROWS = 32 / LANES;
+        const int chunk = lane & (LANES - 1), row = lane / LANES;
 #pragma unroll
-      for (int s = 0; s < SUBS; ++s)
+        for (int r = 0; r < KT; r += ROWS) {
+          const int64_t x = __shfl_sync(~0u, at, r + row);
 #pragma unroll
-        for (int r = 0; r < 2; ++r) {
-          const int64_t x = __shfl_sync(~0u, at, s * 16 + g + 8 * r);
-#pragma unroll
-          for (int k = 0; k < KC; ++k) {
-            const int off = (t + 4 * k) * 16;
+          for (int p = 0; p < PARTS; ++p) {
+            const int off = p * LINE + chunk * 16;
             const bool there = x >= 0 && off < row_bytes;
-            copy_async<16>(dst, there ? kp + x + off : kp, there);
-            dst += 512;
+            copy_async<16>(mine_at + stage * S::kStage + (p * KT + r + row) * LINE +
+                               (LANES == 8 ? chunk ^ ((row & 1) << 2) : chunk) * 16,
+                           there ? kp + x + off : kp, there);
           }
         }
-      dst = mine_at + stage * S::kStage + KT * DP * EL + lane * VB;
+      }
+      uint32_t dst = mine_at + stage * S::kStage + KT * DP * EL + lane * VB;
 #pragma unroll
       for (int s = 0; s < SUBS; ++s)
 #pragma unroll
@@ -238,31 +232,63 @@ __global__ void __launch_bounds__(kDecodeThreads, MmaShape<C, DP, NG>::kCtas) mm
         copy_async<4>(to_scale, reinterpret_cast<const char *>(c.k_scale + at_scale), at >= 0);
         copy_async<4>(to_scale + KT * 4, reinterpret_cast<const char *>(c.v_scale + at_scale), at >= 0);
       }
-    };
-
-    int page = page_of(warp);
-    int next = warp;
-#pragma unroll
-    for (int s = 0; s < S::kStages - 1; ++s) {
-      if (next < tiles) {
-        const int p = page;
-        page = page_of(next + kDecodeWarps);
-        issue(next, s, p);
-      }
-      asm volatile("cp.async.commit_group;" ::: "memory");
-      next += kDecodeWarps;
     }
-    int stage = 0;
-    for (int tile = warp; tile < tiles; tile += kDecodeWarps) {
+    asm volatile("cp.async.commit_group;" ::: "memory");
+  };
+
+  fetch_page();
+#pragma unroll
+  for (int s = 0; s < S::kStages - 1; ++s) issue(s);
+  int stage = 0;  // the next tile's; the one before it is free
+
+  while (use.next(a, warp)) {
+    if (!use.mine) continue;
+    const Segment &seg = use.seg;
+    // Queries: head g (+ 8 ng), the channels of this lane's chunks, two to a register.
+    uint32_t qf[NG][DP / 8];
+    float q_scale[NG][2];
+#pragma unroll
+    for (int ng = 0; ng < NG; ++ng) {
+      const bool there = g + 8 * ng < seg.heads;
+      const uint4 *q = reinterpret_cast<const uint4 *>(static_cast<const char *>(a.q) +
+                                                      2 * (seg.b * a.qb + (seg.head + g + 8 * ng) * a.qh));
+#pragma unroll
+      for (int k = 0; k < DP / 32; ++k) {
+        const int at = Q8 ? (t + 4 * (k / 2)) * 2 + k % 2 : t + 4 * k;  // 8 channels each
+        const uint4 x = there && at * 8 < c.dim ? q[at] : make_uint4(0, 0, 0, 0);
+        qf[ng][4 * k] = x.x, qf[ng][4 * k + 1] = x.y, qf[ng][4 * k + 2] = x.z, qf[ng][4 * k + 3] = x.w;
+      }
+      // bf16 queries become f16 relative to the power of two at their largest
+      float up = 1.f;
+      if (Q8 && a.q_dtype == GAR_BF16) {
+        uint32_t most = 0;
+#pragma unroll
+        for (int i = 0; i < DP / 8; ++i) most = max(most, max(qf[ng][i] & 0x7fffu, (qf[ng][i] >> 16) & 0x7fffu));
+        most = max(most, __shfl_xor_sync(~0u, most, 1));
+        most = max(most, __shfl_xor_sync(~0u, most, 2));
+        const int e = most >> 7;
+        float down = 1.f;
+        if (e > 0 && e < 0xfe) up = __int_as_float(e << 23), down = __int_as_float((254 - e) << 23);
+#pragma unroll
+        for (int i = 0; i < DP / 8; ++i)
+          qf[ng][i] = bits(__floats2half2_rn(__uint_as_float(qf[ng][i] << 16) * down,
+                                             __uint_as_float(qf[ng][i] & 0xffff0000u) * down));
+      }
+      up *= a.scale_log2;
+      q_scale[ng][0] = __shfl_sync(~0u, up, 8 * t);      // lane 4 (2t) holds head 2t's
+      q_scale[ng][1] = __shfl_sync(~0u, up, 8 * t + 4);
+    }
+
+    float o[MT][NG][4] = {};
+    float m[NG][2], l[NG][2] = {};
+    float v_ref = 1e-30f;  // Q8: the value scale that o is relative to
+#pragma unroll
+    for (int ng = 0; ng < NG; ++ng) m[ng][0] = m[ng][1] = -INFINITY;
+
+    for (; use.tile < use.tiles; use.tile += use.step) {
       asm volatile("cp.async.wait_group %0;" ::"n"(S::kStages - 2) : "memory");
       __syncwarp();
-      if (next < tiles) {
-        const int p = page;
-        page = page_of(next + kDecodeWarps);
-        issue(next, stage == 0 ? S::kStages - 1 : stage - 1, p);
-      }
-      asm volatile("cp.async.commit_group;" ::: "memory");
-      next += kDecodeWarps;
+      issue(stage == 0 ? S::kStages - 1 : stage - 1);
       const char *at = mine + stage * S::kStage;
       stage = stage == S::kStages - 1 ? 0 : stage + 1;
       const float *k_scale = reinterpret_cast<const float *>(at + 2 * KT * DP * EL), *v_scale = k_scale + KT;
@@ -273,8 +299,9 @@ __global__ void __launch_bounds__(kDecodeThreads, MmaShape<C, DP, NG>::kCtas) mm
       for (int sub = 0; sub < SUBS; ++sub)
 #pragma unroll
         for (int k = 0; k < KC; ++k) {
-          const uint4 x = *reinterpret_cast<const uint4 *>(at + ((sub * 2 * KC + k) * 32 + lane) * 16);
-          const uint4 y = *reinterpret_cast<const uint4 *>(at + ((sub * 2 * KC + KC + k) * 32 + lane) * 16);
+          const int part = k * 64 / LINE, chunk = (t + 4 * k) % LANES;
+          const char *const x_at = at + (part * KT + sub * 16 + g) * LINE + (LANES == 8 ? chunk ^ ((g & 1) << 2) : chunk) * 16;
+          const uint4 x = *reinterpret_cast<const uint4 *>(x_at), y = *reinterpret_cast<const uint4 *>(x_at + 8 * LINE);
           const uint32_t xs[4] = {x.x, x.y, x.z, x.w}, ys[4] = {y.x, y.y, y.z, y.w};
           if constexpr (!Q8) {
 #pragma unroll
@@ -294,8 +321,8 @@ __global__ void __launch_bounds__(kDecodeThreads, MmaShape<C, DP, NG>::kCtas) mm
             }
           }
         }
-      const int n0 = seg.from + tile * KT;
-      const bool ragged = n0 < lo || n0 + KT > to;
+      const int n0 = seg.from + use.tile * KT;
+      const bool ragged = n0 < seg.lo || n0 + KT > seg.to;
       float top[NG][2];
 #pragma unroll
       for (int ng = 0; ng < NG; ++ng) top[ng][0] = m[ng][0], top[ng][1] = m[ng][1];
@@ -304,7 +331,7 @@ __global__ void __launch_bounds__(kDecodeThreads, MmaShape<C, DP, NG>::kCtas) mm
 #pragma unroll
         for (int r = 0; r < 2; ++r) {
           const int n = n0 + sub * 16 + g + 8 * r;
-          const bool seen = !ragged || (n >= lo && n < to);
+          const bool seen = !ragged || (n >= seg.lo && n < seg.to);
           const float f = Q8 ? k_scale[sub * 16 + g + 8 * r] : 1.f;
 #pragma unroll
           for (int ng = 0; ng < NG; ++ng)
@@ -403,9 +430,9 @@ __global__ void __launch_bounds__(kDecodeThreads, MmaShape<C, DP, NG>::kCtas) mm
           }
         }
     }
-    asm volatile("cp.async.wait_all;" ::: "memory");
-    __syncthreads();  // the tiles' memory becomes the join's
-    float *const o_shared = reinterpret_cast<float *>(shared);
+    // The stage read last holds this warp's o until it is joined.
+    float *const o_mine = reinterpret_cast<float *>(mine + (stage == 0 ? S::kStages - 1 : stage - 1) * S::kStage);
+    __syncwarp();
 #pragma unroll
     for (int ng = 0; ng < NG; ++ng)
 #pragma unroll
@@ -413,8 +440,8 @@ __global__ void __launch_bounds__(kDecodeThreads, MmaShape<C, DP, NG>::kCtas) mm
         const int head = 8 * ng + 2 * t + h;
 #pragma unroll
         for (int d = 4; d < 32; d *= 2) l[ng][h] += __shfl_xor_sync(~0u, l[ng][h], d);
-        if (g == 0) ml[(warp * kMaxGroup + head) * 2] = m[ng][h], ml[(warp * kMaxGroup + head) * 2 + 1] = l[ng][h];
-        float *const row = o_shared + (warp * 8 * NG + head) * S::kRow;
+        if (g == 0) join.ml[warp][head] = make_float2(m[ng][h], l[ng][h]);
+        float *const row = o_mine + head * S::kRow;
 #pragma unroll
         for (int i = 0; i < MT; ++i) {
           constexpr int CE = VB / EL;  // channels of a chunk, two of them in a tile of 16
@@ -423,8 +450,16 @@ __global__ void __launch_bounds__(kDecodeThreads, MmaShape<C, DP, NG>::kCtas) mm
               Q8 ? make_float2(o[i][ng][h] * v_ref, o[i][ng][2 + h] * v_ref) : make_float2(o[i][ng][h], o[i][ng][2 + h]);
         }
       }
-    finish(a, walk, seg, ml, o_shared, 8 * NG, S::kRow);
+    const float *const o_all = reinterpret_cast<const float *>(shared);
+    if (lane == 0) join.at[warp] = (int)(o_mine - o_all);
+    if (use.alone) {
+      join_warps(a, seg, join, o_all, S::kRow, warp, 1, lane, 32, [] { __syncwarp(); });
+    } else {
+      join_warps(a, seg, join, o_all, S::kRow, 0, W, threadIdx.x, 32 * W, [] { __syncthreads(); });
+      if (!seg.whole) join_parts(a, seg, join);
+    }
   }
+  asm volatile("cp.async.wait_all;" ::: "memory");
 }
 
 template <typename C, int DP, int NG> int launch_mma(DecodeArgs a, int sms, cudaStream_t stream) {
@@ -434,7 +469,7 @@ template <typename C, int DP, int NG> int launch_mma(DecodeArgs a, int sms, cuda
   const cudaError_t e =
       cudaFuncSetAttribute(mma_kernel<C, DP, NG>, cudaFuncAttributeMaxDynamicSharedMemorySize, S::kShared);
   if (e != cudaSuccess) return cuda_fail(e, "cudaFuncSetAttribute");
-  mma_kernel<C, DP, NG><<<sms * S::kCtas, kDecodeThreads, S::kShared, stream>>>(a);
+  mma_kernel<C, DP, NG><<<sms, 32 * S::kWarps, S::kShared, stream>>>(a);
   return launched("mma_kernel");
 }
 
