@@ -439,7 +439,13 @@ typedef struct {
 } gar_kv_cache;
 
 /* Bits of the status word. */
-enum { GAR_KV_BAD_SLOT = 1, GAR_KV_BAD_PAGE = 2, GAR_KV_BAD_POSITION = 4, GAR_KV_BAD_LENGTH = 8 };
+enum {
+  GAR_KV_BAD_SLOT = 1,
+  GAR_KV_BAD_PAGE = 2,
+  GAR_KV_BAD_POSITION = 4,
+  GAR_KV_BAD_LENGTH = 8,
+  GAR_KV_TIMEOUT = 16 /* a bounded wait for a copy gave up: the outputs are not valid */
+};
 
 /* Writes the keys and values of `tokens` tokens ([tokens][heads][dim] of dtype GAR_F32,
  * GAR_BF16 or GAR_F16; a cache of float type takes its own type) to the cache slots
@@ -460,8 +466,8 @@ GAR_API int gar_kv_read(const gar_kv_cache *cache, const int64_t *slots, int64_t
                         void *v, int dtype, gar_stream_t stream);
 
 /* Waits for `stream`, then returns GAR_OK if no kernel has set the cache's status word
- * since it was last cleared; else clears it and returns GAR_EINVAL with the bits in *bits
- * (may be NULL) and their meaning in gar_last_error(). */
+ * since it was last cleared; else clears it and returns GAR_EINVAL (GAR_ETIMEOUT for
+ * GAR_KV_TIMEOUT) with the bits in *bits (may be NULL) and their meaning in gar_last_error(). */
 GAR_API int gar_kv_status(const gar_kv_cache *cache, uint32_t *bits, gar_stream_t stream);
 
 typedef struct gar_attn_plan gar_attn_plan;

@@ -309,7 +309,9 @@ int gar_kv_status(const gar_kv_cache *cache, uint32_t *bits, gar_stream_t stream
   if (got & GAR_KV_BAD_PAGE) why += " a page number outside the cache;";
   if (got & GAR_KV_BAD_POSITION) why += " a position outside the table;";
   if (got & GAR_KV_BAD_LENGTH) why += " a length that its pages cannot hold;";
-  return refuse(why);
+  if (got & GAR_KV_TIMEOUT) why += " a copy that did not end;";
+  set_error(why);
+  return got & GAR_KV_TIMEOUT ? GAR_ETIMEOUT : GAR_EINVAL;
 }
 
 }  // extern "C"

@@ -40,6 +40,7 @@ struct DecodeArgs {
   Divide page;
   int most_rows;           // rows that the table's width can hold
   int unit_shift;          // rows of a unit: 1 << unit_shift
+  int box_rows;            // rows of a tensor copy
   int batch, q_heads, group, item_groups, item_heads;  // group: q_heads / kv_heads
   int q_dtype, out_dtype, window;
   bool out_wide;           // four neighbouring outputs can be stored at once

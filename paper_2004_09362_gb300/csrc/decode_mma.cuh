@@ -12,10 +12,15 @@
 //  * O^T = V^T P^T, channels as the 16 rows.  Which channel is which row is free too, so a lane's part of a
 //    V row is whole chunks as well; the pairs of neighbouring rows that the instruction wants are
 //    made with byte permutes.  P^T comes out of the scores' layout by one 8x8 transpose.
-//  * A warp copies its tiles to its own part of shared memory (cp.async, zeros for rows outside the
-//    segment), whole 128-byte lines an instruction, and is the only one to read them: it waits for
-//    its own copies, never for another warp.  It keeps kStages - 1 tiles in flight, and goes on to the
-//    next segment's while the CTA still joins the last one's results.
+//  * Which row of the cache is which row of S^T is free as well, within 8 rows.  Tiles lie in shared
+//    memory as the bulk copies' swizzle leaves them (16-byte chunk c of row r at c ^ (r % 8), for 64-byte
+//    rows at c ^ (r / 2 % 4)), and the order of the rows (key_row) is one for which
+//    both the keys' and the values' reads meet every bank once.
+//  * A warp copies its tiles to its own part of shared memory and is the only one to read them:
+//    it waits for its own copies, never for another warp.  It keeps kStages - 1 tiles in flight, and
+//    goes on to the next segment's while the CTA still joins the last one's results.  One lane issues
+//    a tile's tensor copies; pages whose rows do not come in eights are copied by cp.async, which
+//    costs some 300 instructions a tile for the addresses.
 //  * The warps of a CTA take a segment's tiles in turn and join at its end; an item of at most
 //    kSolo tiles goes to one warp whole, so that short sequences need no barrier at all.
 //
@@ -23,6 +28,8 @@
 // its weight, taken relative to the largest value scale so far so that the weights stay in f16's
 // range.  Weights are split into a high and a low 16-bit part, one product each.
 #pragma once
+
+#include <cuda.h>
 
 #include "decode.cuh"
 
@@ -91,13 +98,34 @@ __device__ __forceinline__ uint32_t transpose8x8(uint32_t x) {
   return y;
 }
 
-template <int BYTES> __device__ __forceinline__ void copy_async(uint32_t to, const char *from, bool there) {
+template <int BYTES> __device__ __forceinline__ void copy_async(uint32_t to, const void *from, bool there) {
   if (BYTES == 16)
     asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(to), "l"(from), "r"(there ? 16 : 0) : "memory");
-  else if (BYTES == 8)
-    asm volatile("cp.async.ca.shared.global [%0], [%1], 8, %2;" ::"r"(to), "l"(from), "r"(there ? 8 : 0) : "memory");
   else
     asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(to), "l"(from), "r"(there ? 4 : 0) : "memory");
+}
+
+// A box of the cache at (byte, row, head, page), zeros outside.
+__device__ __forceinline__ void copy_box(uint32_t to, const CUtensorMap *map, int byte, int row, int head, int page,
+                                         uint32_t barrier) {
+  asm volatile(
+      "cp.async.bulk.tensor.4d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5}], [%6];" ::
+          "r"(to), "l"(map), "r"(byte), "r"(row), "r"(head), "r"(page), "r"(barrier)
+      : "memory");
+}
+
+// Waits for the barrier's phase; false when that takes longer than anything could (some 0.1 s or more).
+__device__ __forceinline__ bool wait_barrier(uint32_t barrier, uint32_t parity) {
+  for (int i = 0; i < 1 << 18; ++i) {
+    uint32_t done;
+    asm volatile(
+        "{.reg .pred p; mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2; selp.u32 %0, 1, 0, p;}"
+        : "=r"(done)
+        : "r"(barrier), "r"(parity)
+        : "memory");
+    if (done) return true;
+  }
+  return false;
 }
 
 template <int N> struct words;
@@ -116,17 +144,31 @@ template <typename C, int DP, int NG> struct MmaShape {
   static constexpr bool Q8 = quantised<C>::value;
   static constexpr int KC = DP * EL / 64;                          // 16-byte chunks of a key row in a lane
   static constexpr int VB = DP * EL / 8 < 16 ? DP * EL / 8 : 16;   // bytes of a value chunk
-  static constexpr int VC = DP * EL / 8 / VB;                      // value chunks of a row in a lane
+  static constexpr int LINE = DP * EL < 128 ? DP * EL : 128;       // bytes of a row that lie together
+  static constexpr int PARTS = DP * EL / LINE;
   static constexpr int KT = DP * EL <= 128 ? 32 : 16;              // rows of a tile
-  static constexpr int kStage = 2 * KT * DP * EL + (Q8 ? 2 * KT * 4 : 0);
-  static constexpr int kStages = kStage > 4096 + 256 ? 3 : 6;
-  static constexpr int kWarps = kStage > 8192 + 256 ? 4 : 8;       // one CTA per SM
+  static constexpr int kTile = 2 * KT * DP * EL;                   // bytes, keys and values
+  static constexpr int kStages = kTile > 4096 ? 3 : 6;
+  static constexpr int kWarps = kTile > 8192 ? 4 : 8;              // one CTA per SM
+  static constexpr int kScales = Q8 ? 2 * KT * 4 : 0;
   // Floats of an o row; a row of o for each head fits a stage.  A few floats more than DP spread
   // the rows over the banks.
-  static constexpr int kRow = 8 * NG * (DP + 4) * 4 <= kStage ? DP + 4 : DP;
-  static_assert(8 * NG * kRow * 4 <= kStage, "o must fit a stage");
-  static constexpr int kShared = kWarps * kStages * kStage;
+  static constexpr int kRow = 8 * NG * (DP + 4) * 4 <= kTile ? DP + 4 : DP;
+  static_assert(8 * NG * kRow * 4 <= kTile, "o must fit a stage");
+  static constexpr int kShared = kWarps * kStages * (kTile + kScales) + 1024;  // from a multiple of 1024 on
 };
+
+// The row of the cache, of 8, that is row i of the scores.
+template <int LINE> __device__ __forceinline__ int key_row(int i) {
+  if (LINE == 128) return i & 1 ? (i + 4) & 7 : i;      // 0 5 2 7 4 1 6 3
+  const int e = i / 2 + (i / 2 & 2);
+  return i & 1 ? e ^ 3 : e;                             // 0 3 1 2 4 7 5 6
+}
+
+// Where 16-byte chunk c of row r of a tile lies.
+template <int LINE> __device__ __forceinline__ int place(int r, int c) {
+  return r * LINE + (LINE == 128 ? c ^ (r & 7) : c ^ (r / 2 & 3)) * 16;
+}
 
 // One warp's way through its CTA's segments, tile by tile.
 template <typename S> struct Tiles {
@@ -147,22 +189,29 @@ template <typename S> struct Tiles {
   }
 };
 
-template <typename C, int DP, int NG>
-__global__ void __launch_bounds__(32 * MmaShape<C, DP, NG>::kWarps, 1) mma_kernel(const DecodeArgs a) {
+template <typename C, int DP, int NG, bool BOXES>
+__global__ void __launch_bounds__(32 * MmaShape<C, DP, NG>::kWarps, 1)
+    mma_kernel(const DecodeArgs a, const __grid_constant__ CUtensorMap k_map, const __grid_constant__ CUtensorMap v_map) {
   using S = MmaShape<C, DP, NG>;
   using T = typename operand<C>::type;
-  constexpr int EL = S::EL, KC = S::KC, VB = S::VB, VC = S::VC, KT = S::KT, SUBS = KT / 16, W = S::kWarps;
+  constexpr int EL = S::EL, KC = S::KC, VB = S::VB, LINE = S::LINE, PARTS = S::PARTS, KT = S::KT, SUBS = KT / 16;
+  constexpr int W = S::kWarps;
   constexpr bool Q8 = S::Q8;
   constexpr int MT = DP / 16;          // tiles of 16 channels of the output
-  constexpr int LINE = DP * EL < 128 ? DP * EL : 128;   // bytes of a row copied by neighbouring lanes
-  constexpr int LANES = LINE / 16, PARTS = DP * EL / LINE;
-  extern __shared__ __align__(16) char shared[];
+  extern __shared__ char shared_from[];
   __shared__ JoinShared<W> join;
+  __shared__ __align__(8) uint64_t barriers[W][S::kStages];
   const gar_kv_cache &c = a.c;
   const int warp = threadIdx.x / 32, lane = threadIdx.x & 31, g = lane / 4, t = lane & 3;
-  char *const mine = shared + warp * (S::kStages * S::kStage);
+  char *const shared = shared_from + (-(uint32_t)__cvta_generic_to_shared(shared_from) & 1023);
+  char *const mine = shared + warp * (S::kStages * S::kTile);
+  float *const scales = reinterpret_cast<float *>(shared + W * S::kStages * S::kTile + warp * (S::kStages * S::kScales));
   const uint32_t mine_at = (uint32_t)__cvta_generic_to_shared(mine);
-  const int row_bytes = c.dim * EL;
+  const uint32_t scales_at = (uint32_t)__cvta_generic_to_shared(scales);
+  const uint32_t barrier = (uint32_t)__cvta_generic_to_shared(barriers[warp]);
+  if (BOXES && lane < S::kStages)
+    asm volatile("mbarrier.init.shared::cta.b64 [%0], 1; fence.mbarrier_init.release.cluster;" ::"r"(barrier + 8 * lane) : "memory");
+  __syncwarp();
 
   Tiles<S> get;   // copies, kStages - 1 tiles ahead of
   get.walk.template start<32 * W>(a);
@@ -179,67 +228,77 @@ __global__ void __launch_bounds__(32 * MmaShape<C, DP, NG>::kWarps, 1) mma_kerne
       if (n >= get.seg.lo && n < get.seg.to) page = a.table[get.seg.b * a.table_stride + a.page(n)];
     }
   };
+  // Starts the copies of get's tile.
   const auto issue = [&](int stage) {
     if (more) {
-      const int n = get.seg.from + get.tile * KT + (lane & (KT - 1));
-      int64_t at = -1, at_scale = 0;  // bytes; elements
-      if (n >= get.seg.lo && n < get.seg.to) {
-        const int r = n - (int)a.page(n) * c.page_size;
-        if ((unsigned)page < (uint64_t)c.pages) {
-          at = (page * c.page_stride + get.seg.kv_head * c.head_stride + r * c.token_stride) * EL;
-          if (Q8) at_scale = page * c.scale_page_stride + r * c.scale_token_stride + get.seg.kv_head * c.scale_head_stride;
-        } else if (c.status) {
-          atomicOr(c.status, GAR_KV_BAD_PAGE);
-        }
+      const int n = get.seg.from + get.tile * KT + (lane & (KT - 1)), r = n - (int)a.page(n) * c.page_size;
+      const bool there = n >= get.seg.lo && n < get.seg.to && (unsigned)page < (uint64_t)c.pages;
+      if (n >= get.seg.lo && n < get.seg.to && !there && c.status) atomicOr(c.status, GAR_KV_BAD_PAGE);
+      const uint32_t tile_at = mine_at + stage * S::kTile;
+      if (Q8 && lane < KT) {
+        const int64_t at = there ? page * c.scale_page_stride + r * c.scale_token_stride +
+                                       get.seg.kv_head * c.scale_head_stride : 0;
+        const uint32_t to = scales_at + stage * S::kScales + lane * 4;
+        copy_async<4>(to, c.k_scale + at, there);
+        copy_async<4>(to + KT * 4, c.v_scale + at, there);
       }
-      get.tile += get.step;
-      fetch_page();
-      const char *const kp = static_cast<const char *>(c.k), *const vp = static_cast<const char *>(c.v);
-      // Keys: LANES lanes a line.  Odd rows swap the halves of a 128-byte line, so that
-      // the 8 lanes that read 4 chunks of two rows at once meet 32 different banks.
-      {
-        constexpr int ROWS = 32 / LANES;
-        const int chunk = lane & (LANES - 1), row = lane / LANES;
+      if constexpr (BOXES) {
+        // A box is a.box_rows rows of one page (those outside the segment too).  A page that no
+        // row of the segment is on has number -1 here and is filled with zeros.
+        const uint32_t bar = barrier + 8 * stage;
+        if (lane == 0)
+          asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(S::kTile) : "memory");
+        for (int r0 = 0; r0 < KT; r0 += a.box_rows) {
+          const unsigned some = __ballot_sync(~0u, there && (lane & (KT - 1)) / a.box_rows * a.box_rows == r0);
+          const int p = __shfl_sync(~0u, page, some ? __ffs(some) - 1 : 0), row = __shfl_sync(~0u, r, r0);
+          if (lane == 0) {
+#pragma unroll
+            for (int i = 0; i < PARTS; ++i) {
+              const uint32_t to = tile_at + (i * KT + r0) * LINE;
+              copy_box(to, &k_map, i * LINE, row, get.seg.kv_head, some ? p : -1, bar);
+              copy_box(to + KT * DP * EL, &v_map, i * LINE, row, get.seg.kv_head, some ? p : -1, bar);
+            }
+          }
+        }
+        get.tile += get.step;
+        fetch_page();
+      } else {
+        const int64_t at =
+            there ? (page * c.page_stride + get.seg.kv_head * c.head_stride + r * c.token_stride) * EL : -1;
+        get.tile += get.step;
+        fetch_page();
+        constexpr int LANES = LINE / 16, ROWS = 32 / LANES;
+        const char *const kp = static_cast<const char *>(c.k), *const vp = static_cast<const char *>(c.v);
+        const int chunk = lane & (LANES - 1);
 #pragma unroll
         for (int r = 0; r < KT; r += ROWS) {
-          const int64_t x = __shfl_sync(~0u, at, r + row);
+          const int row = r + lane / LANES;
+          const int64_t x = __shfl_sync(~0u, at, row);
 #pragma unroll
           for (int p = 0; p < PARTS; ++p) {
             const int off = p * LINE + chunk * 16;
-            const bool there = x >= 0 && off < row_bytes;
-            copy_async<16>(mine_at + stage * S::kStage + (p * KT + r + row) * LINE +
-                               (LANES == 8 ? chunk ^ ((row & 1) << 2) : chunk) * 16,
-                           there ? kp + x + off : kp, there);
+            const bool in = x >= 0 && off < c.dim * EL;
+            const uint32_t to = tile_at + p * KT * LINE + place<LINE>(row, chunk);
+            copy_async<16>(to, in ? kp + x + off : kp, in);
+            copy_async<16>(to + KT * DP * EL, in ? vp + x + off : vp, in);
           }
         }
-      }
-      uint32_t dst = mine_at + stage * S::kStage + KT * DP * EL + lane * VB;
-#pragma unroll
-      for (int s = 0; s < SUBS; ++s)
-#pragma unroll
-        for (int r = 0; r < 4; ++r) {
-          const int64_t x = __shfl_sync(~0u, at, s * 16 + 2 * t + (r & 1) + 8 * (r / 2));
-#pragma unroll
-          for (int k = 0; k < VC; ++k) {
-            const int off = (g + 8 * k) * VB;
-            const bool there = x >= 0 && off < row_bytes;
-            copy_async<VB>(dst, there ? vp + x + off : vp, there);
-            dst += 32 * VB;
-          }
-        }
-      if (Q8 && lane < KT) {
-        const uint32_t to_scale = mine_at + stage * S::kStage + 2 * KT * DP * EL + lane * 4;
-        copy_async<4>(to_scale, reinterpret_cast<const char *>(c.k_scale + at_scale), at >= 0);
-        copy_async<4>(to_scale + KT * 4, reinterpret_cast<const char *>(c.v_scale + at_scale), at >= 0);
       }
     }
-    asm volatile("cp.async.commit_group;" ::: "memory");
+    if (Q8 || !BOXES) asm volatile("cp.async.commit_group;" ::: "memory");
   };
 
   fetch_page();
 #pragma unroll
   for (int s = 0; s < S::kStages - 1; ++s) issue(s);
   int stage = 0;  // the next tile's; the one before it is free
+  uint32_t parity = 0;
+  // This lane's places in a tile: rows g and g + 8 of the scores, rows 2t and 2t + 1 of the values.
+  const int k_at = place<LINE>(key_row<LINE>(g), t);
+  int v_at[2];
+#pragma unroll
+  for (int i = 0; i < 2; ++i)
+    v_at[i] = KT * DP * EL + place<LINE>(key_row<LINE>(2 * t + i), VB == 16 ? g : g / 2) + (VB == 16 ? 0 : (g & 1) * 8);
 
   while (use.next(a, warp)) {
     if (!use.mine) continue;
@@ -286,12 +345,25 @@ __global__ void __launch_bounds__(32 * MmaShape<C, DP, NG>::kWarps, 1) mma_kerne
     for (int ng = 0; ng < NG; ++ng) m[ng][0] = m[ng][1] = -INFINITY;
 
     for (; use.tile < use.tiles; use.tile += use.step) {
-      asm volatile("cp.async.wait_group %0;" ::"n"(S::kStages - 2) : "memory");
+      if (Q8 || !BOXES) asm volatile("cp.async.wait_group %0;" ::"n"(S::kStages - 2) : "memory");
+      if (BOXES && !wait_barrier(barrier + 8 * stage, parity) && c.status) atomicOr(c.status, GAR_KV_TIMEOUT);
       __syncwarp();
       issue(stage == 0 ? S::kStages - 1 : stage - 1);
-      const char *at = mine + stage * S::kStage;
-      stage = stage == S::kStages - 1 ? 0 : stage + 1;
-      const float *k_scale = reinterpret_cast<const float *>(at + 2 * KT * DP * EL), *v_scale = k_scale + KT;
+      char *const at = mine + stage * S::kTile;
+      const float *k_scale = scales + stage * (S::kScales / 4), *v_scale = k_scale + KT;
+      if (++stage == S::kStages) stage = 0, parity ^= 1;
+      const int n0 = seg.from + use.tile * KT;
+      const bool ragged = n0 < seg.lo || n0 + KT > seg.to;
+      if (BOXES && ragged) {
+        // What the copies brought of rows outside the segment must not meet the products: 0 * NaN is NaN.
+        const int n = n0 + lane;
+        if (lane < KT && (n < seg.lo || n >= seg.to))
+          for (int i = 0; i < PARTS; ++i)
+            for (int x = 0; x < LINE; x += 16)
+              *reinterpret_cast<uint4 *>(at + KT * DP * EL + (i * KT + lane) * LINE + x) = make_uint4(0, 0, 0, 0);
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+        __syncwarp();
+      }
 
       // Scores.
       float s[SUBS][NG][4] = {};
@@ -299,8 +371,7 @@ __global__ void __launch_bounds__(32 * MmaShape<C, DP, NG>::kWarps, 1) mma_kerne
       for (int sub = 0; sub < SUBS; ++sub)
 #pragma unroll
         for (int k = 0; k < KC; ++k) {
-          const int part = k * 64 / LINE, chunk = (t + 4 * k) % LANES;
-          const char *const x_at = at + (part * KT + sub * 16 + g) * LINE + (LANES == 8 ? chunk ^ ((g & 1) << 2) : chunk) * 16;
+          const char *const x_at = at + (k * 64 / LINE * KT + sub * 16) * LINE + (LINE == 128 && k % 2 ? k_at ^ 64 : k_at);
           const uint4 x = *reinterpret_cast<const uint4 *>(x_at), y = *reinterpret_cast<const uint4 *>(x_at + 8 * LINE);
           const uint32_t xs[4] = {x.x, x.y, x.z, x.w}, ys[4] = {y.x, y.y, y.z, y.w};
           if constexpr (!Q8) {
@@ -321,8 +392,6 @@ __global__ void __launch_bounds__(32 * MmaShape<C, DP, NG>::kWarps, 1) mma_kerne
             }
           }
         }
-      const int n0 = seg.from + use.tile * KT;
-      const bool ragged = n0 < seg.lo || n0 + KT > seg.to;
       float top[NG][2];
 #pragma unroll
       for (int ng = 0; ng < NG; ++ng) top[ng][0] = m[ng][0], top[ng][1] = m[ng][1];
@@ -330,9 +399,9 @@ __global__ void __launch_bounds__(32 * MmaShape<C, DP, NG>::kWarps, 1) mma_kerne
       for (int sub = 0; sub < SUBS; ++sub)
 #pragma unroll
         for (int r = 0; r < 2; ++r) {
-          const int n = n0 + sub * 16 + g + 8 * r;
+          const int row = sub * 16 + key_row<LINE>(g) + 8 * r, n = n0 + row;
           const bool seen = !ragged || (n >= seg.lo && n < seg.to);
-          const float f = Q8 ? k_scale[sub * 16 + g + 8 * r] : 1.f;
+          const float f = Q8 ? k_scale[row] : 1.f;
 #pragma unroll
           for (int ng = 0; ng < NG; ++ng)
 #pragma unroll
@@ -375,7 +444,7 @@ __global__ void __launch_bounds__(32 * MmaShape<C, DP, NG>::kWarps, 1) mma_kerne
       for (int sub = 0; sub < SUBS; ++sub)
 #pragma unroll
         for (int r = 0; r < 2; ++r) {
-          const float f = Q8 ? v_scale[sub * 16 + g + 8 * r] * v_inverse : 1.f;
+          const float f = Q8 ? v_scale[sub * 16 + key_row<LINE>(g) + 8 * r] * v_inverse : 1.f;
 #pragma unroll
           for (int ng = 0; ng < NG; ++ng) {
             float p[2];
@@ -391,18 +460,18 @@ __global__ void __launch_bounds__(32 * MmaShape<C, DP, NG>::kWarps, 1) mma_kerne
           }
         }
       // Values.
-      const char *const v_at = at + KT * DP * EL + lane * VB;
 #pragma unroll
       for (int sub = 0; sub < SUBS; ++sub)
 #pragma unroll
-        for (int k = 0; k < VC; ++k) {
-          using W = typename words<VB>::type;
+        for (int k = 0; k < PARTS; ++k) {
+          using V = typename words<VB>::type;
           union {
-            W w;
+            V v;
             uint32_t u[VB / 4];
           } x[4];
 #pragma unroll
-          for (int r = 0; r < 4; ++r) x[r].w = *reinterpret_cast<const W *>(v_at + ((sub * 4 + r) * VC + k) * 32 * VB);
+          for (int r = 0; r < 4; ++r)
+            x[r].v = *reinterpret_cast<const V *>(at + (k * KT + sub * 16 + r / 2 * 8) * LINE + v_at[r & 1]);
 #pragma unroll
           for (int i = 0; i < VB / 4; ++i) {
             if constexpr (!Q8) {
@@ -431,7 +500,7 @@ __global__ void __launch_bounds__(32 * MmaShape<C, DP, NG>::kWarps, 1) mma_kerne
         }
     }
     // The stage read last holds this warp's o until it is joined.
-    float *const o_mine = reinterpret_cast<float *>(mine + (stage == 0 ? S::kStages - 1 : stage - 1) * S::kStage);
+    float *const o_mine = reinterpret_cast<float *>(mine + (stage == 0 ? S::kStages - 1 : stage - 1) * S::kTile);
     __syncwarp();
 #pragma unroll
     for (int ng = 0; ng < NG; ++ng)
@@ -450,6 +519,8 @@ __global__ void __launch_bounds__(32 * MmaShape<C, DP, NG>::kWarps, 1) mma_kerne
               Q8 ? make_float2(o[i][ng][h] * v_ref, o[i][ng][2 + h] * v_ref) : make_float2(o[i][ng][h], o[i][ng][2 + h]);
         }
       }
+    // (copies into this stage come after the join's barrier)
+    if (BOXES) asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
     const float *const o_all = reinterpret_cast<const float *>(shared);
     if (lane == 0) join.at[warp] = (int)(o_mine - o_all);
     if (use.alone) {
@@ -462,14 +533,24 @@ __global__ void __launch_bounds__(32 * MmaShape<C, DP, NG>::kWarps, 1) mma_kerne
   asm volatile("cp.async.wait_all;" ::: "memory");
 }
 
+// Maps of the cache as bytes [pages][heads][page_size][dim]; false where it has none.
+bool box_map(const gar_kv_cache &c, void *base, int line, int rows, CUtensorMap *map);
+
 template <typename C, int DP, int NG> int launch_mma(DecodeArgs a, int sms, cudaStream_t stream) {
   using S = MmaShape<C, DP, NG>;
   a.item_heads = std::min(a.group, 8 * NG);
   a.item_groups = (a.group + 8 * NG - 1) / (8 * NG);
-  const cudaError_t e =
-      cudaFuncSetAttribute(mma_kernel<C, DP, NG>, cudaFuncAttributeMaxDynamicSharedMemorySize, S::kShared);
-  if (e != cudaSuccess) return cuda_fail(e, "cudaFuncSetAttribute");
-  mma_kernel<C, DP, NG><<<sms, 32 * S::kWarps, S::kShared, stream>>>(a);
+  // Boxes of as many rows as a page has in a tile: a tile starts at a multiple of KT rows.
+  a.box_rows = a.c.page_size % S::KT == 0 ? S::KT : a.c.page_size % 16 == 0 ? 16 : a.c.page_size % 8 == 0 ? 8 : 0;
+  CUtensorMap maps[2];
+  const bool boxes = a.box_rows && box_map(a.c, a.c.k, S::LINE, a.box_rows, &maps[0]) &&
+                     box_map(a.c, a.c.v, S::LINE, a.box_rows, &maps[1]);
+  const auto kernel = boxes ? mma_kernel<C, DP, NG, true> : mma_kernel<C, DP, NG, false>;
+  static const cudaError_t e[2] = {
+      cudaFuncSetAttribute(mma_kernel<C, DP, NG, false>, cudaFuncAttributeMaxDynamicSharedMemorySize, S::kShared),
+      cudaFuncSetAttribute(mma_kernel<C, DP, NG, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, S::kShared)};
+  if (e[boxes] != cudaSuccess) return cuda_fail(e[boxes], "cudaFuncSetAttribute");
+  kernel<<<sms, 32 * S::kWarps, S::kShared, stream>>>(a, maps[0], maps[1]);
   return launched("mma_kernel");
 }
 

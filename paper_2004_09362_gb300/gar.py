@@ -24,7 +24,7 @@ GAR_GROUP_CYCLIC, GAR_GROUP_XOR = 0, 1
 GAR_F16, GAR_I8, GAR_E4M3 = 3, 4, 5          # decoding operators only
 GAR_ROPE_HALF, GAR_ROPE_INTERLEAVED = 0, 1
 GAR_ROPE_PLAIN, GAR_ROPE_LINEAR, GAR_ROPE_BASE, GAR_ROPE_PARTS = 0, 1, 2, 3
-GAR_KV_BAD_SLOT, GAR_KV_BAD_PAGE, GAR_KV_BAD_POSITION, GAR_KV_BAD_LENGTH = 1, 2, 4, 8
+GAR_KV_BAD_SLOT, GAR_KV_BAD_PAGE, GAR_KV_BAD_POSITION, GAR_KV_BAD_LENGTH, GAR_KV_TIMEOUT = 1, 2, 4, 8, 16
 GAR_MAX_HEAD_DIM = 256
 GAR_FORM_SINGLE, GAR_FORM_BREADTH, GAR_FORM_SPLIT = 0, 1, 2
 GROUPS = {"cyclic": GAR_GROUP_CYCLIC, "xor": GAR_GROUP_XOR}
