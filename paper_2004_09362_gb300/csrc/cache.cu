@@ -15,47 +15,55 @@ struct CacheArgs {
   void *out[2];
   int64_t ts[2], hs[2];        // strides of in[]
   const int64_t *slots;
-  const void *positions;       // null: no rotation
+  const void *positions;
   const float2 *table;
   int64_t table_rows;
-  int64_t rows;                // tokens * heads
+  int rows;                    // tokens * heads
   int rot, interleaved, wide_positions;
   int lanes;                   // power of two: lanes that hold one row
+  bool wide_table;             // a chunk's table entries lie at multiples of 16 bytes
+  Divide heads, page;
 };
 
 // The place of a slot's row, or false where there is none.
 struct Place {
   int64_t at, scale;
 };
-__device__ __forceinline__ bool find(const gar_kv_cache &c, int64_t slot, int head, Place *p) {
+__device__ __forceinline__ bool find(const CacheArgs &a, int64_t slot, int head, Place *p) {
+  const gar_kv_cache &c = a.cache;
   if (slot < 0) return false;
-  int64_t page;
-  int row;
-  if ((uint64_t)slot <= 0xffffffffu) {  // a 32-bit division where it does
-    page = (uint32_t)slot / (uint32_t)c.page_size;
-    row = (int)((uint32_t)slot - (uint32_t)page * (uint32_t)c.page_size);
-  } else {
-    page = slot / c.page_size;
-    row = (int)(slot - page * c.page_size);
-  }
+  const int64_t page = slot < 0x7fffffff ? a.page((uint32_t)slot) : slot / c.page_size;
   if (page >= c.pages) {
     if (c.status) atomicOr(c.status, GAR_KV_BAD_SLOT);
     return false;
   }
+  const int row = (int)(slot - page * c.page_size);
   p->at = page * c.page_stride + head * c.head_stride + row * c.token_stride;
   p->scale = page * c.scale_page_stride + head * c.scale_head_stride + row * c.scale_token_stride;
   return true;
 }
 
+// kChunk elements as they lie in memory, and their values.
+template <typename T> struct alignas(sizeof(T) > 1 ? 16 : 8) raw_chunk {
+  uint32_t w[kChunk * sizeof(T) / 4];
+};
+template <typename T> __device__ __forceinline__ void values(const raw_chunk<T> &r, float (&v)[kChunk]) {
+#pragma unroll
+  for (int k = 0; k < kChunk; k += 2) {
+    float2 x;
+    if constexpr (sizeof(T) == 4)
+      x = make_float2(__uint_as_float(r.w[k]), __uint_as_float(r.w[k + 1]));
+    else if constexpr (sizeof(T) == 2)
+      x = unpack2(r.w[k / 2], T());
+    else
+      x = unpack2((uint16_t)(r.w[k / 4] >> (k & 2) * 8), T());
+    v[k] = x.x, v[k + 1] = x.y;
+  }
+}
+
 template <bool WIDE, typename T> __device__ __forceinline__ void load(const T *p, int from, int dim, float (&v)[kChunk]) {
   if (WIDE) {
-    constexpr int N = sizeof(T) >= 2 ? 16 / sizeof(T) : kChunk;
-#pragma unroll
-    for (int k = 0; k < kChunk; k += N) {
-      const pack<T, N> u = *reinterpret_cast<const pack<T, N> *>(p + from + k);
-#pragma unroll
-      for (int e = 0; e < N; ++e) v[k + e] = to_f32(u.e[e]);
-    }
+    values(*reinterpret_cast<const raw_chunk<T> *>(p + from), v);
   } else {
 #pragma unroll
     for (int k = 0; k < kChunk; ++k) v[k] = from + k < dim ? to_f32(p[from + k]) : 0.f;
@@ -79,16 +87,39 @@ template <bool WIDE, typename T> __device__ __forceinline__ void store(T *p, int
   }
 }
 
-// The channels [from, from + kChunk) of a row rotated; each needs its partner, which is read
-// again (from the row that is in L1 by then) rather than exchanged.
-template <typename T>
-__device__ __forceinline__ void rotate(const CacheArgs &a, const T *row, int64_t token, int from, float (&v)[kChunk]) {
-  if (from >= a.rot) return;
+// The channels [from, from + kChunk) of a row rotated.  With the half layout the channels they
+// pair with are another lane's; they were read into w as well.
+template <bool WIDE, typename T>
+__device__ __forceinline__ void rotate(const CacheArgs &a, const T *row, int64_t token, int from, float (&v)[kChunk],
+                                       const float (&w)[kChunk]) {
   const int64_t pos = a.wide_positions ? static_cast<const int64_t *>(a.positions)[token]
                                        : (int64_t) static_cast<const int32_t *>(a.positions)[token];
   const bool good = (uint64_t)pos < (uint64_t)a.table_rows;
   if (!good && a.cache.status) atomicOr(a.cache.status, GAR_KV_BAD_POSITION);
   const int half = a.rot / 2;
+  const float2 *const t = a.table + (good ? pos * half : 0);
+  if (WIDE && a.wide_table) {
+    if (a.interleaved) {
+      float c[kChunk / 2], s[kChunk / 2];
+      load_rotation<kChunk / 2, true>(t + (good ? from / 2 : 0), good, c, s);
+#pragma unroll
+      for (int k = 0; k < kChunk; k += 2) {
+        const float x = v[k], y = v[k + 1];
+        v[k] = __fsub_rn(__fmul_rn(x, c[k / 2]), __fmul_rn(y, s[k / 2]));
+        v[k + 1] = __fadd_rn(__fmul_rn(y, c[k / 2]), __fmul_rn(x, s[k / 2]));
+      }
+    } else {
+      const bool second = from >= half;
+      float c[kChunk], s[kChunk];
+      load_rotation<kChunk, true>(t + (good ? from - (second ? half : 0) : 0), good, c, s);
+#pragma unroll
+      for (int k = 0; k < kChunk; ++k) {
+        const float x = __fmul_rn(v[k], c[k]), y = __fmul_rn(w[k], s[k]);
+        v[k] = second ? __fadd_rn(x, y) : __fsub_rn(x, y);
+      }
+    }
+    return;
+  }
 #pragma unroll
   for (int k = 0; k < kChunk; ++k) {
     const int c = from + k;
@@ -96,71 +127,117 @@ __device__ __forceinline__ void rotate(const CacheArgs &a, const T *row, int64_t
     const int pair = a.interleaved ? c / 2 : c < half ? c : c - half;
     const bool second = a.interleaved ? c & 1 : c >= half;
     const int other = a.interleaved ? c ^ 1 : second ? c - half : c + half;
-    const float2 cs = good ? __ldg(a.table + pos * half + pair) : make_float2(__int_as_float(0x7fc00000), 0.f);
-    const float w = to_f32(row[other]);
-    v[k] = second ? __fadd_rn(__fmul_rn(v[k], cs.x), __fmul_rn(w, cs.y))
-                  : __fsub_rn(__fmul_rn(v[k], cs.x), __fmul_rn(w, cs.y));
+    const float2 cs = good ? __ldg(t + pair) : make_float2(__int_as_float(0x7fc00000), 0.f);
+    const float x = __fmul_rn(v[k], cs.x), y = __fmul_rn(to_f32(row[other]), cs.y);
+    v[k] = second ? __fadd_rn(x, y) : __fsub_rn(x, y);
   }
 }
 
-// T -> C rows.  a.lanes neighbouring lanes hold a row, kChunk channels each, so that the largest
-// magnitude is found by shuffles and the row is read once.  blockIdx.y: 0 keys, 1 values.
-// Bound by memory.
-template <typename T, typename C, bool WIDE> __global__ void __launch_bounds__(kThreads) write_kernel(const CacheArgs a) {
-  const gar_kv_cache &c = a.cache;
-  const int which = blockIdx.y;
-  const int lane = threadIdx.x & (a.lanes - 1), from = lane * kChunk;
-  const int64_t i = (int64_t)blockIdx.x * (kThreads / a.lanes) + threadIdx.x / a.lanes;
-  Place p;
-  const int64_t token = i / c.heads;
-  const int head = (int)(i - token * c.heads);
-  const bool there = i < a.rows && find(c, a.slots[token], head, &p);
-  const bool mine = there && from < c.dim;
-  float v[kChunk] = {};
-  if (mine) {
-    const T *row = static_cast<const T *>(a.in[which]) + token * a.ts[which] + head * a.hs[which];
-    load<WIDE>(row, from, c.dim, v);
-    if (which == 0 && a.positions) rotate(a, row, token, from, v);
+// The codes' values of a row of which this lane holds v, and its scale.
+template <typename C> __device__ __forceinline__ float quantise(float (&v)[kChunk], int lanes) {
+  float most = 0.f;
+  bool sound = true;
+#pragma unroll
+  for (int k = 0; k < kChunk; ++k) {
+    most = fmaxf(most, fabsf(v[k]));
+    sound &= fabsf(v[k]) <= 3.402823466e38f;
   }
+  if (!sound) most = __int_as_float(0x7f800000);
+  for (int d = lanes / 2; d > 0; d /= 2) most = fmaxf(most, __shfl_xor_sync(~0u, most, d));
+  // An infinity or a NaN in the row: codes 0 under a NaN scale.
+  const bool bad = most > 3.402823466e38f;
+  const float scale = bad ? __int_as_float(0x7fc00000) : __fmul_rn(most, 1.f / quantised<C>::largest);
+#pragma unroll
+  for (int k = 0; k < kChunk; ++k) v[k] = bad || scale == 0.f ? 0.f : __fdiv_rn(v[k], scale);
+  return scale;
+}
+
+// T -> C rows.  a.lanes neighbouring lanes hold a token's row of one head, kChunk channels of the key
+// and of the value each, so that the largest magnitudes are found by shuffles and the rows are
+// read once.  Bound by memory: all loads but the table's go out before any is waited for.
+template <typename T, typename C, bool WIDE, bool ROTATE>
+__global__ void __launch_bounds__(kThreads) write_kernel(const CacheArgs a) {
+  const gar_kv_cache &c = a.cache;
+  const int lane = threadIdx.x & (a.lanes - 1), from = lane * kChunk;
+  const int i = blockIdx.x * (kThreads / a.lanes) + threadIdx.x / a.lanes;
+  const bool any = i < a.rows;
+  const int64_t token = any ? a.heads(i) : 0;
+  const int head = any ? i - (int)token * c.heads : 0;
+  const int64_t slot = any ? a.slots[token] : -1;
+  const T *const k_row = static_cast<const T *>(a.in[0]) + token * a.ts[0] + head * a.hs[0];
+  const T *const v_row = static_cast<const T *>(a.in[1]) + token * a.ts[1] + head * a.hs[1];
+  float k[kChunk] = {}, v[kChunk] = {}, w[kChunk];
+  const bool in = any && from < c.dim, turned = ROTATE && in && from < a.rot;
+  if (in) {
+    load<WIDE>(k_row, from, c.dim, k);
+    load<WIDE>(v_row, from, c.dim, v);
+    if (turned && WIDE && a.wide_table && !a.interleaved) {
+      const int half = a.rot / 2;
+      load<WIDE>(k_row, from >= half ? from - half : from + half, c.dim, w);
+    }
+  }
+  Place p;
+  const bool there = find(a, slot, head, &p);
+  if (turned && there) rotate<WIDE>(a, k_row, token, from, k, w);
   if (quantised<C>::value) {
-    float most = 0.f;
-    bool sound = true;
-#pragma unroll
-    for (int k = 0; k < kChunk; ++k) {
-      most = fmaxf(most, fabsf(v[k]));
-      sound &= fabsf(v[k]) <= 3.402823466e38f;
-    }
-    if (!sound) most = __int_as_float(0x7f800000);
-    for (int d = a.lanes / 2; d > 0; d /= 2) most = fmaxf(most, __shfl_xor_sync(~0u, most, d));
-    // An infinity or a NaN in the row: codes 0 under a NaN scale.
-    const bool bad = most > 3.402823466e38f;
-    const float scale = bad ? __int_as_float(0x7fc00000) : __fmul_rn(most, 1.f / quantised<C>::largest);
-#pragma unroll
-    for (int k = 0; k < kChunk; ++k) v[k] = bad || scale == 0.f ? 0.f : __fdiv_rn(v[k], scale);
-    if (there && lane == 0) (which ? c.v_scale : c.k_scale)[p.scale] = scale;
+    const float k_scale = quantise<C>(k, a.lanes), v_scale = quantise<C>(v, a.lanes);
+    if (there && lane == 0) c.k_scale[p.scale] = k_scale, c.v_scale[p.scale] = v_scale;
   }
-  if (mine) store<WIDE>(static_cast<C *>(which ? c.v : c.k) + p.at, from, c.dim, v);
+  if (in && there) {
+    store<WIDE>(static_cast<C *>(c.k) + p.at, from, c.dim, k);
+    store<WIDE>(static_cast<C *>(c.v) + p.at, from, c.dim, v);
+  }
 }
 
-template <typename T, typename C, bool WIDE> __global__ void __launch_bounds__(kThreads) read_kernel(const CacheArgs a) {
+// C -> T rows, N of them to a lane: a row's place hangs on its slot, so there are fewer bytes in flight.
+template <typename T, typename C, bool WIDE, int N>
+__global__ void __launch_bounds__(kThreads) read_kernel(const CacheArgs a) {
   const gar_kv_cache &c = a.cache;
-  const int which = blockIdx.y;
-  const int lane = threadIdx.x & (a.lanes - 1), from = lane * kChunk;
-  const int64_t i = (int64_t)blockIdx.x * (kThreads / a.lanes) + threadIdx.x / a.lanes;
-  if (i >= a.rows || from >= c.dim) return;
-  Place p;
-  const int64_t token = i / c.heads;
-  const int head = (int)(i - token * c.heads);
-  float v[kChunk] = {};
-  if (find(c, a.slots[token], head, &p)) {
-    load<WIDE>(static_cast<const C *>(which ? c.v : c.k) + p.at, from, c.dim, v);
-    if (quantised<C>::value) {
-      const float scale = (which ? c.v_scale : c.k_scale)[p.scale];
+  const int lane = threadIdx.x & (a.lanes - 1), from = lane * kChunk, step = kThreads / a.lanes;
+  const int i0 = blockIdx.x * (step * N) + threadIdx.x / a.lanes;
+  if (from >= c.dim) return;
+  Place p[N];
+  bool there[N];
 #pragma unroll
-      for (int k = 0; k < kChunk; ++k) v[k] = __fmul_rn(v[k], scale);
+  for (int n = 0; n < N; ++n) {
+    const int i = i0 + n * step;
+    const int token = i < a.rows ? a.heads(i) : 0;
+    there[n] = i < a.rows && find(a, a.slots[token], i - token * c.heads, &p[n]);
+  }
+  raw_chunk<C> k[N], v[N];
+  float k_scale[N], v_scale[N];
+#pragma unroll
+  for (int n = 0; n < N; ++n) {
+    k_scale[n] = v_scale[n] = 0.f;
+    if (there[n]) {
+      if (WIDE) {
+        k[n] = *reinterpret_cast<const raw_chunk<C> *>(static_cast<const C *>(c.k) + p[n].at + from);
+        v[n] = *reinterpret_cast<const raw_chunk<C> *>(static_cast<const C *>(c.v) + p[n].at + from);
+      }
+      if (quantised<C>::value) k_scale[n] = c.k_scale[p[n].scale], v_scale[n] = c.v_scale[p[n].scale];
     }
   }
-  store<WIDE>(static_cast<T *>(a.out[which]) + i * c.dim, from, c.dim, v);
+#pragma unroll
+  for (int n = 0; n < N; ++n) {
+    const int64_t i = i0 + n * step;
+    if (i >= a.rows) break;
+    float x[kChunk] = {}, y[kChunk] = {};
+    if (there[n]) {
+      if (WIDE) {
+        values(k[n], x);
+        values(v[n], y);
+      } else {
+        load<WIDE>(static_cast<const C *>(c.k) + p[n].at, from, c.dim, x);
+        load<WIDE>(static_cast<const C *>(c.v) + p[n].at, from, c.dim, y);
+      }
+    }
+    if (quantised<C>::value) {
+#pragma unroll
+      for (int e = 0; e < kChunk; ++e) x[e] = __fmul_rn(x[e], k_scale[n]), y[e] = __fmul_rn(y[e], v_scale[n]);
+    }
+    store<WIDE>(static_cast<T *>(a.out[0]) + i * c.dim, from, c.dim, x);
+    store<WIDE>(static_cast<T *>(a.out[1]) + i * c.dim, from, c.dim, y);
+  }
 }
 
 // Calls f with the tags of a float type and the cache's type.
@@ -180,15 +257,21 @@ int check_rows(const gar_kv_cache *cache, int dtype, int64_t tokens) {
   return GAR_OK;
 }
 
-// The launch's grid and lanes; false where the rows are too many.
-bool shape(CacheArgs *a, int64_t tokens, dim3 *grid) {
+// Sets the rows and lanes; false where the rows are too many.
+bool shape(CacheArgs *a, int64_t tokens) {
   const int need = (a->cache.dim + kChunk - 1) / kChunk;
   a->lanes = 1;
   while (a->lanes < need) a->lanes *= 2;
-  a->rows = tokens * a->cache.heads;
-  const int64_t per = kThreads / a->lanes, blocks = (a->rows + per - 1) / per;
-  *grid = dim3((unsigned)blocks, 2);
-  return blocks <= 0x7fffffff;
+  if (tokens > 0x7fffffff / 2 / a->cache.heads) return false;
+  a->rows = (int)tokens * a->cache.heads;
+  a->heads = divide_by((uint32_t)a->cache.heads);
+  a->page = divide_by((uint32_t)a->cache.page_size);
+  return true;
+}
+
+int blocks(const CacheArgs &a, int rows_per_lane) {
+  const int per = kThreads / a.lanes * rows_per_lane;
+  return (a.rows + per - 1) / per;
 }
 
 // 16 bytes of `size`-byte elements (8 of one byte) at every multiple of kChunk channels.
@@ -249,18 +332,17 @@ int gar_kv_write(const gar_kv_cache *cache, const void *k, int64_t k_token_strid
   a.slots = slots, a.positions = positions, a.table = reinterpret_cast<const float2 *>(table);
   a.table_rows = table_rows, a.rot = rot, a.interleaved = layout == GAR_ROPE_INTERLEAVED;
   a.wide_positions = position_bytes == 8;
-  dim3 grid;
-  if (!shape(&a, tokens, &grid)) return refuse("too many rows");
+  if (!shape(&a, tokens)) return refuse("too many rows");
   const int n = 16 / size;
+  a.wide_table = (uintptr_t)table % 16 == 0 && rot % (a.interleaved ? kChunk : 2 * kChunk) == 0;
   const bool wide = wide_cache(*cache) && (uintptr_t)k % 16 == 0 && (uintptr_t)v % 16 == 0 && k_token_stride % n == 0 &&
                     k_head_stride % n == 0 && v_token_stride % n == 0 && v_head_stride % n == 0;
   return with_types(dtype, cache->dtype, [&](auto t, auto c) {
     using T = typename decltype(t)::type;
     using C = typename decltype(c)::type;
-    if (wide)
-      write_kernel<T, C, true><<<grid, kThreads, 0, (cudaStream_t)stream>>>(a);
-    else
-      write_kernel<T, C, false><<<grid, kThreads, 0, (cudaStream_t)stream>>>(a);
+    const auto kernel = wide ? (positions ? write_kernel<T, C, true, true> : write_kernel<T, C, true, false>)
+                             : (positions ? write_kernel<T, C, false, true> : write_kernel<T, C, false, false>);
+    kernel<<<blocks(a, 1), kThreads, 0, (cudaStream_t)stream>>>(a);
     return launched("write_kernel");
   });
 }
@@ -278,16 +360,17 @@ int gar_kv_read(const gar_kv_cache *cache, const int64_t *slots, int64_t tokens,
   CacheArgs a{};
   a.cache = *cache;
   a.out[0] = k, a.out[1] = v, a.slots = slots;
-  dim3 grid;
-  if (!shape(&a, tokens, &grid)) return refuse("too many rows");
+  if (!shape(&a, tokens)) return refuse("too many rows");
   const bool wide = wide_cache(*cache) && (uintptr_t)k % 16 == 0 && (uintptr_t)v % 16 == 0;
   return with_types(dtype, cache->dtype, [&](auto t, auto c) {
     using T = typename decltype(t)::type;
     using C = typename decltype(c)::type;
-    if (wide)
-      read_kernel<T, C, true><<<grid, kThreads, 0, (cudaStream_t)stream>>>(a);
+    if (!wide)
+      read_kernel<T, C, false, 1><<<blocks(a, 1), kThreads, 0, (cudaStream_t)stream>>>(a);
+    else if (blocks(a, 4) < 152 * 4)   // too few CTAs to fill the GPU with four rows a lane
+      read_kernel<T, C, true, 1><<<blocks(a, 1), kThreads, 0, (cudaStream_t)stream>>>(a);
     else
-      read_kernel<T, C, false><<<grid, kThreads, 0, (cudaStream_t)stream>>>(a);
+      read_kernel<T, C, true, 4><<<blocks(a, 4), kThreads, 0, (cudaStream_t)stream>>>(a);
     return launched("read_kernel");
   });
 }

@@ -24,12 +24,6 @@ namespace gar {
 constexpr int kMaxGroup = 16;         // query heads of an item
 constexpr int kMaxCtas = 152 * 4;
 
-// n / d for n < 2^31.
-struct Divide {
-  uint32_t mul, shift;
-  __device__ __forceinline__ uint32_t operator()(uint32_t n) const { return (__umulhi(mul, n) + n) >> shift; }
-};
-
 struct DecodeArgs {
   gar_kv_cache c;
   const void *q;

@@ -23,13 +23,6 @@ size_t workspace_bytes(const gar_attn_plan &p) {
   return kCounterBytes + rows * (2 + dim_pad(p.dim)) * sizeof(float);
 }
 
-// Round-up reciprocal: n / d = (umulhi(mul, n) + n) >> shift for n < 2^31.
-Divide divide_by(uint32_t d) {
-  uint32_t shift = 0;
-  while ((1ull << shift) < d) ++shift;
-  return {(uint32_t)(((1ull << 32) * ((1ull << shift) - d)) / d + 1), shift};
-}
-
 // The tensor-core kernels copy 16-byte chunks and take 16-bit queries.
 bool takes_mma(const gar_kv_cache &c, const void *q, int64_t q_batch_stride, int64_t q_head_stride, int q_dtype) {
   const int64_t n = 16 / element_size(c.dtype);

@@ -65,6 +65,85 @@ template <typename T, int N> struct alignas(sizeof(T) * N) pack {
   T e[N];
 };
 
+// 16 bytes of T as they lie in memory, and their values.  Held packed so that many can be in flight.
+template <typename T> struct chunk16 {
+  static constexpr int N = 16 / sizeof(T);
+  uint4 bits;
+};
+__device__ __forceinline__ float2 unpack2(uint32_t x, __nv_bfloat16) {
+  return make_float2(__uint_as_float(x << 16), __uint_as_float(x & 0xffff0000u));
+}
+__device__ __forceinline__ float2 unpack2(uint32_t x, __half) { return __half22float2(*reinterpret_cast<__half2 *>(&x)); }
+__device__ __forceinline__ float2 unpack2(uint16_t x, i8) {
+  return make_float2((float)(int8_t)(x & 0xff), (float)(int8_t)(x >> 8));
+}
+__device__ __forceinline__ float2 unpack2(uint16_t x, e4m3) {
+  uint32_t h2;
+  asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(h2) : "h"(x));
+  return __half22float2(*reinterpret_cast<__half2 *>(&h2));
+}
+__device__ __forceinline__ uint32_t pack2(float2 x, __nv_bfloat16) {
+  const __nv_bfloat162 y = __floats2bfloat162_rn(x.x, x.y);
+  return *reinterpret_cast<const uint32_t *>(&y);
+}
+__device__ __forceinline__ uint32_t pack2(float2 x, __half) {
+  const __half2 y = __floats2half2_rn(x.x, x.y);
+  return *reinterpret_cast<const uint32_t *>(&y);
+}
+template <typename T> __device__ __forceinline__ void unpack(const chunk16<T> &c, float (&v)[chunk16<T>::N]) {
+  const uint32_t w[4] = {c.bits.x, c.bits.y, c.bits.z, c.bits.w};
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    if constexpr (sizeof(T) == 4) {
+      v[i] = __uint_as_float(w[i]);
+    } else {
+      const float2 x = unpack2(w[i], T());
+      v[2 * i] = x.x, v[2 * i + 1] = x.y;
+    }
+  }
+}
+template <typename T> __device__ __forceinline__ chunk16<T> packed(const float (&v)[chunk16<T>::N]) {
+  uint32_t w[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    if constexpr (sizeof(T) == 4)
+      w[i] = __float_as_uint(v[i]);
+    else
+      w[i] = pack2(make_float2(v[2 * i], v[2 * i + 1]), T());
+  }
+  return {make_uint4(w[0], w[1], w[2], w[3])};
+}
+
+// N (cos, sin) entries of a rotation table, 16 bytes a load where WIDE; NaN where `good` is false.
+template <int N, bool WIDE>
+__device__ __forceinline__ void load_rotation(const float2 *t, bool good, float (&c)[N], float (&s)[N]) {
+  const float nan = __int_as_float(0x7fc00000);
+  if (WIDE && N % 2 == 0) {
+#pragma unroll
+    for (int k = 0; k < N; k += 2) {
+      const float4 v = good ? __ldg(reinterpret_cast<const float4 *>(t + k)) : make_float4(nan, nan, nan, nan);
+      c[k] = v.x, s[k] = v.y, c[k + 1] = v.z, s[k + 1] = v.w;
+    }
+  } else {
+#pragma unroll
+    for (int k = 0; k < N; ++k) {
+      const float2 v = good ? __ldg(t + k) : make_float2(nan, nan);
+      c[k] = v.x, s[k] = v.y;
+    }
+  }
+}
+
+// n / d for n < 2^31, d >= 1, by a round-up reciprocal.
+struct Divide {
+  uint32_t mul, shift;
+  __device__ __forceinline__ uint32_t operator()(uint32_t n) const { return (__umulhi(mul, n) + n) >> shift; }
+};
+inline Divide divide_by(uint32_t d) {
+  uint32_t shift = 0;
+  while ((1ull << shift) < d) ++shift;
+  return {(uint32_t)(((1ull << 32) * ((1ull << shift) - d)) / d + 1), shift};
+}
+
 template <typename T> struct type_tag {
   using type = T;
 };

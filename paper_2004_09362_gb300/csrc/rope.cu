@@ -40,18 +40,82 @@ struct RopeArgs {
   float sign;        // -1 turns back
 };
 
+__device__ __forceinline__ int64_t position(const RopeArgs &a, int64_t token) {
+  return a.wide_positions ? static_cast<const int64_t *>(a.positions)[token]
+                          : (int64_t) static_cast<const int32_t *>(a.positions)[token];
+}
+
 // out = x rotated.  Bound by memory: every element is read and written once.
 //
 // A unit is the work of one thread at one head: with the half layout V channels of the
 // first half and the V that pair with them (two 16-byte accesses each way), with the interleaved
 // layout V channels that hold V/2 pairs; the channels past `rot` are copied in units of V.  The
 // rotation depends on token and channel only, so a thread keeps its unit's table entries in
-// registers and takes several heads; the heads' loads are independent, and kUnroll of them are in
-// flight at once.
-template <typename T, int V, bool INTERLEAVED>
-__global__ void __launch_bounds__(256) rope_kernel(const RopeArgs a) {
+// registers and takes several heads; kUnroll heads' loads are in flight at once, the first of
+// them before the token's position is known.
+template <typename T, bool INTERLEAVED> __global__ void __launch_bounds__(256) rope_kernel(const RopeArgs a) {
   constexpr int kUnroll = 4;
-  constexpr int PAIRS = INTERLEAVED ? (V > 1 ? V / 2 : 1) : V;
+  using chunk = chunk16<T>;
+  constexpr int V = chunk::N, PAIRS = INTERLEAVED ? V / 2 : V;
+  const int per_token = a.lanes * a.units;
+  for (int i = threadIdx.x; i < a.block_tokens * per_token; i += blockDim.x) {
+    const int bt = i / per_token, r = i - bt * per_token;
+    const int lane = r / a.units, unit = r - lane * a.units;
+    const int64_t token = (int64_t)blockIdx.x * a.block_tokens + bt;
+    if (token >= a.tokens) return;
+    const bool copy = unit >= a.pair_units;
+    const int at = copy ? a.rot + (unit - a.pair_units) * V : unit * V;
+    const T *x = static_cast<const T *>(a.x) + token * a.xt + at;
+    T *out = static_cast<T *>(a.out) + token * a.ot + at;
+    const int half = a.rot / 2;
+    chunk p[kUnroll], q[kUnroll];
+    const auto load = [&](int h0) {
+#pragma unroll
+      for (int k = 0; k < kUnroll; ++k) {
+        const int h = h0 + k * a.lanes;
+        if (h >= a.heads) break;
+        p[k] = *reinterpret_cast<const chunk *>(x + h * a.xh);
+        if (!INTERLEAVED && !copy) q[k] = *reinterpret_cast<const chunk *>(x + h * a.xh + half);
+      }
+    };
+    load(lane);
+    float c[PAIRS], s[PAIRS];
+    if (!copy) {
+      const int64_t pos = position(a, token);
+      const bool good = (uint64_t)pos < (uint64_t)a.table_rows;
+      load_rotation<PAIRS, true>(a.table + (good ? pos * half + unit * PAIRS : 0), good, c, s);
+#pragma unroll
+      for (int k = 0; k < PAIRS; ++k) s[k] *= a.sign;
+    }
+    for (int h0 = lane; h0 < a.heads;) {
+#pragma unroll
+      for (int k = 0; k < kUnroll; ++k) {
+        const int h = h0 + k * a.lanes;
+        if (h >= a.heads) break;
+        if (!copy) {
+          float u[V], v[V];
+          unpack(p[k], u);
+          if (!INTERLEAVED) unpack(q[k], v);
+#pragma unroll
+          for (int e = 0; e < PAIRS; ++e) {
+            float &y = INTERLEAVED ? u[2 * e] : u[e], &z = INTERLEAVED ? u[2 * e + 1] : v[e];
+            const float y0 = y, z0 = z;
+            y = __fsub_rn(__fmul_rn(y0, c[e]), __fmul_rn(z0, s[e]));
+            z = __fadd_rn(__fmul_rn(z0, c[e]), __fmul_rn(y0, s[e]));
+          }
+          p[k] = packed<T>(u);
+          if (!INTERLEAVED) *reinterpret_cast<chunk *>(out + h * a.oh + half) = packed<T>(v);
+        }
+        *reinterpret_cast<chunk *>(out + h * a.oh) = p[k];
+      }
+      h0 += kUnroll * a.lanes;
+      load(h0);
+    }
+  }
+}
+
+// The same where 16-byte accesses do not fit: one pair, or one copied channel, of every lanes-th head.
+template <typename T> __global__ void __launch_bounds__(256) rope_narrow_kernel(const RopeArgs a, bool interleaved) {
   const int per_token = a.lanes * a.units;
   for (int i = threadIdx.x; i < a.block_tokens * per_token; i += blockDim.x) {
     const int bt = i / per_token, r = i - bt * per_token;
@@ -61,61 +125,29 @@ __global__ void __launch_bounds__(256) rope_kernel(const RopeArgs a) {
     const T *x = static_cast<const T *>(a.x) + token * a.xt;
     T *out = static_cast<T *>(a.out) + token * a.ot;
     if (unit >= a.pair_units) {
-      const int at = a.rot + (unit - a.pair_units) * V;
-      for (int h = lane; h < a.heads; h += a.lanes)
-        *reinterpret_cast<pack<T, V> *>(out + h * a.oh + at) =
-            *reinterpret_cast<const pack<T, V> *>(x + h * a.xh + at);
+      const int at = a.rot + unit - a.pair_units;
+      for (int h = lane; h < a.heads; h += a.lanes) out[h * a.oh + at] = x[h * a.xh + at];
       continue;
     }
-    const int64_t pos = a.wide_positions ? static_cast<const int64_t *>(a.positions)[token]
-                                         : (int64_t) static_cast<const int32_t *>(a.positions)[token];
-    float c[PAIRS], s[PAIRS];
-    if ((uint64_t)pos < (uint64_t)a.table_rows) {
-      const float2 *t = a.table + pos * (a.rot / 2) + unit * PAIRS;
-#pragma unroll
-      for (int k = 0; k < PAIRS; ++k) {
-        const float2 cs = __ldg(t + k);
-        c[k] = cs.x, s[k] = cs.y * a.sign;
-      }
-    } else {
-#pragma unroll
-      for (int k = 0; k < PAIRS; ++k) c[k] = s[k] = __int_as_float(0x7fc00000);
-    }
-    const int at = INTERLEAVED ? unit * PAIRS * 2 : unit * V;
-    const int apart = INTERLEAVED ? V : a.rot / 2;
-    // V == 1 interleaved: one pair, two single accesses
-    constexpr bool TWO = !INTERLEAVED || V == 1;
-    for (int h0 = lane; h0 < a.heads; h0 += kUnroll * a.lanes) {
-      pack<T, V> p[kUnroll], q[kUnroll];
-#pragma unroll
-      for (int k = 0; k < kUnroll; ++k) {
-        const int h = h0 + k * a.lanes;
-        if (h >= a.heads) break;
-        p[k] = *reinterpret_cast<const pack<T, V> *>(x + h * a.xh + at);
-        if (TWO) q[k] = *reinterpret_cast<const pack<T, V> *>(x + h * a.xh + at + apart);
-      }
-#pragma unroll
-      for (int k = 0; k < kUnroll; ++k) {
-        const int h = h0 + k * a.lanes;
-        if (h >= a.heads) break;
-#pragma unroll
-        for (int e = 0; e < PAIRS; ++e) {
-          T *pa = TWO ? &p[k].e[e] : &p[k].e[2 * e % V], *pb = TWO ? &q[k].e[e] : &p[k].e[(2 * e + 1) % V];
-          const float u = to_f32(*pa), v = to_f32(*pb);
-          *pa = from_f32<T>(__fsub_rn(__fmul_rn(u, c[e]), __fmul_rn(v, s[e])));
-          *pb = from_f32<T>(__fadd_rn(__fmul_rn(v, c[e]), __fmul_rn(u, s[e])));
-        }
-        *reinterpret_cast<pack<T, V> *>(out + h * a.oh + at) = p[k];
-        if (TWO) *reinterpret_cast<pack<T, V> *>(out + h * a.oh + at + apart) = q[k];
-      }
+    const int64_t pos = position(a, token);
+    const bool good = (uint64_t)pos < (uint64_t)a.table_rows;
+    float c[1], s[1];
+    load_rotation<1, false>(a.table + (good ? pos * (a.rot / 2) + unit : 0), good, c, s);
+    s[0] *= a.sign;
+    const int at = interleaved ? 2 * unit : unit, to = interleaved ? at + 1 : at + a.rot / 2;
+    for (int h = lane; h < a.heads; h += a.lanes) {
+      const float u = to_f32(x[h * a.xh + at]), v = to_f32(x[h * a.xh + to]);
+      out[h * a.oh + at] = from_f32<T>(__fsub_rn(__fmul_rn(u, c[0]), __fmul_rn(v, s[0])));
+      out[h * a.oh + to] = from_f32<T>(__fadd_rn(__fmul_rn(v, c[0]), __fmul_rn(u, s[0])));
     }
   }
 }
 
-template <typename T, int V> int launch_rope(RopeArgs a, int layout, bool in_place, cudaStream_t stream) {
+template <typename T> int launch_rope(RopeArgs a, int layout, bool in_place, bool wide, cudaStream_t stream) {
   const bool inter = layout == GAR_ROPE_INTERLEAVED;
-  a.pair_units = inter ? (V > 1 ? a.rot / V : a.rot / 2) : a.rot / 2 / V;
-  a.units = a.pair_units + (in_place ? 0 : (a.dim - a.rot) / V);
+  const int v = wide ? chunk16<T>::N : 1;
+  a.pair_units = inter && wide ? a.rot / v : a.rot / 2 / v;
+  a.units = a.pair_units + (in_place ? 0 : (a.dim - a.rot) / v);
   // Several heads to a thread once there are enough threads to fill the GPU without.
   const int64_t all = a.tokens * a.heads * a.units;
   a.lanes = all > (int64_t)152 * 2048 * 4 ? (a.heads + 3) / 4 : a.heads;
@@ -123,10 +155,12 @@ template <typename T, int V> int launch_rope(RopeArgs a, int layout, bool in_pla
   const int64_t blocks = (a.tokens + a.block_tokens - 1) / a.block_tokens;
   if (blocks > 0x7fffffff) return refuse("too many tokens");
   const int threads = std::min(256, (a.block_tokens * a.lanes * a.units + 31) / 32 * 32);
-  if (inter)
-    rope_kernel<T, V, true><<<(unsigned)blocks, threads, 0, stream>>>(a);
+  if (!wide)
+    rope_narrow_kernel<T><<<(unsigned)blocks, threads, 0, stream>>>(a, inter);
+  else if (inter)
+    rope_kernel<T, true><<<(unsigned)blocks, threads, 0, stream>>>(a);
   else
-    rope_kernel<T, V, false><<<(unsigned)blocks, threads, 0, stream>>>(a);
+    rope_kernel<T, false><<<(unsigned)blocks, threads, 0, stream>>>(a);
   return launched("rope_kernel");
 }
 
@@ -210,13 +244,13 @@ int gar_rope(const void *x, int64_t x_token_stride, int64_t x_head_stride, void 
   // The widest vector (16 bytes, else one element) that every address, half and remainder is a multiple of.
   const int v = 16 / size;
   const auto fits = [&](int64_t n) { return n % v == 0; };
-  const bool wide = (uintptr_t)x % 16 == 0 && (uintptr_t)out % 16 == 0 && fits(x_token_stride) && fits(x_head_stride) &&
+  const bool wide = (uintptr_t)x % 16 == 0 && (uintptr_t)table % 16 == 0 && (uintptr_t)out % 16 == 0 && fits(x_token_stride) && fits(x_head_stride) &&
                     fits(out_token_stride) && fits(out_head_stride) && fits(dim) &&
                     fits(layout == GAR_ROPE_HALF ? rot / 2 : rot);
   const cudaStream_t s = (cudaStream_t)stream;
   return with_float(dtype, [&](auto tag) {
     using T = typename decltype(tag)::type;
-    return wide ? launch_rope<T, 16 / sizeof(T)>(a, layout, in_place, s) : launch_rope<T, 1>(a, layout, in_place, s);
+    return launch_rope<T>(a, layout, in_place, wide, s);
   });
 }
 
