@@ -87,6 +87,16 @@ template <bool WIDE, typename T> __device__ __forceinline__ void store(T *p, int
   }
 }
 
+template <bool WIDE, typename T> __device__ __forceinline__ void store_codes(T *p, int from, int dim, const raw_chunk<T> &r) {
+  if (WIDE) {
+    *reinterpret_cast<raw_chunk<T> *>(p + from) = r;
+  } else {
+#pragma unroll
+    for (int k = 0; k < kChunk; ++k)
+      if (from + k < dim) reinterpret_cast<uint8_t *>(p)[from + k] = (uint8_t)(r.w[k / 4] >> 8 * (k % 4));
+  }
+}
+
 // The channels [from, from + kChunk) of a row rotated.  With the half layout the channels they
 // pair with are another lane's; they were read into w as well.
 template <bool WIDE, typename T>
@@ -133,23 +143,43 @@ __device__ __forceinline__ void rotate(const CacheArgs &a, const T *row, int64_t
   }
 }
 
-// The codes' values of a row of which this lane holds v, and its scale.
-template <typename C> __device__ __forceinline__ float quantise(float (&v)[kChunk], int lanes) {
-  float most = 0.f;
-  bool sound = true;
+// Codes of the row of which this lane holds v, and the row's scale.
+//
+// v / scale is rounded as the definition has it, without a division each: for r = 1 / scale rounded to
+// nearest and q = v r, the remainder v - q scale is exact in a fused multiply-add, and
+// q + r (v - q scale) is the correctly rounded quotient (P. Markstein, IBM J. Res. Dev. 34, 1990, theorem 8),
+// as long as nothing underflows; rows of scales under 2^-90 divide.
+template <typename C> __device__ __forceinline__ raw_chunk<C> quantise(const float (&v)[kChunk], int lanes, float *scale) {
+  // Magnitudes compare as integers, NaNs and infinities the largest.
+  uint32_t most = 0;
 #pragma unroll
-  for (int k = 0; k < kChunk; ++k) {
-    most = fmaxf(most, fabsf(v[k]));
-    sound &= fabsf(v[k]) <= 3.402823466e38f;
+  for (int k = 0; k < kChunk; ++k) most = max(most, __float_as_uint(v[k]) & 0x7fffffffu);
+  for (int d = lanes / 2; d > 0; d /= 2) most = max(most, __shfl_xor_sync(~0u, most, d));
+  raw_chunk<C> out;
+  float x[kChunk];
+  const float s = __fmul_rn(__uint_as_float(most), 1.f / quantised<C>::largest);
+  if (most >= 0x7f800000u) {  // an infinity or a NaN in the row: codes 0 under a NaN scale
+    *scale = __int_as_float(0x7fc00000);
+#pragma unroll
+    for (int k = 0; k < kChunk; ++k) x[k] = 0.f;
+  } else {
+    *scale = s;
+    const float r = __frcp_rn(s);
+    if (s >= 0x1p-90f) {
+#pragma unroll
+      for (int k = 0; k < kChunk; ++k) {
+        const float q = __fmul_rn(v[k], r);
+        x[k] = __fmaf_rn(__fmaf_rn(-q, s, v[k]), r, q);
+      }
+    } else {
+#pragma unroll
+      for (int k = 0; k < kChunk; ++k)
+        x[k] = s == 0.f ? 0.f : fminf(fmaxf(__fdiv_rn(v[k], s), -quantised<C>::largest), quantised<C>::largest);
+    }
   }
-  if (!sound) most = __int_as_float(0x7f800000);
-  for (int d = lanes / 2; d > 0; d /= 2) most = fmaxf(most, __shfl_xor_sync(~0u, most, d));
-  // An infinity or a NaN in the row: codes 0 under a NaN scale.
-  const bool bad = most > 3.402823466e38f;
-  const float scale = bad ? __int_as_float(0x7fc00000) : __fmul_rn(most, 1.f / quantised<C>::largest);
 #pragma unroll
-  for (int k = 0; k < kChunk; ++k) v[k] = bad || scale == 0.f ? 0.f : __fdiv_rn(v[k], scale);
-  return scale;
+  for (int k = 0; k < kChunk; k += 4) out.w[k / 4] = codes4(x[k], x[k + 1], x[k + 2], x[k + 3], C());
+  return out;
 }
 
 // T -> C rows.  a.lanes neighbouring lanes hold a token's row of one head, kChunk channels of the key
@@ -179,11 +209,15 @@ __global__ void __launch_bounds__(kThreads) write_kernel(const CacheArgs a) {
   Place p;
   const bool there = find(a, slot, head, &p);
   if (turned && there) rotate<WIDE>(a, k_row, token, from, k, w);
-  if (quantised<C>::value) {
-    const float k_scale = quantise<C>(k, a.lanes), v_scale = quantise<C>(v, a.lanes);
+  if constexpr (quantised<C>::value) {
+    float k_scale, v_scale;
+    const raw_chunk<C> k_codes = quantise<C>(k, a.lanes, &k_scale), v_codes = quantise<C>(v, a.lanes, &v_scale);
     if (there && lane == 0) c.k_scale[p.scale] = k_scale, c.v_scale[p.scale] = v_scale;
-  }
-  if (in && there) {
+    if (in && there) {
+      store_codes<WIDE>(static_cast<C *>(c.k) + p.at, from, c.dim, k_codes);
+      store_codes<WIDE>(static_cast<C *>(c.v) + p.at, from, c.dim, v_codes);
+    }
+  } else if (in && there) {
     store<WIDE>(static_cast<C *>(c.k) + p.at, from, c.dim, k);
     store<WIDE>(static_cast<C *>(c.v) + p.at, from, c.dim, v);
   }

@@ -2,13 +2,16 @@
 // among CTAs, and the join of partial results.
 //
 // Work.  An item is one sequence, one cached head and a group of up to kMaxGroup of the query heads
-// that read it.  Its rows are cut into units of 64 (more where the line would pass 2^31 units);
-// the items' units stand one behind the other in one line, and CTA i of N takes the i-th of
-// N equal shares of the line.  So every CTA has the same number of rows to read whatever the
-// lengths are, one long sequence is spread over the whole GPU, and thousands of short ones
-// are not split at all.  Where the line is longer than the CTAs are many, each item counts one
-// unit more, for what it costs beside its rows.  The lengths are read on the device: nothing waits for the
-// host, and a captured launch stays right when they change.
+// that read it.  The CTAs share the items' rows in one of two ways.
+//  * A segment each: every item is cut into parts of as many rows, the fewest (a multiple of 64) for which
+//    there are no more parts than CTAs.  Taken for up to 32 sequences where no part is over 5/4 of an equal
+//    share.  It leaves a CTA one segment to start and to join.
+//  * A line: the items' rows, in units of 64 (more where the line would pass 2^30 units), stand one
+//    behind the other, and CTA i of N takes the i-th of N equal shares.  So every CTA has the same number
+//    of rows to read whatever the lengths are, and thousands of short sequences are not split at all.  Each item
+//    counts one unit more, for what it costs beside its rows.
+// The lengths are read on the device: nothing waits for the host, and a captured launch stays
+// right when they change.
 //
 // Join.  A segment is the part of an item that one CTA takes.  Each keeps the running maximum m
 // of the scores (in units of log 2), l = sum 2^(score - m) and o = sum 2^(score - m) v.  Where an
@@ -33,7 +36,7 @@ struct DecodeArgs {
   const int32_t *table, *lengths;
   Divide page;
   int most_rows;           // rows that the table's width can hold
-  int unit_shift;          // rows of a unit: 1 << unit_shift
+  int unit;                // rows of a unit of the line
   int box_rows;            // rows of a tensor copy
   int batch, q_heads, group, item_groups, item_heads;  // group: q_heads / kv_heads
   int q_dtype, out_dtype, window;
@@ -51,7 +54,8 @@ struct Span {
   int lo, hi, base;        // rows [lo, hi); base: lo rounded down to a multiple of 32
 };
 
-__device__ __forceinline__ Span span_of(const DecodeArgs &a, int n) {
+// The span of a length, in units of `unit` rows.
+__device__ __forceinline__ Span span_of(const DecodeArgs &a, int n, int unit) {
   Span s;
   if (n < 0 || n > a.most_rows) {
     if (a.c.status) atomicOr(a.c.status, GAR_KV_BAD_LENGTH);
@@ -60,89 +64,88 @@ __device__ __forceinline__ Span span_of(const DecodeArgs &a, int n) {
   s.hi = n;
   s.lo = a.window > 0 && n > a.window ? n - a.window : 0;
   s.base = s.lo & ~31;
-  s.units = max(1, (s.hi - s.base + (1 << a.unit_shift) - 1) >> a.unit_shift);
+  s.units = max(1, (int)(((unsigned)(s.hi - s.base) + unit - 1) / (unsigned)unit));
   return s;
 }
 
-// Rows [max(lo, from), to) of one item.
+// Rows [lo, to) of one item.
 struct Segment {
   int b, kv_head, head, heads;  // head: the first of the item's query heads
-  int lo, from, to;             // from is a multiple of 32
+  int lo, from, to;             // from: lo rounded down to a multiple of 32
   bool whole;
   int slot;                     // where the partial result goes
   int first, parts;             // the item's CTAs
   bool first_late;              // the first of them begins before the item does
 };
 
-// Walks one CTA's share.  All threads hold the same state.
+// Walks one CTA's share.
 struct Walk {
   int pos, end, per;
   int item;                     // where in the line the item at pos begins
-  int b, hh, lead;
-  int ahead;                    // length of sequence b + 1
+  int b, hh, lead, unit;        // unit: rows
   bool first_segment;
   Span s;
 
-  __device__ __forceinline__ int length(const DecodeArgs &a, int i) const { return i < a.batch ? a.lengths[i] : 0; }
-
-  template <int THREADS> __device__ __forceinline__ void start(const DecodeArgs &a) {
-    // Each thread adds up a run of sequences, a scan over the threads follows, and the thread
-    // whose run holds the share's start looks it up.
-    __shared__ int sums[THREADS / 32];
-    __shared__ int found_item, found_b;
-    const int per_thread = (a.batch + THREADS - 1) / THREADS;
-    const int b0 = min(a.batch, (int)threadIdx.x * per_thread), b1 = min(a.batch, b0 + per_thread);
-    const int items = a.c.heads * a.item_groups;
-    int mine = 0;
-    for (int i = b0; i < b1; ++i) mine += span_of(a, a.lengths[i]).units;
-    int scan = mine;
+  // By each warp on its own: a lane adds up a run of sequences, a scan over the lanes follows, and
+  // the lane whose run holds the share's start looks it up.
+  __device__ __forceinline__ void start(const DecodeArgs &a) {
+    const int lane = threadIdx.x & 31, run = (a.batch + 31) / 32;
+    const int b0 = min(a.batch, lane * run), b1 = min(a.batch, b0 + run);
+    const int items = a.c.heads * a.item_groups, ctas = gridDim.x;
+    unit = a.unit;
+    int mine = 0, n = 0;
+    for (int i = b0; i < b1; ++i) mine += span_of(a, n = a.lengths[i], unit).units;
+    int total = __reduce_add_sync(~0u, mine);
+    lead = 1;
+    const int share = (total * items + ctas - 1) / ctas;  // in units; a part has no fewer
+    if (run <= 1 && a.batch * items <= ctas) {
+      for (int u = share; u <= share + share / 4 && u <= (1 << 30) / a.unit; u += max(1, share / 16)) {
+        const int parts = b0 < b1 ? span_of(a, n, u * a.unit).units : 0, all = __reduce_add_sync(~0u, parts);
+        if (all * items <= ctas) {
+          unit = u * a.unit, lead = 0, mine = parts, total = all;
+          break;
+        }
+      }
+    }
+    total = (total + lead * a.batch) * items, mine = (mine + lead * (b1 - b0)) * items;
+    int before = mine;
 #pragma unroll
     for (int d = 1; d < 32; d *= 2) {
-      const int up = __shfl_up_sync(~0u, scan, d);
-      if ((threadIdx.x & 31) >= d) scan += up;
+      const int up = __shfl_up_sync(~0u, before, d);
+      if (lane >= d) before += up;
     }
-    if ((threadIdx.x & 31) == 31) sums[threadIdx.x / 32] = scan;
-    __syncthreads();
-    int before = scan - mine, total = 0;
-#pragma unroll
-    for (int w = 0; w < THREADS / 32; ++w) {
-      if (w < threadIdx.x / 32) before += sums[w];
-      total += sums[w];
-    }
-    lead = total * items > (int)gridDim.x ? 1 : 0;
-    total = (total + lead * a.batch) * items;
-    before = (before + lead * b0) * items, mine = (mine + lead * (b1 - b0)) * items;
-    per = (total + gridDim.x - 1) / gridDim.x;
+    before -= mine;
+    per = (total + ctas - 1) / ctas;
     pos = min(total, (int)blockIdx.x * per);
     end = min(total, pos + per);
-    if (pos >= before && pos < before + mine) {
-      int i = b0;
-      for (; i < b1; ++i) {
-        const int n = (span_of(a, a.lengths[i]).units + lead) * items;
-        if (pos < before + n) break;
-        before += n;
-      }
-      found_b = i, found_item = before;
-    }
-    __syncthreads();
     if (pos >= end) return;
-    enter(a, found_b, a.lengths[found_b]);
-    hh = (pos - found_item) / s.units;
-    item = found_item + hh * s.units;
+    int i = b0;
+    const bool here = pos >= before && pos < before + mine;
+    if (here)
+      for (; i < b1; ++i) {
+        n = a.lengths[i];
+        const int units = (span_of(a, n, unit).units + lead) * items;
+        if (pos < before + units) break;
+        before += units;
+      }
+    const int from = __ffs(__ballot_sync(~0u, here)) - 1;
+    before = __shfl_sync(~0u, before, from);
+    enter(a, __shfl_sync(~0u, i, from), __shfl_sync(~0u, n, from));
+    hh = (pos - before) / s.units;
+    item = before + hh * s.units;
     first_segment = true;
   }
 
   __device__ __forceinline__ void enter(const DecodeArgs &a, int sequence, int n) {
     b = sequence;
-    s = span_of(a, n);
+    s = span_of(a, n, unit);
     s.units += lead;
-    ahead = length(a, b + 1);
   }
 
   __device__ __forceinline__ bool next(const DecodeArgs &a, Segment *g) {
     if (pos >= end) return false;
     if (!first_segment) {
-      if (++hh == a.c.heads * a.item_groups) hh = 0, enter(a, b + 1, ahead);
+      if (++hh == a.c.heads * a.item_groups) hh = 0, enter(a, b + 1, a.lengths[b + 1]);
       item = pos;
     }
     const int u = pos - item, n = min(s.units - u, end - pos);
@@ -151,8 +154,8 @@ struct Walk {
     const int sub = (hh - g->kv_head * a.item_groups) * a.item_heads;
     g->head = g->kv_head * a.group + sub;
     g->heads = min(a.item_heads, a.group - sub);
-    g->from = s.base + (max(0, u - lead) << a.unit_shift);
-    g->to = min(s.hi, s.base + (max(0, u + n - lead) << a.unit_shift));
+    g->from = s.base + max(0, u - lead) * unit;
+    g->to = (int)min((unsigned)s.hi, (unsigned)s.base + (unsigned)max(0, u + n - lead) * unit);
     g->lo = max(s.lo, g->from);
     g->whole = n == s.units;
     g->first = blockIdx.x, g->parts = 1, g->slot = 0, g->first_late = false;
@@ -233,91 +236,116 @@ template <int WARPS> struct JoinShared {
   int at[WARPS];                   // where in shared memory its o begins, in floats
   float weight[WARPS][kMaxGroup];  // 2^(m_w - m)
   float l[WARPS][kMaxGroup];       // l of the join that begins with this warp
-  float m[kMaxGroup];
-  bool last;
+  bool last[WARPS];
 };
 
-// Joins the (m, l, o) of `count` warps from `first` on, by the `threads` threads that
-// call it, and writes the item's output, or the segment's partial result.
-// Warp w holds head h's o at o[at[w] + h * row], 16-byte aligned.
-template <int WARPS, typename Barrier>
-__device__ __forceinline__ void join_warps(const DecodeArgs &a, const Segment &g, JoinShared<WARPS> &sh, const float *o, int row,
-                                           int first, int count, int thread, int threads, Barrier barrier) {
-  barrier();
-  if (thread < g.heads) {
-    const int h = thread;
-    float m = -INFINITY, l = 0.f;
-    for (int w = first; w < first + count; ++w) m = fmaxf(m, sh.ml[w][h].x);
-    for (int w = first; w < first + count; ++w) {
-      const float f = exp2_fast(sh.ml[w][h].x - offset_of(m));
-      sh.weight[w][h] = f;
-      l += f * sh.ml[w][h].y;
-    }
-    sh.l[first][h] = l;
-    if (g.whole)
-      store_lse(a, g, h, m, l);
+// `count` warps from `first` on that work on one segment.  Groups of a size are of the same warps
+// (one warp apart), so the size can name the barrier.
+struct Group {
+  int first, count;
+  __device__ __forceinline__ void sync() const {
+    if (count == 1)
+      __syncwarp();
     else
-      a.part_ml[g.slot * kMaxGroup + h] = make_float2(m, l);
+      asm volatile("bar.sync %0, %1;" ::"r"(count), "r"(32 * count) : "memory");
   }
-  barrier();
+  __device__ __forceinline__ int thread() const { return threadIdx.x - 32 * first; }
+};
+
+// Joins the (m, l, o) of a group's warps and writes the item's output, or the segment's partial
+// result.  Warp w holds head h's o at o[at[w] + h * row], 16-byte aligned.
+template <int WARPS>
+__device__ __forceinline__ void join_warps(const DecodeArgs &a, const Segment &g, Group group, JoinShared<WARPS> &sh,
+                                           const float *o, int row) {
+  static_assert(WARPS <= 16, "16 lanes hold a head's warps");
+  const int thread = group.thread(), threads = 32 * group.count;
+  group.sync();
+  for (int i = thread; i - (int)(threadIdx.x & 31) < g.heads * 16; i += threads) {
+    const int h = i / 16, w = i & 15;
+    const float2 v = w < group.count && h < g.heads ? sh.ml[group.first + w][h] : make_float2(-INFINITY, 0.f);
+    float m = v.x;
+#pragma unroll
+    for (int d = 8; d > 0; d /= 2) m = fmaxf(m, __shfl_xor_sync(~0u, m, d));
+    const float f = exp2_fast(v.x - offset_of(m));
+    float l = f * v.y;
+#pragma unroll
+    for (int d = 8; d > 0; d /= 2) l += __shfl_xor_sync(~0u, l, d);
+    if (h < g.heads) {
+      if (w < group.count) sh.weight[group.first + w][h] = f;
+      if (w == 0) {
+        sh.l[group.first][h] = l;
+        if (g.whole)
+          store_lse(a, g, h, m, l);
+        else
+          a.part_ml[g.slot * kMaxGroup + h] = make_float2(m, l);
+      }
+    }
+  }
+  group.sync();
   const int columns = (a.c.dim + 3) / 4;
   for (int i = thread; i < g.heads * columns; i += threads) {
     const int h = i / columns, d = (i - h * columns) * 4;
     float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
-    for (int w = first; w < first + count; ++w) {
+#pragma unroll 4
+    for (int w = group.first; w < group.first + group.count; ++w) {
       const float f = sh.weight[w][h];
       const float4 y = *reinterpret_cast<const float4 *>(o + sh.at[w] + h * row + d);
       x.x += f * y.x, x.y += f * y.y, x.z += f * y.z, x.w += f * y.w;
     }
     if (g.whole)
-      store_out4(a, g, h, d, x, sh.l[first][h]);
+      store_out4(a, g, h, d, x, sh.l[group.first][h]);
     else
       *reinterpret_cast<float4 *>(a.part_o + (int64_t)(g.slot * kMaxGroup + h) * a.dim_pad + d) = x;
   }
-  barrier();
+  group.sync();
 }
 
-// After join_warps by the whole CTA: where the item has several parts, the last CTA to get here
-// joins them.  A lane for each part finds the maximum; then every thread has the loads of 8 parts
-// in flight (a long sequence alone has some 20 parts of 4 KB for each cached head).
+// After join_warps: where the item has several parts, the last group to get here joins them, 8 parts' loads in flight a thread (a long sequence alone has some 20 parts of 4 KB for
+// each cached head).
 template <int WARPS>
-__device__ __forceinline__ void join_parts(const DecodeArgs &a, const Segment &g, JoinShared<WARPS> &sh) {
-  __threadfence();
-  __syncthreads();
-  // The counter returns to zero with the last arrival.
-  if (threadIdx.x == 0) sh.last = atomicInc(a.count + g.first, g.parts - 1) == (unsigned)g.parts - 1;
-  __syncthreads();
-  if (sh.last) {
+__device__ __forceinline__ void join_parts(const DecodeArgs &a, const Segment &g, Group group, JoinShared<WARPS> &sh) {
+  if (group.thread() == 0) {
+    __threadfence();  // after join_warps' barrier: what the group has stored is seen before the count
+    // The counter returns to zero with the last arrival.
+    sh.last[group.first] = atomicInc(a.count + g.first, g.parts - 1) == (unsigned)g.parts - 1;
     __threadfence();
-    const int warp = threadIdx.x / 32, lane = threadIdx.x & 31;
-    for (int h = warp; h < g.heads; h += WARPS) {
-      float m = -INFINITY;
-      for (int p = lane; p < g.parts; p += 32) m = fmaxf(m, __ldcg(a.part_ml + slot_of(g, p) * kMaxGroup + h).x);
-#pragma unroll
-      for (int d = 16; d > 0; d /= 2) m = fmaxf(m, __shfl_xor_sync(~0u, m, d));
-      if (lane == 0) sh.m[h] = m;
-    }
-    __syncthreads();
+  }
+  group.sync();
+  if (sh.last[group.first]) {
+    constexpr int N = 8;
     const int columns = (a.c.dim + 3) / 4;
-    for (int i = threadIdx.x; i < g.heads * columns; i += 32 * WARPS) {
+    for (int i = group.thread(); i < g.heads * columns; i += 32 * group.count) {
       const int h = i / columns, d = (i - h * columns) * 4;
-      const float m = sh.m[h], off = offset_of(m);
-      float l = 0.f;
+      float m = -INFINITY, l = 0.f;
       float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll 8
-      for (int p = 0; p < g.parts; ++p) {
-        const int at = slot_of(g, p) * kMaxGroup + h;
-        const float2 v = __ldcg(a.part_ml + at);
-        const float4 y = __ldcg(reinterpret_cast<const float4 *>(a.part_o + (int64_t)at * a.dim_pad + d));
-        const float f = exp2_fast(v.x - off);
-        l += f * v.y;
-        x.x += f * y.x, x.y += f * y.y, x.z += f * y.z, x.w += f * y.w;
+      for (int p0 = 0; p0 < g.parts; p0 += N) {
+        float2 v[N];
+        float4 y[N];
+        float top = m;
+#pragma unroll
+        for (int k = 0; k < N; ++k) {
+          const int at = slot_of(g, min(p0 + k, g.parts - 1)) * kMaxGroup + h;
+          v[k] = __ldcg(a.part_ml + at);
+          y[k] = __ldcg(reinterpret_cast<const float4 *>(a.part_o + (int64_t)at * a.dim_pad + d));
+        }
+#pragma unroll
+        for (int k = 0; k < N; ++k) top = fmaxf(top, v[k].x);
+        const float off = offset_of(top), shrink = exp2_fast(m - off);
+        m = top, l *= shrink;
+        x.x *= shrink, x.y *= shrink, x.z *= shrink, x.w *= shrink;
+#pragma unroll
+        for (int k = 0; k < N; ++k)
+          if (p0 + k < g.parts) {
+            const float f = exp2_fast(v[k].x - off);
+            l += f * v[k].y;
+            x.x += f * y[k].x, x.y += f * y[k].y, x.z += f * y[k].z, x.w += f * y[k].w;
+          }
       }
       store_out4(a, g, h, d, x, l);
       if (d == 0) store_lse(a, g, h, m, l);
     }
   }
-  __syncthreads();
+  group.sync();
 }
 
 int decode_general(const DecodeArgs &a, int sms, cudaStream_t stream);

@@ -156,9 +156,9 @@ int gar_decode_attention(gar_attn_plan *plan, const gar_kv_cache *cache, const v
   // Units as large as it takes for the whole line to stay below 2^30 of them.
   const int64_t items = (int64_t)batch * plan->kv_heads * ((a.group + 7) / 8);
   if (items >= 1 << 28) return refuse("too many sequences and heads");
-  a.unit_shift = 6;
-  while (items * ((a.most_rows >> a.unit_shift) + 3) >= 1 << 30) ++a.unit_shift;
-  if (a.unit_shift > 15) return refuse("too many sequences and heads for tables this wide");
+  a.unit = 64;
+  while (items * (a.most_rows / a.unit + 3) >= 1 << 30) a.unit *= 2;
+  if (a.unit > 32768) return refuse("too many sequences and heads for tables this wide");
   const cudaStream_t s = (cudaStream_t)stream;
   if (!takes_mma(*cache, q, q_batch_stride, q_head_stride, q_dtype)) return decode_general(a, plan->sms, s);
   switch (cache->dtype) {

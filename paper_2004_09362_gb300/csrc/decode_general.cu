@@ -23,7 +23,8 @@ template <typename T, int J> __global__ void __launch_bounds__(kThreads) general
   const int row = lane / 8, head = lane & 7;
   const int o_row = J * 32;
   Walk walk;
-  walk.start<kThreads>(a);
+  walk.start(a);
+  const Group group{0, kWarps};
   if (lane == 0) join.at[warp] = warp * kHeads * o_row;
   Segment g;
   while (walk.next(a, &g)) {
@@ -115,8 +116,8 @@ template <typename T, int J> __global__ void __launch_bounds__(kThreads) general
     for (int h = 0; h < kHeads; ++h)
 #pragma unroll
       for (int j = 0; j < J; ++j) o_shared[(warp * kHeads + h) * o_row + lane + 32 * j] = o[h][j];
-    join_warps(a, g, join, o_shared, o_row, 0, kWarps, threadIdx.x, kThreads, [] { __syncthreads(); });
-    if (!g.whole) join_parts(a, g, join);
+    join_warps(a, g, group, join, o_shared, o_row);
+    if (!g.whole) join_parts(a, g, group, join);
   }
 }
 

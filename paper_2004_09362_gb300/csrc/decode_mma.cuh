@@ -22,7 +22,7 @@
 //    a tile's tensor copies; pages whose rows do not come in eights are copied by cp.async, which
 //    costs some 300 instructions a tile for the addresses.
 //  * The warps of a CTA take a segment's tiles in turn and join at its end; an item of at most
-//    kSolo tiles goes to one warp whole, so that short sequences need no barrier at all.
+//    kSolo tiles goes to one warp whole, so that short sequences need no barrier.
 //
 // 8-bit codes become f16, exactly; a row's key scale multiplies its scores, its value scale
 // its weight, taken relative to the largest value scale so far so that the weights stay in f16's
@@ -148,8 +148,10 @@ template <typename C, int DP, int NG> struct MmaShape {
   static constexpr int PARTS = DP * EL / LINE;
   static constexpr int KT = DP * EL <= 128 ? 32 : 16;              // rows of a tile
   static constexpr int kTile = 2 * KT * DP * EL;                   // bytes, keys and values
-  static constexpr int kStages = kTile > 4096 ? 3 : 6;
-  static constexpr int kWarps = kTile > 8192 ? 4 : 8;              // one CTA per SM
+  // One CTA per SM; its 192 KB of tiles are divided among as many warps as the registers allow.
+  static constexpr int kWarps = kTile > 8192 ? 4 : NG == 1 && DP <= 128 ? 12 : 8;
+  static constexpr int kStages = 196608 / kWarps / kTile;
+  static_assert(kStages >= 2, "a tile in use and one on its way");
   static constexpr int kScales = Q8 ? 2 * KT * 4 : 0;
   // Floats of an o row; a row of o for each head fits a stage.  A few floats more than DP spread
   // the rows over the banks.
@@ -170,24 +172,13 @@ template <int LINE> __device__ __forceinline__ int place(int r, int c) {
   return r * LINE + (LINE == 128 ? c ^ (r & 7) : c ^ (r / 2 & 3)) * 16;
 }
 
-// One warp's way through its CTA's segments, tile by tile.
-template <typename S> struct Tiles {
-  Walk walk;
+// A segment that a warp has to do with, and which of its tiles are the warp's.
+struct Work {
   Segment seg;
-  int ordinal, tile, step, tiles;
-  bool alone, mine;  // alone: the segment is one warp's; mine: this warp has to do with it
-
-  __device__ __forceinline__ bool next(const DecodeArgs &a, int warp) {
-    if (!walk.next(a, &seg)) return false;
-    tiles = (max(0, seg.to - seg.from) + S::KT - 1) / S::KT;
-    alone = seg.whole && tiles <= kSolo;
-    mine = !alone || ordinal % S::kWarps == warp;
-    if (!mine) tiles = 0;
-    tile = alone ? 0 : warp, step = alone ? 1 : S::kWarps;
-    ++ordinal;
-    return true;
-  }
+  Group group;
+  int tile, step, tiles;
 };
+constexpr int kAhead = 4;  // segments that a warp's copies can be ahead
 
 template <typename C, int DP, int NG, bool BOXES>
 __global__ void __launch_bounds__(32 * MmaShape<C, DP, NG>::kWarps, 1)
@@ -213,86 +204,119 @@ __global__ void __launch_bounds__(32 * MmaShape<C, DP, NG>::kWarps, 1)
     asm volatile("mbarrier.init.shared::cta.b64 [%0], 1; fence.mbarrier_init.release.cluster;" ::"r"(barrier + 8 * lane) : "memory");
   __syncwarp();
 
-  Tiles<S> get;   // copies, kStages - 1 tiles ahead of
-  get.walk.template start<32 * W>(a);
-  get.ordinal = get.tile = get.tiles = 0;
-  Tiles<S> use = get;
-  bool more = get.next(a, warp);
-  int page = -1;  // of this lane's row of get's tile, fetched one tile before it is needed
-
-  const auto fetch_page = [&] {
-    while (more && get.tile >= get.tiles) more = get.next(a, warp);
+  // The copies' side of this warp: it walks the segments, notes in `works` those that the warp has to do
+  // with, and copies their tiles.
+  __shared__ Walk walks[W];
+  __shared__ Work works[W][kAhead];
+  Walk &walk = walks[warp];
+  {
+    Walk w;
+    w.start(a);
+    if (lane == 0) walk = w;
+    __syncwarp();
+  }
+  int noted = 0, done = 0, ordinal = 0;  // works noted and done; segments walked
+  struct {
+    int from, lo, to, b, kv_head, tile, step, tiles;
+  } get{};
+  bool walking = true, ready = false;    // ready: get's tile exists and its pages are known
+  int page = -1;                         // of this lane's row of get's tile
+  const auto advance = [&] {
+    while (get.tile >= get.tiles && walking && noted - done < kAhead) {
+      Walk w = walk;
+      Work x;
+      __syncwarp();
+      if (!(walking = w.next(a, &x.seg))) break;
+      const int tiles = (max(0, x.seg.to - x.seg.from) + KT - 1) / KT;
+      // Few tiles of a whole item, or hardly any: one warp's, in turn.  Else tile by tile the warps'.
+      const bool alone = tiles <= (x.seg.whole ? kSolo : 1);
+      x.group = alone ? Group{ordinal % W, 1} : Group{0, min(W, tiles)};
+      x.tile = alone ? 0 : warp, x.step = alone ? 1 : W;
+      const bool mine = warp >= x.group.first && warp < x.group.first + x.group.count;
+      x.tiles = mine ? tiles : 0;
+      ++ordinal;
+      if (lane == 0) {
+        walk = w;
+        if (mine) works[warp][noted % kAhead] = x;
+      }
+      __syncwarp();
+      noted += mine;
+      get = {x.seg.from, x.seg.lo, x.seg.to, x.seg.b, x.seg.kv_head, x.tile, x.step, x.tiles};
+    }
+    ready = get.tile < get.tiles;
     page = -1;
-    if (more) {
-      const int n = get.seg.from + get.tile * KT + (lane & (KT - 1));
-      if (n >= get.seg.lo && n < get.seg.to) page = a.table[get.seg.b * a.table_stride + a.page(n)];
+    if (ready) {
+      const int n = get.from + get.tile * KT + (lane & (KT - 1));
+      if (n >= get.lo && n < get.to) page = a.table[get.b * a.table_stride + a.page(n)];
     }
   };
   // Starts the copies of get's tile.
   const auto issue = [&](int stage) {
-    if (more) {
-      const int n = get.seg.from + get.tile * KT + (lane & (KT - 1)), r = n - (int)a.page(n) * c.page_size;
-      const bool there = n >= get.seg.lo && n < get.seg.to && (unsigned)page < (uint64_t)c.pages;
-      if (n >= get.seg.lo && n < get.seg.to && !there && c.status) atomicOr(c.status, GAR_KV_BAD_PAGE);
-      const uint32_t tile_at = mine_at + stage * S::kTile;
-      if (Q8 && lane < KT) {
-        const int64_t at = there ? page * c.scale_page_stride + r * c.scale_token_stride +
-                                       get.seg.kv_head * c.scale_head_stride : 0;
-        const uint32_t to = scales_at + stage * S::kScales + lane * 4;
-        copy_async<4>(to, c.k_scale + at, there);
-        copy_async<4>(to + KT * 4, c.v_scale + at, there);
-      }
-      if constexpr (BOXES) {
-        // A box is a.box_rows rows of one page (those outside the segment too).  A page that no
-        // row of the segment is on has number -1 here and is filled with zeros.
-        const uint32_t bar = barrier + 8 * stage;
-        if (lane == 0)
-          asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(S::kTile) : "memory");
-        for (int r0 = 0; r0 < KT; r0 += a.box_rows) {
-          const unsigned some = __ballot_sync(~0u, there && (lane & (KT - 1)) / a.box_rows * a.box_rows == r0);
-          const int p = __shfl_sync(~0u, page, some ? __ffs(some) - 1 : 0), row = __shfl_sync(~0u, r, r0);
-          if (lane == 0) {
+    const int n = get.from + get.tile * KT + (lane & (KT - 1)), r = n - (int)a.page(n) * c.page_size;
+    const bool there = n >= get.lo && n < get.to && (unsigned)page < (uint64_t)c.pages;
+    if (n >= get.lo && n < get.to && !there && c.status) atomicOr(c.status, GAR_KV_BAD_PAGE);
+    const uint32_t tile_at = mine_at + stage * S::kTile;
+    if (Q8 && lane < KT) {
+      const int64_t at = there ? page * c.scale_page_stride + r * c.scale_token_stride +
+                                     get.kv_head * c.scale_head_stride : 0;
+      const uint32_t to = scales_at + stage * S::kScales + lane * 4;
+      copy_async<4>(to, c.k_scale + at, there);
+      copy_async<4>(to + KT * 4, c.v_scale + at, there);
+    }
+    if constexpr (BOXES) {
+      // A box is a.box_rows rows of one page (those outside the segment too).  A page that no
+      // row of the segment is on has number -1 here and is filled with zeros.
+      const uint32_t bar = barrier + 8 * stage;
+      if (lane == 0)
+        asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(S::kTile) : "memory");
+      for (int r0 = 0; r0 < KT; r0 += a.box_rows) {
+        const unsigned some = __ballot_sync(~0u, there && (lane & (KT - 1)) / a.box_rows * a.box_rows == r0);
+        const int p = __shfl_sync(~0u, page, some ? __ffs(some) - 1 : 0), row = __shfl_sync(~0u, r, r0);
+        if (lane == 0) {
 #pragma unroll
-            for (int i = 0; i < PARTS; ++i) {
-              const uint32_t to = tile_at + (i * KT + r0) * LINE;
-              copy_box(to, &k_map, i * LINE, row, get.seg.kv_head, some ? p : -1, bar);
-              copy_box(to + KT * DP * EL, &v_map, i * LINE, row, get.seg.kv_head, some ? p : -1, bar);
-            }
+          for (int i = 0; i < PARTS; ++i) {
+            const uint32_t to = tile_at + (i * KT + r0) * LINE;
+            copy_box(to, &k_map, i * LINE, row, get.kv_head, some ? p : -1, bar);
+            copy_box(to + KT * DP * EL, &v_map, i * LINE, row, get.kv_head, some ? p : -1, bar);
           }
         }
-        get.tile += get.step;
-        fetch_page();
+      }
       } else {
-        const int64_t at =
-            there ? (page * c.page_stride + get.seg.kv_head * c.head_stride + r * c.token_stride) * EL : -1;
-        get.tile += get.step;
-        fetch_page();
+      const int64_t at =
+          there ? (page * c.page_stride + get.kv_head * c.head_stride + r * c.token_stride) * EL : -1;
         constexpr int LANES = LINE / 16, ROWS = 32 / LANES;
-        const char *const kp = static_cast<const char *>(c.k), *const vp = static_cast<const char *>(c.v);
-        const int chunk = lane & (LANES - 1);
+      const char *const kp = static_cast<const char *>(c.k), *const vp = static_cast<const char *>(c.v);
+      const int chunk = lane & (LANES - 1);
 #pragma unroll
-        for (int r = 0; r < KT; r += ROWS) {
-          const int row = r + lane / LANES;
-          const int64_t x = __shfl_sync(~0u, at, row);
+      for (int r = 0; r < KT; r += ROWS) {
+        const int row = r + lane / LANES;
+        const int64_t x = __shfl_sync(~0u, at, row);
 #pragma unroll
-          for (int p = 0; p < PARTS; ++p) {
-            const int off = p * LINE + chunk * 16;
-            const bool in = x >= 0 && off < c.dim * EL;
-            const uint32_t to = tile_at + p * KT * LINE + place<LINE>(row, chunk);
-            copy_async<16>(to, in ? kp + x + off : kp, in);
-            copy_async<16>(to + KT * DP * EL, in ? vp + x + off : vp, in);
-          }
+        for (int p = 0; p < PARTS; ++p) {
+          const int off = p * LINE + chunk * 16;
+          const bool in = x >= 0 && off < c.dim * EL;
+          const uint32_t to = tile_at + p * KT * LINE + place<LINE>(row, chunk);
+          copy_async<16>(to, in ? kp + x + off : kp, in);
+          copy_async<16>(to + KT * DP * EL, in ? vp + x + off : vp, in);
         }
       }
     }
     if (Q8 || !BOXES) asm volatile("cp.async.commit_group;" ::: "memory");
+    get.tile += get.step;
+    advance();
+  };
+  int in = 0, out = 0, flying = 0;  // stages copied into and used next; tiles on their way or here
+  uint32_t parity = 0;
+  const auto pump = [&](int most) {
+    while (flying < most) {
+      if (!ready) advance();
+      if (!ready) break;
+      issue(in);
+      if (++in == S::kStages) in = 0;
+      ++flying;
+    }
   };
 
-  fetch_page();
-#pragma unroll
-  for (int s = 0; s < S::kStages - 1; ++s) issue(s);
-  int stage = 0;  // the next tile's; the one before it is free
-  uint32_t parity = 0;
   // This lane's places in a tile: rows g and g + 8 of the scores, rows 2t and 2t + 1 of the values.
   const int k_at = place<LINE>(key_row<LINE>(g), t);
   int v_at[2];
@@ -300,23 +324,31 @@ __global__ void __launch_bounds__(32 * MmaShape<C, DP, NG>::kWarps, 1)
   for (int i = 0; i < 2; ++i)
     v_at[i] = KT * DP * EL + place<LINE>(key_row<LINE>(2 * t + i), VB == 16 ? g : g / 2) + (VB == 16 ? 0 : (g & 1) * 8);
 
-  while (use.next(a, warp)) {
-    if (!use.mine) continue;
-    const Segment &seg = use.seg;
-    // Queries: head g (+ 8 ng), the channels of this lane's chunks, two to a register.
-    uint32_t qf[NG][DP / 8];
-    float q_scale[NG][2];
+  // Queries: head g (+ 8 ng), the channels of this lane's chunks, two to a register.
+  uint32_t qf[NG][DP / 8];
+  const auto load_queries = [&] {
+    const Segment &seg = works[warp][done % kAhead].seg;
+    const char *const q0 = static_cast<const char *>(a.q) + 2 * (seg.b * a.qb + (seg.head + g) * a.qh);
 #pragma unroll
     for (int ng = 0; ng < NG; ++ng) {
       const bool there = g + 8 * ng < seg.heads;
-      const uint4 *q = reinterpret_cast<const uint4 *>(static_cast<const char *>(a.q) +
-                                                      2 * (seg.b * a.qb + (seg.head + g + 8 * ng) * a.qh));
+      const uint4 *q = reinterpret_cast<const uint4 *>(q0 + 2 * 8 * ng * a.qh);
 #pragma unroll
       for (int k = 0; k < DP / 32; ++k) {
         const int at = Q8 ? (t + 4 * (k / 2)) * 2 + k % 2 : t + 4 * k;  // 8 channels each
         const uint4 x = there && at * 8 < c.dim ? q[at] : make_uint4(0, 0, 0, 0);
         qf[ng][4 * k] = x.x, qf[ng][4 * k + 1] = x.y, qf[ng][4 * k + 2] = x.z, qf[ng][4 * k + 3] = x.w;
       }
+    }
+  };
+
+  advance();
+  if (noted) load_queries();
+  pump(S::kStages - 1);
+  while (done < noted) {
+    float q_scale[NG][2];
+#pragma unroll
+    for (int ng = 0; ng < NG; ++ng) {
       // bf16 queries become f16 relative to the power of two at their largest
       float up = 1.f;
       if (Q8 && a.q_dtype == GAR_BF16) {
@@ -344,20 +376,29 @@ __global__ void __launch_bounds__(32 * MmaShape<C, DP, NG>::kWarps, 1)
 #pragma unroll
     for (int ng = 0; ng < NG; ++ng) m[ng][0] = m[ng][1] = -INFINITY;
 
-    for (; use.tile < use.tiles; use.tile += use.step) {
-      if (Q8 || !BOXES) asm volatile("cp.async.wait_group %0;" ::"n"(S::kStages - 2) : "memory");
-      if (BOXES && !wait_barrier(barrier + 8 * stage, parity) && c.status) atomicOr(c.status, GAR_KV_TIMEOUT);
+    int from, lo, to, tile, step, tiles;
+    {
+      const Work &x = works[warp][done % kAhead];
+      from = x.seg.from, lo = x.seg.lo, to = x.seg.to, tile = x.tile, step = x.step, tiles = x.tiles;
+    }
+    for (; tile < tiles; tile += step) {
+      if (Q8 || !BOXES) {
+        if (flying == S::kStages - 1)
+          asm volatile("cp.async.wait_group %0;" ::"n"(S::kStages - 2) : "memory");
+        else
+          asm volatile("cp.async.wait_group 0;" ::: "memory");
+      }
+      if (BOXES && !wait_barrier(barrier + 8 * out, parity) && c.status) atomicOr(c.status, GAR_KV_TIMEOUT);
       __syncwarp();
-      issue(stage == 0 ? S::kStages - 1 : stage - 1);
-      char *const at = mine + stage * S::kTile;
-      const float *k_scale = scales + stage * (S::kScales / 4), *v_scale = k_scale + KT;
-      if (++stage == S::kStages) stage = 0, parity ^= 1;
-      const int n0 = seg.from + use.tile * KT;
-      const bool ragged = n0 < seg.lo || n0 + KT > seg.to;
+      pump(S::kStages);
+      char *const at = mine + out * S::kTile;
+      const float *k_scale = scales + out * (S::kScales / 4), *v_scale = k_scale + KT;
+      const int n0 = from + tile * KT;
+      const bool ragged = n0 < lo || n0 + KT > to;
       if (BOXES && ragged) {
         // What the copies brought of rows outside the segment must not meet the products: 0 * NaN is NaN.
         const int n = n0 + lane;
-        if (lane < KT && (n < seg.lo || n >= seg.to))
+        if (lane < KT && (n < lo || n >= to))
           for (int i = 0; i < PARTS; ++i)
             for (int x = 0; x < LINE; x += 16)
               *reinterpret_cast<uint4 *>(at + KT * DP * EL + (i * KT + lane) * LINE + x) = make_uint4(0, 0, 0, 0);
@@ -400,7 +441,7 @@ __global__ void __launch_bounds__(32 * MmaShape<C, DP, NG>::kWarps, 1)
 #pragma unroll
         for (int r = 0; r < 2; ++r) {
           const int row = sub * 16 + key_row<LINE>(g) + 8 * r, n = n0 + row;
-          const bool seen = !ragged || (n >= seg.lo && n < seg.to);
+          const bool seen = !ragged || (n >= lo && n < to);
           const float f = Q8 ? k_scale[row] : 1.f;
 #pragma unroll
           for (int ng = 0; ng < NG; ++ng)
@@ -498,9 +539,11 @@ __global__ void __launch_bounds__(32 * MmaShape<C, DP, NG>::kWarps, 1)
             }
           }
         }
+      --flying;
+      if (++out == S::kStages) out = 0, parity ^= 1;
     }
     // The stage read last holds this warp's o until it is joined.
-    float *const o_mine = reinterpret_cast<float *>(mine + (stage == 0 ? S::kStages - 1 : stage - 1) * S::kTile);
+    float *const o_mine = reinterpret_cast<float *>(mine + (out == 0 ? S::kStages - 1 : out - 1) * S::kTile);
     __syncwarp();
 #pragma unroll
     for (int ng = 0; ng < NG; ++ng)
@@ -523,14 +566,16 @@ __global__ void __launch_bounds__(32 * MmaShape<C, DP, NG>::kWarps, 1)
     if (BOXES) asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
     const float *const o_all = reinterpret_cast<const float *>(shared);
     if (lane == 0) join.at[warp] = (int)(o_mine - o_all);
-    if (use.alone) {
-      join_warps(a, seg, join, o_all, S::kRow, warp, 1, lane, 32, [] { __syncwarp(); });
-    } else {
-      join_warps(a, seg, join, o_all, S::kRow, 0, W, threadIdx.x, 32 * W, [] { __syncthreads(); });
-      if (!seg.whole) join_parts(a, seg, join);
-    }
+    const Segment seg = works[warp][done % kAhead].seg;
+    const Group group = works[warp][done % kAhead].group;
+    __syncwarp();
+    // The next segment's first tiles and queries come while this one is joined.
+    ++done;
+    pump(S::kStages - 1);
+    if (done < noted) load_queries();
+    join_warps(a, seg, group, join, o_all, S::kRow);
+    if (!seg.whole) join_parts(a, seg, group, join);
   }
-  asm volatile("cp.async.wait_all;" ::: "memory");
 }
 
 // Maps of the cache as bytes [pages][heads][page_size][dim]; false where it has none.

@@ -36,15 +36,20 @@ template <> __device__ __forceinline__ __nv_bfloat16 from_f32<__nv_bfloat16>(flo
   return __float2bfloat16_rn(x);
 }
 template <> __device__ __forceinline__ __half from_f32<__half>(float x) { return __float2half_rn(x); }
-// Quantised codes of x / scale, to the nearest, ties to even; |x / scale| is at most a
-// rounding error over the type's largest value unless the scale is a subnormal.
-template <> __device__ __forceinline__ i8 from_f32<i8>(float x) {
-  return i8{(int8_t)__float2int_rn(fminf(fmaxf(x, -127.f), 127.f))};
+// Four 8-bit codes of values within the type's range (a rounding error over it counts as within), to
+// the nearest, ties to even.
+__device__ __forceinline__ uint32_t codes4(float a, float b, float c, float d, i8) {
+  // Adding 1.5 * 2^23 rounds to an integer and leaves it in the low bits.
+  const float big = 12582912.f;
+  const uint32_t x = __byte_perm(__float_as_uint(__fadd_rn(a, big)), __float_as_uint(__fadd_rn(b, big)), 0x0040);
+  const uint32_t y = __byte_perm(__float_as_uint(__fadd_rn(c, big)), __float_as_uint(__fadd_rn(d, big)), 0x0040);
+  return __byte_perm(x, y, 0x5410);
 }
-template <> __device__ __forceinline__ e4m3 from_f32<e4m3>(float x) {
-  uint16_t r;
-  asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(r) : "f"(0.f), "f"(x));
-  return e4m3{(uint8_t)(r & 0xff)};
+__device__ __forceinline__ uint32_t codes4(float a, float b, float c, float d, e4m3) {
+  uint16_t x, y;
+  asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(x) : "f"(b), "f"(a));
+  asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(y) : "f"(d), "f"(c));
+  return (uint32_t)x | (uint32_t)y << 16;
 }
 
 template <typename T> struct quantised {
