@@ -478,6 +478,8 @@ typedef struct gar_attn_plan gar_attn_plan;
 GAR_API int gar_attn_plan_create(gar_attn_plan **out, int q_heads, int kv_heads, int dim);
 /* NULL is a no-op.  No work using the plan may still be running. */
 GAR_API void gar_attn_plan_destroy(gar_attn_plan *plan);
+/* The plan's numbers (each may be NULL).  Host-only. */
+GAR_API int gar_attn_plan_shape(const gar_attn_plan *plan, int *q_heads, int *kv_heads, int *dim);
 /* Bytes of device workspace a plan needs (whatever the batch and the lengths).  Host-only. */
 GAR_API int gar_attn_plan_bytes(const gar_attn_plan *plan, size_t *workspace_bytes);
 /* Attaches the caller's workspace (16-byte aligned) and clears its counters, waiting until

@@ -4,23 +4,27 @@ Usage: python -m paper_2004_09362_gb300.build   (or via __graft_entry__.build())
 
 Each translation unit compiles in parallel into _build/, then one link step writes
 paper_2004_09362_gb300/libgar.so.  Rebuilds only when a source is newer than the
-library.  The generated fused/batched kernels are compiled later, at plan time, by
+library.  The Python calls of the decoding operators (csrc/marshal.cpp) become
+paper_2004_09362_gb300/_marshal.so, linked to it and to torch.  The generated fused/batched kernels are compiled later, at plan time, by
 NVRTC inside the library.
 """
 
 from __future__ import annotations
 
 import concurrent.futures as cf
+import importlib.util
 import os
 import shutil
 import subprocess
 import sys
+import sysconfig
 
 PKG = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(PKG)
 CSRC = os.path.join(PKG, "csrc")
 INCLUDE = os.path.join(ROOT, "include")
 OUT = os.path.join(PKG, "libgar.so")
+MARSHAL = os.path.join(PKG, "_marshal.so")
 BUILD = os.path.join(ROOT, "_build")
 
 SOURCES = ["api.cpp", "plan.cpp", "codegen.cpp", "jit.cpp", "step_kernels.cu", "rope.cu", "cache.cu",
@@ -50,10 +54,10 @@ def _cuda_lib_dir(nvcc: str) -> str:
 
 
 def _stale() -> bool:
-    if not os.path.exists(OUT):
+    if not os.path.exists(OUT) or not os.path.exists(MARSHAL):
         return True
-    t = os.path.getmtime(OUT)
-    deps = [os.path.join(CSRC, f) for f in SOURCES + HEADERS]
+    t = min(os.path.getmtime(OUT), os.path.getmtime(MARSHAL))
+    deps = [os.path.join(CSRC, f) for f in SOURCES + HEADERS + ["marshal.cpp"]]
     deps += [os.path.join(INCLUDE, "gar.h"), os.path.abspath(__file__)]
     return any(os.path.getmtime(d) > t for d in deps)
 
@@ -89,8 +93,20 @@ def _build(verbose: bool) -> str:
             print(r.stdout, r.stderr, file=sys.stderr)
         return obj
 
-    with cf.ThreadPoolExecutor(max_workers=len(SOURCES)) as ex:
+    def compile_marshal() -> str:
+        obj = os.path.join(BUILD, "marshal.o")
+        inc = os.path.join(_torch_dir(), "include")
+        cuda = os.path.join(os.path.dirname(os.path.dirname(os.path.realpath(nvcc))), "include")
+        _run(["g++", "-O2", "-std=c++17", "-fPIC", "-fvisibility=hidden", "-I", inc, "-I",
+              os.path.join(inc, "torch", "csrc", "api", "include"), "-I", sysconfig.get_paths()["include"],
+              "-I", cuda, "-I", "/usr/local/cuda/include", "-c", os.path.join(CSRC, "marshal.cpp"), "-o", obj],
+             "g++ failed for marshal.cpp")
+        return obj
+
+    with cf.ThreadPoolExecutor(max_workers=len(SOURCES) + 1) as ex:
+        marshal = ex.submit(compile_marshal)
         objs = list(ex.map(compile_one, SOURCES))
+        marshal_obj = marshal.result()
     tmp = OUT + f".tmp{os.getpid()}"
     cmd = [nvcc, *ARCH, "-shared", "-o", tmp, *objs, "-L", libdir, "-lnvrtc",
            "-Xlinker", "-rpath", "-Xlinker", libdir]
@@ -98,7 +114,22 @@ def _build(verbose: bool) -> str:
     if r.returncode != 0:
         raise RuntimeError(f"link failed:\n{r.stdout}\n{r.stderr}")
     os.replace(tmp, OUT)
+    lib = os.path.join(_torch_dir(), "lib")
+    tmp = MARSHAL + f".tmp{os.getpid()}"
+    _run(["g++", "-shared", "-o", tmp, marshal_obj, "-L", PKG, "-lgar", "-L", lib, "-ltorch_python", "-ltorch_cpu",
+          "-lc10", "-lc10_cuda", "-Wl,-rpath,$ORIGIN", "-Wl,-rpath," + lib], "link of _marshal.so failed")
+    os.replace(tmp, MARSHAL)
     return OUT
+
+
+def _torch_dir() -> str:
+    return list(importlib.util.find_spec("torch").submodule_search_locations)[0]
+
+
+def _run(cmd, what: str) -> None:
+    r = subprocess.run(cmd, capture_output=True, text=True)
+    if r.returncode != 0:
+        raise RuntimeError(f"{what}:\n{r.stdout}\n{r.stderr}")
 
 
 if __name__ == "__main__":

@@ -73,6 +73,14 @@ int gar_attn_plan_create(gar_attn_plan **out, int q_heads, int kv_heads, int dim
 
 void gar_attn_plan_destroy(gar_attn_plan *plan) { delete plan; }
 
+int gar_attn_plan_shape(const gar_attn_plan *plan, int *q_heads, int *kv_heads, int *dim) {
+  if (plan == nullptr) return refuse("null plan");
+  if (q_heads) *q_heads = plan->q_heads;
+  if (kv_heads) *kv_heads = plan->kv_heads;
+  if (dim) *dim = plan->dim;
+  return GAR_OK;
+}
+
 int gar_attn_plan_bytes(const gar_attn_plan *plan, size_t *bytes) {
   if (plan == nullptr || bytes == nullptr) return refuse("null plan or output");
   *bytes = workspace_bytes(*plan);

@@ -1,0 +1,380 @@
+// Python calls of the decoding operators: checks of tensors and marshalling of their addresses,
+// sizes and strides to the C entry points.  Compiled because a call of these operators takes the GPU 2 us
+// upwards, and the same checks took the interpreter 8 us and more; nothing is computed here.
+#define PY_SSIZE_T_CLEAN
+#include <Python.h>
+
+#include <ATen/core/Tensor.h>
+#include <ATen/ops/empty.h>
+#include <c10/cuda/CUDAGuard.h>
+#include <c10/cuda/CUDAStream.h>
+#include <torch/csrc/autograd/python_variable.h>
+
+#include <cmath>
+#include <stdexcept>
+#include <string>
+
+#include "../../include/gar.h"
+
+namespace {
+
+using at::Tensor;
+
+// Carries a Python exception that is already set.
+struct python_error {};
+
+[[noreturn]] void bad(const std::string &why) { throw std::invalid_argument(why); }
+
+// The arguments of a call, by the names of its parameters; the first `needed` must be there.
+template <int N> struct Arguments {
+  PyObject *at[N] = {};
+  Arguments(const char *call, const char *const (&names)[N], int needed, PyObject *const *args, Py_ssize_t n, PyObject *kw) {
+    const auto type_error = [&](const std::string &why) {
+      PyErr_SetString(PyExc_TypeError, (std::string(call) + "() " + why).c_str());
+      throw python_error();
+    };
+    if (n > N) type_error("takes at most " + std::to_string(N) + " arguments");
+    for (Py_ssize_t i = 0; i < n; ++i) at[i] = args[i];
+    const Py_ssize_t k = kw ? PyTuple_GET_SIZE(kw) : 0;
+    for (Py_ssize_t j = 0; j < k; ++j) {
+      PyObject *key = PyTuple_GET_ITEM(kw, j);
+      int i = 0;
+      while (i < N && PyUnicode_CompareWithASCIIString(key, names[i]) != 0) ++i;
+      const char *name = PyUnicode_AsUTF8(key);
+      if (i == N) type_error(std::string("got an unexpected argument '") + (name ? name : "?") + "'");
+      if (at[i]) type_error(std::string("got two values for '") + names[i] + "'");
+      at[i] = args[n + j];
+    }
+    for (int i = 0; i < needed; ++i)
+      if (!at[i]) type_error(std::string("needs '") + names[i] + "'");
+    for (int i = 0; i < N; ++i)
+      if (at[i] == Py_None) at[i] = nullptr;
+    for (int i = 0; i < needed; ++i)
+      if (!at[i]) type_error(std::string("needs '") + names[i] + "', not None");
+  }
+};
+
+const Tensor &tensor(PyObject *o, const char *what) {
+  if (!THPVariable_Check(o)) {
+    PyErr_SetString(PyExc_TypeError, (std::string(what) + " must be a tensor").c_str());
+    throw python_error();
+  }
+  return THPVariable_Unpack(o);
+}
+
+int64_t integer(PyObject *o) {
+  const long long v = PyLong_AsLongLong(o);
+  if (v == -1 && PyErr_Occurred()) throw python_error();
+  return v;
+}
+
+double number(PyObject *o) {
+  const double v = PyFloat_AsDouble(o);
+  if (v == -1 && PyErr_Occurred()) throw python_error();
+  return v;
+}
+
+bool truth(PyObject *o) {
+  const int v = o ? PyObject_IsTrue(o) : 0;
+  if (v < 0) throw python_error();
+  return v;
+}
+
+// An address that a Python object keeps as an integer.
+template <typename T> T *handle(PyObject *o, const char *attribute, const char *what) {
+  PyObject *v = PyObject_GetAttrString(o, attribute);
+  if (!v) throw python_error();
+  void *p = PyLong_AsVoidPtr(v);
+  Py_DECREF(v);
+  if (PyErr_Occurred()) throw python_error();
+  if (!p) bad(what);
+  return static_cast<T *>(p);
+}
+
+int dtype_of(const Tensor &t, const char *what) {
+  switch (t.scalar_type()) {
+    case at::kFloat: return GAR_F32;
+    case at::kBFloat16: return GAR_BF16;
+    case at::kHalf: return GAR_F16;
+    case at::kChar: return GAR_I8;
+    case at::kFloat8_e4m3fn: return GAR_E4M3;
+    default: bad(std::string(what) + ": this dtype is not supported");
+  }
+}
+
+// [tokens, heads, dim] on the GPU, the channels of a head contiguous.
+const Tensor &rows(PyObject *o, const char *what) {
+  const Tensor &t = tensor(o, what);
+  if (t.dim() != 3) bad(std::string(what) + " must be [tokens, heads, dim]");
+  if (t.stride(2) != 1 && t.size(2) > 1) bad(std::string(what) + ": the channels of a head must be contiguous");
+  if (!t.is_cuda()) bad(std::string(what) + " must be a CUDA tensor");
+  return t;
+}
+
+// n contiguous integers on the GPU, 8 bytes wide or (`narrow`) 4.
+const Tensor &integers(PyObject *o, int64_t n, bool narrow, bool wide, const char *what) {
+  const Tensor &t = tensor(o, what);
+  if (t.dim() != 1 || (n >= 0 && t.size(0) != n) || !t.is_cuda() || (t.size(0) > 1 && t.stride(0) != 1))
+    bad(std::string(what) + " must be contiguous integers on the GPU, one for each token or sequence");
+  const auto type = t.scalar_type();
+  if (!(wide && type == at::kLong) && !(narrow && type == at::kInt)) bad(std::string(what) + ": this dtype is not supported");
+  return t;
+}
+
+const Tensor &rotations(PyObject *o, int64_t dim) {
+  const Tensor &t = tensor(o, "table");
+  if (t.dim() != 3 || t.size(2) != 2 || t.scalar_type() != at::kFloat || !t.is_cuda() || !t.is_contiguous())
+    bad("the table must be a contiguous float32 CUDA tensor [positions, rot / 2, 2]");
+  if (t.size(1) < 1 || 2 * t.size(1) > dim)
+    bad("the table rotates " + std::to_string(2 * t.size(1)) + " channels, the heads have " + std::to_string(dim));
+  return t;
+}
+
+int layout_of(PyObject *o) {
+  if (!o) return GAR_ROPE_HALF;
+  if (PyUnicode_Check(o)) {
+    if (PyUnicode_CompareWithASCIIString(o, "half") == 0) return GAR_ROPE_HALF;
+    if (PyUnicode_CompareWithASCIIString(o, "interleaved") == 0) return GAR_ROPE_INTERLEAVED;
+    bad("unknown layout");
+  }
+  return (int)integer(o);
+}
+
+// The stream of a call: torch's current one, a torch stream, or a raw handle.
+struct Stream {
+  gar_stream_t raw;
+  bool other;  // not torch's current stream
+  explicit Stream(PyObject *o) {
+    const cudaStream_t current = c10::cuda::getCurrentCUDAStream().stream();
+    raw = current;
+    if (o) {
+      PyObject *v = PyLong_Check(o) ? Py_NewRef(o) : PyObject_GetAttrString(o, "cuda_stream");
+      if (!v) throw python_error();
+      raw = static_cast<gar_stream_t>(PyLong_AsVoidPtr(v));
+      Py_DECREF(v);
+      if (PyErr_Occurred()) throw python_error();
+    }
+    other = raw != current;
+  }
+  // An output that the call fills: allocated under its stream, so that its memory is not given away
+  // while that stream uses it.
+  Tensor empty(at::IntArrayRef shape, at::ScalarType type, const Tensor &like) const {
+    const auto options = at::TensorOptions().dtype(type).device(like.device());
+    if (!other) return at::empty(shape, options);
+    c10::cuda::CUDAStreamGuard guard(c10::cuda::getStreamFromExternal(raw, like.get_device()));
+    return at::empty(shape, options);
+  }
+};
+
+void check(int rc, const char *where) {
+  if (rc == GAR_OK) return;
+  PyObject *m = PyImport_ImportModule("paper_2004_09362_gb300.gar");
+  PyObject *r = m ? PyObject_CallMethod(m, "_check", "is", rc, where) : nullptr;
+  Py_XDECREF(r);
+  Py_XDECREF(m);
+  throw python_error();
+}
+
+template <typename F> PyObject *guarded(F f) noexcept {
+  try {
+    return f();
+  } catch (const python_error &) {
+  } catch (const std::invalid_argument &e) {
+    PyErr_SetString(PyExc_ValueError, e.what());
+  } catch (const std::exception &e) {
+    PyErr_SetString(PyExc_RuntimeError, e.what());
+  } catch (...) {
+    PyErr_SetString(PyExc_RuntimeError, "unknown C++ exception");
+  }
+  return nullptr;
+}
+
+PyObject *rope(PyObject *, PyObject *const *args, Py_ssize_t n, PyObject *kw) {
+  return guarded([&] {
+    static const char *const names[] = {"x", "positions", "table", "layout", "inverse", "out", "stream"};
+    const Arguments<7> a("gar_rope", names, 3, args, n, kw);
+    const Tensor &x = rows(a.at[0], "x"), &table = rotations(a.at[2], x.size(2));
+    const Tensor &positions = integers(a.at[1], x.size(0), true, true, "positions");
+    const Stream stream(a.at[6]);
+    Tensor out;
+    if (a.at[5]) {
+      out = rows(a.at[5], "out");
+      if (out.scalar_type() != x.scalar_type() || out.sizes() != x.sizes()) bad("out must have x's shape and dtype");
+    } else {
+      out = stream.empty(x.sizes(), x.scalar_type(), x);
+    }
+    check(gar_rope(x.data_ptr(), x.stride(0), x.stride(1), out.data_ptr(), out.stride(0), out.stride(1), dtype_of(x, "x"),
+                   x.size(0), (int)x.size(1), (int)x.size(2), 2 * (int)table.size(1), positions.data_ptr(),
+                   (int)positions.element_size(), static_cast<const float *>(table.data_ptr()), table.size(0),
+                   layout_of(a.at[3]), truth(a.at[4]), stream.raw),
+          "gar_rope");
+    return a.at[5] ? Py_NewRef(a.at[5]) : THPVariable_Wrap(std::move(out));
+  });
+}
+
+PyObject *kv_write(PyObject *, PyObject *const *args, Py_ssize_t n, PyObject *kw) {
+  return guarded([&] {
+    static const char *const names[] = {"cache", "k", "v", "slots", "positions", "table", "layout", "stream"};
+    const Arguments<8> a("gar_kv_write", names, 4, args, n, kw);
+    const gar_kv_cache *cache = handle<gar_kv_cache>(a.at[0], "address", "the cache has no address");
+    const Tensor &k = rows(a.at[1], "k"), &v = rows(a.at[2], "v");
+    if (k.sizes() != v.sizes() || k.scalar_type() != v.scalar_type() || k.size(1) != cache->heads || k.size(2) != cache->dim)
+      bad("k and v must be [tokens, heads, dim] of the cache's heads and dim, alike in dtype");
+    const Tensor &slots = integers(a.at[3], k.size(0), false, true, "slots");
+    if (!a.at[4] != !a.at[5]) bad("positions and table go together");
+    const void *positions = nullptr;
+    const float *table = nullptr;
+    int width = 8, rot = 0;
+    int64_t table_rows = 0;
+    if (a.at[4]) {
+      const Tensor &t = rotations(a.at[5], k.size(2)), &p = integers(a.at[4], k.size(0), true, true, "positions");
+      positions = p.data_ptr(), width = (int)p.element_size(), table = static_cast<const float *>(t.data_ptr());
+      table_rows = t.size(0), rot = 2 * (int)t.size(1);
+    }
+    const Stream stream(a.at[7]);
+    check(gar_kv_write(cache, k.data_ptr(), k.stride(0), k.stride(1), v.data_ptr(), v.stride(0), v.stride(1),
+                       dtype_of(k, "k"), k.size(0), static_cast<const int64_t *>(slots.data_ptr()), positions, width, table,
+                       table_rows, rot, layout_of(a.at[6]), stream.raw),
+          "gar_kv_write");
+    return Py_NewRef(Py_None);
+  });
+}
+
+PyObject *kv_read(PyObject *, PyObject *const *args, Py_ssize_t n, PyObject *kw) {
+  return guarded([&] {
+    static const char *const names[] = {"cache", "slots", "dtype", "out", "stream"};
+    const Arguments<5> a("gar_kv_read", names, 2, args, n, kw);
+    const gar_kv_cache *cache = handle<gar_kv_cache>(a.at[0], "address", "the cache has no address");
+    const Tensor &slots = integers(a.at[1], -1, false, true, "slots");
+    const Stream stream(a.at[4]);
+    Tensor k, v;
+    const int64_t shape[3] = {slots.size(0), cache->heads, cache->dim};
+    if (a.at[3]) {
+      if (!PyTuple_Check(a.at[3]) || PyTuple_GET_SIZE(a.at[3]) != 2) bad("out must be a pair of tensors");
+      k = tensor(PyTuple_GET_ITEM(a.at[3], 0), "out"), v = tensor(PyTuple_GET_ITEM(a.at[3], 1), "out");
+      for (const Tensor &t : {k, v})
+        if (t.sizes() != at::IntArrayRef(shape) || t.scalar_type() != k.scalar_type() || !t.is_cuda() || !t.is_contiguous())
+          bad("out must be two contiguous CUDA tensors [tokens, heads, dim] of one dtype");
+    } else {
+      at::ScalarType type = cache->dtype == GAR_F32 ? at::kFloat : cache->dtype == GAR_F16 ? at::kHalf : at::kBFloat16;
+      if (a.at[2]) {
+        const char *s = PyUnicode_Check(a.at[2]) ? PyUnicode_AsUTF8(a.at[2]) : nullptr;
+        const std::string name = s ? s : "?";
+        if (name == "f32")
+          type = at::kFloat;
+        else if (name == "bf16")
+          type = at::kBFloat16;
+        else if (name == "f16")
+          type = at::kHalf;
+        else
+          bad("unknown dtype '" + name + "'");
+      }
+      k = stream.empty(shape, type, slots), v = stream.empty(shape, type, slots);
+    }
+    check(gar_kv_read(cache, static_cast<const int64_t *>(slots.data_ptr()), slots.size(0), k.data_ptr(), v.data_ptr(),
+                      dtype_of(k, "out"), stream.raw),
+          "gar_kv_read");
+    if (a.at[3]) return Py_NewRef(a.at[3]);
+    PyObject *pair = PyTuple_New(2);
+    if (!pair) throw python_error();
+    PyTuple_SET_ITEM(pair, 0, THPVariable_Wrap(std::move(k)));
+    PyTuple_SET_ITEM(pair, 1, THPVariable_Wrap(std::move(v)));
+    return pair;
+  });
+}
+
+PyObject *decode_attention(PyObject *, PyObject *const *args, Py_ssize_t n, PyObject *kw) {
+  return guarded([&] {
+    static const char *const names[] = {"plan",  "q",      "cache", "page_table", "lengths",
+                                        "scale", "window", "out",   "lse",        "stream"};
+    const Arguments<10> a("gar_decode_attention", names, 5, args, n, kw);
+    gar_attn_plan *plan = handle<gar_attn_plan>(a.at[0], "address", "plan destroyed");
+    const gar_kv_cache *cache = handle<gar_kv_cache>(a.at[2], "address", "the cache has no address");
+    const Tensor &q = rows(a.at[1], "q"), &lengths = integers(a.at[4], q.size(0), true, false, "lengths");
+    const Tensor &table = tensor(a.at[3], "page_table");
+    if (table.dim() != 2 || table.size(0) != q.size(0) || table.scalar_type() != at::kInt || !table.is_cuda() ||
+        (table.stride(1) != 1 && table.size(1) > 1))
+      bad("page_table must be int32 [batch, width] on the GPU with contiguous rows");
+    int shape[3];
+    check(gar_attn_plan_shape(plan, &shape[0], &shape[1], &shape[2]), "gar_attn_plan_shape");
+    if (q.size(1) != shape[0] || q.size(2) != shape[2])
+      bad("q must be [batch, " + std::to_string(shape[0]) + ", " + std::to_string(shape[2]) + "]");
+    const Stream stream(a.at[9]);
+    // The workspace comes with the first call.
+    PyObject *ws = PyObject_GetAttrString(a.at[0], "workspace");
+    const bool without = ws == Py_None;
+    Py_XDECREF(ws);
+    if (!ws) throw python_error();
+    if (without) {
+      PyObject *m = PyImport_ImportModule("paper_2004_09362_gb300.gar");
+      PyObject *r = m ? PyObject_CallMethod(m, "_ensure_attn_workspace", "OO", a.at[0], a.at[1]) : nullptr;
+      Py_XDECREF(m);
+      if (!r) throw python_error();
+      Py_DECREF(r);
+    }
+    Tensor out, lse;
+    if (a.at[7]) {
+      out = rows(a.at[7], "out");
+      if (out.sizes() != q.sizes()) bad("out must have q's shape");
+    } else {
+      out = stream.empty(q.sizes(), q.scalar_type(), q);
+    }
+    const bool given = a.at[8] && !PyBool_Check(a.at[8]), wanted = given || truth(a.at[8]);
+    if (given) {
+      lse = tensor(a.at[8], "lse");
+      if (lse.scalar_type() != at::kFloat || lse.sizes() != q.sizes().slice(0, 2) || !lse.is_contiguous() || !lse.is_cuda())
+        bad("lse must be a contiguous float32 CUDA tensor [batch, q_heads]");
+    } else if (wanted) {
+      lse = stream.empty(q.sizes().slice(0, 2), at::kFloat, q);
+    }
+    const double scale = a.at[5] ? number(a.at[5]) : 1.0 / std::sqrt((double)shape[2]);
+    check(gar_decode_attention(plan, cache, q.data_ptr(), q.stride(0), q.stride(1), dtype_of(q, "q"), out.data_ptr(),
+                               out.stride(0), out.stride(1), dtype_of(out, "out"),
+                               wanted ? static_cast<float *>(lse.data_ptr()) : nullptr,
+                               static_cast<const int32_t *>(table.data_ptr()), table.stride(0), (int)table.size(1),
+                               static_cast<const int32_t *>(lengths.data_ptr()), (int)q.size(0), (float)scale,
+                               a.at[6] ? (int)integer(a.at[6]) : 0, stream.raw),
+          "gar_decode_attention");
+    PyObject *first = a.at[7] ? Py_NewRef(a.at[7]) : THPVariable_Wrap(std::move(out));
+    if (!wanted) return first;
+    PyObject *pair = first ? PyTuple_New(2) : nullptr;
+    if (!pair) throw python_error();
+    PyTuple_SET_ITEM(pair, 0, first);
+    PyTuple_SET_ITEM(pair, 1, given ? Py_NewRef(a.at[8]) : THPVariable_Wrap(std::move(lse)));
+    return pair;
+  });
+}
+
+
+PyMethodDef methods[] = {
+    {"gar_rope", (PyCFunction)(void (*)())rope, METH_FASTCALL | METH_KEYWORDS,
+     "gar_rope(x, positions, table, layout='half', inverse=False, out=None, stream=None)\n--\n\n"
+     "x [tokens, heads, dim] with its first rot channels rotated by the table's rows at\n"
+     "`positions` (int32 or int64); out may be x.  With inverse, the gradient: x is grad_out, the result\n"
+     "grad_x.  layout: 'half' or 'interleaved'."},
+    {"gar_kv_write", (PyCFunction)(void (*)())kv_write, METH_FASTCALL | METH_KEYWORDS,
+     "gar_kv_write(cache, k, v, slots, positions=None, table=None, layout='half', stream=None)\n--\n\n"
+     "Writes k, v [tokens, heads, dim] to the cache's slots (int64; negative: skipped),\n"
+     "quantised where the cache is; with positions and table, the keys rotated first."},
+    {"gar_kv_read", (PyCFunction)(void (*)())kv_read, METH_FASTCALL | METH_KEYWORDS,
+     "gar_kv_read(cache, slots, dtype=None, out=None, stream=None)\n--\n\n"
+     "(k, v), each [tokens, heads, dim], of the cache's slots; rows of negative slots are 0.\n"
+     "dtype: 'f32', 'bf16' or 'f16' (default: the cache's, bf16 for an 8-bit one); out: a pair of\n"
+     "contiguous tensors to fill instead."},
+    {"gar_decode_attention", (PyCFunction)(void (*)())decode_attention, METH_FASTCALL | METH_KEYWORDS,
+     "gar_decode_attention(plan, q, cache, page_table, lengths, scale=None, window=0, out=None,\n"
+     "                     lse=None, stream=None)\n--\n\n"
+     "Attention of q [batch, q_heads, dim] over each sequence's cached rows.\n\n"
+     "page_table: int32 [batch, width]; lengths: int32 [batch], the new token's row included.\n"
+     "scale: dim**-0.5 by default.  window: only the last `window` rows (0: all).  out: q's shape, of\n"
+     "q's dtype or float32.  lse: True, or a contiguous float32 [batch, q_heads] tensor, returns\n"
+     "(out, log of the sum of weights); else returns out.  The plan's workspace is allocated on its\n"
+     "first call; make one before capturing calls into a CUDA graph."},
+    {nullptr, nullptr, 0, nullptr}};
+
+PyModuleDef module = {PyModuleDef_HEAD_INIT, "_marshal", "Compiled calls of the decoding operators.", -1, methods,
+                      nullptr,               nullptr,    nullptr,                                     nullptr};
+
+}  // namespace
+
+PyMODINIT_FUNC PyInit__marshal(void) { return PyModule_Create(&module); }

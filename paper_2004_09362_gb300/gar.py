@@ -51,7 +51,7 @@ EXPORTS = (
     "gar_cost_model", "gar_optimal_steps", "gar_plan_status", "gar_plan_debug_barrier",
     "gar_plan_create_group", "gar_rope_frequencies", "gar_rope_table", "gar_rope", "gar_kv_write",
     "gar_kv_read", "gar_kv_status", "gar_attn_plan_create", "gar_attn_plan_destroy",
-    "gar_attn_plan_bytes", "gar_attn_plan_set_workspace", "gar_decode_attention",
+    "gar_attn_plan_shape", "gar_attn_plan_bytes", "gar_attn_plan_set_workspace", "gar_decode_attention",
 )
 
 
@@ -123,6 +123,7 @@ def _load():
         "gar_kv_status": (i32, [P_(gar_kv_cache), P_(ctypes.c_uint32), vp]),
         "gar_attn_plan_create": (i32, [P_(vp), i32, i32, i32]),
         "gar_attn_plan_destroy": (None, [vp]),
+        "gar_attn_plan_shape": (i32, [vp, P_(i32), P_(i32), P_(i32)]),
         "gar_attn_plan_bytes": (i32, [vp, P_(sz)]),
         "gar_attn_plan_set_workspace": (i32, [vp, vp, sz]),
         "gar_decode_attention": (i32, [vp, P_(gar_kv_cache), vp, i64, i64, i32, vp, i64, i64, i32, vp, vp,
@@ -478,38 +479,6 @@ def _dtype_of(t, what: str) -> int:
     return code
 
 
-def _rows(t, what: str):
-    """Checks [tokens, heads, dim] with contiguous channels; returns its shape and strides."""
-    if t.dim() != 3:
-        raise ValueError(f"{what} must be [tokens, heads, dim]")
-    shape, stride = t.shape, t.stride()
-    if stride[2] != 1 and shape[2] > 1:
-        raise ValueError(f"{what}: the channels of a head must be contiguous")
-    if not t.is_cuda:
-        raise ValueError(f"{what} must be a CUDA tensor")
-    return shape, stride
-
-
-def _integers(t, n: int, what: str, sizes=(4, 8)) -> int:
-    """Checks n contiguous integers on the GPU; returns their width in bytes."""
-    if t.dim() != 1 or t.shape[0] != n or not t.is_cuda or (n > 1 and t.stride(0) != 1):
-        raise ValueError(f"{what} must be {n} contiguous integers on the GPU")
-    size = t.element_size()
-    if size not in sizes or t.is_floating_point() or t.is_complex():
-        raise ValueError(f"{what}: dtype {t.dtype} is not supported")
-    return size
-
-
-def _check_table(table, dim: int):
-    shape = table.shape
-    if len(shape) != 3 or shape[2] != 2 or table.element_size() != 4 or not table.is_floating_point() \
-            or not table.is_cuda or not table.is_contiguous():
-        raise ValueError("the table must be a contiguous float32 CUDA tensor [positions, rot / 2, 2]")
-    if not 0 < 2 * shape[1] <= dim:
-        raise ValueError(f"the table rotates {2 * shape[1]} channels, the heads have {dim}")
-    return shape
-
-
 def _empty(shape, dtype, device, stream):
     """An output that the call on `stream` (None, a torch stream or a raw handle) fills: allocated
     under that stream, so that its memory is not given away while that stream uses it."""
@@ -542,24 +511,6 @@ def gar_rope_table(count: int, frequencies, magnitude: float = 1.0, first: int =
     _check(_lib.gar_rope_table(table.data_ptr(), int(first), int(count), 2 * n, f, float(magnitude),
                                _stream_handle(stream)), "gar_rope_table")
     return table
-
-
-def gar_rope(x, positions, table, layout="half", inverse: bool = False, out=None, stream=None):
-    """x [tokens, heads, dim] with its first rot channels rotated by the table's rows at
-    `positions`; out may be x.  With inverse, the gradient: x is grad_out, the result grad_x."""
-    shape, xs = _rows(x, "x")
-    tshape = _check_table(table, shape[2])
-    width = _integers(positions, shape[0], "positions")
-    if out is None:
-        out = _empty(shape, x.dtype, x.device, stream)
-    elif out.dtype != x.dtype or out.shape != shape:
-        raise ValueError("out must have x's shape and dtype")
-    _, os_ = _rows(out, "out")
-    _check(_lib.gar_rope(x.data_ptr(), xs[0], xs[1], out.data_ptr(), os_[0], os_[1], _dtype_of(x, "x"),
-                         shape[0], shape[1], shape[2], 2 * tshape[1], positions.data_ptr(), width,
-                         table.data_ptr(), tshape[0], _code(layout, ROPE_LAYOUTS, "layout"),
-                         1 if inverse else 0, _stream_handle(stream)), "gar_rope")
-    return out
 
 
 class KVCache:
@@ -599,60 +550,12 @@ class KVCache:
         self.k, self.v, self.k_scale, self.v_scale = k, v, k_scale, v_scale
         self.heads, self.dim, self.page_size, self.pages, self.dtype = heads, dim, page_size, pages, dtype
         self._c = c
-        self._ref = ctypes.byref(c)
-
-
-def gar_kv_write(cache: KVCache, k, v, slots, positions=None, table=None, layout="half", stream=None) -> None:
-    """Writes k, v [tokens, heads, dim] to the cache's slots (int64; negative: skipped),
-    quantised where the cache is; with positions and table, the keys rotated first."""
-    shape, ks = _rows(k, "k")
-    vshape, vs = _rows(v, "v")
-    if shape != vshape or k.dtype != v.dtype or shape[1] != cache.heads or shape[2] != cache.dim:
-        raise ValueError("k and v must be [tokens, heads, dim] of the cache's heads and dim, alike in dtype")
-    _integers(slots, shape[0], "slots", (8,))
-    if (positions is None) != (table is None):
-        raise ValueError("positions and table go together")
-    pos, width, tab, trows, rot = None, 8, None, 0, 0
-    if positions is not None:
-        tshape = _check_table(table, shape[2])
-        width = _integers(positions, shape[0], "positions")
-        pos, tab, trows, rot = positions.data_ptr(), table.data_ptr(), tshape[0], 2 * tshape[1]
-    _check(_lib.gar_kv_write(cache._ref, k.data_ptr(), ks[0], ks[1], v.data_ptr(), vs[0], vs[1],
-                             _dtype_of(k, "k"), shape[0], slots.data_ptr(), pos, width, tab, trows, rot,
-                             _code(layout, ROPE_LAYOUTS, "layout"), _stream_handle(stream)), "gar_kv_write")
-
-
-def gar_kv_read(cache: KVCache, slots, dtype=None, out=None, stream=None):
-    """(k, v), each [tokens, heads, dim], of the cache's slots; rows of negative slots are 0.
-    dtype: "f32", "bf16" or "f16" (default: the cache's, bf16 for an 8-bit one); out: a pair of
-    contiguous tensors to fill instead."""
-    import torch
-    n = slots.shape[0] if slots.dim() == 1 else -1
-    _integers(slots, n, "slots", (8,))
-    if out is None:
-        kinds = {"f32": torch.float32, "bf16": torch.bfloat16, "f16": torch.float16}
-        if dtype is None:
-            kind = torch.bfloat16 if cache.dtype in (GAR_I8, GAR_E4M3) else cache.k.dtype
-        elif dtype in kinds:
-            kind = kinds[dtype]
-        else:
-            raise ValueError(f"unknown dtype {dtype!r}")
-        both = _empty((2, n, cache.heads, cache.dim), kind, slots.device, stream)
-        k, v = both[0], both[1]
-    else:
-        k, v = out
-        want = (n, cache.heads, cache.dim)
-        if tuple(k.shape) != want or tuple(v.shape) != want or k.dtype != v.dtype \
-                or not (k.is_cuda and v.is_cuda and k.is_contiguous() and v.is_contiguous()):
-            raise ValueError("out must be two contiguous CUDA tensors [tokens, heads, dim] of one dtype")
-    _check(_lib.gar_kv_read(cache._ref, slots.data_ptr(), n, k.data_ptr(), v.data_ptr(), _dtype_of(k, "out"),
-                            _stream_handle(stream)), "gar_kv_read")
-    return k, v
+        self.address = ctypes.addressof(c)
 
 
 def gar_kv_status(cache: KVCache, stream=None) -> None:
     """Waits for the stream; raises GarError if a kernel met an index out of range since the last call."""
-    _check(_lib.gar_kv_status(cache._ref, None, _stream_handle(stream)), "gar_kv_status")
+    _check(_lib.gar_kv_status(ctypes.byref(cache._c), None, _stream_handle(stream)), "gar_kv_status")
 
 
 class AttnPlan:
@@ -661,8 +564,8 @@ class AttnPlan:
 
     def __init__(self, handle: int, q_heads: int, kv_heads: int, dim: int):
         self._h = ctypes.c_void_p(handle)
+        self.address = handle
         self.q_heads, self.kv_heads, self.dim = q_heads, kv_heads, dim
-        self.default_scale = dim ** -0.5
         self.workspace = None
 
     @property
@@ -689,6 +592,14 @@ def gar_attn_plan_destroy(plan: AttnPlan) -> None:
     if plan._h:
         _lib.gar_attn_plan_destroy(plan._h)
         plan._h = ctypes.c_void_p(None)
+        plan.address = 0
+
+
+def gar_attn_plan_shape(plan: AttnPlan):
+    """(q_heads, kv_heads, dim)."""
+    v = [ctypes.c_int() for _ in range(3)]
+    _check(_lib.gar_attn_plan_shape(plan.handle, *[ctypes.byref(x) for x in v]), "gar_attn_plan_shape")
+    return tuple(x.value for x in v)
 
 
 def gar_attn_plan_bytes(plan: AttnPlan) -> int:
@@ -702,47 +613,22 @@ def gar_attn_plan_set_workspace(plan: AttnPlan, ptr: int, nbytes: int) -> None:
            "gar_attn_plan_set_workspace")
 
 
-def gar_decode_attention(plan: AttnPlan, q, cache: KVCache, page_table, lengths, scale=None, window: int = 0,
-                         out=None, lse=None, stream=None):
-    """Attention of q [batch, q_heads, dim] over each sequence's cached rows.
-
-    page_table: int32 [batch, width]; lengths: int32 [batch], the new token's row included.
-    scale: dim**-0.5 by default.  window: only the last `window` rows (0: all).  out: q's shape, of
-    q's dtype or float32.  lse: True, or a contiguous float32 [batch, q_heads] tensor, returns
-    (out, log of the sum of weights); else returns out.  The plan's workspace is allocated on its
-    first call; make one before capturing calls into a CUDA graph."""
+def _ensure_attn_workspace(plan: AttnPlan, like) -> None:
+    """Allocates the plan's workspace next to the tensor `like` and attaches it."""
     import torch
-    shape, qs = _rows(q, "q")
-    batch, q_heads, dim = shape
-    if q_heads != plan.q_heads or dim != plan.dim:
-        raise ValueError(f"q must be [batch, {plan.q_heads}, {plan.dim}]")
-    if lengths.dtype != torch.int32 or page_table.dtype != torch.int32:
-        raise ValueError("page_table and lengths must be int32")
-    _integers(lengths, batch, "lengths", (4,))
-    tshape, ts = page_table.shape, page_table.stride()
-    if len(tshape) != 2 or tshape[0] != batch or not page_table.is_cuda or (ts[1] != 1 and tshape[1] > 1):
-        raise ValueError(f"page_table must be [{batch}, width] on the GPU with contiguous rows")
-    handle = _stream_handle(stream)
-    if plan.workspace is None:
-        n = gar_attn_plan_bytes(plan)
-        plan.workspace = _empty((n,), torch.uint8, q.device, stream)
-        torch.cuda.synchronize()            # what held this memory before is done
-        gar_attn_plan_set_workspace(plan, plan.workspace.data_ptr(), n)
-    if out is None:
-        out = _empty(shape, q.dtype, q.device, stream)
-    if lse is True:
-        lse = _empty((batch, q_heads), torch.float32, q.device, stream)
-    if out.shape != shape:
-        raise ValueError("out must have q's shape")
-    lse_ptr = None
-    if lse is not None and lse is not False:
-        if lse.dtype != torch.float32 or lse.shape != shape[:2] or not lse.is_contiguous() or not lse.is_cuda:
-            raise ValueError("lse must be a contiguous float32 CUDA tensor [batch, q_heads]")
-        lse_ptr = lse.data_ptr()
-    _, os_ = _rows(out, "out")
-    _check(_lib.gar_decode_attention(plan._h, cache._ref, q.data_ptr(), qs[0], qs[1], _dtype_of(q, "q"),
-                                     out.data_ptr(), os_[0], os_[1], _dtype_of(out, "out"), lse_ptr,
-                                     page_table.data_ptr(), ts[0], tshape[1], lengths.data_ptr(), batch,
-                                     plan.default_scale if scale is None else float(scale), int(window), handle),
-           "gar_decode_attention")
-    return out if lse_ptr is None else (out, lse)
+    n = gar_attn_plan_bytes(plan)
+    workspace = torch.empty(n, dtype=torch.uint8, device=like.device)
+    torch.cuda.synchronize()                # what held this memory before is done
+    gar_attn_plan_set_workspace(plan, workspace.data_ptr(), n)
+    plan.workspace = workspace
+
+
+def __getattr__(name):
+    """The calls of a decoding step (gar_rope, gar_kv_write, gar_kv_read, gar_decode_attention) are
+    compiled (csrc/marshal.cpp) and loaded on first use, with torch."""
+    if name in ("gar_rope", "gar_kv_write", "gar_kv_read", "gar_decode_attention"):
+        import torch  # noqa: F401  (its libraries are the module's)
+        from . import _marshal
+        globals()[name] = getattr(_marshal, name)
+        return globals()[name]
+    raise AttributeError(f"module {__name__!r} has no attribute {name!r}")
