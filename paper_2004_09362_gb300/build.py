@@ -117,7 +117,7 @@ def _build(verbose: bool) -> str:
     lib = os.path.join(_torch_dir(), "lib")
     tmp = MARSHAL + f".tmp{os.getpid()}"
     _run(["g++", "-shared", "-o", tmp, marshal_obj, "-L", PKG, "-lgar", "-L", lib, "-ltorch_python", "-ltorch_cpu",
-          "-lc10", "-lc10_cuda", "-Wl,-rpath,$ORIGIN", "-Wl,-rpath," + lib], "link of _marshal.so failed")
+          "-ltorch_cuda", "-lc10", "-lc10_cuda", "-Wl,-rpath,$ORIGIN", "-Wl,-rpath," + lib], "link of _marshal.so failed")
     os.replace(tmp, MARSHAL)
     return OUT
 

@@ -37,7 +37,7 @@ struct DecodeArgs {
   Divide page;
   int most_rows;           // rows that the table's width can hold
   int unit;                // rows of a unit of the line
-  int box_rows;            // rows of a tensor copy
+  int box_shift;           // log2 of the tensor copies that a tile's rows take
   int batch, q_heads, group, item_groups, item_heads;  // group: q_heads / kv_heads
   int q_dtype, out_dtype, window;
   bool out_wide;           // four neighbouring outputs can be stored at once

@@ -146,7 +146,7 @@ template <typename C, int DP, int NG> struct MmaShape {
   static constexpr int VB = DP * EL / 8 < 16 ? DP * EL / 8 : 16;   // bytes of a value chunk
   static constexpr int LINE = DP * EL < 128 ? DP * EL : 128;       // bytes of a row that lie together
   static constexpr int PARTS = DP * EL / LINE;
-  static constexpr int KT = DP * EL <= 128 ? 32 : 16;              // rows of a tile
+  static constexpr int kLogTile = DP * EL <= 128 ? 5 : 4, KT = 1 << kLogTile;  // rows of a tile
   static constexpr int kTile = 2 * KT * DP * EL;                   // bytes, keys and values
   // One CTA per SM; its 192 KB of tiles are divided among as many warps as the registers allow.
   static constexpr int kWarps = kTile > 8192 ? 4 : NG == 1 && DP <= 128 ? 12 : 8;
@@ -220,7 +220,36 @@ __global__ void __launch_bounds__(32 * MmaShape<C, DP, NG>::kWarps, 1)
     int from, lo, to, b, kv_head, tile, step, tiles;
   } get{};
   bool walking = true, ready = false;    // ready: get's tile exists and its pages are known
-  int page = -1;                         // of this lane's row of get's tile
+  // The cache rows of get's tile.  Copied row by row: the page of this lane's row of the tile.  In boxes: this
+  // lane's box (lane % boxes of a tile) of the (lane / boxes)-th of the warp's next tiles, its page and the row
+  // in it, and the same of the tiles after those.
+  struct Rows {
+    int page, row;
+  } rows{-1, 0}, later{-1, 0};
+  int held = 0;                          // boxes: tiles of `rows` that have been copied
+  const int box_shift = BOXES ? a.box_shift : 0, box_tiles = 32 >> box_shift;
+  const auto find_rows = [&](int tile) {
+    int n;
+    Rows x{-1, 0};
+    bool there;
+    if (BOXES) {
+      tile += (lane >> box_shift) * get.step;
+      n = get.from + tile * KT + (lane & ((1 << box_shift) - 1)) * (KT >> box_shift);
+      there = tile < get.tiles && n < get.to && n + (KT >> box_shift) > get.lo;
+    } else {
+      n = get.from + tile * KT + (lane & (KT - 1));
+      there = n >= get.lo && n < get.to;
+    }
+    if (there) {
+      const int p = (int)a.page(n);
+      x.page = a.table[get.b * a.table_stride + p], x.row = n - p * c.page_size;
+      if ((unsigned)x.page >= (uint64_t)c.pages) {
+        x.page = -1;
+        if (c.status) atomicOr(c.status, GAR_KV_BAD_PAGE);
+      }
+    }
+    return x;
+  };
   const auto advance = [&] {
     while (get.tile >= get.tiles && walking && noted - done < kAhead) {
       Walk w = walk;
@@ -244,58 +273,62 @@ __global__ void __launch_bounds__(32 * MmaShape<C, DP, NG>::kWarps, 1)
       get = {x.seg.from, x.seg.lo, x.seg.to, x.seg.b, x.seg.kv_head, x.tile, x.step, x.tiles};
     }
     ready = get.tile < get.tiles;
-    page = -1;
     if (ready) {
-      const int n = get.from + get.tile * KT + (lane & (KT - 1));
-      if (n >= get.lo && n < get.to) page = a.table[get.b * a.table_stride + a.page(n)];
+      rows = find_rows(get.tile);
+      held = 0;
+      if (BOXES) later = find_rows(get.tile + box_tiles * get.step);
     }
   };
-  // Starts the copies of get's tile.
+  // Starts the copies of get's tile and goes to the next.
   const auto issue = [&](int stage) {
-    const int n = get.from + get.tile * KT + (lane & (KT - 1)), r = n - (int)a.page(n) * c.page_size;
-    const bool there = n >= get.lo && n < get.to && (unsigned)page < (uint64_t)c.pages;
-    if (n >= get.lo && n < get.to && !there && c.status) atomicOr(c.status, GAR_KV_BAD_PAGE);
     const uint32_t tile_at = mine_at + stage * S::kTile;
+    const int n = get.from + get.tile * KT + (lane & (KT - 1));
+    int page = rows.page, row = rows.row;
+    if (BOXES) {
+      const int box = (lane & (KT - 1)) >> (S::kLogTile - box_shift), from = (held << box_shift) + box;
+      page = __shfl_sync(~0u, page, from);
+      row = __shfl_sync(~0u, row, from) + (lane & ((KT >> box_shift) - 1));
+    }
+    const bool there = page >= 0 && n >= get.lo && n < get.to;
     if (Q8 && lane < KT) {
-      const int64_t at = there ? page * c.scale_page_stride + r * c.scale_token_stride +
-                                     get.kv_head * c.scale_head_stride : 0;
+      const int64_t at =
+          there ? page * c.scale_page_stride + row * c.scale_token_stride + get.kv_head * c.scale_head_stride : 0;
       const uint32_t to = scales_at + stage * S::kScales + lane * 4;
       copy_async<4>(to, c.k_scale + at, there);
       copy_async<4>(to + KT * 4, c.v_scale + at, there);
     }
     if constexpr (BOXES) {
-      // A box is a.box_rows rows of one page (those outside the segment too).  A page that no
-      // row of the segment is on has number -1 here and is filled with zeros.
+      // A box is rows of one page, those outside the segment too; all of a box that has no page is
+      // filled with zeros.
       const uint32_t bar = barrier + 8 * stage;
       if (lane == 0)
         asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(S::kTile) : "memory");
-      for (int r0 = 0; r0 < KT; r0 += a.box_rows) {
-        const unsigned some = __ballot_sync(~0u, there && (lane & (KT - 1)) / a.box_rows * a.box_rows == r0);
-        const int p = __shfl_sync(~0u, page, some ? __ffs(some) - 1 : 0), row = __shfl_sync(~0u, r, r0);
+      for (int i = 0; i < 1 << box_shift; ++i) {
+        const int p = __shfl_sync(~0u, rows.page, (held << box_shift) + i);
+        const int r = __shfl_sync(~0u, rows.row, (held << box_shift) + i);
         if (lane == 0) {
 #pragma unroll
-          for (int i = 0; i < PARTS; ++i) {
-            const uint32_t to = tile_at + (i * KT + r0) * LINE;
-            copy_box(to, &k_map, i * LINE, row, get.kv_head, some ? p : -1, bar);
-            copy_box(to + KT * DP * EL, &v_map, i * LINE, row, get.kv_head, some ? p : -1, bar);
+          for (int k = 0; k < PARTS; ++k) {
+            const uint32_t to = tile_at + (k * KT + (i * KT >> box_shift)) * LINE;
+            copy_box(to, &k_map, k * LINE, r, get.kv_head, p, bar);
+            copy_box(to + KT * DP * EL, &v_map, k * LINE, r, get.kv_head, p, bar);
           }
         }
       }
-      } else {
-      const int64_t at =
-          there ? (page * c.page_stride + get.kv_head * c.head_stride + r * c.token_stride) * EL : -1;
-        constexpr int LANES = LINE / 16, ROWS = 32 / LANES;
+    } else {
+      const int64_t at = there ? (page * c.page_stride + get.kv_head * c.head_stride + row * c.token_stride) * EL : -1;
+      constexpr int LANES = LINE / 16, ROWS = 32 / LANES;
       const char *const kp = static_cast<const char *>(c.k), *const vp = static_cast<const char *>(c.v);
       const int chunk = lane & (LANES - 1);
 #pragma unroll
       for (int r = 0; r < KT; r += ROWS) {
-        const int row = r + lane / LANES;
-        const int64_t x = __shfl_sync(~0u, at, row);
+        const int to_row = r + lane / LANES;
+        const int64_t x = __shfl_sync(~0u, at, to_row);
 #pragma unroll
         for (int p = 0; p < PARTS; ++p) {
           const int off = p * LINE + chunk * 16;
           const bool in = x >= 0 && off < c.dim * EL;
-          const uint32_t to = tile_at + p * KT * LINE + place<LINE>(row, chunk);
+          const uint32_t to = tile_at + p * KT * LINE + place<LINE>(to_row, chunk);
           copy_async<16>(to, in ? kp + x + off : kp, in);
           copy_async<16>(to + KT * DP * EL, in ? vp + x + off : vp, in);
         }
@@ -303,7 +336,14 @@ __global__ void __launch_bounds__(32 * MmaShape<C, DP, NG>::kWarps, 1)
     }
     if (Q8 || !BOXES) asm volatile("cp.async.commit_group;" ::: "memory");
     get.tile += get.step;
-    advance();
+    if (get.tile >= get.tiles) {
+      advance();
+    } else if (!BOXES) {
+      rows = find_rows(get.tile);
+    } else if (++held == box_tiles) {
+      rows = later, held = 0;
+      later = find_rows(get.tile + box_tiles * get.step);
+    }
   };
   int in = 0, out = 0, flying = 0;  // stages copied into and used next; tiles on their way or here
   uint32_t parity = 0;
@@ -586,10 +626,11 @@ template <typename C, int DP, int NG> int launch_mma(DecodeArgs a, int sms, cuda
   a.item_heads = std::min(a.group, 8 * NG);
   a.item_groups = (a.group + 8 * NG - 1) / (8 * NG);
   // Boxes of as many rows as a page has in a tile: a tile starts at a multiple of KT rows.
-  a.box_rows = a.c.page_size % S::KT == 0 ? S::KT : a.c.page_size % 16 == 0 ? 16 : a.c.page_size % 8 == 0 ? 8 : 0;
+  const int box_rows = a.c.page_size % S::KT == 0 ? S::KT : a.c.page_size % 16 == 0 ? 16 : 8;
+  a.box_shift = box_rows == S::KT ? 0 : box_rows * 2 == S::KT ? 1 : 2;
   CUtensorMap maps[2];
-  const bool boxes = a.box_rows && box_map(a.c, a.c.k, S::LINE, a.box_rows, &maps[0]) &&
-                     box_map(a.c, a.c.v, S::LINE, a.box_rows, &maps[1]);
+  const bool boxes = a.c.page_size % 8 == 0 && box_map(a.c, a.c.k, S::LINE, box_rows, &maps[0]) &&
+                     box_map(a.c, a.c.v, S::LINE, box_rows, &maps[1]);
   const auto kernel = boxes ? mma_kernel<C, DP, NG, true> : mma_kernel<C, DP, NG, false>;
   static const cudaError_t e[2] = {
       cudaFuncSetAttribute(mma_kernel<C, DP, NG, false>, cudaFuncAttributeMaxDynamicSharedMemorySize, S::kShared),

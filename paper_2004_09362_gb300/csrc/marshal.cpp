@@ -5,12 +5,13 @@
 #include <Python.h>
 
 #include <ATen/core/Tensor.h>
-#include <ATen/ops/empty.h>
+#include <ATen/cuda/EmptyTensor.h>
 #include <c10/cuda/CUDAGuard.h>
 #include <c10/cuda/CUDAStream.h>
 #include <torch/csrc/autograd/python_variable.h>
 
 #include <cmath>
+#include <optional>
 #include <stdexcept>
 #include <string>
 
@@ -159,10 +160,9 @@ struct Stream {
   // An output that the call fills: allocated under its stream, so that its memory is not given away
   // while that stream uses it.
   Tensor empty(at::IntArrayRef shape, at::ScalarType type, const Tensor &like) const {
-    const auto options = at::TensorOptions().dtype(type).device(like.device());
-    if (!other) return at::empty(shape, options);
+    if (!other) return at::detail::empty_cuda(shape, type, like.device(), std::nullopt);
     c10::cuda::CUDAStreamGuard guard(c10::cuda::getStreamFromExternal(raw, like.get_device()));
-    return at::empty(shape, options);
+    return at::detail::empty_cuda(shape, type, like.device(), std::nullopt);
   }
 };
 

@@ -513,6 +513,21 @@ def gar_rope_table(count: int, frequencies, magnitude: float = 1.0, first: int =
     return table
 
 
+_status_words = None, 0      # zeros on the GPU, and how many of them caches have taken
+
+
+def _status_word(device):
+    """A zero that no cache has had before (as a tensor, so that it stays allocated)."""
+    global _status_words
+    import torch
+    words, used = _status_words
+    if words is None or used == words.shape[0] or words.device != device:
+        words, used = torch.zeros(1024, dtype=torch.int32, device=device), 0
+        torch.cuda.synchronize()
+    _status_words = words, used + 1
+    return words[used]
+
+
 class KVCache:
     """A paged cache over the caller's tensors (which it keeps alive).
 
@@ -523,33 +538,29 @@ class KVCache:
 
     def __init__(self, k, v, k_scale=None, v_scale=None):
         import torch
-        if k.dim() != 4 or k.shape != v.shape or k.dtype != v.dtype or k.stride() != v.stride():
+        shape, stride = k.shape, k.stride()
+        if len(shape) != 4 or shape != v.shape or k.dtype != v.dtype or stride != v.stride():
             raise ValueError("k and v must be [pages, heads, page_size, dim], alike in shape, dtype and strides")
-        pages, heads, page_size, dim = k.shape
-        if k.stride(3) != 1 and dim > 1:
+        if stride[3] != 1 and shape[3] > 1:
             raise ValueError("the channels of a head must be contiguous")
         dtype = _dtype_of(k, "cache")
         scaled = dtype in (GAR_I8, GAR_E4M3)
         if scaled != (k_scale is not None) or scaled != (v_scale is not None):
             raise ValueError("scales go with the 8-bit types, and only with them")
-        c = gar_kv_cache(k=k.data_ptr(), v=v.data_ptr(), pages=pages, page_stride=k.stride(0),
-                         head_stride=k.stride(1), token_stride=k.stride(2), dtype=dtype, heads=heads,
-                         dim=dim, page_size=page_size)
-        tensors = [k, v]
+        scale_stride, scale_at = (0, 0, 0), (None, None)
         if scaled:
-            if (k_scale.shape != k.shape[:3] or v_scale.shape != k.shape[:3] or k_scale.stride() != v_scale.stride()
+            scale_stride, scale_at = k_scale.stride(), (k_scale.data_ptr(), v_scale.data_ptr())
+            if (k_scale.shape != shape[:3] or v_scale.shape != shape[:3] or scale_stride != v_scale.stride()
                     or k_scale.dtype != torch.float32 or v_scale.dtype != torch.float32):
                 raise ValueError("scales must be float32 [pages, heads, page_size], alike in strides")
-            c.k_scale, c.v_scale = k_scale.data_ptr(), v_scale.data_ptr()
-            c.scale_page_stride, c.scale_head_stride, c.scale_token_stride = k_scale.stride()
-            tensors += [k_scale, v_scale]
-        if not all(t.is_cuda for t in tensors):
+        if not (k.is_cuda and v.is_cuda) or scaled and not (k_scale.is_cuda and v_scale.is_cuda):
             raise ValueError("a cache is of CUDA tensors")
-        self.status = torch.zeros(1, dtype=torch.int32, device=k.device)
-        c.status = self.status.data_ptr()
         self.k, self.v, self.k_scale, self.v_scale = k, v, k_scale, v_scale
-        self.heads, self.dim, self.page_size, self.pages, self.dtype = heads, dim, page_size, pages, dtype
-        self._c = c
+        self.status = _status_word(k.device)
+        self.pages, self.heads, self.page_size, self.dim = shape
+        self.dtype = dtype
+        self._c = c = gar_kv_cache(k.data_ptr(), v.data_ptr(), *scale_at, self.status.data_ptr(), shape[0], *stride[:3],
+                                   *scale_stride, dtype, shape[1], shape[3], shape[2])
         self.address = ctypes.addressof(c)
 
 
