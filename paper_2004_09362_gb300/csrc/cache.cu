@@ -6,7 +6,6 @@
 namespace gar {
 namespace {
 
-constexpr int kChunk = 8;      // channels a lane holds
 constexpr int kThreads = 256;
 
 struct CacheArgs {
@@ -43,65 +42,70 @@ __device__ __forceinline__ bool find(const CacheArgs &a, int64_t slot, int head,
   return true;
 }
 
-// kChunk elements as they lie in memory, and their values.
-template <typename T> struct alignas(sizeof(T) > 1 ? 16 : 8) raw_chunk {
-  uint32_t w[kChunk * sizeof(T) / 4];
+// N elements as they lie in memory, and their values.
+template <typename T, int N> struct alignas(sizeof(T) * N < 16 ? sizeof(T) * N : 16) raw_chunk {
+  uint32_t w[N * sizeof(T) / 4];
 };
-template <typename T> __device__ __forceinline__ void values(const raw_chunk<T> &r, float (&v)[kChunk]) {
+template <typename T, int N> __device__ __forceinline__ void values(const raw_chunk<T, N> &r, float2 (&v)[N / 2]) {
 #pragma unroll
-  for (int k = 0; k < kChunk; k += 2) {
-    float2 x;
-    if constexpr (sizeof(T) == 4)
-      x = make_float2(__uint_as_float(r.w[k]), __uint_as_float(r.w[k + 1]));
-    else if constexpr (sizeof(T) == 2)
-      x = unpack2(r.w[k / 2], T());
-    else
-      x = unpack2((uint16_t)(r.w[k / 4] >> (k & 2) * 8), T());
-    v[k] = x.x, v[k + 1] = x.y;
-  }
-}
-
-template <bool WIDE, typename T> __device__ __forceinline__ void load(const T *p, int from, int dim, float (&v)[kChunk]) {
-  if (WIDE) {
-    values(*reinterpret_cast<const raw_chunk<T> *>(p + from), v);
-  } else {
-#pragma unroll
-    for (int k = 0; k < kChunk; ++k) v[k] = from + k < dim ? to_f32(p[from + k]) : 0.f;
-  }
-}
-
-template <bool WIDE, typename T> __device__ __forceinline__ void store(T *p, int from, int dim, const float (&v)[kChunk]) {
-  if (WIDE) {
-    constexpr int N = sizeof(T) >= 2 ? 16 / sizeof(T) : kChunk;
-#pragma unroll
-    for (int k = 0; k < kChunk; k += N) {
-      pack<T, N> u;
-#pragma unroll
-      for (int e = 0; e < N; ++e) u.e[e] = from_f32<T>(v[k + e]);
-      *reinterpret_cast<pack<T, N> *>(p + from + k) = u;
+  for (int k = 0; k < N; k += 4) {
+    if constexpr (sizeof(T) == 4) {
+      v[k / 2] = make_float2(__uint_as_float(r.w[k]), __uint_as_float(r.w[k + 1]));
+      v[k / 2 + 1] = make_float2(__uint_as_float(r.w[k + 2]), __uint_as_float(r.w[k + 3]));
+    } else if constexpr (sizeof(T) == 2) {
+      v[k / 2] = unpack2(r.w[k / 2], T()), v[k / 2 + 1] = unpack2(r.w[k / 2 + 1], T());
+    } else {
+      unpack4(r.w[k / 4], &v[k / 2], &v[k / 2 + 1], T());
     }
-  } else {
-#pragma unroll
-    for (int k = 0; k < kChunk; ++k)
-      if (from + k < dim) p[from + k] = from_f32<T>(v[k]);
   }
 }
 
-template <bool WIDE, typename T> __device__ __forceinline__ void store_codes(T *p, int from, int dim, const raw_chunk<T> &r) {
+// Channels [from, from + N) of a row, zeros past its end.  WIDE: all are there and aligned.
+template <bool WIDE, typename T, int N> __device__ __forceinline__ void load(const T *p, int from, int dim, float2 (&v)[N / 2]) {
   if (WIDE) {
-    *reinterpret_cast<raw_chunk<T> *>(p + from) = r;
+    values(*reinterpret_cast<const raw_chunk<T, N> *>(p + from), v);
   } else {
 #pragma unroll
-    for (int k = 0; k < kChunk; ++k)
+    for (int k = 0; k < N; k += 2)
+      v[k / 2] = make_float2(from + k < dim ? to_f32(p[from + k]) : 0.f, from + k + 1 < dim ? to_f32(p[from + k + 1]) : 0.f);
+  }
+}
+
+template <bool WIDE, typename T, int N>
+__device__ __forceinline__ void store(T *p, int from, int dim, const float2 (&v)[N / 2]) {
+  if constexpr (WIDE) {
+    raw_chunk<T, N> r;
+#pragma unroll
+    for (int k = 0; k < N; k += 2) {
+      if constexpr (sizeof(T) == 4)
+        r.w[k] = __float_as_uint(v[k / 2].x), r.w[k + 1] = __float_as_uint(v[k / 2].y);
+      else
+        r.w[k / 2] = pack2(v[k / 2], T());
+    }
+    *reinterpret_cast<raw_chunk<T, N> *>(p + from) = r;
+  } else {
+#pragma unroll
+    for (int k = 0; k < N; ++k)
+      if (from + k < dim) p[from + k] = from_f32<T>(k % 2 ? v[k / 2].y : v[k / 2].x);
+  }
+}
+
+template <bool WIDE, typename T, int N>
+__device__ __forceinline__ void store_codes(T *p, int from, int dim, const raw_chunk<T, N> &r) {
+  if (WIDE) {
+    *reinterpret_cast<raw_chunk<T, N> *>(p + from) = r;
+  } else {
+#pragma unroll
+    for (int k = 0; k < N; ++k)
       if (from + k < dim) reinterpret_cast<uint8_t *>(p)[from + k] = (uint8_t)(r.w[k / 4] >> 8 * (k % 4));
   }
 }
 
-// The channels [from, from + kChunk) of a row rotated.  With the half layout the channels they
+// The channels [from, from + N) of a row rotated.  With the half layout the channels they
 // pair with are another lane's; they were read into w as well.
-template <bool WIDE, typename T>
-__device__ __forceinline__ void rotate(const CacheArgs &a, const T *row, int64_t token, int from, float (&v)[kChunk],
-                                       const float (&w)[kChunk]) {
+template <bool WIDE, typename T, int N>
+__device__ __forceinline__ void rotate(const CacheArgs &a, const T *row, int64_t token, int from, float2 (&v)[N / 2],
+                                       const float2 (&w)[N / 2]) {
   const int64_t pos = a.wide_positions ? static_cast<const int64_t *>(a.positions)[token]
                                        : (int64_t) static_cast<const int32_t *>(a.positions)[token];
   const bool good = (uint64_t)pos < (uint64_t)a.table_rows;
@@ -110,38 +114,44 @@ __device__ __forceinline__ void rotate(const CacheArgs &a, const T *row, int64_t
   const float2 *const t = a.table + (good ? pos * half : 0);
   if (WIDE && a.wide_table) {
     if (a.interleaved) {
-      float c[kChunk / 2], s[kChunk / 2];
-      load_rotation<kChunk / 2, true>(t + (good ? from / 2 : 0), good, c, s);
+      float c[N / 2], s[N / 2];
+      load_rotation<N / 2, true>(t + (good ? from / 2 : 0), good, c, s);
 #pragma unroll
-      for (int k = 0; k < kChunk; k += 2) {
-        const float x = v[k], y = v[k + 1];
-        v[k] = __fsub_rn(__fmul_rn(x, c[k / 2]), __fmul_rn(y, s[k / 2]));
-        v[k + 1] = __fadd_rn(__fmul_rn(y, c[k / 2]), __fmul_rn(x, s[k / 2]));
+      for (int k = 0; k < N / 2; ++k) {
+        const float2 x = v[k];
+        v[k].x = __fsub_rn(__fmul_rn(x.x, c[k]), __fmul_rn(x.y, s[k]));
+        v[k].y = __fadd_rn(__fmul_rn(x.y, c[k]), __fmul_rn(x.x, s[k]));
       }
     } else {
       const bool second = from >= half;
-      float c[kChunk], s[kChunk];
-      load_rotation<kChunk, true>(t + (good ? from - (second ? half : 0) : 0), good, c, s);
+      float c[N], s[N];
+      load_rotation<N, true>(t + (good ? from - (second ? half : 0) : 0), good, c, s);
 #pragma unroll
-      for (int k = 0; k < kChunk; ++k) {
-        const float x = __fmul_rn(v[k], c[k]), y = __fmul_rn(w[k], s[k]);
-        v[k] = second ? __fadd_rn(x, y) : __fsub_rn(x, y);
+      for (int k = 0; k < N / 2; ++k) {  // (one by one: paired, the compiler would fuse product and sum)
+        const float2 x = make_float2(__fmul_rn(v[k].x, c[2 * k]), __fmul_rn(v[k].y, c[2 * k + 1]));
+        const float2 y = make_float2(__fmul_rn(w[k].x, s[2 * k]), __fmul_rn(w[k].y, s[2 * k + 1]));
+        v[k].x = second ? __fadd_rn(x.x, y.x) : __fsub_rn(x.x, y.x);
+        v[k].y = second ? __fadd_rn(x.y, y.y) : __fsub_rn(x.y, y.y);
       }
     }
     return;
   }
 #pragma unroll
-  for (int k = 0; k < kChunk; ++k) {
+  for (int k = 0; k < N; ++k) {
     const int c = from + k;
     if (c >= a.rot) break;
     const int pair = a.interleaved ? c / 2 : c < half ? c : c - half;
     const bool second = a.interleaved ? c & 1 : c >= half;
     const int other = a.interleaved ? c ^ 1 : second ? c - half : c + half;
     const float2 cs = good ? __ldg(t + pair) : make_float2(__int_as_float(0x7fc00000), 0.f);
-    const float x = __fmul_rn(v[k], cs.x), y = __fmul_rn(to_f32(row[other]), cs.y);
-    v[k] = second ? __fadd_rn(x, y) : __fsub_rn(x, y);
+    float &x = k % 2 ? v[k / 2].y : v[k / 2].x;
+    const float p = __fmul_rn(x, cs.x), q = __fmul_rn(to_f32(row[other]), cs.y);
+    x = second ? __fadd_rn(p, q) : __fsub_rn(p, q);
   }
 }
+
+// y / s within [-most, most], for rows of tiny scales (out of line: rarely called).
+__device__ __noinline__ float divided(float y, float s, float most) { return fminf(fmaxf(__fdiv_rn(y, s), -most), most); }
 
 // Codes of the row of which this lane holds v, and the row's scale.
 //
@@ -149,46 +159,50 @@ __device__ __forceinline__ void rotate(const CacheArgs &a, const T *row, int64_t
 // nearest and q = v r, the remainder v - q scale is exact in a fused multiply-add, and
 // q + r (v - q scale) is the correctly rounded quotient (P. Markstein, IBM J. Res. Dev. 34, 1990, theorem 8),
 // as long as nothing underflows; rows of scales under 2^-90 divide.
-template <typename C> __device__ __forceinline__ raw_chunk<C> quantise(const float (&v)[kChunk], int lanes, float *scale) {
+template <typename C, int N>
+__device__ __forceinline__ raw_chunk<C, N> quantise(const float2 (&v)[N / 2], int lanes, float *scale) {
   // Magnitudes compare as integers, NaNs and infinities the largest.
   uint32_t most = 0;
 #pragma unroll
-  for (int k = 0; k < kChunk; ++k) most = max(most, __float_as_uint(v[k]) & 0x7fffffffu);
+  for (int k = 0; k < N / 2; ++k)
+    most = max(most, max(__float_as_uint(v[k].x) & 0x7fffffffu, __float_as_uint(v[k].y) & 0x7fffffffu));
   for (int d = lanes / 2; d > 0; d /= 2) most = max(most, __shfl_xor_sync(~0u, most, d));
-  raw_chunk<C> out;
-  float x[kChunk];
+  raw_chunk<C, N> out;
+  float2 x[N / 2];
   const float s = __fmul_rn(__uint_as_float(most), 1.f / quantised<C>::largest);
-  if (most >= 0x7f800000u) {  // an infinity or a NaN in the row: codes 0 under a NaN scale
-    *scale = __int_as_float(0x7fc00000);
-#pragma unroll
-    for (int k = 0; k < kChunk; ++k) x[k] = 0.f;
-  } else {
+  if (most < 0x7f800000u && s >= 0x1p-90f) {
     *scale = s;
     const float r = __frcp_rn(s);
-    if (s >= 0x1p-90f) {
+    const float2 r2 = make_float2(r, r), minus = make_float2(-s, -s);
 #pragma unroll
-      for (int k = 0; k < kChunk; ++k) {
-        const float q = __fmul_rn(v[k], r);
-        x[k] = __fmaf_rn(__fmaf_rn(-q, s, v[k]), r, q);
-      }
-    } else {
+    for (int k = 0; k < N / 2; ++k) {
+      const float2 q = mul2(v[k], r2);
+      x[k] = fma2(fma2(q, minus, v[k]), r2, q);
+    }
+  } else {
+    // An infinity or a NaN in the row: codes 0 under a NaN scale.
+    const bool bad = most >= 0x7f800000u;
+    *scale = bad ? __int_as_float(0x7fc00000) : s;
 #pragma unroll
-      for (int k = 0; k < kChunk; ++k)
-        x[k] = s == 0.f ? 0.f : fminf(fmaxf(__fdiv_rn(v[k], s), -quantised<C>::largest), quantised<C>::largest);
+    for (int k = 0; k < N / 2; ++k) {
+      x[k].x = bad || s == 0.f ? 0.f : divided(v[k].x, s, quantised<C>::largest);
+      x[k].y = bad || s == 0.f ? 0.f : divided(v[k].y, s, quantised<C>::largest);
     }
   }
 #pragma unroll
-  for (int k = 0; k < kChunk; k += 4) out.w[k / 4] = codes4(x[k], x[k + 1], x[k + 2], x[k + 3], C());
+  for (int k = 0; k < N; k += 4) out.w[k / 4] = codes4(x[k / 2].x, x[k / 2].y, x[k / 2 + 1].x, x[k / 2 + 1].y, C());
   return out;
 }
 
-// T -> C rows.  a.lanes neighbouring lanes hold a token's row of one head, kChunk channels of the key
+// T -> C rows.  a.lanes neighbouring lanes hold a token's row of one head, N channels of the key
 // and of the value each, so that the largest magnitudes are found by shuffles and the rows are
-// read once.  Bound by memory: all loads but the table's go out before any is waited for.
-template <typename T, typename C, bool WIDE, bool ROTATE>
+// read once.  All loads but the table's go out before any is waited for.  Near the rate of memory, but
+// with some 100 instructions a row of 128 channels it comes near the rate of issue as well: N = 16 where the
+// channels allow it halves the part of them that finds the rows.
+template <typename T, typename C, int N, bool WIDE, bool ROTATE>
 __global__ void __launch_bounds__(kThreads) write_kernel(const CacheArgs a) {
   const gar_kv_cache &c = a.cache;
-  const int lane = threadIdx.x & (a.lanes - 1), from = lane * kChunk;
+  const int lane = threadIdx.x & (a.lanes - 1), from = lane * N;
   const int i = blockIdx.x * (kThreads / a.lanes) + threadIdx.x / a.lanes;
   const bool any = i < a.rows;
   const int64_t token = any ? a.heads(i) : 0;
@@ -196,81 +210,84 @@ __global__ void __launch_bounds__(kThreads) write_kernel(const CacheArgs a) {
   const int64_t slot = any ? a.slots[token] : -1;
   const T *const k_row = static_cast<const T *>(a.in[0]) + token * a.ts[0] + head * a.hs[0];
   const T *const v_row = static_cast<const T *>(a.in[1]) + token * a.ts[1] + head * a.hs[1];
-  float k[kChunk] = {}, v[kChunk] = {}, w[kChunk];
+  float2 k[N / 2] = {}, v[N / 2] = {}, w[N / 2];
   const bool in = any && from < c.dim, turned = ROTATE && in && from < a.rot;
   if (in) {
-    load<WIDE>(k_row, from, c.dim, k);
-    load<WIDE>(v_row, from, c.dim, v);
+    load<WIDE, T, N>(k_row, from, c.dim, k);
+    load<WIDE, T, N>(v_row, from, c.dim, v);
     if (turned && WIDE && a.wide_table && !a.interleaved) {
       const int half = a.rot / 2;
-      load<WIDE>(k_row, from >= half ? from - half : from + half, c.dim, w);
+      load<WIDE, T, N>(k_row, from >= half ? from - half : from + half, c.dim, w);
     }
   }
   Place p;
   const bool there = find(a, slot, head, &p);
-  if (turned && there) rotate<WIDE>(a, k_row, token, from, k, w);
+  if (turned && there) rotate<WIDE, T, N>(a, k_row, token, from, k, w);
   if constexpr (quantised<C>::value) {
     float k_scale, v_scale;
-    const raw_chunk<C> k_codes = quantise<C>(k, a.lanes, &k_scale), v_codes = quantise<C>(v, a.lanes, &v_scale);
+    const raw_chunk<C, N> k_codes = quantise<C, N>(k, a.lanes, &k_scale), v_codes = quantise<C, N>(v, a.lanes, &v_scale);
     if (there && lane == 0) c.k_scale[p.scale] = k_scale, c.v_scale[p.scale] = v_scale;
     if (in && there) {
       store_codes<WIDE>(static_cast<C *>(c.k) + p.at, from, c.dim, k_codes);
       store_codes<WIDE>(static_cast<C *>(c.v) + p.at, from, c.dim, v_codes);
     }
   } else if (in && there) {
-    store<WIDE>(static_cast<C *>(c.k) + p.at, from, c.dim, k);
-    store<WIDE>(static_cast<C *>(c.v) + p.at, from, c.dim, v);
+    store<WIDE, C, N>(static_cast<C *>(c.k) + p.at, from, c.dim, k);
+    store<WIDE, C, N>(static_cast<C *>(c.v) + p.at, from, c.dim, v);
   }
 }
 
-// C -> T rows, N of them to a lane: a row's place hangs on its slot, so there are fewer bytes in flight.
-template <typename T, typename C, bool WIDE, int N>
+// C -> T rows, M of them to a lane: a row's place hangs on its slot, so that fewer bytes would be in flight.
+template <typename T, typename C, int N, bool WIDE, int M>
 __global__ void __launch_bounds__(kThreads) read_kernel(const CacheArgs a) {
   const gar_kv_cache &c = a.cache;
-  const int lane = threadIdx.x & (a.lanes - 1), from = lane * kChunk, step = kThreads / a.lanes;
-  const int i0 = blockIdx.x * (step * N) + threadIdx.x / a.lanes;
+  const int lane = threadIdx.x & (a.lanes - 1), from = lane * N, step = kThreads / a.lanes;
+  const int i0 = blockIdx.x * (step * M) + threadIdx.x / a.lanes;
   if (from >= c.dim) return;
-  Place p[N];
-  bool there[N];
+  Place p[M];
+  bool there[M];
 #pragma unroll
-  for (int n = 0; n < N; ++n) {
-    const int i = i0 + n * step;
+  for (int m = 0; m < M; ++m) {
+    const int i = i0 + m * step;
     const int token = i < a.rows ? a.heads(i) : 0;
-    there[n] = i < a.rows && find(a, a.slots[token], i - token * c.heads, &p[n]);
+    there[m] = i < a.rows && find(a, a.slots[token], i - token * c.heads, &p[m]);
   }
-  raw_chunk<C> k[N], v[N];
-  float k_scale[N], v_scale[N];
+  raw_chunk<C, N> k[M], v[M];
+  float k_scale[M], v_scale[M];
 #pragma unroll
-  for (int n = 0; n < N; ++n) {
-    k_scale[n] = v_scale[n] = 0.f;
-    if (there[n]) {
+  for (int m = 0; m < M; ++m) {
+    k_scale[m] = v_scale[m] = 0.f;
+    if (there[m]) {
       if (WIDE) {
-        k[n] = *reinterpret_cast<const raw_chunk<C> *>(static_cast<const C *>(c.k) + p[n].at + from);
-        v[n] = *reinterpret_cast<const raw_chunk<C> *>(static_cast<const C *>(c.v) + p[n].at + from);
+        k[m] = *reinterpret_cast<const raw_chunk<C, N> *>(static_cast<const C *>(c.k) + p[m].at + from);
+        v[m] = *reinterpret_cast<const raw_chunk<C, N> *>(static_cast<const C *>(c.v) + p[m].at + from);
       }
-      if (quantised<C>::value) k_scale[n] = c.k_scale[p[n].scale], v_scale[n] = c.v_scale[p[n].scale];
+      if (quantised<C>::value) k_scale[m] = c.k_scale[p[m].scale], v_scale[m] = c.v_scale[p[m].scale];
     }
   }
 #pragma unroll
-  for (int n = 0; n < N; ++n) {
-    const int64_t i = i0 + n * step;
+  for (int m = 0; m < M; ++m) {
+    const int64_t i = i0 + m * step;
     if (i >= a.rows) break;
-    float x[kChunk] = {}, y[kChunk] = {};
-    if (there[n]) {
+    float2 x[N / 2] = {}, y[N / 2] = {};
+    if (there[m]) {
       if (WIDE) {
-        values(k[n], x);
-        values(v[n], y);
+        values(k[m], x);
+        values(v[m], y);
       } else {
-        load<WIDE>(static_cast<const C *>(c.k) + p[n].at, from, c.dim, x);
-        load<WIDE>(static_cast<const C *>(c.v) + p[n].at, from, c.dim, y);
+        load<WIDE, C, N>(static_cast<const C *>(c.k) + p[m].at, from, c.dim, x);
+        load<WIDE, C, N>(static_cast<const C *>(c.v) + p[m].at, from, c.dim, y);
       }
     }
     if (quantised<C>::value) {
 #pragma unroll
-      for (int e = 0; e < kChunk; ++e) x[e] = __fmul_rn(x[e], k_scale[n]), y[e] = __fmul_rn(y[e], v_scale[n]);
+      for (int e = 0; e < N / 2; ++e) {
+        x[e] = mul2(x[e], make_float2(k_scale[m], k_scale[m]));
+        y[e] = mul2(y[e], make_float2(v_scale[m], v_scale[m]));
+      }
     }
-    store<WIDE>(static_cast<T *>(a.out[0]) + i * c.dim, from, c.dim, x);
-    store<WIDE>(static_cast<T *>(a.out[1]) + i * c.dim, from, c.dim, y);
+    store<WIDE, T, N>(static_cast<T *>(a.out[0]) + i * c.dim, from, c.dim, x);
+    store<WIDE, T, N>(static_cast<T *>(a.out[1]) + i * c.dim, from, c.dim, y);
   }
 }
 
@@ -291,9 +308,9 @@ int check_rows(const gar_kv_cache *cache, int dtype, int64_t tokens) {
   return GAR_OK;
 }
 
-// Sets the rows and lanes; false where the rows are too many.
-bool shape(CacheArgs *a, int64_t tokens) {
-  const int need = (a->cache.dim + kChunk - 1) / kChunk;
+// Sets the rows and the lanes of N channels each; false where the rows are too many.
+bool shape(CacheArgs *a, int64_t tokens, int n) {
+  const int need = (a->cache.dim + n - 1) / n;
   a->lanes = 1;
   while (a->lanes < need) a->lanes *= 2;
   if (tokens > 0x7fffffff / 2 / a->cache.heads) return false;
@@ -308,11 +325,17 @@ int blocks(const CacheArgs &a, int rows_per_lane) {
   return (a.rows + per - 1) / per;
 }
 
-// 16 bytes of `size`-byte elements (8 of one byte) at every multiple of kChunk channels.
-bool wide_cache(const gar_kv_cache &c) {
-  const uintptr_t a = element_size(c.dtype) == 1 ? 8 : 16;
-  return (uintptr_t)c.k % a == 0 && (uintptr_t)c.v % a == 0 && c.dim % kChunk == 0 && c.page_stride % kChunk == 0 &&
-         c.head_stride % kChunk == 0 && c.token_stride % kChunk == 0;
+// Whether every n channels of the cache (n: 8 or 16) can be accessed as raw_chunk.
+bool wide_cache(const gar_kv_cache &c, int n) {
+  const uintptr_t a = std::min(16, element_size(c.dtype) * n);
+  return (uintptr_t)c.k % a == 0 && (uintptr_t)c.v % a == 0 && c.dim % n == 0 && c.page_stride % n == 0 &&
+         c.head_stride % n == 0 && c.token_stride % n == 0;
+}
+
+// The channels of a lane: 16 where the cache's are 8-bit codes and there are rows enough to fill the GPU
+// four times over with half the lanes, else 8.
+int lane_channels(const gar_kv_cache &c, int64_t tokens) {
+  return element_size(c.dtype) == 1 && wide_cache(c, 16) && tokens * c.heads * (c.dim / 16) >= 152 * 2048 ? 16 : 8;
 }
 
 }  // namespace
@@ -366,16 +389,21 @@ int gar_kv_write(const gar_kv_cache *cache, const void *k, int64_t k_token_strid
   a.slots = slots, a.positions = positions, a.table = reinterpret_cast<const float2 *>(table);
   a.table_rows = table_rows, a.rot = rot, a.interleaved = layout == GAR_ROPE_INTERLEAVED;
   a.wide_positions = position_bytes == 8;
-  if (!shape(&a, tokens)) return refuse("too many rows");
   const int n = 16 / size;
-  a.wide_table = (uintptr_t)table % 16 == 0 && rot % (a.interleaved ? kChunk : 2 * kChunk) == 0;
-  const bool wide = wide_cache(*cache) && (uintptr_t)k % 16 == 0 && (uintptr_t)v % 16 == 0 && k_token_stride % n == 0 &&
-                    k_head_stride % n == 0 && v_token_stride % n == 0 && v_head_stride % n == 0;
+  const bool rows_wide = (uintptr_t)k % 16 == 0 && (uintptr_t)v % 16 == 0 && k_token_stride % n == 0 &&
+                         k_head_stride % n == 0 && v_token_stride % n == 0 && v_head_stride % n == 0;
+  const int channels = rows_wide && (!positions || rot % 32 == 0) ? lane_channels(*cache, tokens) : 8;
+  const bool wide = rows_wide && wide_cache(*cache, channels);
+  if (!shape(&a, tokens, channels)) return refuse("too many rows");
+  a.wide_table = (uintptr_t)table % 16 == 0 && rot % (a.interleaved ? channels : 2 * channels) == 0;
   return with_types(dtype, cache->dtype, [&](auto t, auto c) {
     using T = typename decltype(t)::type;
     using C = typename decltype(c)::type;
-    const auto kernel = wide ? (positions ? write_kernel<T, C, true, true> : write_kernel<T, C, true, false>)
-                             : (positions ? write_kernel<T, C, false, true> : write_kernel<T, C, false, false>);
+    auto kernel = wide ? (positions ? write_kernel<T, C, 8, true, true> : write_kernel<T, C, 8, true, false>)
+                       : (positions ? write_kernel<T, C, 8, false, true> : write_kernel<T, C, 8, false, false>);
+    if constexpr (quantised<C>::value) {
+      if (channels == 16) kernel = positions ? write_kernel<T, C, 16, true, true> : write_kernel<T, C, 16, true, false>;
+    }
     kernel<<<blocks(a, 1), kThreads, 0, (cudaStream_t)stream>>>(a);
     return launched("write_kernel");
   });
@@ -394,17 +422,24 @@ int gar_kv_read(const gar_kv_cache *cache, const int64_t *slots, int64_t tokens,
   CacheArgs a{};
   a.cache = *cache;
   a.out[0] = k, a.out[1] = v, a.slots = slots;
-  if (!shape(&a, tokens)) return refuse("too many rows");
-  const bool wide = wide_cache(*cache) && (uintptr_t)k % 16 == 0 && (uintptr_t)v % 16 == 0;
+  const bool rows_wide = (uintptr_t)k % 16 == 0 && (uintptr_t)v % 16 == 0;
+  const int channels = rows_wide ? lane_channels(*cache, tokens) : 8;
+  const bool wide = rows_wide && wide_cache(*cache, channels) && (int64_t)cache->dim * size % 16 == 0;
+  if (!shape(&a, tokens, channels)) return refuse("too many rows");
   return with_types(dtype, cache->dtype, [&](auto t, auto c) {
     using T = typename decltype(t)::type;
     using C = typename decltype(c)::type;
-    if (!wide)
-      read_kernel<T, C, false, 1><<<blocks(a, 1), kThreads, 0, (cudaStream_t)stream>>>(a);
-    else if (blocks(a, 4) < 152 * 4)   // too few CTAs to fill the GPU with four rows a lane
-      read_kernel<T, C, true, 1><<<blocks(a, 1), kThreads, 0, (cudaStream_t)stream>>>(a);
-    else
-      read_kernel<T, C, true, 4><<<blocks(a, 4), kThreads, 0, (cudaStream_t)stream>>>(a);
+    auto kernel = wide ? read_kernel<T, C, 8, true, 1> : read_kernel<T, C, 8, false, 1>;
+    int rows = 1;
+    if (wide && blocks(a, 4) >= 152 * 2) {  // CTAs enough to fill the GPU with four rows a lane
+      kernel = read_kernel<T, C, 8, true, 4>, rows = 4;
+      if constexpr (quantised<C>::value) {
+        if (channels == 16) kernel = read_kernel<T, C, 16, true, 4>;
+      }
+    } else if constexpr (quantised<C>::value) {
+      if (channels == 16) kernel = read_kernel<T, C, 16, true, 1>;
+    }
+    kernel<<<blocks(a, rows), kThreads, 0, (cudaStream_t)stream>>>(a);
     return launched("read_kernel");
   });
 }

@@ -36,14 +36,38 @@ template <> __device__ __forceinline__ __nv_bfloat16 from_f32<__nv_bfloat16>(flo
   return __float2bfloat16_rn(x);
 }
 template <> __device__ __forceinline__ __half from_f32<__half>(float x) { return __float2half_rn(x); }
+// Two 32-bit operations in one instruction, each rounded as the single one.
+__device__ __forceinline__ float2 mul2(float2 a, float2 b) {
+  float2 r;
+  asm("{.reg .b64 x, y; mov.b64 x, {%2, %3}; mov.b64 y, {%4, %5}; mul.rn.f32x2 x, x, y; mov.b64 {%0, %1}, x;}"
+      : "=f"(r.x), "=f"(r.y)
+      : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+  return r;
+}
+__device__ __forceinline__ float2 add2(float2 a, float2 b) {
+  float2 r;
+  asm("{.reg .b64 x, y; mov.b64 x, {%2, %3}; mov.b64 y, {%4, %5}; add.rn.f32x2 x, x, y; mov.b64 {%0, %1}, x;}"
+      : "=f"(r.x), "=f"(r.y)
+      : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+  return r;
+}
+__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
+  float2 r;
+  asm("{.reg .b64 x, y, z; mov.b64 x, {%2, %3}; mov.b64 y, {%4, %5}; mov.b64 z, {%6, %7}; fma.rn.f32x2 x, x, y, z; "
+      "mov.b64 {%0, %1}, x;}"
+      : "=f"(r.x), "=f"(r.y)
+      : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y), "f"(c.x), "f"(c.y));
+  return r;
+}
+
 // Four 8-bit codes of values within the type's range (a rounding error over it counts as within), to
 // the nearest, ties to even.
 __device__ __forceinline__ uint32_t codes4(float a, float b, float c, float d, i8) {
   // Adding 1.5 * 2^23 rounds to an integer and leaves it in the low bits.
-  const float big = 12582912.f;
-  const uint32_t x = __byte_perm(__float_as_uint(__fadd_rn(a, big)), __float_as_uint(__fadd_rn(b, big)), 0x0040);
-  const uint32_t y = __byte_perm(__float_as_uint(__fadd_rn(c, big)), __float_as_uint(__fadd_rn(d, big)), 0x0040);
-  return __byte_perm(x, y, 0x5410);
+  const float2 big = make_float2(12582912.f, 12582912.f);
+  const float2 ab = add2(make_float2(a, b), big), cd = add2(make_float2(c, d), big);
+  return __byte_perm(__byte_perm(__float_as_uint(ab.x), __float_as_uint(ab.y), 0x0040),
+                     __byte_perm(__float_as_uint(cd.x), __float_as_uint(cd.y), 0x0040), 0x5410);
 }
 __device__ __forceinline__ uint32_t codes4(float a, float b, float c, float d, e4m3) {
   uint16_t x, y;
@@ -79,13 +103,19 @@ __device__ __forceinline__ float2 unpack2(uint32_t x, __nv_bfloat16) {
   return make_float2(__uint_as_float(x << 16), __uint_as_float(x & 0xffff0000u));
 }
 __device__ __forceinline__ float2 unpack2(uint32_t x, __half) { return __half22float2(*reinterpret_cast<__half2 *>(&x)); }
-__device__ __forceinline__ float2 unpack2(uint16_t x, i8) {
-  return make_float2((float)(int8_t)(x & 0xff), (float)(int8_t)(x >> 8));
+// Four 8-bit codes' values.
+__device__ __forceinline__ void unpack4(uint32_t x, float2 *ab, float2 *cd, i8) {
+  // 0x4b000000 + u is 2^23 + u; with u = code + 128, taking away 2^23 + 128 leaves the code.
+  const uint32_t u = x ^ 0x80808080u, e = 0x4b000000u;
+  const float2 off = make_float2(-8388736.f, -8388736.f);
+  *ab = add2(make_float2(__uint_as_float(__byte_perm(u, e, 0x7440)), __uint_as_float(__byte_perm(u, e, 0x7441))), off);
+  *cd = add2(make_float2(__uint_as_float(__byte_perm(u, e, 0x7442)), __uint_as_float(__byte_perm(u, e, 0x7443))), off);
 }
-__device__ __forceinline__ float2 unpack2(uint16_t x, e4m3) {
-  uint32_t h2;
-  asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(h2) : "h"(x));
-  return __half22float2(*reinterpret_cast<__half2 *>(&h2));
+__device__ __forceinline__ void unpack4(uint32_t x, float2 *ab, float2 *cd, e4m3) {
+  uint32_t l, h;
+  asm("{.reg .b16 a, b; mov.b32 {a, b}, %2; cvt.rn.f16x2.e4m3x2 %0, a; cvt.rn.f16x2.e4m3x2 %1, b;}" : "=r"(l), "=r"(h) : "r"(x));
+  *ab = __half22float2(*reinterpret_cast<__half2 *>(&l));
+  *cd = __half22float2(*reinterpret_cast<__half2 *>(&h));
 }
 __device__ __forceinline__ uint32_t pack2(float2 x, __nv_bfloat16) {
   const __nv_bfloat162 y = __floats2bfloat162_rn(x.x, x.y);
