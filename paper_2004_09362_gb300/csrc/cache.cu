@@ -7,6 +7,7 @@ namespace gar {
 namespace {
 
 constexpr int kThreads = 256;
+constexpr int kReadRows = 4;   // rows of a lane where there are many
 
 struct CacheArgs {
   gar_kv_cache cache;
@@ -17,10 +18,10 @@ struct CacheArgs {
   const void *positions;
   const float2 *table;
   int64_t table_rows;
-  int rows;                    // tokens * heads
+  int rows;                    // tokens * heads; writing: tokens * runs
+  int run, runs;               // writing: heads that the same lanes take, and such runs of a token
   int rot, interleaved, wide_positions;
   int lanes;                   // power of two: lanes that hold one row
-  bool wide_table;             // a chunk's table entries lie at multiples of 16 bytes
   Divide heads, page;
 };
 
@@ -101,139 +102,225 @@ __device__ __forceinline__ void store_codes(T *p, int from, int dim, const raw_c
   }
 }
 
-// The channels [from, from + N) of a row rotated.  With the half layout the channels they
-// pair with are another lane's; they were read into w as well.
-template <bool WIDE, typename T, int N>
-__device__ __forceinline__ void rotate(const CacheArgs &a, const T *row, int64_t token, int from, float2 (&v)[N / 2],
-                                       const float2 (&w)[N / 2]) {
+// How keys are rotated: not at all; by the half layout, a lane's channels half of them from each side; by the
+// interleaved layout; any way, channel by channel.
+enum { TURN_NONE, TURN_HALF, TURN_PAIRS, TURN_ANY };
+
+// A token's row of the table, null where the position is outside (and stands for NaN).
+__device__ __forceinline__ const float2 *find_turn(const CacheArgs &a, int64_t token) {
   const int64_t pos = a.wide_positions ? static_cast<const int64_t *>(a.positions)[token]
                                        : (int64_t) static_cast<const int32_t *>(a.positions)[token];
-  const bool good = (uint64_t)pos < (uint64_t)a.table_rows;
-  if (!good && a.cache.status) atomicOr(a.cache.status, GAR_KV_BAD_POSITION);
-  const int half = a.rot / 2;
-  const float2 *const t = a.table + (good ? pos * half : 0);
-  if (WIDE && a.wide_table) {
-    if (a.interleaved) {
-      float c[N / 2], s[N / 2];
-      load_rotation<N / 2, true>(t + (good ? from / 2 : 0), good, c, s);
+  if ((uint64_t)pos < (uint64_t)a.table_rows) return a.table + pos * (a.rot / 2);
+  if (a.cache.status) atomicOr(a.cache.status, GAR_KV_BAD_POSITION);
+  return nullptr;
+}
+
+// A lane's channels rotated, by the entries c and s of their pairs.
+template <int TURN, typename T, int N, int E>
+__device__ __forceinline__ void rotate(const CacheArgs &a, const float2 *t, const float (&c)[E], const float (&s)[E],
+                                       const T *row, int from, float2 (&v)[N / 2]) {
+  if constexpr (TURN == TURN_PAIRS) {
 #pragma unroll
-      for (int k = 0; k < N / 2; ++k) {
-        const float2 x = v[k];
-        v[k].x = __fsub_rn(__fmul_rn(x.x, c[k]), __fmul_rn(x.y, s[k]));
-        v[k].y = __fadd_rn(__fmul_rn(x.y, c[k]), __fmul_rn(x.x, s[k]));
-      }
-    } else {
-      const bool second = from >= half;
-      float c[N], s[N];
-      load_rotation<N, true>(t + (good ? from - (second ? half : 0) : 0), good, c, s);
-#pragma unroll
-      for (int k = 0; k < N / 2; ++k) {  // (one by one: paired, the compiler would fuse product and sum)
-        const float2 x = make_float2(__fmul_rn(v[k].x, c[2 * k]), __fmul_rn(v[k].y, c[2 * k + 1]));
-        const float2 y = make_float2(__fmul_rn(w[k].x, s[2 * k]), __fmul_rn(w[k].y, s[2 * k + 1]));
-        v[k].x = second ? __fadd_rn(x.x, y.x) : __fsub_rn(x.x, y.x);
-        v[k].y = second ? __fadd_rn(x.y, y.y) : __fsub_rn(x.y, y.y);
-      }
+    for (int k = 0; k < N / 2; ++k) {
+      const float2 x = v[k];
+      v[k].x = __fsub_rn(__fmul_rn(x.x, c[k]), __fmul_rn(x.y, s[k]));
+      v[k].y = __fadd_rn(__fmul_rn(x.y, c[k]), __fmul_rn(x.x, s[k]));
     }
-    return;
-  }
+  } else if constexpr (TURN == TURN_HALF) {
 #pragma unroll
-  for (int k = 0; k < N; ++k) {
-    const int c = from + k;
-    if (c >= a.rot) break;
-    const int pair = a.interleaved ? c / 2 : c < half ? c : c - half;
-    const bool second = a.interleaved ? c & 1 : c >= half;
-    const int other = a.interleaved ? c ^ 1 : second ? c - half : c + half;
-    const float2 cs = good ? __ldg(t + pair) : make_float2(__int_as_float(0x7fc00000), 0.f);
-    float &x = k % 2 ? v[k / 2].y : v[k / 2].x;
-    const float p = __fmul_rn(x, cs.x), q = __fmul_rn(to_f32(row[other]), cs.y);
-    x = second ? __fadd_rn(p, q) : __fsub_rn(p, q);
+    for (int k = 0; k < N / 4; ++k) {  // (one by one: paired, the compiler would fuse product and sum)
+      const float2 x = v[k], y = v[k + N / 4];
+      v[k].x = __fsub_rn(__fmul_rn(x.x, c[2 * k]), __fmul_rn(y.x, s[2 * k]));
+      v[k].y = __fsub_rn(__fmul_rn(x.y, c[2 * k + 1]), __fmul_rn(y.y, s[2 * k + 1]));
+      v[k + N / 4].x = __fadd_rn(__fmul_rn(y.x, c[2 * k]), __fmul_rn(x.x, s[2 * k]));
+      v[k + N / 4].y = __fadd_rn(__fmul_rn(y.y, c[2 * k + 1]), __fmul_rn(x.y, s[2 * k + 1]));
+    }
+  } else {
+    const int half = a.rot / 2;
+#pragma unroll
+    for (int k = 0; k < N; ++k) {
+      const int at = from + k;
+      if (at >= a.rot) break;
+      const int pair = a.interleaved ? at / 2 : at < half ? at : at - half;
+      const bool second = a.interleaved ? at & 1 : at >= half;
+      const int other = a.interleaved ? at ^ 1 : second ? at - half : at + half;
+      const float2 cs = t ? __ldg(t + pair) : make_float2(__int_as_float(0x7fc00000), 0.f);
+      float &x = k % 2 ? v[k / 2].y : v[k / 2].x;
+      const float p = __fmul_rn(x, cs.x), q = __fmul_rn(to_f32(row[other]), cs.y);
+      x = second ? __fadd_rn(p, q) : __fsub_rn(p, q);
+    }
   }
 }
 
-// y / s within [-most, most], for rows of tiny scales (out of line: rarely called).
-__device__ __noinline__ float divided(float y, float s, float most) { return fminf(fmaxf(__fdiv_rn(y, s), -most), most); }
+// The largest magnitude of N values as the bits of a float: magnitudes compare as integers, infinities
+// and NaNs the largest.
+template <int N> __device__ __forceinline__ uint32_t largest(const float2 (&v)[N]) {
+  uint32_t most = 0;
+#pragma unroll
+  for (int k = 0; k < N; ++k)
+    most = max(most, max(__float_as_uint(v[k].x) & 0x7fffffffu, __float_as_uint(v[k].y) & 0x7fffffffu));
+  return most;
+}
+// The same of 16-bit floats as they lie in memory, two a word.
+template <typename T, int N> __device__ __forceinline__ uint32_t largest(const raw_chunk<T, N> &r) {
+  static_assert(sizeof(T) == 2, "16-bit floats");
+  uint32_t m = r.w[0] & 0x7fff7fffu;
+#pragma unroll
+  for (int k = 1; k < N / 2; ++k) m = __vmaxu2(m, r.w[k] & 0x7fff7fffu);
+  const float2 x = unpack2(m, T());
+  return max(__float_as_uint(x.x), __float_as_uint(x.y));
+}
 
-// Codes of the row of which this lane holds v, and the row's scale.
+// 1 / s rounded to nearest, for normal s whose reciprocal is normal.  One Newton step from a reciprocal that is off by at
+// most one unit rounds correctly but for significands of all ones (Markstein, the same paper), whose
+// reciprocal is one unit over a power of two.  (The rounded reciprocal as a call would cost the kernel its registers.)
+__device__ __forceinline__ float reciprocal(float s) {
+  float r;
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(s));
+  r = __fmaf_rn(__fmaf_rn(-s, r, 1.f), r, r);
+  const uint32_t b = __float_as_uint(s);
+  return (b & 0x7fffffu) == 0x7fffffu ? __uint_as_float((253u << 23) - (b & 0x7f800000u) + 1) : r;
+}
+
+// Codes of the row of which this lane holds v, `most` the largest of them, and the row's scale.
 //
 // v / scale is rounded as the definition has it, without a division each: for r = 1 / scale rounded to
 // nearest and q = v r, the remainder v - q scale is exact in a fused multiply-add, and
-// q + r (v - q scale) is the correctly rounded quotient (P. Markstein, IBM J. Res. Dev. 34, 1990, theorem 8),
-// as long as nothing underflows; rows of scales under 2^-90 divide.
+// q + r (v - q scale) is the correctly rounded quotient (P. Markstein, IBM J. Res. Dev. 34, 1990),
+// as long as nothing underflows; rows of scales under 2^-90 are multiplied by 2^100 first.  Codes of a row with
+// an infinity or a NaN mean nothing: its scale is a NaN.
 template <typename C, int N>
-__device__ __forceinline__ raw_chunk<C, N> quantise(const float2 (&v)[N / 2], int lanes, float *scale) {
-  // Magnitudes compare as integers, NaNs and infinities the largest.
-  uint32_t most = 0;
-#pragma unroll
-  for (int k = 0; k < N / 2; ++k)
-    most = max(most, max(__float_as_uint(v[k].x) & 0x7fffffffu, __float_as_uint(v[k].y) & 0x7fffffffu));
+__device__ __forceinline__ raw_chunk<C, N> quantise(float2 (&v)[N / 2], uint32_t most, int lanes, float *scale) {
   for (int d = lanes / 2; d > 0; d /= 2) most = max(most, __shfl_xor_sync(~0u, most, d));
-  raw_chunk<C, N> out;
-  float2 x[N / 2];
-  const float s = __fmul_rn(__uint_as_float(most), 1.f / quantised<C>::largest);
-  if (most < 0x7f800000u && s >= 0x1p-90f) {
-    *scale = s;
-    const float r = __frcp_rn(s);
-    const float2 r2 = make_float2(r, r), minus = make_float2(-s, -s);
+  float s = __fmul_rn(__uint_as_float(most), 1.f / quantised<C>::largest);
+  *scale = most >= 0x7f800000u ? __int_as_float(0x7fc00000) : s;
+  const bool tiny = s < 0x1p-90f;
+  if (tiny) {
+    s *= 0x1p100f;
 #pragma unroll
-    for (int k = 0; k < N / 2; ++k) {
-      const float2 q = mul2(v[k], r2);
-      x[k] = fma2(fma2(q, minus, v[k]), r2, q);
-    }
-  } else {
-    // An infinity or a NaN in the row: codes 0 under a NaN scale.
-    const bool bad = most >= 0x7f800000u;
-    *scale = bad ? __int_as_float(0x7fc00000) : s;
-#pragma unroll
-    for (int k = 0; k < N / 2; ++k) {
-      x[k].x = bad || s == 0.f ? 0.f : divided(v[k].x, s, quantised<C>::largest);
-      x[k].y = bad || s == 0.f ? 0.f : divided(v[k].y, s, quantised<C>::largest);
-    }
+    for (int k = 0; k < N / 2; ++k) v[k] = mul2(v[k], make_float2(0x1p100f, 0x1p100f));
   }
+  const float r = s > 0.f ? reciprocal(s) : 0.f;
+  const float2 r2 = make_float2(r, r), minus = make_float2(-s, -s);
 #pragma unroll
-  for (int k = 0; k < N; k += 4) out.w[k / 4] = codes4(x[k / 2].x, x[k / 2].y, x[k / 2 + 1].x, x[k / 2 + 1].y, C());
+  for (int k = 0; k < N / 2; ++k) {
+    const float2 q = mul2(v[k], r2);
+    v[k] = fma2(fma2(q, minus, v[k]), r2, q);
+  }
+  if (tiny) {  // a subnormal scale may be rounded far down
+    constexpr float top = quantised<C>::largest;
+#pragma unroll
+    for (int k = 0; k < N / 2; ++k)
+      v[k] = make_float2(fminf(fmaxf(v[k].x, -top), top), fminf(fmaxf(v[k].y, -top), top));
+  }
+  raw_chunk<C, N> out;
+#pragma unroll
+  for (int k = 0; k < N; k += 4) out.w[k / 4] = codes4(v[k / 2].x, v[k / 2].y, v[k / 2 + 1].x, v[k / 2 + 1].y, C());
   return out;
 }
 
 // T -> C rows.  a.lanes neighbouring lanes hold a token's row of one head, N channels of the key
 // and of the value each, so that the largest magnitudes are found by shuffles and the rows are
-// read once.  All loads but the table's go out before any is waited for.  Near the rate of memory, but
-// with some 100 instructions a row of 128 channels it comes near the rate of issue as well: N = 16 where the
-// channels allow it halves the part of them that finds the rows.
-template <typename T, typename C, int N, bool WIDE, bool ROTATE>
-__global__ void __launch_bounds__(kThreads) write_kernel(const CacheArgs a) {
+// read once.  With RUN they take a.run heads of the token one after the other, the next one's loads in flight while
+// one is worked on: the slot is looked up and the table's entries are read (512 bytes for rows of 256) once for
+// all of them.  Bound by memory, not far from the rate of issue; the registers are held down to
+// keep 32 warps an SM, which was worth up to a third of the time.
+template <typename T, typename C, int N, bool RUN, bool WIDE, int TURN>
+__global__ void __launch_bounds__(kThreads, RUN ? 4 : 1) write_kernel(const CacheArgs a) {
+  static_assert(N == 8, "two words of codes, a half of a chunk each");
   const gar_kv_cache &c = a.cache;
   const int lane = threadIdx.x & (a.lanes - 1), from = lane * N;
   const int i = blockIdx.x * (kThreads / a.lanes) + threadIdx.x / a.lanes;
   const bool any = i < a.rows;
   const int64_t token = any ? a.heads(i) : 0;
-  const int head = any ? i - (int)token * c.heads : 0;
+  const int first = any ? (i - (int)token * a.runs) * a.run : 0, end = any ? min(first + a.run, c.heads) : 0;
   const int64_t slot = any ? a.slots[token] : -1;
-  const T *const k_row = static_cast<const T *>(a.in[0]) + token * a.ts[0] + head * a.hs[0];
-  const T *const v_row = static_cast<const T *>(a.in[1]) + token * a.ts[1] + head * a.hs[1];
-  float2 k[N / 2] = {}, v[N / 2] = {}, w[N / 2];
-  const bool in = any && from < c.dim, turned = ROTATE && in && from < a.rot;
-  if (in) {
-    load<WIDE, T, N>(k_row, from, c.dim, k);
-    load<WIDE, T, N>(v_row, from, c.dim, v);
-    if (turned && WIDE && a.wide_table && !a.interleaved) {
-      const int half = a.rot / 2;
-      load<WIDE, T, N>(k_row, from >= half ? from - half : from + half, c.dim, w);
+  const T *const k_rows = static_cast<const T *>(a.in[0]) + token * a.ts[0];
+  const T *const v_rows = static_cast<const T *>(a.in[1]) + token * a.ts[1];
+  const bool in = any && from < c.dim, turned = TURN != TURN_NONE && in && from < a.rot;
+  // The lane's channels: [from, from + N), but with TURN_HALF N / 2 each from two places.
+  const int lower = TURN == TURN_HALF && from < a.rot ? from / 2 : from;
+  const int upper = TURN == TURN_HALF && from < a.rot ? from / 2 + a.rot / 2 : from + N / 2;
+  constexpr int E = TURN == TURN_HALF || TURN == TURN_PAIRS ? N / 2 : 1;
+  float cosine[E], sine[E];
+  const float2 *turn = nullptr;
+  Place p{};
+  struct Raw {
+    raw_chunk<T, N> k, v;
+  } now, next;
+  using Side = raw_chunk<T, N / 2>;
+  using Codes = raw_chunk<C, N / 2>;
+  const auto fetch = [&](Raw &r, int h) {
+    if (WIDE && in && h < end) {
+      const T *const k = k_rows + h * a.hs[0], *const v = v_rows + h * a.hs[1];
+      if (TURN == TURN_HALF) {
+        *reinterpret_cast<Side *>(r.k.w) = *reinterpret_cast<const Side *>(k + lower);
+        *reinterpret_cast<Side *>(r.k.w + sizeof(Side) / 4) = *reinterpret_cast<const Side *>(k + upper);
+      } else {
+        r.k = *reinterpret_cast<const raw_chunk<T, N> *>(k + from);
+      }
+      r.v = *reinterpret_cast<const raw_chunk<T, N> *>(v + from);
     }
+  };
+  fetch(now, first);
+  const bool there = find(a, slot, first, &p);
+  if (turned && there) {
+    turn = find_turn(a, token);
+    if constexpr (TURN == TURN_HALF || TURN == TURN_PAIRS)
+      load_rotation<E, true>(turn ? turn + from / 2 : nullptr, turn != nullptr, cosine, sine);
   }
-  Place p;
-  const bool there = find(a, slot, head, &p);
-  if (turned && there) rotate<WIDE, T, N>(a, k_row, token, from, k, w);
-  if constexpr (quantised<C>::value) {
-    float k_scale, v_scale;
-    const raw_chunk<C, N> k_codes = quantise<C, N>(k, a.lanes, &k_scale), v_codes = quantise<C, N>(v, a.lanes, &v_scale);
-    if (there && lane == 0) c.k_scale[p.scale] = k_scale, c.v_scale[p.scale] = v_scale;
-    if (in && there) {
-      store_codes<WIDE>(static_cast<C *>(c.k) + p.at, from, c.dim, k_codes);
-      store_codes<WIDE>(static_cast<C *>(c.v) + p.at, from, c.dim, v_codes);
+  // All lanes of a warp go round as often: the shuffles are the warp's.
+  for (int j = 0; j < (RUN ? a.run : 1); ++j) {
+    const int h = first + j;
+    if (RUN) fetch(next, h + 1);
+    const bool mine = in && h < end, here = there && h < end;
+    float2 k[N / 2] = {}, v[N / 2] = {};
+    if (mine) {
+      if (WIDE) {
+        values(now.k, k);
+        values(now.v, v);
+      } else {
+        load<WIDE, T, N>(k_rows + h * a.hs[0], from, c.dim, k);
+        load<WIDE, T, N>(v_rows + h * a.hs[1], from, c.dim, v);
+      }
+      if (turned && there) rotate<TURN, T, N, E>(a, turn, cosine, sine, k_rows + h * a.hs[0], from, k);
     }
-  } else if (in && there) {
-    store<WIDE, C, N>(static_cast<C *>(c.k) + p.at, from, c.dim, k);
-    store<WIDE, C, N>(static_cast<C *>(c.v) + p.at, from, c.dim, v);
+    if constexpr (quantised<C>::value) {
+      uint32_t k_most, v_most;
+      if constexpr (WIDE && sizeof(T) == 2) {
+        k_most = mine ? (TURN == TURN_NONE ? largest(now.k) : largest(k)) : 0;
+        v_most = mine ? largest(now.v) : 0;
+      } else {
+        k_most = largest(k), v_most = largest(v);
+      }
+      float k_scale, v_scale;
+      const raw_chunk<C, N> k_codes = quantise<C, N>(k, k_most, a.lanes, &k_scale);
+      const raw_chunk<C, N> v_codes = quantise<C, N>(v, v_most, a.lanes, &v_scale);
+      if (here && lane == 0) c.k_scale[p.scale] = k_scale, c.v_scale[p.scale] = v_scale;
+      if (mine && here) {
+        C *const row = static_cast<C *>(c.k) + p.at;
+        if constexpr (TURN == TURN_HALF) {
+          *reinterpret_cast<Codes *>(row + lower) = *reinterpret_cast<const Codes *>(k_codes.w);
+          *reinterpret_cast<Codes *>(row + upper) = *reinterpret_cast<const Codes *>(k_codes.w + sizeof(Codes) / 4);
+        } else {
+          store_codes<WIDE>(row, from, c.dim, k_codes);
+        }
+        store_codes<WIDE>(static_cast<C *>(c.v) + p.at, from, c.dim, v_codes);
+      }
+      p.scale += c.scale_head_stride;
+    } else if (mine && here) {
+      C *const row = static_cast<C *>(c.k) + p.at;
+      if constexpr (TURN == TURN_HALF) {
+        const float2 x[N / 4] = {k[0], k[1]}, y[N / 4] = {k[2], k[3]};
+        store<WIDE, C, N / 2>(row, lower, c.dim, x);
+        store<WIDE, C, N / 2>(row, upper, c.dim, y);
+      } else {
+        store<WIDE, C, N>(row, from, c.dim, k);
+      }
+      store<WIDE, C, N>(static_cast<C *>(c.v) + p.at, from, c.dim, v);
+    }
+    p.at += c.head_stride;
+    if (RUN) now = next;
   }
 }
 
@@ -332,12 +419,6 @@ bool wide_cache(const gar_kv_cache &c, int n) {
          c.head_stride % n == 0 && c.token_stride % n == 0;
 }
 
-// The channels of a lane: 16 where the cache's are 8-bit codes and there are rows enough to fill the GPU
-// four times over with half the lanes, else 8.
-int lane_channels(const gar_kv_cache &c, int64_t tokens) {
-  return element_size(c.dtype) == 1 && wide_cache(c, 16) && tokens * c.heads * (c.dim / 16) >= 152 * 2048 ? 16 : 8;
-}
-
 }  // namespace
 
 int check_cache(const gar_kv_cache *c) {
@@ -392,20 +473,30 @@ int gar_kv_write(const gar_kv_cache *cache, const void *k, int64_t k_token_strid
   const int n = 16 / size;
   const bool rows_wide = (uintptr_t)k % 16 == 0 && (uintptr_t)v % 16 == 0 && k_token_stride % n == 0 &&
                          k_head_stride % n == 0 && v_token_stride % n == 0 && v_head_stride % n == 0;
-  const int channels = rows_wide && (!positions || rot % 32 == 0) ? lane_channels(*cache, tokens) : 8;
-  const bool wide = rows_wide && wide_cache(*cache, channels);
-  if (!shape(&a, tokens, channels)) return refuse("too many rows");
-  a.wide_table = (uintptr_t)table % 16 == 0 && rot % (a.interleaved ? channels : 2 * channels) == 0;
+  const int turn = positions ? (a.interleaved ? TURN_PAIRS : TURN_HALF) : TURN_NONE;
+  const bool turn_wide = turn == TURN_NONE || ((uintptr_t)table % 16 == 0 && rot % 8 == 0);
+  const bool wide = rows_wide && turn_wide && wide_cache(*cache, 8);
+  if (!shape(&a, tokens, 8)) return refuse("too many rows");
+  // One head at a time until the GPU is full, then up to 8 for the sake of what they share.
+  a.run = wide && blocks(a, 1) >= 152 * 16 ? std::min(8, cache->heads) : 1;
+  a.runs = (cache->heads + a.run - 1) / a.run;
+  a.rows = (int)tokens * a.runs;
+  a.heads = divide_by((uint32_t)a.runs);
   return with_types(dtype, cache->dtype, [&](auto t, auto c) {
     using T = typename decltype(t)::type;
     using C = typename decltype(c)::type;
-    auto kernel = wide ? (positions ? write_kernel<T, C, 8, true, true> : write_kernel<T, C, 8, true, false>)
-                       : (positions ? write_kernel<T, C, 8, false, true> : write_kernel<T, C, 8, false, false>);
-    if constexpr (quantised<C>::value) {
-      if (channels == 16) kernel = positions ? write_kernel<T, C, 16, true, true> : write_kernel<T, C, 16, true, false>;
-    }
-    kernel<<<blocks(a, 1), kThreads, 0, (cudaStream_t)stream>>>(a);
-    return launched("write_kernel");
+    const auto pick = [&](auto kernel) {
+      kernel<<<blocks(a, 1), kThreads, 0, (cudaStream_t)stream>>>(a);
+      return launched("write_kernel");
+    };
+    if (!wide) return pick(positions ? write_kernel<T, C, 8, false, false, TURN_ANY> : write_kernel<T, C, 8, false, false, TURN_NONE>);
+    if (a.run == 1)
+      return pick(turn == TURN_NONE   ? write_kernel<T, C, 8, false, true, TURN_NONE>
+                  : turn == TURN_HALF ? write_kernel<T, C, 8, false, true, TURN_HALF>
+                                      : write_kernel<T, C, 8, false, true, TURN_PAIRS>);
+    return pick(turn == TURN_NONE   ? write_kernel<T, C, 8, true, true, TURN_NONE>
+                : turn == TURN_HALF ? write_kernel<T, C, 8, true, true, TURN_HALF>
+                                    : write_kernel<T, C, 8, true, true, TURN_PAIRS>);
   });
 }
 
@@ -423,22 +514,15 @@ int gar_kv_read(const gar_kv_cache *cache, const int64_t *slots, int64_t tokens,
   a.cache = *cache;
   a.out[0] = k, a.out[1] = v, a.slots = slots;
   const bool rows_wide = (uintptr_t)k % 16 == 0 && (uintptr_t)v % 16 == 0;
-  const int channels = rows_wide ? lane_channels(*cache, tokens) : 8;
-  const bool wide = rows_wide && wide_cache(*cache, channels) && (int64_t)cache->dim * size % 16 == 0;
-  if (!shape(&a, tokens, channels)) return refuse("too many rows");
+  const bool wide = rows_wide && wide_cache(*cache, 8) && (int64_t)cache->dim * size % 16 == 0;
+  if (!shape(&a, tokens, 8)) return refuse("too many rows");
   return with_types(dtype, cache->dtype, [&](auto t, auto c) {
     using T = typename decltype(t)::type;
     using C = typename decltype(c)::type;
     auto kernel = wide ? read_kernel<T, C, 8, true, 1> : read_kernel<T, C, 8, false, 1>;
     int rows = 1;
-    if (wide && blocks(a, 4) >= 152 * 2) {  // CTAs enough to fill the GPU with four rows a lane
-      kernel = read_kernel<T, C, 8, true, 4>, rows = 4;
-      if constexpr (quantised<C>::value) {
-        if (channels == 16) kernel = read_kernel<T, C, 16, true, 4>;
-      }
-    } else if constexpr (quantised<C>::value) {
-      if (channels == 16) kernel = read_kernel<T, C, 16, true, 1>;
-    }
+    if (wide && blocks(a, kReadRows) >= 152 * 4)  // enough CTAs to fill the GPU
+      kernel = read_kernel<T, C, 8, true, kReadRows>, rows = kReadRows;
     kernel<<<blocks(a, rows), kThreads, 0, (cudaStream_t)stream>>>(a);
     return launched("read_kernel");
   });
