@@ -228,6 +228,7 @@ __device__ __forceinline__ raw_chunk<C, N> quantise(float2 (&v)[N / 2], uint32_t
 template <typename T, typename C, int N, bool RUN, bool WIDE, int TURN>
 __global__ void __launch_bounds__(kThreads, RUN ? 4 : 1) write_kernel(const CacheArgs a) {
   static_assert(N == 8, "two words of codes, a half of a chunk each");
+  after_earlier_kernels();
   const gar_kv_cache &c = a.cache;
   const int lane = threadIdx.x & (a.lanes - 1), from = lane * N;
   const int i = blockIdx.x * (kThreads / a.lanes) + threadIdx.x / a.lanes;
@@ -327,6 +328,7 @@ __global__ void __launch_bounds__(kThreads, RUN ? 4 : 1) write_kernel(const Cach
 // C -> T rows, M of them to a lane: a row's place hangs on its slot, so that fewer bytes would be in flight.
 template <typename T, typename C, int N, bool WIDE, int M>
 __global__ void __launch_bounds__(kThreads) read_kernel(const CacheArgs a) {
+  after_earlier_kernels();
   const gar_kv_cache &c = a.cache;
   const int lane = threadIdx.x & (a.lanes - 1), from = lane * N, step = kThreads / a.lanes;
   const int i0 = blockIdx.x * (step * M) + threadIdx.x / a.lanes;
@@ -486,8 +488,7 @@ int gar_kv_write(const gar_kv_cache *cache, const void *k, int64_t k_token_strid
     using T = typename decltype(t)::type;
     using C = typename decltype(c)::type;
     const auto pick = [&](auto kernel) {
-      kernel<<<blocks(a, 1), kThreads, 0, (cudaStream_t)stream>>>(a);
-      return launched("write_kernel");
+      return launch("gar_kv_write", kernel, blocks(a, 1), kThreads, 0, stream, a);
     };
     if (!wide) return pick(positions ? write_kernel<T, C, 8, false, false, TURN_ANY> : write_kernel<T, C, 8, false, false, TURN_NONE>);
     if (a.run == 1)
@@ -523,8 +524,7 @@ int gar_kv_read(const gar_kv_cache *cache, const int64_t *slots, int64_t tokens,
     int rows = 1;
     if (wide && blocks(a, kReadRows) >= 152 * 4)  // enough CTAs to fill the GPU
       kernel = read_kernel<T, C, 8, true, kReadRows>, rows = kReadRows;
-    kernel<<<blocks(a, rows), kThreads, 0, (cudaStream_t)stream>>>(a);
-    return launched("read_kernel");
+    return launch("gar_kv_read", kernel, blocks(a, rows), kThreads, 0, stream, a);
   });
 }
 

@@ -348,10 +348,10 @@ __device__ __forceinline__ void join_parts(const DecodeArgs &a, const Segment &g
   group.sync();
 }
 
-int decode_general(const DecodeArgs &a, int sms, cudaStream_t stream);
-int decode_mma_bf16(const DecodeArgs &a, int sms, cudaStream_t stream);
-int decode_mma_f16(const DecodeArgs &a, int sms, cudaStream_t stream);
-int decode_mma_i8(const DecodeArgs &a, int sms, cudaStream_t stream);
-int decode_mma_e4m3(const DecodeArgs &a, int sms, cudaStream_t stream);
+int decode_general(const DecodeArgs &a, int sms, gar_stream_t stream);
+int decode_mma_bf16(const DecodeArgs &a, int sms, gar_stream_t stream);
+int decode_mma_f16(const DecodeArgs &a, int sms, gar_stream_t stream);
+int decode_mma_i8(const DecodeArgs &a, int sms, gar_stream_t stream);
+int decode_mma_e4m3(const DecodeArgs &a, int sms, gar_stream_t stream);
 
 }  // namespace gar

@@ -167,13 +167,12 @@ int gar_decode_attention(gar_attn_plan *plan, const gar_kv_cache *cache, const v
   a.unit = 64;
   while (items * (a.most_rows / a.unit + 3) >= 1 << 30) a.unit *= 2;
   if (a.unit > 32768) return refuse("too many sequences and heads for tables this wide");
-  const cudaStream_t s = (cudaStream_t)stream;
-  if (!takes_mma(*cache, q, q_batch_stride, q_head_stride, q_dtype)) return decode_general(a, plan->sms, s);
+  if (!takes_mma(*cache, q, q_batch_stride, q_head_stride, q_dtype)) return decode_general(a, plan->sms, stream);
   switch (cache->dtype) {
-    case GAR_BF16: return decode_mma_bf16(a, plan->sms, s);
-    case GAR_F16: return decode_mma_f16(a, plan->sms, s);
-    case GAR_I8: return decode_mma_i8(a, plan->sms, s);
-    default: return decode_mma_e4m3(a, plan->sms, s);
+    case GAR_BF16: return decode_mma_bf16(a, plan->sms, stream);
+    case GAR_F16: return decode_mma_f16(a, plan->sms, stream);
+    case GAR_I8: return decode_mma_i8(a, plan->sms, stream);
+    default: return decode_mma_e4m3(a, plan->sms, stream);
   }
 }
 

@@ -22,6 +22,7 @@ template <typename T, int J> __global__ void __launch_bounds__(kThreads) general
   const int warp = threadIdx.x / 32, lane = threadIdx.x & 31;
   const int row = lane / 8, head = lane & 7;
   const int o_row = J * 32;
+  after_earlier_kernels();
   Walk walk;
   walk.start(a);
   const Group group{0, kWarps};
@@ -121,21 +122,20 @@ template <typename T, int J> __global__ void __launch_bounds__(kThreads) general
   }
 }
 
-template <typename T, int J> int launch(DecodeArgs a, int sms, cudaStream_t stream) {
+template <typename T, int J> int launch_general(DecodeArgs a, int sms, gar_stream_t stream) {
   const size_t shared = sizeof(float) * kWarps * kHeads * J * 32;
   a.item_heads = std::min(a.group, kHeads);
   a.item_groups = (a.group + kHeads - 1) / kHeads;
-  general_kernel<T, J><<<sms * (J <= 4 ? 4 : 2), kThreads, shared, stream>>>(a);
-  return launched("general_kernel");
+  return launch("gar_decode_attention", general_kernel<T, J>, sms * (J <= 4 ? 4 : 2), kThreads, shared, stream, a);
 }
 
-template <typename T> int by_dim(const DecodeArgs &a, int sms, cudaStream_t stream) {
-  return a.c.dim <= 64 ? launch<T, 2>(a, sms, stream) : a.c.dim <= 128 ? launch<T, 4>(a, sms, stream) : launch<T, 8>(a, sms, stream);
+template <typename T> int by_dim(const DecodeArgs &a, int sms, gar_stream_t stream) {
+  return a.c.dim <= 64 ? launch_general<T, 2>(a, sms, stream) : a.c.dim <= 128 ? launch_general<T, 4>(a, sms, stream) : launch_general<T, 8>(a, sms, stream);
 }
 
 }  // namespace
 
-int decode_general(const DecodeArgs &a, int sms, cudaStream_t stream) {
+int decode_general(const DecodeArgs &a, int sms, gar_stream_t stream) {
   switch (a.c.dtype) {
     case GAR_F32: return by_dim<float>(a, sms, stream);
     case GAR_BF16: return by_dim<__nv_bfloat16>(a, sms, stream);

@@ -202,7 +202,12 @@ __global__ void __launch_bounds__(32 * MmaShape<C, DP, NG>::kWarps, 1)
   const uint32_t barrier = (uint32_t)__cvta_generic_to_shared(barriers[warp]);
   if (BOXES && lane < S::kStages)
     asm volatile("mbarrier.init.shared::cta.b64 [%0], 1; fence.mbarrier_init.release.cluster;" ::"r"(barrier + 8 * lane) : "memory");
+  if (BOXES && threadIdx.x == 0) {
+    asm volatile("prefetch.tensormap [%0];" ::"l"(&k_map) : "memory");
+    asm volatile("prefetch.tensormap [%0];" ::"l"(&v_map) : "memory");
+  }
   __syncwarp();
+  after_earlier_kernels();
 
   // The copies' side of this warp: it walks the segments, notes in `works` those that the warp has to do
   // with, and copies their tiles.
@@ -621,7 +626,7 @@ __global__ void __launch_bounds__(32 * MmaShape<C, DP, NG>::kWarps, 1)
 // Maps of the cache as bytes [pages][heads][page_size][dim]; false where it has none.
 bool box_map(const gar_kv_cache &c, void *base, int line, int rows, CUtensorMap *map);
 
-template <typename C, int DP, int NG> int launch_mma(DecodeArgs a, int sms, cudaStream_t stream) {
+template <typename C, int DP, int NG> int launch_mma(DecodeArgs a, int sms, gar_stream_t stream) {
   using S = MmaShape<C, DP, NG>;
   a.item_heads = std::min(a.group, 8 * NG);
   a.item_groups = (a.group + 8 * NG - 1) / (8 * NG);
@@ -636,11 +641,10 @@ template <typename C, int DP, int NG> int launch_mma(DecodeArgs a, int sms, cuda
       cudaFuncSetAttribute(mma_kernel<C, DP, NG, false>, cudaFuncAttributeMaxDynamicSharedMemorySize, S::kShared),
       cudaFuncSetAttribute(mma_kernel<C, DP, NG, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, S::kShared)};
   if (e[boxes] != cudaSuccess) return cuda_fail(e[boxes], "cudaFuncSetAttribute");
-  kernel<<<sms, 32 * S::kWarps, S::kShared, stream>>>(a, maps[0], maps[1]);
-  return launched("mma_kernel");
+  return launch("gar_decode_attention", kernel, sms, 32 * S::kWarps, S::kShared, stream, a, maps[0], maps[1]);
 }
 
-template <typename C> int decode_mma(const DecodeArgs &a, int sms, cudaStream_t stream) {
+template <typename C> int decode_mma(const DecodeArgs &a, int sms, gar_stream_t stream) {
   const bool two = a.group > 8;
   if (a.c.dim <= 64) return two ? launch_mma<C, 64, 2>(a, sms, stream) : launch_mma<C, 64, 1>(a, sms, stream);
   if (a.c.dim <= 128) return two ? launch_mma<C, 128, 2>(a, sms, stream) : launch_mma<C, 128, 1>(a, sms, stream);

@@ -4,5 +4,5 @@
 #include "decode_mma.cuh"
 
 namespace gar {
-int decode_mma_e4m3(const DecodeArgs &a, int sms, cudaStream_t stream) { return decode_mma<e4m3>(a, sms, stream); }
+int decode_mma_e4m3(const DecodeArgs &a, int sms, gar_stream_t stream) { return decode_mma<e4m3>(a, sms, stream); }
 }  // namespace gar

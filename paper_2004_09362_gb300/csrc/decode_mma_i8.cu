@@ -4,5 +4,5 @@
 #include "decode_mma.cuh"
 
 namespace gar {
-int decode_mma_i8(const DecodeArgs &a, int sms, cudaStream_t stream) { return decode_mma<i8>(a, sms, stream); }
+int decode_mma_i8(const DecodeArgs &a, int sms, gar_stream_t stream) { return decode_mma<i8>(a, sms, stream); }
 }  // namespace gar

@@ -193,9 +193,26 @@ template <typename F> int with_float(int dtype, F f) {
   return f(type_tag<__half>{});
 }
 
-inline int launched(const char *what) {
-  const cudaError_t e = cudaGetLastError();
+// Launches a kernel that begins with after_earlier_kernels().  It may become resident while the kernel before it on
+// the stream is still running (programmatic dependent launch), which hides the 2 us that a launch takes;
+// it touches no memory before that kernel has completed.
+template <typename... P, typename... A>
+int launch(const char *what, void (*kernel)(P...), int64_t blocks, int threads, size_t shared, gar_stream_t stream,
+           const A &...args) {
+  cudaLaunchAttribute attribute{};
+  attribute.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attribute.val.programmaticStreamSerializationAllowed = 1;
+  cudaLaunchConfig_t config{};
+  config.gridDim = dim3((unsigned)blocks), config.blockDim = dim3((unsigned)threads);
+  config.dynamicSmemBytes = shared, config.stream = (cudaStream_t)stream;
+  config.attrs = &attribute, config.numAttrs = 1;
+  const cudaError_t e = cudaLaunchKernelEx(&config, kernel, args...);
   return e == cudaSuccess ? GAR_OK : cuda_fail(e, what);
+}
+
+// Lets the next such kernel become resident, and waits for the ones before this.
+__device__ __forceinline__ void after_earlier_kernels() {
+  asm volatile("griddepcontrol.launch_dependents; griddepcontrol.wait;" ::: "memory");
 }
 
 inline int refuse(const std::string &why) {

@@ -14,6 +14,7 @@ struct Frequencies {
 // One thread per entry.  64-bit sincos: this GPU is slow at it, and a table is made once.
 __global__ void rope_table_kernel(float2 *table, int64_t first, int64_t count, int pairs, double magnitude,
                                   const __grid_constant__ Frequencies fr) {
+  after_earlier_kernels();
   const int64_t n = count * pairs, step = (int64_t)gridDim.x * blockDim.x;
   for (int64_t i = (int64_t)blockIdx.x * blockDim.x + threadIdx.x; i < n; i += step) {
     const int64_t row = i / pairs;
@@ -57,6 +58,7 @@ template <typename T, bool INTERLEAVED> __global__ void __launch_bounds__(256) r
   constexpr int kUnroll = 4;
   using chunk = chunk16<T>;
   constexpr int V = chunk::N, PAIRS = INTERLEAVED ? V / 2 : V;
+  after_earlier_kernels();
   const int per_token = a.lanes * a.units;
   for (int i = threadIdx.x; i < a.block_tokens * per_token; i += blockDim.x) {
     const int bt = i / per_token, r = i - bt * per_token;
@@ -116,6 +118,7 @@ template <typename T, bool INTERLEAVED> __global__ void __launch_bounds__(256) r
 
 // The same where 16-byte accesses do not fit: one pair, or one copied channel, of every lanes-th head.
 template <typename T> __global__ void __launch_bounds__(256) rope_narrow_kernel(const RopeArgs a, bool interleaved) {
+  after_earlier_kernels();
   const int per_token = a.lanes * a.units;
   for (int i = threadIdx.x; i < a.block_tokens * per_token; i += blockDim.x) {
     const int bt = i / per_token, r = i - bt * per_token;
@@ -143,7 +146,7 @@ template <typename T> __global__ void __launch_bounds__(256) rope_narrow_kernel(
   }
 }
 
-template <typename T> int launch_rope(RopeArgs a, int layout, bool in_place, bool wide, cudaStream_t stream) {
+template <typename T> int launch_rope(RopeArgs a, int layout, bool in_place, bool wide, gar_stream_t stream) {
   const bool inter = layout == GAR_ROPE_INTERLEAVED;
   const int v = wide ? chunk16<T>::N : 1;
   a.pair_units = inter && wide ? a.rot / v : a.rot / 2 / v;
@@ -155,13 +158,8 @@ template <typename T> int launch_rope(RopeArgs a, int layout, bool in_place, boo
   const int64_t blocks = (a.tokens + a.block_tokens - 1) / a.block_tokens;
   if (blocks > 0x7fffffff) return refuse("too many tokens");
   const int threads = std::min(256, (a.block_tokens * a.lanes * a.units + 31) / 32 * 32);
-  if (!wide)
-    rope_narrow_kernel<T><<<(unsigned)blocks, threads, 0, stream>>>(a, inter);
-  else if (inter)
-    rope_kernel<T, true><<<(unsigned)blocks, threads, 0, stream>>>(a);
-  else
-    rope_kernel<T, false><<<(unsigned)blocks, threads, 0, stream>>>(a);
-  return launched("rope_kernel");
+  if (!wide) return launch("gar_rope", rope_narrow_kernel<T>, blocks, threads, 0, stream, a, inter);
+  return launch("gar_rope", inter ? rope_kernel<T, true> : rope_kernel<T, false>, blocks, threads, 0, stream, a);
 }
 
 }  // namespace
@@ -210,9 +208,8 @@ int gar_rope_table(float *table, int64_t first, int64_t count, int rot, const do
   Frequencies fr{};
   std::copy(frequencies, frequencies + rot / 2, fr.f);
   const int64_t blocks = std::min<int64_t>((count * (rot / 2) + 255) / 256, 152 * 64);
-  rope_table_kernel<<<(unsigned)blocks, 256, 0, (cudaStream_t)stream>>>(reinterpret_cast<float2 *>(table), first, count,
-                                                                       rot / 2, magnitude, fr);
-  return launched("rope_table_kernel");
+  return launch("gar_rope_table", rope_table_kernel, blocks, 256, 0, stream, reinterpret_cast<float2 *>(table), first, count,
+                rot / 2, magnitude, fr);
 }
 
 int gar_rope(const void *x, int64_t x_token_stride, int64_t x_head_stride, void *out, int64_t out_token_stride,
@@ -247,10 +244,9 @@ int gar_rope(const void *x, int64_t x_token_stride, int64_t x_head_stride, void 
   const bool wide = (uintptr_t)x % 16 == 0 && (uintptr_t)table % 16 == 0 && (uintptr_t)out % 16 == 0 && fits(x_token_stride) && fits(x_head_stride) &&
                     fits(out_token_stride) && fits(out_head_stride) && fits(dim) &&
                     fits(layout == GAR_ROPE_HALF ? rot / 2 : rot);
-  const cudaStream_t s = (cudaStream_t)stream;
   return with_float(dtype, [&](auto tag) {
     using T = typename decltype(tag)::type;
-    return launch_rope<T>(a, layout, in_place, wide, s);
+    return launch_rope<T>(a, layout, in_place, wide, stream);
   });
 }
 
