@@ -353,5 +353,8 @@ int decode_mma_bf16(const DecodeArgs &a, int sms, gar_stream_t stream);
 int decode_mma_f16(const DecodeArgs &a, int sms, gar_stream_t stream);
 int decode_mma_i8(const DecodeArgs &a, int sms, gar_stream_t stream);
 int decode_mma_e4m3(const DecodeArgs &a, int sms, gar_stream_t stream);
+int decode_mma_f32(const DecodeArgs &a, int sms, gar_stream_t stream);
+int decode_mma_i8_f32(const DecodeArgs &a, int sms, gar_stream_t stream);    // 32-bit queries
+int decode_mma_e4m3_f32(const DecodeArgs &a, int sms, gar_stream_t stream);
 
 }  // namespace gar

@@ -23,11 +23,12 @@ size_t workspace_bytes(const gar_attn_plan &p) {
   return kCounterBytes + rows * (2 + dim_pad(p.dim)) * sizeof(float);
 }
 
-// The tensor-core kernels copy 16-byte chunks and take 16-bit queries.
+// The tensor-core kernels copy 16-byte chunks.
 bool takes_mma(const gar_kv_cache &c, const void *q, int64_t q_batch_stride, int64_t q_head_stride, int q_dtype) {
-  const int64_t n = 16 / element_size(c.dtype);
-  return c.dtype != GAR_F32 && q_dtype != GAR_F32 && (uintptr_t)q % 16 == 0 && q_batch_stride % 8 == 0 &&
-         q_head_stride % 8 == 0 && (uintptr_t)c.k % 16 == 0 && (uintptr_t)c.v % 16 == 0 && c.dim % n == 0 && c.page_stride % n == 0 && c.head_stride % n == 0 && c.token_stride % n == 0;
+  const int64_t n = 16 / element_size(c.dtype), m = 16 / element_size(q_dtype);
+  return (uintptr_t)q % 16 == 0 && q_batch_stride % m == 0 && q_head_stride % m == 0 && (uintptr_t)c.k % 16 == 0 &&
+         (uintptr_t)c.v % 16 == 0 && c.dim % n == 0 && c.page_stride % n == 0 && c.head_stride % n == 0 &&
+         c.token_stride % n == 0;
 }
 
 }  // namespace
@@ -168,11 +169,13 @@ int gar_decode_attention(gar_attn_plan *plan, const gar_kv_cache *cache, const v
   while (items * (a.most_rows / a.unit + 3) >= 1 << 30) a.unit *= 2;
   if (a.unit > 32768) return refuse("too many sequences and heads for tables this wide");
   if (!takes_mma(*cache, q, q_batch_stride, q_head_stride, q_dtype)) return decode_general(a, plan->sms, stream);
+  const bool q32 = q_dtype == GAR_F32;
   switch (cache->dtype) {
+    case GAR_F32: return decode_mma_f32(a, plan->sms, stream);
     case GAR_BF16: return decode_mma_bf16(a, plan->sms, stream);
     case GAR_F16: return decode_mma_f16(a, plan->sms, stream);
-    case GAR_I8: return decode_mma_i8(a, plan->sms, stream);
-    default: return decode_mma_e4m3(a, plan->sms, stream);
+    case GAR_I8: return (q32 ? decode_mma_i8_f32 : decode_mma_i8)(a, plan->sms, stream);
+    default: return (q32 ? decode_mma_e4m3_f32 : decode_mma_e4m3)(a, plan->sms, stream);
   }
 }
 

@@ -1,4 +1,4 @@
-// Decode attention without tensor cores: 32-bit caches and queries, odd head sizes, unaligned rows.
+// Decode attention without tensor cores: head sizes and rows that are no multiple of 16 bytes.
 #include <algorithm>
 
 #include "decode.cuh"

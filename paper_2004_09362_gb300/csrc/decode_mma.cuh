@@ -1,5 +1,4 @@
-// Decode attention on tensor cores, for 16-bit queries over a 16- or 8-bit cache whose rows are
-// 16-byte aligned.
+// Decode attention on tensor cores, over a cache whose rows are 16-byte aligned.
 //
 // Bound by memory: each cached row is read once for up to 8 NG query heads.  Per 16 rows of 128
 // channels the products take 40 (NG = 1) warp-wide m16n8k16 instructions, a small part of
@@ -26,7 +25,12 @@
 //
 // 8-bit codes become f16, exactly; a row's key scale multiplies its scores, its value scale
 // its weight, taken relative to the largest value scale so far so that the weights stay in f16's
-// range.  Weights are split into a high and a low 16-bit part, one product each.
+// range.  Weights are split into a high and a low 16-bit part, one product each; so are 32-bit queries of
+// an 8-bit cache.
+//
+// In a 32-bit cache everything is split in two, x = high + low with 11 significant bits each (TF32), and a
+// product is high high + high low + low high: off by 2^-21 relative at most.  Where that gives a score
+// that is no number (an infinite key: infinity times a low part of zero), the score is summed again without.
 #pragma once
 
 #include <cuda.h>
@@ -58,6 +62,28 @@ __device__ __forceinline__ void mma<__nv_bfloat16>(float (&d)[4], uint32_t a0, u
   asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
       : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
       : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+
+// Channels by 8 rows of the cache, in TF32.
+__device__ __forceinline__ void mma_tf32(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0,
+                                         uint32_t b1) {
+  asm("mma.sync.aligned.m16n8k8.row.col.f32.tf32.tf32.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+      : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+      : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+struct Split {
+  uint32_t high, low;
+};
+__device__ __forceinline__ Split split32(uint32_t x) {
+  Split s;
+  asm("cvt.rna.tf32.f32 %0, %1;" : "=r"(s.high) : "f"(__uint_as_float(x)));
+  s.low = __float_as_uint(__uint_as_float(x) - __uint_as_float(s.high));
+  return s;
+}
+__device__ __forceinline__ void mma_split(float (&d)[4], const Split (&a)[4], Split b0, Split b1) {
+  mma_tf32(d, a[0].low, a[1].low, a[2].low, a[3].low, b0.high, b1.high);
+  mma_tf32(d, a[0].high, a[1].high, a[2].high, a[3].high, b0.low, b1.low);
+  mma_tf32(d, a[0].high, a[1].high, a[2].high, a[3].high, b0.high, b1.high);
 }
 
 __device__ __forceinline__ uint32_t bits(__half2 x) { return *reinterpret_cast<uint32_t *>(&x); }
@@ -138,7 +164,8 @@ template <> struct words<8> {
 
 constexpr int kSolo = 4;
 
-// DP: the head's channels rounded up to 64, 128 or 256; NG: groups of 8 query heads.
+// DP: the head's channels rounded up to 64, 128 or 256; NG: groups of 8 query heads.  (The queries' type has no part
+// in it.)
 template <typename C, int DP, int NG> struct MmaShape {
   static constexpr int EL = sizeof(C);
   static constexpr bool Q8 = quantised<C>::value;
@@ -148,10 +175,10 @@ template <typename C, int DP, int NG> struct MmaShape {
   static constexpr int PARTS = DP * EL / LINE;
   static constexpr int kLogTile = DP * EL <= 128 ? 5 : 4, KT = 1 << kLogTile;  // rows of a tile
   static constexpr int kTile = 2 * KT * DP * EL;                   // bytes, keys and values
-  // One CTA per SM; its 192 KB of tiles are divided among as many warps as the registers allow.
-  static constexpr int kWarps = kTile > 8192 ? 4 : NG == 1 && DP <= 128 ? 12 : 8;
+  // One CTA per SM; its 192 KB of tiles are divided among as many warps as the registers allow, two tiles each at least.
+  static constexpr int kMost = 196608 / kTile / 2, kLike = NG == 1 && DP <= 128 ? 12 : 8;
+  static constexpr int kWarps = kMost < kLike ? kMost : kLike;
   static constexpr int kStages = 196608 / kWarps / kTile;
-  static_assert(kStages >= 2, "a tile in use and one on its way");
   static constexpr int kScales = Q8 ? 2 * KT * 4 : 0;
   // Floats of an o row; a row of o for each head fits a stage.  A few floats more than DP spread
   // the rows over the banks.
@@ -180,15 +207,16 @@ struct Work {
 };
 constexpr int kAhead = 4;  // segments that a warp's copies can be ahead
 
-template <typename C, int DP, int NG, bool BOXES>
+template <typename C, int DP, int NG, bool BOXES, bool Q32>
 __global__ void __launch_bounds__(32 * MmaShape<C, DP, NG>::kWarps, 1)
     mma_kernel(const DecodeArgs a, const __grid_constant__ CUtensorMap k_map, const __grid_constant__ CUtensorMap v_map) {
   using S = MmaShape<C, DP, NG>;
   using T = typename operand<C>::type;
   constexpr int EL = S::EL, KC = S::KC, VB = S::VB, LINE = S::LINE, PARTS = S::PARTS, KT = S::KT, SUBS = KT / 16;
   constexpr int W = S::kWarps;
-  constexpr bool Q8 = S::Q8;
+  constexpr bool Q8 = S::Q8, F32 = std::is_same<C, float>::value;
   constexpr int MT = DP / 16;          // tiles of 16 channels of the output
+  constexpr int QW = Q32 ? DP / 4 : DP / 8;  // words of a head's queries in a lane
   extern __shared__ char shared_from[];
   __shared__ JoinShared<W> join;
   __shared__ __align__(8) uint64_t barriers[W][S::kStages];
@@ -362,26 +390,28 @@ __global__ void __launch_bounds__(32 * MmaShape<C, DP, NG>::kWarps, 1)
     }
   };
 
-  // This lane's places in a tile: rows g and g + 8 of the scores, rows 2t and 2t + 1 of the values.
+  // This lane's places in a tile: rows g and g + 8 of the scores, rows 2t and 2t + 1 of the values (32 bits: t, t + 4).
   const int k_at = place<LINE>(key_row<LINE>(g), t);
   int v_at[2];
 #pragma unroll
   for (int i = 0; i < 2; ++i)
-    v_at[i] = KT * DP * EL + place<LINE>(key_row<LINE>(2 * t + i), VB == 16 ? g : g / 2) + (VB == 16 ? 0 : (g & 1) * 8);
+    v_at[i] = KT * DP * EL + place<LINE>(key_row<LINE>(F32 ? t + 4 * i : 2 * t + i), VB == 16 ? g : g / 2) +
+              (VB == 16 ? 0 : (g & 1) * 8);
 
-  // Queries: head g (+ 8 ng), the channels of this lane's chunks, two to a register.
-  uint32_t qf[NG][DP / 8];
+  // Queries: head g (+ 8 ng), the channels of this lane's chunks.
+  uint32_t qf[NG][QW];
   const auto load_queries = [&] {
     const Segment &seg = works[warp][done % kAhead].seg;
-    const char *const q0 = static_cast<const char *>(a.q) + 2 * (seg.b * a.qb + (seg.head + g) * a.qh);
+    constexpr int QB = Q32 ? 4 : 2, V = 16 / QB, PER = 16 / EL / V;  // 16 bytes have V channels, a chunk PER times as many
+    const char *const q0 = static_cast<const char *>(a.q) + QB * (seg.b * a.qb + (seg.head + g) * a.qh);
 #pragma unroll
     for (int ng = 0; ng < NG; ++ng) {
       const bool there = g + 8 * ng < seg.heads;
-      const uint4 *q = reinterpret_cast<const uint4 *>(q0 + 2 * 8 * ng * a.qh);
+      const uint4 *q = reinterpret_cast<const uint4 *>(q0 + QB * 8 * ng * a.qh);
 #pragma unroll
-      for (int k = 0; k < DP / 32; ++k) {
-        const int at = Q8 ? (t + 4 * (k / 2)) * 2 + k % 2 : t + 4 * k;  // 8 channels each
-        const uint4 x = there && at * 8 < c.dim ? q[at] : make_uint4(0, 0, 0, 0);
+      for (int k = 0; k < QW / 4; ++k) {
+        const int at = (t + 4 * (k / PER)) * PER + k % PER;
+        const uint4 x = there && at * V < c.dim ? q[at] : make_uint4(0, 0, 0, 0);
         qf[ng][4 * k] = x.x, qf[ng][4 * k + 1] = x.y, qf[ng][4 * k + 2] = x.z, qf[ng][4 * k + 3] = x.w;
       }
     }
@@ -394,21 +424,32 @@ __global__ void __launch_bounds__(32 * MmaShape<C, DP, NG>::kWarps, 1)
     float q_scale[NG][2];
 #pragma unroll
     for (int ng = 0; ng < NG; ++ng) {
-      // bf16 queries become f16 relative to the power of two at their largest
+      // Over an 8-bit cache bf16 and 32-bit queries become f16 relative to the power of two at their largest.
       float up = 1.f;
-      if (Q8 && a.q_dtype == GAR_BF16) {
+      if (Q8 && (Q32 || a.q_dtype == GAR_BF16)) {
         uint32_t most = 0;
 #pragma unroll
-        for (int i = 0; i < DP / 8; ++i) most = max(most, max(qf[ng][i] & 0x7fffu, (qf[ng][i] >> 16) & 0x7fffu));
+        for (int i = 0; i < QW; ++i)
+          most = Q32 ? max(most, qf[ng][i] & 0x7fffffffu)
+                     : max(most, max((qf[ng][i] & 0x7fffu) << 16, qf[ng][i] & 0x7fff0000u));
         most = max(most, __shfl_xor_sync(~0u, most, 1));
         most = max(most, __shfl_xor_sync(~0u, most, 2));
-        const int e = most >> 7;
+        const int e = most >> 23;
         float down = 1.f;
         if (e > 0 && e < 0xfe) up = __int_as_float(e << 23), down = __int_as_float((254 - e) << 23);
+        if constexpr (Q32) {
+          uint32_t hi[QW / 2], low[QW / 2];
 #pragma unroll
-        for (int i = 0; i < DP / 8; ++i)
-          qf[ng][i] = bits(__floats2half2_rn(__uint_as_float(qf[ng][i] << 16) * down,
-                                             __uint_as_float(qf[ng][i] & 0xffff0000u) * down));
+          for (int i = 0; i < QW / 2; ++i)
+            split<__half>(__uint_as_float(qf[ng][2 * i]) * down, __uint_as_float(qf[ng][2 * i + 1]) * down, &hi[i], &low[i]);
+#pragma unroll
+          for (int i = 0; i < QW / 2; ++i) qf[ng][i] = hi[i], qf[ng][QW / 2 + i] = low[i];
+        } else {
+#pragma unroll
+          for (int i = 0; i < QW; ++i)
+            qf[ng][i] = bits(__floats2half2_rn(__uint_as_float(qf[ng][i] << 16) * down,
+                                               __uint_as_float(qf[ng][i] & 0xffff0000u) * down));
+        }
       }
       up *= a.scale_log2;
       q_scale[ng][0] = __shfl_sync(~0u, up, 8 * t);      // lane 4 (2t) holds head 2t's
@@ -460,7 +501,15 @@ __global__ void __launch_bounds__(32 * MmaShape<C, DP, NG>::kWarps, 1)
           const char *const x_at = at + (k * 64 / LINE * KT + sub * 16) * LINE + (LINE == 128 && k % 2 ? k_at ^ 64 : k_at);
           const uint4 x = *reinterpret_cast<const uint4 *>(x_at), y = *reinterpret_cast<const uint4 *>(x_at + 8 * LINE);
           const uint32_t xs[4] = {x.x, x.y, x.z, x.w}, ys[4] = {y.x, y.y, y.z, y.w};
-          if constexpr (!Q8) {
+          if constexpr (F32) {
+#pragma unroll
+            for (int i = 0; i < 4; i += 2) {
+              const Split x4[4] = {split32(xs[i]), split32(ys[i]), split32(xs[i + 1]), split32(ys[i + 1])};
+#pragma unroll
+              for (int ng = 0; ng < NG; ++ng)
+                mma_split(s[sub][ng], x4, split32(qf[ng][k * 4 + i]), split32(qf[ng][k * 4 + i + 1]));
+            }
+          } else if constexpr (!Q8) {
 #pragma unroll
             for (int i = 0; i < 4; i += 2)
 #pragma unroll
@@ -473,11 +522,36 @@ __global__ void __launch_bounds__(32 * MmaShape<C, DP, NG>::kWarps, 1)
               expand<C>(xs[i], &a0, &a2);
               expand<C>(ys[i], &a1, &a3);
 #pragma unroll
-              for (int ng = 0; ng < NG; ++ng)
+              for (int ng = 0; ng < NG; ++ng) {
+                if (Q32)
+                  mma<T>(s[sub][ng], a0, a1, a2, a3, qf[ng][QW / 2 + k * 8 + 2 * i], qf[ng][QW / 2 + k * 8 + 2 * i + 1]);
                 mma<T>(s[sub][ng], a0, a1, a2, a3, qf[ng][k * 8 + 2 * i], qf[ng][k * 8 + 2 * i + 1]);
+              }
             }
           }
         }
+      if constexpr (F32) {
+        bool odd = false;
+#pragma unroll
+        for (int ng = 0; ng < NG; ++ng)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) odd |= s[0][ng][i] != s[0][ng][i];
+        if (__any_sync(~0u, odd)) {
+          const Segment &seg = works[warp][done % kAhead].seg;
+#pragma unroll
+          for (int ng = 0; ng < NG; ++ng)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              const int head = 8 * ng + 2 * t + i % 2, row = key_row<LINE>(g) + i / 2 * 8;
+              const float *q = static_cast<const float *>(a.q) + seg.b * a.qb + (seg.head + head) * a.qh;
+              float x = 0.f;
+              if (head < seg.heads)
+                for (int d = 0; d < c.dim; ++d)
+                  x = fmaf(q[d], *reinterpret_cast<const float *>(at + d / 32 * KT * LINE + place<LINE>(row, d / 4 & 7) + d % 4 * 4), x);
+              s[0][ng][i] = x;
+            }
+        }
+      }
       float top[NG][2];
 #pragma unroll
       for (int ng = 0; ng < NG; ++ng) top[ng][0] = m[ng][0], top[ng][1] = m[ng][1];
@@ -525,7 +599,7 @@ __global__ void __launch_bounds__(32 * MmaShape<C, DP, NG>::kWarps, 1)
           }
       }
       // Weights, in the layout of the second product's right operand.
-      uint32_t hi[SUBS][NG][2], low[SUBS][NG][2];
+      uint32_t hi[SUBS][NG][F32 ? 4 : 2], low[SUBS][NG][F32 ? 4 : 2];
 #pragma unroll
       for (int sub = 0; sub < SUBS; ++sub)
 #pragma unroll
@@ -540,9 +614,21 @@ __global__ void __launch_bounds__(32 * MmaShape<C, DP, NG>::kWarps, 1)
               l[ng][h] += p[h];
               if (Q8) p[h] *= f;
             }
-            split<T>(p[0], p[1], &hi[sub][ng][r], &low[sub][ng][r]);
-            hi[sub][ng][r] = transpose8x8(hi[sub][ng][r]);
-            low[sub][ng][r] = transpose8x8(low[sub][ng][r]);
+            if constexpr (F32) {
+              // Row t (i = 0) or t + 4 of these 8 rows and head g, for this lane: the lane that has them is known.
+#pragma unroll
+              for (int i = 0; i < 2; ++i) {
+                const int from_lane = (t + 4 * i) * 4 + g / 2;
+                const float x = __shfl_sync(~0u, p[0], from_lane), y = __shfl_sync(~0u, p[1], from_lane);
+                const Split w = split32(__float_as_uint(g & 1 ? y : x));
+                hi[sub][ng][2 * r + i] = w.high, low[sub][ng][2 * r + i] = w.low;
+              }
+            }
+            if constexpr (!F32) {
+              split<T>(p[0], p[1], &hi[sub][ng][r], &low[sub][ng][r]);
+              hi[sub][ng][r] = transpose8x8(hi[sub][ng][r]);
+              low[sub][ng][r] = transpose8x8(low[sub][ng][r]);
+            }
           }
         }
       // Values.
@@ -560,7 +646,20 @@ __global__ void __launch_bounds__(32 * MmaShape<C, DP, NG>::kWarps, 1)
             x[r].v = *reinterpret_cast<const V *>(at + (k * KT + sub * 16 + r / 2 * 8) * LINE + v_at[r & 1]);
 #pragma unroll
           for (int i = 0; i < VB / 4; ++i) {
-            if constexpr (!Q8) {
+            if constexpr (F32) {
+              // x[2r], x[2r + 1]: rows t and t + 4 of the r-th 8; words i and i + 1 are two channels.
+              if (i % 2 == 0) {
+#pragma unroll
+                for (int r = 0; r < 2; ++r) {
+                  const Split v4[4] = {split32(x[2 * r].u[i]), split32(x[2 * r].u[i + 1]), split32(x[2 * r + 1].u[i]),
+                                       split32(x[2 * r + 1].u[i + 1])};
+#pragma unroll
+                  for (int ng = 0; ng < NG; ++ng)
+                    mma_split(o[k * 2 + i / 2][ng], v4, Split{hi[sub][ng][2 * r], low[sub][ng][2 * r]},
+                              Split{hi[sub][ng][2 * r + 1], low[sub][ng][2 * r + 1]});
+                }
+              }
+            } else if constexpr (!Q8) {
               const uint32_t a0 = __byte_perm(x[0].u[i], x[1].u[i], 0x5410), a1 = __byte_perm(x[0].u[i], x[1].u[i], 0x7632);
               const uint32_t a2 = __byte_perm(x[2].u[i], x[3].u[i], 0x5410), a3 = __byte_perm(x[2].u[i], x[3].u[i], 0x7632);
 #pragma unroll
@@ -626,7 +725,7 @@ __global__ void __launch_bounds__(32 * MmaShape<C, DP, NG>::kWarps, 1)
 // Maps of the cache as bytes [pages][heads][page_size][dim]; false where it has none.
 bool box_map(const gar_kv_cache &c, void *base, int line, int rows, CUtensorMap *map);
 
-template <typename C, int DP, int NG> int launch_mma(DecodeArgs a, int sms, gar_stream_t stream) {
+template <typename C, int DP, int NG, bool Q32> int launch_mma(DecodeArgs a, int sms, gar_stream_t stream) {
   using S = MmaShape<C, DP, NG>;
   a.item_heads = std::min(a.group, 8 * NG);
   a.item_groups = (a.group + 8 * NG - 1) / (8 * NG);
@@ -636,19 +735,21 @@ template <typename C, int DP, int NG> int launch_mma(DecodeArgs a, int sms, gar_
   CUtensorMap maps[2];
   const bool boxes = a.c.page_size % 8 == 0 && box_map(a.c, a.c.k, S::LINE, box_rows, &maps[0]) &&
                      box_map(a.c, a.c.v, S::LINE, box_rows, &maps[1]);
-  const auto kernel = boxes ? mma_kernel<C, DP, NG, true> : mma_kernel<C, DP, NG, false>;
+  constexpr auto rowwise = mma_kernel<C, DP, NG, false, Q32>, boxed = mma_kernel<C, DP, NG, true, Q32>;
   static const cudaError_t e[2] = {
-      cudaFuncSetAttribute(mma_kernel<C, DP, NG, false>, cudaFuncAttributeMaxDynamicSharedMemorySize, S::kShared),
-      cudaFuncSetAttribute(mma_kernel<C, DP, NG, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, S::kShared)};
+      cudaFuncSetAttribute(rowwise, cudaFuncAttributeMaxDynamicSharedMemorySize, S::kShared),
+      cudaFuncSetAttribute(boxed, cudaFuncAttributeMaxDynamicSharedMemorySize, S::kShared)};
   if (e[boxes] != cudaSuccess) return cuda_fail(e[boxes], "cudaFuncSetAttribute");
-  return launch("gar_decode_attention", kernel, sms, 32 * S::kWarps, S::kShared, stream, a, maps[0], maps[1]);
+  return launch("gar_decode_attention", boxes ? boxed : rowwise, sms, 32 * S::kWarps, S::kShared, stream, a, maps[0],
+                maps[1]);
 }
 
-template <typename C> int decode_mma(const DecodeArgs &a, int sms, gar_stream_t stream) {
+template <typename C, bool Q32> int decode_mma(const DecodeArgs &a, int sms, gar_stream_t stream) {
   const bool two = a.group > 8;
-  if (a.c.dim <= 64) return two ? launch_mma<C, 64, 2>(a, sms, stream) : launch_mma<C, 64, 1>(a, sms, stream);
-  if (a.c.dim <= 128) return two ? launch_mma<C, 128, 2>(a, sms, stream) : launch_mma<C, 128, 1>(a, sms, stream);
-  return launch_mma<C, 256, 1>(a, sms, stream);
+  if (a.c.dim <= 64) return two ? launch_mma<C, 64, 2, Q32>(a, sms, stream) : launch_mma<C, 64, 1, Q32>(a, sms, stream);
+  if (a.c.dim <= 128)
+    return two ? launch_mma<C, 128, 2, Q32>(a, sms, stream) : launch_mma<C, 128, 1, Q32>(a, sms, stream);
+  return launch_mma<C, 256, 1, Q32>(a, sms, stream);
 }
 
 }  // namespace gar

@@ -1,0 +1,8 @@
+// Decode attention on tensor cores: a cache of this type.
+#include <algorithm>
+
+#include "decode_mma.cuh"
+
+namespace gar {
+int decode_mma_f32(const DecodeArgs &a, int sms, gar_stream_t stream) { return decode_mma<float, true>(a, sms, stream); }
+}  // namespace gar

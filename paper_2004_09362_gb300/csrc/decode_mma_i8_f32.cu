@@ -1,0 +1,8 @@
+// Decode attention on tensor cores: 32-bit queries over a cache of 8-bit codes.
+#include <algorithm>
+
+#include "decode_mma.cuh"
+
+namespace gar {
+int decode_mma_i8_f32(const DecodeArgs &a, int sms, gar_stream_t stream) { return decode_mma<i8, true>(a, sms, stream); }
+}  // namespace gar
