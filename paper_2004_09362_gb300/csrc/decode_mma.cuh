@@ -28,6 +28,10 @@
 // range.  Weights are split into a high and a low 16-bit part, one product each; so are 32-bit queries of
 // an 8-bit cache.
 //
+// The tensor cores cut their sums off rather than round them: in long sums that is a bias (4e-5 relative after
+// 100000 rows).  So they sum no more than the products of one tile; those sums are added up, and rescaled
+// where the maximum has grown, by fused multiply-adds in 32 bits.
+//
 // In a 32-bit cache everything is split in two, x = high + low with 11 significant bits each (TF32), and a
 // product is high high + high low + low high: off by 2^-21 relative at most.  Where that gives a score
 // that is no number (an infinite key: infinity times a low part of zero), the score is summed again without.
@@ -80,9 +84,10 @@ __device__ __forceinline__ Split split32(uint32_t x) {
   s.low = __float_as_uint(__uint_as_float(x) - __uint_as_float(s.high));
   return s;
 }
-__device__ __forceinline__ void mma_split(float (&d)[4], const Split (&a)[4], Split b0, Split b1) {
-  mma_tf32(d, a[0].low, a[1].low, a[2].low, a[3].low, b0.high, b1.high);
-  mma_tf32(d, a[0].high, a[1].high, a[2].high, a[3].high, b0.low, b1.low);
+// d += the high parts' product, e += the others'.
+__device__ __forceinline__ void mma_split(float (&d)[4], float (&e)[4], const Split (&a)[4], Split b0, Split b1) {
+  mma_tf32(e, a[0].low, a[1].low, a[2].low, a[3].low, b0.high, b1.high);
+  mma_tf32(e, a[0].high, a[1].high, a[2].high, a[3].high, b0.low, b1.low);
   mma_tf32(d, a[0].high, a[1].high, a[2].high, a[3].high, b0.high, b1.high);
 }
 
@@ -493,9 +498,11 @@ __global__ void __launch_bounds__(32 * MmaShape<C, DP, NG>::kWarps, 1)
       }
 
       // Scores.
-      float s[SUBS][NG][4] = {};
+      constexpr int CHAINS = F32 ? 5 : 2;  // sums that are added up at the end (the last of 5: the low parts')
+      float s[SUBS][NG][4];
 #pragma unroll
-      for (int sub = 0; sub < SUBS; ++sub)
+      for (int sub = 0; sub < SUBS; ++sub) {
+        float part[CHAINS][NG][4] = {};
 #pragma unroll
         for (int k = 0; k < KC; ++k) {
           const char *const x_at = at + (k * 64 / LINE * KT + sub * 16) * LINE + (LINE == 128 && k % 2 ? k_at ^ 64 : k_at);
@@ -507,14 +514,14 @@ __global__ void __launch_bounds__(32 * MmaShape<C, DP, NG>::kWarps, 1)
               const Split x4[4] = {split32(xs[i]), split32(ys[i]), split32(xs[i + 1]), split32(ys[i + 1])};
 #pragma unroll
               for (int ng = 0; ng < NG; ++ng)
-                mma_split(s[sub][ng], x4, split32(qf[ng][k * 4 + i]), split32(qf[ng][k * 4 + i + 1]));
+                mma_split(part[k % 4][ng], part[CHAINS - 1][ng], x4, split32(qf[ng][k * 4 + i]), split32(qf[ng][k * 4 + i + 1]));
             }
           } else if constexpr (!Q8) {
 #pragma unroll
             for (int i = 0; i < 4; i += 2)
 #pragma unroll
               for (int ng = 0; ng < NG; ++ng)
-                mma<T>(s[sub][ng], xs[i], ys[i], xs[i + 1], ys[i + 1], qf[ng][k * 4 + i], qf[ng][k * 4 + i + 1]);
+                mma<T>(part[i / 2][ng], xs[i], ys[i], xs[i + 1], ys[i + 1], qf[ng][k * 4 + i], qf[ng][k * 4 + i + 1]);
           } else {
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
@@ -524,12 +531,21 @@ __global__ void __launch_bounds__(32 * MmaShape<C, DP, NG>::kWarps, 1)
 #pragma unroll
               for (int ng = 0; ng < NG; ++ng) {
                 if (Q32)
-                  mma<T>(s[sub][ng], a0, a1, a2, a3, qf[ng][QW / 2 + k * 8 + 2 * i], qf[ng][QW / 2 + k * 8 + 2 * i + 1]);
-                mma<T>(s[sub][ng], a0, a1, a2, a3, qf[ng][k * 8 + 2 * i], qf[ng][k * 8 + 2 * i + 1]);
+                  mma<T>(part[i % 2][ng], a0, a1, a2, a3, qf[ng][QW / 2 + k * 8 + 2 * i], qf[ng][QW / 2 + k * 8 + 2 * i + 1]);
+                mma<T>(part[i % 2][ng], a0, a1, a2, a3, qf[ng][k * 8 + 2 * i], qf[ng][k * 8 + 2 * i + 1]);
               }
             }
           }
         }
+#pragma unroll
+        for (int ng = 0; ng < NG; ++ng)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            float x = part[0][ng][i] + part[1][ng][i];
+            if constexpr (F32) x = (x + (part[2][ng][i] + part[3][ng][i])) + part[4][ng][i];
+            s[sub][ng][i] = x;
+          }
+      }
       if constexpr (F32) {
         bool odd = false;
 #pragma unroll
@@ -580,24 +596,23 @@ __global__ void __launch_bounds__(32 * MmaShape<C, DP, NG>::kWarps, 1)
           for (int d = 4; d < 32; d *= 2) top[ng][h] = fmaxf(top[ng][h], __shfl_xor_sync(~0u, top[ng][h], d));
           grown |= top[ng][h] > m[ng][h];
         }
+      grown = __any_sync(~0u, grown);
       float v_inverse = 1.f, v_shrink = 1.f;
       if (Q8) {
         const float most = __uint_as_float(__reduce_max_sync(~0u, __float_as_uint(v_scale[lane & (KT - 1)]) & 0x7fffffffu));
-        if (most > v_ref) v_shrink = v_ref / most, v_ref = most, grown = true;
+        if (most > v_ref) v_shrink = v_ref / most, v_ref = most;
         v_inverse = 1.f / v_ref;
       }
-      if (__any_sync(~0u, grown)) {
+      float shrink[NG][2];
 #pragma unroll
-        for (int ng = 0; ng < NG; ++ng)
+      for (int ng = 0; ng < NG; ++ng)
 #pragma unroll
-          for (int h = 0; h < 2; ++h) {
-            const float f = exp2_fast(m[ng][h] - offset_of(top[ng][h]));
-            m[ng][h] = top[ng][h];
-            l[ng][h] *= f;
-#pragma unroll
-            for (int i = 0; i < MT; ++i) o[i][ng][h] *= f * v_shrink, o[i][ng][2 + h] *= f * v_shrink;
-          }
-      }
+        for (int h = 0; h < 2; ++h) {
+          shrink[ng][h] = grown ? exp2_fast(m[ng][h] - offset_of(top[ng][h])) : 1.f;
+          m[ng][h] = top[ng][h];
+          l[ng][h] *= shrink[ng][h];
+          if (Q8) shrink[ng][h] *= v_shrink;
+        }
       // Weights, in the layout of the second product's right operand.
       uint32_t hi[SUBS][NG][F32 ? 4 : 2], low[SUBS][NG][F32 ? 4 : 2];
 #pragma unroll
@@ -632,55 +647,55 @@ __global__ void __launch_bounds__(32 * MmaShape<C, DP, NG>::kWarps, 1)
           }
         }
       // Values.
+      constexpr int TILES = VB / EL / 2;  // tiles of 16 channels that a chunk has part in
 #pragma unroll
-      for (int sub = 0; sub < SUBS; ++sub)
+      for (int k = 0; k < PARTS; ++k)
 #pragma unroll
-        for (int k = 0; k < PARTS; ++k) {
+        for (int sub = 0; sub < SUBS; ++sub) {
           using V = typename words<VB>::type;
           union {
             V v;
             uint32_t u[VB / 4];
-          } x[4];
+          } y[4];
 #pragma unroll
           for (int r = 0; r < 4; ++r)
-            x[r].v = *reinterpret_cast<const V *>(at + (k * KT + sub * 16 + r / 2 * 8) * LINE + v_at[r & 1]);
+            y[r].v = *reinterpret_cast<const V *>(at + (k * KT + sub * 16 + r / 2 * 8) * LINE + v_at[r & 1]);
 #pragma unroll
-          for (int i = 0; i < VB / 4; ++i) {
+          for (int i = 0; i < TILES; ++i) {
+            float d[NG][4] = {}, e[NG][4] = {};
             if constexpr (F32) {
-              // x[2r], x[2r + 1]: rows t and t + 4 of the r-th 8; words i and i + 1 are two channels.
-              if (i % 2 == 0) {
+              // y[2r], y[2r + 1]: rows t and t + 4 of the r-th 8; words 2i and 2i + 1 are two channels.
 #pragma unroll
-                for (int r = 0; r < 2; ++r) {
-                  const Split v4[4] = {split32(x[2 * r].u[i]), split32(x[2 * r].u[i + 1]), split32(x[2 * r + 1].u[i]),
-                                       split32(x[2 * r + 1].u[i + 1])};
+              for (int r = 0; r < 2; ++r) {
+                const Split v4[4] = {split32(y[2 * r].u[2 * i]), split32(y[2 * r].u[2 * i + 1]),
+                                     split32(y[2 * r + 1].u[2 * i]), split32(y[2 * r + 1].u[2 * i + 1])};
 #pragma unroll
-                  for (int ng = 0; ng < NG; ++ng)
-                    mma_split(o[k * 2 + i / 2][ng], v4, Split{hi[sub][ng][2 * r], low[sub][ng][2 * r]},
-                              Split{hi[sub][ng][2 * r + 1], low[sub][ng][2 * r + 1]});
-                }
-              }
-            } else if constexpr (!Q8) {
-              const uint32_t a0 = __byte_perm(x[0].u[i], x[1].u[i], 0x5410), a1 = __byte_perm(x[0].u[i], x[1].u[i], 0x7632);
-              const uint32_t a2 = __byte_perm(x[2].u[i], x[3].u[i], 0x5410), a3 = __byte_perm(x[2].u[i], x[3].u[i], 0x7632);
-#pragma unroll
-              for (int ng = 0; ng < NG; ++ng) {
-                mma<T>(o[k * 4 + i][ng], a0, a1, a2, a3, hi[sub][ng][0], hi[sub][ng][1]);
-                mma<T>(o[k * 4 + i][ng], a0, a1, a2, a3, low[sub][ng][0], low[sub][ng][1]);
+                for (int ng = 0; ng < NG; ++ng)
+                  mma_split(d[ng], e[ng], v4, Split{hi[sub][ng][2 * r], low[sub][ng][2 * r]},
+                            Split{hi[sub][ng][2 * r + 1], low[sub][ng][2 * r + 1]});
               }
             } else {
+              uint32_t a0, a1, a2, a3;
+              if constexpr (Q8) {
+                expand<C>(__byte_perm(y[0].u[i / 2], y[1].u[i / 2], i % 2 ? 0x7362 : 0x5140), &a0, &a1);
+                expand<C>(__byte_perm(y[2].u[i / 2], y[3].u[i / 2], i % 2 ? 0x7362 : 0x5140), &a2, &a3);
+              } else {
+                a0 = __byte_perm(y[0].u[i], y[1].u[i], 0x5410), a1 = __byte_perm(y[0].u[i], y[1].u[i], 0x7632);
+                a2 = __byte_perm(y[2].u[i], y[3].u[i], 0x5410), a3 = __byte_perm(y[2].u[i], y[3].u[i], 0x7632);
+              }
 #pragma unroll
-              for (int j = 0; j < 2; ++j) {
-                uint32_t a0, a1, a2, a3;
-                expand<C>(__byte_perm(x[0].u[i], x[1].u[i], j ? 0x7362 : 0x5140), &a0, &a1);
-                expand<C>(__byte_perm(x[2].u[i], x[3].u[i], j ? 0x7362 : 0x5140), &a2, &a3);
-#pragma unroll
-                for (int ng = 0; ng < NG; ++ng) {
-                  float(&d)[4] = o[(k * (VB / 4) + i) * 2 + j][ng];
-                  mma<T>(d, a0, a1, a2, a3, hi[sub][ng][0], hi[sub][ng][1]);
-                  mma<T>(d, a0, a1, a2, a3, low[sub][ng][0], low[sub][ng][1]);
-                }
+              for (int ng = 0; ng < NG; ++ng) {
+                mma<T>(d[ng], a0, a1, a2, a3, hi[sub][ng][0], hi[sub][ng][1]);
+                mma<T>(d[ng], a0, a1, a2, a3, low[sub][ng][0], low[sub][ng][1]);
               }
             }
+#pragma unroll
+            for (int ng = 0; ng < NG; ++ng)
+#pragma unroll
+              for (int j = 0; j < 4; ++j) {
+                float &z = o[k * TILES + i][ng][j];
+                z = fmaf(z, sub == 0 ? shrink[ng][j & 1] : 1.f, F32 ? d[ng][j] + e[ng][j] : d[ng][j]);
+              }
           }
         }
       --flying;
