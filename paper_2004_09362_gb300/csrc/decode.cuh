@@ -39,6 +39,7 @@ struct DecodeArgs {
   int unit;                // rows of a unit of the line
   int box_shift;           // log2 of the tensor copies that a tile's rows take
   int batch, q_heads, group, item_groups, item_heads;  // group: q_heads / kv_heads
+  Divide items;            // by a sequence's items
   int q_dtype, out_dtype, window;
   bool out_wide;           // four neighbouring outputs can be stored at once
   float scale_log2;        // scale * log2(e)
@@ -171,6 +172,75 @@ struct Walk {
   }
 };
 
+// A segment as it is noted for later: 32 bytes.
+struct alignas(16) Note {
+  int from, to, lo, b;
+  int hh, item, units;  // the sequence's item; where it begins in the line, and its units
+  short whole, first;   // all of the item; the first segment of its CTA
+};
+static_assert(sizeof(Note) == 32, "two 16-byte accesses");
+
+// Notes a CTA's segments, kNotes at a time, a lane for each.
+constexpr int kNotes = 16;
+struct Notes {
+  int begin, end, per, lead, unit;  // of the walk
+  int next_item, at;                // the first item that is not noted yet, and where in the line it begins
+
+  __device__ __forceinline__ void start(const DecodeArgs &a) {
+    Walk w;
+    w.start(a);
+    begin = w.pos, end = w.end, per = w.per, lead = w.lead, unit = w.unit;
+    next_item = at = 0;
+    if (begin < end) next_item = w.b * (a.c.heads * a.item_groups) + w.hh, at = w.item;
+  }
+  __device__ __forceinline__ bool more() const { return at < end && begin < end; }
+
+  // Lane i < kNotes: the i-th of the next segments, or none (from > to).
+  __device__ __forceinline__ bool next(const DecodeArgs &a, Note *n) {
+    const int lane = threadIdx.x & 31, items = a.c.heads * a.item_groups;
+    const int item = next_item + min(lane, kNotes - 1);
+    n->b = (int)a.items((uint32_t)item);
+    n->hh = item - n->b * items;
+    Span s{};
+    if (n->b < a.batch) {
+      s = span_of(a, a.lengths[n->b], unit);
+      s.units += lead;
+    }
+    int upto = s.units;
+#pragma unroll
+    for (int d = 1; d < kNotes; d *= 2) {
+      const int up = __shfl_up_sync(~0u, upto, d);
+      if (lane >= d) upto += up;
+    }
+    n->item = at + upto - s.units, n->units = s.units;
+    const int u0 = max(begin, n->item) - n->item, u1 = min(end, n->item + s.units) - n->item;
+    n->from = s.base + max(0, u0 - lead) * unit;
+    n->to = (int)min((unsigned)s.hi, (unsigned)s.base + (unsigned)max(0, u1 - lead) * unit);
+    n->lo = max(s.lo, n->from);
+    n->whole = u0 == 0 && u1 == s.units, n->first = n->item + u0 == begin;
+    next_item += kNotes;
+    at += __shfl_sync(~0u, upto, kNotes - 1);
+    return lane < kNotes && n->b < a.batch && u0 < u1;
+  }
+
+  __device__ __forceinline__ void segment(const DecodeArgs &a, const Note &n, Segment *g) const {
+    g->b = n.b;
+    g->kv_head = a.item_groups == 1 ? n.hh : n.hh / a.item_groups;
+    const int sub = (n.hh - g->kv_head * a.item_groups) * a.item_heads;
+    g->head = g->kv_head * a.group + sub;
+    g->heads = min(a.item_heads, a.group - sub);
+    g->from = n.from, g->to = n.to, g->lo = n.lo;
+    g->whole = n.whole;
+    g->first = blockIdx.x, g->parts = 1, g->slot = 0, g->first_late = false;
+    if (!n.whole) {
+      g->slot = 2 * blockIdx.x + (n.first ? 0 : 1);
+      g->first = n.item / per;
+      g->parts = (n.item + n.units - 1) / per - g->first + 1;
+      g->first_late = g->first * per < n.item;
+    }
+  }
+};
+
 // The place of part i of an item: its CTA's second segment when that CTA's share begins before the item.
 __device__ __forceinline__ int slot_of(const Segment &g, int i) {
   return 2 * (g.first + i) + (i == 0 && g.first_late ? 1 : 0);
@@ -204,6 +274,20 @@ __device__ __forceinline__ void store_lse(const DecodeArgs &a, const Segment &g,
   if (a.lse) a.lse[(int64_t)g.b * a.q_heads + g.head + h] = l == 0.f ? -INFINITY : (m + log2f(l)) * 0.693147180559945f;
 }
 
+// Four neighbouring elements of the output, where a.out_wide says that they can be stored at once.
+__device__ __forceinline__ void store_wide4(const DecodeArgs &a, int64_t at, float x, float y, float z, float w) {
+  if (a.out_dtype == GAR_F32) {
+    *reinterpret_cast<float4 *>(static_cast<float *>(a.out) + at) = make_float4(x, y, z, w);
+    return;
+  }
+  uint2 v;
+  if (a.out_dtype == GAR_BF16)
+    v = make_uint2(pack2(make_float2(x, y), __nv_bfloat16()), pack2(make_float2(z, w), __nv_bfloat16()));
+  else
+    v = make_uint2(pack2(make_float2(x, y), __half()), pack2(make_float2(z, w), __half()));
+  *reinterpret_cast<uint2 *>(static_cast<char *>(a.out) + 2 * at) = v;
+}
+
 // Four neighbouring channels [d, d + 4) of query head h's output, x / l.
 __device__ __forceinline__ void store_out4(const DecodeArgs &a, const Segment &g, int h, int d, float4 x, float l) {
   const float f = 1.f / l;
@@ -212,22 +296,7 @@ __device__ __forceinline__ void store_out4(const DecodeArgs &a, const Segment &g
   else
     x.x *= f, x.y *= f, x.z *= f, x.w *= f;
   const int64_t at = g.b * a.ob + (g.head + h) * a.oh + d;
-  if (a.out_wide) {
-    if (a.out_dtype == GAR_F32) {
-      *reinterpret_cast<float4 *>(static_cast<float *>(a.out) + at) = x;
-    } else {
-      uint2 y;
-      if (a.out_dtype == GAR_BF16) {
-        const __nv_bfloat162 p = __floats2bfloat162_rn(x.x, x.y), q = __floats2bfloat162_rn(x.z, x.w);
-        y = make_uint2(*reinterpret_cast<const uint32_t *>(&p), *reinterpret_cast<const uint32_t *>(&q));
-      } else {
-        const __half2 p = __floats2half2_rn(x.x, x.y), q = __floats2half2_rn(x.z, x.w);
-        y = make_uint2(*reinterpret_cast<const uint32_t *>(&p), *reinterpret_cast<const uint32_t *>(&q));
-      }
-      *reinterpret_cast<uint2 *>(static_cast<char *>(a.out) + 2 * at) = y;
-    }
-    return;
-  }
+  if (a.out_wide) return store_wide4(a, at, x.x, x.y, x.z, x.w);
   for (int i = 0; i < 4 && d + i < a.c.dim; ++i) store_out(a, at + i, i == 0 ? x.x : i == 1 ? x.y : i == 2 ? x.z : x.w);
 }
 
@@ -254,7 +323,8 @@ struct Group {
 
 // Joins the (m, l, o) of a group's warps and writes the item's output, or the segment's partial
 // result.  Warp w holds head h's o at o[at[w] + h * row], 16-byte aligned.
-template <int WARPS>
+// With TWIST its channel d is at d ^ (h & 6).
+template <int WARPS, bool TWIST = false>
 __device__ __forceinline__ void join_warps(const DecodeArgs &a, const Segment &g, Group group, JoinShared<WARPS> &sh,
                                            const float *o, int row) {
   static_assert(WARPS <= 16, "16 lanes hold a head's warps");
@@ -289,9 +359,10 @@ __device__ __forceinline__ void join_warps(const DecodeArgs &a, const Segment &g
 #pragma unroll 4
     for (int w = group.first; w < group.first + group.count; ++w) {
       const float f = sh.weight[w][h];
-      const float4 y = *reinterpret_cast<const float4 *>(o + sh.at[w] + h * row + d);
+      const float4 y = *reinterpret_cast<const float4 *>(o + sh.at[w] + h * row + (TWIST ? d ^ (h & 4) : d));
       x.x += f * y.x, x.y += f * y.y, x.z += f * y.z, x.w += f * y.w;
     }
+    if (TWIST && (h & 2)) x = make_float4(x.z, x.w, x.x, x.y);
     if (g.whole)
       store_out4(a, g, h, d, x, sh.l[group.first][h]);
     else

@@ -204,14 +204,6 @@ template <int LINE> __device__ __forceinline__ int place(int r, int c) {
   return r * LINE + (LINE == 128 ? c ^ (r & 7) : c ^ (r / 2 & 3)) * 16;
 }
 
-// A segment that a warp has to do with, and which of its tiles are the warp's.
-struct Work {
-  Segment seg;
-  Group group;
-  int tile, step, tiles;
-};
-constexpr int kAhead = 4;  // segments that a warp's copies can be ahead
-
 template <typename C, int DP, int NG, bool BOXES, bool Q32>
 __global__ void __launch_bounds__(32 * MmaShape<C, DP, NG>::kWarps, 1)
     mma_kernel(const DecodeArgs a, const __grid_constant__ CUtensorMap k_map, const __grid_constant__ CUtensorMap v_map) {
@@ -242,22 +234,50 @@ __global__ void __launch_bounds__(32 * MmaShape<C, DP, NG>::kWarps, 1)
   __syncwarp();
   after_earlier_kernels();
 
-  // The copies' side of this warp: it walks the segments, notes in `works` those that the warp has to do
-  // with, and copies their tiles.
-  __shared__ Walk walks[W];
-  __shared__ Work works[W][kAhead];
-  Walk &walk = walks[warp];
+  // The warp's notes of the CTA's segments, two halves of kNotes that are filled in turn; a bit for each
+  // that the warp has to do with.  The copies are ahead of the products by a half at most.
+  __shared__ Notes course[W];
+  __shared__ Note notes[W][2 * kNotes];
+  Note *const note = notes[warp];
   {
-    Walk w;
-    w.start(a);
-    if (lane == 0) walk = w;
+    Notes n;
+    n.start(a);
+    if (lane == 0) course[warp] = n;
     __syncwarp();
   }
-  int noted = 0, done = 0, ordinal = 0;  // works noted and done; segments walked
+  uint32_t mine_mask = 0;                // of the notes that are not done
+  uint32_t copied_mask = 0;              // of those, the ones whose copies have been started
+  int filled = 0;                        // halves
+  bool more = course[warp].more();
+  const auto tiles_of = [&](const Note &n) { return (max(0, n.to - n.from) + KT - 1) / KT; };
+  // Few tiles of a whole item, or hardly any: one warp's, in turn.  Else tile by tile the warps'.
+  const auto group_of = [&](int i, const Note &n) {
+    const int tiles = tiles_of(n);
+    return tiles <= (n.whole ? kSolo : 1) ? Group{i % W, 1} : Group{0, min(W, tiles)};
+  };
+  const auto fill = [&] {
+    Notes c = course[warp];
+    __syncwarp();
+    Note n;
+    const bool there = c.next(a, &n);
+    const Group group = group_of(filled * kNotes + lane, n);
+    if (there) note[(filled & 1) * kNotes + lane] = n;
+    if (lane == 0) course[warp] = c;
+    const uint32_t mine = __ballot_sync(~0u, there && warp >= group.first && warp < group.first + group.count);
+    mine_mask |= mine << (filled & 1) * kNotes;
+    ++filled;
+    more = c.more();
+    __syncwarp();
+  };
+  // The notes in order: the older half's bits first.  (With an odd number of halves filled the first is the newer.)
+  const auto first_of = [&](uint32_t mask) {
+    const uint32_t older = filled & 1 ? mask & 0xffff0000u : mask & 0xffffu;
+    return __ffs(older ? older : mask) - 1;
+  };
   struct {
     int from, lo, to, b, kv_head, tile, step, tiles;
-  } get{};
-  bool walking = true, ready = false;    // ready: get's tile exists and its pages are known
+  } get{};                               // what is being copied
+  bool ready = false;                    // get's tile exists and its pages are known
   // The cache rows of get's tile.  Copied row by row: the page of this lane's row of the tile.  In boxes: this
   // lane's box (lane % boxes of a tile) of the (lane / boxes)-th of the warp's next tiles, its page and the row
   // in it, and the same of the tiles after those.
@@ -289,26 +309,21 @@ __global__ void __launch_bounds__(32 * MmaShape<C, DP, NG>::kWarps, 1)
     return x;
   };
   const auto advance = [&] {
-    while (get.tile >= get.tiles && walking && noted - done < kAhead) {
-      Walk w = walk;
-      Work x;
-      __syncwarp();
-      if (!(walking = w.next(a, &x.seg))) break;
-      const int tiles = (max(0, x.seg.to - x.seg.from) + KT - 1) / KT;
-      // Few tiles of a whole item, or hardly any: one warp's, in turn.  Else tile by tile the warps'.
-      const bool alone = tiles <= (x.seg.whole ? kSolo : 1);
-      x.group = alone ? Group{ordinal % W, 1} : Group{0, min(W, tiles)};
-      x.tile = alone ? 0 : warp, x.step = alone ? 1 : W;
-      const bool mine = warp >= x.group.first && warp < x.group.first + x.group.count;
-      x.tiles = mine ? tiles : 0;
-      ++ordinal;
-      if (lane == 0) {
-        walk = w;
-        if (mine) works[warp][noted % kAhead] = x;
+    while (get.tile >= get.tiles) {
+      uint32_t left = mine_mask & ~copied_mask;
+      if (left == 0) {
+        // The half to be filled next must be done with.
+        if (!more || (mine_mask & (filled & 1 ? 0xffff0000u : 0xffffu))) break;
+        fill();
+        continue;
       }
-      __syncwarp();
-      noted += mine;
-      get = {x.seg.from, x.seg.lo, x.seg.to, x.seg.b, x.seg.kv_head, x.tile, x.step, x.tiles};
+      const int i = first_of(left);
+      copied_mask |= 1u << i;
+      const Note n = note[i];
+      const int half = i / kNotes, age = (filled & 1) == half ? 2 : 1;  // halves filled since this one began
+      const Group group = group_of((filled - age) * kNotes + i % kNotes, n);
+      get = {n.from, n.lo, n.to, n.b, a.item_groups == 1 ? n.hh : n.hh / a.item_groups,
+             group.count == 1 ? 0 : warp, group.count == 1 ? 1 : W, tiles_of(n)};
     }
     ready = get.tile < get.tiles;
     if (ready) {
@@ -405,8 +420,7 @@ __global__ void __launch_bounds__(32 * MmaShape<C, DP, NG>::kWarps, 1)
 
   // Queries: head g (+ 8 ng), the channels of this lane's chunks.
   uint32_t qf[NG][QW];
-  const auto load_queries = [&] {
-    const Segment &seg = works[warp][done % kAhead].seg;
+  const auto load_queries = [&](const Segment &seg) {
     constexpr int QB = Q32 ? 4 : 2, V = 16 / QB, PER = 16 / EL / V;  // 16 bytes have V channels, a chunk PER times as many
     const char *const q0 = static_cast<const char *>(a.q) + QB * (seg.b * a.qb + (seg.head + g) * a.qh);
 #pragma unroll
@@ -422,10 +436,33 @@ __global__ void __launch_bounds__(32 * MmaShape<C, DP, NG>::kWarps, 1)
     }
   };
 
+  // The next segment that the warp has to do with: its rows and which tiles are the warp's.
+  int using_note = 0, from = 0, lo = 0, to = 0, tile = 0, step = 1, tiles = 0;
+  const auto group_in_use = [&] {
+    const int half = using_note / kNotes, age = (filled & 1) == half ? 2 : 1;
+    return group_of((filled - age) * kNotes + using_note % kNotes, note[using_note]);
+  };
+  const auto segment_in_use = [&] {
+    Segment seg;
+    course[warp].segment(a, note[using_note], &seg);
+    return seg;
+  };
+  const auto take = [&] {
+    if (mine_mask == 0) advance();  // (fills)
+    if (mine_mask == 0) return false;
+    using_note = first_of(mine_mask);
+    const Segment seg = segment_in_use();
+    load_queries(seg);
+    const Group group = group_in_use();
+    from = seg.from, lo = seg.lo, to = seg.to;
+    tile = group.count == 1 ? 0 : warp, step = group.count == 1 ? 1 : W, tiles = tiles_of(note[using_note]);
+    return true;
+  };
+
   advance();
-  if (noted) load_queries();
+  bool have = take();
   pump(S::kStages - 1);
-  while (done < noted) {
+  while (have) {
     float q_scale[NG][2];
 #pragma unroll
     for (int ng = 0; ng < NG; ++ng) {
@@ -467,11 +504,6 @@ __global__ void __launch_bounds__(32 * MmaShape<C, DP, NG>::kWarps, 1)
 #pragma unroll
     for (int ng = 0; ng < NG; ++ng) m[ng][0] = m[ng][1] = -INFINITY;
 
-    int from, lo, to, tile, step, tiles;
-    {
-      const Work &x = works[warp][done % kAhead];
-      from = x.seg.from, lo = x.seg.lo, to = x.seg.to, tile = x.tile, step = x.step, tiles = x.tiles;
-    }
     for (; tile < tiles; tile += step) {
       if (Q8 || !BOXES) {
         if (flying == S::kStages - 1)
@@ -553,7 +585,7 @@ __global__ void __launch_bounds__(32 * MmaShape<C, DP, NG>::kWarps, 1)
 #pragma unroll
           for (int i = 0; i < 4; ++i) odd |= s[0][ng][i] != s[0][ng][i];
         if (__any_sync(~0u, odd)) {
-          const Segment &seg = works[warp][done % kAhead].seg;
+          const Segment seg = segment_in_use();
 #pragma unroll
           for (int ng = 0; ng < NG; ++ng)
 #pragma unroll
@@ -701,6 +733,38 @@ __global__ void __launch_bounds__(32 * MmaShape<C, DP, NG>::kWarps, 1)
       --flying;
       if (++out == S::kStages) out = 0, parity ^= 1;
     }
+#pragma unroll
+    for (int ng = 0; ng < NG; ++ng)
+#pragma unroll
+      for (int h = 0; h < 2; ++h)
+#pragma unroll
+        for (int d = 4; d < 32; d *= 2) l[ng][h] += __shfl_xor_sync(~0u, l[ng][h], d);
+    constexpr int CE = VB / EL;  // channels of a chunk, two of them in a tile of 16
+    const Segment ended = segment_in_use();
+    const Group by = group_in_use();
+    if (by.count == 1 && ended.whole && a.out_wide) {
+      // One warp's alone: straight to the output, whole chunks at a time.
+#pragma unroll
+      for (int ng = 0; ng < NG; ++ng)
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          const int head = 8 * ng + 2 * t + h;
+          if (head >= ended.heads) continue;
+          if (g == 0) store_lse(a, ended, head, m[ng][h], l[ng][h]);
+          const float f = l[ng][h] == 0.f ? 0.f : (Q8 ? v_ref : 1.f) / l[ng][h];
+#pragma unroll
+          for (int i = 0; i < MT; i += 2) {
+            const int k = i / (CE / 2), d = (g + 8 * k) * CE + i % (CE / 2) * 2;
+            float4 x = make_float4(o[i][ng][h], o[i][ng][2 + h], o[i + 1][ng][h], o[i + 1][ng][2 + h]);
+            if (l[ng][h] == 0.f) x = make_float4(0.f, 0.f, 0.f, 0.f);
+            if (d < c.dim) store_wide4(a, ended.b * a.ob + (ended.head + head) * a.oh + d, x.x * f, x.y * f, x.z * f, x.w * f);
+          }
+        }
+      mine_mask &= ~(1u << using_note), copied_mask &= ~(1u << using_note);
+      pump(S::kStages - 1);
+      have = take();
+      continue;
+    }
     // The stage read last holds this warp's o until it is joined.
     float *const o_mine = reinterpret_cast<float *>(mine + (out == 0 ? S::kStages - 1 : out - 1) * S::kTile);
     __syncwarp();
@@ -709,14 +773,12 @@ __global__ void __launch_bounds__(32 * MmaShape<C, DP, NG>::kWarps, 1)
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
         const int head = 8 * ng + 2 * t + h;
-#pragma unroll
-        for (int d = 4; d < 32; d *= 2) l[ng][h] += __shfl_xor_sync(~0u, l[ng][h], d);
         if (g == 0) join.ml[warp][head] = make_float2(m[ng][h], l[ng][h]);
         float *const row = o_mine + head * S::kRow;
 #pragma unroll
         for (int i = 0; i < MT; ++i) {
-          constexpr int CE = VB / EL;  // channels of a chunk, two of them in a tile of 16
-          const int k = i / (CE / 2), d = (g + 8 * k) * CE + i % (CE / 2) * 2;
+          // Two neighbouring channels, at a place that depends on the head so that the lanes meet all banks.
+          const int k = i / (CE / 2), d = ((g + 8 * k) * CE + i % (CE / 2) * 2) ^ (head & 6);
           *reinterpret_cast<float2 *>(row + d) =
               Q8 ? make_float2(o[i][ng][h] * v_ref, o[i][ng][2 + h] * v_ref) : make_float2(o[i][ng][h], o[i][ng][2 + h]);
         }
@@ -725,15 +787,12 @@ __global__ void __launch_bounds__(32 * MmaShape<C, DP, NG>::kWarps, 1)
     if (BOXES) asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
     const float *const o_all = reinterpret_cast<const float *>(shared);
     if (lane == 0) join.at[warp] = (int)(o_mine - o_all);
-    const Segment seg = works[warp][done % kAhead].seg;
-    const Group group = works[warp][done % kAhead].group;
-    __syncwarp();
     // The next segment's first tiles and queries come while this one is joined.
-    ++done;
+    mine_mask &= ~(1u << using_note), copied_mask &= ~(1u << using_note);
     pump(S::kStages - 1);
-    if (done < noted) load_queries();
-    join_warps(a, seg, group, join, o_all, S::kRow);
-    if (!seg.whole) join_parts(a, seg, group, join);
+    have = take();
+    join_warps<W, true>(a, ended, by, join, o_all, S::kRow);
+    if (!ended.whole) join_parts(a, ended, by, join);
   }
 }
 
@@ -744,6 +803,7 @@ template <typename C, int DP, int NG, bool Q32> int launch_mma(DecodeArgs a, int
   using S = MmaShape<C, DP, NG>;
   a.item_heads = std::min(a.group, 8 * NG);
   a.item_groups = (a.group + 8 * NG - 1) / (8 * NG);
+  a.items = divide_by((uint32_t)(a.c.heads * a.item_groups));
   // Boxes of as many rows as a page has in a tile: a tile starts at a multiple of KT rows.
   const int box_rows = a.c.page_size % S::KT == 0 ? S::KT : a.c.page_size % 16 == 0 ? 16 : 8;
   a.box_shift = box_rows == S::KT ? 0 : box_rows * 2 == S::KT ? 1 : 2;
