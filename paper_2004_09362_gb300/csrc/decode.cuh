@@ -38,6 +38,7 @@ struct DecodeArgs {
   int most_rows;           // rows that the table's width can hold
   int unit;                // rows of a unit of the line
   int box_shift;           // log2 of the tensor copies that a tile's rows take
+  bool box_lines;          // a tensor copy brings whole rows, not one line of them
   int batch, q_heads, group, item_groups, item_heads;  // group: q_heads / kv_heads
   Divide items;            // by a sequence's items
   int q_dtype, out_dtype, window;

@@ -136,12 +136,12 @@ template <int BYTES> __device__ __forceinline__ void copy_async(uint32_t to, con
     asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(to), "l"(from), "r"(there ? 4 : 0) : "memory");
 }
 
-// A box of the cache at (byte, row, head, page), zeros outside.
+// A box of the cache at (byte, row, line, head, page), zeros outside.
 __device__ __forceinline__ void copy_box(uint32_t to, const CUtensorMap *map, int byte, int row, int head, int page,
                                          uint32_t barrier) {
   asm volatile(
-      "cp.async.bulk.tensor.4d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5}], [%6];" ::
-          "r"(to), "l"(map), "r"(byte), "r"(row), "r"(head), "r"(page), "r"(barrier)
+      "cp.async.bulk.tensor.5d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5, %6}], "
+      "[%7];" ::"r"(to), "l"(map), "r"(byte), "r"(row), "r"(0), "r"(head), "r"(page), "r"(barrier)
       : "memory");
 }
 
@@ -360,11 +360,16 @@ __global__ void __launch_bounds__(32 * MmaShape<C, DP, NG>::kWarps, 1)
         const int p = __shfl_sync(~0u, rows.page, (held << box_shift) + i);
         const int r = __shfl_sync(~0u, rows.row, (held << box_shift) + i);
         if (lane == 0) {
-#pragma unroll
-          for (int k = 0; k < PARTS; ++k) {
-            const uint32_t to = tile_at + (k * KT + (i * KT >> box_shift)) * LINE;
-            copy_box(to, &k_map, k * LINE, r, get.kv_head, p, bar);
-            copy_box(to + KT * DP * EL, &v_map, k * LINE, r, get.kv_head, p, bar);
+          const uint32_t to = tile_at + (i * KT >> box_shift) * LINE;
+          if (PARTS == 1 || a.box_lines) {
+            copy_box(to, &k_map, 0, r, get.kv_head, p, bar);
+            copy_box(to + KT * DP * EL, &v_map, 0, r, get.kv_head, p, bar);
+          } else {
+#pragma unroll 1
+            for (int k = 0; k < PARTS; ++k) {
+              copy_box(to + k * KT * LINE, &k_map, k * LINE, r, get.kv_head, p, bar);
+              copy_box(to + k * KT * LINE + KT * DP * EL, &v_map, k * LINE, r, get.kv_head, p, bar);
+            }
           }
         }
       }
@@ -796,8 +801,9 @@ __global__ void __launch_bounds__(32 * MmaShape<C, DP, NG>::kWarps, 1)
   }
 }
 
-// Maps of the cache as bytes [pages][heads][page_size][dim]; false where it has none.
-bool box_map(const gar_kv_cache &c, void *base, int line, int rows, CUtensorMap *map);
+// A map of the cache's bytes as [pages][heads][lines of a row][page_size][line], boxes of `lines` lines of `rows` rows;
+// false where it has none.
+bool box_map(const gar_kv_cache &c, void *base, int line, int lines, int rows, CUtensorMap *map);
 
 template <typename C, int DP, int NG, bool Q32> int launch_mma(DecodeArgs a, int sms, gar_stream_t stream) {
   using S = MmaShape<C, DP, NG>;
@@ -808,8 +814,11 @@ template <typename C, int DP, int NG, bool Q32> int launch_mma(DecodeArgs a, int
   const int box_rows = a.c.page_size % S::KT == 0 ? S::KT : a.c.page_size % 16 == 0 ? 16 : 8;
   a.box_shift = box_rows == S::KT ? 0 : box_rows * 2 == S::KT ? 1 : 2;
   CUtensorMap maps[2];
-  const bool boxes = a.c.page_size % 8 == 0 && box_map(a.c, a.c.k, S::LINE, box_rows, &maps[0]) &&
-                     box_map(a.c, a.c.v, S::LINE, box_rows, &maps[1]);
+  // All lines of a row at once where they are whole, else one by one, zeros past the row's end.
+  a.box_lines = a.c.dim * S::EL == DP * S::EL;
+  const int lines = a.box_lines ? S::PARTS : 1;
+  const bool boxes = a.c.page_size % 8 == 0 && box_map(a.c, a.c.k, S::LINE, lines, box_rows, &maps[0]) &&
+                     box_map(a.c, a.c.v, S::LINE, lines, box_rows, &maps[1]);
   constexpr auto rowwise = mma_kernel<C, DP, NG, false, Q32>, boxed = mma_kernel<C, DP, NG, true, Q32>;
   static const cudaError_t e[2] = {
       cudaFuncSetAttribute(rowwise, cudaFuncAttributeMaxDynamicSharedMemorySize, S::kShared),
