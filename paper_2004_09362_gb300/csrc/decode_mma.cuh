@@ -145,6 +145,13 @@ __device__ __forceinline__ void copy_box(uint32_t to, const CUtensorMap *map, in
       : "memory");
 }
 
+// Neighbouring bytes, a multiple of 16 of them at a multiple of 16.
+__device__ __forceinline__ void copy_bytes(uint32_t to, const void *from, int bytes, uint32_t barrier) {
+  asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(to), "l"(from),
+               "r"(bytes), "r"(barrier)
+               : "memory");
+}
+
 // Waits for the barrier's phase; false when that takes longer than anything could (some 0.1 s or more).
 __device__ __forceinline__ bool wait_barrier(uint32_t barrier, uint32_t parity) {
   for (int i = 0; i < 1 << 18; ++i) {
@@ -333,17 +340,18 @@ __global__ void __launch_bounds__(32 * MmaShape<C, DP, NG>::kWarps, 1)
     }
   };
   // Starts the copies of get's tile and goes to the next.
+  const bool box_scales = BOXES && Q8 && a.box_scales, groups = !BOXES || (Q8 && !box_scales);
   const auto issue = [&](int stage) {
     const uint32_t tile_at = mine_at + stage * S::kTile;
     const int n = get.from + get.tile * KT + (lane & (KT - 1));
     int page = rows.page, row = rows.row;
-    if (BOXES) {
+    if (BOXES && groups) {
       const int box = (lane & (KT - 1)) >> (S::kLogTile - box_shift), from = (held << box_shift) + box;
       page = __shfl_sync(~0u, page, from);
       row = __shfl_sync(~0u, row, from) + (lane & ((KT >> box_shift) - 1));
     }
     const bool there = page >= 0 && n >= get.lo && n < get.to;
-    if (Q8 && lane < KT) {
+    if (Q8 && groups && lane < KT) {
       const int64_t at =
           there ? page * c.scale_page_stride + row * c.scale_token_stride + get.kv_head * c.scale_head_stride : 0;
       const uint32_t to = scales_at + stage * S::kScales + lane * 4;
@@ -351,25 +359,38 @@ __global__ void __launch_bounds__(32 * MmaShape<C, DP, NG>::kWarps, 1)
       copy_async<4>(to + KT * 4, c.v_scale + at, there);
     }
     if constexpr (BOXES) {
-      // A box is rows of one page, those outside the segment too; all of a box that has no page is
-      // filled with zeros.
+      // The lanes that hold the tile's boxes copy them.  A box is rows of one page, those outside the segment too;
+      // all of a box that has no page is filled with zeros.
       const uint32_t bar = barrier + 8 * stage;
-      if (lane == 0)
-        asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(S::kTile) : "memory");
-      for (int i = 0; i < 1 << box_shift; ++i) {
-        const int p = __shfl_sync(~0u, rows.page, (held << box_shift) + i);
-        const int r = __shfl_sync(~0u, rows.row, (held << box_shift) + i);
-        if (lane == 0) {
-          const uint32_t to = tile_at + (i * KT >> box_shift) * LINE;
-          if (PARTS == 1 || a.box_lines) {
-            copy_box(to, &k_map, 0, r, get.kv_head, p, bar);
-            copy_box(to + KT * DP * EL, &v_map, 0, r, get.kv_head, p, bar);
-          } else {
+      const bool holds = lane >> box_shift == held;
+      const int box = lane & ((1 << box_shift) - 1), scale_bytes = (KT >> box_shift) * 4;
+      const unsigned with_page = Q8 ? __ballot_sync(~0u, holds && rows.page >= 0) : 0;
+      if (holds) {
+        if (box == 0)
+          asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar),
+                       "r"(S::kTile + (box_scales ? __popc(with_page) * 2 * scale_bytes : 0))
+                       : "memory");
+        const uint32_t to = tile_at + (box * KT >> box_shift) * LINE;
+        if (PARTS == 1 || a.box_lines) {
+          copy_box(to, &k_map, 0, rows.row, get.kv_head, rows.page, bar);
+          copy_box(to + KT * DP * EL, &v_map, 0, rows.row, get.kv_head, rows.page, bar);
+        } else {
 #pragma unroll 1
-            for (int k = 0; k < PARTS; ++k) {
-              copy_box(to + k * KT * LINE, &k_map, k * LINE, r, get.kv_head, p, bar);
-              copy_box(to + k * KT * LINE + KT * DP * EL, &v_map, k * LINE, r, get.kv_head, p, bar);
-            }
+          for (int k = 0; k < PARTS; ++k) {
+            copy_box(to + k * KT * LINE, &k_map, k * LINE, rows.row, get.kv_head, rows.page, bar);
+            copy_box(to + k * KT * LINE + KT * DP * EL, &v_map, k * LINE, rows.row, get.kv_head, rows.page, bar);
+          }
+        }
+        if (box_scales) {
+          const uint32_t scale_to = scales_at + stage * S::kScales + box * scale_bytes;
+          if (rows.page >= 0) {
+            const int64_t at = rows.page * c.scale_page_stride + get.kv_head * c.scale_head_stride + rows.row;
+            copy_bytes(scale_to, c.k_scale + at, scale_bytes, bar);
+            copy_bytes(scale_to + KT * 4, c.v_scale + at, scale_bytes, bar);
+          } else {
+            float *const zero = scales + stage * (S::kScales / 4) + box * (KT >> box_shift);
+            for (int i = 0; i < KT >> box_shift; ++i) zero[i] = zero[KT + i] = 0.f;
+            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
           }
         }
       }
@@ -392,7 +413,7 @@ __global__ void __launch_bounds__(32 * MmaShape<C, DP, NG>::kWarps, 1)
         }
       }
     }
-    if (Q8 || !BOXES) asm volatile("cp.async.commit_group;" ::: "memory");
+    if (groups) asm volatile("cp.async.commit_group;" ::: "memory");
     get.tile += get.step;
     if (get.tile >= get.tiles) {
       advance();
@@ -510,7 +531,7 @@ __global__ void __launch_bounds__(32 * MmaShape<C, DP, NG>::kWarps, 1)
     for (int ng = 0; ng < NG; ++ng) m[ng][0] = m[ng][1] = -INFINITY;
 
     for (; tile < tiles; tile += step) {
-      if (Q8 || !BOXES) {
+      if (groups) {
         if (flying == S::kStages - 1)
           asm volatile("cp.async.wait_group %0;" ::"n"(S::kStages - 2) : "memory");
         else
@@ -526,10 +547,12 @@ __global__ void __launch_bounds__(32 * MmaShape<C, DP, NG>::kWarps, 1)
       if (BOXES && ragged) {
         // What the copies brought of rows outside the segment must not meet the products: 0 * NaN is NaN.
         const int n = n0 + lane;
-        if (lane < KT && (n < lo || n >= to))
+        if (lane < KT && (n < lo || n >= to)) {
+          if (Q8) scales[out * (S::kScales / 4) + KT + lane] = 0.f;
           for (int i = 0; i < PARTS; ++i)
             for (int x = 0; x < LINE; x += 16)
               *reinterpret_cast<uint4 *>(at + KT * DP * EL + (i * KT + lane) * LINE + x) = make_uint4(0, 0, 0, 0);
+        }
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
         __syncwarp();
       }
@@ -816,6 +839,8 @@ template <typename C, int DP, int NG, bool Q32> int launch_mma(DecodeArgs a, int
   CUtensorMap maps[2];
   // All lines of a row at once where they are whole, else one by one, zeros past the row's end.
   a.box_lines = a.c.dim * S::EL == DP * S::EL;
+  a.box_scales = (uintptr_t)a.c.k_scale % 16 == 0 && (uintptr_t)a.c.v_scale % 16 == 0 && a.c.scale_token_stride == 1 &&
+                 a.c.scale_page_stride % 4 == 0 && a.c.scale_head_stride % 4 == 0;
   const int lines = a.box_lines ? S::PARTS : 1;
   const bool boxes = a.c.page_size % 8 == 0 && box_map(a.c, a.c.k, S::LINE, lines, box_rows, &maps[0]) &&
                      box_map(a.c, a.c.v, S::LINE, lines, box_rows, &maps[1]);
