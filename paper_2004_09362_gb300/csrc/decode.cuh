@@ -52,6 +52,16 @@ struct DecodeArgs {
   int dim_pad;             // floats of a stored o row
 };
 
+// x / d; a division in 32-bit floats, put right, where they hold x (the compiler's takes three times as long).
+__device__ __forceinline__ int quotient(int x, int d) {
+  if (x >= 1 << 23) return x / d;
+  float r;
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"((float)d));
+  int q = (int)((float)x * r);
+  const int rest = x - q * d;
+  return rest >= d ? q + 1 : rest < 0 ? q - 1 : q;
+}
+
 struct Span {
   int units;
   int lo, hi, base;        // rows [lo, hi); base: lo rounded down to a multiple of 32
@@ -67,7 +77,9 @@ __device__ __forceinline__ Span span_of(const DecodeArgs &a, int n, int unit) {
   s.hi = n;
   s.lo = a.window > 0 && n > a.window ? n - a.window : 0;
   s.base = s.lo & ~31;
-  s.units = max(1, (int)(((unsigned)(s.hi - s.base) + unit - 1) / (unsigned)unit));
+  // (no more than 2^31: the sum of two ints)
+  const unsigned up = (unsigned)(s.hi - s.base) + unit - 1;
+  s.units = max(1, unit == 64 ? (int)(up >> 6) : up < 1u << 23 ? quotient((int)up, unit) : (int)(up / (unsigned)unit));
   return s;
 }
 
@@ -100,13 +112,23 @@ struct Walk {
     for (int i = b0; i < b1; ++i) mine += span_of(a, n = a.lengths[i], unit).units;
     int total = __reduce_add_sync(~0u, mine);
     lead = 1;
-    const int share = (total * items + ctas - 1) / ctas;  // in units; a part has no fewer
     if (run <= 1 && a.batch * items <= ctas) {
-      for (int u = share; u <= share + share / 4 && u <= (1 << 30) / a.unit; u += max(1, share / 16)) {
+      // Parts of an equal share, or 9/8 or 5/4 of one.  Units that are no more than the CTAs are such parts already.
+      const int share = total * items <= ctas ? 1 : quotient(total * items + ctas - 1, ctas);
+      if (share == 1) lead = 0;
+      const auto fits = [&](int u) {
+        if (u > (1 << 30) / a.unit) return false;
         const int parts = b0 < b1 ? span_of(a, n, u * a.unit).units : 0, all = __reduce_add_sync(~0u, parts);
-        if (all * items <= ctas) {
-          unit = u * a.unit, lead = 0, mine = parts, total = all;
-          break;
+        if (all * items > ctas) return false;
+        unit = u * a.unit, lead = 0, mine = parts, total = all;
+        return true;
+      };
+      if (share > 1 && !fits(share)) {
+        const int total0 = total, mine0 = mine;
+        if (fits((share * 10 + 7) / 8)) {
+          const int unit1 = unit, total1 = total, mine1 = mine;
+          unit = a.unit, total = total0, mine = mine0;
+          if (!fits((share * 9 + 7) / 8)) unit = unit1, total = total1, mine = mine1;
         }
       }
     }
@@ -118,13 +140,13 @@ struct Walk {
       if (lane >= d) before += up;
     }
     before -= mine;
-    per = (total + ctas - 1) / ctas;
+    per = total <= ctas ? 1 : quotient(total + ctas - 1, ctas);
     pos = min(total, (int)blockIdx.x * per);
     end = min(total, pos + per);
     if (pos >= end) return;
     int i = b0;
     const bool here = pos >= before && pos < before + mine;
-    if (here)
+    if (here && run > 1)
       for (; i < b1; ++i) {
         n = a.lengths[i];
         const int units = (span_of(a, n, unit).units + lead) * items;
@@ -134,7 +156,7 @@ struct Walk {
     const int from = __ffs(__ballot_sync(~0u, here)) - 1;
     before = __shfl_sync(~0u, before, from);
     enter(a, __shfl_sync(~0u, i, from), __shfl_sync(~0u, n, from));
-    hh = (pos - before) / s.units;
+    hh = quotient(pos - before, s.units);
     item = before + hh * s.units;
     first_segment = true;
   }
@@ -164,8 +186,8 @@ struct Walk {
     g->first = blockIdx.x, g->parts = 1, g->slot = 0, g->first_late = false;
     if (!g->whole) {
       g->slot = 2 * blockIdx.x + (first_segment ? 0 : 1);
-      g->first = item / per;
-      g->parts = (item + s.units - 1) / per - g->first + 1;
+      g->first = quotient(item, per);
+      g->parts = quotient(item + s.units - 1, per) - g->first + 1;
       g->first_late = g->first * per < item;
     }
     pos += n;
@@ -236,8 +258,8 @@ struct Notes {
     g->first = blockIdx.x, g->parts = 1, g->slot = 0, g->first_late = false;
     if (!n.whole) {
       g->slot = 2 * blockIdx.x + (n.first ? 0 : 1);
-      g->first = n.item / per;
-      g->parts = (n.item + n.units - 1) / per - g->first + 1;
+      g->first = quotient(n.item, per);
+      g->parts = quotient(n.item + n.units - 1, per) - g->first + 1;
       g->first_late = g->first * per < n.item;
     }
   }
@@ -378,10 +400,11 @@ __device__ __forceinline__ void join_warps(const DecodeArgs &a, const Segment &g
 template <int WARPS>
 __device__ __forceinline__ void join_parts(const DecodeArgs &a, const Segment &g, Group group, JoinShared<WARPS> &sh) {
   if (group.thread() == 0) {
-    __threadfence();  // after join_warps' barrier: what the group has stored is seen before the count
+    // After join_warps' barrier: what the group has stored is seen before the count, and what others have stored after it.
     // The counter returns to zero with the last arrival.
-    sh.last[group.first] = atomicInc(a.count + g.first, g.parts - 1) == (unsigned)g.parts - 1;
-    __threadfence();
+    unsigned int before;
+    asm volatile("atom.acq_rel.gpu.global.inc.u32 %0, [%1], %2;" : "=r"(before) : "l"(a.count + g.first), "r"(g.parts - 1) : "memory");
+    sh.last[group.first] = before == (unsigned)g.parts - 1;
   }
   group.sync();
   if (sh.last[group.first]) {

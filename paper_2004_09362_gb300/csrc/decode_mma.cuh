@@ -24,8 +24,8 @@
 //    kSolo tiles goes to one warp whole, so that short sequences need no barrier.
 //
 // 8-bit codes become f16, exactly; a row's key scale multiplies its scores, its value scale
-// its weight, taken relative to the largest value scale so far so that the weights stay in f16's
-// range.  Weights are split into a high and a low 16-bit part, one product each; so are 32-bit queries of
+// its weight, taken relative to the largest value scale so far (and times 2^14) so that the weights stay in
+// f16's range.  Weights are split into a high and a low 16-bit part, one product each; so are 32-bit queries of
 // an 8-bit cache.
 //
 // The tensor cores cut their sums off rather than round them: in long sums that is a bias (4e-5 relative after
@@ -175,6 +175,7 @@ template <> struct words<8> {
 };
 
 constexpr int kSolo = 4;
+constexpr float kWeightUnit = 16384.f;  // what the largest weight over an 8-bit cache is in f16
 
 // DP: the head's channels rounded up to 64, 128 or 256; NG: groups of 8 query heads.  (The queries' type has no part
 // in it.)
@@ -661,7 +662,7 @@ __global__ void __launch_bounds__(32 * MmaShape<C, DP, NG>::kWarps, 1)
       if (Q8) {
         const float most = __uint_as_float(__reduce_max_sync(~0u, __float_as_uint(v_scale[lane & (KT - 1)]) & 0x7fffffffu));
         if (most > v_ref) v_shrink = v_ref / most, v_ref = most;
-        v_inverse = 1.f / v_ref;
+        v_inverse = kWeightUnit / v_ref;
       }
       float shrink[NG][2];
 #pragma unroll
@@ -779,7 +780,7 @@ __global__ void __launch_bounds__(32 * MmaShape<C, DP, NG>::kWarps, 1)
           const int head = 8 * ng + 2 * t + h;
           if (head >= ended.heads) continue;
           if (g == 0) store_lse(a, ended, head, m[ng][h], l[ng][h]);
-          const float f = l[ng][h] == 0.f ? 0.f : (Q8 ? v_ref : 1.f) / l[ng][h];
+          const float f = l[ng][h] == 0.f ? 0.f : (Q8 ? v_ref / kWeightUnit : 1.f) / l[ng][h];
 #pragma unroll
           for (int i = 0; i < MT; i += 2) {
             const int k = i / (CE / 2), d = (g + 8 * k) * CE + i % (CE / 2) * 2;
@@ -794,6 +795,7 @@ __global__ void __launch_bounds__(32 * MmaShape<C, DP, NG>::kWarps, 1)
       continue;
     }
     // The stage read last holds this warp's o until it is joined.
+    const float v_unit = v_ref / kWeightUnit;
     float *const o_mine = reinterpret_cast<float *>(mine + (out == 0 ? S::kStages - 1 : out - 1) * S::kTile);
     __syncwarp();
 #pragma unroll
@@ -808,7 +810,7 @@ __global__ void __launch_bounds__(32 * MmaShape<C, DP, NG>::kWarps, 1)
           // Two neighbouring channels, at a place that depends on the head so that the lanes meet all banks.
           const int k = i / (CE / 2), d = ((g + 8 * k) * CE + i % (CE / 2) * 2) ^ (head & 6);
           *reinterpret_cast<float2 *>(row + d) =
-              Q8 ? make_float2(o[i][ng][h] * v_ref, o[i][ng][2 + h] * v_ref) : make_float2(o[i][ng][h], o[i][ng][2 + h]);
+              Q8 ? make_float2(o[i][ng][h] * v_unit, o[i][ng][2 + h] * v_unit) : make_float2(o[i][ng][h], o[i][ng][2 + h]);
         }
       }
     // (copies into this stage come after the join's barrier)
