@@ -4,8 +4,8 @@
 // Work.  An item is one sequence, one cached head and a group of up to kMaxGroup of the query heads
 // that read it.  The CTAs share the items' rows in one of two ways.
 //  * A segment each: every item is cut into parts of as many rows, the fewest (a multiple of 64) for which
-//    there are no more parts than CTAs.  Taken for up to 32 sequences where no part is over 5/4 of an equal
-//    share.  It leaves a CTA one segment to start and to join.
+//    there are no more parts than CTAs.  Taken for up to 32 sequences where a part is at most 5/4 of an equal
+//    share, or 192 KB more: a second segment to start, and to join, takes a CTA as long as those.
 //  * A line: the items' rows, in units of 64 (more where the line would pass 2^30 units), stand one
 //    behind the other, and CTA i of N takes the i-th of N equal shares.  So every CTA has the same number
 //    of rows to read whatever the lengths are, and thousands of short sequences are not split at all.  Each item
@@ -37,6 +37,7 @@ struct DecodeArgs {
   Divide page;
   int most_rows;           // rows that the table's width can hold
   int unit;                // rows of a unit of the line
+  int slack;               // units of 192 KB
   int box_shift;           // log2 of the tensor copies that a tile's rows take
   bool box_lines;          // a tensor copy brings whole rows, not one line of them
   bool box_scales;         // the scales of a tensor copy's rows are 16-byte pieces side by side
@@ -113,23 +114,27 @@ struct Walk {
     int total = __reduce_add_sync(~0u, mine);
     lead = 1;
     if (run <= 1 && a.batch * items <= ctas) {
-      // Parts of an equal share, or 9/8 or 5/4 of one.  Units that are no more than the CTAs are such parts already.
+      // The smallest parts that are no more than the CTAs, from an equal share on.  Units that are no more than the
+      // CTAs are such parts already.
       const int share = total * items <= ctas ? 1 : quotient(total * items + ctas - 1, ctas);
       if (share == 1) lead = 0;
-      const auto fits = [&](int u) {
-        if (u > (1 << 30) / a.unit) return false;
-        const int parts = b0 < b1 ? span_of(a, n, u * a.unit).units : 0, all = __reduce_add_sync(~0u, parts);
-        if (all * items > ctas) return false;
-        unit = u * a.unit, lead = 0, mine = parts, total = all;
-        return true;
+      const auto parts_of = [&](int u, int *parts) {
+        *parts = b0 < b1 ? span_of(a, n, u * a.unit).units : 0;
+        return __reduce_add_sync(~0u, *parts);
       };
-      if (share > 1 && !fits(share)) {
-        const int total0 = total, mine0 = mine;
-        if (fits((share * 10 + 7) / 8)) {
-          const int unit1 = unit, total1 = total, mine1 = mine;
-          unit = a.unit, total = total0, mine = mine0;
-          if (!fits((share * 9 + 7) / 8)) unit = unit1, total = total1, mine = mine1;
+      int over = share + max(share / 4, a.slack), parts, all;
+      if (share > 1 && over <= (1 << 30) / a.unit && (all = parts_of(over, &parts)) * items <= ctas) {
+        int under = share - 1;  // does not fit, or is too small
+        while (over - under > max(1, share / 16)) {
+          const int u = under == share - 1 ? share : (over + under) / 2;
+          int its_parts;
+          const int its_all = parts_of(u, &its_parts);
+          if (its_all * items <= ctas)
+            over = u, parts = its_parts, all = its_all;
+          else
+            under = u;
         }
+        unit = over * a.unit, lead = 0, mine = parts, total = all;
       }
     }
     total = (total + lead * a.batch) * items, mine = (mine + lead * (b1 - b0)) * items;
