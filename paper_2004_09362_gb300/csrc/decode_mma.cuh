@@ -839,8 +839,9 @@ template <typename C, int DP, int NG, bool Q32> int launch_mma(DecodeArgs a, int
   const int box_rows = a.c.page_size % S::KT == 0 ? S::KT : a.c.page_size % 16 == 0 ? 16 : 8;
   a.box_shift = box_rows == S::KT ? 0 : box_rows * 2 == S::KT ? 1 : 2;
   CUtensorMap maps[2];
-  // All lines of a row at once where they are whole, else one by one, zeros past the row's end.
-  a.box_lines = a.c.dim * S::EL == DP * S::EL;
+  // All lines of a row at once where they are whole and a box has all of a tile's rows (a tile's lines lie KT rows
+  // apart), else one by one, zeros past the row's end.
+  a.box_lines = a.c.dim == DP && a.box_shift == 0;
   a.box_scales = (uintptr_t)a.c.k_scale % 16 == 0 && (uintptr_t)a.c.v_scale % 16 == 0 && a.c.scale_token_stride == 1 &&
                  a.c.scale_page_stride % 4 == 0 && a.c.scale_head_stride % 4 == 0;
   const int lines = a.box_lines ? S::PARTS : 1;

@@ -663,3 +663,109 @@ def test_streams_and_graphs():
         main.wait_stream(side)
     torch.cuda.synchronize()
     assert all(torch.equal(a, b) for a, b in zip(got, want))
+
+
+# ---------------------------------------------------------------------------- the kernels' other paths
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("kind,dtype", [("bf16", "bf16"), ("i8", "bf16"), ("f32", "f32")])
+def test_attention_of_thousands_of_short_sequences(kind, dtype):
+    """More segments to a CTA than it notes at a time, many of them empty."""
+    lengths = [(i * 7) % 90 if i % 3 else (i % 5 == 0) * 150 for i in range(2500)]
+    cache, table, lens, q, kvs = _attn_case(lengths, 8, 4, 64, 16, kind, dtype)
+    plan = gar.gar_attn_plan_create(8, 4, 64)
+    out, lse = gar.gar_decode_attention(plan, q, cache, table, lens, lse=True)
+    some = [i for i in range(len(lengths)) if i % 37 == 0 or lengths[i] == 150]
+    _check_attn(out[some], lse[some], q[some], [kvs[i] for i in some], [lengths[i] for i in some], 0, 0.125, dtype)
+    empty = lens == 0
+    assert bool((out[empty] == 0).all()) and bool((lse[empty] == -math.inf).all()) and bool(lse[~empty].isfinite().all())
+    assert torch.equal(out, gar.gar_decode_attention(plan, q, cache, table, lens))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("batch", [1, 31, 32, 33, 200])
+@pytest.mark.parametrize("window", [0, 300])
+def test_attention_both_ways_of_sharing(batch, window):
+    """Batches on both sides of where the rows are shared out another way."""
+    lengths = [1 + (b * 1013) % 1777 for b in range(batch)]
+    cache, table, lens, q, kvs = _attn_case(lengths, 6, 3, 128, 8, "bf16", "bf16")
+    plan = gar.gar_attn_plan_create(6, 3, 128)
+    out, lse = gar.gar_decode_attention(plan, q, cache, table, lens, window=window, lse=True)
+    _check_attn(out, lse, q, kvs, lengths, window, 128 ** -0.5, "bf16")
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("kind,dtype", [("i8", "f16"), ("e4m3", "bf16"), ("bf16", "bf16"), ("f16", "f16"), ("f32", "f32")])
+def test_attention_strides_and_alignments(kind, dtype):
+    """Caches cut out of larger tensors, scales with strides of their own, queries that are not aligned."""
+    lengths, heads, dim, page = [70, 33, 1], 2, 64, 16
+    base, table, lens, q, kvs = _attn_case(lengths, 6, heads, dim, page, kind, dtype)
+    plan = gar.gar_attn_plan_create(6, heads, dim)
+    want = gar.gar_decode_attention(plan, q, base, table, lens)
+    n = base.k.shape[0]
+
+    def copy_into(width, offset):
+        wide = [torch.zeros((n, heads, page, width), dtype=torch.float32, device="cuda").to(base.k.dtype) for _ in range(2)]
+        cut = [t[..., offset:offset + dim] for t in wide]
+        for c, x in zip(cut, (base.k, base.v)):
+            (c.view(torch.uint8) if kind in QMAX else c).copy_(x.view(torch.uint8) if kind in QMAX else x)
+        return cut
+
+    step = 16 // base.k.element_size()
+    for width, offset in ((dim + step, 0), (dim + step, step), (dim + 1, 1), (dim + 3, 0)):
+        scales = [] if kind not in QMAX else [base.k_scale, base.v_scale]
+        got = gar.gar_decode_attention(plan, q, gar.KVCache(*copy_into(width, offset), *scales), table, lens)
+        close = 2 * ROUND[dtype] * want.float().abs() + 2.0 ** -14 * want.float().abs().max()
+        assert bool(((got.float() - want.float()).abs() <= close).all())
+    if kind in QMAX:
+        for make in (lambda s: torch.stack([s, s], -1)[..., 0], lambda s: s.transpose(1, 2).contiguous().transpose(1, 2),
+                     lambda s: torch.nn.functional.pad(s, (1, 2))[..., 1:-2]):
+            got = gar.gar_decode_attention(plan, q, gar.KVCache(base.k, base.v, make(base.k_scale), make(base.v_scale)), table, lens)
+            assert torch.equal(got, want)
+    shifted = torch.zeros(len(lengths) * 6 * dim + 1, dtype=q.dtype, device="cuda")[1:].view(len(lengths), 6, dim)
+    shifted.copy_(q)
+    got = gar.gar_decode_attention(plan, shifted, base, table, lens)
+    assert bool(((got.float() - want.float()).abs() <= 2 * ROUND[dtype] * want.float().abs() + 2.0 ** -14 * want.float().abs().max()).all())
+    into = torch.zeros(len(lengths), 6, dim + 1, dtype=q.dtype, device="cuda")
+    gar.gar_decode_attention(plan, q, base, table, lens, out=into[..., 1:])
+    assert torch.equal(into[..., 1:], want) and bool((into[..., 0] == 0).all())
+
+
+@pytest.mark.gpu
+def test_attention_holds_its_sums_in_32_bits():
+    """All-positive values over 200000 rows: a sum that is cut off at each step would be off by 1e-4."""
+    n, dim = 200000, 128
+    for dtype in ("bf16", "f32"):
+        k = torch.zeros(n // 64, 1, 64, dim, device="cuda", dtype=TORCH[dtype])
+        v = (_randn((n // 64, 1, 64, dim), dtype, 1).float().abs() + 1).to(TORCH[dtype])
+        table = torch.arange(n // 64, dtype=torch.int32, device="cuda")[None].repeat(152, 1)   # one CTA for each sequence
+        lens = torch.full((152,), n, dtype=torch.int32, device="cuda")
+        plan = gar.gar_attn_plan_create(1, 1, dim)
+        out = torch.empty(152, 1, dim, device="cuda")
+        gar.gar_decode_attention(plan, _randn((152, 1, dim), dtype, 2), gar.KVCache(k, v), table, lens, out=out)
+        want = v.double().mean((0, 1, 2))
+        # weights are all 1; 12 warps' sums of n / 12 rows, 16 at a time, then their join: random roundings of
+        # u each, at most n / 192 of them in a row
+        assert float(((out[:, 0].double() - want) / want).abs().max()) <= 2 * (n / 192) ** 0.5 * U32 + 2.0 ** -21
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("kind", ["i8", "e4m3"])
+def test_attention_rows_of_very_different_scales(kind):
+    """Values a million times smaller than others of the sequence, with nearly all of the weight."""
+    cache, table, lens, q, kvs = _attn_case([100], 2, 1, 64, 16, kind, "f32")
+    row = 37
+    page, at = table[0, row // 16].long(), row % 16
+    cache.k.view(torch.uint8)[page, 0, at] = torch.tensor([100] * 64, dtype=torch.int8, device="cuda").to(cache.k.dtype).view(torch.uint8)
+    cache.k_scale[page, 0, at], cache.v_scale[page, 0, at] = 0.1, 1e-8
+    q[:] = 0.5
+    k, v = gar.gar_kv_read(cache, page * 16 + torch.arange(16, device="cuda"), "f32")
+    kvs = [[x.clone() for x in kvs[0]]]
+    kvs[0][0][row], kvs[0][1][row] = k[at].double(), v[at].double()
+    plan = gar.gar_attn_plan_create(2, 1, 64)
+    out, lse = gar.gar_decode_attention(plan, q, cache, table, lens, lse=True)
+    y = torch.einsum("hd,nhd->hn", q[0].double(), kvs[0][0].repeat_interleave(2, 1)) / 8
+    want = torch.einsum("hn,nhd->hd", torch.softmax(y, -1), kvs[0][1].repeat_interleave(2, 1))
+    assert float(torch.softmax(y, -1)[:, row].min()) > 1 - 1e-9
+    # the weight is 2^14 * 1e-6 in f16, in two parts: off by 2^-25 of f16's unit, 2^-11 of it in the worst case
+    assert float((out[0].double() - want).norm() / want.norm()) <= 2.0 ** -10
