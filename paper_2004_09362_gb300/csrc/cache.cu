@@ -248,7 +248,7 @@ __global__ void __launch_bounds__(kThreads, RUN ? 4 : 1) write_kernel(const Cach
   Place p{};
   struct Raw {
     raw_chunk<T, N> k, v;
-  } now, next;
+  } now{}, next{};
   using Side = raw_chunk<T, N / 2>;
   using Codes = raw_chunk<C, N / 2>;
   const auto fetch = [&](Raw &r, int h) {
@@ -273,32 +273,31 @@ __global__ void __launch_bounds__(kThreads, RUN ? 4 : 1) write_kernel(const Cach
   // All lanes of a warp go round as often: the shuffles are the warp's.
   for (int j = 0; j < (RUN ? a.run : 1); ++j) {
     const int h = first + j;
-    if (RUN) fetch(next, h + 1);
-    const bool mine = in && h < end, here = there && h < end;
-    float2 k[N / 2] = {}, v[N / 2] = {};
-    if (mine) {
-      if (WIDE) {
-        values(now.k, k);
-        values(now.v, v);
-      } else {
-        load<WIDE, T, N>(k_rows + h * a.hs[0], from, c.dim, k);
-        load<WIDE, T, N>(v_rows + h * a.hs[1], from, c.dim, v);
-      }
-      if (turned && there) rotate<TURN, T, N, E>(a, turn, cosine, sine, k_rows + h * a.hs[0], from, k);
+    if (RUN && h + 1 < first + a.run) fetch(next, h + 1);
+    const bool mine = in && there && h < end;
+    // (Lanes and heads with nothing to do go along with zeros or with what they had.)
+    float2 k[N / 2], v[N / 2];
+    if (WIDE) {
+      values(now.k, k);
+      values(now.v, v);
+    } else {
+      load<WIDE, T, N>(k_rows + h * a.hs[0], from, in && h < end ? c.dim : 0, k);
+      load<WIDE, T, N>(v_rows + h * a.hs[1], from, in && h < end ? c.dim : 0, v);
     }
+    if (TURN != TURN_NONE && turned && there && h < end)
+      rotate<TURN, T, N, E>(a, turn, cosine, sine, k_rows + h * a.hs[0], from, k);
     if constexpr (quantised<C>::value) {
       uint32_t k_most, v_most;
       if constexpr (WIDE && sizeof(T) == 2) {
-        k_most = mine ? (TURN == TURN_NONE ? largest(now.k) : largest(k)) : 0;
-        v_most = mine ? largest(now.v) : 0;
+        k_most = TURN == TURN_NONE ? largest(now.k) : largest(k), v_most = largest(now.v);
       } else {
         k_most = largest(k), v_most = largest(v);
       }
       float k_scale, v_scale;
       const raw_chunk<C, N> k_codes = quantise<C, N>(k, k_most, a.lanes, &k_scale);
       const raw_chunk<C, N> v_codes = quantise<C, N>(v, v_most, a.lanes, &v_scale);
-      if (here && lane == 0) c.k_scale[p.scale] = k_scale, c.v_scale[p.scale] = v_scale;
-      if (mine && here) {
+      if (mine && lane == 0) c.k_scale[p.scale] = k_scale, c.v_scale[p.scale] = v_scale;
+      if (mine) {
         C *const row = static_cast<C *>(c.k) + p.at;
         if constexpr (TURN == TURN_HALF) {
           *reinterpret_cast<Codes *>(row + lower) = *reinterpret_cast<const Codes *>(k_codes.w);
@@ -309,7 +308,7 @@ __global__ void __launch_bounds__(kThreads, RUN ? 4 : 1) write_kernel(const Cach
         store_codes<WIDE>(static_cast<C *>(c.v) + p.at, from, c.dim, v_codes);
       }
       p.scale += c.scale_head_stride;
-    } else if (mine && here) {
+    } else if (mine) {
       C *const row = static_cast<C *>(c.k) + p.at;
       if constexpr (TURN == TURN_HALF) {
         const float2 x[N / 4] = {k[0], k[1]}, y[N / 4] = {k[2], k[3]};
