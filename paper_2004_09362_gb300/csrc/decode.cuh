@@ -9,7 +9,7 @@
 //  * A line: the items' rows, in units of 64 (more where the line would pass 2^30 units), stand one
 //    behind the other, and CTA i of N takes the i-th of N equal shares.  So every CTA has the same number
 //    of rows to read whatever the lengths are, and thousands of short sequences are not split at all.  Each item
-//    counts one unit more, for what it costs beside its rows.
+//    counts 192 KB of rows more, for what a segment costs beside its rows, or the items' mean where that is less.
 // The lengths are read on the device: nothing waits for the host, and a captured launch stays
 // right when they change.
 //
@@ -112,7 +112,7 @@ struct Walk {
     int mine = 0, n = 0;
     for (int i = b0; i < b1; ++i) mine += span_of(a, n = a.lengths[i], unit).units;
     int total = __reduce_add_sync(~0u, mine);
-    lead = 1;
+    lead = min(a.slack, quotient(total, a.batch));
     if (run <= 1 && a.batch * items <= ctas) {
       // The smallest parts that are no more than the CTAs, from an equal share on.  Units that are no more than the
       // CTAs are such parts already.

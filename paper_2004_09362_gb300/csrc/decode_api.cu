@@ -170,7 +170,7 @@ int gar_decode_attention(gar_attn_plan *plan, const gar_kv_cache *cache, const v
   const int64_t items = (int64_t)batch * plan->kv_heads * ((a.group + 7) / 8);
   if (items >= 1 << 28) return refuse("too many sequences and heads");
   a.unit = 64;
-  while (items * (a.most_rows / a.unit + 3) >= 1 << 30) a.unit *= 2;
+  while (items * (a.most_rows / a.unit + 3) * 2 >= 1 << 30) a.unit *= 2;
   a.slack = std::max(1, 196608 / (128 * cache->dim * element_size(cache->dtype)));
   if (a.unit > 32768) return refuse("too many sequences and heads for tables this wide");
   if (!takes_mma(*cache, q, q_batch_stride, q_head_stride, q_dtype)) return decode_general(a, plan->sms, stream);
