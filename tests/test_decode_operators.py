@@ -69,7 +69,7 @@ def _rope_raw(x=4096, out=8192, dtype=gar.GAR_BF16, tokens=4, heads=2, dim=64, r
 @pytest.mark.parametrize("bad,code", [
     (dict(x=None), -1), (dict(out=None), -1), (dict(positions=None), -1), (dict(table=None), -1), (dict(dtype=gar.GAR_I32), -1),
     (dict(dtype=gar.GAR_I8), -1), (dict(dim=257, rot=64), -1), (dict(rot=3), -1), (dict(rot=66), -1), (dict(rot=0), -1),
-    (dict(tokens=-1), -1), (dict(heads=-1), -1), (dict(layout=2), -1), (dict(width=2), -1), (dict(rows=-1), -1),
+    (dict(tokens=-1), -1), (dict(heads=-1), -1), (dict(heads=(1 << 20) + 1), -1), (dict(layout=2), -1), (dict(width=2), -1), (dict(rows=-1), -1),
     (dict(x=4097), -3), (dict(table=4100), -3), (dict(positions=4100), -3), (dict(out=4096, os_=(64, 64)), -1)])
 def test_rope_refusals(bad, code):
     assert _rope_raw(**bad) == code
@@ -124,6 +124,12 @@ def test_plan_refusals(args):
     with pytest.raises(gar.GarError) as e:
         gar.gar_attn_plan_create(*args)
     assert e.value.code == -1
+
+
+def test_plan_shape():
+    plan = gar.gar_attn_plan_create(6, 2, 80)
+    assert gar.gar_attn_plan_shape(plan) == (6, 2, 80)
+    assert gar._lib.gar_attn_plan_shape(None, None, None, None) == -1
 
 
 def test_attention_refusals_without_a_gpu():
@@ -692,6 +698,17 @@ def test_attention_both_ways_of_sharing(batch, window):
     plan = gar.gar_attn_plan_create(6, 3, 128)
     out, lse = gar.gar_decode_attention(plan, q, cache, table, lens, window=window, lse=True)
     _check_attn(out, lse, q, kvs, lengths, window, 128 ** -0.5, "bf16")
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("kind,dtype,dim", [("bf16", "bf16", 64), ("e4m3", "f16", 128), ("f32", "f32", 48), ("f16", "f16", 33)])
+def test_attention_of_few_heads_over_ragged_sequences(kind, dtype, dim):
+    """Shares of the rows that are smaller than what an item counts beside them, so that some hold no row of theirs."""
+    lengths = [0 if b % 4 == 3 else 3000 if b % 4 == 2 else 1 + b * 61 for b in range(40)]
+    cache, table, lens, q, kvs = _attn_case(lengths, 4, 1, dim, 16, kind, dtype)
+    plan = gar.gar_attn_plan_create(4, 1, dim)
+    out, lse = gar.gar_decode_attention(plan, q, cache, table, lens, lse=True)
+    _check_attn(out, lse, q, kvs, lengths, 0, dim ** -0.5, dtype)
 
 
 @pytest.mark.gpu
