@@ -38,9 +38,7 @@ struct DecodeArgs {
   int most_rows;           // rows that the table's width can hold
   int unit;                // rows of a unit of the line
   int slack;               // units of 192 KB
-  int box_shift;           // log2 of the tensor copies that a tile's rows take
-  bool box_lines;          // a tensor copy brings whole rows, not one line of them
-  bool box_scales;         // the scales of a tensor copy's rows are 16-byte pieces side by side
+  int solo;                // tiles of an item that a warp takes whole
   int batch, q_heads, group, item_groups, item_heads;  // group: q_heads / kv_heads
   Divide items;            // by a sequence's items
   int q_dtype, out_dtype, window;

@@ -33,7 +33,7 @@ bool takes_mma(const gar_kv_cache &c, const void *q, int64_t q_batch_stride, int
 
 }  // namespace
 
-bool box_map(const gar_kv_cache &c, void *base, int line, int lines, int rows, CUtensorMap *map) {
+bool box_map(const gar_kv_cache &c, void *base, int rows, CUtensorMap *map) {
   using Encode = CUresult (*)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *,
                               const cuuint64_t *, const cuuint32_t *, const cuuint32_t *, CUtensorMapInterleave,
                               CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
@@ -45,16 +45,13 @@ bool box_map(const gar_kv_cache &c, void *base, int line, int lines, int rows, C
   }();
   if (encode == nullptr || c.pages < 1) return false;
   const int size = element_size(c.dtype);
-  // One line at a time, the row is one long line, so that what a box has past its end is zero.
-  const cuuint64_t row = (cuuint64_t)c.dim * size;
-  const cuuint64_t extent[5] = {lines > 1 ? (cuuint64_t)line : row, (cuuint64_t)c.page_size, (cuuint64_t)lines, (cuuint64_t)c.heads,
-                                (cuuint64_t)c.pages};
-  const cuuint64_t stride[4] = {(cuuint64_t)c.token_stride * size, (cuuint64_t)line, (cuuint64_t)c.head_stride * size,
+  const cuuint32_t line = 128, lines = (cuuint32_t)(c.dim * size) / line;
+  const cuuint64_t extent[5] = {line, (cuuint64_t)c.page_size, lines, (cuuint64_t)c.heads, (cuuint64_t)c.pages};
+  const cuuint64_t stride[4] = {(cuuint64_t)c.token_stride * size, line, (cuuint64_t)c.head_stride * size,
                                 (cuuint64_t)c.page_stride * size};
-  const cuuint32_t box[5] = {(cuuint32_t)line, (cuuint32_t)rows, (cuuint32_t)lines, 1, 1}, step[5] = {1, 1, 1, 1, 1};
+  const cuuint32_t box[5] = {line, (cuuint32_t)rows, lines, 1, 1}, step[5] = {1, 1, 1, 1, 1};
   return encode(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 5, base, extent, stride, box, step, CU_TENSOR_MAP_INTERLEAVE_NONE,
-                line == 128 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
-                CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+                CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
 }  // namespace gar

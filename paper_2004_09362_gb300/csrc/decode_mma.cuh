@@ -136,20 +136,13 @@ template <int BYTES> __device__ __forceinline__ void copy_async(uint32_t to, con
     asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(to), "l"(from), "r"(there ? 4 : 0) : "memory");
 }
 
-// A box of the cache at (byte, row, line, head, page), zeros outside.
-__device__ __forceinline__ void copy_box(uint32_t to, const CUtensorMap *map, int byte, int row, int head, int page,
+// The rows of the cache from (row, head, page) on that a tile holds, zeros outside.
+__device__ __forceinline__ void copy_box(uint32_t to, const CUtensorMap *map, int row, int head, int page,
                                          uint32_t barrier) {
   asm volatile(
       "cp.async.bulk.tensor.5d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5, %6}], "
-      "[%7];" ::"r"(to), "l"(map), "r"(byte), "r"(row), "r"(0), "r"(head), "r"(page), "r"(barrier)
+      "[%7];" ::"r"(to), "l"(map), "r"(0), "r"(row), "r"(0), "r"(head), "r"(page), "r"(barrier)
       : "memory");
-}
-
-// Neighbouring bytes, a multiple of 16 of them at a multiple of 16.
-__device__ __forceinline__ void copy_bytes(uint32_t to, const void *from, int bytes, uint32_t barrier) {
-  asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(to), "l"(from),
-               "r"(bytes), "r"(barrier)
-               : "memory");
 }
 
 // Waits for the barrier's phase; false when that takes longer than anything could (some 0.1 s or more).
@@ -174,7 +167,6 @@ template <> struct words<8> {
   using type = uint2;
 };
 
-constexpr int kSolo = 4;
 constexpr float kWeightUnit = 16384.f;  // what the largest weight over an 8-bit cache is in f16
 
 // DP: the head's channels rounded up to 64, 128 or 256; NG: groups of 8 query heads.  (The queries' type has no part
@@ -192,6 +184,8 @@ template <typename C, int DP, int NG> struct MmaShape {
   static constexpr int kMost = 196608 / kTile / 2, kLike = NG == 1 && DP <= 128 ? 12 : 8;
   static constexpr int kWarps = kMost < kLike ? kMost : kLike;
   static constexpr int kStages = 196608 / kWarps / kTile;
+  // Whole rows of at least 512 bytes can be copied as boxes.
+  static constexpr bool kBoxes = DP == 256 && !Q8;
   static constexpr int kScales = Q8 ? 2 * KT * 4 : 0;
   // Floats of an o row; a row of o for each head fits a stage.  A few floats more than DP spread
   // the rows over the banks.
@@ -261,7 +255,7 @@ __global__ void __launch_bounds__(32 * MmaShape<C, DP, NG>::kWarps, 1)
   // Few tiles of a whole item, or hardly any: one warp's, in turn.  Else tile by tile the warps'.
   const auto group_of = [&](int i, const Note &n) {
     const int tiles = tiles_of(n);
-    return tiles <= (n.whole ? kSolo : 1) ? Group{i % W, 1} : Group{0, min(W, tiles)};
+    return tiles <= (n.whole ? a.solo : 1) ? Group{i % W, 1} : Group{0, min(W, tiles)};
   };
   const auto fill = [&] {
     Notes c = course[warp];
@@ -286,22 +280,20 @@ __global__ void __launch_bounds__(32 * MmaShape<C, DP, NG>::kWarps, 1)
     int from, lo, to, b, kv_head, tile, step, tiles;
   } get{};                               // what is being copied
   bool ready = false;                    // get's tile exists and its pages are known
-  // The cache rows of get's tile.  Copied row by row: the page of this lane's row of the tile.  In boxes: this
-  // lane's box (lane % boxes of a tile) of the (lane / boxes)-th of the warp's next tiles, its page and the row
-  // in it, and the same of the tiles after those.
+  // The cache rows of get's tile.  Copied row by row: this lane's row of the tile, its page and the row in it.  In
+  // boxes: the first row of the lane-th of the warp's next tiles, and of the 32 tiles after those.
   struct Rows {
     int page, row;
   } rows{-1, 0}, later{-1, 0};
   int held = 0;                          // boxes: tiles of `rows` that have been copied
-  const int box_shift = BOXES ? a.box_shift : 0, box_tiles = 32 >> box_shift;
   const auto find_rows = [&](int tile) {
     int n;
     Rows x{-1, 0};
     bool there;
     if (BOXES) {
-      tile += (lane >> box_shift) * get.step;
-      n = get.from + tile * KT + (lane & ((1 << box_shift) - 1)) * (KT >> box_shift);
-      there = tile < get.tiles && n < get.to && n + (KT >> box_shift) > get.lo;
+      tile += lane * get.step;
+      n = get.from + tile * KT;
+      there = tile < get.tiles && n < get.to && n + KT > get.lo;
     } else {
       n = get.from + tile * KT + (lane & (KT - 1));
       there = n >= get.lo && n < get.to;
@@ -337,65 +329,31 @@ __global__ void __launch_bounds__(32 * MmaShape<C, DP, NG>::kWarps, 1)
     if (ready) {
       rows = find_rows(get.tile);
       held = 0;
-      if (BOXES) later = find_rows(get.tile + box_tiles * get.step);
+      if (BOXES) later = find_rows(get.tile + 32 * get.step);
     }
   };
   // Starts the copies of get's tile and goes to the next.
-  const bool box_scales = BOXES && Q8 && a.box_scales, groups = !BOXES || (Q8 && !box_scales);
   const auto issue = [&](int stage) {
     const uint32_t tile_at = mine_at + stage * S::kTile;
-    const int n = get.from + get.tile * KT + (lane & (KT - 1));
-    int page = rows.page, row = rows.row;
-    if (BOXES && groups) {
-      const int box = (lane & (KT - 1)) >> (S::kLogTile - box_shift), from = (held << box_shift) + box;
-      page = __shfl_sync(~0u, page, from);
-      row = __shfl_sync(~0u, row, from) + (lane & ((KT >> box_shift) - 1));
-    }
-    const bool there = page >= 0 && n >= get.lo && n < get.to;
-    if (Q8 && groups && lane < KT) {
-      const int64_t at =
-          there ? page * c.scale_page_stride + row * c.scale_token_stride + get.kv_head * c.scale_head_stride : 0;
-      const uint32_t to = scales_at + stage * S::kScales + lane * 4;
-      copy_async<4>(to, c.k_scale + at, there);
-      copy_async<4>(to + KT * 4, c.v_scale + at, there);
-    }
     if constexpr (BOXES) {
-      // The lanes that hold the tile's boxes copy them.  A box is rows of one page, those outside the segment too;
-      // all of a box that has no page is filled with zeros.
+      // The lane that holds the tile copies it: rows of one page, those outside the segment too; zeros where there
+      // is no page.
       const uint32_t bar = barrier + 8 * stage;
-      const bool holds = lane >> box_shift == held;
-      const int box = lane & ((1 << box_shift) - 1), scale_bytes = (KT >> box_shift) * 4;
-      const unsigned with_page = Q8 ? __ballot_sync(~0u, holds && rows.page >= 0) : 0;
-      if (holds) {
-        if (box == 0)
-          asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar),
-                       "r"(S::kTile + (box_scales ? __popc(with_page) * 2 * scale_bytes : 0))
-                       : "memory");
-        const uint32_t to = tile_at + (box * KT >> box_shift) * LINE;
-        if (PARTS == 1 || a.box_lines) {
-          copy_box(to, &k_map, 0, rows.row, get.kv_head, rows.page, bar);
-          copy_box(to + KT * DP * EL, &v_map, 0, rows.row, get.kv_head, rows.page, bar);
-        } else {
-#pragma unroll 1
-          for (int k = 0; k < PARTS; ++k) {
-            copy_box(to + k * KT * LINE, &k_map, k * LINE, rows.row, get.kv_head, rows.page, bar);
-            copy_box(to + k * KT * LINE + KT * DP * EL, &v_map, k * LINE, rows.row, get.kv_head, rows.page, bar);
-          }
-        }
-        if (box_scales) {
-          const uint32_t scale_to = scales_at + stage * S::kScales + box * scale_bytes;
-          if (rows.page >= 0) {
-            const int64_t at = rows.page * c.scale_page_stride + get.kv_head * c.scale_head_stride + rows.row;
-            copy_bytes(scale_to, c.k_scale + at, scale_bytes, bar);
-            copy_bytes(scale_to + KT * 4, c.v_scale + at, scale_bytes, bar);
-          } else {
-            float *const zero = scales + stage * (S::kScales / 4) + box * (KT >> box_shift);
-            for (int i = 0; i < KT >> box_shift; ++i) zero[i] = zero[KT + i] = 0.f;
-            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-          }
-        }
+      if (lane == held) {
+        asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(S::kTile) : "memory");
+        copy_box(tile_at, &k_map, rows.row, get.kv_head, rows.page, bar);
+        copy_box(tile_at + KT * DP * EL, &v_map, rows.row, get.kv_head, rows.page, bar);
       }
     } else {
+      const int n = get.from + get.tile * KT + (lane & (KT - 1)), page = rows.page, row = rows.row;
+      const bool there = page >= 0 && n >= get.lo && n < get.to;
+      if (Q8 && lane < KT) {
+        const int64_t scale_at =
+            there ? page * c.scale_page_stride + row * c.scale_token_stride + get.kv_head * c.scale_head_stride : 0;
+        const uint32_t to = scales_at + stage * S::kScales + lane * 4;
+        copy_async<4>(to, c.k_scale + scale_at, there);
+        copy_async<4>(to + KT * 4, c.v_scale + scale_at, there);
+      }
       const int64_t at = there ? (page * c.page_stride + get.kv_head * c.head_stride + row * c.token_stride) * EL : -1;
       constexpr int LANES = LINE / 16, ROWS = 32 / LANES;
       const char *const kp = static_cast<const char *>(c.k), *const vp = static_cast<const char *>(c.v);
@@ -413,16 +371,16 @@ __global__ void __launch_bounds__(32 * MmaShape<C, DP, NG>::kWarps, 1)
           copy_async<16>(to + KT * DP * EL, in ? vp + x + off : vp, in);
         }
       }
+      asm volatile("cp.async.commit_group;" ::: "memory");
     }
-    if (groups) asm volatile("cp.async.commit_group;" ::: "memory");
     get.tile += get.step;
     if (get.tile >= get.tiles) {
       advance();
     } else if (!BOXES) {
       rows = find_rows(get.tile);
-    } else if (++held == box_tiles) {
+    } else if (++held == 32) {
       rows = later, held = 0;
-      later = find_rows(get.tile + box_tiles * get.step);
+      later = find_rows(get.tile + 32 * get.step);
     }
   };
   int in = 0, out = 0, flying = 0;  // stages copied into and used next; tiles on their way or here
@@ -532,13 +490,14 @@ __global__ void __launch_bounds__(32 * MmaShape<C, DP, NG>::kWarps, 1)
     for (int ng = 0; ng < NG; ++ng) m[ng][0] = m[ng][1] = -INFINITY;
 
     for (; tile < tiles; tile += step) {
-      if (groups) {
+      if (BOXES) {
+        if (!wait_barrier(barrier + 8 * out, parity) && c.status) atomicOr(c.status, GAR_KV_TIMEOUT);
+      } else {
         if (flying == S::kStages - 1)
           asm volatile("cp.async.wait_group %0;" ::"n"(S::kStages - 2) : "memory");
         else
           asm volatile("cp.async.wait_group 0;" ::: "memory");
       }
-      if (BOXES && !wait_barrier(barrier + 8 * out, parity) && c.status) atomicOr(c.status, GAR_KV_TIMEOUT);
       __syncwarp();
       pump(S::kStages);
       char *const at = mine + out * S::kTile;
@@ -548,12 +507,10 @@ __global__ void __launch_bounds__(32 * MmaShape<C, DP, NG>::kWarps, 1)
       if (BOXES && ragged) {
         // What the copies brought of rows outside the segment must not meet the products: 0 * NaN is NaN.
         const int n = n0 + lane;
-        if (lane < KT && (n < lo || n >= to)) {
-          if (Q8) scales[out * (S::kScales / 4) + KT + lane] = 0.f;
+        if (lane < KT && (n < lo || n >= to))
           for (int i = 0; i < PARTS; ++i)
             for (int x = 0; x < LINE; x += 16)
               *reinterpret_cast<uint4 *>(at + KT * DP * EL + (i * KT + lane) * LINE + x) = make_uint4(0, 0, 0, 0);
-        }
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
         __syncwarp();
       }
@@ -826,34 +783,28 @@ __global__ void __launch_bounds__(32 * MmaShape<C, DP, NG>::kWarps, 1)
   }
 }
 
-// A map of the cache's bytes as [pages][heads][lines of a row][page_size][line], boxes of `lines` lines of `rows` rows;
+// A map of the cache's bytes as [pages][heads][lines of a row][page_size][128], boxes of the lines of `rows` rows;
 // false where it has none.
-bool box_map(const gar_kv_cache &c, void *base, int line, int lines, int rows, CUtensorMap *map);
+bool box_map(const gar_kv_cache &c, void *base, int rows, CUtensorMap *map);
 
 template <typename C, int DP, int NG, bool Q32> int launch_mma(DecodeArgs a, int sms, gar_stream_t stream) {
   using S = MmaShape<C, DP, NG>;
   a.item_heads = std::min(a.group, 8 * NG);
   a.item_groups = (a.group + 8 * NG - 1) / (8 * NG);
   a.items = divide_by((uint32_t)(a.c.heads * a.item_groups));
-  // Boxes of as many rows as a page has in a tile: a tile starts at a multiple of KT rows.
-  const int box_rows = a.c.page_size % S::KT == 0 ? S::KT : a.c.page_size % 16 == 0 ? 16 : 8;
-  a.box_shift = box_rows == S::KT ? 0 : box_rows * 2 == S::KT ? 1 : 2;
+  a.solo = std::min(64, std::max(4, (int)(2 * (int64_t)a.batch * a.c.heads * a.item_groups / sms)));
   CUtensorMap maps[2];
-  // All lines of a row at once where they are whole and a box has all of a tile's rows (a tile's lines lie KT rows
-  // apart), else one by one, zeros past the row's end.
-  a.box_lines = a.c.dim == DP && a.box_shift == 0;
-  a.box_scales = (uintptr_t)a.c.k_scale % 16 == 0 && (uintptr_t)a.c.v_scale % 16 == 0 && a.c.scale_token_stride == 1 &&
-                 a.c.scale_page_stride % 4 == 0 && a.c.scale_head_stride % 4 == 0;
-  const int lines = a.box_lines ? S::PARTS : 1;
-  const bool boxes = a.c.page_size % 8 == 0 && box_map(a.c, a.c.k, S::LINE, lines, box_rows, &maps[0]) &&
-                     box_map(a.c, a.c.v, S::LINE, lines, box_rows, &maps[1]);
-  constexpr auto rowwise = mma_kernel<C, DP, NG, false, Q32>, boxed = mma_kernel<C, DP, NG, true, Q32>;
-  static const cudaError_t e[2] = {
-      cudaFuncSetAttribute(rowwise, cudaFuncAttributeMaxDynamicSharedMemorySize, S::kShared),
-      cudaFuncSetAttribute(boxed, cudaFuncAttributeMaxDynamicSharedMemorySize, S::kShared)};
-  if (e[boxes] != cudaSuccess) return cuda_fail(e[boxes], "cudaFuncSetAttribute");
-  return launch("gar_decode_attention", boxes ? boxed : rowwise, sms, 32 * S::kWarps, S::kShared, stream, a, maps[0],
-                maps[1]);
+  const auto run = [&](auto boxes) {
+    constexpr auto kernel = mma_kernel<C, DP, NG, decltype(boxes)::value, Q32>;
+    static const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, S::kShared);
+    if (e != cudaSuccess) return cuda_fail(e, "cudaFuncSetAttribute");
+    return launch("gar_decode_attention", kernel, sms, 32 * S::kWarps, S::kShared, stream, a, maps[0], maps[1]);
+  };
+  if constexpr (S::kBoxes)
+    if (a.c.dim == DP && a.c.page_size % S::KT == 0 && box_map(a.c, a.c.k, S::KT, &maps[0]) &&
+        box_map(a.c, a.c.v, S::KT, &maps[1]))
+      return run(std::true_type{});
+  return run(std::false_type{});
 }
 
 template <typename C, bool Q32> int decode_mma(const DecodeArgs &a, int sms, gar_stream_t stream) {
