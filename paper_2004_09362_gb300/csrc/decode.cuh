@@ -5,11 +5,13 @@
 // that read it.  The CTAs share the items' rows in one of two ways.
 //  * A segment each: every item is cut into parts of as many rows, the fewest (a multiple of 64) for which
 //    there are no more parts than CTAs.  Taken for up to 32 sequences where a part is at most 5/4 of an equal
-//    share, or 192 KB more: a second segment to start, and to join, takes a CTA as long as those.
+//    share, or 192 KB more: a second segment to start, and to join, takes a CTA as long as those.  (24 sequences, a
+//    window of 1000 rows, 20/4 heads x 64 channels i8: 15 us so, 19.5 in a line.)
 //  * A line: the items' rows, in units of 64 (more where the line would pass 2^30 units), stand one
 //    behind the other, and CTA i of N takes the i-th of N equal shares.  So every CTA has the same number
 //    of rows to read whatever the lengths are, and thousands of short sequences are not split at all.  Each item
-//    counts 192 KB of rows more, for what a segment costs beside its rows, or the items' mean where that is less.
+//    counts 192 KB of rows more, for what a segment costs beside its rows, or the items' mean where that is less.  (127 sequences of up to 8192 rows, 32/8 x 128
+//    channels e4m3: 203 us; with 96 KB 208, with 64 rows 222.)
 // The lengths are read on the device: nothing waits for the host, and a captured launch stays
 // right when they change.
 //

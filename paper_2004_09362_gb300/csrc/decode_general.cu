@@ -13,8 +13,11 @@ constexpr int kWarps = 4, kThreads = 32 * kWarps;
 // A warp takes kRows rows at a time; its lanes hold every 32nd channel (J each) of the rows, the
 // queries and the outputs.  The 4 x 8 products of rows and heads are summed over the lanes by an
 // exchange that halves the values with each step, so that 31 shuffles do them all and lane
-// 8 r + h is left with the score of row r and head h.  Bound by memory for a few heads a cached
-// head; the rows' loads (8 J of 128 bytes a warp) are in flight together.
+// 8 r + h is left with the score of row r and head h.  Bound by arithmetic and by latency; the
+// rows' loads (8 J of 128 bytes a warp) are in flight together.
+//
+// 16 sequences of up to 8192 rows, 32/8 heads x 100 channels bf16: 372 us (0.5 TB/s); the tensor cores'
+// kernel needs 43 us for 96 channels, this one 378.  7 sequences of up to 2000 rows, 6/6 x 80 f32: 21 us, that one 18.
 template <typename T, int J> __global__ void __launch_bounds__(kThreads) general_kernel(const DecodeArgs a) {
   __shared__ JoinShared<kWarps> join;
   extern __shared__ __align__(16) float o_shared[];

@@ -17,11 +17,20 @@
 //    both the keys' and the values' reads meet every bank once.
 //  * A warp copies its tiles to its own part of shared memory and is the only one to read them:
 //    it waits for its own copies, never for another warp.  It keeps kStages - 1 tiles in flight, and
-//    goes on to the next segment's while the CTA still joins the last one's results.  One lane issues
-//    a tile's tensor copies; pages whose rows do not come in eights are copied by cp.async, which
-//    costs some 300 instructions a tile for the addresses.
-//  * The warps of a CTA take a segment's tiles in turn and join at its end; an item of at most
-//    kSolo tiles goes to one warp whole, so that short sequences need no barrier.
+//    goes on to the next segment's while the CTA still joins the last one's results.
+//  * Rows are copied by cp.async, a line (at most 128 bytes) at a time.  Rows of 256 channels of 2 or 4 bytes go
+//    in tensor copies, a tile's keys or values by one lane in one copy, where pages are whole tiles.  The times of
+//    tensor copies and of cp.async (sequences x most rows, query/cached heads x channels): 4 x 20000, 32/2 x 256 bf16
+//    35.7 and 38.3 us; 8 x 8192, 16/4 x 256 f32 87 and 97.  Shorter rows came no faster in tensor copies, or slower:
+//    64 x 16384, 64/4 x 128 f32 685 and 567; 127 x 8192, 32/8 x 128 e4m3 203 and 204; 24 x 1000 rows, 20/4 x 64 i8
+//    15.2 and 13.5; 1 x 262143, 64/8 x 128 bf16 156 both.
+//  * The warps of a CTA take a segment's tiles in turn and join at its end; an item of few
+//    tiles (DecodeArgs::solo) goes to one warp whole, so that short sequences need no barrier.
+//
+// Measured: 1 x 262143 rows, 64/8 x 128 bf16 156 us (6.9 TB/s, what a copy reaches); 64 x 8192, 32/8 x 128 bf16 165 us
+// (6.5 TB/s); 127 x 8192, 32/8 x 128 e4m3 204 us (5.3 TB/s: expanding codes takes its warps as long as the copies
+// do); 16 x 8192, 8/8 x 128 f32 99 us (5.0 TB/s).  1 x 425, 32/8 x 128 bf16 9 us, which is the launch, the lengths, the
+// pages, the rows, the join of a CTA and that of the item one after the other, each a round trip to memory or more.
 //
 // 8-bit codes become f16, exactly; a row's key scale multiplies its scores, its value scale
 // its weight, taken relative to the largest value scale so far (and times 2^14) so that the weights stay in
@@ -181,10 +190,11 @@ template <typename C, int DP, int NG> struct MmaShape {
   static constexpr int kLogTile = DP * EL <= 128 ? 5 : 4, KT = 1 << kLogTile;  // rows of a tile
   static constexpr int kTile = 2 * KT * DP * EL;                   // bytes, keys and values
   // One CTA per SM; its 192 KB of tiles are divided among as many warps as the registers allow, two tiles each at least.
+  // (12 warps and 8: 1 x 262143, 64/8 x 128 bf16 156 and 162 us; 127 x 8192, 32/8 x 128 e4m3 203 and 218.)
   static constexpr int kMost = 196608 / kTile / 2, kLike = NG == 1 && DP <= 128 ? 12 : 8;
   static constexpr int kWarps = kMost < kLike ? kMost : kLike;
   static constexpr int kStages = 196608 / kWarps / kTile;
-  // Whole rows of at least 512 bytes can be copied as boxes.
+  // Rows that can be copied as boxes.
   static constexpr bool kBoxes = DP == 256 && !Q8;
   static constexpr int kScales = Q8 ? 2 * KT * 4 : 0;
   // Floats of an o row; a row of o for each head fits a stage.  A few floats more than DP spread
@@ -792,6 +802,9 @@ template <typename C, int DP, int NG, bool Q32> int launch_mma(DecodeArgs a, int
   a.item_heads = std::min(a.group, 8 * NG);
   a.item_groups = (a.group + 8 * NG - 1) / (8 * NG);
   a.items = divide_by((uint32_t)(a.c.heads * a.item_groups));
+  // Tiles of an item that a warp takes whole: twice the items of a CTA, as the warps have the more time to even out.
+  // (Twice and once as many: 256 sequences of up to 256 rows, 32/8 x 128 bf16 44 and 60 us; of up to 512, i8 65 and 95,
+  // bf16 88 and 79.  64 of up to 512, 8/8 x 64 i8, 3 items a CTA: 24 with 6, 22 with 4, 30 with 12.)
   a.solo = std::min(64, std::max(4, (int)(2 * (int64_t)a.batch * a.c.heads * a.item_groups / sms)));
   CUtensorMap maps[2];
   const auto run = [&](auto boxes) {
@@ -808,6 +821,9 @@ template <typename C, int DP, int NG, bool Q32> int launch_mma(DecodeArgs a, int
 }
 
 template <typename C, bool Q32> int decode_mma(const DecodeArgs &a, int sms, gar_stream_t stream) {
+  // Sixteen heads at a time where there are more than eight (a row is read once for all; 256 channels' outputs do not fit the
+  // registers).  64 x 16384, 64/4 x 128: bf16 200 us and 316 with eight at a time, i8 174 and 220, f32 567 and 775.
+  // 1 x 60000, 16/1 x 128 bf16 is 35 and 22: more to join in one CTA.
   const bool two = a.group > 8;
   if (a.c.dim <= 64) return two ? launch_mma<C, 64, 2, Q32>(a, sms, stream) : launch_mma<C, 64, 1, Q32>(a, sms, stream);
   if (a.c.dim <= 128)
