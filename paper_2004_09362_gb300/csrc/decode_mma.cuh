@@ -28,8 +28,8 @@
 //    tiles (DecodeArgs::solo) goes to one warp whole, so that short sequences need no barrier.
 //
 // Measured: 1 x 262143 rows, 64/8 x 128 bf16 156 us (6.9 TB/s, what a copy reaches); 64 x 8192, 32/8 x 128 bf16 165 us
-// (6.5 TB/s); 127 x 8192, 32/8 x 128 e4m3 204 us (5.3 TB/s: expanding codes takes its warps as long as the copies
-// do); 16 x 8192, 8/8 x 128 f32 99 us (5.0 TB/s).  1 x 425, 32/8 x 128 bf16 9 us, which is the launch, the lengths, the
+// (6.5 TB/s); 127 x 8192, 32/8 x 128 e4m3 204 us (5.3 TB/s: its
+// warps wait for their own instructions, the expansion of the codes among them, as long as for copies); 16 x 8192, 8/8 x 128 f32 99 us (5.0 TB/s).  1 x 425, 32/8 x 128 bf16 9 us, which is the launch, the lengths, the
 // pages, the rows, the join of a CTA and that of the item one after the other, each a round trip to memory or more.
 //
 // 8-bit codes become f16, exactly; a row's key scale multiplies its scores, its value scale
