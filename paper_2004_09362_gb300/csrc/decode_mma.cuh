@@ -178,15 +178,16 @@ template <> struct words<8> {
 
 constexpr float kWeightUnit = 16384.f;  // what the largest weight over an 8-bit cache is in f16
 
-// DP: the head's channels rounded up to 64, 128 or 256; NG: groups of 8 query heads.  (The queries' type has no part
+// DP: the head's channels rounded up to 64, 96 (no 8-bit), 128, 192 or 256; NG: groups of 8 query heads.  (The queries' type has no part
 // in it.)
 template <typename C, int DP, int NG> struct MmaShape {
   static constexpr int EL = sizeof(C);
   static constexpr bool Q8 = quantised<C>::value;
   static constexpr int KC = DP * EL / 64;                          // 16-byte chunks of a key row in a lane
-  static constexpr int VB = DP * EL / 8 < 16 ? DP * EL / 8 : 16;   // bytes of a value chunk
-  static constexpr int LINE = DP * EL < 128 ? DP * EL : 128;       // bytes of a row that lie together
+  static constexpr int LINE = DP * EL % 128 ? 64 : 128;            // bytes of a row that lie together
+  static constexpr int VB = LINE / 8;                              // bytes of a value chunk
   static constexpr int PARTS = DP * EL / LINE;
+  static_assert(PARTS * LINE == DP * EL, "whole lines");
   static constexpr int kLogTile = DP * EL <= 128 ? 5 : 4, KT = 1 << kLogTile;  // rows of a tile
   static constexpr int kTile = 2 * KT * DP * EL;                   // bytes, keys and values
   // One CTA per SM; its 192 KB of tiles are divided among as many warps as the registers allow, two tiles each at least.
@@ -825,10 +826,16 @@ template <typename C, bool Q32> int decode_mma(const DecodeArgs &a, int sms, gar
   // registers).  64 x 16384, 64/4 x 128: bf16 200 us and 316 with eight at a time, i8 174 and 220, f32 567 and 775.
   // 1 x 60000, 16/1 x 128 bf16 is 35 and 22: more to join in one CTA.
   const bool two = a.group > 8;
+  // The channels that a tile is made for: a size more costs the copies' zeros, the products and the room of the tiles.  96
+  // and 192 were worth (16 x 8192, 16/4 heads, in place of 128 and 256): 80 f32 42 us, 57; 96 bf16 25 and 26; 192 f32 92 and
+  // 169, bf16 42 and 45, i8 37 and 42.  (96 channels of 8 bits are no whole lines of 64 bytes.)
   if (a.c.dim <= 64) return two ? launch_mma<C, 64, 2, Q32>(a, sms, stream) : launch_mma<C, 64, 1, Q32>(a, sms, stream);
+  if constexpr (sizeof(C) > 1)
+    if (a.c.dim <= 96)
+      return two ? launch_mma<C, 96, 2, Q32>(a, sms, stream) : launch_mma<C, 96, 1, Q32>(a, sms, stream);
   if (a.c.dim <= 128)
     return two ? launch_mma<C, 128, 2, Q32>(a, sms, stream) : launch_mma<C, 128, 1, Q32>(a, sms, stream);
-  return launch_mma<C, 256, 1, Q32>(a, sms, stream);
+  return a.c.dim <= 192 ? launch_mma<C, 192, 1, Q32>(a, sms, stream) : launch_mma<C, 256, 1, Q32>(a, sms, stream);
 }
 
 }  // namespace gar

@@ -701,6 +701,18 @@ def test_attention_both_ways_of_sharing(batch, window):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("kind,dtype", [("bf16", "bf16"), ("f16", "f16"), ("f32", "f32"), ("i8", "f32"), ("e4m3", "bf16")])
+@pytest.mark.parametrize("dim,q_heads", [(48, 2), (72, 5), (96, 12), (112, 3), (144, 4), (176, 11), (192, 1), (208, 9)])
+def test_attention_head_sizes(kind, dtype, dim, q_heads):
+    """On both sides of the sizes that the tiles are made for, groups of one row of heads and of two."""
+    lengths = [300, 0, 33, 1, 5000]
+    cache, table, lens, q, kvs = _attn_case(lengths, q_heads, 1, dim, 16, kind, dtype)
+    plan = gar.gar_attn_plan_create(q_heads, 1, dim)
+    out, lse = gar.gar_decode_attention(plan, q, cache, table, lens, lse=True)
+    _check_attn(out, lse, q, kvs, lengths, 0, dim ** -0.5, dtype)
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("kind,dtype,dim", [("bf16", "bf16", 64), ("e4m3", "f16", 128), ("f32", "f32", 48), ("f16", "f16", 33)])
 def test_attention_of_few_heads_over_ragged_sequences(kind, dtype, dim):
     """Shares of the rows that are smaller than what an item counts beside them, so that some hold no row of theirs."""
