@@ -89,11 +89,6 @@ template <> struct quantised<e4m3> {
   static constexpr float largest = 448.f;
 };
 
-// N elements of T as one aligned access.
-template <typename T, int N> struct alignas(sizeof(T) * N) pack {
-  T e[N];
-};
-
 // 16 bytes of T as they lie in memory, and their values.  Held packed so that many can be in flight.
 template <typename T> struct chunk16 {
   static constexpr int N = 16 / sizeof(T);
