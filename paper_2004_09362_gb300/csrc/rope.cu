@@ -246,9 +246,9 @@ int gar_rope(const void *x, int64_t x_token_stride, int64_t x_head_stride, void 
   // The widest vector (16 bytes, else one element) that every address, half and remainder is a multiple of.
   const int v = 16 / size;
   const auto fits = [&](int64_t n) { return n % v == 0; };
-  const bool wide = (uintptr_t)x % 16 == 0 && (uintptr_t)table % 16 == 0 && (uintptr_t)out % 16 == 0 && fits(x_token_stride) && fits(x_head_stride) &&
-                    fits(out_token_stride) && fits(out_head_stride) && fits(dim) &&
-                    fits(layout == GAR_ROPE_HALF ? rot / 2 : rot);
+  const bool wide = (uintptr_t)x % 16 == 0 && (uintptr_t)table % 16 == 0 && (uintptr_t)out % 16 == 0 &&
+                    fits(x_token_stride) && fits(x_head_stride) && fits(out_token_stride) && fits(out_head_stride) &&
+                    fits(dim) && fits(layout == GAR_ROPE_HALF ? rot / 2 : rot);
   return with_float(dtype, [&](auto tag) {
     using T = typename decltype(tag)::type;
     return launch_rope<T>(a, layout, in_place, wide, stream);
