@@ -35,7 +35,7 @@
 // 8-bit codes become f16, exactly; a row's key scale multiplies its scores, its value scale
 // its weight, taken relative to the largest value scale so far (and times 2^14) so that the weights stay in
 // f16's range.  Weights are split into a high and a low 16-bit part, one product each; so are 32-bit queries of
-// an 8-bit cache.
+// an 8-bit cache.  Weights over an f16 cache are multiplied by 2^14 too.
 //
 // The tensor cores cut their sums off rather than round them: in long sums that is a bias (4e-5 relative after
 // 100000 rows).  So they sum no more than the products of one tile; those sums are added up, and rescaled
@@ -176,7 +176,9 @@ template <> struct words<8> {
   using type = uint2;
 };
 
-constexpr float kWeightUnit = 16384.f;  // what the largest weight over an 8-bit cache is in f16
+// What the largest weight is in f16 parts: their smallest step, 2^-24, is 2^-38 of it.  (With 1 the weights under 2^-25 of the
+// largest vanish: 16384 rows of 2^-22 beside one whose value is zero came out 8 % short.)
+constexpr float kWeightUnit = 16384.f;
 
 // DP: the head's channels rounded up to 64, 96 (no 8-bit), 128, 192 or 256; NG: groups of 8 query heads.  (The queries' type has no part
 // in it.)
@@ -224,7 +226,7 @@ __global__ void __launch_bounds__(32 * MmaShape<C, DP, NG>::kWarps, 1)
   using T = typename operand<C>::type;
   constexpr int EL = S::EL, KC = S::KC, VB = S::VB, LINE = S::LINE, PARTS = S::PARTS, KT = S::KT, SUBS = KT / 16;
   constexpr int W = S::kWarps;
-  constexpr bool Q8 = S::Q8, F32 = std::is_same<C, float>::value;
+  constexpr bool Q8 = S::Q8, F32 = std::is_same<C, float>::value, F16 = std::is_same<C, __half>::value;
   constexpr int MT = DP / 16;          // tiles of 16 channels of the output
   constexpr int QW = Q32 ? DP / 4 : DP / 8;  // words of a head's queries in a lane
   extern __shared__ char shared_from[];
@@ -648,7 +650,7 @@ __global__ void __launch_bounds__(32 * MmaShape<C, DP, NG>::kWarps, 1)
       for (int sub = 0; sub < SUBS; ++sub)
 #pragma unroll
         for (int r = 0; r < 2; ++r) {
-          const float f = Q8 ? v_scale[sub * 16 + key_row<LINE>(g) + 8 * r] * v_inverse : 1.f;
+          const float f = Q8 ? v_scale[sub * 16 + key_row<LINE>(g) + 8 * r] * v_inverse : F16 ? kWeightUnit : 1.f;
 #pragma unroll
           for (int ng = 0; ng < NG; ++ng) {
             float p[2];
@@ -656,7 +658,7 @@ __global__ void __launch_bounds__(32 * MmaShape<C, DP, NG>::kWarps, 1)
             for (int h = 0; h < 2; ++h) {
               p[h] = exp2_fast(s[sub][ng][2 * r + h] - offset_of(m[ng][h]));
               l[ng][h] += p[h];
-              if (Q8) p[h] *= f;
+              if (Q8 || F16) p[h] *= f;
             }
             if constexpr (F32) {
               // Row t (i = 0) or t + 4 of these 8 rows and head g, for this lane: the lane that has them is known.
@@ -737,6 +739,7 @@ __global__ void __launch_bounds__(32 * MmaShape<C, DP, NG>::kWarps, 1)
 #pragma unroll
         for (int d = 4; d < 32; d *= 2) l[ng][h] += __shfl_xor_sync(~0u, l[ng][h], d);
     constexpr int CE = VB / EL;  // channels of a chunk, two of them in a tile of 16
+    const float v_unit = Q8 ? v_ref / kWeightUnit : F16 ? 1.f / kWeightUnit : 1.f;
     const Segment ended = segment_in_use();
     const Group by = group_in_use();
     if (by.count == 1 && ended.whole && a.out_wide) {
@@ -748,7 +751,7 @@ __global__ void __launch_bounds__(32 * MmaShape<C, DP, NG>::kWarps, 1)
           const int head = 8 * ng + 2 * t + h;
           if (head >= ended.heads) continue;
           if (g == 0) store_lse(a, ended, head, m[ng][h], l[ng][h]);
-          const float f = l[ng][h] == 0.f ? 0.f : (Q8 ? v_ref / kWeightUnit : 1.f) / l[ng][h];
+          const float f = l[ng][h] == 0.f ? 0.f : v_unit / l[ng][h];
 #pragma unroll
           for (int i = 0; i < MT; i += 2) {
             const int k = i / (CE / 2), d = (g + 8 * k) * CE + i % (CE / 2) * 2;
@@ -763,7 +766,6 @@ __global__ void __launch_bounds__(32 * MmaShape<C, DP, NG>::kWarps, 1)
       continue;
     }
     // The stage read last holds this warp's o until it is joined.
-    const float v_unit = v_ref / kWeightUnit;
     float *const o_mine = reinterpret_cast<float *>(mine + (out == 0 ? S::kStages - 1 : out - 1) * S::kTile);
     __syncwarp();
 #pragma unroll
@@ -778,7 +780,7 @@ __global__ void __launch_bounds__(32 * MmaShape<C, DP, NG>::kWarps, 1)
           // Two neighbouring channels, at a place that depends on the head so that the lanes meet all banks.
           const int k = i / (CE / 2), d = ((g + 8 * k) * CE + i % (CE / 2) * 2) ^ (head & 6);
           *reinterpret_cast<float2 *>(row + d) =
-              Q8 ? make_float2(o[i][ng][h] * v_unit, o[i][ng][2 + h] * v_unit) : make_float2(o[i][ng][h], o[i][ng][2 + h]);
+              Q8 || F16 ? make_float2(o[i][ng][h] * v_unit, o[i][ng][2 + h] * v_unit) : make_float2(o[i][ng][h], o[i][ng][2 + h]);
         }
       }
     // (copies into this stage come after the join's barrier)
