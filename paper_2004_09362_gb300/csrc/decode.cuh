@@ -16,7 +16,8 @@
 // right when they change.
 //
 // Join.  A segment is the part of an item that one CTA takes.  Each keeps the running maximum m
-// of the scores (in units of log 2), l = sum 2^(score - m) and o = sum 2^(score - m) v.  Where an
+// of the scores (in units of log 2; over 8-bit caches another number that o and l are relative to),
+// l = sum 2^(score - m) and o = sum 2^(score - m) v.  Where an
 // item has several segments, each CTA stores (m, l, o), and the one that arrives last at the
 // item's counter adds them up in the order of the rows (so the bits do not depend on who
 // was last):  m = max m_i,  l = sum l_i 2^(m_i - m),  o likewise.

@@ -33,8 +33,9 @@
 // pages, the rows, the join of a CTA and that of the item one after the other, each a round trip to memory or more.
 //
 // 8-bit codes become f16, exactly; a row's key scale multiplies its scores, its value scale
-// its weight, taken relative to the largest value scale so far (and times 2^14) so that the weights stay in
-// f16's range.  Weights are split into a high and a low 16-bit part, one product each; so are 32-bit queries of
+// its weight.  That product has to stay in f16's range, so a head's running maximum m is that of score + log2 of the value
+// scale, and o and l are relative to it: the products are at most 1, and 2^14 once split.  A row of little
+// weight takes no bits from the others, however large its scale.  Weights are split into a high and a low 16-bit part, one product each; so are 32-bit queries of
 // an 8-bit cache.  Weights over an f16 cache are multiplied by 2^14 too.
 //
 // The tensor cores cut their sums off rather than round them: in long sums that is a bias (4e-5 relative after
@@ -206,6 +207,14 @@ template <typename C, int DP, int NG> struct MmaShape {
   static_assert(8 * NG * kRow * 4 <= kTile, "o must fit a stage");
   static constexpr int kShared = kWarps * kStages * (kTile + kScales) + 1024;  // from a multiple of 1024 on
 };
+
+// log2 of a value scale, near enough for a reference.  Within [-96, 120], whatever the scale (zero, an infinity, NaN), so that the
+// sum l of 2^(score - m) stays finite and does not vanish.
+__device__ __forceinline__ float scale_log2(float x) {
+  float y;
+  asm("lg2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(fabsf(x)));
+  return fminf(fmaxf(y, -96.f), 120.f);
+}
 
 // The row of the cache, of 8, that is row i of the scores.
 template <int LINE> __device__ __forceinline__ int key_row(int i) {
@@ -498,7 +507,6 @@ __global__ void __launch_bounds__(32 * MmaShape<C, DP, NG>::kWarps, 1)
 
     float o[MT][NG][4] = {};
     float m[NG][2], l[NG][2] = {};
-    float v_ref = 1e-30f;  // Q8: the value scale that o is relative to
 #pragma unroll
     for (int ng = 0; ng < NG; ++ng) m[ng][0] = m[ng][1] = -INFINITY;
 
@@ -608,14 +616,14 @@ __global__ void __launch_bounds__(32 * MmaShape<C, DP, NG>::kWarps, 1)
         for (int r = 0; r < 2; ++r) {
           const int row = sub * 16 + key_row<LINE>(g) + 8 * r, n = n0 + row;
           const bool seen = !ragged || (n >= lo && n < to);
-          const float f = Q8 ? k_scale[row] : 1.f;
+          const float f = Q8 ? k_scale[row] : 1.f, f_log2 = Q8 ? scale_log2(v_scale[row]) : 0.f;
 #pragma unroll
           for (int ng = 0; ng < NG; ++ng)
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
               float &x = s[sub][ng][2 * r + h];
               x = seen ? x * (Q8 ? f * q_scale[ng][h] : q_scale[ng][h]) : -INFINITY;
-              top[ng][h] = fmaxf(top[ng][h], x);
+              top[ng][h] = fmaxf(top[ng][h], Q8 ? x + f_log2 : x);
             }
         }
       bool grown = false;
@@ -628,12 +636,6 @@ __global__ void __launch_bounds__(32 * MmaShape<C, DP, NG>::kWarps, 1)
           grown |= top[ng][h] > m[ng][h];
         }
       grown = __any_sync(~0u, grown);
-      float v_inverse = 1.f, v_shrink = 1.f;
-      if (Q8) {
-        const float most = __uint_as_float(__reduce_max_sync(~0u, __float_as_uint(v_scale[lane & (KT - 1)]) & 0x7fffffffu));
-        if (most > v_ref) v_shrink = v_ref / most, v_ref = most;
-        v_inverse = kWeightUnit / v_ref;
-      }
       float shrink[NG][2];
 #pragma unroll
       for (int ng = 0; ng < NG; ++ng)
@@ -642,7 +644,6 @@ __global__ void __launch_bounds__(32 * MmaShape<C, DP, NG>::kWarps, 1)
           shrink[ng][h] = grown ? exp2_fast(m[ng][h] - offset_of(top[ng][h])) : 1.f;
           m[ng][h] = top[ng][h];
           l[ng][h] *= shrink[ng][h];
-          if (Q8) shrink[ng][h] *= v_shrink;
         }
       // Weights, in the layout of the second product's right operand.
       uint32_t hi[SUBS][NG][F32 ? 4 : 2], low[SUBS][NG][F32 ? 4 : 2];
@@ -650,7 +651,7 @@ __global__ void __launch_bounds__(32 * MmaShape<C, DP, NG>::kWarps, 1)
       for (int sub = 0; sub < SUBS; ++sub)
 #pragma unroll
         for (int r = 0; r < 2; ++r) {
-          const float f = Q8 ? v_scale[sub * 16 + key_row<LINE>(g) + 8 * r] * v_inverse : F16 ? kWeightUnit : 1.f;
+          const float f = Q8 ? v_scale[sub * 16 + key_row<LINE>(g) + 8 * r] : 1.f;
 #pragma unroll
           for (int ng = 0; ng < NG; ++ng) {
             float p[2];
@@ -658,7 +659,8 @@ __global__ void __launch_bounds__(32 * MmaShape<C, DP, NG>::kWarps, 1)
             for (int h = 0; h < 2; ++h) {
               p[h] = exp2_fast(s[sub][ng][2 * r + h] - offset_of(m[ng][h]));
               l[ng][h] += p[h];
-              if (Q8 || F16) p[h] *= f;
+              if (Q8) p[h] *= f;
+              if (Q8 || F16) p[h] *= kWeightUnit;
             }
             if constexpr (F32) {
               // Row t (i = 0) or t + 4 of these 8 rows and head g, for this lane: the lane that has them is known.
@@ -739,7 +741,7 @@ __global__ void __launch_bounds__(32 * MmaShape<C, DP, NG>::kWarps, 1)
 #pragma unroll
         for (int d = 4; d < 32; d *= 2) l[ng][h] += __shfl_xor_sync(~0u, l[ng][h], d);
     constexpr int CE = VB / EL;  // channels of a chunk, two of them in a tile of 16
-    const float v_unit = Q8 ? v_ref / kWeightUnit : F16 ? 1.f / kWeightUnit : 1.f;
+    constexpr float v_unit = Q8 || F16 ? 1.f / kWeightUnit : 1.f;
     const Segment ended = segment_in_use();
     const Group by = group_in_use();
     if (by.count == 1 && ended.whole && a.out_wide) {

@@ -49,3 +49,81 @@ def test_small_weights_of_f16_values(dim, heads, page, n, t):
     e = 4 * U32 * float(y.abs().max())
     tol = (2 * e + 2.0 ** -21 + 2 * n * U32) * want + n * 2.0 ** -39 * float(p.max()) * rows.amax(0)
     assert bool(((out[0].double() - want).abs() <= tol).all())
+
+
+def _cached(kind, k_codes, k_scale, v_codes, v_scale, page):
+    """A cache of one head that holds rows of given codes and scales, and those rows in 64 bits."""
+    n, dim = k_codes.shape
+    pages = -(-n // page)
+    rows = []
+    tensors = []
+    for codes, scale in ((k_codes, k_scale), (v_codes, v_scale)):
+        t = torch.zeros(pages * page, dim, dtype=torch.int8, device="cuda").view(kind)
+        t.view(torch.uint8)[:n] = codes.to(kind).view(torch.uint8)
+        s = torch.zeros(pages * page, device="cuda")
+        s[:n] = scale
+        tensors += [t.view(pages, 1, page, dim), s.view(pages, 1, page)]
+        rows.append(codes.to(kind).double() * s[:n].double()[:, None])
+    cache = gar.KVCache(tensors[0], tensors[2], tensors[1], tensors[3])
+    return cache, torch.arange(pages, dtype=torch.int32, device="cuda")[None], rows[0], rows[1]
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("kind", [torch.int8, torch.float8_e4m3fn])
+@pytest.mark.parametrize("dim,heads,dtype", [(64, 1, torch.float32), (128, 12, torch.bfloat16), (256, 4, torch.float16), (192, 8, torch.float32)])
+@pytest.mark.parametrize("n", [20, 300, 5000])
+@pytest.mark.parametrize("small", [1e-6, 1e-9, 1e-11, 1e-20])
+def test_value_scales_of_rows_without_weight(kind, dim, heads, dtype, n, small):
+    """The rows that have the weight have value scales a million times smaller, and less, than those that have none.  (All
+    the others' weights together, 2^-126 of a row's, times the quotient of the scales is below 2^-50.)"""
+    g = _gen(n)
+    heavy = torch.zeros(n, dtype=torch.bool, device="cuda")
+    heavy[n // 2], heavy[n - 1] = True, True
+    codes = [torch.randint(-120, 121, (n, dim), generator=g, device="cuda").float() for _ in range(2)]
+    codes[0][:, 0] = torch.where(heavy, 100.0, -100.0)
+    codes[0][:, 1:] = 0
+    k_scale = torch.full((n,), 0.01, device="cuda")
+    v_scale = torch.where(heavy, small, 1.0) * (torch.rand(n, generator=g, device="cuda") + 0.5)
+    cache, table, k, v = _cached(kind, codes[0], k_scale, codes[1], v_scale, 16)
+    q = torch.zeros(1, heads, dim, dtype=dtype, device="cuda")
+    q[..., 0] = 1
+    out, lse = torch.empty(1, heads, dim, device="cuda"), torch.empty(1, heads, device="cuda")
+    lens = torch.tensor([n], dtype=torch.int32, device="cuda")
+    plan = gar.gar_attn_plan_create(heads, 1, dim)
+    scale = 64.0                            # scores of about +-64: the light rows weigh e^-128
+    gar.gar_decode_attention(plan, q, cache, table, lens, scale=scale, out=out, lse=lse)
+    y = k[:, 0] * scale
+    p = torch.softmax(y, 0)
+    want, size = p @ v, p @ v.abs()
+    # a score: two scales and the constant rounded, their products, the difference to the reference (|log2 scale| <= 67 of it)
+    e = 6 * U32 * float(y.abs().max() + 67)
+    tol = (2 * e + 2.0 ** -21 + 2 * n * U32) * size + n * 2.0 ** -39 * float((p * v_scale).max()) * 128
+    assert bool(((out[0].double() - want).abs() <= tol).all())
+    assert bool(((lse[0].double() - torch.logsumexp(y, 0)).abs() <= e + 2.0 ** -21 + n * U32 + 2.0 ** -22 * float(y.abs().max())).all())
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("kind", [torch.int8, torch.float8_e4m3fn])
+def test_value_scales_at_the_ends_of_their_range(kind):
+    """Scales of zero, subnormal, next to the largest; an infinite or NaN scale gives no number rather than a finite one."""
+    dim, n = 64, 48
+    g = _gen(5)
+    codes = [torch.randint(-120, 121, (n, dim), generator=g, device="cuda").float() for _ in range(2)]
+    q = torch.full((1, 1, dim), 0.01, device="cuda")
+    lens = torch.tensor([n], dtype=torch.int32, device="cuda")
+    plan = gar.gar_attn_plan_create(1, 1, dim)
+    for low, high in ((0.0, 0.0), (0.0, 1.0), (1e-42, 1e-42), (1e-28, 1e-28), (1e-30, 1e30), (1e36, 1e36), (1e-3, float("inf")), (1e-3, float("nan"))):
+        v_scale = torch.full((n,), low, device="cuda")
+        v_scale[n // 2] = high
+        cache, table, k, v = _cached(kind, codes[0], torch.full((n,), 0.01, device="cuda"), codes[1], v_scale, 16)
+        out, lse = gar.gar_decode_attention(plan, q, cache, table, lens, lse=True)
+        y = (k @ q[0, 0].double()) / 8
+        p = torch.softmax(y, 0)
+        assert bool((lse[0].double() - torch.logsumexp(y, 0)).abs() <= 1e-4), (low, high)     # unharmed by the values
+        if not math.isfinite(high):
+            assert not bool(out.isfinite().any())
+            continue
+        size = p @ v.abs()
+        # the largest product of weight and scale counts as 2^-96 at least
+        tol = 2.0 ** -16 * size + n * 2.0 ** -39 * max(float((p * v_scale).max()), 2.0 ** -96) * 128
+        assert bool(((out[0, 0].double() - p @ v).abs() <= tol).all()), (low, high)
