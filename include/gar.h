@@ -504,7 +504,8 @@ GAR_API int gar_attn_plan_set_workspace(gar_attn_plan *plan, void *dev_ptr, size
  * rounding of out; weights enter the products as two parts (of 16 bits: about 2^-17 relative,
  * over an f16 cache 2^-22 of the weight or 2^-39 of the largest, whichever is more; over an
  * 8-bit one the same of the products of weights and value scales, the largest counted as 2^-96 at least;
- * over a 32-bit cache 2^-21, keys and values too).  An infinity among attended values may come
+ * over a 32-bit cache 2^-21, keys and values too).  Over an 8-bit cache a channel of a bf16 or 32-bit
+ * query is off by 2^-22 of itself or 2^-39 of the head's largest, whichever is more.  An infinity among attended values may come
  * out as a NaN.  Results do not depend on timing: partial results
  * are joined in the order of the rows. */
 GAR_API int gar_decode_attention(gar_attn_plan *plan, const gar_kv_cache *cache, const void *q,

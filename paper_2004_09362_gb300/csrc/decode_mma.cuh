@@ -473,7 +473,9 @@ __global__ void __launch_bounds__(32 * MmaShape<C, DP, NG>::kWarps, 1)
     float q_scale[NG][2];
 #pragma unroll
     for (int ng = 0; ng < NG; ++ng) {
-      // Over an 8-bit cache bf16 and 32-bit queries become f16 relative to the power of two at their largest.
+      // Over an 8-bit cache bf16 and 32-bit queries become f16, the head's largest brought to [2^14, 2^15): the smallest
+      // step of f16 is then 2^-38 of it.  (Brought to [1, 2) that was 2^-24: a channel of 2^-20 beside one that the keys have as
+      // zero kept 4 bits.)
       float up = 1.f;
       if (Q8 && (Q32 || a.q_dtype == GAR_BF16)) {
         uint32_t most = 0;
@@ -483,9 +485,9 @@ __global__ void __launch_bounds__(32 * MmaShape<C, DP, NG>::kWarps, 1)
                      : max(most, max((qf[ng][i] & 0x7fffu) << 16, qf[ng][i] & 0x7fff0000u));
         most = max(most, __shfl_xor_sync(~0u, most, 1));
         most = max(most, __shfl_xor_sync(~0u, most, 2));
-        const int e = most >> 23;
-        float down = 1.f;
-        if (e > 0 && e < 0xfe) up = __int_as_float(e << 23), down = __int_as_float((254 - e) << 23);
+        const int e = min(max((int)(most >> 23), 15), 254);  // (of an infinity or a NaN as of the largest number)
+        up = __int_as_float((e - 14) << 23);
+        const float down = __int_as_float((268 - e) << 23);
         if constexpr (Q32) {
           uint32_t hi[QW / 2], low[QW / 2];
 #pragma unroll

@@ -127,3 +127,40 @@ def test_value_scales_at_the_ends_of_their_range(kind):
         # the largest product of weight and scale counts as 2^-96 at least
         tol = 2.0 ** -16 * size + n * 2.0 ** -39 * max(float((p * v_scale).max()), 2.0 ** -96) * 128
         assert bool(((out[0, 0].double() - p @ v).abs() <= tol).all()), (low, high)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("kind", [torch.int8, torch.float8_e4m3fn])
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32, torch.float16])
+@pytest.mark.parametrize("dim,heads", [(64, 1), (128, 12), (192, 4), (256, 8)])
+@pytest.mark.parametrize("large", [2.0 ** 10, 2.0 ** 18, 2.0 ** 24, 2.0 ** 100])
+def test_queries_with_one_large_channel_over_8_bits(kind, dtype, dim, heads, large):
+    """One channel of the query is much larger than the others, and the keys have it as zero: the scores are those of
+    the others.  (Over bf16 and 32-bit queries alike; f16 ones hold 65504 at most.)"""
+    if dtype == torch.float16:
+        large = min(large, 2.0 ** 15)
+    n = 200
+    g = _gen(dim)
+    codes = [torch.randint(-120, 121, (n, dim), generator=g, device="cuda").float() for _ in range(2)]
+    codes[0][:, 5] = 0
+    ones = torch.ones(n, device="cuda")
+    cache, table, k, v = _cached(kind, codes[0], 0.01 * ones, codes[1], 0.01 * ones, 16)
+    q = torch.randn(1, heads, dim, generator=g, device="cuda").to(dtype)
+    q[..., 5] = large
+    for tiny in (1.0, 2.0 ** -120) if dtype != torch.float16 else (1.0,):    # queries whose channels are next to subnormal too
+        x = q if tiny == 1.0 else (q.double() * tiny).to(dtype)
+        scale = 0.125 if tiny == 1.0 else 0.125 * 2.0 ** 100
+        plan = gar.gar_attn_plan_create(heads, 1, dim)
+        out, lse = torch.empty(1, heads, dim, device="cuda"), torch.empty(1, heads, device="cuda")
+        gar.gar_decode_attention(plan, x, cache, table, torch.tensor([n], dtype=torch.int32, device="cuda"), scale=scale, out=out, lse=lse)
+        x = x[0].double()
+        y, size = x @ k.T * scale, x.abs() @ k.abs().T * scale
+        # a sum of dim products, two scales and a constant, the difference to the reference; the query's own parts
+        # (channels under 2^-126 of 32 bits are taken as zero where they are subnormal: none is here for 1, and for tiny
+        # ones they are within the same 2^-39 of the largest)
+        parts = scale * x.abs().amax(-1, keepdim=True) * 2.0 ** -39 * k.abs().sum(-1)
+        e = ((dim + 6) * U32 * size + 2.0 ** -22 * size + parts).amax(-1) + 8 * U32
+        assert bool(((lse[0].double() - torch.logsumexp(y, -1)).abs() <= e + 2.0 ** -21 + n * U32 + 2.0 ** -22 * y.abs().amax(-1)).all()), tiny
+        p = torch.softmax(y, -1)
+        tol = (2 * e[:, None] + 2.0 ** -21 + 2 * n * U32) * (p @ v.abs()) + n * 2.0 ** -39 * 128 * 0.01
+        assert bool(((out[0].double() - p @ v).abs() <= tol).all()), tiny
