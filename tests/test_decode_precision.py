@@ -164,3 +164,28 @@ def test_queries_with_one_large_channel_over_8_bits(kind, dtype, dim, heads, lar
         p = torch.softmax(y, -1)
         tol = (2 * e[:, None] + 2.0 ** -21 + 2 * n * U32) * (p @ v.abs()) + n * 2.0 ** -39 * 128 * 0.01
         assert bool(((out[0].double() - p @ v).abs() <= tol).all()), tiny
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dim,heads", [(4, 1), (8, 9), (16, 2), (64, 8), (80, 12), (128, 1), (192, 5), (256, 8)])
+@pytest.mark.parametrize("n", [1, 40, 300, 5000])
+def test_products_of_32_bit_caches(dim, heads, n):
+    """What is promised of a 32-bit cache: products off by 2^-21.  Numbers as a high part of 11 bits and a low one (12 at most, of
+    which the product takes 11: 2^-23), the product of the low parts (2^-22) left out: 2 * 2^-23 + 2^-22."""
+    g = _gen(dim + n)
+    page = 16
+    pages = -(-n // page)
+    k, v = (torch.randn(pages, 1, page, dim, generator=g, device="cuda") for _ in range(2))
+    q = torch.randn(1, heads, dim, generator=g, device="cuda") / 4
+    plan = gar.gar_attn_plan_create(heads, 1, dim)
+    table = torch.arange(pages, dtype=torch.int32, device="cuda")[None]
+    out, lse = gar.gar_decode_attention(plan, q, gar.KVCache(k, v), table, torch.tensor([n], dtype=torch.int32, device="cuda"), lse=True)
+    scale = dim ** -0.5
+    x, rows, values = q[0].double(), k.view(-1, dim)[:n].double(), v.view(-1, dim)[:n].double()
+    y, size = x @ rows.T * scale, x.abs() @ rows.abs().T * scale
+    e = (((dim + 4) * U32 + 2.0 ** -21) * size).amax(-1)
+    p = torch.softmax(y, -1)
+    tol = (2 * e[:, None] + 2.0 ** -21 + 2.0 ** -21 + 2 * n * U32) * (p @ values.abs()) + U32 * (p @ values).abs()
+    assert bool(((out[0].double() - p @ values).abs() <= tol).all())
+    want = torch.logsumexp(y, -1)
+    assert bool(((lse[0].double() - want).abs() <= e + 2.0 ** -22 + n * U32 + 2.0 ** -22 * want.abs()).all())
