@@ -300,14 +300,17 @@ PyObject *decode_attention(PyObject *, PyObject *const *args, Py_ssize_t n, PyOb
     if (q.size(1) != shape[0] || q.size(2) != shape[2])
       bad("q must be [batch, " + std::to_string(shape[0]) + ", " + std::to_string(shape[2]) + "]");
     const Stream stream(a.at[9]);
-    // The workspace comes with the first call.
-    PyObject *ws = PyObject_GetAttrString(a.at[0], "workspace");
-    const bool without = ws == Py_None;
-    Py_XDECREF(ws);
-    if (!ws) throw python_error();
-    if (without) {
+    // The workspace comes with the first call; that the stream of a call uses it is known to its allocator.
+    PyObject *last = PyObject_GetAttrString(a.at[0], "stream");
+    if (!last) throw python_error();
+    const bool known = last != Py_None && PyLong_AsVoidPtr(last) == static_cast<void *>(stream.raw);
+    Py_DECREF(last);
+    if (PyErr_Occurred()) throw python_error();
+    if (!known) {
       PyObject *m = PyImport_ImportModule("paper_2004_09362_gb300.gar");
-      PyObject *r = m ? PyObject_CallMethod(m, "_ensure_attn_workspace", "OO", a.at[0], a.at[1]) : nullptr;
+      PyObject *r = m ? PyObject_CallMethod(m, "_use_workspace", "OOK", a.at[0], a.at[1],
+                                            (unsigned long long)(uintptr_t)stream.raw)
+                      : nullptr;
       Py_XDECREF(m);
       if (!r) throw python_error();
       Py_DECREF(r);

@@ -571,13 +571,16 @@ def gar_kv_status(cache: KVCache, stream=None) -> None:
 
 class AttnPlan:
     """Owns a gar_attn_plan* and the torch tensor that backs its workspace.  The workspace holds
-    one call's partial results: keep a plan's calls on one stream, or use a plan for each."""
+    one call's partial results: keep a plan's calls on one stream, or use a plan for each.  A plan may be dropped
+    while its calls are still running; a CUDA graph that holds some needs it as long as it is replayed.  A
+    stream that is given as a raw handle has to outlive the plan."""
 
     def __init__(self, handle: int, q_heads: int, kv_heads: int, dim: int):
         self._h = ctypes.c_void_p(handle)
         self.address = handle
         self.q_heads, self.kv_heads, self.dim = q_heads, kv_heads, dim
         self.workspace = None
+        self.stream = None          # handle of the last call's stream
 
     @property
     def handle(self) -> ctypes.c_void_p:
@@ -624,14 +627,21 @@ def gar_attn_plan_set_workspace(plan: AttnPlan, ptr: int, nbytes: int) -> None:
            "gar_attn_plan_set_workspace")
 
 
-def _ensure_attn_workspace(plan: AttnPlan, like) -> None:
-    """Allocates the plan's workspace next to the tensor `like` and attaches it."""
+def _use_workspace(plan: AttnPlan, like, raw: int) -> None:
+    """Before a call on the stream of handle `raw` that is not the last call's: the plan's workspace is
+    allocated next to the tensor `like`, under that stream, and attached; or its memory is kept, when
+    the plan is dropped, until that stream has done what it has been given too."""
     import torch
-    n = gar_attn_plan_bytes(plan)
-    workspace = torch.empty(n, dtype=torch.uint8, device=like.device)
-    torch.cuda.synchronize()                # what held this memory before is done
-    gar_attn_plan_set_workspace(plan, workspace.data_ptr(), n)
-    plan.workspace = workspace
+    stream = torch.cuda.ExternalStream(raw)
+    if plan.workspace is None:
+        n = gar_attn_plan_bytes(plan)
+        workspace = _empty(n, torch.uint8, like.device, stream)
+        torch.cuda.synchronize()            # what held this memory before is done
+        gar_attn_plan_set_workspace(plan, workspace.data_ptr(), n)
+        plan.workspace = workspace
+    else:
+        plan.workspace.record_stream(stream)
+    plan.stream = raw
 
 
 def __getattr__(name):

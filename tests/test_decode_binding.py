@@ -1,0 +1,75 @@
+"""The decoding operators' Python calls: memory, streams, devices, types and gradients."""
+
+import gc
+import types
+
+import pytest
+import torch
+
+from paper_2004_09362_gb300 import gar
+
+
+class _Recorded:
+    """Stands for a workspace tensor."""
+
+    def __init__(self):
+        self.streams = []
+
+    def data_ptr(self):
+        return 4096
+
+    def record_stream(self, stream):
+        self.streams.append(stream)
+
+
+def test_workspace_is_kept_for_every_stream_that_uses_it(monkeypatch):
+    """A plan's workspace is allocated under the first call's stream, and later calls' streams are recorded."""
+    under, attached = [], []
+    monkeypatch.setattr(torch.cuda, "ExternalStream", lambda raw, device=None: raw)
+    monkeypatch.setattr(torch.cuda, "synchronize", lambda *a: None)
+    made = _Recorded()
+    monkeypatch.setattr(gar, "_empty", lambda shape, dtype, device, stream: under.append(stream) or made)
+    monkeypatch.setattr(gar, "gar_attn_plan_set_workspace", lambda plan, ptr, n: attached.append((ptr, n)))
+    plan = gar.gar_attn_plan_create(4, 2, 64)
+    like = types.SimpleNamespace(device=torch.device("cpu"))
+    gar._use_workspace(plan, like, 7000)
+    assert under == [7000] and attached == [(4096, gar.gar_attn_plan_bytes(plan))] and plan.stream == 7000
+    gar._use_workspace(plan, like, 8000)
+    assert made.streams == [8000] and plan.stream == 8000 and len(under) == 1
+    gar._use_workspace(plan, like, 7000)
+    assert made.streams == [8000, 7000] and len(under) == 1
+
+
+def _problem(batch=3, q_heads=8, kv_heads=2, dim=64, length=2000, seed=0):
+    g = torch.Generator(device="cuda")
+    g.manual_seed(seed)
+    pages = -(-length // 16) * batch
+    k, v = (torch.randn(pages, kv_heads, 16, dim, generator=g, device="cuda").bfloat16() for _ in range(2))
+    table = torch.arange(pages, dtype=torch.int32, device="cuda").view(batch, -1)
+    q = torch.randn(batch, q_heads, dim, generator=g, device="cuda").bfloat16()
+    return gar.KVCache(k, v), table, torch.full((batch,), length, dtype=torch.int32, device="cuda"), q
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("first_on_side", [True, False])
+def test_plan_dropped_while_its_call_is_pending(first_on_side):
+    """The call waits on a side stream; its plan is dropped, and memory of the workspace's size is taken and written on the main one."""
+    cache, table, lens, q = _problem()
+    plan = gar.gar_attn_plan_create(8, 2, 64)
+    want = gar.gar_decode_attention(plan, q, cache, table, lens)
+    side = torch.cuda.Stream()
+    if first_on_side:
+        plan = gar.gar_attn_plan_create(8, 2, 64)
+        with torch.cuda.stream(side):           # allocates; nothing is pending yet
+            gar.gar_decode_attention(plan, q, cache, table, lens)
+    torch.cuda.synchronize()
+    n, at = plan.workspace.numel(), plan.workspace.data_ptr()
+    with torch.cuda.stream(side):
+        torch.cuda._sleep(200_000_000)          # some 0.1 s
+    got = gar.gar_decode_attention(plan, q, cache, table, lens, stream=side)
+    del plan
+    gc.collect()
+    taken = [torch.full((n,), 255, dtype=torch.uint8, device="cuda") for _ in range(3)]
+    assert all(t.data_ptr() != at for t in taken)
+    torch.cuda.synchronize()
+    assert torch.equal(got, want) and all(bool((t == 255).all()) for t in taken)
