@@ -623,8 +623,12 @@ def gar_attn_plan_bytes(plan: AttnPlan) -> int:
 
 
 def gar_attn_plan_set_workspace(plan: AttnPlan, ptr: int, nbytes: int) -> None:
+    """Attaches the caller's memory, which has to last as long as the plan's calls run; 0 detaches it.  Without,
+    the first call allocates a workspace."""
     _check(_lib.gar_attn_plan_set_workspace(plan.handle, ctypes.c_void_p(int(ptr) or None), int(nbytes)),
            "gar_attn_plan_set_workspace")
+    plan.workspace = (int(ptr), int(nbytes)) if ptr else None
+    plan.stream = None
 
 
 def _use_workspace(plan: AttnPlan, like, raw: int) -> None:
@@ -639,7 +643,7 @@ def _use_workspace(plan: AttnPlan, like, raw: int) -> None:
         torch.cuda.synchronize()            # what held this memory before is done
         gar_attn_plan_set_workspace(plan, workspace.data_ptr(), n)
         plan.workspace = workspace
-    else:
+    elif not isinstance(plan.workspace, tuple):     # (else the caller's)
         plan.workspace.record_stream(stream)
     plan.stream = raw
 

@@ -73,3 +73,35 @@ def test_plan_dropped_while_its_call_is_pending(first_on_side):
     assert all(t.data_ptr() != at for t in taken)
     torch.cuda.synchronize()
     assert torch.equal(got, want) and all(bool((t == 255).all()) for t in taken)
+
+
+def test_a_workspace_of_the_callers_own_is_used(monkeypatch):
+    monkeypatch.setattr(torch.cuda, "ExternalStream", lambda raw, device=None: raw)
+    calls = []
+    monkeypatch.setattr(gar._lib, "gar_attn_plan_set_workspace", lambda plan, ptr, n: calls.append(ptr.value) or 0)
+
+    def never(*a):
+        raise AssertionError("allocates")
+
+    monkeypatch.setattr(gar, "_empty", never)
+    plan = gar.gar_attn_plan_create(4, 2, 64)
+    gar.gar_attn_plan_set_workspace(plan, 4096, gar.gar_attn_plan_bytes(plan))
+    like = types.SimpleNamespace(device=torch.device("cpu"))
+    gar._use_workspace(plan, like, 7000)
+    gar._use_workspace(plan, like, 8000)
+    assert calls == [4096] and plan.stream == 8000
+    gar.gar_attn_plan_set_workspace(plan, 0, 0)
+    assert calls == [4096, None] and plan.workspace is None and plan.stream is None
+
+
+@pytest.mark.gpu
+def test_attention_with_the_callers_workspace():
+    cache, table, lens, q = _problem()
+    want = gar.gar_decode_attention(gar.gar_attn_plan_create(8, 2, 64), q, cache, table, lens)
+    plan = gar.gar_attn_plan_create(8, 2, 64)
+    n = gar.gar_attn_plan_bytes(plan)
+    mine = torch.full((n,), 255, dtype=torch.uint8, device="cuda")
+    torch.cuda.synchronize()
+    gar.gar_attn_plan_set_workspace(plan, mine.data_ptr(), n)
+    assert torch.equal(gar.gar_decode_attention(plan, q, cache, table, lens), want)
+    assert bool((mine != 255).any()) and plan.workspace == (mine.data_ptr(), n)
