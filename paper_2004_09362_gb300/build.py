@@ -30,7 +30,7 @@ BUILD = os.path.join(ROOT, "_build")
 SOURCES = ["api.cpp", "plan.cpp", "codegen.cpp", "jit.cpp", "step_kernels.cu", "rope.cu", "cache.cu",
            "decode_api.cu", "decode_general.cu", "decode_mma_bf16.cu", "decode_mma_f16.cu", "decode_mma_i8.cu",
            "decode_mma_e4m3.cu", "decode_mma_f32.cu", "decode_mma_i8_f32.cu", "decode_mma_e4m3_f32.cu"]
-HEADERS = ["gar_internal.hpp", "gar_device.cuh", "decode.cuh", "decode_mma.cuh"]
+HEADERS = ["gar_internal.hpp", "gar_device.cuh", "decode.cuh", "decode_mma.cuh", "device_once.hpp"]
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 
 

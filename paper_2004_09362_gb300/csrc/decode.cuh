@@ -52,6 +52,7 @@ struct DecodeArgs {
   float *part_o;
   unsigned int *count;
   int dim_pad;             // floats of a stored o row
+  int device;              // the launch's
 };
 
 // x / d; a division in 32-bit floats, put right, where they hold x (the compiler's takes three times as long).

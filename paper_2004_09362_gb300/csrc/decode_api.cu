@@ -160,7 +160,7 @@ int gar_decode_attention(gar_attn_plan *plan, const gar_kv_cache *cache, const v
   a.count = reinterpret_cast<unsigned *>(ws);
   a.part_ml = reinterpret_cast<float2 *>(ws + kCounterBytes);
   a.part_o = reinterpret_cast<float *>(a.part_ml + (size_t)kMaxCtas * 2 * kMaxGroup);
-  a.dim_pad = dim_pad(plan->dim);
+  a.dim_pad = dim_pad(plan->dim), a.device = dev;
   a.out_wide = (uintptr_t)out % (4 * element_size(out_dtype)) == 0 && plan->dim % 4 == 0 && out_batch_stride % 4 == 0 &&
                out_head_stride % 4 == 0;
   // Units as large as it takes for the whole line to stay below 2^30 of them.

@@ -50,6 +50,7 @@
 #include <cuda.h>
 
 #include "decode.cuh"
+#include "device_once.hpp"
 
 namespace gar {
 
@@ -816,8 +817,11 @@ template <typename C, int DP, int NG, bool Q32> int launch_mma(DecodeArgs a, int
   CUtensorMap maps[2];
   const auto run = [&](auto boxes) {
     constexpr auto kernel = mma_kernel<C, DP, NG, decltype(boxes)::value, Q32>;
-    static const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, S::kShared);
-    if (e != cudaSuccess) return cuda_fail(e, "cudaFuncSetAttribute");
+    static DeviceSet allowed;
+    const int e = once_for_device(allowed, a.device, [&] {
+      return (int)cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, S::kShared);
+    });
+    if (e != 0) return cuda_fail((cudaError_t)e, "cudaFuncSetAttribute");
     return launch("gar_decode_attention", kernel, sms, 32 * S::kWarps, S::kShared, stream, a, maps[0], maps[1]);
   };
   if constexpr (S::kBoxes)

@@ -1,6 +1,9 @@
 """The decoding operators' Python calls: memory, streams, devices, types and gradients."""
 
 import gc
+import os
+import re
+import subprocess
 import types
 
 import pytest
@@ -105,3 +108,28 @@ def test_attention_with_the_callers_workspace():
     gar.gar_attn_plan_set_workspace(plan, mine.data_ptr(), n)
     assert torch.equal(gar.gar_decode_attention(plan, q, cache, table, lens), want)
     assert bool((mine != 255).any()) and plan.workspace == (mine.data_ptr(), n)
+
+
+def test_what_belongs_to_a_device_is_done_for_each(tmp_path):
+    """The kernels' shared memory is allowed for each device that they are launched on, and again after a refusal."""
+    csrc = os.path.join(os.path.dirname(gar.__file__), "csrc")
+    (tmp_path / "t.cpp").write_text("""
+        #include "device_once.hpp"
+        #include <cstdio>
+        #include <initializer_list>
+        int main() {
+          static gar::DeviceSet set;
+          for (int device : {0, 0, 1, 63, 0, 1, 63, 64, 64, 2, 2, 2}) {
+            int called = 0;
+            static int left = 1;   // device 2 is refused once
+            const int e = gar::once_for_device(set, device, [&] { called = 1; return device == 2 && left-- > 0 ? 7 : 0; });
+            std::printf("%d%d ", called, e);
+          }
+        }""")
+    exe = str(tmp_path / "t")
+    subprocess.run(["g++", "-std=c++17", "-I", csrc, str(tmp_path / "t.cpp"), "-o", exe], check=True)
+    got = subprocess.run([exe], capture_output=True, text=True, check=True).stdout.split()
+    assert got == ["10", "00", "10", "10", "00", "00", "00", "10", "10", "17", "10", "00"]
+    for name in os.listdir(csrc):           # and nothing keeps such a result for the process
+        with open(os.path.join(csrc, name)) as f:
+            assert not re.search(r"static\s+(const\s+)?(cudaError_t|CUresult)\s+\w+\s*=", f.read()), name
