@@ -6,6 +6,7 @@
 
 #include <ATen/core/Tensor.h>
 #include <ATen/cuda/EmptyTensor.h>
+#include <c10/cuda/CUDAFunctions.h>
 #include <c10/cuda/CUDAGuard.h>
 #include <c10/cuda/CUDAStream.h>
 #include <torch/csrc/autograd/python_variable.h>
@@ -81,9 +82,19 @@ bool truth(PyObject *o) {
   return v;
 }
 
+// Names of attributes, made once.
+struct Names {
+  PyObject *address = PyUnicode_InternFromString("address"), *device_index = PyUnicode_InternFromString("device_index"),
+           *stream = PyUnicode_InternFromString("stream");
+};
+const Names &names_of() {
+  static const Names n;
+  return n;
+}
+
 // An address that a Python object keeps as an integer.
-template <typename T> T *handle(PyObject *o, const char *attribute, const char *what) {
-  PyObject *v = PyObject_GetAttrString(o, attribute);
+template <typename T> T *handle(PyObject *o, const char *what) {
+  PyObject *v = PyObject_GetAttr(o, names_of().address);
   if (!v) throw python_error();
   void *p = PyLong_AsVoidPtr(v);
   Py_DECREF(v);
@@ -129,6 +140,34 @@ const Tensor &rotations(PyObject *o, int64_t dim) {
   if (t.size(1) < 1 || 2 * t.size(1) > dim)
     bad("the table rotates " + std::to_string(2 * t.size(1)) + " channels, the heads have " + std::to_string(dim));
   return t;
+}
+
+// The GPU that a call's tensors are on: one for all, and the current one.
+class Device {
+  int at = -1;
+
+ public:
+  void add(int device, const char *what) {
+    if (at < 0) at = device;
+    if (device != at)
+      bad(std::string(what) + " is on GPU " + std::to_string(device) + ", what comes before it on GPU " + std::to_string(at));
+  }
+  void add(const Tensor &t, const char *what) { add(t.get_device(), what); }
+  void check() const {
+    const int current = c10::cuda::current_device();
+    if (at != current)
+      bad("the tensors are on GPU " + std::to_string(at) + ", the current device is GPU " + std::to_string(current));
+  }
+};
+
+// The GPU of a cache.
+int device_of(PyObject *cache) {
+  PyObject *v = PyObject_GetAttr(cache, names_of().device_index);
+  if (!v) throw python_error();
+  const long d = PyLong_AsLong(v);
+  Py_DECREF(v);
+  if (PyErr_Occurred()) throw python_error();
+  return (int)d;
 }
 
 int layout_of(PyObject *o) {
@@ -195,14 +234,17 @@ PyObject *rope(PyObject *, PyObject *const *args, Py_ssize_t n, PyObject *kw) {
     const Arguments<7> a("gar_rope", names, 3, args, n, kw);
     const Tensor &x = rows(a.at[0], "x"), &table = rotations(a.at[2], x.size(2));
     const Tensor &positions = integers(a.at[1], x.size(0), true, true, "positions");
-    const Stream stream(a.at[6]);
     Tensor out;
+    Device device;
+    device.add(x, "x"), device.add(positions, "positions"), device.add(table, "table");
     if (a.at[5]) {
       out = rows(a.at[5], "out");
       if (out.scalar_type() != x.scalar_type() || out.sizes() != x.sizes()) bad("out must have x's shape and dtype");
-    } else {
-      out = stream.empty(x.sizes(), x.scalar_type(), x);
+      device.add(out, "out");
     }
+    device.check();
+    const Stream stream(a.at[6]);
+    if (!a.at[5]) out = stream.empty(x.sizes(), x.scalar_type(), x);
     check(gar_rope(x.data_ptr(), x.stride(0), x.stride(1), out.data_ptr(), out.stride(0), out.stride(1), dtype_of(x, "x"),
                    x.size(0), (int)x.size(1), (int)x.size(2), 2 * (int)table.size(1), positions.data_ptr(),
                    (int)positions.element_size(), static_cast<const float *>(table.data_ptr()), table.size(0),
@@ -216,7 +258,7 @@ PyObject *kv_write(PyObject *, PyObject *const *args, Py_ssize_t n, PyObject *kw
   return guarded([&] {
     static const char *const names[] = {"cache", "k", "v", "slots", "positions", "table", "layout", "stream"};
     const Arguments<8> a("gar_kv_write", names, 4, args, n, kw);
-    const gar_kv_cache *cache = handle<gar_kv_cache>(a.at[0], "address", "the cache has no address");
+    const gar_kv_cache *cache = handle<gar_kv_cache>(a.at[0], "the cache has no address");
     const Tensor &k = rows(a.at[1], "k"), &v = rows(a.at[2], "v");
     if (k.sizes() != v.sizes() || k.scalar_type() != v.scalar_type() || k.size(1) != cache->heads || k.size(2) != cache->dim)
       bad("k and v must be [tokens, heads, dim] of the cache's heads and dim, alike in dtype");
@@ -226,11 +268,15 @@ PyObject *kv_write(PyObject *, PyObject *const *args, Py_ssize_t n, PyObject *kw
     const float *table = nullptr;
     int width = 8, rot = 0;
     int64_t table_rows = 0;
+    Device device;
+    device.add(device_of(a.at[0]), "cache"), device.add(k, "k"), device.add(v, "v"), device.add(slots, "slots");
     if (a.at[4]) {
       const Tensor &t = rotations(a.at[5], k.size(2)), &p = integers(a.at[4], k.size(0), true, true, "positions");
       positions = p.data_ptr(), width = (int)p.element_size(), table = static_cast<const float *>(t.data_ptr());
       table_rows = t.size(0), rot = 2 * (int)t.size(1);
+      device.add(p, "positions"), device.add(t, "table");
     }
+    device.check();
     const Stream stream(a.at[7]);
     check(gar_kv_write(cache, k.data_ptr(), k.stride(0), k.stride(1), v.data_ptr(), v.stride(0), v.stride(1),
                        dtype_of(k, "k"), k.size(0), static_cast<const int64_t *>(slots.data_ptr()), positions, width, table,
@@ -244,10 +290,11 @@ PyObject *kv_read(PyObject *, PyObject *const *args, Py_ssize_t n, PyObject *kw)
   return guarded([&] {
     static const char *const names[] = {"cache", "slots", "dtype", "out", "stream"};
     const Arguments<5> a("gar_kv_read", names, 2, args, n, kw);
-    const gar_kv_cache *cache = handle<gar_kv_cache>(a.at[0], "address", "the cache has no address");
+    const gar_kv_cache *cache = handle<gar_kv_cache>(a.at[0], "the cache has no address");
     const Tensor &slots = integers(a.at[1], -1, false, true, "slots");
-    const Stream stream(a.at[4]);
     Tensor k, v;
+    Device device;
+    device.add(device_of(a.at[0]), "cache"), device.add(slots, "slots");
     const int64_t shape[3] = {slots.size(0), cache->heads, cache->dim};
     if (a.at[3]) {
       if (!PyTuple_Check(a.at[3]) || PyTuple_GET_SIZE(a.at[3]) != 2) bad("out must be a pair of tensors");
@@ -255,7 +302,11 @@ PyObject *kv_read(PyObject *, PyObject *const *args, Py_ssize_t n, PyObject *kw)
       for (const Tensor &t : {k, v})
         if (t.sizes() != at::IntArrayRef(shape) || t.scalar_type() != k.scalar_type() || !t.is_cuda() || !t.is_contiguous())
           bad("out must be two contiguous CUDA tensors [tokens, heads, dim] of one dtype");
-    } else {
+      device.add(k, "out"), device.add(v, "out");
+    }
+    device.check();
+    const Stream stream(a.at[4]);
+    if (!a.at[3]) {
       at::ScalarType type = cache->dtype == GAR_F32 ? at::kFloat : cache->dtype == GAR_F16 ? at::kHalf : at::kBFloat16;
       if (a.at[2]) {
         const char *s = PyUnicode_Check(a.at[2]) ? PyUnicode_AsUTF8(a.at[2]) : nullptr;
@@ -288,8 +339,8 @@ PyObject *decode_attention(PyObject *, PyObject *const *args, Py_ssize_t n, PyOb
     static const char *const names[] = {"plan",  "q",      "cache", "page_table", "lengths",
                                         "scale", "window", "out",   "lse",        "stream"};
     const Arguments<10> a("gar_decode_attention", names, 5, args, n, kw);
-    gar_attn_plan *plan = handle<gar_attn_plan>(a.at[0], "address", "plan destroyed");
-    const gar_kv_cache *cache = handle<gar_kv_cache>(a.at[2], "address", "the cache has no address");
+    gar_attn_plan *plan = handle<gar_attn_plan>(a.at[0], "plan destroyed");
+    const gar_kv_cache *cache = handle<gar_kv_cache>(a.at[2], "the cache has no address");
     const Tensor &q = rows(a.at[1], "q"), &lengths = integers(a.at[4], q.size(0), true, false, "lengths");
     const Tensor &table = tensor(a.at[3], "page_table");
     if (table.dim() != 2 || table.size(0) != q.size(0) || table.scalar_type() != at::kInt || !table.is_cuda() ||
@@ -299,9 +350,25 @@ PyObject *decode_attention(PyObject *, PyObject *const *args, Py_ssize_t n, PyOb
     check(gar_attn_plan_shape(plan, &shape[0], &shape[1], &shape[2]), "gar_attn_plan_shape");
     if (q.size(1) != shape[0] || q.size(2) != shape[2])
       bad("q must be [batch, " + std::to_string(shape[0]) + ", " + std::to_string(shape[2]) + "]");
+    Tensor out, lse;
+    Device device;
+    device.add(device_of(a.at[2]), "cache"), device.add(q, "q"), device.add(table, "page_table"), device.add(lengths, "lengths");
+    if (a.at[7]) {
+      out = rows(a.at[7], "out");
+      if (out.sizes() != q.sizes()) bad("out must have q's shape");
+      device.add(out, "out");
+    }
+    const bool given = a.at[8] && !PyBool_Check(a.at[8]), wanted = given || truth(a.at[8]);
+    if (given) {
+      lse = tensor(a.at[8], "lse");
+      if (lse.scalar_type() != at::kFloat || lse.sizes() != q.sizes().slice(0, 2) || !lse.is_contiguous() || !lse.is_cuda())
+        bad("lse must be a contiguous float32 CUDA tensor [batch, q_heads]");
+      device.add(lse, "lse");
+    }
+    device.check();
     const Stream stream(a.at[9]);
     // The workspace comes with the first call; that the stream of a call uses it is known to its allocator.
-    PyObject *last = PyObject_GetAttrString(a.at[0], "stream");
+    PyObject *last = PyObject_GetAttr(a.at[0], names_of().stream);
     if (!last) throw python_error();
     const bool known = last != Py_None && PyLong_AsVoidPtr(last) == static_cast<void *>(stream.raw);
     Py_DECREF(last);
@@ -315,21 +382,8 @@ PyObject *decode_attention(PyObject *, PyObject *const *args, Py_ssize_t n, PyOb
       if (!r) throw python_error();
       Py_DECREF(r);
     }
-    Tensor out, lse;
-    if (a.at[7]) {
-      out = rows(a.at[7], "out");
-      if (out.sizes() != q.sizes()) bad("out must have q's shape");
-    } else {
-      out = stream.empty(q.sizes(), q.scalar_type(), q);
-    }
-    const bool given = a.at[8] && !PyBool_Check(a.at[8]), wanted = given || truth(a.at[8]);
-    if (given) {
-      lse = tensor(a.at[8], "lse");
-      if (lse.scalar_type() != at::kFloat || lse.sizes() != q.sizes().slice(0, 2) || !lse.is_contiguous() || !lse.is_cuda())
-        bad("lse must be a contiguous float32 CUDA tensor [batch, q_heads]");
-    } else if (wanted) {
-      lse = stream.empty(q.sizes().slice(0, 2), at::kFloat, q);
-    }
+    if (!a.at[7]) out = stream.empty(q.sizes(), q.scalar_type(), q);
+    if (wanted && !given) lse = stream.empty(q.sizes().slice(0, 2), at::kFloat, q);
     const double scale = a.at[5] ? number(a.at[5]) : 1.0 / std::sqrt((double)shape[2]);
     check(gar_decode_attention(plan, cache, q.data_ptr(), q.stride(0), q.stride(1), dtype_of(q, "q"), out.data_ptr(),
                                out.stride(0), out.stride(1), dtype_of(out, "out"),

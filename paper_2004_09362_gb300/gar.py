@@ -549,13 +549,18 @@ class KVCache:
             raise ValueError("scales go with the 8-bit types, and only with them")
         scale_stride, scale_at = (0, 0, 0), (None, None)
         if scaled:
-            scale_stride, scale_at = k_scale.stride(), (k_scale.data_ptr(), v_scale.data_ptr())
+            scale_stride = k_scale.stride()
             if (k_scale.shape != shape[:3] or v_scale.shape != shape[:3] or scale_stride != v_scale.stride()
                     or k_scale.dtype != torch.float32 or v_scale.dtype != torch.float32):
                 raise ValueError("scales must be float32 [pages, heads, page_size], alike in strides")
         if not (k.is_cuda and v.is_cuda) or scaled and not (k_scale.is_cuda and v_scale.is_cuda):
             raise ValueError("a cache is of CUDA tensors")
+        if any(t.device != k.device for t in ((v, k_scale, v_scale) if scaled else (v,))):
+            raise ValueError("a cache's tensors must be on one GPU")
+        if scaled:
+            scale_at = k_scale.data_ptr(), v_scale.data_ptr()
         self.k, self.v, self.k_scale, self.v_scale = k, v, k_scale, v_scale
+        self.device_index = k.get_device()
         self.status = _status_word(k.device)
         self.pages, self.heads, self.page_size, self.dim = shape
         self.dtype = dtype

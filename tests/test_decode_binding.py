@@ -1,13 +1,17 @@
 """The decoding operators' Python calls: memory, streams, devices, types and gradients."""
 
+import ctypes
 import gc
 import os
 import re
 import subprocess
 import types
+from unittest import mock
 
 import pytest
 import torch
+from torch._subclasses import fake_tensor
+from torch._subclasses.fake_tensor import FakeTensorMode
 
 from paper_2004_09362_gb300 import gar
 
@@ -133,3 +137,65 @@ def test_what_belongs_to_a_device_is_done_for_each(tmp_path):
     for name in os.listdir(csrc):           # and nothing keeps such a result for the process
         with open(os.path.join(csrc, name)) as f:
             assert not re.search(r"static\s+(const\s+)?(cudaError_t|CUresult)\s+\w+\s*=", f.read()), name
+
+
+def _fake(shape, dtype=torch.bfloat16, device=0):
+    """A tensor that says it is on a GPU, there or not; it has no memory."""
+    with mock.patch.object(fake_tensor, "init_gpu_context", lambda device: None, create=True), FakeTensorMode():
+        return torch.empty(shape, dtype=dtype, device=f"cuda:{int(device)}")
+
+
+def _fake_cache(device, heads=2, dim=64, page_size=16):
+    """A KVCache over addresses that nothing reads."""
+    cache = gar.KVCache.__new__(gar.KVCache)
+    cache._c = gar.gar_kv_cache(4096, 8192, None, None, None, 4, heads * page_size * dim, page_size * dim, dim, 0, 0, 0, gar.GAR_BF16,
+                                heads, dim, page_size)
+    cache.address, cache.device_index = ctypes.addressof(cache._c), device
+    return cache
+
+
+def _calls(devices):
+    """(name, number of tensors, call): the call with tensor i on GPU devices[i]."""
+    d = list(devices) + [0] * 8
+    i64, i32, f32 = torch.int64, torch.int32, torch.float32
+
+    def rope():
+        gar.gar_rope(_fake((4, 2, 64), device=d[0]), _fake(4, i64, d[1]), _fake((8, 32, 2), f32, d[2]), out=_fake((4, 2, 64), device=d[3]))
+
+    def write():
+        gar.gar_kv_write(_fake_cache(d[0]), _fake((4, 2, 64), device=d[1]), _fake((4, 2, 64), device=d[2]), _fake(4, i64, d[3]),
+                         _fake(4, i64, d[4]), _fake((8, 32, 2), f32, d[5]))
+
+    def read():
+        gar.gar_kv_read(_fake_cache(d[0]), _fake(4, i64, d[1]), out=(_fake((4, 2, 64), device=d[2]), _fake((4, 2, 64), device=d[3])))
+
+    def attention():
+        gar.gar_decode_attention(gar.gar_attn_plan_create(4, 2, 64), _fake((3, 4, 64), device=d[0]), _fake_cache(d[1]), _fake((3, 2), i32, d[2]),
+                                 _fake(3, i32, d[3]), out=_fake((3, 4, 64), device=d[4]), lse=_fake((3, 4), f32, d[5]))
+    return {"rope": (4, rope), "write": (6, write), "read": (4, read), "attention": (6, attention)}
+
+
+@pytest.mark.parametrize("name", ["rope", "write", "read", "attention"])
+def test_tensors_of_two_gpus_are_refused(name):
+    for i in range(_calls([])[name][0]):
+        with pytest.raises(ValueError, match="on GPU 1, |on GPU 0, "):
+            _calls([int(j == i) for j in range(6)])[name][1]()
+
+
+def test_a_cache_on_two_gpus_is_refused():
+    shape = (4, 2, 16, 64)
+    for i in range(4):
+        t = [_fake(shape, torch.int8, i == 0), _fake(shape, torch.int8, i == 1), _fake(shape[:3], torch.float32, i == 2),
+             _fake(shape[:3], torch.float32, i == 3)]
+        with pytest.raises(ValueError, match="one GPU"):
+            gar.KVCache(*t)
+    with pytest.raises(ValueError, match="one GPU"):
+        gar.KVCache(_fake(shape), _fake(shape, device=1))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("name", ["rope", "write", "read", "attention"])
+def test_tensors_of_a_gpu_that_is_not_current_are_refused(name):
+    torch.zeros(1, device="cuda")
+    with pytest.raises(ValueError, match="the current device is GPU 0"):
+        _calls([1] * 6)[name][1]()
