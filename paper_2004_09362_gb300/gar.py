@@ -513,18 +513,17 @@ def gar_rope_table(count: int, frequencies, magnitude: float = 1.0, first: int =
     return table
 
 
-_status_words = None, 0      # zeros on the GPU, and how many of them caches have taken
+_status_words = {}      # of each GPU: zeros there, and how many of them caches have taken
 
 
 def _status_word(device):
-    """A zero that no cache has had before (as a tensor, so that it stays allocated)."""
-    global _status_words
+    """A zero on the GPU `device` that no cache has had before (as a tensor, so that it stays allocated)."""
     import torch
-    words, used = _status_words
-    if words is None or used == words.shape[0] or words.device != device:
+    words, used = _status_words.get(device, (None, 0))
+    if words is None or used == words.shape[0]:
         words, used = torch.zeros(1024, dtype=torch.int32, device=device), 0
-        torch.cuda.synchronize()
-    _status_words = words, used + 1
+        torch.cuda.synchronize(device)
+    _status_words[device] = words, used + 1
     return words[used]
 
 

@@ -199,3 +199,32 @@ def test_tensors_of_a_gpu_that_is_not_current_are_refused(name):
     torch.zeros(1, device="cuda")
     with pytest.raises(ValueError, match="the current device is GPU 0"):
         _calls([1] * 6)[name][1]()
+
+
+class _Words:
+    """Stands for a tensor of status words on a GPU."""
+    made = []
+
+    def __init__(self, n, dtype=None, device=None):
+        self.shape, self.device = (n,), device
+        _Words.made.append(self)
+
+    def __getitem__(self, i):
+        return id(self), i
+
+
+@pytest.fixture
+def status_words(monkeypatch):
+    waited = []
+    _Words.made = []
+    monkeypatch.setattr(gar, "_status_words", {})
+    monkeypatch.setattr(torch, "zeros", _Words)
+    monkeypatch.setattr(torch.cuda, "synchronize", waited.append)
+    return waited
+
+
+def test_status_words_of_two_gpus(status_words):
+    """Each GPU has words of its own, made once and waited for on that GPU."""
+    a, b = torch.device("cuda:0"), torch.device("cuda:1")
+    got = [gar._status_word(d) for d in (a, b, a, b, a)]
+    assert len(set(got)) == 5 and [w.device for w in _Words.made] == [a, b] and status_words == [a, b]
