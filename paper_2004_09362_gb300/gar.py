@@ -9,6 +9,7 @@ from __future__ import annotations
 
 import ctypes
 import os
+import threading
 from typing import Sequence
 
 import numpy as np
@@ -514,17 +515,19 @@ def gar_rope_table(count: int, frequencies, magnitude: float = 1.0, first: int =
 
 
 _status_words = {}      # of each GPU: zeros there, and how many of them caches have taken
+_status_lock = threading.Lock()
 
 
 def _status_word(device):
     """A zero on the GPU `device` that no cache has had before (as a tensor, so that it stays allocated)."""
     import torch
-    words, used = _status_words.get(device, (None, 0))
-    if words is None or used == words.shape[0]:
-        words, used = torch.zeros(1024, dtype=torch.int32, device=device), 0
-        torch.cuda.synchronize(device)
-    _status_words[device] = words, used + 1
-    return words[used]
+    with _status_lock:
+        words, used = _status_words.get(device, (None, 0))
+        if words is None or used == words.shape[0]:
+            words, used = torch.zeros(1024, dtype=torch.int32, device=device), 0
+            torch.cuda.synchronize(device)
+        _status_words[device] = words, used + 1
+        return words[used]
 
 
 class KVCache:

@@ -5,6 +5,8 @@ import gc
 import os
 import re
 import subprocess
+import threading
+import time
 import types
 from unittest import mock
 
@@ -228,3 +230,19 @@ def test_status_words_of_two_gpus(status_words):
     a, b = torch.device("cuda:0"), torch.device("cuda:1")
     got = [gar._status_word(d) for d in (a, b, a, b, a)]
     assert len(set(got)) == 5 and [w.device for w in _Words.made] == [a, b] and status_words == [a, b]
+
+
+def test_threads_take_different_status_words(status_words, monkeypatch):
+    """A thread that is stopped between looking and taking (here while the words are made) leaves none for two."""
+    def slow(device):
+        status_words.append(device)
+        time.sleep(0.05)
+
+    monkeypatch.setattr(torch.cuda, "synchronize", slow)
+    got = []
+    threads = [threading.Thread(target=lambda: got.append(gar._status_word(torch.device("cuda:0")))) for _ in range(8)]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    assert len(set(got)) == 8 and len(_Words.made) == 1
