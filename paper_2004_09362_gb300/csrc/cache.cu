@@ -145,7 +145,7 @@ __device__ __forceinline__ void rotate(const CacheArgs &a, const float2 *t, cons
       const int pair = a.interleaved ? at / 2 : at < half ? at : at - half;
       const bool second = a.interleaved ? at & 1 : at >= half;
       const int other = a.interleaved ? at ^ 1 : second ? at - half : at + half;
-      const float2 cs = t ? __ldg(t + pair) : make_float2(__int_as_float(0x7fc00000), 0.f);
+      const float2 cs = t ? t[pair] : make_float2(__int_as_float(0x7fc00000), 0.f);
       float &x = k % 2 ? v[k / 2].y : v[k / 2].x;
       const float p = __fmul_rn(x, cs.x), q = __fmul_rn(to_f32(row[other]), cs.y);
       x = second ? __fadd_rn(p, q) : __fsub_rn(p, q);

@@ -151,13 +151,13 @@ __device__ __forceinline__ void load_rotation(const float2 *t, bool good, float 
   if (WIDE && N % 2 == 0) {
 #pragma unroll
     for (int k = 0; k < N; k += 2) {
-      const float4 v = good ? __ldg(reinterpret_cast<const float4 *>(t + k)) : make_float4(nan, nan, nan, nan);
+      const float4 v = good ? *reinterpret_cast<const float4 *>(t + k) : make_float4(nan, nan, nan, nan);
       c[k] = v.x, s[k] = v.y, c[k + 1] = v.z, s[k + 1] = v.w;
     }
   } else {
 #pragma unroll
     for (int k = 0; k < N; ++k) {
-      const float2 v = good ? __ldg(t + k) : make_float2(nan, nan);
+      const float2 v = good ? t[k] : make_float2(nan, nan);
       c[k] = v.x, s[k] = v.y;
     }
   }
