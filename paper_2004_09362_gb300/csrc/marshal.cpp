@@ -9,6 +9,7 @@
 #include <c10/cuda/CUDAFunctions.h>
 #include <c10/cuda/CUDAGuard.h>
 #include <c10/cuda/CUDAStream.h>
+#include <torch/csrc/autograd/custom_function.h>
 #include <torch/csrc/autograd/python_variable.h>
 
 #include <cmath>
@@ -184,6 +185,7 @@ int layout_of(PyObject *o) {
 struct Stream {
   gar_stream_t raw;
   bool other;  // not torch's current stream
+  explicit Stream(gar_stream_t raw) : raw(raw), other(raw != c10::cuda::getCurrentCUDAStream().stream()) {}
   explicit Stream(PyObject *o) {
     const cudaStream_t current = c10::cuda::getCurrentCUDAStream().stream();
     raw = current;
@@ -205,6 +207,14 @@ struct Stream {
   }
 };
 
+// Whether a gradient is asked of any of the tensors (null and undefined ones aside).
+bool graded_any(std::initializer_list<const Tensor *> tensors) {
+  if (!at::GradMode::is_enabled()) return false;
+  for (const Tensor *t : tensors)
+    if (t && t->defined() && t->requires_grad()) return true;
+  return false;
+}
+
 void check(int rc, const char *where) {
   if (rc == GAR_OK) return;
   PyObject *m = PyImport_ImportModule("paper_2004_09362_gb300.gar");
@@ -214,9 +224,20 @@ void check(int rc, const char *where) {
   throw python_error();
 }
 
+// A refused call where there may be no Python.
+struct call_failed : std::runtime_error {
+  int rc;
+  const char *where;
+  call_failed(int rc, const char *where) : std::runtime_error(std::string(where) + ": " + gar_last_error()), rc(rc), where(where) {}
+};
+
 template <typename F> PyObject *guarded(F f) noexcept {
   try {
-    return f();
+    try {
+      return f();
+    } catch (const call_failed &e) {
+      check(e.rc, e.where);
+    }
   } catch (const python_error &) {
   } catch (const std::invalid_argument &e) {
     PyErr_SetString(PyExc_ValueError, e.what());
@@ -227,6 +248,39 @@ template <typename F> PyObject *guarded(F f) noexcept {
   }
   return nullptr;
 }
+
+int rope_into(const Tensor &x, const Tensor &positions, const Tensor &table, int layout, bool inverse, const Tensor &out,
+              gar_stream_t stream) {
+  return gar_rope(x.data_ptr(), x.stride(0), x.stride(1), out.data_ptr(), out.stride(0), out.stride(1), dtype_of(x, "x"),
+                  x.size(0), (int)x.size(1), (int)x.size(2), 2 * (int)table.size(1), positions.data_ptr(),
+                  (int)positions.element_size(), static_cast<const float *>(table.data_ptr()), table.size(0), layout, inverse,
+                  stream);
+}
+
+// The rotation as a step that gradients go through: theirs is the rotation back.  (Without Python: gradients are computed
+// on threads of autograd's, under the stream that was torch's current one.)
+struct RopeStep : torch::autograd::Function<RopeStep> {
+  static Tensor forward(torch::autograd::AutogradContext *ctx, const Tensor &x, const Tensor &positions, const Tensor &table,
+                        int64_t layout, bool inverse, int64_t raw) {
+    ctx->save_for_backward({positions, table});
+    ctx->saved_data["layout"] = layout;
+    ctx->saved_data["inverse"] = inverse;
+    const Stream stream(reinterpret_cast<gar_stream_t>(raw));
+    const Tensor out = stream.empty(x.sizes(), x.scalar_type(), x);
+    if (const int rc = rope_into(x, positions, table, (int)layout, inverse, out, stream.raw)) throw call_failed(rc, "gar_rope");
+    return out;
+  }
+  static torch::autograd::variable_list backward(torch::autograd::AutogradContext *ctx, torch::autograd::variable_list grads) {
+    const auto saved = ctx->get_saved_variables();
+    Tensor grad = grads[0];
+    if (!grad.defined()) return {Tensor(), Tensor(), Tensor(), Tensor(), Tensor(), Tensor()};
+    if (grad.size(2) > 1 && grad.stride(2) != 1) grad = grad.contiguous();
+    const c10::cuda::CUDAGuard guard(grad.device());
+    const Tensor out = apply(grad, saved[0], saved[1], ctx->saved_data["layout"].toInt(), !ctx->saved_data["inverse"].toBool(),
+                             (int64_t)(intptr_t)c10::cuda::getCurrentCUDAStream().stream());
+    return {out, Tensor(), Tensor(), Tensor(), Tensor(), Tensor()};
+  }
+};
 
 PyObject *rope(PyObject *, PyObject *const *args, Py_ssize_t n, PyObject *kw) {
   return guarded([&] {
@@ -242,14 +296,15 @@ PyObject *rope(PyObject *, PyObject *const *args, Py_ssize_t n, PyObject *kw) {
       if (out.scalar_type() != x.scalar_type() || out.sizes() != x.sizes()) bad("out must have x's shape and dtype");
       device.add(out, "out");
     }
+    const bool graded = graded_any({&x, &table, &out});
+    if (graded && (a.at[5] || table.requires_grad()))
+      bad(a.at[5] ? "out= goes with tensors that need no gradient" : "the table gets no gradient: detach it");
+    const int layout = layout_of(a.at[3]), inverse = truth(a.at[4]);
     device.check();
     const Stream stream(a.at[6]);
+    if (graded) return THPVariable_Wrap(RopeStep::apply(x, positions, table, (int64_t)layout, (bool)inverse, (int64_t)(intptr_t)stream.raw));
     if (!a.at[5]) out = stream.empty(x.sizes(), x.scalar_type(), x);
-    check(gar_rope(x.data_ptr(), x.stride(0), x.stride(1), out.data_ptr(), out.stride(0), out.stride(1), dtype_of(x, "x"),
-                   x.size(0), (int)x.size(1), (int)x.size(2), 2 * (int)table.size(1), positions.data_ptr(),
-                   (int)positions.element_size(), static_cast<const float *>(table.data_ptr()), table.size(0),
-                   layout_of(a.at[3]), truth(a.at[4]), stream.raw),
-          "gar_rope");
+    check(rope_into(x, positions, table, layout, inverse, out, stream.raw), "gar_rope");
     return a.at[5] ? Py_NewRef(a.at[5]) : THPVariable_Wrap(std::move(out));
   });
 }
@@ -408,7 +463,7 @@ PyMethodDef methods[] = {
      "gar_rope(x, positions, table, layout='half', inverse=False, out=None, stream=None)\n--\n\n"
      "x [tokens, heads, dim] with its first rot channels rotated by the table's rows at\n"
      "`positions` (int32 or int64); out may be x.  With inverse, the gradient: x is grad_out, the result\n"
-     "grad_x.  layout: 'half' or 'interleaved'."},
+     "grad_x.  layout: 'half' or 'interleaved'.  Gradients flow through a call without out, but not to the table."},
     {"gar_kv_write", (PyCFunction)(void (*)())kv_write, METH_FASTCALL | METH_KEYWORDS,
      "gar_kv_write(cache, k, v, slots, positions=None, table=None, layout='half', stream=None)\n--\n\n"
      "Writes k, v [tokens, heads, dim] to the cache's slots (int64; negative: skipped),\n"

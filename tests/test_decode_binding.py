@@ -246,3 +246,70 @@ def test_threads_take_different_status_words(status_words, monkeypatch):
     for t in threads:
         t.join()
     assert len(set(got)) == 8 and len(_Words.made) == 1
+
+
+def test_rotation_into_memory_has_no_gradient():
+    table, pos = _fake((8, 32, 2), torch.float32), _fake(4, torch.int64)
+    for x, out in ((_fake((4, 2, 64)).requires_grad_(), _fake((4, 2, 64))), (_fake((4, 2, 64)), _fake((4, 2, 64)).requires_grad_())):
+        with pytest.raises(ValueError, match="gradient"):
+            gar.gar_rope(x, pos, table, out=out)
+    with pytest.raises(ValueError, match="gradient"):
+        gar.gar_rope(_fake((4, 2, 64)), pos, table.requires_grad_())
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("layout", ["half", "interleaved"])
+@pytest.mark.parametrize("dtype,dim,rot", [(torch.float32, 20, 12), (torch.bfloat16, 128, 128)])
+def test_gradients_through_the_rotation(layout, dtype, dim, rot):
+    f, m = gar.gar_rope_frequencies(rot, 10000.0, "parts", 2.0, 32.0)
+    table = gar.gar_rope_table(50, f, m)
+    pos = torch.arange(7, device="cuda") * 5
+    x = torch.randn(7, 3, dim, device="cuda").to(dtype).requires_grad_()
+    g = torch.randn(7, 3, dim, device="cuda").to(dtype)
+    plain = gar.gar_rope(x.detach(), pos, table, layout)
+    assert not plain.requires_grad
+    y = gar.gar_rope(x, pos, table, layout)
+    assert y.requires_grad and torch.equal(y, plain)
+    grad, = torch.autograd.grad(y, x, g)
+    assert torch.equal(grad, gar.gar_rope(g, pos, table, layout, inverse=True))
+    # a gradient that is one number everywhere (strides of zero), and one of another order
+    grad, = torch.autograd.grad(gar.gar_rope(x, pos, table, layout).sum(), x)
+    assert torch.equal(grad, gar.gar_rope(torch.ones_like(g), pos, table, layout, inverse=True))
+    turned = g.permute(2, 1, 0).contiguous().permute(2, 1, 0)
+    grad, = torch.autograd.grad(gar.gar_rope(x, pos, table, layout, inverse=True), x, turned)
+    assert torch.equal(grad, gar.gar_rope(g, pos, table, layout))
+    # the gradient's own gradient is the rotation again
+    h = torch.randn_like(g).requires_grad_()
+    grad, = torch.autograd.grad(gar.gar_rope(x, pos, table, layout), x, h, create_graph=True)
+    again, = torch.autograd.grad(grad, h, g)
+    assert torch.equal(again, gar.gar_rope(g, pos, table, layout))
+    # under a stream of the call's own
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    y = gar.gar_rope(x, pos, table, layout, stream=side)
+    torch.cuda.current_stream().wait_stream(side)
+    grad, = torch.autograd.grad(y, x, g)
+    assert torch.equal(y, plain) and torch.equal(grad, gar.gar_rope(g, pos, table, layout, inverse=True))
+    with torch.no_grad():
+        assert not gar.gar_rope(x, pos, table, layout).requires_grad
+        assert torch.equal(gar.gar_rope(x, pos, table, layout, out=torch.empty_like(g)), plain)
+    if dtype == torch.float32:              # 32-bit differences of a linear map, whatever the step
+        loss = lambda t: (gar.gar_rope(t, pos, table, layout).double() * g.double()).sum()
+        grad, = torch.autograd.grad(loss(x), x)
+        with torch.no_grad():
+            for i in range(0, x.numel(), 37):
+                t = x.detach().clone()
+                t.view(-1)[i] += 1
+                step = float(t.view(-1)[i] - x.view(-1)[i])
+                d = float(loss(t) - loss(x)) / step
+                # two channels differ, each off by at most 4u(|u| + |v|)m in both evaluations
+                assert abs(d - float(grad.view(-1)[i])) <= 64 * 2.0 ** -24 * float((x.abs().max() + 1) * g.abs().max()) * m
+    many = torch.ones(1, 1, dim, device="cuda", dtype=dtype).expand(1, (1 << 20) + 1, dim)
+    for t in (many, many.clone().requires_grad_()):
+        with pytest.raises(gar.GarError, match="heads"):
+            gar.gar_rope(t, pos[:1], table, layout)
+    table2 = table.clone()
+    y = gar.gar_rope(x, pos, table2, layout)
+    table2 += 1
+    with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+        torch.autograd.grad(y, x, g)
