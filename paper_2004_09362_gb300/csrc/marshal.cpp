@@ -215,6 +215,11 @@ bool graded_any(std::initializer_list<const Tensor *> tensors) {
   return false;
 }
 
+// For calls that no gradient goes through.
+void refuse_graded(std::initializer_list<const Tensor *> tensors) {
+  if (graded_any(tensors)) bad("this call has no gradient: detach its tensors, or call it under torch.no_grad()");
+}
+
 void check(int rc, const char *where) {
   if (rc == GAR_OK) return;
   PyObject *m = PyImport_ImportModule("paper_2004_09362_gb300.gar");
@@ -318,6 +323,7 @@ PyObject *kv_write(PyObject *, PyObject *const *args, Py_ssize_t n, PyObject *kw
     if (k.sizes() != v.sizes() || k.scalar_type() != v.scalar_type() || k.size(1) != cache->heads || k.size(2) != cache->dim)
       bad("k and v must be [tokens, heads, dim] of the cache's heads and dim, alike in dtype");
     const Tensor &slots = integers(a.at[3], k.size(0), false, true, "slots");
+    refuse_graded({&k, &v});
     if (!a.at[4] != !a.at[5]) bad("positions and table go together");
     const void *positions = nullptr;
     const float *table = nullptr;
@@ -330,6 +336,7 @@ PyObject *kv_write(PyObject *, PyObject *const *args, Py_ssize_t n, PyObject *kw
       positions = p.data_ptr(), width = (int)p.element_size(), table = static_cast<const float *>(t.data_ptr());
       table_rows = t.size(0), rot = 2 * (int)t.size(1);
       device.add(p, "positions"), device.add(t, "table");
+      refuse_graded({&t});
     }
     device.check();
     const Stream stream(a.at[7]);
@@ -358,6 +365,7 @@ PyObject *kv_read(PyObject *, PyObject *const *args, Py_ssize_t n, PyObject *kw)
         if (t.sizes() != at::IntArrayRef(shape) || t.scalar_type() != k.scalar_type() || !t.is_cuda() || !t.is_contiguous())
           bad("out must be two contiguous CUDA tensors [tokens, heads, dim] of one dtype");
       device.add(k, "out"), device.add(v, "out");
+      refuse_graded({&k, &v});
     }
     device.check();
     const Stream stream(a.at[4]);
@@ -420,6 +428,7 @@ PyObject *decode_attention(PyObject *, PyObject *const *args, Py_ssize_t n, PyOb
         bad("lse must be a contiguous float32 CUDA tensor [batch, q_heads]");
       device.add(lse, "lse");
     }
+    refuse_graded({&q, &out, &lse});
     device.check();
     const Stream stream(a.at[9]);
     // The workspace comes with the first call; that the stream of a call uses it is known to its allocator.
@@ -467,7 +476,8 @@ PyMethodDef methods[] = {
     {"gar_kv_write", (PyCFunction)(void (*)())kv_write, METH_FASTCALL | METH_KEYWORDS,
      "gar_kv_write(cache, k, v, slots, positions=None, table=None, layout='half', stream=None)\n--\n\n"
      "Writes k, v [tokens, heads, dim] to the cache's slots (int64; negative: skipped),\n"
-     "quantised where the cache is; with positions and table, the keys rotated first."},
+     "quantised where the cache is; with positions and table, the keys rotated first.  Has no gradient, nor have\n"
+     "the calls that read the cache: tensors that ask for one are refused."},
     {"gar_kv_read", (PyCFunction)(void (*)())kv_read, METH_FASTCALL | METH_KEYWORDS,
      "gar_kv_read(cache, slots, dtype=None, out=None, stream=None)\n--\n\n"
      "(k, v), each [tokens, heads, dim], of the cache's slots; rows of negative slots are 0.\n"

@@ -559,6 +559,8 @@ class KVCache:
             raise ValueError("a cache is of CUDA tensors")
         if any(t.device != k.device for t in ((v, k_scale, v_scale) if scaled else (v,))):
             raise ValueError("a cache's tensors must be on one GPU")
+        if torch.is_grad_enabled() and any(t.requires_grad for t in ((k, v, k_scale, v_scale) if scaled else (k, v))):
+            raise ValueError("a cache has no gradient: detach its tensors")
         if scaled:
             scale_at = k_scale.data_ptr(), v_scale.data_ptr()
         self.k, self.v, self.k_scale, self.v_scale = k, v, k_scale, v_scale

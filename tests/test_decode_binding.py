@@ -313,3 +313,36 @@ def test_gradients_through_the_rotation(layout, dtype, dim, rot):
     table2 += 1
     with pytest.raises(RuntimeError, match="modified by an inplace operation"):
         torch.autograd.grad(y, x, g)
+
+
+def test_calls_without_a_gradient_refuse_tensors_that_ask_for_one():
+    i64, i32, f32 = torch.int64, torch.int32, torch.float32
+    k, g = _fake((4, 2, 64)), _fake((4, 2, 64)).requires_grad_()
+    cache, slots, table = _fake_cache(0), _fake(4, i64), _fake((8, 32, 2), f32)
+    plan, pages, lens = gar.gar_attn_plan_create(2, 2, 64), _fake((4, 2), i32), _fake(4, i32)
+    lse = _fake((4, 2), f32).requires_grad_()
+    for call in (lambda: gar.gar_kv_write(cache, g, k, slots), lambda: gar.gar_kv_write(cache, k, g, slots),
+                 lambda: gar.gar_kv_write(cache, k, k, slots, slots, _fake((8, 32, 2), f32).requires_grad_()),
+                 lambda: gar.gar_kv_read(cache, slots, out=(k, g)), lambda: gar.gar_decode_attention(plan, g, cache, pages, lens),
+                 lambda: gar.gar_decode_attention(plan, k, cache, pages, lens, out=g),
+                 lambda: gar.gar_decode_attention(plan, k, cache, pages, lens, lse=lse)):
+        with pytest.raises(ValueError, match="gradient"):
+            call()
+    x = _fake((4, 2, 16, 64))
+    with pytest.raises(ValueError, match="gradient"):
+        gar.KVCache(x, _fake((4, 2, 16, 64)).requires_grad_())
+
+
+@pytest.mark.gpu
+def test_without_gradients_the_same_tensors_are_taken():
+    cache, table, lens, q = _problem()
+    plan = gar.gar_attn_plan_create(8, 2, 64)
+    want = gar.gar_decode_attention(plan, q, cache, table, lens)
+    q.requires_grad_()
+    for off in (torch.no_grad(), torch.inference_mode()):
+        with off:
+            assert torch.equal(gar.gar_decode_attention(plan, q, cache, table, lens), want)
+            k = q[:, :2].contiguous()
+            gar.gar_kv_write(cache, k, k, torch.arange(3, device="cuda"))
+            assert torch.equal(gar.gar_kv_read(cache, torch.arange(3, device="cuda"))[0], k)
+            cache, table, lens, _ = _problem()
