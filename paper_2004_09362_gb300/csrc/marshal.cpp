@@ -86,7 +86,7 @@ bool truth(PyObject *o) {
 // Names of attributes, made once.
 struct Names {
   PyObject *address = PyUnicode_InternFromString("address"), *device_index = PyUnicode_InternFromString("device_index"),
-           *stream = PyUnicode_InternFromString("stream");
+           *stream = PyUnicode_InternFromString("stream"), *tensors = PyUnicode_InternFromString("tensors");
 };
 const Names &names_of() {
   static const Names n;
@@ -215,6 +215,22 @@ bool graded_any(std::initializer_list<const Tensor *> tensors) {
   return false;
 }
 
+// Counts a tensor's memory as changed, so that autograd sees it where it has kept the tensor.  (Tensors of inference mode
+// are not counted.)
+void changed(const Tensor &t) {
+  if (!t.is_inference()) t.unsafeGetTensorImpl()->bump_version();
+}
+
+// The same of a cache's.
+void changed_cache(PyObject *cache) {
+  PyObject *tensors = PyObject_GetAttr(cache, names_of().tensors);
+  if (!tensors) throw python_error();
+  const Py_ssize_t n = PyTuple_Check(tensors) ? PyTuple_GET_SIZE(tensors) : 0;
+  for (Py_ssize_t i = 0; i < n; ++i)
+    if (THPVariable_Check(PyTuple_GET_ITEM(tensors, i))) changed(THPVariable_Unpack(PyTuple_GET_ITEM(tensors, i)));
+  Py_DECREF(tensors);
+}
+
 // For calls that no gradient goes through.
 void refuse_graded(std::initializer_list<const Tensor *> tensors) {
   if (graded_any(tensors)) bad("this call has no gradient: detach its tensors, or call it under torch.no_grad()");
@@ -310,7 +326,9 @@ PyObject *rope(PyObject *, PyObject *const *args, Py_ssize_t n, PyObject *kw) {
     if (graded) return THPVariable_Wrap(RopeStep::apply(x, positions, table, (int64_t)layout, (bool)inverse, (int64_t)(intptr_t)stream.raw));
     if (!a.at[5]) out = stream.empty(x.sizes(), x.scalar_type(), x);
     check(rope_into(x, positions, table, layout, inverse, out, stream.raw), "gar_rope");
-    return a.at[5] ? Py_NewRef(a.at[5]) : THPVariable_Wrap(std::move(out));
+    if (!a.at[5]) return THPVariable_Wrap(std::move(out));
+    changed(out);
+    return Py_NewRef(a.at[5]);
   });
 }
 
@@ -344,6 +362,7 @@ PyObject *kv_write(PyObject *, PyObject *const *args, Py_ssize_t n, PyObject *kw
                        dtype_of(k, "k"), k.size(0), static_cast<const int64_t *>(slots.data_ptr()), positions, width, table,
                        table_rows, rot, layout_of(a.at[6]), stream.raw),
           "gar_kv_write");
+    changed_cache(a.at[0]);
     return Py_NewRef(Py_None);
   });
 }
@@ -388,7 +407,10 @@ PyObject *kv_read(PyObject *, PyObject *const *args, Py_ssize_t n, PyObject *kw)
     check(gar_kv_read(cache, static_cast<const int64_t *>(slots.data_ptr()), slots.size(0), k.data_ptr(), v.data_ptr(),
                       dtype_of(k, "out"), stream.raw),
           "gar_kv_read");
-    if (a.at[3]) return Py_NewRef(a.at[3]);
+    if (a.at[3]) {
+      changed(k), changed(v);
+      return Py_NewRef(a.at[3]);
+    }
     PyObject *pair = PyTuple_New(2);
     if (!pair) throw python_error();
     PyTuple_SET_ITEM(pair, 0, THPVariable_Wrap(std::move(k)));
@@ -456,6 +478,8 @@ PyObject *decode_attention(PyObject *, PyObject *const *args, Py_ssize_t n, PyOb
                                static_cast<const int32_t *>(lengths.data_ptr()), (int)q.size(0), (float)scale,
                                a.at[6] ? (int)integer(a.at[6]) : 0, stream.raw),
           "gar_decode_attention");
+    if (a.at[7]) changed(out);
+    if (given) changed(lse);
     PyObject *first = a.at[7] ? Py_NewRef(a.at[7]) : THPVariable_Wrap(std::move(out));
     if (!wanted) return first;
     PyObject *pair = first ? PyTuple_New(2) : nullptr;

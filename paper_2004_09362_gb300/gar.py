@@ -565,6 +565,7 @@ class KVCache:
             scale_at = k_scale.data_ptr(), v_scale.data_ptr()
         self.k, self.v, self.k_scale, self.v_scale = k, v, k_scale, v_scale
         self.device_index = k.get_device()
+        self.tensors = (k, v, k_scale, v_scale) if scaled else (k, v)       # what gar_kv_write changes
         self.status = _status_word(k.device)
         self.pages, self.heads, self.page_size, self.dim = shape
         self.dtype = dtype

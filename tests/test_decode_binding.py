@@ -346,3 +346,35 @@ def test_without_gradients_the_same_tensors_are_taken():
             gar.gar_kv_write(cache, k, k, torch.arange(3, device="cuda"))
             assert torch.equal(gar.gar_kv_read(cache, torch.arange(3, device="cuda"))[0], k)
             cache, table, lens, _ = _problem()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("kind", [torch.bfloat16, torch.int8])
+def test_autograd_sees_what_calls_write(kind):
+    """Memory that a call has written counts as changed: a tensor that autograd has kept is not used with other contents."""
+    shape = (2, 2, 16, 64)
+    k, v = (torch.zeros(shape, device="cuda").to(kind) for _ in range(2))
+    scales = [torch.zeros(shape[:3], device="cuda") for _ in range(2 if kind == torch.int8 else 0)]
+    cache = gar.KVCache(k, v, *scales)
+    x = torch.randn(4, 2, 64, device="cuda").bfloat16()
+    slots, table = torch.arange(4, device="cuda"), gar.gar_rope_table(8, gar.gar_rope_frequencies(64)[0])
+    plan, pages = gar.gar_attn_plan_create(2, 2, 64), torch.zeros(4, 1, dtype=torch.int32, device="cuda")
+    lens = torch.full((4,), 4, dtype=torch.int32, device="cuda")
+    a, b, lse = torch.empty_like(x), torch.empty_like(x), torch.empty(4, 2, device="cuda")
+    for call, written in ((lambda: gar.gar_kv_write(cache, x, x, slots), [k, v, *scales]),
+                          (lambda: gar.gar_rope(x, slots, table, out=a), [a]),
+                          (lambda: gar.gar_kv_read(cache, slots, out=(a, b)), [a, b]),
+                          (lambda: gar.gar_decode_attention(plan, x, cache, pages, lens, out=a, lse=lse), [a, lse])):
+        others = [t for t in (k, v, *scales, x, a, b, lse) if all(t is not w for w in written)]
+        before = [t._version for t in written + others]
+        call()
+        assert [t._version - n for t, n in zip(written + others, before)] == [1] * len(written) + [0] * len(others)
+    y = a.detach().requires_grad_()         # shares a's memory and count
+    z = (y * y).sum()
+    gar.gar_rope(x, slots, table, out=a)
+    with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+        z.backward()
+    with torch.inference_mode():
+        t = torch.empty_like(x)
+    gar.gar_rope(x, slots, table, out=t)    # not counted, and taken
+    assert torch.equal(t, a)
