@@ -154,10 +154,11 @@ class Device {
       bad(std::string(what) + " is on GPU " + std::to_string(device) + ", what comes before it on GPU " + std::to_string(at));
   }
   void add(const Tensor &t, const char *what) { add(t.get_device(), what); }
-  void check() const {
+  int check() const {
     const int current = c10::cuda::current_device();
     if (at != current)
       bad("the tensors are on GPU " + std::to_string(at) + ", the current device is GPU " + std::to_string(current));
+    return current;
   }
 };
 
@@ -186,8 +187,8 @@ struct Stream {
   gar_stream_t raw;
   bool other;  // not torch's current stream
   explicit Stream(gar_stream_t raw) : raw(raw), other(raw != c10::cuda::getCurrentCUDAStream().stream()) {}
-  explicit Stream(PyObject *o) {
-    const cudaStream_t current = c10::cuda::getCurrentCUDAStream().stream();
+  Stream(PyObject *o, int device) {
+    const cudaStream_t current = c10::cuda::getCurrentCUDAStream((c10::DeviceIndex)device).stream();
     raw = current;
     if (o) {
       PyObject *v = PyLong_Check(o) ? Py_NewRef(o) : PyObject_GetAttrString(o, "cuda_stream");
@@ -321,8 +322,7 @@ PyObject *rope(PyObject *, PyObject *const *args, Py_ssize_t n, PyObject *kw) {
     if (graded && (a.at[5] || table.requires_grad()))
       bad(a.at[5] ? "out= goes with tensors that need no gradient" : "the table gets no gradient: detach it");
     const int layout = layout_of(a.at[3]), inverse = truth(a.at[4]);
-    device.check();
-    const Stream stream(a.at[6]);
+    const Stream stream(a.at[6], device.check());
     if (graded) return THPVariable_Wrap(RopeStep::apply(x, positions, table, (int64_t)layout, (bool)inverse, (int64_t)(intptr_t)stream.raw));
     if (!a.at[5]) out = stream.empty(x.sizes(), x.scalar_type(), x);
     check(rope_into(x, positions, table, layout, inverse, out, stream.raw), "gar_rope");
@@ -356,8 +356,7 @@ PyObject *kv_write(PyObject *, PyObject *const *args, Py_ssize_t n, PyObject *kw
       device.add(p, "positions"), device.add(t, "table");
       refuse_graded({&t});
     }
-    device.check();
-    const Stream stream(a.at[7]);
+    const Stream stream(a.at[7], device.check());
     check(gar_kv_write(cache, k.data_ptr(), k.stride(0), k.stride(1), v.data_ptr(), v.stride(0), v.stride(1),
                        dtype_of(k, "k"), k.size(0), static_cast<const int64_t *>(slots.data_ptr()), positions, width, table,
                        table_rows, rot, layout_of(a.at[6]), stream.raw),
@@ -386,8 +385,7 @@ PyObject *kv_read(PyObject *, PyObject *const *args, Py_ssize_t n, PyObject *kw)
       device.add(k, "out"), device.add(v, "out");
       refuse_graded({&k, &v});
     }
-    device.check();
-    const Stream stream(a.at[4]);
+    const Stream stream(a.at[4], device.check());
     if (!a.at[3]) {
       at::ScalarType type = cache->dtype == GAR_F32 ? at::kFloat : cache->dtype == GAR_F16 ? at::kHalf : at::kBFloat16;
       if (a.at[2]) {
@@ -451,8 +449,7 @@ PyObject *decode_attention(PyObject *, PyObject *const *args, Py_ssize_t n, PyOb
       device.add(lse, "lse");
     }
     refuse_graded({&q, &out, &lse});
-    device.check();
-    const Stream stream(a.at[9]);
+    const Stream stream(a.at[9], device.check());
     // The workspace comes with the first call; that the stream of a call uses it is known to its allocator.
     PyObject *last = PyObject_GetAttr(a.at[0], names_of().stream);
     if (!last) throw python_error();
