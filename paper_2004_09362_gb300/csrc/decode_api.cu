@@ -23,6 +23,14 @@ size_t workspace_bytes(const gar_attn_plan &p) {
   return kCounterBytes + rows * (2 + dim_pad(p.dim)) * sizeof(float);
 }
 
+// Rows of a unit of the line: as many as it takes for the whole line, each item counted twice at most, to stay below 2^30
+// units, or 0 where 2^15 do not.
+int unit_of(int64_t items, int most_rows) {
+  for (int unit = 64; unit <= 32768; unit *= 2)
+    if (items * (most_rows / unit + 3) * 2 < 1 << 30) return unit;
+  return 0;
+}
+
 // The tensor-core kernels copy 16-byte chunks.
 bool takes_mma(const gar_kv_cache &c, const void *q, int64_t q_batch_stride, int64_t q_head_stride, int q_dtype) {
   const int64_t n = 16 / element_size(c.dtype), m = 16 / element_size(q_dtype);
@@ -134,6 +142,11 @@ int gar_decode_attention(gar_attn_plan *plan, const gar_kv_cache *cache, const v
     set_error("a buffer is not aligned to its elements");
     return GAR_EALIGN;
   }
+  // Row numbers stay below 2^31 with room for a tile past the end.
+  const int most_rows = (int)std::min<int64_t>((int64_t)table_width * cache->page_size, 0x7fffffff - 65536);
+  const int group = plan->q_heads / plan->kv_heads;
+  const int unit = unit_of((int64_t)batch * plan->kv_heads * ((group + 7) / 8), most_rows);
+  if (unit == 0) return refuse("too many sequences and heads for tables this wide");
   if (plan->ws == nullptr) {
     set_error("gar_attn_plan_set_workspace has not been called");
     return GAR_ENOWS;
@@ -151,9 +164,7 @@ int gar_decode_attention(gar_attn_plan *plan, const gar_kv_cache *cache, const v
   a.qb = q_batch_stride, a.qh = q_head_stride, a.ob = out_batch_stride, a.oh = out_head_stride;
   a.table = page_table, a.table_stride = table_stride, a.lengths = lengths;
   a.page = divide_by((uint32_t)cache->page_size);
-  // Row numbers stay below 2^31 with room for a tile past the end.
-  a.most_rows = (int)std::min<int64_t>((int64_t)table_width * cache->page_size, 0x7fffffff - 65536);
-  a.batch = batch, a.q_heads = plan->q_heads, a.group = plan->q_heads / plan->kv_heads;
+  a.most_rows = most_rows, a.batch = batch, a.q_heads = plan->q_heads, a.group = group;
   a.q_dtype = q_dtype, a.out_dtype = out_dtype, a.window = window;
   a.scale_log2 = (float)((double)scale * 1.4426950408889634);
   char *ws = static_cast<char *>(plan->ws);
@@ -163,13 +174,8 @@ int gar_decode_attention(gar_attn_plan *plan, const gar_kv_cache *cache, const v
   a.dim_pad = dim_pad(plan->dim), a.device = dev;
   a.out_wide = (uintptr_t)out % (4 * element_size(out_dtype)) == 0 && plan->dim % 4 == 0 && out_batch_stride % 4 == 0 &&
                out_head_stride % 4 == 0;
-  // Units as large as it takes for the whole line to stay below 2^30 of them.
-  const int64_t items = (int64_t)batch * plan->kv_heads * ((a.group + 7) / 8);
-  if (items >= 1 << 28) return refuse("too many sequences and heads");
-  a.unit = 64;
-  while (items * (a.most_rows / a.unit + 3) * 2 >= 1 << 30) a.unit *= 2;
+  a.unit = unit;
   a.slack = std::max(1, 196608 / (128 * cache->dim * element_size(cache->dtype)));
-  if (a.unit > 32768) return refuse("too many sequences and heads for tables this wide");
   if (!takes_mma(*cache, q, q_batch_stride, q_head_stride, q_dtype)) return decode_general(a, plan->sms, stream);
   const bool q32 = q_dtype == GAR_F32;
   switch (cache->dtype) {

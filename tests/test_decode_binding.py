@@ -378,3 +378,21 @@ def test_autograd_sees_what_calls_write(kind):
         t = torch.empty_like(x)
     gar.gar_rope(x, slots, table, out=t)    # not counted, and taken
     assert torch.equal(t, a)
+
+
+def test_more_items_than_the_line_has_room_for_are_refused():
+    """Counts of sequences times heads up to the largest that an int holds: refused, or taken as far as to the missing
+    workspace (-6), never a number that the line cannot hold."""
+    cache = gar.gar_kv_cache(4096, 8192, None, None, None, 4, 1024, 1024, 64, 0, 0, 0, gar.GAR_BF16, 1, 64, 16)
+
+    def call(batch, width, heads=1):
+        plan = gar.gar_attn_plan_create(heads, 1, 64)
+        return gar._lib.gar_decode_attention(plan.handle, cache, 4096, 64 * heads, 64, gar.GAR_BF16, 8192, 64 * heads, 64, gar.GAR_BF16, None,
+                                             4096, width, width, 4096, batch, 0.125, 0, None)
+
+    assert call(178956970, 0) == -6 and call(178956971, 0) == -1
+    for batch in (178956971, 200000000, (1 << 28) - 1, 1 << 28, 2 ** 31 - 1):
+        for width in (0, 1, 100, 2 ** 31 - 1):
+            assert call(batch, width) == -1, (batch, width)
+    assert call(8000, 2 ** 31 - 1) == -6 and call(9000, 2 ** 31 - 1) == -1      # 2^31 / 2^15 units of each sequence
+    assert call(22369621, 0, 64) == -6 and call(22369622, 0, 64) == -1          # 8 groups of query heads
