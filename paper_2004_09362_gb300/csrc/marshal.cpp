@@ -12,6 +12,7 @@
 #include <torch/csrc/autograd/custom_function.h>
 #include <torch/csrc/autograd/python_variable.h>
 
+#include <climits>
 #include <cmath>
 #include <optional>
 #include <stdexcept>
@@ -71,6 +72,12 @@ int64_t integer(PyObject *o) {
   return v;
 }
 
+// A number that the C entry points take as an int.
+int narrow(int64_t v, const char *what) {
+  if (v < INT_MIN || v > INT_MAX) bad(std::string(what) + " is out of range: " + std::to_string(v));
+  return (int)v;
+}
+
 double number(PyObject *o) {
   const double v = PyFloat_AsDouble(o);
   if (v == -1 && PyErr_Occurred()) throw python_error();
@@ -121,6 +128,7 @@ const Tensor &rows(PyObject *o, const char *what) {
   if (t.dim() != 3) bad(std::string(what) + " must be [tokens, heads, dim]");
   if (t.stride(2) != 1 && t.size(2) > 1) bad(std::string(what) + ": the channels of a head must be contiguous");
   if (!t.is_cuda()) bad(std::string(what) + " must be a CUDA tensor");
+  narrow(t.size(1), "the number of heads"), narrow(t.size(2), "the number of channels");
   return t;
 }
 
@@ -179,7 +187,7 @@ int layout_of(PyObject *o) {
     if (PyUnicode_CompareWithASCIIString(o, "interleaved") == 0) return GAR_ROPE_INTERLEAVED;
     bad("unknown layout");
   }
-  return (int)integer(o);
+  return narrow(integer(o), "layout");
 }
 
 // The stream of a call: torch's current one, a torch stream, or a raw handle.
@@ -342,6 +350,7 @@ PyObject *kv_write(PyObject *, PyObject *const *args, Py_ssize_t n, PyObject *kw
       bad("k and v must be [tokens, heads, dim] of the cache's heads and dim, alike in dtype");
     const Tensor &slots = integers(a.at[3], k.size(0), false, true, "slots");
     refuse_graded({&k, &v});
+    const int layout = layout_of(a.at[6]);
     if (!a.at[4] != !a.at[5]) bad("positions and table go together");
     const void *positions = nullptr;
     const float *table = nullptr;
@@ -359,7 +368,7 @@ PyObject *kv_write(PyObject *, PyObject *const *args, Py_ssize_t n, PyObject *kw
     const Stream stream(a.at[7], device.check());
     check(gar_kv_write(cache, k.data_ptr(), k.stride(0), k.stride(1), v.data_ptr(), v.stride(0), v.stride(1),
                        dtype_of(k, "k"), k.size(0), static_cast<const int64_t *>(slots.data_ptr()), positions, width, table,
-                       table_rows, rot, layout_of(a.at[6]), stream.raw),
+                       table_rows, rot, layout, stream.raw),
           "gar_kv_write");
     changed_cache(a.at[0]);
     return Py_NewRef(Py_None);
@@ -429,6 +438,8 @@ PyObject *decode_attention(PyObject *, PyObject *const *args, Py_ssize_t n, PyOb
     if (table.dim() != 2 || table.size(0) != q.size(0) || table.scalar_type() != at::kInt || !table.is_cuda() ||
         (table.stride(1) != 1 && table.size(1) > 1))
       bad("page_table must be int32 [batch, width] on the GPU with contiguous rows");
+    const int batch = narrow(q.size(0), "the batch"), width = narrow(table.size(1), "the page table's width");
+    const int window = a.at[6] ? narrow(integer(a.at[6]), "window") : 0;
     int shape[3];
     check(gar_attn_plan_shape(plan, &shape[0], &shape[1], &shape[2]), "gar_attn_plan_shape");
     if (q.size(1) != shape[0] || q.size(2) != shape[2])
@@ -471,9 +482,8 @@ PyObject *decode_attention(PyObject *, PyObject *const *args, Py_ssize_t n, PyOb
     check(gar_decode_attention(plan, cache, q.data_ptr(), q.stride(0), q.stride(1), dtype_of(q, "q"), out.data_ptr(),
                                out.stride(0), out.stride(1), dtype_of(out, "out"),
                                wanted ? static_cast<float *>(lse.data_ptr()) : nullptr,
-                               static_cast<const int32_t *>(table.data_ptr()), table.stride(0), (int)table.size(1),
-                               static_cast<const int32_t *>(lengths.data_ptr()), (int)q.size(0), (float)scale,
-                               a.at[6] ? (int)integer(a.at[6]) : 0, stream.raw),
+                               static_cast<const int32_t *>(table.data_ptr()), table.stride(0), width,
+                               static_cast<const int32_t *>(lengths.data_ptr()), batch, (float)scale, window, stream.raw),
           "gar_decode_attention");
     if (a.at[7]) changed(out);
     if (given) changed(lse);

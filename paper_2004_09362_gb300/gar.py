@@ -492,12 +492,21 @@ def _empty(shape, dtype, device, stream):
         return torch.empty(shape, dtype=dtype, device=device)
 
 
+def _narrow(v, what: str) -> int:
+    """A number that the C entry points take as an int."""
+    v = int(v)
+    if not -2 ** 31 <= v < 2 ** 31:
+        raise ValueError(f"{what} is out of range: {v}")
+    return v
+
+
 def gar_rope_frequencies(rot: int, base: float = 10000.0, scaling="plain", factor: float = 1.0,
                          original: float = 1.0):
     """(rot/2 frequencies in radians per position, magnitude of the rotation)."""
-    f = (ctypes.c_double * max(1, min(int(rot), GAR_MAX_HEAD_DIM) // 2))()
+    rot = _narrow(rot, "rot")
+    f = (ctypes.c_double * max(1, min(rot, GAR_MAX_HEAD_DIM) // 2))()
     m = ctypes.c_double()
-    _check(_lib.gar_rope_frequencies(int(rot), float(base), _code(scaling, ROPE_SCALINGS, "scaling"),
+    _check(_lib.gar_rope_frequencies(rot, float(base), _narrow(_code(scaling, ROPE_SCALINGS, "scaling"), "scaling"),
                                      float(factor), float(original), f, ctypes.byref(m)),
            "gar_rope_frequencies")
     return list(f), m.value
@@ -543,6 +552,8 @@ class KVCache:
         shape, stride = k.shape, k.stride()
         if len(shape) != 4 or shape != v.shape or k.dtype != v.dtype or stride != v.stride():
             raise ValueError("k and v must be [pages, heads, page_size, dim], alike in shape, dtype and strides")
+        for n, what in zip(shape[1:], ("heads", "page_size", "dim")):
+            _narrow(n, what)
         if stride[3] != 1 and shape[3] > 1:
             raise ValueError("the channels of a head must be contiguous")
         dtype = _dtype_of(k, "cache")
@@ -607,9 +618,9 @@ class AttnPlan:
 
 def gar_attn_plan_create(q_heads: int, kv_heads: int, dim: int) -> AttnPlan:
     h = ctypes.c_void_p()
-    _check(_lib.gar_attn_plan_create(ctypes.byref(h), int(q_heads), int(kv_heads), int(dim)),
-           "gar_attn_plan_create")
-    return AttnPlan(h.value, int(q_heads), int(kv_heads), int(dim))
+    q_heads, kv_heads, dim = _narrow(q_heads, "q_heads"), _narrow(kv_heads, "kv_heads"), _narrow(dim, "dim")
+    _check(_lib.gar_attn_plan_create(ctypes.byref(h), q_heads, kv_heads, dim), "gar_attn_plan_create")
+    return AttnPlan(h.value, q_heads, kv_heads, dim)
 
 
 def gar_attn_plan_destroy(plan: AttnPlan) -> None:

@@ -396,3 +396,25 @@ def test_more_items_than_the_line_has_room_for_are_refused():
             assert call(batch, width) == -1, (batch, width)
     assert call(8000, 2 ** 31 - 1) == -6 and call(9000, 2 ** 31 - 1) == -1      # 2^31 / 2^15 units of each sequence
     assert call(22369621, 0, 64) == -6 and call(22369622, 0, 64) == -1          # 8 groups of query heads
+
+
+def test_numbers_past_an_int_are_refused():
+    """They were cut to 32 bits: a window of 2^32 + 5 rows was one of 5."""
+    i64, i32, f32 = torch.int64, torch.int32, torch.float32
+    x, pos, table, cache = _fake((4, 2, 64)), _fake(4, i64), _fake((8, 32, 2), f32), _fake_cache(0)
+    plan, pages, lens = gar.gar_attn_plan_create(2, 2, 64), _fake((4, 2), i32), _fake(4, i32)
+    many = (1 << 32) + 2
+    for call in (lambda: gar.gar_rope(x, pos, table, 1 << 32), lambda: gar.gar_rope(x, pos, table, -(1 << 32) + 1),
+                 lambda: gar.gar_kv_write(cache, x, x, pos, pos, table, 1 << 32),
+                 lambda: gar.gar_rope(_fake((4, many, 64)), pos, table), lambda: gar.gar_kv_write(cache, *[_fake((4, many, 64))] * 2, pos),
+                 lambda: gar.gar_kv_write(cache, *[_fake((4, 2, many + 62))] * 2, pos),
+                 lambda: gar.gar_decode_attention(plan, x, cache, pages, lens, window=(1 << 32) + 5),
+                 lambda: gar.gar_decode_attention(plan, x, cache, pages, lens, window=-(1 << 32) + 5),
+                 lambda: gar.gar_decode_attention(plan, x, cache, _fake((4, many), i32), lens),
+                 lambda: gar.gar_decode_attention(plan, _fake((many, 2, 64)), cache, _fake((many, 2), i32), _fake(many, i32)),
+                 lambda: gar.gar_attn_plan_create(many, 1, 64), lambda: gar.gar_attn_plan_create(2, many, 64),
+                 lambda: gar.gar_attn_plan_create(2, 2, many), lambda: gar.gar_rope_frequencies(many + 62),
+                 lambda: gar.gar_rope_frequencies(64, scaling=1 << 32), lambda: gar.KVCache(*[_fake((1, many, 1, 4))] * 2),
+                 lambda: gar.KVCache(*[_fake((1, 1, many, 4))] * 2), lambda: gar.KVCache(*[_fake((1, 1, 1, many))] * 2)):
+        with pytest.raises(ValueError, match="out of range"):
+            call()
