@@ -100,8 +100,31 @@ const Names &names_of() {
   return n;
 }
 
-// An address that a Python object keeps as an integer.
+// The Python classes that keep the C objects.
+PyObject *class_of(const char *name) {
+  PyObject *m = PyImport_ImportModule("paper_2004_09362_gb300.gar");
+  PyObject *c = m ? PyObject_GetAttrString(m, name) : nullptr;
+  Py_XDECREF(m);
+  if (!c) throw python_error();
+  if (!PyType_Check(c)) bad(std::string(name) + " is no class");
+  return c;
+}
+template <typename T> PyTypeObject *owner();
+template <> PyTypeObject *owner<gar_kv_cache>() {
+  static PyObject *const c = class_of("KVCache");
+  return reinterpret_cast<PyTypeObject *>(c);
+}
+template <> PyTypeObject *owner<gar_attn_plan>() {
+  static PyObject *const c = class_of("AttnPlan");
+  return reinterpret_cast<PyTypeObject *>(c);
+}
+
+// The C object of a Python object of its class.
 template <typename T> T *handle(PyObject *o, const char *what) {
+  if (!PyObject_TypeCheck(o, owner<T>())) {
+    PyErr_Format(PyExc_TypeError, "needs a %s, not a %s", owner<T>()->tp_name, Py_TYPE(o)->tp_name);
+    throw python_error();
+  }
   PyObject *v = PyObject_GetAttr(o, names_of().address);
   if (!v) throw python_error();
   void *p = PyLong_AsVoidPtr(v);

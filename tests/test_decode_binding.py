@@ -418,3 +418,26 @@ def test_numbers_past_an_int_are_refused():
                  lambda: gar.KVCache(*[_fake((1, 1, many, 4))] * 2), lambda: gar.KVCache(*[_fake((1, 1, 1, many))] * 2)):
         with pytest.raises(ValueError, match="out of range"):
             call()
+
+
+def test_objects_of_another_class_are_refused():
+    """A plan where the cache belongs, and the other way round, has an address too: of something else."""
+    i64, i32 = torch.int64, torch.int32
+    x, slots, pages, lens = _fake((4, 2, 64)), _fake(4, i64), _fake((4, 2), i32), _fake(4, i32)
+    cache, plan = _fake_cache(0), gar.gar_attn_plan_create(2, 2, 64)
+
+    class Own(gar.KVCache):
+        pass
+
+    other = types.SimpleNamespace(address=cache.address, device_index=0, stream=None)
+    for wrong in (plan, other, 5, "cache"):
+        for call in (lambda: gar.gar_kv_write(wrong, x, x, slots), lambda: gar.gar_kv_read(wrong, slots),
+                     lambda: gar.gar_decode_attention(plan, x, wrong, pages, lens)):
+            with pytest.raises(TypeError, match="KVCache"):
+                call()
+    for wrong in (cache, other, 5):
+        with pytest.raises(TypeError, match="AttnPlan"):
+            gar.gar_decode_attention(wrong, x, cache, pages, lens)
+    cache.__class__ = Own                   # a class of the caller's own made from it is one
+    with pytest.raises(ValueError, match="alike"):
+        gar.gar_kv_write(cache, x, x[:1], slots)
