@@ -5,7 +5,8 @@ Usage: python -m paper_2004_09362_gb300.build   (or via __graft_entry__.build())
 Each translation unit compiles in parallel into _build/, then one link step writes
 paper_2004_09362_gb300/libgar.so.  Rebuilds only when a source is newer than the
 library.  The Python calls of the decoding operators (csrc/marshal.cpp) become
-paper_2004_09362_gb300/_marshal.so, linked to it and to torch.  The generated fused/batched kernels are compiled later, at plan time, by
+paper_2004_09362_gb300/_marshal.so, linked to it and to torch, and built again when torch or Python is another
+one; without torch it is left out.  The generated fused/batched kernels are compiled later, at plan time, by
 NVRTC inside the library.
 """
 
@@ -53,31 +54,59 @@ def _cuda_lib_dir(nvcc: str) -> str:
     return os.path.join(root, "lib64")
 
 
-def _stale() -> bool:
-    if not os.path.exists(OUT) or not os.path.exists(MARSHAL):
+def _older(target: str, sources) -> bool:
+    if not os.path.exists(target):
         return True
-    t = min(os.path.getmtime(OUT), os.path.getmtime(MARSHAL))
-    deps = [os.path.join(CSRC, f) for f in SOURCES + HEADERS + ["marshal.cpp"]]
-    deps += [os.path.join(INCLUDE, "gar.h"), os.path.abspath(__file__)]
-    return any(os.path.getmtime(d) > t for d in deps)
+    t = os.path.getmtime(target)
+    return any(os.path.getmtime(d) > t for d in [*sources, os.path.join(INCLUDE, "gar.h"), os.path.abspath(__file__)])
+
+
+def _library_stale() -> bool:
+    return _older(OUT, [os.path.join(CSRC, f) for f in SOURCES + HEADERS])
+
+
+def _torch_dir() -> str | None:
+    spec = importlib.util.find_spec("torch")
+    return list(spec.submodule_search_locations)[0] if spec else None
+
+
+def _made_for() -> str:
+    """What _marshal.so is compiled against beside its sources: this Python and this torch."""
+    with open(os.path.join(_torch_dir(), "version.py")) as f:
+        return "\n".join([sys.version, _torch_dir(), f.read()])
+
+
+def _marshal_stale() -> bool:
+    stamp = os.path.join(BUILD, "marshal.for")
+    if _older(MARSHAL, [os.path.join(CSRC, "marshal.cpp")]) or not os.path.exists(stamp):
+        return True
+    with open(stamp) as f:
+        return f.read() != _made_for()
 
 
 def build(force: bool = False, verbose: bool = False) -> str:
-    """Builds libgar.so when a source is newer than it (or always with force).  Holds a
-    file lock, so concurrent callers (test workers) build once."""
+    """Builds libgar.so, and where there is torch _marshal.so, when a source is newer than it (or always with
+    force).  The library comes first: a failure of the other leaves it built.  Holds a file lock, so
+    concurrent callers (test workers) build once."""
     import fcntl
     os.makedirs(BUILD, exist_ok=True)
     with open(os.path.join(BUILD, ".lock"), "w") as lock:
         fcntl.flock(lock, fcntl.LOCK_EX)
-        if not force and not _stale():
-            return OUT
-        return _build(verbose)
+        library = force or _library_stale()
+        marshal = _torch_dir() is not None and (force or _marshal_stale())
+        if library or marshal:
+            with cf.ThreadPoolExecutor(max_workers=len(SOURCES) + 1) as ex:
+                obj = ex.submit(_compile_marshal) if marshal else None
+                if library:
+                    _build_library(ex, verbose)
+                if marshal:
+                    _link_marshal(obj.result())
+        return OUT
 
 
-def _build(verbose: bool) -> str:
+def _build_library(ex, verbose: bool) -> None:
     nvcc = _nvcc()
     libdir = _cuda_lib_dir(nvcc)
-    os.makedirs(BUILD, exist_ok=True)
     common = ["-O3", "-std=c++17", "-lineinfo", "-Xcompiler", "-fPIC", "-I", INCLUDE,
               "-Xcompiler", "-fvisibility=hidden"]
 
@@ -86,50 +115,47 @@ def _build(verbose: bool) -> str:
         cmd = [nvcc, *ARCH, *common, "-c", os.path.join(CSRC, src), "-o", obj]
         if src.endswith(".cu"):
             cmd += ["-Xptxas", "-warn-spills"]
-        r = subprocess.run(cmd, capture_output=True, text=True)
-        if r.returncode != 0:
-            raise RuntimeError(f"nvcc failed for {src}:\n{r.stdout}\n{r.stderr}")
+        r = _run(cmd, f"nvcc failed for {src}")
         if verbose and (r.stdout or r.stderr):
             print(r.stdout, r.stderr, file=sys.stderr)
         return obj
 
-    def compile_marshal() -> str:
-        obj = os.path.join(BUILD, "marshal.o")
-        inc = os.path.join(_torch_dir(), "include")
-        cuda = os.path.join(os.path.dirname(os.path.dirname(os.path.realpath(nvcc))), "include")
-        _run(["g++", "-O2", "-std=c++17", "-fPIC", "-fvisibility=hidden", "-I", inc, "-I",
-              os.path.join(inc, "torch", "csrc", "api", "include"), "-I", sysconfig.get_paths()["include"],
-              "-I", cuda, "-I", "/usr/local/cuda/include", "-c", os.path.join(CSRC, "marshal.cpp"), "-o", obj],
-             "g++ failed for marshal.cpp")
-        return obj
-
-    with cf.ThreadPoolExecutor(max_workers=len(SOURCES) + 1) as ex:
-        marshal = ex.submit(compile_marshal)
-        objs = list(ex.map(compile_one, SOURCES))
-        marshal_obj = marshal.result()
+    objs = list(ex.map(compile_one, SOURCES))
     tmp = OUT + f".tmp{os.getpid()}"
-    cmd = [nvcc, *ARCH, "-shared", "-o", tmp, *objs, "-L", libdir, "-lnvrtc",
-           "-Xlinker", "-rpath", "-Xlinker", libdir]
-    r = subprocess.run(cmd, capture_output=True, text=True)
-    if r.returncode != 0:
-        raise RuntimeError(f"link failed:\n{r.stdout}\n{r.stderr}")
+    _run([nvcc, *ARCH, "-shared", "-o", tmp, *objs, "-L", libdir, "-lnvrtc",
+          "-Xlinker", "-rpath", "-Xlinker", libdir], "link failed")
     os.replace(tmp, OUT)
+
+
+def _compile_marshal() -> str:
+    obj = os.path.join(BUILD, "marshal.o")
+    inc = os.path.join(_torch_dir(), "include")
+    cuda = os.path.join(os.path.dirname(os.path.dirname(os.path.realpath(_nvcc()))), "include")
+    _run(["g++", "-O2", "-std=c++17", "-fPIC", "-fvisibility=hidden", "-I", inc, "-I",
+          os.path.join(inc, "torch", "csrc", "api", "include"), "-I", sysconfig.get_paths()["include"],
+          "-I", cuda, "-I", "/usr/local/cuda/include", "-c", os.path.join(CSRC, "marshal.cpp"), "-o", obj],
+         "g++ failed for marshal.cpp")
+    return obj
+
+
+def _link_marshal(obj: str) -> None:
     lib = os.path.join(_torch_dir(), "lib")
     tmp = MARSHAL + f".tmp{os.getpid()}"
-    _run(["g++", "-shared", "-o", tmp, marshal_obj, "-L", PKG, "-lgar", "-L", lib, "-ltorch_python", "-ltorch_cpu",
+    _run(["g++", "-shared", "-o", tmp, obj, "-L", PKG, "-lgar", "-L", lib, "-ltorch_python", "-ltorch_cpu",
           "-ltorch_cuda", "-lc10", "-lc10_cuda", "-Wl,-rpath,$ORIGIN", "-Wl,-rpath," + lib], "link of _marshal.so failed")
     os.replace(tmp, MARSHAL)
-    return OUT
+    with open(os.path.join(BUILD, "marshal.for"), "w") as f:
+        f.write(_made_for())
 
 
-def _torch_dir() -> str:
-    return list(importlib.util.find_spec("torch").submodule_search_locations)[0]
-
-
-def _run(cmd, what: str) -> None:
-    r = subprocess.run(cmd, capture_output=True, text=True)
+def _run(cmd, what: str):
+    try:
+        r = subprocess.run(cmd, capture_output=True, text=True)
+    except FileNotFoundError as e:
+        raise RuntimeError(f"{what}: {e}") from e
     if r.returncode != 0:
         raise RuntimeError(f"{what}:\n{r.stdout}\n{r.stderr}")
+    return r
 
 
 if __name__ == "__main__":

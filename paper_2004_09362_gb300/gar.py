@@ -674,6 +674,8 @@ def __getattr__(name):
     compiled (csrc/marshal.cpp) and loaded on first use, with torch."""
     if name in ("gar_rope", "gar_kv_write", "gar_kv_read", "gar_decode_attention"):
         import torch  # noqa: F401  (its libraries are the module's)
+        if not os.path.exists(os.path.join(_HERE, "_marshal.so")):
+            raise ImportError("_marshal.so not built; run __graft_entry__.build() where torch is installed")
         from . import _marshal
         globals()[name] = getattr(_marshal, name)
         return globals()[name]
