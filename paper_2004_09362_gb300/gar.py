@@ -37,7 +37,6 @@ DTYPES = {"f32": GAR_F32, "bf16": GAR_BF16, "i32": GAR_I32}
 OPS = {"sum": GAR_SUM, "max": GAR_MAX, "min": GAR_MIN}
 MODES = {"step": GAR_STEP_FAITHFUL, "step_faithful": GAR_STEP_FAITHFUL, "fused": GAR_FUSED,
          "persistent": GAR_STEP_PERSISTENT}
-ROPE_LAYOUTS = {"half": GAR_ROPE_HALF, "interleaved": GAR_ROPE_INTERLEAVED}
 ROPE_SCALINGS = {"plain": GAR_ROPE_PLAIN, "linear": GAR_ROPE_LINEAR, "base": GAR_ROPE_BASE,
                  "parts": GAR_ROPE_PARTS}
 ELEM_SIZE = {GAR_F32: 4, GAR_BF16: 2, GAR_I32: 4}

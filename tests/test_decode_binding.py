@@ -441,3 +441,14 @@ def test_objects_of_another_class_are_refused():
     cache.__class__ = Own                   # a class of the caller's own made from it is one
     with pytest.raises(ValueError, match="alike"):
         gar.gar_kv_write(cache, x, x[:1], slots)
+
+
+def test_names_of_layouts_are_the_headers():
+    """The compiled calls know them alone; their codes are the header's."""
+    x, pos, table = _fake((4, 2, 64)), _fake(4, torch.int64), _fake((8, 32, 2), torch.float32, 1)
+    for layout in ("half", "interleaved", gar.GAR_ROPE_HALF, gar.GAR_ROPE_INTERLEAVED):
+        with pytest.raises(ValueError, match="GPU 1"):
+            gar.gar_rope(x, pos, table, layout)
+    with pytest.raises(ValueError, match="layout"):
+        gar.gar_rope(x, pos, _fake((8, 32, 2), torch.float32), "third")
+    assert not hasattr(gar, "ROPE_LAYOUTS")
