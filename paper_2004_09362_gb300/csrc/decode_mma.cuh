@@ -28,8 +28,9 @@
 //    tiles (DecodeArgs::solo) goes to one warp whole, so that short sequences need no barrier.
 //
 // Measured: 1 x 262143 rows, 64/8 x 128 bf16 156 us (6.9 TB/s, what a copy reaches); 64 x 8192, 32/8 x 128 bf16 165 us
-// (6.5 TB/s); 127 x 8192, 32/8 x 128 e4m3 204 us (5.3 TB/s: its
-// warps wait for their own instructions, the expansion of the codes among them, as long as for copies); 16 x 8192, 8/8 x 128 f32 99 us (5.0 TB/s).  1 x 425, 32/8 x 128 bf16 9 us, which is the launch, the lengths, the
+// (6.5 TB/s); 127 x 8192, 32/8 x 128 e4m3 205 us (5.3 TB/s: its
+// warps wait for their own instructions, the expansion of the codes among them, as long as for copies), i8 223, with 32-bit queries
+// 235 and 255; 16 x 8192, 8/8 x 128 f32 99 us (5.0 TB/s).  1 x 425, 32/8 x 128 bf16 9 us, which is the launch, the lengths, the
 // pages, the rows, the join of a CTA and that of the item one after the other, each a round trip to memory or more.
 //
 // 8-bit codes become f16, exactly; a row's key scale multiplies its scores, its value scale
@@ -833,8 +834,9 @@ template <typename C, int DP, int NG, bool Q32> int launch_mma(DecodeArgs a, int
 
 template <typename C, bool Q32> int decode_mma(const DecodeArgs &a, int sms, gar_stream_t stream) {
   // Sixteen heads at a time where there are more than eight (a row is read once for all; 256 channels' outputs do not fit the
-  // registers).  64 x 16384, 64/4 x 128: bf16 200 us and 316 with eight at a time, i8 174 and 220, f32 567 and 775.
-  // 1 x 60000, 16/1 x 128 bf16 is 35 and 22: more to join in one CTA.
+  // registers).  64 x 16384, 64/4 x 128: bf16 202 us and 321 with eight at a time, i8 179 and 217, f32 573 and 761; 64 x 2000 bf16
+  // 54 and 57, 8 x 60000, 16/1 x 128 39 and 38.  The slower of the two for one long sequence, 1 x 60000 36 and 22, 1 x 262143 55 and 42:
+  // more to join in one CTA.
   const bool two = a.group > 8;
   // The channels that a tile is made for: a size more costs the copies' zeros, the products and the room of the tiles.  96
   // and 192 were worth (16 x 8192, 16/4 heads, in place of 128 and 256): 80 f32 42 us, 57; 96 bf16 25 and 26; 192 f32 92 and
