@@ -283,6 +283,13 @@ __device__ __forceinline__ float exp2_fast(float x) {
   return y;
 }
 
+// x 2^d.  FAR: also where 2^d alone vanishes (d under -126) and x is as much larger than 1.
+template <bool FAR> __device__ __forceinline__ float scaled(float x, float d) {
+  if (!FAR) return x * exp2_fast(d);
+  const float near = fmaxf(d, -100.f);
+  return x * exp2_fast(near) * exp2_fast(d - near);
+}
+
 // m as an exponent's offset: nothing seen yet (-infinity) leaves 2^-infinity = 0 rather than NaN.
 __device__ __forceinline__ float offset_of(float m) { return m == -INFINITY ? 0.f : m; }
 
@@ -354,8 +361,8 @@ struct Group {
 
 // Joins the (m, l, o) of a group's warps and writes the item's output, or the segment's partial
 // result.  Warp w holds head h's o at o[at[w] + h * row], 16-byte aligned.
-// With TWIST its channel d is at d ^ (h & 6).
-template <int WARPS, bool TWIST = false>
+// With TWIST its channel d is at d ^ (h & 6); with FAR l may be far from 1 (8-bit caches).
+template <int WARPS, bool TWIST = false, bool FAR = false>
 __device__ __forceinline__ void join_warps(const DecodeArgs &a, const Segment &g, Group group, JoinShared<WARPS> &sh,
                                            const float *o, int row) {
   static_assert(WARPS <= 16, "16 lanes hold a head's warps");
@@ -368,7 +375,7 @@ __device__ __forceinline__ void join_warps(const DecodeArgs &a, const Segment &g
 #pragma unroll
     for (int d = 8; d > 0; d /= 2) m = fmaxf(m, __shfl_xor_sync(~0u, m, d));
     const float f = exp2_fast(v.x - offset_of(m));
-    float l = f * v.y;
+    float l = FAR ? scaled<FAR>(v.y, v.x - offset_of(m)) : f * v.y;
 #pragma unroll
     for (int d = 8; d > 0; d /= 2) l += __shfl_xor_sync(~0u, l, d);
     if (h < g.heads) {
@@ -405,7 +412,7 @@ __device__ __forceinline__ void join_warps(const DecodeArgs &a, const Segment &g
 // After join_warps: where the item has several parts, the last group to get here joins them, 8 parts' loads in flight a
 // thread (a long sequence alone has some 20 parts of 4 KB for each cached head; 16 at once cost the kernel registers:
 // 1 x 425 rows, 32/8 heads x 128 bf16 10.1 us in place of 8.9, 127 x 8192 e4m3 213 in place of 205).
-template <int WARPS>
+template <int WARPS, bool FAR = false>
 __device__ __forceinline__ void join_parts(const DecodeArgs &a, const Segment &g, Group group, JoinShared<WARPS> &sh) {
   if (group.thread() == 0) {
     // After join_warps' barrier: what the group has stored is seen before the count, and what others have stored after it.
@@ -435,13 +442,13 @@ __device__ __forceinline__ void join_parts(const DecodeArgs &a, const Segment &g
 #pragma unroll
         for (int k = 0; k < N; ++k) top = fmaxf(top, v[k].x);
         const float off = offset_of(top), shrink = exp2_fast(m - off);
-        m = top, l *= shrink;
+        l = FAR ? scaled<FAR>(l, m - off) : l * shrink, m = top;
         x.x *= shrink, x.y *= shrink, x.z *= shrink, x.w *= shrink;
 #pragma unroll
         for (int k = 0; k < N; ++k)
           if (p0 + k < g.parts) {
             const float f = exp2_fast(v[k].x - off);
-            l += f * v[k].y;
+            l += FAR ? scaled<FAR>(v[k].y, v[k].x - off) : f * v[k].y;
             x.x += f * y[k].x, x.y += f * y[k].y, x.z += f * y[k].z, x.w += f * y[k].w;
           }
       }

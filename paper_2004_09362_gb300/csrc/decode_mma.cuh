@@ -28,9 +28,9 @@
 //    tiles (DecodeArgs::solo) goes to one warp whole, so that short sequences need no barrier.
 //
 // Measured: 1 x 262143 rows, 64/8 x 128 bf16 156 us (6.9 TB/s, what a copy reaches); 64 x 8192, 32/8 x 128 bf16 165 us
-// (6.5 TB/s); 127 x 8192, 32/8 x 128 e4m3 205 us (5.3 TB/s: its
-// warps wait for their own instructions, the expansion of the codes among them, as long as for copies), i8 223, with 32-bit queries
-// 235 and 255; 16 x 8192, 8/8 x 128 f32 99 us (5.0 TB/s).  1 x 425, 32/8 x 128 bf16 9 us, which is the launch, the lengths, the
+// (6.5 TB/s); 127 x 8192, 32/8 x 128 e4m3 206 us (5.3 TB/s: its
+// warps wait for their own instructions, the expansion of the codes among them, as long as for copies), i8 229, with 32-bit queries
+// 233 and 250; 16 x 8192, 8/8 x 128 f32 99 us (5.0 TB/s).  1 x 425, 32/8 x 128 bf16 9 us, which is the launch, the lengths, the
 // pages, the rows, the join of a CTA and that of the item one after the other, each a round trip to memory or more.
 //
 // 8-bit codes become f16, exactly; a row's key scale multiplies its scores, its value scale
@@ -211,7 +211,8 @@ template <typename C, int DP, int NG> struct MmaShape {
 };
 
 // log2 of a value scale, near enough for a reference.  Within [-96, 120], whatever the scale (zero, an infinity, NaN), so that the
-// sum l of 2^(score - m) stays finite and does not vanish.
+// sum l of 2^(score - m) stays finite and does not vanish.  (Next to a scale of 2^s weights under 2^(s - 126) of the largest count
+// nothing.)
 __device__ __forceinline__ float scale_log2(float x) {
   float y;
   asm("lg2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(fabsf(x)));
@@ -645,9 +646,11 @@ __global__ void __launch_bounds__(32 * MmaShape<C, DP, NG>::kWarps, 1)
       for (int ng = 0; ng < NG; ++ng)
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
-          shrink[ng][h] = grown ? exp2_fast(m[ng][h] - offset_of(top[ng][h])) : 1.f;
+          // (rows with values of zero, say, at 2^-96: l may be 2^96 and the next reference larger by 2^96 and more)
+          const float d = m[ng][h] - offset_of(top[ng][h]);
+          shrink[ng][h] = grown ? exp2_fast(d) : 1.f;
+          l[ng][h] = !Q8 ? l[ng][h] * shrink[ng][h] : grown ? scaled<Q8>(l[ng][h], d) : l[ng][h];
           m[ng][h] = top[ng][h];
-          l[ng][h] *= shrink[ng][h];
         }
       // Weights, in the layout of the second product's right operand.
       uint32_t hi[SUBS][NG][F32 ? 4 : 2], low[SUBS][NG][F32 ? 4 : 2];
@@ -797,8 +800,8 @@ __global__ void __launch_bounds__(32 * MmaShape<C, DP, NG>::kWarps, 1)
     mine_mask &= ~(1u << using_note), copied_mask &= ~(1u << using_note);
     pump(S::kStages - 1);
     have = take();
-    join_warps<W, true>(a, ended, by, join, o_all, S::kRow);
-    if (!ended.whole) join_parts(a, ended, by, join);
+    join_warps<W, true, Q8>(a, ended, by, join, o_all, S::kRow);
+    if (!ended.whole) join_parts<W, Q8>(a, ended, by, join);
   }
 }
 

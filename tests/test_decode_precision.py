@@ -189,3 +189,28 @@ def test_products_of_32_bit_caches(dim, heads, n):
     assert bool(((out[0].double() - p @ values).abs() <= tol).all())
     want = torch.logsumexp(y, -1)
     assert bool(((lse[0].double() - want).abs() <= e + 2.0 ** -22 + n * U32 + 2.0 ** -22 * want.abs()).all())
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("kind", [torch.int8, torch.float8_e4m3fn])
+@pytest.mark.parametrize("low,high", [(0.0, 1.0), (0.0, 1e12), (1e-35, 1e10), (0.0, 1e30), (1e-30, 1e30)])
+@pytest.mark.parametrize("n", [40, 100, 700, 20000])
+@pytest.mark.parametrize("large_last", [True, False])
+def test_value_scales_far_apart_with_equal_weights(kind, low, high, n, large_last):
+    """Rows of values of zero, or next to it, weigh as much as rows of large ones, whichever come first: across tiles, warps and
+    CTAs."""
+    dim, heads = 64, 3
+    codes = torch.full((n, dim), 100.0, device="cuda")
+    large = torch.arange(n, device="cuda") * 4 >= 3 * n
+    if not large_last:
+        large = large.flip(0)
+    v_scale = torch.where(large, high, low).float()
+    cache, table, k, v = _cached(kind, torch.zeros(n, dim, device="cuda"), torch.ones(n, device="cuda"), codes, v_scale, 16)
+    q = torch.ones(1, heads, dim, device="cuda")
+    plan = gar.gar_attn_plan_create(heads, 1, dim)
+    out, lse = gar.gar_decode_attention(plan, q, cache, table, torch.tensor([n], dtype=torch.int32, device="cuda"), lse=True)
+    # weights are all alike: each 2^x by 2^-22, its difference to the reference (of up to 220) rounded, two parts by 2^-22; sums by n u
+    tol = 2.0 ** -22 + 220 * U32 + 2.0 ** -22 + 2 * n * U32
+    assert bool(((lse.double() - math.log(n)).abs() <= tol + 2.0 ** -21 * math.log(n)).all())
+    want = v.mean(0)
+    assert bool(((out[0].double() - want).abs() <= 2 * tol * want).all())
