@@ -488,6 +488,11 @@ GAR_API int gar_attn_plan_bytes(const gar_attn_plan *plan, size_t *workspace_byt
  * each stream. */
 GAR_API int gar_attn_plan_set_workspace(gar_attn_plan *plan, void *dev_ptr, size_t bytes);
 
+/* The waits for copies of gar_decode_attention (rows of 512 bytes and more; no counterpart in the paper): each is
+ * bounded, some 0.1 s; one that runs out sets GAR_KV_TIMEOUT, and its warp leaves out the rest of its rows.  tile >= 0: waits
+ * for a segment's tiles from that one on report that they ran out, which tests that path; negative: none do. */
+GAR_API int gar_attn_plan_debug_wait(gar_attn_plan *plan, int tile);
+
 /* For each sequence b and query head h, over the cached rows n in [lengths[b] - window,
  * lengths[b]) (all below lengths[b] when window is 0):
  *   out = sum_n softmax_n(scale q.k_n) v_n,   lse = ln sum_n exp(scale q.k_n).

@@ -53,6 +53,7 @@ struct DecodeArgs {
   unsigned int *count;
   int dim_pad;             // floats of a stored o row
   int device;              // the launch's
+  int give_up;             // a segment's tiles from this one on count as copies that did not end
 };
 
 // x / d; a division in 32-bit floats, put right, where they hold x (the compiler's takes three times as long).

@@ -1,5 +1,6 @@
 // Decode attention: plans, workspaces, checks of arguments, choice of the kernel.
 #include <algorithm>
+#include <climits>
 #include <cmath>
 #include <new>
 
@@ -8,6 +9,7 @@
 struct gar_attn_plan {
   int q_heads, kv_heads, dim;
   int device = -1, sms = 0;
+  int give_up = INT_MAX;
   void *ws = nullptr;
 };
 
@@ -121,6 +123,12 @@ int gar_attn_plan_set_workspace(gar_attn_plan *plan, void *dev_ptr, size_t bytes
   return GAR_OK;
 }
 
+int gar_attn_plan_debug_wait(gar_attn_plan *plan, int tile) {
+  if (plan == nullptr) return refuse("null plan");
+  plan->give_up = tile < 0 ? INT_MAX : tile;
+  return GAR_OK;
+}
+
 int gar_decode_attention(gar_attn_plan *plan, const gar_kv_cache *cache, const void *q, int64_t q_batch_stride,
                          int64_t q_head_stride, int q_dtype, void *out, int64_t out_batch_stride,
                          int64_t out_head_stride, int out_dtype, float *lse, const int32_t *page_table,
@@ -171,7 +179,7 @@ int gar_decode_attention(gar_attn_plan *plan, const gar_kv_cache *cache, const v
   a.count = reinterpret_cast<unsigned *>(ws);
   a.part_ml = reinterpret_cast<float2 *>(ws + kCounterBytes);
   a.part_o = reinterpret_cast<float *>(a.part_ml + (size_t)kMaxCtas * 2 * kMaxGroup);
-  a.dim_pad = dim_pad(plan->dim), a.device = dev;
+  a.dim_pad = dim_pad(plan->dim), a.device = dev, a.give_up = plan->give_up;
   a.out_wide = (uintptr_t)out % (4 * element_size(out_dtype)) == 0 && plan->dim % 4 == 0 && out_batch_stride % 4 == 0 &&
                out_head_stride % 4 == 0;
   a.unit = unit;

@@ -333,8 +333,9 @@ __global__ void __launch_bounds__(32 * MmaShape<C, DP, NG>::kWarps, 1)
     }
     return x;
   };
+  bool late = false;                     // boxes: a wait ran out; nothing is copied any more, and the rest left out
   const auto advance = [&] {
-    while (get.tile >= get.tiles) {
+    while (get.tile >= get.tiles || (BOXES && late)) {
       uint32_t left = mine_mask & ~copied_mask;
       if (left == 0) {
         // The half to be filled next must be done with.
@@ -411,7 +412,7 @@ __global__ void __launch_bounds__(32 * MmaShape<C, DP, NG>::kWarps, 1)
   int in = 0, out = 0, flying = 0;  // stages copied into and used next; tiles on their way or here
   uint32_t parity = 0;
   const auto pump = [&](int most) {
-    while (flying < most) {
+    while (flying < most && !(BOXES && late)) {
       if (!ready) advance();
       if (!ready) break;
       issue(in);
@@ -517,7 +518,11 @@ __global__ void __launch_bounds__(32 * MmaShape<C, DP, NG>::kWarps, 1)
 
     for (; tile < tiles; tile += step) {
       if (BOXES) {
-        if (!wait_barrier(barrier + 8 * out, parity) && c.status) atomicOr(c.status, GAR_KV_TIMEOUT);
+        late = __any_sync(~0u, late || tile >= a.give_up || !wait_barrier(barrier + 8 * out, parity));
+        if (late) {
+          if (c.status) atomicOr(c.status, GAR_KV_TIMEOUT);
+          break;
+        }
       } else {
         if (flying == S::kStages - 1)
           asm volatile("cp.async.wait_group %0;" ::"n"(S::kStages - 2) : "memory");
@@ -803,6 +808,9 @@ __global__ void __launch_bounds__(32 * MmaShape<C, DP, NG>::kWarps, 1)
     join_warps<W, true, Q8>(a, ended, by, join, o_all, S::kRow);
     if (!ended.whole) join_parts<W, Q8>(a, ended, by, join);
   }
+  if (BOXES && late)                     // what is on its way lands before the CTA's memory is another's
+    for (int i = out; i < out + flying; ++i)
+      wait_barrier(barrier + 8 * (i < S::kStages ? i : i - S::kStages), i < S::kStages ? parity : parity ^ 1);
 }
 
 // A map of the cache's bytes as [pages][heads][lines of a row][page_size][128], boxes of the lines of `rows` rows;

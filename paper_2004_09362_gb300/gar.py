@@ -51,7 +51,7 @@ EXPORTS = (
     "gar_cost_model", "gar_optimal_steps", "gar_plan_status", "gar_plan_debug_barrier",
     "gar_plan_create_group", "gar_rope_frequencies", "gar_rope_table", "gar_rope", "gar_kv_write",
     "gar_kv_read", "gar_kv_status", "gar_attn_plan_create", "gar_attn_plan_destroy",
-    "gar_attn_plan_shape", "gar_attn_plan_bytes", "gar_attn_plan_set_workspace", "gar_decode_attention",
+    "gar_attn_plan_shape", "gar_attn_plan_bytes", "gar_attn_plan_set_workspace", "gar_attn_plan_debug_wait", "gar_decode_attention",
 )
 
 
@@ -126,6 +126,7 @@ def _load():
         "gar_attn_plan_shape": (i32, [vp, P_(i32), P_(i32), P_(i32)]),
         "gar_attn_plan_bytes": (i32, [vp, P_(sz)]),
         "gar_attn_plan_set_workspace": (i32, [vp, vp, sz]),
+        "gar_attn_plan_debug_wait": (i32, [vp, i32]),
         "gar_decode_attention": (i32, [vp, P_(gar_kv_cache), vp, i64, i64, i32, vp, i64, i64, i32, vp, vp,
                                        i64, i32, vp, i32, f32, i32, vp]),
     }
@@ -649,6 +650,11 @@ def gar_attn_plan_set_workspace(plan: AttnPlan, ptr: int, nbytes: int) -> None:
            "gar_attn_plan_set_workspace")
     plan.workspace = (int(ptr), int(nbytes)) if ptr else None
     plan.stream = None
+
+
+def gar_attn_plan_debug_wait(plan: AttnPlan, tile: int = -1) -> None:
+    """Waits for copies of a segment's tiles from `tile` on report that they ran out (-1: none do)."""
+    _check(_lib.gar_attn_plan_debug_wait(plan.handle, _narrow(tile, "tile")), "gar_attn_plan_debug_wait")
 
 
 def _use_workspace(plan: AttnPlan, like, raw: int) -> None:
