@@ -422,7 +422,7 @@ def _plain_verify(s):
         accepted = torch.zeros(batch, dtype=torch.int64, device="cuda")
         rest = _clamped(s["target"][:, 0].double())
     total = rest.cumsum(-1)
-    u = s["uniform"][each, accepted].double()[:, None]
+    u = s["uniform"][:, -1].double()[:, None]    # a number of its own: those before it decided on the drafts
     past = total > u * total[:, -1:]
     last = torch.where(rest > 0, torch.arange(vocab, device="cuda"), -1).amax(-1)
     token = torch.where(past.any(-1), past.long().argmax(-1), last)
@@ -551,7 +551,7 @@ def _exact_verify(c, seed):
         if r is None or not bool(r.any()):
             r = s["target"][b, i].double()
         total = r.cumsum(0)
-        k = int(torch.searchsorted(total, uniform[b][i] * total[-1:], right=True)[0])
+        k = int(torch.searchsorted(total, uniform[b][-1] * total[-1:], right=True)[0])
         tokens[b, i] = k if k < c["vocab"] else int(r.nonzero().max())
         accepted[b] = i
     return {"tokens": tokens.cuda(), "accepted": accepted.cuda()}
