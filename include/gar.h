@@ -520,6 +520,81 @@ GAR_API int gar_decode_attention(gar_attn_plan *plan, const gar_kv_cache *cache,
                                  int64_t table_stride, int table_width, const int32_t *lengths,
                                  int batch, float scale, int window, gar_stream_t stream);
 
+/* ---------------------------------------------------------------------------------------
+ * Serving a batch: attention over a prefix that sequences share, what is kept of a cache of
+ * limited size, and which drafted tokens stand.  The conventions of the decoding operators
+ * hold; the paper has no counterpart. */
+
+/* Bytes of the workspace of a gar_prefix_attention call of `batch` sequences in `groups` groups.  Host-only. */
+GAR_API int gar_prefix_attention_bytes(const gar_attn_plan *plan, int batch, int groups, size_t *bytes);
+
+/* Attention of one new token per sequence, as gar_decode_attention, where the sequences b of a group
+ * g = b / (batch / groups) share the rows that come first: those of prefix_table[g], below prefix_lengths[g];
+ * they are read once for all of the group.  Then come the sequence's own, page_table[b] below
+ * lengths[b]:
+ *   out = sum_n softmax_n(scale q.k_n) v_n,   lse = ln sum_n exp(scale q.k_n)
+ * over both.  batch is a multiple of groups.  Drafted tokens are such sequences: the tokens of one context are a group,
+ * their own rows the pages that they were written to, each length one more than the one before.
+ * Pages, lengths, strides, dtypes, precision and what the status word says are as in gar_decode_attention;
+ * prefix_lengths count in [0, prefix_width * page_size].
+ * workspace: 16-byte aligned, at least gar_prefix_attention_bytes, one for each call that may run at the same time
+ * (what it held before does not matter).  The plan's own workspace is used too. */
+GAR_API int gar_prefix_attention(gar_attn_plan *plan, const gar_kv_cache *cache, const void *q, int64_t q_batch_stride,
+                                 int64_t q_head_stride, int q_dtype, void *out, int64_t out_batch_stride,
+                                 int64_t out_head_stride, int out_dtype, float *lse, const int32_t *prefix_table,
+                                 int64_t prefix_stride, int prefix_width, const int32_t *prefix_lengths, int groups,
+                                 const int32_t *page_table, int64_t table_stride, int table_width,
+                                 const int32_t *lengths, int batch, float scale, void *workspace,
+                                 size_t workspace_bytes, gar_stream_t stream);
+
+/* The attention weights that cached rows gather:
+ *   out[b][h][n] = weights[b][h][n] + sum over the queries j of cached head h of exp(scale q_j.k_n - lse[b][j])
+ * for the rows n in [lengths[b] - window, lengths[b]) (all below lengths[b] when window is 0); out = weights
+ * elsewhere.  q: [batch][q_heads][dim] of dtype GAR_BF16, GAR_F16 or GAR_F32, the cache of its type or of an 8-bit one;
+ * q_heads a multiple of the cache's heads.  lse: contiguous [batch][q_heads], as gar_decode_attention or
+ * gar_prefix_attention gives it; a head whose lse is -infinity adds nothing.  weights, out: [batch][heads][rows] of floats,
+ * rows contiguous; out may equal weights with equal strides, other overlaps are undefined.  Lengths past `rows` count as
+ * past the table.  A row on a page outside the cache counts as zeros.  Scores and sums are held in 32 bits; over 8-bit caches
+ * a channel of a query is off by 2^-22 of itself or 2^-39 of the head's largest, whichever is more. */
+GAR_API int gar_kv_weigh(const gar_kv_cache *cache, const void *q, int64_t q_batch_stride, int64_t q_head_stride, int q_dtype,
+                         int q_heads, const float *lse, const float *weights, int64_t weights_batch_stride,
+                         int64_t weights_head_stride, float *out, int64_t out_batch_stride, int64_t out_head_stride, int64_t rows,
+                         const int32_t *page_table, int64_t table_stride, int table_width, const int32_t *lengths, int batch,
+                         float scale, int window, gar_stream_t stream);
+
+/* Cuts each sequence down to its `keep` rows of most weight.  Where lengths[b] > keep, each head on its own keeps: the
+ * rows below `first`; those whose position is above the largest of its rows' positions less `recent`; then the
+ * others by their weight, the largest first (a NaN counts as less than any number); of equal ones the lower row.  Rows
+ * stay where they are as far as that goes: the i-th of the rows below `keep` that go is overwritten, keys, values
+ * and scales, by the i-th of the rows from `keep` on that stay.  A row below `first` is never written, so a prefix
+ * shared by sequences may lie there; no other page may be in two sequences' tables.
+ * weights, positions: [batch][heads][rows], contiguous; out_weights and out_positions the same shape: entries of rows that
+ * moved go with them, and rows past what is left hold 0 and -1, as new tokens find them.  out_lengths[b] =
+ * min(lengths[b], keep).  The outputs overlap no input.  lengths count in [0, min(rows, table_width * page_size)]; what
+ * lies on a page outside the cache is not copied.  first + recent <= keep, keep >= 1, rows <= 2^24. */
+GAR_API int gar_kv_evict(const gar_kv_cache *cache, const float *weights, const int32_t *positions, int64_t rows,
+                         const int32_t *page_table, int64_t table_stride, int table_width, const int32_t *lengths, int batch,
+                         int keep, int first, int recent, float *out_weights, int32_t *out_positions, int32_t *out_lengths,
+                         gar_stream_t stream);
+
+/* Which of the tokens that a draft proposed stand, so that what comes out is distributed as the target's.
+ * target: [batch][drafts + 1][vocab] probabilities p_i, draft: [batch][drafts][vocab] probabilities q_i that the i-th
+ * token was drawn from, both of dtype GAR_F32, GAR_BF16 or GAR_F16 with strides, a row's entries contiguous.
+ * What is not above 0 (NaN too) counts as 0, what is above 1 as 1.  tokens: [batch][drafts] integers of token_bytes (4
+ * or 8); a negative one ends the sequence's drafts there.  uniform: [batch][drafts + 1] independent numbers
+ * in [0, 1), one for each draft and one for the token after them; what is not above 0 (NaN too) counts as 0.
+ * Draft i stands if those before it do and uniform_i q_i(token_i) < p_i(token_i); a token from vocab on does not.
+ * After the a drafts that stand comes one more token, drawn with u = uniform_drafts, the last: where a draft was refused from
+ * r = max(p_a - q_a, 0), or from r = p_a where that is all zero; where there are no more drafts from r = p_a.  It is the
+ * first v with r(0) + ... + r(v) > u (r(0) + ... + r(vocab - 1)), or, where there is none, the last with r(v) > 0, or -1.
+ * Products are exact; sums are held in twice 32 bits, about 2^-45 of the sum.
+ * out_tokens: [batch][drafts + 1] of token_bytes: the drafts that stand, that token, then -1.  accepted: [batch], a.
+ * All integers and uniform are contiguous; out_tokens may not overlap tokens. */
+GAR_API int gar_verify_drafts(const void *target, int64_t target_batch_stride, int64_t target_row_stride, const void *draft,
+                              int64_t draft_batch_stride, int64_t draft_row_stride, int dtype, int64_t vocab,
+                              const void *tokens, int token_bytes, const float *uniform, int batch, int drafts,
+                              void *out_tokens, int32_t *accepted, gar_stream_t stream);
+
 /* Library self-test for build checks: generates and compiles (host-only, no GPU) the
  * fused kernels of a few plans.  Returns GAR_OK or GAR_EJIT. */
 GAR_API int gar_selftest_compile(void);

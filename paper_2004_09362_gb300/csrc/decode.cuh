@@ -43,6 +43,10 @@ struct DecodeArgs {
   int slack;               // units of 192 KB
   int solo;                // tiles of an item that a warp takes whole
   int batch, q_heads, group, item_groups, item_heads;  // group: q_heads / kv_heads
+  // Sequences that share their rows count as one: its query m of a cached head is query m % heads_each, of that head, of
+  // its sequence m / heads_each (share: its sequences; 0: there is nothing to share).
+  int share, heads_each;
+  Divide by_heads;         // by heads_each
   Divide items;            // by a sequence's items
   int q_dtype, out_dtype, window;
   bool out_wide;           // four neighbouring outputs can be stored at once
@@ -55,6 +59,14 @@ struct DecodeArgs {
   int device;              // the launch's
   int give_up;             // a segment's tiles from this one on count as copies that did not end
 };
+
+// Rows of a unit of the line: as many as it takes for the whole line, each item counted twice at most, to stay below 2^30
+// units, or 0 where 2^15 do not.
+inline int unit_of(int64_t items, int most_rows) {
+  for (int unit = 64; unit <= 32768; unit *= 2)
+    if (items * (most_rows / unit + 3) * 2 < 1 << 30) return unit;
+  return 0;
+}
 
 // x / d; a division in 32-bit floats, put right, where they hold x (the compiler's takes three times as long).
 __device__ __forceinline__ int quotient(int x, int d) {
@@ -301,6 +313,13 @@ __device__ __forceinline__ void store_out(const DecodeArgs &a, int64_t at, float
     static_cast<__nv_bfloat16 *>(a.out)[at] = from_f32<__nv_bfloat16>(x);
   else
     static_cast<__half *>(a.out)[at] = from_f32<__half>(x);
+}
+
+// Where the queries of head h of a segment are.
+__device__ __forceinline__ int64_t query_at(const DecodeArgs &a, const Segment &g, int h) {
+  if (a.share == 0) return g.b * a.qb + (g.head + h) * a.qh;
+  const int m = g.head + h - g.kv_head * a.group, i = (int)a.by_heads((uint32_t)m);
+  return ((int64_t)g.b * a.share + i) * a.qb + (g.kv_head * a.heads_each + (m - i * a.heads_each)) * a.qh;
 }
 
 __device__ __forceinline__ float load_q(const DecodeArgs &a, int64_t at) {

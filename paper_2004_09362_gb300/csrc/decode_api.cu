@@ -1,10 +1,11 @@
-// Decode attention: plans, workspaces, checks of arguments, choice of the kernel.
+// Decode attention, and that over shared prefixes: plans, workspaces, checks of arguments, choice of the kernel.
 #include <algorithm>
 #include <climits>
 #include <cmath>
 #include <new>
 
 #include "decode_mma.cuh"
+#include "prefix.cuh"
 
 struct gar_attn_plan {
   int q_heads, kv_heads, dim;
@@ -23,14 +24,6 @@ int dim_pad(int dim) { return (dim + 31) / 32 * 32; }
 size_t workspace_bytes(const gar_attn_plan &p) {
   const size_t rows = (size_t)kMaxCtas * 2 * kMaxGroup;
   return kCounterBytes + rows * (2 + dim_pad(p.dim)) * sizeof(float);
-}
-
-// Rows of a unit of the line: as many as it takes for the whole line, each item counted twice at most, to stay below 2^30
-// units, or 0 where 2^15 do not.
-int unit_of(int64_t items, int most_rows) {
-  for (int unit = 64; unit <= 32768; unit *= 2)
-    if (items * (most_rows / unit + 3) * 2 < 1 << 30) return unit;
-  return 0;
 }
 
 // The tensor-core kernels copy 16-byte chunks.
@@ -64,6 +57,73 @@ bool box_map(const gar_kv_cache &c, void *base, int rows, CUtensorMap *map) {
                 CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
+}  // namespace gar
+
+namespace gar {
+namespace {
+
+int check_types(const gar_attn_plan *plan, const gar_kv_cache *cache, int q_dtype, int out_dtype) {
+  if (plan == nullptr) return refuse("null plan");
+  if (int rc = check_cache(cache)) return rc;
+  if (cache->heads != plan->kv_heads || cache->dim != plan->dim) return refuse("the cache's heads or dim are not the plan's");
+  if (!float_type(q_dtype)) return refuse("q is GAR_F32, GAR_BF16 or GAR_F16");
+  if (float_type(cache->dtype) && cache->dtype != q_dtype) return refuse("a cache of float type goes with queries of its type");
+  if (out_dtype != q_dtype && out_dtype != GAR_F32) return refuse("out is of q's type or GAR_F32");
+  return GAR_OK;
+}
+
+int check_groups(const gar_attn_plan *plan, int batch, int groups) {
+  if (batch < 0 || groups < 0 || (batch > 0 && (groups == 0 || batch % groups)))
+    return refuse("the batch must be a multiple of the groups");
+  if ((int64_t)batch * plan->q_heads > INT_MAX / 2) return refuse("too many sequences and heads");
+  return GAR_OK;
+}
+
+// The arguments that follow from the plan, the cache and what a call has set.
+int complete(const gar_attn_plan *plan, const gar_kv_cache *cache, int table_width, float scale, DecodeArgs *a) {
+  // Row numbers stay below 2^31 with room for a tile past the end.
+  const int most_rows = (int)std::min<int64_t>((int64_t)table_width * cache->page_size, 0x7fffffff - 65536);
+  const int unit = unit_of((int64_t)a->batch * plan->kv_heads * ((a->group + 7) / 8), most_rows);
+  if (unit == 0) return refuse("too many sequences and heads for tables this wide");
+  if (plan->ws == nullptr) {
+    set_error("gar_attn_plan_set_workspace has not been called");
+    return GAR_ENOWS;
+  }
+  int dev = -1;
+  const cudaError_t e = cudaGetDevice(&dev);
+  if (e != cudaSuccess) return cuda_fail(e, "cudaGetDevice");
+  if (dev != plan->device) {
+    set_error("the plan's workspace is on another device");
+    return GAR_ESTATE;
+  }
+  a->c = *cache;
+  a->page = divide_by((uint32_t)cache->page_size);
+  a->most_rows = most_rows, a->q_heads = a->group * plan->kv_heads;
+  a->scale_log2 = (float)((double)scale * 1.4426950408889634);
+  char *ws = static_cast<char *>(plan->ws);
+  a->count = reinterpret_cast<unsigned *>(ws);
+  a->part_ml = reinterpret_cast<float2 *>(ws + kCounterBytes);
+  a->part_o = reinterpret_cast<float *>(a->part_ml + (size_t)kMaxCtas * 2 * kMaxGroup);
+  a->dim_pad = dim_pad(plan->dim), a->device = dev, a->give_up = plan->give_up;
+  a->out_wide = (uintptr_t)a->out % (4 * element_size(a->out_dtype)) == 0 && plan->dim % 4 == 0 && a->ob % 4 == 0 && a->oh % 4 == 0;
+  a->unit = unit;
+  a->slack = std::max(1, 196608 / (128 * cache->dim * element_size(cache->dtype)));
+  return GAR_OK;
+}
+
+int decode(const gar_attn_plan *plan, const DecodeArgs &a, gar_stream_t stream) {
+  if (!takes_mma(a.c, a.q, a.qb, a.qh, a.q_dtype)) return decode_general(a, plan->sms, stream);
+  const bool q32 = a.q_dtype == GAR_F32;
+  switch (a.c.dtype) {
+    case GAR_F32: return decode_mma_f32(a, plan->sms, stream);
+    case GAR_BF16: return decode_mma_bf16(a, plan->sms, stream);
+    case GAR_F16: return decode_mma_f16(a, plan->sms, stream);
+    case GAR_I8: return (q32 ? decode_mma_i8_f32 : decode_mma_i8)(a, plan->sms, stream);
+    default: return (q32 ? decode_mma_e4m3_f32 : decode_mma_e4m3)(a, plan->sms, stream);
+  }
+}
+
+}  // namespace
 }  // namespace gar
 
 using namespace gar;
@@ -134,12 +194,7 @@ int gar_decode_attention(gar_attn_plan *plan, const gar_kv_cache *cache, const v
                          int64_t out_head_stride, int out_dtype, float *lse, const int32_t *page_table,
                          int64_t table_stride, int table_width, const int32_t *lengths, int batch, float scale,
                          int window, gar_stream_t stream) {
-  if (plan == nullptr) return refuse("null plan");
-  if (int rc = check_cache(cache)) return rc;
-  if (cache->heads != plan->kv_heads || cache->dim != plan->dim) return refuse("the cache's heads or dim are not the plan's");
-  if (!float_type(q_dtype)) return refuse("q is GAR_F32, GAR_BF16 or GAR_F16");
-  if (float_type(cache->dtype) && cache->dtype != q_dtype) return refuse("a cache of float type goes with queries of its type");
-  if (out_dtype != q_dtype && out_dtype != GAR_F32) return refuse("out is of q's type or GAR_F32");
+  if (int rc = check_types(plan, cache, q_dtype, out_dtype)) return rc;
   if (batch < 0 || table_width < 0 || window < 0) return refuse("negative batch, table_width or window");
   if (!std::isfinite(scale)) return refuse("scale must be finite");
   if (batch == 0) return GAR_OK;
@@ -150,49 +205,73 @@ int gar_decode_attention(gar_attn_plan *plan, const gar_kv_cache *cache, const v
     set_error("a buffer is not aligned to its elements");
     return GAR_EALIGN;
   }
-  // Row numbers stay below 2^31 with room for a tile past the end.
-  const int most_rows = (int)std::min<int64_t>((int64_t)table_width * cache->page_size, 0x7fffffff - 65536);
-  const int group = plan->q_heads / plan->kv_heads;
-  const int unit = unit_of((int64_t)batch * plan->kv_heads * ((group + 7) / 8), most_rows);
-  if (unit == 0) return refuse("too many sequences and heads for tables this wide");
-  if (plan->ws == nullptr) {
-    set_error("gar_attn_plan_set_workspace has not been called");
-    return GAR_ENOWS;
-  }
-  int dev = -1;
-  const cudaError_t e = cudaGetDevice(&dev);
-  if (e != cudaSuccess) return cuda_fail(e, "cudaGetDevice");
-  if (dev != plan->device) {
-    set_error("the plan's workspace is on another device");
-    return GAR_ESTATE;
-  }
   DecodeArgs a{};
-  a.c = *cache;
   a.q = q, a.out = out, a.lse = lse;
   a.qb = q_batch_stride, a.qh = q_head_stride, a.ob = out_batch_stride, a.oh = out_head_stride;
   a.table = page_table, a.table_stride = table_stride, a.lengths = lengths;
-  a.page = divide_by((uint32_t)cache->page_size);
-  a.most_rows = most_rows, a.batch = batch, a.q_heads = plan->q_heads, a.group = group;
-  a.q_dtype = q_dtype, a.out_dtype = out_dtype, a.window = window;
-  a.scale_log2 = (float)((double)scale * 1.4426950408889634);
-  char *ws = static_cast<char *>(plan->ws);
-  a.count = reinterpret_cast<unsigned *>(ws);
-  a.part_ml = reinterpret_cast<float2 *>(ws + kCounterBytes);
-  a.part_o = reinterpret_cast<float *>(a.part_ml + (size_t)kMaxCtas * 2 * kMaxGroup);
-  a.dim_pad = dim_pad(plan->dim), a.device = dev, a.give_up = plan->give_up;
-  a.out_wide = (uintptr_t)out % (4 * element_size(out_dtype)) == 0 && plan->dim % 4 == 0 && out_batch_stride % 4 == 0 &&
-               out_head_stride % 4 == 0;
-  a.unit = unit;
-  a.slack = std::max(1, 196608 / (128 * cache->dim * element_size(cache->dtype)));
-  if (!takes_mma(*cache, q, q_batch_stride, q_head_stride, q_dtype)) return decode_general(a, plan->sms, stream);
-  const bool q32 = q_dtype == GAR_F32;
-  switch (cache->dtype) {
-    case GAR_F32: return decode_mma_f32(a, plan->sms, stream);
-    case GAR_BF16: return decode_mma_bf16(a, plan->sms, stream);
-    case GAR_F16: return decode_mma_f16(a, plan->sms, stream);
-    case GAR_I8: return (q32 ? decode_mma_i8_f32 : decode_mma_i8)(a, plan->sms, stream);
-    default: return (q32 ? decode_mma_e4m3_f32 : decode_mma_e4m3)(a, plan->sms, stream);
+  a.batch = batch, a.q_dtype = q_dtype, a.out_dtype = out_dtype, a.window = window;
+  a.group = plan->q_heads / plan->kv_heads;
+  if (int rc = complete(plan, cache, table_width, scale, &a)) return rc;
+  return decode(plan, a, stream);
+}
+
+int gar_prefix_attention_bytes(const gar_attn_plan *plan, int batch, int groups, size_t *bytes) {
+  if (plan == nullptr || bytes == nullptr) return refuse("null plan or output");
+  if (int rc = check_groups(plan, batch, groups)) return rc;
+  *bytes = prefix_workspace(batch, plan->q_heads, plan->dim, nullptr, nullptr);
+  return GAR_OK;
+}
+
+int gar_prefix_attention(gar_attn_plan *plan, const gar_kv_cache *cache, const void *q, int64_t q_batch_stride,
+                         int64_t q_head_stride, int q_dtype, void *out, int64_t out_batch_stride, int64_t out_head_stride,
+                         int out_dtype, float *lse, const int32_t *prefix_table, int64_t prefix_stride, int prefix_width,
+                         const int32_t *prefix_lengths, int groups, const int32_t *page_table, int64_t table_stride,
+                         int table_width, const int32_t *lengths, int batch, float scale, void *workspace,
+                         size_t workspace_bytes, gar_stream_t stream) {
+  if (int rc = check_types(plan, cache, q_dtype, out_dtype)) return rc;
+  if (int rc = check_groups(plan, batch, groups)) return rc;
+  if (table_width < 0 || prefix_width < 0) return refuse("negative table_width or prefix_width");
+  if (!std::isfinite(scale)) return refuse("scale must be finite");
+  if (batch == 0) return GAR_OK;
+  if (q == nullptr || out == nullptr || lengths == nullptr || prefix_lengths == nullptr ||
+      (page_table == nullptr && table_width > 0) || (prefix_table == nullptr && prefix_width > 0))
+    return refuse("null pointer");
+  if ((uintptr_t)q % element_size(q_dtype) || (uintptr_t)out % element_size(out_dtype) || (uintptr_t)lse % 4 ||
+      (uintptr_t)page_table % 4 || (uintptr_t)lengths % 4 || (uintptr_t)prefix_table % 4 || (uintptr_t)prefix_lengths % 4) {
+    set_error("a buffer is not aligned to its elements");
+    return GAR_EALIGN;
   }
+  if ((uintptr_t)workspace % 16) {
+    set_error("the workspace must be 16-byte aligned");
+    return GAR_EALIGN;
+  }
+  const int dim = plan->dim, heads = plan->q_heads, group = heads / plan->kv_heads, share = batch / groups;
+  PrefixParts parts[2];
+  if (workspace == nullptr || workspace_bytes < prefix_workspace(batch, heads, dim, static_cast<char *>(workspace), parts)) {
+    set_error("the workspace is smaller than gar_prefix_attention_bytes");
+    return GAR_ENOWS;
+  }
+  // The parts' results: the sequences' own rows, and the prefixes with a group's queries as those of one sequence.
+  DecodeArgs a{};
+  a.q = q, a.qb = q_batch_stride, a.qh = q_head_stride, a.q_dtype = q_dtype, a.out_dtype = GAR_F32;
+  DecodeArgs own = a, prefix = a;
+  const int64_t row = parts[0].row;
+  own.out = parts[0].out, own.lse = parts[0].lse, own.ob = heads * row, own.oh = row;
+  own.table = page_table, own.table_stride = table_stride, own.lengths = lengths;
+  own.batch = batch, own.group = group;
+  prefix.out = parts[1].out, prefix.lse = parts[1].lse, prefix.ob = share * heads * row, prefix.oh = row;
+  prefix.table = prefix_table, prefix.table_stride = prefix_stride, prefix.lengths = prefix_lengths;
+  prefix.batch = groups, prefix.group = share * group;
+  prefix.share = share, prefix.heads_each = group, prefix.by_heads = divide_by((uint32_t)group);
+  if (int rc = complete(plan, cache, table_width, scale, &own)) return rc;
+  if (int rc = complete(plan, cache, prefix_width, scale, &prefix)) return rc;
+  if (int rc = decode(plan, prefix, stream)) return rc;
+  if (int rc = decode(plan, own, stream)) return rc;
+  JoinArgs j{};
+  j.parts[0] = parts[0], j.parts[1] = parts[1];
+  j.out = out, j.ob = out_batch_stride, j.oh = out_head_stride, j.out_dtype = out_dtype, j.lse = lse;
+  j.rows = (int64_t)batch * heads, j.dim = dim, j.heads = heads, j.group = group, j.share = share;
+  return join_prefix(j, stream);
 }
 
 }  // extern "C"

@@ -38,7 +38,7 @@ template <typename T, int J> __global__ void __launch_bounds__(kThreads) general
 #pragma unroll
       for (int j = 0; j < J; ++j) {
         const int d = lane + 32 * j;
-        q[h][j] = h < g.heads && d < c.dim ? load_q(a, g.b * a.qb + (g.head + h) * a.qh + d) : 0.f;
+        q[h][j] = h < g.heads && d < c.dim ? load_q(a, query_at(a, g, h) + d) : 0.f;
         o[h][j] = 0.f;
       }
     const int lo = g.lo;

@@ -433,11 +433,10 @@ __global__ void __launch_bounds__(32 * MmaShape<C, DP, NG>::kWarps, 1)
   uint32_t qf[NG][QW];
   const auto load_queries = [&](const Segment &seg) {
     constexpr int QB = Q32 ? 4 : 2, V = 16 / QB, PER = 16 / EL / V;  // 16 bytes have V channels, a chunk PER times as many
-    const char *const q0 = static_cast<const char *>(a.q) + QB * (seg.b * a.qb + (seg.head + g) * a.qh);
 #pragma unroll
     for (int ng = 0; ng < NG; ++ng) {
       const bool there = g + 8 * ng < seg.heads;
-      const uint4 *q = reinterpret_cast<const uint4 *>(q0 + QB * 8 * ng * a.qh);
+      const uint4 *q = reinterpret_cast<const uint4 *>(static_cast<const char *>(a.q) + QB * query_at(a, seg, g + 8 * ng));
 #pragma unroll
       for (int k = 0; k < QW / 4; ++k) {
         const int at = (t + 4 * (k / PER)) * PER + k % PER;
@@ -608,7 +607,7 @@ __global__ void __launch_bounds__(32 * MmaShape<C, DP, NG>::kWarps, 1)
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
               const int head = 8 * ng + 2 * t + i % 2, row = key_row<LINE>(g) + i / 2 * 8;
-              const float *q = static_cast<const float *>(a.q) + seg.b * a.qb + (seg.head + head) * a.qh;
+              const float *q = static_cast<const float *>(a.q) + query_at(a, seg, head);
               float x = 0.f;
               if (head < seg.heads)
                 for (int d = 0; d < c.dim; ++d)

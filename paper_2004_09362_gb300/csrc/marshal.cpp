@@ -449,6 +449,21 @@ PyObject *kv_read(PyObject *, PyObject *const *args, Py_ssize_t n, PyObject *kw)
   });
 }
 
+// The plan's workspace comes with the first call; that the stream of a call uses it is known to its allocator.
+void use_workspace(PyObject *plan, PyObject *like, const Stream &stream) {
+  PyObject *last = PyObject_GetAttr(plan, names_of().stream);
+  if (!last) throw python_error();
+  const bool known = last != Py_None && PyLong_AsVoidPtr(last) == static_cast<void *>(stream.raw);
+  Py_DECREF(last);
+  if (PyErr_Occurred()) throw python_error();
+  if (known) return;
+  PyObject *m = PyImport_ImportModule("paper_2004_09362_gb300.gar");
+  PyObject *r = m ? PyObject_CallMethod(m, "_use_workspace", "OOK", plan, like, (unsigned long long)(uintptr_t)stream.raw) : nullptr;
+  Py_XDECREF(m);
+  if (!r) throw python_error();
+  Py_DECREF(r);
+}
+
 PyObject *decode_attention(PyObject *, PyObject *const *args, Py_ssize_t n, PyObject *kw) {
   return guarded([&] {
     static const char *const names[] = {"plan",  "q",      "cache", "page_table", "lengths",
@@ -484,21 +499,7 @@ PyObject *decode_attention(PyObject *, PyObject *const *args, Py_ssize_t n, PyOb
     }
     refuse_graded({&q, &out, &lse});
     const Stream stream(a.at[9], device.check());
-    // The workspace comes with the first call; that the stream of a call uses it is known to its allocator.
-    PyObject *last = PyObject_GetAttr(a.at[0], names_of().stream);
-    if (!last) throw python_error();
-    const bool known = last != Py_None && PyLong_AsVoidPtr(last) == static_cast<void *>(stream.raw);
-    Py_DECREF(last);
-    if (PyErr_Occurred()) throw python_error();
-    if (!known) {
-      PyObject *m = PyImport_ImportModule("paper_2004_09362_gb300.gar");
-      PyObject *r = m ? PyObject_CallMethod(m, "_use_workspace", "OOK", a.at[0], a.at[1],
-                                            (unsigned long long)(uintptr_t)stream.raw)
-                      : nullptr;
-      Py_XDECREF(m);
-      if (!r) throw python_error();
-      Py_DECREF(r);
-    }
+    use_workspace(a.at[0], a.at[1], stream);
     if (!a.at[7]) out = stream.empty(q.sizes(), q.scalar_type(), q);
     if (wanted && !given) lse = stream.empty(q.sizes().slice(0, 2), at::kFloat, q);
     const double scale = a.at[5] ? number(a.at[5]) : 1.0 / std::sqrt((double)shape[2]);
@@ -517,6 +518,236 @@ PyObject *decode_attention(PyObject *, PyObject *const *args, Py_ssize_t n, PyOb
     PyTuple_SET_ITEM(pair, 0, first);
     PyTuple_SET_ITEM(pair, 1, given ? Py_NewRef(a.at[8]) : THPVariable_Wrap(std::move(lse)));
     return pair;
+  });
+}
+
+// int32 [batch, width] on the GPU, each row contiguous.
+const Tensor &pages_of(PyObject *o, int64_t batch, const char *what) {
+  const Tensor &t = tensor(o, what);
+  if (t.dim() != 2 || (batch >= 0 && t.size(0) != batch) || t.scalar_type() != at::kInt || !t.is_cuda() ||
+      (t.stride(1) != 1 && t.size(1) > 1))
+    bad(std::string(what) + " must be int32 [batch, width] on the GPU with contiguous rows");
+  narrow(t.size(1), "the page table's width");
+  return t;
+}
+
+// No element twice (an expanded tensor's are): for outputs.
+void refuse_expanded(const Tensor &t, const char *what) {
+  for (int64_t i = 0; i < t.dim(); ++i)
+    if (t.size(i) > 1 && t.stride(i) == 0) bad(std::string(what) + " has elements that share memory");
+}
+
+// A contiguous tensor of a shape and a type on the GPU.
+const Tensor &exactly(PyObject *o, at::IntArrayRef shape, at::ScalarType type, const char *what) {
+  const Tensor &t = tensor(o, what);
+  if (t.sizes() != shape || t.scalar_type() != type || !t.is_cuda() || !t.is_contiguous()) {
+    std::string n;
+    for (int64_t x : shape) n += (n.empty() ? "" : ", ") + std::to_string(x);
+    bad(std::string(what) + " must be a contiguous " + (type == at::kFloat ? "float32" : type == at::kInt ? "int32" : "int64") +
+        " CUDA tensor [" + n + "]");
+  }
+  return t;
+}
+
+PyObject *tuple_of(std::initializer_list<PyObject *> items) {
+  PyObject *t = PyTuple_New((Py_ssize_t)items.size());
+  Py_ssize_t i = 0;
+  for (PyObject *x : items) {
+    if (t)
+      PyTuple_SET_ITEM(t, i++, x);
+    else
+      Py_XDECREF(x);
+  }
+  if (!t) throw python_error();
+  return t;
+}
+
+PyObject *prefix_attention(PyObject *, PyObject *const *args, Py_ssize_t n, PyObject *kw) {
+  return guarded([&] {
+    static const char *const names[] = {"plan",       "q",       "cache", "prefix_table", "prefix_lengths",
+                                        "page_table", "lengths", "scale", "out",          "lse", "stream"};
+    const Arguments<11> a("gar_prefix_attention", names, 7, args, n, kw);
+    gar_attn_plan *plan = handle<gar_attn_plan>(a.at[0], "plan destroyed");
+    const gar_kv_cache *cache = handle<gar_kv_cache>(a.at[2], "the cache has no address");
+    const Tensor &q = rows(a.at[1], "q"), &lengths = integers(a.at[6], q.size(0), true, false, "lengths");
+    const Tensor &table = pages_of(a.at[5], q.size(0), "page_table"), &prefix = pages_of(a.at[3], -1, "prefix_table");
+    const Tensor &prefix_lengths = integers(a.at[4], prefix.size(0), true, false, "prefix_lengths");
+    const int batch = narrow(q.size(0), "the batch"), groups = narrow(prefix.size(0), "the number of prefixes");
+    int shape[3];
+    check(gar_attn_plan_shape(plan, &shape[0], &shape[1], &shape[2]), "gar_attn_plan_shape");
+    if (q.size(1) != shape[0] || q.size(2) != shape[2])
+      bad("q must be [batch, " + std::to_string(shape[0]) + ", " + std::to_string(shape[2]) + "]");
+    Tensor out, lse;
+    Device device;
+    device.add(device_of(a.at[2]), "cache"), device.add(q, "q"), device.add(prefix, "prefix_table");
+    device.add(prefix_lengths, "prefix_lengths"), device.add(table, "page_table"), device.add(lengths, "lengths");
+    if (a.at[8]) {
+      out = rows(a.at[8], "out");
+      if (out.sizes() != q.sizes()) bad("out must have q's shape");
+      refuse_expanded(out, "out");
+      device.add(out, "out");
+    }
+    const bool given = a.at[9] && !PyBool_Check(a.at[9]), wanted = given || truth(a.at[9]);
+    if (given) {
+      lse = exactly(a.at[9], q.sizes().slice(0, 2), at::kFloat, "lse");
+      device.add(lse, "lse");
+    }
+    refuse_graded({&q, &out, &lse});
+    const Stream stream(a.at[10], device.check());
+    size_t bytes = 0;
+    check(gar_prefix_attention_bytes(plan, batch, groups, &bytes), "gar_prefix_attention_bytes");
+    use_workspace(a.at[0], a.at[1], stream);
+    // (freed at the end: for what comes next on the stream)
+    const Tensor workspace = stream.empty({(int64_t)bytes}, at::kByte, q);
+    if (!a.at[8]) out = stream.empty(q.sizes(), q.scalar_type(), q);
+    if (wanted && !given) lse = stream.empty(q.sizes().slice(0, 2), at::kFloat, q);
+    const double scale = a.at[7] ? number(a.at[7]) : 1.0 / std::sqrt((double)shape[2]);
+    check(gar_prefix_attention(plan, cache, q.data_ptr(), q.stride(0), q.stride(1), dtype_of(q, "q"), out.data_ptr(),
+                               out.stride(0), out.stride(1), dtype_of(out, "out"),
+                               wanted ? static_cast<float *>(lse.data_ptr()) : nullptr,
+                               static_cast<const int32_t *>(prefix.data_ptr()), prefix.stride(0), (int)prefix.size(1),
+                               static_cast<const int32_t *>(prefix_lengths.data_ptr()), groups,
+                               static_cast<const int32_t *>(table.data_ptr()), table.stride(0), (int)table.size(1),
+                               static_cast<const int32_t *>(lengths.data_ptr()), batch, (float)scale, workspace.data_ptr(), bytes,
+                               stream.raw),
+          "gar_prefix_attention");
+    if (a.at[8]) changed(out);
+    if (given) changed(lse);
+    PyObject *first = a.at[8] ? Py_NewRef(a.at[8]) : THPVariable_Wrap(std::move(out));
+    if (!wanted) return first;
+    return tuple_of({first, given ? Py_NewRef(a.at[9]) : THPVariable_Wrap(std::move(lse))});
+  });
+}
+
+PyObject *kv_weigh(PyObject *, PyObject *const *args, Py_ssize_t n, PyObject *kw) {
+  return guarded([&] {
+    static const char *const names[] = {"q", "cache", "page_table", "lengths", "lse", "weights", "scale", "window", "out", "stream"};
+    const Arguments<10> a("gar_kv_weigh", names, 6, args, n, kw);
+    const gar_kv_cache *cache = handle<gar_kv_cache>(a.at[1], "the cache has no address");
+    const Tensor &q = rows(a.at[0], "q"), &lengths = integers(a.at[3], q.size(0), true, false, "lengths");
+    const Tensor &table = pages_of(a.at[2], q.size(0), "page_table"), &lse = exactly(a.at[4], q.sizes().slice(0, 2), at::kFloat, "lse");
+    if (q.size(2) != cache->dim) bad("q must have the cache's channels");
+    const auto check_weights = [&](const Tensor &t, const char *what) {
+      if (t.dim() != 3 || t.size(0) != q.size(0) || t.size(1) != cache->heads || t.scalar_type() != at::kFloat || !t.is_cuda() ||
+          (t.stride(2) != 1 && t.size(2) > 1))
+        bad(std::string(what) + " must be float32 [batch, the cache's heads, rows] on the GPU with contiguous rows");
+    };
+    const Tensor &weights = tensor(a.at[5], "weights");
+    check_weights(weights, "weights");
+    Tensor out;
+    Device device;
+    device.add(device_of(a.at[1]), "cache"), device.add(q, "q"), device.add(table, "page_table"), device.add(lengths, "lengths");
+    device.add(lse, "lse"), device.add(weights, "weights");
+    if (a.at[8]) {
+      out = tensor(a.at[8], "out");
+      check_weights(out, "out");
+      if (out.sizes() != weights.sizes()) bad("out must have weights' shape");
+      refuse_expanded(out, "out");
+      device.add(out, "out");
+    }
+    refuse_graded({&q, &lse, &weights, &out});
+    const int batch = narrow(q.size(0), "the batch"), window = a.at[7] ? narrow(integer(a.at[7]), "window") : 0;
+    const Stream stream(a.at[9], device.check());
+    if (!a.at[8]) out = stream.empty(weights.sizes(), at::kFloat, q);
+    const double scale = a.at[6] ? number(a.at[6]) : 1.0 / std::sqrt((double)cache->dim);
+    check(gar_kv_weigh(cache, q.data_ptr(), q.stride(0), q.stride(1), dtype_of(q, "q"), (int)q.size(1),
+                       static_cast<const float *>(lse.data_ptr()), static_cast<const float *>(weights.data_ptr()), weights.stride(0),
+                       weights.stride(1), static_cast<float *>(out.data_ptr()), out.stride(0), out.stride(1), weights.size(2),
+                       static_cast<const int32_t *>(table.data_ptr()), table.stride(0), (int)table.size(1),
+                       static_cast<const int32_t *>(lengths.data_ptr()), batch, (float)scale, window, stream.raw),
+          "gar_kv_weigh");
+    if (!a.at[8]) return THPVariable_Wrap(std::move(out));
+    changed(out);
+    return Py_NewRef(a.at[8]);
+  });
+}
+
+PyObject *kv_evict(PyObject *, PyObject *const *args, Py_ssize_t n, PyObject *kw) {
+  return guarded([&] {
+    static const char *const names[] = {"cache", "weights", "positions", "page_table", "lengths", "keep", "first", "recent", "out", "stream"};
+    const Arguments<10> a("gar_kv_evict", names, 6, args, n, kw);
+    const gar_kv_cache *cache = handle<gar_kv_cache>(a.at[0], "the cache has no address");
+    const Tensor &any = tensor(a.at[1], "weights");
+    if (any.dim() != 3 || any.size(1) != cache->heads) bad("weights must be [batch, the cache's heads, rows]");
+    const Tensor &weights = exactly(a.at[1], any.sizes(), at::kFloat, "weights");
+    const Tensor &positions = exactly(a.at[2], weights.sizes(), at::kInt, "positions");
+    const int64_t count = weights.size(0);
+    const Tensor &table = pages_of(a.at[3], count, "page_table"), &lengths = integers(a.at[4], count, true, false, "lengths");
+    const int batch = narrow(count, "the batch"), keep = narrow(integer(a.at[5]), "keep"),
+              first = a.at[6] ? narrow(integer(a.at[6]), "first") : 0, recent = a.at[7] ? narrow(integer(a.at[7]), "recent") : 0;
+    Tensor out[3];
+    Device device;
+    device.add(device_of(a.at[0]), "cache"), device.add(weights, "weights"), device.add(positions, "positions");
+    device.add(table, "page_table"), device.add(lengths, "lengths");
+    if (a.at[8]) {
+      if (!PyTuple_Check(a.at[8]) || PyTuple_GET_SIZE(a.at[8]) != 3) bad("out must be three tensors: weights, positions, lengths");
+      out[0] = exactly(PyTuple_GET_ITEM(a.at[8], 0), weights.sizes(), at::kFloat, "out's weights");
+      out[1] = exactly(PyTuple_GET_ITEM(a.at[8], 1), weights.sizes(), at::kInt, "out's positions");
+      out[2] = exactly(PyTuple_GET_ITEM(a.at[8], 2), {count}, at::kInt, "out's lengths");
+      for (const Tensor &t : out) device.add(t, "out");
+    }
+    refuse_graded({&weights, &out[0]});
+    const Stream stream(a.at[9], device.check());
+    if (!a.at[8]) {
+      out[0] = stream.empty(weights.sizes(), at::kFloat, weights), out[1] = stream.empty(weights.sizes(), at::kInt, weights);
+      out[2] = stream.empty({count}, at::kInt, weights);
+    }
+    check(gar_kv_evict(cache, static_cast<const float *>(weights.data_ptr()), static_cast<const int32_t *>(positions.data_ptr()),
+                       weights.size(2), static_cast<const int32_t *>(table.data_ptr()), table.stride(0), (int)table.size(1),
+                       static_cast<const int32_t *>(lengths.data_ptr()), batch, keep, first, recent,
+                       static_cast<float *>(out[0].data_ptr()), static_cast<int32_t *>(out[1].data_ptr()),
+                       static_cast<int32_t *>(out[2].data_ptr()), stream.raw),
+          "gar_kv_evict");
+    changed_cache(a.at[0]);
+    if (a.at[8]) {
+      for (const Tensor &t : out) changed(t);
+      return Py_NewRef(a.at[8]);
+    }
+    return tuple_of({THPVariable_Wrap(std::move(out[0])), THPVariable_Wrap(std::move(out[1])), THPVariable_Wrap(std::move(out[2]))});
+  });
+}
+
+PyObject *verify_drafts(PyObject *, PyObject *const *args, Py_ssize_t n, PyObject *kw) {
+  return guarded([&] {
+    static const char *const names[] = {"target", "draft", "tokens", "uniform", "out", "stream"};
+    const Arguments<6> a("gar_verify_drafts", names, 4, args, n, kw);
+    const auto table = [&](PyObject *o, const char *what) -> const Tensor & {
+      const Tensor &t = tensor(o, what);
+      if (t.dim() != 3 || !t.is_cuda() || (t.stride(2) != 1 && t.size(2) > 1))
+        bad(std::string(what) + " must be [batch, drafts, vocab] on the GPU with contiguous rows");
+      return t;
+    };
+    const Tensor &target = table(a.at[0], "target"), &draft = table(a.at[1], "draft"), &given = tensor(a.at[2], "tokens");
+    const int64_t batch = target.size(0), drafts = draft.size(1), vocab = target.size(2);
+    if (draft.size(0) != batch || draft.size(2) != vocab || target.size(1) != drafts + 1 || target.scalar_type() != draft.scalar_type())
+      bad("target must be [batch, drafts + 1, vocab] and draft [batch, drafts, vocab], alike in dtype");
+    const auto type = given.scalar_type();
+    if (type != at::kLong && type != at::kInt) bad("tokens: this dtype is not supported");
+    const int64_t shape[2] = {batch, drafts}, longer[2] = {batch, drafts + 1};
+    const Tensor &tokens = exactly(a.at[2], shape, type, "tokens"), &uniform = exactly(a.at[3], longer, at::kFloat, "uniform");
+    Tensor out[2];
+    Device device;
+    device.add(target, "target"), device.add(draft, "draft"), device.add(tokens, "tokens"), device.add(uniform, "uniform");
+    if (a.at[4]) {
+      if (!PyTuple_Check(a.at[4]) || PyTuple_GET_SIZE(a.at[4]) != 2) bad("out must be two tensors: tokens, accepted");
+      out[0] = exactly(PyTuple_GET_ITEM(a.at[4], 0), longer, type, "out's tokens");
+      out[1] = exactly(PyTuple_GET_ITEM(a.at[4], 1), {batch}, at::kInt, "out's accepted");
+      device.add(out[0], "out"), device.add(out[1], "out");
+    }
+    refuse_graded({&target, &draft, &uniform});
+    const Stream stream(a.at[5], device.check());
+    if (!a.at[4]) out[0] = stream.empty(longer, type, target), out[1] = stream.empty({batch}, at::kInt, target);
+    check(gar_verify_drafts(target.data_ptr(), target.stride(0), target.stride(1), draft.data_ptr(), draft.stride(0), draft.stride(1),
+                            dtype_of(target, "target"), vocab, tokens.data_ptr(), (int)tokens.element_size(),
+                            static_cast<const float *>(uniform.data_ptr()), narrow(batch, "the batch"),
+                            narrow(drafts, "the number of drafts"), out[0].data_ptr(), static_cast<int32_t *>(out[1].data_ptr()),
+                            stream.raw),
+          "gar_verify_drafts");
+    if (a.at[4]) {
+      changed(out[0]), changed(out[1]);
+      return Py_NewRef(a.at[4]);
+    }
+    return tuple_of({THPVariable_Wrap(std::move(out[0])), THPVariable_Wrap(std::move(out[1]))});
   });
 }
 
@@ -546,6 +777,30 @@ PyMethodDef methods[] = {
      "q's dtype or float32.  lse: True, or a contiguous float32 [batch, q_heads] tensor, returns\n"
      "(out, log of the sum of weights); else returns out.  The plan's workspace is allocated on its\n"
      "first call; make one before capturing calls into a CUDA graph."},
+    {"gar_prefix_attention", (PyCFunction)(void (*)())prefix_attention, METH_FASTCALL | METH_KEYWORDS,
+     "gar_prefix_attention(plan, q, cache, prefix_table, prefix_lengths, page_table, lengths,\n"
+     "                     scale=None, out=None, lse=None, stream=None)\n--\n\n"
+     "Attention of q [batch, q_heads, dim] over a prefix that sequences share, then each one's own rows.\n\n"
+     "prefix_table: int32 [groups, width]; prefix_lengths: int32 [groups].  Each batch / groups neighbouring sequences\n"
+     "share a prefix, which is read once for them.  The rest is as in gar_decode_attention; drafted tokens of a\n"
+     "context are such sequences, whose own rows are the drafts before them and themselves."},
+    {"gar_kv_weigh", (PyCFunction)(void (*)())kv_weigh, METH_FASTCALL | METH_KEYWORDS,
+     "gar_kv_weigh(q, cache, page_table, lengths, lse, weights, scale=None, window=0, out=None, stream=None)\n--\n\n"
+     "weights float32 [batch, cached heads, rows] plus what each row gets in the attention of q [batch, q_heads, dim]:\n"
+     "the sum of exp(scale q.k - lse) over its head's queries.  lse: float32 [batch, q_heads], as the attention gave it.  out may be\n"
+     "weights.  Has no gradient."},
+    {"gar_kv_evict", (PyCFunction)(void (*)())kv_evict, METH_FASTCALL | METH_KEYWORDS,
+     "gar_kv_evict(cache, weights, positions, page_table, lengths, keep, first=0, recent=0, out=None, stream=None)\n--\n\n"
+     "Cuts each sequence of more than `keep` rows down to that many, in each head those of most weight, moving kept rows of\n"
+     "the cache to the places of rows that go.  The `first` rows and those of the `recent` last positions are kept whatever\n"
+     "they weigh.  weights: float32, positions: int32, both contiguous [batch, cached heads, rows].  Returns the weights and positions of what is left\n"
+     "(0 and -1 past it) and the lengths; out: three tensors to fill instead."},
+    {"gar_verify_drafts", (PyCFunction)(void (*)())verify_drafts, METH_FASTCALL | METH_KEYWORDS,
+     "gar_verify_drafts(target, draft, tokens, uniform, out=None, stream=None)\n--\n\n"
+     "Which drafted tokens stand, and the token after them.  target [batch, drafts + 1, vocab] and draft [batch, drafts, vocab]:\n"
+     "probabilities; tokens: int32 or int64 [batch, drafts], negative from where a sequence has no more; uniform:\n"
+     "float32 [batch, drafts + 1] in [0, 1).  Returns tokens [batch, drafts + 1] (those that stand, the next one, then -1) and\n"
+     "int32 [batch], how many stand; out: two tensors to fill instead."},
     {nullptr, nullptr, 0, nullptr}};
 
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_marshal", "Compiled calls of the decoding operators.", -1, methods,

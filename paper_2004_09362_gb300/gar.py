@@ -52,6 +52,7 @@ EXPORTS = (
     "gar_plan_create_group", "gar_rope_frequencies", "gar_rope_table", "gar_rope", "gar_kv_write",
     "gar_kv_read", "gar_kv_status", "gar_attn_plan_create", "gar_attn_plan_destroy",
     "gar_attn_plan_shape", "gar_attn_plan_bytes", "gar_attn_plan_set_workspace", "gar_attn_plan_debug_wait", "gar_decode_attention",
+    "gar_prefix_attention_bytes", "gar_prefix_attention", "gar_kv_weigh", "gar_kv_evict", "gar_verify_drafts",
 )
 
 
@@ -129,6 +130,13 @@ def _load():
         "gar_attn_plan_debug_wait": (i32, [vp, i32]),
         "gar_decode_attention": (i32, [vp, P_(gar_kv_cache), vp, i64, i64, i32, vp, i64, i64, i32, vp, vp,
                                        i64, i32, vp, i32, f32, i32, vp]),
+        "gar_prefix_attention_bytes": (i32, [vp, i32, i32, P_(sz)]),
+        "gar_prefix_attention": (i32, [vp, P_(gar_kv_cache), vp, i64, i64, i32, vp, i64, i64, i32, vp, vp, i64, i32, vp,
+                                       i32, vp, i64, i32, vp, i32, f32, vp, sz, vp]),
+        "gar_kv_weigh": (i32, [P_(gar_kv_cache), vp, i64, i64, i32, i32, vp, vp, i64, i64, vp, i64, i64, i64, vp, i64, i32,
+                               vp, i32, f32, i32, vp]),
+        "gar_kv_evict": (i32, [P_(gar_kv_cache), vp, vp, i64, vp, i64, i32, vp, i32, i32, i32, i32, vp, vp, vp, vp]),
+        "gar_verify_drafts": (i32, [vp, i64, i64, vp, i64, i64, i32, i64, vp, i32, vp, i32, i32, vp, vp, vp]),
     }
     for name, (res, args) in sig.items():
         fn = getattr(lib, name)
@@ -674,10 +682,20 @@ def _use_workspace(plan: AttnPlan, like, raw: int) -> None:
     plan.stream = raw
 
 
+def gar_prefix_attention_bytes(plan: AttnPlan, batch: int, groups: int) -> int:
+    n = ctypes.c_size_t()
+    _check(_lib.gar_prefix_attention_bytes(plan.handle, _narrow(batch, "batch"), _narrow(groups, "groups"), ctypes.byref(n)),
+           "gar_prefix_attention_bytes")
+    return n.value
+
+
+_COMPILED = ("gar_rope", "gar_kv_write", "gar_kv_read", "gar_decode_attention", "gar_prefix_attention", "gar_kv_weigh",
+             "gar_kv_evict", "gar_verify_drafts")
+
+
 def __getattr__(name):
-    """The calls of a decoding step (gar_rope, gar_kv_write, gar_kv_read, gar_decode_attention) are
-    compiled (csrc/marshal.cpp) and loaded on first use, with torch."""
-    if name in ("gar_rope", "gar_kv_write", "gar_kv_read", "gar_decode_attention"):
+    """The calls of a decoding step (_COMPILED) are compiled (csrc/marshal.cpp) and loaded on first use, with torch."""
+    if name in _COMPILED:
         import torch  # noqa: F401  (its libraries are the module's)
         if not os.path.exists(os.path.join(_HERE, "_marshal.so")):
             raise ImportError("_marshal.so not built; run __graft_entry__.build() where torch is installed")
