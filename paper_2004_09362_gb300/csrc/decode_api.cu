@@ -79,6 +79,22 @@ int check_groups(const gar_attn_plan *plan, int batch, int groups) {
   return GAR_OK;
 }
 
+// Queries of a cached head and a prefix from which on the prefix goes to the tensor cores' own memory, 128 at a time.
+constexpr int kManyQueries = 24;
+
+bool many_queries(const gar_attn_plan &plan, int batch, int groups) {
+  return groups > 0 && plan.dim <= 128 && (int64_t)(batch / groups) * (plan.q_heads / plan.kv_heads) >= kManyQueries;
+}
+int blocks_of(int rows) { return rows > 128 ? (rows + 255) / 256 : 1; }
+
+// Bytes of a call's workspace: the own rows' results, and the prefixes' as they come from either way.
+size_t prefix_bytes(const gar_attn_plan &plan, int batch, int groups) {
+  const size_t both = prefix_workspace(batch, plan.q_heads, plan.dim, nullptr, nullptr);
+  if (!many_queries(plan, batch, groups)) return both;
+  const int items = groups * plan.kv_heads * blocks_of(batch / groups * (plan.q_heads / plan.kv_heads));
+  return std::max(both, both / 2 + prefix_partials(items, plan.dim, nullptr, nullptr));
+}
+
 // The arguments that follow from the plan, the cache and what a call has set.
 int complete(const gar_attn_plan *plan, const gar_kv_cache *cache, int table_width, float scale, DecodeArgs *a) {
   // Row numbers stay below 2^31 with room for a tile past the end.
@@ -218,7 +234,7 @@ int gar_decode_attention(gar_attn_plan *plan, const gar_kv_cache *cache, const v
 int gar_prefix_attention_bytes(const gar_attn_plan *plan, int batch, int groups, size_t *bytes) {
   if (plan == nullptr || bytes == nullptr) return refuse("null plan or output");
   if (int rc = check_groups(plan, batch, groups)) return rc;
-  *bytes = prefix_workspace(batch, plan->q_heads, plan->dim, nullptr, nullptr);
+  *bytes = prefix_bytes(*plan, batch, groups);
   return GAR_OK;
 }
 
@@ -247,10 +263,11 @@ int gar_prefix_attention(gar_attn_plan *plan, const gar_kv_cache *cache, const v
   }
   const int dim = plan->dim, heads = plan->q_heads, group = heads / plan->kv_heads, share = batch / groups;
   PrefixParts parts[2];
-  if (workspace == nullptr || workspace_bytes < prefix_workspace(batch, heads, dim, static_cast<char *>(workspace), parts)) {
+  if (workspace == nullptr || workspace_bytes < prefix_bytes(*plan, batch, groups)) {
     set_error("the workspace is smaller than gar_prefix_attention_bytes");
     return GAR_ENOWS;
   }
+  const size_t half = prefix_workspace(batch, heads, dim, static_cast<char *>(workspace), parts) / 2;
   // The parts' results: the sequences' own rows, and the prefixes with a group's queries as those of one sequence.
   DecodeArgs a{};
   a.q = q, a.qb = q_batch_stride, a.qh = q_head_stride, a.q_dtype = q_dtype, a.out_dtype = GAR_F32;
@@ -265,12 +282,29 @@ int gar_prefix_attention(gar_attn_plan *plan, const gar_kv_cache *cache, const v
   prefix.share = share, prefix.heads_each = group, prefix.by_heads = divide_by((uint32_t)group);
   if (int rc = complete(plan, cache, table_width, scale, &own)) return rc;
   if (int rc = complete(plan, cache, prefix_width, scale, &prefix)) return rc;
-  if (int rc = decode(plan, prefix, stream)) return rc;
-  if (int rc = decode(plan, own, stream)) return rc;
   JoinArgs j{};
   j.parts[0] = parts[0], j.parts[1] = parts[1];
   j.out = out, j.ob = out_batch_stride, j.oh = out_head_stride, j.out_dtype = out_dtype, j.lse = lse;
   j.rows = (int64_t)batch * heads, j.dim = dim, j.heads = heads, j.group = group, j.share = share;
+  const int64_t several = 4 * element_size(out_dtype);
+  j.wide = (uintptr_t)out % several == 0 && dim % 4 == 0 && out_batch_stride % 4 == 0 && out_head_stride % 4 == 0;
+  const int rows = share * group, blocks = blocks_of(rows);
+  if (many_queries(*plan, batch, groups) && element_size(cache->dtype) == 2 && takes_mma(*cache, q, q_batch_stride, q_head_stride, q_dtype) &&
+      (int64_t)groups * plan->kv_heads * blocks * (prefix.most_rows / kKeys + 2) < 1 << 30) {
+    PrefixArgs p{};
+    p.c = *cache, p.q = q, p.qb = q_batch_stride, p.qh = q_head_stride;
+    p.table = prefix_table, p.table_stride = prefix_stride, p.lengths = prefix_lengths;
+    p.page = prefix.page, p.by_heads = prefix.by_heads, p.most_rows = prefix.most_rows;
+    p.groups = groups, p.share = share, p.heads_each = group, p.rows = rows, p.blocks = blocks;
+    p.scale_log2 = std::fabs(prefix.scale_log2), p.negate = prefix.scale_log2 < 0.f ? 0x80008000u : 0u;
+    p.ctas = plan->sms, p.device = plan->device, p.give_up = plan->give_up, p.pair = rows > 128;
+    prefix_partials(groups * plan->kv_heads * blocks, dim, static_cast<char *>(workspace) + half, &p);
+    if (int rc = prefix_mma(p, stream)) return rc;
+    if (int rc = decode(plan, own, stream)) return rc;
+    return join_partials(p, j, stream);
+  }
+  if (int rc = decode(plan, prefix, stream)) return rc;
+  if (int rc = decode(plan, own, stream)) return rc;
   return join_prefix(j, stream);
 }
 
