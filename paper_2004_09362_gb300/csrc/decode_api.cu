@@ -81,11 +81,14 @@ int check_groups(const gar_attn_plan *plan, int batch, int groups) {
 
 // Queries of a cached head and a prefix from which on the prefix goes to the tensor cores' own memory, 128 at a time.
 constexpr int kManyQueries = 24;
+constexpr int kManyItems = 1024;  // blocks of queries at most: each has 132 KB of partial results
+int blocks_of(int rows) { return rows > 128 ? (rows + 255) / 256 : 1; }
 
 bool many_queries(const gar_attn_plan &plan, int batch, int groups) {
-  return groups > 0 && plan.dim <= 128 && (int64_t)(batch / groups) * (plan.q_heads / plan.kv_heads) >= kManyQueries;
+  if (groups == 0 || plan.dim > 128) return false;
+  const int rows = batch / groups * (plan.q_heads / plan.kv_heads);
+  return rows >= kManyQueries && (int64_t)groups * plan.kv_heads * blocks_of(rows) <= kManyItems;
 }
-int blocks_of(int rows) { return rows > 128 ? (rows + 255) / 256 : 1; }
 
 // Bytes of a call's workspace: the own rows' results, and the prefixes' as they come from either way.
 size_t prefix_bytes(const gar_attn_plan &plan, int batch, int groups) {

@@ -192,13 +192,13 @@ template <typename F> int with_float(int dtype, F f) {
 // the stream is still running (programmatic dependent launch), which hides the 2 us that a launch takes;
 // it touches no memory before that kernel has completed.
 template <typename... P, typename... A>
-int launch(const char *what, void (*kernel)(P...), int64_t blocks, int threads, size_t shared, gar_stream_t stream,
+int launch(const char *what, void (*kernel)(P...), dim3 blocks, int threads, size_t shared, gar_stream_t stream,
            const A &...args) {
   cudaLaunchAttribute attribute{};
   attribute.id = cudaLaunchAttributeProgrammaticStreamSerialization;
   attribute.val.programmaticStreamSerializationAllowed = 1;
   cudaLaunchConfig_t config{};
-  config.gridDim = dim3((unsigned)blocks), config.blockDim = dim3((unsigned)threads);
+  config.gridDim = blocks, config.blockDim = dim3((unsigned)threads);
   config.dynamicSmemBytes = shared, config.stream = (cudaStream_t)stream;
   config.attrs = &attribute, config.numAttrs = 1;
   const cudaError_t e = cudaLaunchKernelEx(&config, kernel, args...);

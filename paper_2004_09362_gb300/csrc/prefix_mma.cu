@@ -5,7 +5,7 @@
 // the products.  A CTA keeps two streams of such tiles going, so that one's products run while the other's weights are computed: two
 // blocks of queries over the same rows (pair), or the even and the odd tiles of rows for one block.
 //
-//  * 2 warps copy the rows, by cp.async since pages may be of any size, to a ring of tiles in shared memory.
+//  * 4 warps copy the rows, by cp.async since pages may be of any size, to a ring of tiles in shared memory.
 //  * A thread for each stream issues its products.  S and O are in tensor memory, 128 columns each.
 //  * 4 warps for each stream turn S to P, a query to a thread: no exchange between lanes.  P goes where S was, as two 16-bit parts
 //    (its sum is 17 bits or more), 16 columns each for 32 rows.
@@ -23,9 +23,9 @@
 namespace gar {
 namespace {
 
-constexpr int kThreads = 32 * 12;  // (more than 12 warps get no more than 128 registers a thread)
-enum { kWeights = 0, kCopies = 8, kIssue = 10 };  // first warps of a part of the work
-constexpr int kCopyRows = 64;      // of a tile, copied by one warp
+constexpr int kThreads = 32 * 16;  // at 128 registers; the weights' 8 warps take 64 of them from each thread of the others
+enum { kWeights = 0, kCopies = 8, kIssue = 12 };  // first warps of a part of the work
+constexpr int kCopyRows = 32;      // of a tile, copied by one warp
 
 template <typename T> struct Parts;
 template <> struct Parts<__nv_bfloat16> {
@@ -36,12 +36,28 @@ template <> struct Parts<__half> {
   static constexpr float kLazy = 5.f, kUnit = 10.f;
 };
 
+// Two weights as a high and a low part each.  (bf16: the high part is cut off, the low one rounded: 2^-16 of the weight.)
+__device__ __forceinline__ void split_weights(float2 p, uint32_t *hi, uint32_t *lo, __nv_bfloat16) {
+  const uint32_t x = __float_as_uint(p.x), y = __float_as_uint(p.y);
+  *hi = __byte_perm(x, y, 0x7632);
+  *lo = pack2(add2(p, make_float2(__uint_as_float(x & 0xffff0000u ^ 0x80000000u), __uint_as_float(y & 0xffff0000u ^ 0x80000000u))), __nv_bfloat16());
+}
+__device__ __forceinline__ void split_weights(float2 p, uint32_t *hi, uint32_t *lo, __half) {
+  *hi = pack2(p, __half());
+  *lo = pack2(fma2(unpack2(*hi, __half()), make_float2(-1.f, -1.f), p), __half());
+}
+
+__device__ __forceinline__ float max3(float a, float b, float c) {
+  float r;
+  asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+  return r;
+}
+
 template <int DP, bool PAIR> struct PrefixShape {
   static constexpr int kTile = kKeys * DP * 2;     // bytes of a tile's keys, or values
   static constexpr int kQueries = (PAIR ? 2 : 1) * kTile;
   static constexpr int kStages = (227 * 1024 - 2048 - kQueries) / kTile < 12 ? (227 * 1024 - 2048 - kQueries) / kTile : 12;
   static constexpr int kShared = kQueries + kStages * kTile + 1024;
-  static constexpr int kFlying = kStages - 1;      // tiles on their way
 };
 
 // One part of an item: tiles [from, from + tiles) of its rows.
@@ -103,7 +119,7 @@ template <typename T, int DP, bool PAIR> __global__ void __launch_bounds__(kThre
   constexpr int N = S::kStages, ROW = DP * 2, CHUNKS = ROW / 16;
   constexpr bool BF16 = std::is_same<T, __nv_bfloat16>::value;
   extern __shared__ char shared_from[];
-  __shared__ __align__(8) uint64_t full[N], empty[N], scores[2], weights[2], values[2], drained[2];
+  __shared__ __align__(8) uint64_t full[N], empty[N], scores[2], weights[2][2], values[2], drained[2];
   __shared__ uint32_t tensor_at;
   __shared__ int late_flag;
   const uint32_t shared = (uint32_t)__cvta_generic_to_shared(shared_from) + 1023 & ~1023u;
@@ -115,9 +131,10 @@ template <typename T, int DP, bool PAIR> __global__ void __launch_bounds__(kThre
   if (warp == kIssue) tensor_alloc((uint32_t)__cvta_generic_to_shared(&tensor_at));
   if (threadIdx.x == 0) {
     late_flag = 0;
-    for (int i = 0; i < N; ++i) init_barrier(at(full[i]), 64), init_barrier(at(empty[i]), PAIR ? 2 : 1);
+    for (int i = 0; i < N; ++i) init_barrier(at(full[i]), 128), init_barrier(at(empty[i]), PAIR ? 2 : 1);
     for (int s = 0; s < 2; ++s) {
-      init_barrier(at(scores[s]), 1), init_barrier(at(weights[s]), 128), init_barrier(at(values[s]), 1);
+      init_barrier(at(scores[s]), 1), init_barrier(at(values[s]), 1);
+      init_barrier(at(weights[s][0]), 128), init_barrier(at(weights[s][1]), 128);
       init_barrier(at(drained[s]), 1);
     }
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -128,10 +145,30 @@ template <typename T, int DP, bool PAIR> __global__ void __launch_bounds__(kThre
   const uint32_t tensor = tensor_at;
   after_earlier_kernels();
 
-  PrefixWalk walk;
-  walk.start(a);
+  // Each warp's walk, kept out of the registers between parts.
+  __shared__ PrefixWalk walks[kThreads / 32];
+  {
+    PrefixWalk walk;
+    walk.start(a);
+    if (lane == 0) walks[warp] = walk;
+    __syncwarp();
+  }
   PrefixPart part;
-  if (warp >= kIssue) {
+  const auto next_part = [&] {
+    PrefixWalk walk = walks[warp];
+    const bool is = walk.next(a, &part);
+    __syncwarp();
+    if (lane == 0) walks[warp] = walk;
+    __syncwarp();
+    return is;
+  };
+  if (warp >= kCopies)
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 64;");
+  else
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 192;");
+  if (warp >= kIssue + 2) {
+    // (two warps fill up the fourth warpgroup)
+  } else if (warp >= kIssue) {
     // Issues the products of one stream.
     const int s = warp - kIssue;
     const uint32_t s_at = tensor + 256 * s, o_at = s_at + 128;
@@ -139,15 +176,16 @@ template <typename T, int DP, bool PAIR> __global__ void __launch_bounds__(kThre
     const uint32_t q_at = shared + (PAIR ? s * S::kTile : 0);
     int done = 0, pos = 0;
     bool good = true;
-    while (walk.next(a, &part)) {
+    while (next_part()) {
       asm volatile("bar.sync 2, 320;" ::: "memory");  // (the queries are there)
       if (lane == 0) {
-        for (int j = PAIR ? 0 : s; good && j < part.tiles; j += PAIR ? 1 : 2) {
-          const int k = pos + 2 * j, v = k + 1;
-          good = j < a.give_up && wait_phase(at(full[k % N]), k / N & 1, late) && (done == 0 || wait_phase(at(values[s]), done - 1 & 1, late));
-          if (!good) break;
+        constexpr int STEP = PAIR ? 1 : 2;
+        const auto scores_of = [&](int j) {
+          const int k = pos + 2 * j;
+          if (j >= a.give_up || !wait_phase(at(full[k % N]), k / N & 1, late)) return false;
+          shared_for_mma();
           tensor_after_sync();
-          const uint32_t k_at = ring + k % N * S::kTile, v_at = ring + v % N * S::kTile;
+          const uint32_t k_at = ring + k % N * S::kTile;
 #pragma unroll
           for (int i = 0; i < DP / 16; ++i) {
             const uint32_t off = i / 4 * (kKeys * 128) + i % 4 * 32;
@@ -155,19 +193,34 @@ template <typename T, int DP, bool PAIR> __global__ void __launch_bounds__(kThre
           }
           commit(at(scores[s]));
           commit(at(empty[k % N]));
-          good = wait_phase(at(weights[s]), done & 1, late) && wait_phase(at(full[v % N]), v / N & 1, late);
-          if (!good) break;
-          tensor_after_sync();
+          return true;
+        };
+        const int first = PAIR ? 0 : s;
+        if (good && first < part.tiles) good = scores_of(first);
+        for (int j = first; good && j < part.tiles; j += STEP) {
+          const int v = pos + 2 * j + 1;
+          const uint32_t v_at = ring + v % N * S::kTile;
+          good = wait_phase(at(full[v % N]), v / N & 1, late);
+          shared_for_mma();
 #pragma unroll
-          for (int i = 0; i < kKeys / 16; ++i) {
-            const uint32_t p_at = s_at + i / 2 * 32 + i % 2 * 8;
-            const uint64_t b = operand_mn_major(v_at + i * 2048, kKeys * 128);
-            product_tensor(o_at, p_at, b, values_kind, j > (PAIR ? 0 : s) || i > 0);
-            product_tensor(o_at, p_at + 16, b, values_kind, true);
+          for (int half = 0; half < 2; ++half) {
+            good = good && wait_phase(at(weights[s][half]), done & 1, late);
+            if (!good) break;
+            tensor_after_sync();
+#pragma unroll
+            for (int i = half * (kKeys / 32); i < (half + 1) * (kKeys / 32); ++i) {
+              const uint32_t p_at = s_at + i / 2 * 32 + i % 2 * 8;
+              const uint64_t b = operand_mn_major(v_at + i * 2048, kKeys * 128);
+              product_tensor(o_at, p_at, b, values_kind, j > first || i > 0);
+              product_tensor(o_at, p_at + 16, b, values_kind, true);
+            }
           }
+          if (!good) break;
           commit(at(values[s]));
           commit(at(empty[v % N]));
           ++done;
+          // The next scores go where these weights are: a thread's products run in the order that they are issued in.
+          if (j + STEP < part.tiles) good = scores_of(j + STEP);
         }
         if (!good) *late = 1;
       }
@@ -182,37 +235,37 @@ template <typename T, int DP, bool PAIR> __global__ void __launch_bounds__(kThre
     }
     __syncwarp();
   } else if (warp >= kCopies) {
-    // Copies tiles: a warp half of the rows of each.
+    // Copies tiles: a warp a quarter of the rows of each.
     const int w = warp - kCopies;
     const gar_kv_cache &c = a.c;
     const char *const kp = static_cast<const char *>(c.k), *const vp = static_cast<const char *>(c.v);
     int pos = 0;       // the next tile's place in the ring
-    const auto signal = [&](int left) {
-      // Of the last kFlying + 1 tiles the oldest but `left` are there.
-      if (left == S::kFlying)
-        asm volatile("cp.async.wait_group %0;" ::"n"(S::kFlying) : "memory");
-      else
-        asm volatile("cp.async.wait_group 0;" ::: "memory");
-      shared_for_mma();
-    };
-    int signalled = 0;
     bool good = true;
     constexpr int PER = 32 / CHUNKS;  // rows that the warp copies at a time
     const int chunk = lane % CHUNKS, sub = lane / CHUNKS;
-    while (good && walk.next(a, &part)) {
-      const auto find = [&](int tile, int half) {
-        const int n = (part.from + tile) * kKeys + w * kCopyRows + half * 32 + lane;
-        if (tile >= part.tiles || n >= part.rows) return (int64_t)-1;
-        const int p = (int)a.page((uint32_t)n), page = a.table[part.g * a.table_stride + p];
-        if ((unsigned)page >= (uint64_t)c.pages) {
+    while (good && next_part()) {
+      // The page of this lane's row of a tile: looked up a tile before it is used, and checked only then.
+      struct Found {
+        int page, in;  // in: the row of the page, or -1
+      };
+      const auto look = [&](int tile) {
+        const int n = (part.from + tile) * kKeys + w * kCopyRows + lane;
+        if (tile >= part.tiles || n >= part.rows) return Found{0, -1};
+        const int p = (int)a.page((uint32_t)n);
+        return Found{a.table[part.g * a.table_stride + p], n - p * c.page_size};
+      };
+      const auto place = [&](Found f) {
+        if (f.in < 0) return (int64_t)-1;
+        if ((unsigned)f.page >= (uint64_t)c.pages) {
           if (c.status) atomicOr(c.status, GAR_KV_BAD_PAGE);
           return (int64_t)-1;
         }
-        return page * c.page_stride + part.kv * c.head_stride + (n - p * c.page_size) * c.token_stride;
+        return f.page * c.page_stride + part.kv * c.head_stride + f.in * c.token_stride;
       };
-      int64_t row[2] = {find(0, 0), find(0, 1)};
+      Found found = look(0);
       for (int j = 0; good && j < part.tiles; ++j) {
-        const int64_t later[2] = {find(j + 1, 0), find(j + 1, 1)};
+        const int64_t row = place(found);
+        found = look(j + 1);
 #pragma unroll
         for (int half = 0; half < 2; ++half) {  // keys, values
           const int stage = pos % N;
@@ -224,25 +277,17 @@ template <typename T, int DP, bool PAIR> __global__ void __launch_bounds__(kThre
 #pragma unroll
           for (int r = 0; r < kCopyRows; r += PER) {
             const int to = r + sub, line_row = w * kCopyRows + to;
-            const int64_t x = __shfl_sync(~0u, row[r / 32], to & 31);
+            const int64_t x = __shfl_sync(~0u, row, to);
             const bool in = x >= 0 && chunk * 8 < c.dim;
             copy_async<16>(tile + chunk / 8 * (kKeys * 128) + line_row * 128 + ((chunk ^ line_row) & 7) * 16,
                            in ? base + x * 2 + chunk * 16 : base, in);
           }
-          asm volatile("cp.async.commit_group;" ::: "memory");
+          arrive_after_copies(at(full[stage]));
           ++pos;
-          if (pos - signalled > S::kFlying) {
-            signal(S::kFlying);
-            arrive(at(full[signalled % N]));
-            ++signalled;
-          }
         }
-        row[0] = later[0], row[1] = later[1];
       }
     }
-    signal(0);
-    if (good)
-      for (; signalled < pos; ++signalled) arrive(at(full[signalled % N]));
+    asm volatile("cp.async.wait_all;" ::: "memory");
   } else {
     // Turns scores to weights.
     const int s = warp / 4, quarter = warp & 3, row = quarter * 32 + lane;
@@ -250,20 +295,31 @@ template <typename T, int DP, bool PAIR> __global__ void __launch_bounds__(kThre
     int done = 0;
     bool good = true;
     // (After a wait that ran out the barriers of the parts that are left are still met.)
-    while (walk.next(a, &part)) {
+    while (next_part()) {
       asm volatile("bar.sync 1, 256;" ::: "memory");  // (both streams are done with the last part's queries)
       // Queries: row m is that of the prefix's sequence m / heads_each.
       const int row0 = part.block * (PAIR ? 256 : 128), many = min(a.rows - row0, PAIR ? 256 : 128);
-      for (int i = threadIdx.x; i < (PAIR ? 256 : 128) * CHUNKS; i += 256) {
-        const int r = i / CHUNKS, chunk = i % CHUNKS, m = row0 + r;
-        uint4 x = make_uint4(0, 0, 0, 0);
-        if (r < many && chunk * 8 < a.c.dim) {
-          const int b = (int)a.by_heads((uint32_t)m), h = part.kv * a.heads_each + (m - b * a.heads_each);
-          x = *reinterpret_cast<const uint4 *>(static_cast<const char *>(a.q) +
-                                               2 * (((int64_t)part.g * a.share + b) * a.qb + h * a.qh) + chunk * 16);
-          x.x ^= a.negate, x.y ^= a.negate, x.z ^= a.negate, x.w ^= a.negate;
+      constexpr int ALL = (PAIR ? 256 : 128) * CHUNKS / 256, AT_ONCE = 8;
+      static_assert(ALL % 4 == 0, "whole rounds");
+#pragma unroll 1
+      for (int i0 = 0; i0 < ALL; i0 += ALL < AT_ONCE ? ALL : AT_ONCE) {
+        uint4 x[ALL < AT_ONCE ? ALL : AT_ONCE];
+#pragma unroll
+        for (int i = 0; i < (ALL < AT_ONCE ? ALL : AT_ONCE); ++i) {
+          const int at_chunk = (i0 + i) * 256 + threadIdx.x, r = at_chunk / CHUNKS, chunk = at_chunk % CHUNKS, m = row0 + r;
+          x[i] = make_uint4(0, 0, 0, 0);
+          if (r < many && chunk * 8 < a.c.dim) {
+            const int b = (int)a.by_heads((uint32_t)m), h = part.kv * a.heads_each + (m - b * a.heads_each);
+            x[i] = *reinterpret_cast<const uint4 *>(static_cast<const char *>(a.q) +
+                                                    2 * (((int64_t)part.g * a.share + b) * a.qb + h * a.qh) + chunk * 16);
+          }
         }
-        *reinterpret_cast<uint4 *>(shared_p + r / 128 * S::kTile + chunk / 8 * (kKeys * 128) + r % 128 * 128 + ((chunk ^ r) & 7) * 16) = x;
+#pragma unroll
+        for (int i = 0; i < (ALL < AT_ONCE ? ALL : AT_ONCE); ++i) {
+          const int at_chunk = (i0 + i) * 256 + threadIdx.x, r = at_chunk / CHUNKS, chunk = at_chunk % CHUNKS;
+          x[i].x ^= a.negate, x[i].y ^= a.negate, x[i].z ^= a.negate, x[i].w ^= a.negate;
+          *reinterpret_cast<uint4 *>(shared_p + r / 128 * S::kTile + chunk / 8 * (kKeys * 128) + r % 128 * 128 + ((chunk ^ r) & 7) * 16) = x[i];
+        }
       }
       shared_for_mma();
       asm volatile("bar.sync 2, 320;" ::: "memory");
@@ -278,24 +334,23 @@ template <typename T, int DP, bool PAIR> __global__ void __launch_bounds__(kThre
         tensor_after_sync();
         if (!idle) {
           const int n = part.rows - (part.from + j) * kKeys;  // rows of the tile that exist: n or all
-          float top = -INFINITY;
+          uint32_t x[4][32];
 #pragma unroll
-          for (int c = 0; c < kKeys; c += 32) {
-            uint32_t x[32];
-            tensor_load32(x, s_at + c);
-            wait_tensor_loads(x);
-            float part_top[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
-            if (n - c >= 32) {
+          for (int c = 0; c < 4; ++c) tensor_load32(x[c], s_at + 32 * c);
+          wait_tensor_loads(x[0]);
 #pragma unroll
-              for (int i = 0; i < 32; ++i) part_top[i % 4] = fmaxf(part_top[i % 4], __uint_as_float(x[i]));
-            } else {
+          for (int c = 1; c < 4; ++c) loaded(x[c]);
+          if (n < kKeys) {
 #pragma unroll
-              for (int i = 0; i < 32; ++i)
-                if (c + i < n) part_top[i % 4] = fmaxf(part_top[i % 4], __uint_as_float(x[i]));
-            }
-            top = fmaxf(top, fmaxf(fmaxf(part_top[0], part_top[1]), fmaxf(part_top[2], part_top[3])));
+            for (int i = 0; i < kKeys; ++i)
+              if (i >= n) x[i / 32][i % 32] = 0xff800000u;  // -infinity: its weight is 0
           }
-          top *= a.scale_log2;
+          float tops[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll
+          for (int i = 0; i < 32; i += 2)
+#pragma unroll
+            for (int c = 0; c < 4; ++c) tops[c] = max3(tops[c], __uint_as_float(x[c][i]), __uint_as_float(x[c][i + 1]));
+          const float top = fmaxf(max3(tops[0], tops[1], tops[2]), tops[3]) * a.scale_log2;
           const bool grown = top > m + Parts<T>::kLazy;
           if (__any_sync(~0u, grown)) {
             const float shrink = grown ? exp2_fast(m - top) : 1.f;  // (0 at first)
@@ -303,39 +358,42 @@ template <typename T, int DP, bool PAIR> __global__ void __launch_bounds__(kThre
             l *= shrink;
             if (!first) {
 #pragma unroll 1
-              for (int c = 0; c < DP; c += 32) {
-                uint32_t x[32];
-                tensor_load32(x, o_at + c);
-                wait_tensor_loads(x);
+              for (int c = 0; c < DP; c += 8) {
+                uint32_t y[8];
+                tensor_load8(y, o_at + c);
 #pragma unroll
-                for (int i = 0; i < 32; ++i) x[i] = __float_as_uint(__uint_as_float(x[i]) * shrink);
-                tensor_store32(o_at + c, x);
+                for (int i = 0; i < 8; ++i) y[i] = __float_as_uint(__uint_as_float(y[i]) * shrink);
+                tensor_store8(o_at + c, y);
               }
             }
           }
           const float off = Parts<T>::kUnit - offset_of(m);
-          float sum[4] = {};
+          const float2 scale2 = make_float2(a.scale_log2, a.scale_log2), off2 = make_float2(off, off);
+          float2 sum[2] = {};
 #pragma unroll
-          for (int c = 0; c < kKeys; c += 32) {
-            uint32_t x[32], y[32];
-            tensor_load32(x, s_at + c);
-            wait_tensor_loads(x);
-            const bool whole = n - c >= 32;
+          for (int c = 0; c < 4; ++c) {
+            uint32_t y[32];
 #pragma unroll
             for (int i = 0; i < 32; i += 2) {
-              float p = exp2_fast(fmaf(__uint_as_float(x[i]), a.scale_log2, off)), q = exp2_fast(fmaf(__uint_as_float(x[i + 1]), a.scale_log2, off));
-              if (!whole) p = c + i < n ? p : 0.f, q = c + i + 1 < n ? q : 0.f;
-              sum[i % 4] += p, sum[i % 4 + 1] += q;
-              split<T>(p, q, &y[i / 2], &y[16 + i / 2]);
+              float2 p = fma2(make_float2(__uint_as_float(x[c][i]), __uint_as_float(x[c][i + 1])), scale2, off2);
+              p.x = exp2_fast(p.x), p.y = exp2_fast(p.y);
+              sum[i / 2 % 2] = add2(sum[i / 2 % 2], p);
+              split_weights(p, &y[i / 2], &y[16 + i / 2], T());
             }
-            tensor_store32(s_at + c, y);
+            tensor_store32(s_at + 32 * c, y);
+            if (c == 1) {  // half of the products can begin
+              wait_tensor_stores();
+              tensor_before_sync();
+              arrive(at(weights[s][0]));
+            }
           }
-          l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+          l += (sum[0].x + sum[1].x) + (sum[0].y + sum[1].y);
           wait_tensor_stores();
         }
+        if (idle) arrive(at(weights[s][0]));
         first = false;
         tensor_before_sync();
-        arrive(at(weights[s]));
+        arrive(at(weights[s][1]));
       }
       if (!good) continue;
       // This part's result, in units of one.
@@ -372,10 +430,13 @@ template <typename T, int DP, bool PAIR> __global__ void __launch_bounds__(kThre
   if (threadIdx.x == 0 && late_flag && a.c.status) atomicOr(a.c.status, GAR_KV_TIMEOUT);
 }
 
-constexpr int kJoinThreads = 256, kJoinRows = 32;
+constexpr int kJoinThreads = 256, kJoinRows = 32, kJoinChannels = 32;
 
-// Joins the parts of 32 queries of an item, and their sequences' own rows': a query to a lane, four channels at a time to a warp.
+// Joins the parts of 32 queries of an item and their sequences' own rows' results, for 32 channels: a query to a lane, four
+// channels to a warp.
 template <int DP> __global__ void __launch_bounds__(kJoinThreads) join_kernel(const PrefixArgs a, const JoinArgs j) {
+  extern __shared__ float factors[];  // [part][query]: what the part counts for
+  __shared__ float tops[kJoinThreads / 32][32], sums[kJoinThreads / 32][32];
   after_earlier_kernels();
   const int lane = threadIdx.x & 31, warp = threadIdx.x / 32, per_item = (a.pair ? 256 : 128) / kJoinRows;
   const int item = blockIdx.x / per_item, items = a.c.heads * a.blocks, g = item / items, in_group = item - g * items;
@@ -384,62 +445,71 @@ template <int DP> __global__ void __launch_bounds__(kJoinThreads) join_kernel(co
   if (row - lane >= a.rows) return;
   const int2 line = prefix_line(a, g, false);
   const int per = share_of(line.x, a.ctas), tiles = prefix_tiles(prefix_rows(a, g, false)), begin = line.y + in_group * tiles;
-  const int first = tiles ? begin / per : 0, parts = tiles ? (begin + tiles - 1) / per - first + 1 : 0;
-  const int subs = a.pair ? 1 : 2, sub0 = a.pair ? in_block / 128 : 0, in_sub = in_block % 128 + lane;
+  const int first = tiles ? begin / per : 0, subs = a.pair ? 1 : 2;
+  const int parts = tiles ? ((begin + tiles - 1) / per - first + 1) * subs : 0;
+  const int sub0 = a.pair ? in_block / 128 : 0, in_sub = in_block % 128 + lane, step = a.pair ? 2 : 1;  // places of 128 rows
   const bool there = row < a.rows;
   const int i = (int)a.by_heads((uint32_t)min(row, a.rows - 1)), h = kv * a.heads_each + (min(row, a.rows - 1) - i * a.heads_each);
   const int64_t b = (int64_t)g * a.share + i, own_at = b * j.heads + h;
   const float own = __ldcg(j.parts[0].lse + own_at) * 1.44269504088896341f;
-  const float2 *const ml = a.ml + ((int64_t)first + item) * 256 + sub0 * 128 + in_sub;
+  const float2 *const ml = a.ml + (((int64_t)first + item) * 2 + sub0) * 128 + in_sub;
   float top = own;
-  for (int p = 0; p < parts; ++p)
-    for (int s = 0; s < subs; ++s) top = fmaxf(top, __ldcg(ml + p * 256 + s * 128).x);
-  const float off = offset_of(top), own_weight = exp2_fast(own - off);
-  float l = own_weight;
-  for (int p = 0; p < parts; ++p)
-    for (int s = 0; s < subs; ++s) {
-      const float2 x = __ldcg(ml + p * 256 + s * 128);
-      l += exp2_fast(x.x - off) * x.y;
-    }
-  const float inverse = l == 0.f ? 0.f : 1.f / l;
-  if (warp == 0 && there && j.lse) j.lse[own_at] = l == 0.f ? -INFINITY : (off + log2f(l)) * 0.693147180559945f;
-  for (int d = warp * 4; d < j.dim; d += kJoinThreads / 32 * 4) {
-    float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
-    const float *const q = j.parts[0].out + own_at * j.parts[0].row + d;
-    if (own_weight > 0.f || own_weight != own_weight) {
-      const float4 y = __ldcg(reinterpret_cast<const float4 *>(q));
-      x.x = own_weight * y.x, x.y = own_weight * y.y, x.z = own_weight * y.z, x.w = own_weight * y.w;
-    }
-    const float4 *const o = reinterpret_cast<const float4 *>(a.o) + (((int64_t)first + item) * 2 + sub0) * (DP / 4 * 128) + d / 4 * 128 + in_sub;
 #pragma unroll 4
-    for (int p = 0; p < parts * subs; ++p) {
-      const int at = subs == 2 ? p : 2 * p;
-      const float2 v = __ldcg(ml + at * 128);
-      const float f = exp2_fast(v.x - off);
-      const float4 y = __ldcg(o + (int64_t)at * (DP / 4 * 128));
-      if (!(f == 0.f)) x.x += f * y.x, x.y += f * y.y, x.z += f * y.z, x.w += f * y.w;
-    }
-    x.x *= inverse, x.y *= inverse, x.z *= inverse, x.w *= inverse;
-    if (!there) continue;
-    const int64_t at = b * j.ob + h * j.oh + d;
-    const float z[4] = {x.x, x.y, x.z, x.w};
-    if (j.out_dtype == GAR_F32) {
-      float *const out = static_cast<float *>(j.out) + at;
-      if (j.wide)
-        *reinterpret_cast<float4 *>(out) = x;
+  for (int p = warp; p < parts; p += kJoinThreads / 32) top = fmaxf(top, __ldcg(ml + p * step * 128).x);
+  tops[warp][lane] = top;
+  __syncthreads();
+#pragma unroll
+  for (int w = 0; w < kJoinThreads / 32; ++w) top = fmaxf(top, tops[w][lane]);
+  const float off = offset_of(top), own_weight = exp2_fast(own - off);
+  float l = 0.f;
+#pragma unroll 4
+  for (int p = warp; p < parts; p += kJoinThreads / 32) {
+    const float2 x = __ldcg(ml + p * step * 128);
+    const float f = exp2_fast(x.x - off);
+    factors[p * 32 + lane] = f;
+    l += f * x.y;
+  }
+  sums[warp][lane] = l;
+  __syncthreads();
+  l = own_weight;
+#pragma unroll
+  for (int w = 0; w < kJoinThreads / 32; ++w) l += sums[w][lane];
+  const float inverse = l == 0.f ? 0.f : 1.f / l;
+  if (warp == 0 && blockIdx.y == 0 && there && j.lse) j.lse[own_at] = l == 0.f ? -INFINITY : (off + log2f(l)) * 0.693147180559945f;
+  const int d = blockIdx.y * kJoinChannels + warp * 4;
+  if (d >= j.dim) return;
+  float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
+  if (!(own_weight == 0.f)) {
+    const float4 y = __ldcg(reinterpret_cast<const float4 *>(j.parts[0].out + own_at * j.parts[0].row + d));
+    x.x = own_weight * y.x, x.y = own_weight * y.y, x.z = own_weight * y.z, x.w = own_weight * y.w;
+  }
+  const float4 *const o = reinterpret_cast<const float4 *>(a.o) + ((((int64_t)first + item) * 2 + sub0) * (DP / 4) + d / 4) * 128 + in_sub;
+#pragma unroll 8
+  for (int p = 0; p < parts; ++p) {
+    const float f = factors[p * 32 + lane];
+    const float4 y = __ldcg(o + (int64_t)p * step * (DP / 4 * 128));
+    // (a part without rows has left no o)
+    if (!(f == 0.f)) x.x += f * y.x, x.y += f * y.y, x.z += f * y.z, x.w += f * y.w;
+  }
+  if (!there) return;
+  const float z[4] = {x.x * inverse, x.y * inverse, x.z * inverse, x.w * inverse};
+  const int64_t at = b * j.ob + h * j.oh + d;
+  if (j.out_dtype == GAR_F32) {
+    float *const out = static_cast<float *>(j.out) + at;
+    if (j.wide)
+      *reinterpret_cast<float4 *>(out) = make_float4(z[0], z[1], z[2], z[3]);
+    else
+      for (int k = 0; k < 4 && d + k < j.dim; ++k) out[k] = z[k];
+  } else if (j.wide) {
+    const float2 u = make_float2(z[0], z[1]), v = make_float2(z[2], z[3]);
+    *reinterpret_cast<uint2 *>(static_cast<char *>(j.out) + 2 * at) =
+        j.out_dtype == GAR_BF16 ? make_uint2(pack2(u, __nv_bfloat16()), pack2(v, __nv_bfloat16())) : make_uint2(pack2(u, __half()), pack2(v, __half()));
+  } else {
+    for (int k = 0; k < 4 && d + k < j.dim; ++k) {
+      if (j.out_dtype == GAR_BF16)
+        static_cast<__nv_bfloat16 *>(j.out)[at + k] = from_f32<__nv_bfloat16>(z[k]);
       else
-        for (int k = 0; k < 4 && d + k < j.dim; ++k) out[k] = z[k];
-    } else if (j.wide) {
-      const uint2 y = j.out_dtype == GAR_BF16 ? make_uint2(pack2(make_float2(x.x, x.y), __nv_bfloat16()), pack2(make_float2(x.z, x.w), __nv_bfloat16()))
-                                              : make_uint2(pack2(make_float2(x.x, x.y), __half()), pack2(make_float2(x.z, x.w), __half()));
-      *reinterpret_cast<uint2 *>(static_cast<char *>(j.out) + 2 * at) = y;
-    } else {
-      for (int k = 0; k < 4 && d + k < j.dim; ++k) {
-        if (j.out_dtype == GAR_BF16)
-          static_cast<__nv_bfloat16 *>(j.out)[at + k] = from_f32<__nv_bfloat16>(z[k]);
-        else
-          static_cast<__half *>(j.out)[at + k] = from_f32<__half>(z[k]);
-      }
+        static_cast<__half *>(j.out)[at + k] = from_f32<__half>(z[k]);
     }
   }
 }
@@ -474,7 +544,9 @@ int prefix_mma(const PrefixArgs &a, gar_stream_t stream) {
 
 int join_partials(const PrefixArgs &a, const JoinArgs &j, gar_stream_t stream) {
   const int64_t blocks = (int64_t)a.groups * a.c.heads * a.blocks * ((a.pair ? 256 : 128) / kJoinRows);
-  return launch("gar_prefix_attention", a.c.dim <= 64 ? join_kernel<64> : join_kernel<128>, blocks, kJoinThreads, 0, stream, a, j);
+  return launch("gar_prefix_attention", a.c.dim <= 64 ? join_kernel<64> : join_kernel<128>,
+                dim3((unsigned)blocks, (unsigned)((a.c.dim + kJoinChannels - 1) / kJoinChannels)), kJoinThreads,
+                (size_t)(a.pair ? 1 : 2) * a.ctas * 32 * sizeof(float), stream, a, j);
 }
 
 }  // namespace gar
