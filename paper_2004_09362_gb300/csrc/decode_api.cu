@@ -36,7 +36,7 @@ bool takes_mma(const gar_kv_cache &c, const void *q, int64_t q_batch_stride, int
 
 }  // namespace
 
-bool box_map(const gar_kv_cache &c, void *base, int rows, CUtensorMap *map) {
+bool box_map(const gar_kv_cache &c, void *base, int rows, bool all_lines, CUtensorMap *map) {
   using Encode = CUresult (*)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *,
                               const cuuint64_t *, const cuuint32_t *, const cuuint32_t *, CUtensorMapInterleave,
                               CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
@@ -52,7 +52,7 @@ bool box_map(const gar_kv_cache &c, void *base, int rows, CUtensorMap *map) {
   const cuuint64_t extent[5] = {line, (cuuint64_t)c.page_size, lines, (cuuint64_t)c.heads, (cuuint64_t)c.pages};
   const cuuint64_t stride[4] = {(cuuint64_t)c.token_stride * size, line, (cuuint64_t)c.head_stride * size,
                                 (cuuint64_t)c.page_stride * size};
-  const cuuint32_t box[5] = {line, (cuuint32_t)rows, lines, 1, 1}, step[5] = {1, 1, 1, 1, 1};
+  const cuuint32_t box[5] = {line, (cuuint32_t)rows, all_lines ? lines : 1, 1, 1}, step[5] = {1, 1, 1, 1, 1};
   return encode(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 5, base, extent, stride, box, step, CU_TENSOR_MAP_INTERLEAVE_NONE,
                 CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
@@ -299,10 +299,17 @@ int gar_prefix_attention(gar_attn_plan *plan, const gar_kv_cache *cache, const v
     p.table = prefix_table, p.table_stride = prefix_stride, p.lengths = prefix_lengths;
     p.page = prefix.page, p.by_heads = prefix.by_heads, p.most_rows = prefix.most_rows;
     p.groups = groups, p.share = share, p.heads_each = group, p.rows = rows, p.blocks = blocks;
-    p.scale_log2 = std::fabs(prefix.scale_log2), p.negate = prefix.scale_log2 < 0.f ? 0x80008000u : 0u;
+    // (not zero: rows past the end have scores of -infinity)
+    p.scale_log2 = std::max(std::fabs(prefix.scale_log2), 1e-37f), p.negate = prefix.scale_log2 < 0.f ? 0x80008000u : 0u;
     p.ctas = plan->sms, p.device = plan->device, p.give_up = plan->give_up, p.pair = rows > 128;
     prefix_partials(groups * plan->kv_heads * blocks, dim, static_cast<char *>(workspace) + half, &p);
-    if (int rc = prefix_mma(p, stream)) return rc;
+    // Boxes of 8 rows and more that tiles consist of.
+    for (int r = kKeys; r >= 8 && p.box == 0; r /= 2)
+      if (cache->page_size % r == 0 && (r == kKeys || cache->page_size == r)) p.box = r;
+    CUtensorMap maps[2] = {};
+    if (dim % 64 || p.box == 0 || !box_map(*cache, cache->k, p.box, false, &maps[0]) || !box_map(*cache, cache->v, p.box, false, &maps[1]))
+      p.box = 0;
+    if (int rc = prefix_mma(p, maps, stream)) return rc;
     if (int rc = decode(plan, own, stream)) return rc;
     return join_partials(p, j, stream);
   }

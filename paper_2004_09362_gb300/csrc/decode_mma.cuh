@@ -812,9 +812,9 @@ __global__ void __launch_bounds__(32 * MmaShape<C, DP, NG>::kWarps, 1)
       wait_barrier(barrier + 8 * (i < S::kStages ? i : i - S::kStages), i < S::kStages ? parity : parity ^ 1);
 }
 
-// A map of the cache's bytes as [pages][heads][lines of a row][page_size][128], boxes of the lines of `rows` rows;
-// false where it has none.
-bool box_map(const gar_kv_cache &c, void *base, int rows, CUtensorMap *map);
+// A map of the cache's bytes as [pages][heads][lines of a row][page_size][128], boxes of the lines (or one line) of `rows`
+// rows; false where it has none.
+bool box_map(const gar_kv_cache &c, void *base, int rows, bool all_lines, CUtensorMap *map);
 
 template <typename C, int DP, int NG, bool Q32> int launch_mma(DecodeArgs a, int sms, gar_stream_t stream) {
   using S = MmaShape<C, DP, NG>;
@@ -836,8 +836,8 @@ template <typename C, int DP, int NG, bool Q32> int launch_mma(DecodeArgs a, int
     return launch("gar_decode_attention", kernel, sms, 32 * S::kWarps, S::kShared, stream, a, maps[0], maps[1]);
   };
   if constexpr (S::kBoxes)
-    if (a.c.dim == DP && a.c.page_size % S::KT == 0 && box_map(a.c, a.c.k, S::KT, &maps[0]) &&
-        box_map(a.c, a.c.v, S::KT, &maps[1]))
+    if (a.c.dim == DP && a.c.page_size % S::KT == 0 && box_map(a.c, a.c.k, S::KT, true, &maps[0]) &&
+        box_map(a.c, a.c.v, S::KT, true, &maps[1]))
       return run(std::true_type{});
   return run(std::false_type{});
 }

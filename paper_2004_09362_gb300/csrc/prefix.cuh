@@ -1,6 +1,8 @@
 // Attention over shared prefixes: its parts' results and their join.
 #pragma once
 
+#include <cuda.h>
+
 #include "gar_device.cuh"
 
 namespace gar {
@@ -24,6 +26,7 @@ struct PrefixArgs {
   float scale_log2;        // of the scores, not negative: q is negated where it was
   uint32_t negate;         // bits of q that are turned over
   int ctas, device, give_up;
+  int box;                 // rows of the boxes that a tile can be copied in, or 0
   bool pair;
   // Partial results of CTA i and item j at place i + j: [2][128] (m, l) and [2][channels / 4][128][4] o.
   float2 *ml;
@@ -74,7 +77,7 @@ int join_prefix(const JoinArgs &a, gar_stream_t stream);
 
 // Places for partial results: of every CTA, and one for each item beyond an item that a CTA begins with.
 size_t prefix_partials(int items, int dim, char *base, PrefixArgs *a);
-int prefix_mma(const PrefixArgs &a, gar_stream_t stream);
+int prefix_mma(const PrefixArgs &a, const CUtensorMap (&maps)[2], gar_stream_t stream);
 int join_partials(const PrefixArgs &a, const JoinArgs &j, gar_stream_t stream);
 
 }  // namespace gar

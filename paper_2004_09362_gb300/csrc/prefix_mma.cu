@@ -47,6 +47,14 @@ __device__ __forceinline__ void split_weights(float2 p, uint32_t *hi, uint32_t *
   *lo = pack2(fma2(unpack2(*hi, __half()), make_float2(-1.f, -1.f), p), __half());
 }
 
+// One line of a box of rows of the cache.
+__device__ __forceinline__ void copy_line(uint32_t to, const CUtensorMap *map, int row, int line, int head, int page, uint32_t barrier) {
+  asm volatile(
+      "cp.async.bulk.tensor.5d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5, %6}], "
+      "[%7];" ::"r"(to), "l"(map), "r"(0), "r"(row), "r"(line), "r"(head), "r"(page), "r"(barrier)
+      : "memory");
+}
+
 __device__ __forceinline__ float max3(float a, float b, float c) {
   float r;
   asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
@@ -57,6 +65,7 @@ template <int DP, bool PAIR> struct PrefixShape {
   static constexpr int kTile = kKeys * DP * 2;     // bytes of a tile's keys, or values
   static constexpr int kQueries = (PAIR ? 2 : 1) * kTile;
   static constexpr int kStages = (227 * 1024 - 2048 - kQueries) / kTile < 12 ? (227 * 1024 - 2048 - kQueries) / kTile : 12;
+  static_assert(PAIR || kStages % 2 == 0, "two rings");
   static constexpr int kShared = kQueries + kStages * kTile + 1024;
 };
 
@@ -114,14 +123,18 @@ struct PrefixWalk {
   }
 };
 
-template <typename T, int DP, bool PAIR> __global__ void __launch_bounds__(kThreads, 1) prefix_kernel(const PrefixArgs a) {
+template <typename T, int DP, bool PAIR> __global__ void __launch_bounds__(kThreads, 1)
+    prefix_kernel(const PrefixArgs a, const __grid_constant__ CUtensorMap k_map, const __grid_constant__ CUtensorMap v_map) {
   using S = PrefixShape<DP, PAIR>;
-  constexpr int N = S::kStages, ROW = DP * 2, CHUNKS = ROW / 16;
+  // The ring's stages: both streams read each tile of it, or each stream has half of the stages for its own.  (With one ring
+  // for both, a stream that is a lap ahead of the other would take that one's tile, not there yet, for its own: a barrier tells a phase
+  // from the next, but not from the one after that.)
+  constexpr int N = S::kStages, RING = PAIR ? N : N / 2, ROW = DP * 2, CHUNKS = ROW / 16;
   constexpr bool BF16 = std::is_same<T, __nv_bfloat16>::value;
   extern __shared__ char shared_from[];
   __shared__ __align__(8) uint64_t full[N], empty[N], scores[2], weights[2][2], values[2], drained[2];
   __shared__ uint32_t tensor_at;
-  __shared__ int late_flag;
+  __shared__ int late_flag, copied[2];
   const uint32_t shared = (uint32_t)__cvta_generic_to_shared(shared_from) + 1023 & ~1023u;
   char *const shared_p = shared_from + (shared - (uint32_t)__cvta_generic_to_shared(shared_from));
   const uint32_t ring = shared + S::kQueries;
@@ -131,10 +144,10 @@ template <typename T, int DP, bool PAIR> __global__ void __launch_bounds__(kThre
   if (warp == kIssue) tensor_alloc((uint32_t)__cvta_generic_to_shared(&tensor_at));
   if (threadIdx.x == 0) {
     late_flag = 0;
-    for (int i = 0; i < N; ++i) init_barrier(at(full[i]), 128), init_barrier(at(empty[i]), PAIR ? 2 : 1);
+    for (int i = 0; i < N; ++i) init_barrier(at(full[i]), a.box > 0 ? 4 : 128), init_barrier(at(empty[i]), PAIR ? 2 : 1);
     for (int s = 0; s < 2; ++s) {
       init_barrier(at(scores[s]), 1), init_barrier(at(values[s]), 1);
-      init_barrier(at(weights[s][0]), 128), init_barrier(at(weights[s][1]), 128);
+      init_barrier(at(weights[s][0]), 4), init_barrier(at(weights[s][1]), 4);
       init_barrier(at(drained[s]), 1);
     }
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -174,33 +187,35 @@ template <typename T, int DP, bool PAIR> __global__ void __launch_bounds__(kThre
     const uint32_t s_at = tensor + 256 * s, o_at = s_at + 128;
     constexpr uint32_t scores_kind = product_of(BF16, kKeys, false), values_kind = product_of(BF16, DP, true);
     const uint32_t q_at = shared + (PAIR ? s * S::kTile : 0);
-    int done = 0, pos = 0;
+    const int stage0 = PAIR ? 0 : s * RING;
+    int done = 0, pos = 0;  // pos: the stream's next tile of keys or values
     bool good = true;
     while (next_part()) {
       asm volatile("bar.sync 2, 320;" ::: "memory");  // (the queries are there)
       if (lane == 0) {
         constexpr int STEP = PAIR ? 1 : 2;
         const auto scores_of = [&](int j) {
-          const int k = pos + 2 * j;
-          if (j >= a.give_up || !wait_phase(at(full[k % N]), k / N & 1, late)) return false;
+          const int k = stage0 + pos % RING;
+          if (j >= a.give_up || !wait_phase(at(full[k]), pos / RING & 1, late)) return false;
           shared_for_mma();
           tensor_after_sync();
-          const uint32_t k_at = ring + k % N * S::kTile;
+          const uint32_t k_at = ring + k * S::kTile;
 #pragma unroll
           for (int i = 0; i < DP / 16; ++i) {
             const uint32_t off = i / 4 * (kKeys * 128) + i % 4 * 32;
             product(s_at, operand_k_major(q_at + off), operand_k_major(k_at + off), scores_kind, i > 0);
           }
           commit(at(scores[s]));
-          commit(at(empty[k % N]));
+          commit(at(empty[k]));
+          ++pos;
           return true;
         };
         const int first = PAIR ? 0 : s;
         if (good && first < part.tiles) good = scores_of(first);
         for (int j = first; good && j < part.tiles; j += STEP) {
-          const int v = pos + 2 * j + 1;
-          const uint32_t v_at = ring + v % N * S::kTile;
-          good = wait_phase(at(full[v % N]), v / N & 1, late);
+          const int v = stage0 + pos % RING;
+          const uint32_t v_at = ring + v * S::kTile;
+          good = wait_phase(at(full[v]), pos / RING & 1, late);
           shared_for_mma();
 #pragma unroll
           for (int half = 0; half < 2; ++half) {
@@ -217,15 +232,14 @@ template <typename T, int DP, bool PAIR> __global__ void __launch_bounds__(kThre
           }
           if (!good) break;
           commit(at(values[s]));
-          commit(at(empty[v % N]));
-          ++done;
+          commit(at(empty[v]));
+          ++pos, ++done;
           // The next scores go where these weights are: a thread's products run in the order that they are issued in.
           if (j + STEP < part.tiles) good = scores_of(j + STEP);
         }
         if (!good) *late = 1;
       }
       __syncwarp();
-      pos += 2 * part.tiles;
     }
     if (lane == 0) {
       // Nothing is on its way any more when the tensor memory is given back.
@@ -239,20 +253,14 @@ template <typename T, int DP, bool PAIR> __global__ void __launch_bounds__(kThre
     const int w = warp - kCopies;
     const gar_kv_cache &c = a.c;
     const char *const kp = static_cast<const char *>(c.k), *const vp = static_cast<const char *>(c.v);
-    int pos = 0;       // the next tile's place in the ring
+    int pos[2] = {0, 0};  // the next tile of keys or values, of each ring
     bool good = true;
     constexpr int PER = 32 / CHUNKS;  // rows that the warp copies at a time
     const int chunk = lane % CHUNKS, sub = lane / CHUNKS;
     while (good && next_part()) {
-      // The page of this lane's row of a tile: looked up a tile before it is used, and checked only then.
+      // Pages are looked up a tile before they are used, and checked only then.
       struct Found {
         int page, in;  // in: the row of the page, or -1
-      };
-      const auto look = [&](int tile) {
-        const int n = (part.from + tile) * kKeys + w * kCopyRows + lane;
-        if (tile >= part.tiles || n >= part.rows) return Found{0, -1};
-        const int p = (int)a.page((uint32_t)n);
-        return Found{a.table[part.g * a.table_stride + p], n - p * c.page_size};
       };
       const auto place = [&](Found f) {
         if (f.in < 0) return (int64_t)-1;
@@ -262,14 +270,52 @@ template <typename T, int DP, bool PAIR> __global__ void __launch_bounds__(kThre
         }
         return f.page * c.page_stride + part.kv * c.head_stride + f.in * c.token_stride;
       };
-      Found found = look(0);
+      // Whole tiles go in boxes where pages allow it: the page of this lane's box and the row in it.
+      const int boxes = a.box > 0 ? kKeys / a.box : 1, box = lane % boxes, line = lane / boxes;
+      const auto in_boxes = [&](int tile) { return a.box > 0 && (part.from + tile + 1) * kKeys <= part.rows; };
+      const auto look_any = [&](int tile) {
+        const int n = (part.from + tile) * kKeys + (in_boxes(tile) ? box * a.box : w * kCopyRows + lane);
+        Found f{0, -1};
+        if (tile < part.tiles && n < part.rows) {
+          const int p = (int)a.page((uint32_t)n);
+          f.page = a.table[part.g * a.table_stride + p], f.in = n - p * c.page_size;
+        }
+        return f;
+      };
+      Found found = look_any(0);
       for (int j = 0; good && j < part.tiles; ++j) {
-        const int64_t row = place(found);
-        found = look(j + 1);
+        const Found now = found;
+        found = look_any(j + 1);
+        if (in_boxes(j)) {
+          // One line (128 bytes) of a box's rows to a lane.  What is on no page becomes zeros.
+          if (w == 0 && (unsigned)now.page >= (uint64_t)c.pages && c.status) atomicOr(c.status, GAR_KV_BAD_PAGE);
+#pragma unroll 1
+          for (int half = 0; half < 2; ++half) {
+            int &its = PAIR || j % 2 == 0 ? pos[0] : pos[1];
+            const int stage = (PAIR ? 0 : j % 2 * RING) + its % RING;
+            good = good && (its < RING || wait_phase(at(empty[stage]), (its / RING - 1) & 1, late));
+            good = __all_sync(~0u, good);
+            if (!good) break;
+            if (w == 0) {
+              if (lane == 0)
+                asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(at(full[stage])), "r"(S::kTile) : "memory");
+              __syncwarp();
+              if (line < DP / 64)
+                copy_line(ring + stage * S::kTile + line * (kKeys * 128) + box * (a.box * 128), half ? &v_map : &k_map, now.in, line,
+                          part.kv, now.page, at(full[stage]));
+            } else if (lane == 0) {
+              arrive(at(full[stage]));
+            }
+            ++its;
+          }
+          continue;
+        }
+        const int64_t row = place(now);
 #pragma unroll
         for (int half = 0; half < 2; ++half) {  // keys, values
-          const int stage = pos % N;
-          good = good && (pos < N || wait_phase(at(empty[stage]), (pos / N - 1) & 1, late));
+          int &its = PAIR || j % 2 == 0 ? pos[0] : pos[1];
+          const int stage = (PAIR ? 0 : j % 2 * RING) + its % RING;
+          good = good && (its < RING || wait_phase(at(empty[stage]), (its / RING - 1) & 1, late));
           good = __all_sync(~0u, good);
           if (!good) break;
           const char *const base = half ? vp : kp;
@@ -282,12 +328,20 @@ template <typename T, int DP, bool PAIR> __global__ void __launch_bounds__(kThre
             copy_async<16>(tile + chunk / 8 * (kKeys * 128) + line_row * 128 + ((chunk ^ line_row) & 7) * 16,
                            in ? base + x * 2 + chunk * 16 : base, in);
           }
-          arrive_after_copies(at(full[stage]));
-          ++pos;
+          if (a.box > 0) {  // (a last tile after boxes)
+            asm volatile("cp.async.wait_all;" ::: "memory");
+            shared_for_mma();
+            __syncwarp();
+            if (lane == 0) arrive(at(full[stage]));
+          } else {
+            arrive_after_copies(at(full[stage]));
+          }
+          ++its;
         }
       }
     }
     asm volatile("cp.async.wait_all;" ::: "memory");
+    if (threadIdx.x == 32 * kCopies) copied[0] = pos[0], copied[1] = pos[1];
   } else {
     // Turns scores to weights.
     const int s = warp / 4, quarter = warp & 3, row = quarter * 32 + lane;
@@ -384,16 +438,20 @@ template <typename T, int DP, bool PAIR> __global__ void __launch_bounds__(kThre
             if (c == 1) {  // half of the products can begin
               wait_tensor_stores();
               tensor_before_sync();
-              arrive(at(weights[s][0]));
+              __syncwarp();
+              if (lane == 0) arrive(at(weights[s][0]));
+              __syncwarp();
             }
           }
           l += (sum[0].x + sum[1].x) + (sum[0].y + sum[1].y);
           wait_tensor_stores();
         }
-        if (idle) arrive(at(weights[s][0]));
+        if (idle && lane == 0) arrive(at(weights[s][0]));
         first = false;
         tensor_before_sync();
-        arrive(at(weights[s][1]));
+        __syncwarp();
+        if (lane == 0) arrive(at(weights[s][1]));
+        __syncwarp();
       }
       if (!good) continue;
       // This part's result, in units of one.
@@ -427,7 +485,13 @@ template <typename T, int DP, bool PAIR> __global__ void __launch_bounds__(kThre
   __syncthreads();
   tensor_after_sync();
   if (warp == kIssue) tensor_free(tensor);
-  if (threadIdx.x == 0 && late_flag && a.c.status) atomicOr(a.c.status, GAR_KV_TIMEOUT);
+  if (late_flag && threadIdx.x == 32 * kCopies) {
+    if (a.c.status) atomicOr(a.c.status, GAR_KV_TIMEOUT);
+    // What is on its way lands before the CTA's memory is another's.
+    int never = 0;
+    for (int s = 0; s < (PAIR ? 1 : 2); ++s)
+      for (int i = max(0, copied[s] - RING); i < copied[s]; ++i) wait_phase(at(full[s * RING + i % RING]), i / RING & 1, &never);
+  }
 }
 
 constexpr int kJoinThreads = 256, kJoinRows = 32, kJoinChannels = 32;
@@ -514,14 +578,14 @@ template <int DP> __global__ void __launch_bounds__(kJoinThreads) join_kernel(co
   }
 }
 
-template <typename T, int DP, bool PAIR> int launch_prefix(const PrefixArgs &a, gar_stream_t stream) {
+template <typename T, int DP, bool PAIR> int launch_prefix(const PrefixArgs &a, const CUtensorMap (&maps)[2], gar_stream_t stream) {
   constexpr auto kernel = prefix_kernel<T, DP, PAIR>;
   static DeviceSet allowed;
   const int e = once_for_device(allowed, a.device, [&] {
     return (int)cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, PrefixShape<DP, PAIR>::kShared);
   });
   if (e != 0) return cuda_fail((cudaError_t)e, "cudaFuncSetAttribute");
-  return launch("gar_prefix_attention", kernel, a.ctas, kThreads, PrefixShape<DP, PAIR>::kShared, stream, a);
+  return launch("gar_prefix_attention", kernel, a.ctas, kThreads, PrefixShape<DP, PAIR>::kShared, stream, a, maps[0], maps[1]);
 }
 
 }  // namespace
@@ -533,11 +597,11 @@ size_t prefix_partials(int items, int dim, char *base, PrefixArgs *a) {
   return sums + places * 256 * dp * sizeof(float);
 }
 
-int prefix_mma(const PrefixArgs &a, gar_stream_t stream) {
+int prefix_mma(const PrefixArgs &a, const CUtensorMap (&maps)[2], gar_stream_t stream) {
   const auto run = [&](auto t) {
     using T = typename decltype(t)::type;
-    if (a.c.dim <= 64) return a.pair ? launch_prefix<T, 64, true>(a, stream) : launch_prefix<T, 64, false>(a, stream);
-    return a.pair ? launch_prefix<T, 128, true>(a, stream) : launch_prefix<T, 128, false>(a, stream);
+    if (a.c.dim <= 64) return a.pair ? launch_prefix<T, 64, true>(a, maps, stream) : launch_prefix<T, 64, false>(a, maps, stream);
+    return a.pair ? launch_prefix<T, 128, true>(a, maps, stream) : launch_prefix<T, 128, false>(a, maps, stream);
   };
   return a.c.dtype == GAR_BF16 ? run(type_tag<__nv_bfloat16>{}) : run(type_tag<__half>{});
 }

@@ -96,12 +96,12 @@ def test_verify_refusals(bad, code):
 
 # ---------------------------------------------------------------------------- attention over shared prefixes
 
-def _prefix_case(prefixes, own, share, q_heads, kv_heads, dim, page_size, kind, dtype, seed=0, order="head", sharp=1.0):
+def _prefix_case(prefixes, own, share, q_heads, kv_heads, dim, page_size, kind, dtype, seed=0, order="head", sharp=1.0, every=1):
     """(cache, prefix table and lengths, table and lengths, q, each sequence's keys and values in 64 bits)."""
     cache, table, lens, _, kvs = _attn_case(prefixes + own, q_heads, kv_heads, dim, page_size, kind, dtype, seed, order)
     groups = len(prefixes)
     q = _randn((len(own), q_heads, dim), dtype, seed + 7) * sharp
-    both = [tuple(torch.cat([kvs[b // share][i], kvs[groups + b][i]]) for i in (0, 1)) for b in range(len(own))]
+    both = [tuple(torch.cat([kvs[b // share][i], kvs[groups + b][i]]) for i in (0, 1)) for b in range(0, len(own), every)]
     return cache, table[:groups], lens[:groups], table[groups:], lens[groups:], q, both
 
 
@@ -117,7 +117,7 @@ def _check_prefix(out, lse, q, both, scale, out_type):
             assert bool((out[b] == 0).all()) and bool((lse[b] == -math.inf).all())
             continue
         y = torch.einsum("hd,nhd->hn", q[b].double(), k) * scale
-        e = ((q.shape[2] + 4) * U32 * scale * torch.einsum("hd,nhd->hn", q[b].double().abs(), k.abs())).amax(-1)
+        e = ((q.shape[2] + 4) * U32 * abs(scale) * torch.einsum("hd,nhd->hn", q[b].double().abs(), k.abs())).amax(-1)
         p = torch.softmax(y, -1)
         want, size = torch.einsum("hn,nhd->hd", p, v), torch.einsum("hn,nhd->hd", p, v.abs())
         want_lse = torch.logsumexp(y, -1)
@@ -172,6 +172,32 @@ def test_prefix_attention_of_many_queries(kind, dtype, dim, share, q_heads, kv_h
     again = gar.gar_prefix_attention(plan, q, cache, pt, pn, t, n, lse=True)
     assert torch.equal(out, again[0]) and torch.equal(lse, again[1])
     gar.gar_kv_status(cache)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("kind,dim,page_size,share,prefix", [
+    ("bf16", 128, 64, 32, 60000), ("f16", 64, 128, 32, 50001), ("bf16", 128, 256, 64, 33000), ("f16", 128, 24, 32, 40000),
+    ("bf16", 64, 32, 100, 40129), ("bf16", 96, 16, 24, 40000), ("f16", 128, 8, 64, 20000)])
+def test_prefix_attention_many_tiles_each(kind, dim, page_size, share, prefix):
+    """Parts of dozens of tiles: every stage of the ring is used many times; results do not depend on timing."""
+    own = [(7 * b) % 40 for b in range(share)]
+    cache, pt, pn, t, n, q, both = _prefix_case([prefix], own, share, 32, 8, dim, page_size, kind, kind, sharp=2.0, every=9)
+    plan = gar.gar_attn_plan_create(32, 8, dim)
+    out, lse = gar.gar_prefix_attention(plan, q, cache, pt, pn, t, n, lse=True)
+    for _ in range(20):
+        again = gar.gar_prefix_attention(plan, q, cache, pt, pn, t, n, lse=True)
+        assert torch.equal(out, again[0]) and torch.equal(lse, again[1])
+    _check_prefix(out[::9], lse[::9], q[::9], both, dim ** -0.5, kind)
+    gar.gar_kv_status(cache)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("scale", [0.0, -0.1])
+def test_prefix_attention_scales(scale):
+    cache, pt, pn, t, n, q, both = _prefix_case([300], [b % 9 for b in range(40)], 40, 4, 2, 64, 16, "bf16", "bf16")
+    plan = gar.gar_attn_plan_create(4, 2, 64)
+    out, lse = gar.gar_prefix_attention(plan, q, cache, pt, pn, t, n, scale=scale, lse=True)
+    _check_prefix(out, lse, q, both, scale, "bf16")
 
 
 @pytest.mark.gpu
