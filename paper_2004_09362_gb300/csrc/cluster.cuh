@@ -24,8 +24,8 @@ __device__ __forceinline__ uint32_t in_cta(const void *p, int rank) {
 __device__ __forceinline__ void store_in_cta(int *p, int rank, int x) {
   asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(in_cta(p, rank)), "r"(x) : "memory");
 }
-__device__ __forceinline__ void store_in_cta(double *p, int rank, double x) {
-  asm volatile("st.shared::cluster.f64 [%0], %1;" ::"r"(in_cta(p, rank)), "d"(x) : "memory");
+__device__ __forceinline__ void store_in_cta(float2 *p, int rank, float2 x) {
+  asm volatile("st.shared::cluster.v2.f32 [%0], {%1, %2};" ::"r"(in_cta(p, rank)), "f"(x.x), "f"(x.y) : "memory");
 }
 __device__ __forceinline__ int load_from_cta(const int *p, int rank) {
   int x;

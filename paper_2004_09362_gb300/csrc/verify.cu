@@ -6,12 +6,14 @@
 //
 // Bound by memory: of all the probabilities only one row of the target and one of the draft are needed
 // whole, those at the first draft that does not stand (the drafts' own probabilities are a few words).  A cluster of CTAs
-// takes a sequence, each warp a run of neighbouring tokens; the warps' sums are exchanged through the cluster's shared memory, every
-// warp finds the run in which the running sum passes, and the warp of that run reads it again (from the L2).
+// takes a sequence, each warp a run of neighbouring tokens, whose pieces a lane sums side by side; the warps' sums are exchanged through
+// the cluster's shared memory, every warp finds the run in which the running sum passes, and the warp of that run reads one of its
+// pieces again (from the L2).
 //
 // The token is a choice at a border between running sums, so these have to be better than 32 bits: after 131072 terms a sum in 32 bits
-// is off by more than a whole token's share.  A lane adds in twice 32 bits (the error of each addition is computed
-// exactly and added up beside it: Knuth's TwoSum), lanes and warps in 64 bits, which this GPU does at 1/64 the rate.
+// is off by more than a whole token's share.  All sums are held in twice 32 bits: the error of each addition is computed
+// exactly and added up beside it (Knuth's TwoSum).  64 bits are out of the question, this GPU does two such additions a clock and SM:
+// the warps' sums and scans alone, of 57 x 50021 bf16, cost 40 us of 72 in 64 bits.
 #include <climits>
 
 #include "cluster.cuh"
@@ -19,8 +21,10 @@
 namespace gar {
 namespace {
 
-constexpr int kThreads = 512, kWarps = kThreads / 32;
+constexpr int kThreads = 256, kWarps = kThreads / 32;
 constexpr int kMostCtas = 8;  // of a cluster
+constexpr int kSubs = 4;      // pieces of a warp's run
+constexpr int kGroup = 4;     // neighbouring tokens of a lane
 
 struct VerifyArgs {
   const void *target, *draft;
@@ -30,7 +34,7 @@ struct VerifyArgs {
   int32_t *accepted;
   const float *uniform;
   int vocab, drafts, ctas;
-  int run;                   // tokens of a warp
+  int piece;                 // tokens of a piece of a warp's run
   bool wide;                 // 64-bit tokens
 };
 
@@ -43,10 +47,45 @@ struct Sum {
     high = t;
   }
 };
-
-template <typename T> __device__ __forceinline__ float probability(const T *p) {
-  return fminf(fmaxf(to_f32(*p), 0.f), 1.f);  // (of a NaN and a number the number)
+// The low part no more than a rounding error of the high one.
+__device__ __forceinline__ Sum neat(Sum a) {
+  Sum s;
+  s.high = a.high + a.low, s.low = a.low - (s.high - a.high);
+  return s;
 }
+__device__ __forceinline__ Sum operator+(Sum a, Sum b) {
+  a.add(b.high, b.low);
+  return neat(a);
+}
+__device__ __forceinline__ Sum operator*(Sum a, float x) {
+  Sum s;
+  s.high = a.high * x, s.low = fmaf(a.high, x, -s.high) + a.low * x;
+  return neat(s);
+}
+__device__ __forceinline__ bool operator>(Sum a, Sum b) { return a.high > b.high || (a.high == b.high && a.low > b.low); }
+__device__ __forceinline__ Sum up(Sum a, int d) {
+  Sum s;
+  s.high = __shfl_up_sync(~0u, a.high, d), s.low = __shfl_up_sync(~0u, a.low, d);
+  return s;
+}
+__device__ __forceinline__ Sum from_lane(Sum a, int lane) {
+  Sum s;
+  s.high = __shfl_sync(~0u, a.high, lane), s.low = __shfl_sync(~0u, a.low, lane);
+  return s;
+}
+// The sums over the lanes up to each.
+__device__ __forceinline__ Sum running(Sum a) {
+#pragma unroll
+  for (int d = 1; d < 32; d *= 2) {
+    const Sum x = up(a, d);
+    if ((int)(threadIdx.x & 31) >= d) a = x + a;
+  }
+  return a;
+}
+
+// Within [0, 1]; of a NaN 0.
+__device__ __forceinline__ float probable(float x) { return __saturatef(x); }
+template <typename T> __device__ __forceinline__ float probability(const T *p) { return probable(to_f32(*p)); }
 
 __device__ __forceinline__ int64_t token_at(const VerifyArgs &a, int64_t i) {
   return a.wide ? static_cast<const int64_t *>(a.tokens)[i] : (int64_t) static_cast<const int32_t *>(a.tokens)[i];
@@ -62,77 +101,169 @@ __device__ __forceinline__ void put_token(const VerifyArgs &a, int64_t i, int64_
 template <typename T> struct Row {
   const T *p, *q;
   bool less;
-  __device__ __forceinline__ double operator()(int v) const {
-    const double x = (double)probability(p + v) - (less ? (double)probability(q + v) : 0.);
-    return x > 0. ? x : 0.;
-  }
 };
 
-template <typename T> __device__ __forceinline__ double run_sum(const Row<T> &row, int from, int to) {
-  constexpr int N = 8;  // loads of each row in flight
+// max(p - q, 0), exactly.
+__device__ __forceinline__ Sum remaining(float p, float q) {
+  const float x = probable(p), y = probable(q), d = x - y, b = d - x;
   Sum s;
-  for (int v0 = from + (int)(threadIdx.x & 31); v0 < to; v0 += 32 * N) {
-    float p[N], q[N];
+  if (d > 0.f) s.high = d, s.low = (x - (d - b)) - (y + b);
+  return s;
+}
+
+// kGroup neighbouring tokens as they lie in memory: loaded at once where they are aligned, else one by one.  (What is loaded is
+// taken apart later, when all loads are on their way.)
+template <typename T, bool WIDE> struct Group;
+template <typename T> struct Group<T, true> {
+  static_assert(kGroup == 4, "four or eight bytes a pair");
+  uint32_t w[kGroup * sizeof(T) / 4];
+  __device__ __forceinline__ void load(const T *p, bool there) {
+    if constexpr (sizeof(T) == 4) {
+      const uint4 x = there ? __ldg(reinterpret_cast<const uint4 *>(p)) : make_uint4(0, 0, 0, 0);
+      w[0] = x.x, w[1] = x.y, w[2] = x.z, w[3] = x.w;
+    } else {
+      const uint2 x = there ? __ldg(reinterpret_cast<const uint2 *>(p)) : make_uint2(0, 0);
+      w[0] = x.x, w[1] = x.y;
+    }
+  }
+  __device__ __forceinline__ float2 pair(int i) const {
+    if constexpr (sizeof(T) == 4)
+      return make_float2(__uint_as_float(w[2 * i]), __uint_as_float(w[2 * i + 1]));
+    else
+      return unpack2(w[i], T());
+  }
+};
+template <typename T> struct Group<T, false> {
+  T x[kGroup];
+  __device__ __forceinline__ void load(const T *p, bool there) {
 #pragma unroll
-    for (int i = 0; i < N; ++i) {
-      const int v = v0 + 32 * i;
-      p[i] = v < to ? probability(row.p + v) : 0.f;
-      q[i] = row.less && v < to ? probability(row.q + v) : 0.f;
+    for (int i = 0; i < kGroup; ++i) x[i] = there ? p[i] : T(0.f);
+  }
+  __device__ __forceinline__ float2 pair(int i) const { return make_float2(to_f32(x[2 * i]), to_f32(x[2 * i + 1])); }
+};
+// A group at the row's ends, token by token.
+template <typename T> __device__ __forceinline__ void load_ends(const T *p, int v, int vocab, float (&x)[kGroup]) {
+#pragma unroll
+  for (int i = 0; i < kGroup; ++i) x[i] = (unsigned)(v + i) < (unsigned)vocab ? to_f32(p[v + i]) : 0.f;
+}
+enum { DRAFT_NONE, DRAFT_WIDE, DRAFT_NARROW };  // how the draft's row is read
+
+// Two sums side by side.
+struct Sums {
+  float2 high = {0.f, 0.f}, low = {0.f, 0.f};
+};
+__device__ __forceinline__ float2 sub2(float2 a, float2 b) { return fma2(b, make_float2(-1.f, -1.f), a); }
+
+// d + rest = max(p - q, 0), exactly; then the same of high + d, whose rest goes to the low part.
+__device__ __forceinline__ void add_pair(Sums &s, float2 p, float2 q) {
+  const float2 x = make_float2(probable(p.x), probable(p.y));
+  const float2 y = make_float2(fminf(probable(q.x), x.x), fminf(probable(q.y), x.y));
+  const float2 d = sub2(x, y), b = sub2(d, x), rest = sub2(sub2(x, sub2(d, b)), add2(y, b));
+  const float2 t = add2(s.high, d), c = sub2(t, s.high);
+  s.low = add2(s.low, add2(add2(sub2(s.high, sub2(t, c)), sub2(d, c)), rest));
+  s.high = t;
+}
+
+// A lane's part of the sums of a run's kSubs pieces.  Groups of tokens begin `shift` tokens early, where the target's row is
+// aligned.
+template <typename T, int DRAFT>
+__device__ __forceinline__ void add_run(const Row<T> &row, int64_t from, int piece, int vocab, int shift, Sums (&s)[kSubs]) {
+  const int lane = threadIdx.x & 31;
+#pragma unroll 1
+  for (int k = lane * kGroup; k < piece; k += 32 * kGroup) {
+    Group<T, true> p[kSubs];
+    Group<T, DRAFT == DRAFT_WIDE> q[kSubs];
+    int v[kSubs];
+#pragma unroll
+    for (int i = 0; i < kSubs; ++i) {
+      v[i] = (int)min(from + i * piece + k - shift, (int64_t)vocab);
+      const bool there = v[i] >= 0 && v[i] + kGroup <= vocab;
+      p[i].load(row.p + v[i], there);
+      if (DRAFT != DRAFT_NONE) q[i].load(row.q + v[i], there);
     }
 #pragma unroll
-    for (int i = 0; i < N; ++i) {
-      const float d = p[i] - q[i];
-      if (d > 0.f) {
-        const float b = d - p[i];
-        s.add(d, (p[i] - (d - b)) - (q[i] + b));
+    for (int i = 0; i < kSubs; ++i) {
+#pragma unroll
+      for (int j = 0; j < kGroup / 2; ++j) add_pair(s[i], p[i].pair(j), DRAFT != DRAFT_NONE ? q[i].pair(j) : make_float2(0.f, 0.f));
+      if (v[i] < vocab && (v[i] < 0 || v[i] + kGroup > vocab)) {
+        float x[kGroup], y[kGroup] = {};
+        load_ends(row.p, v[i], vocab, x);
+        if (DRAFT != DRAFT_NONE) load_ends(row.q, v[i], vocab, y);
+#pragma unroll
+        for (int j = 0; j < kGroup; j += 2) add_pair(s[i], make_float2(x[j], x[j + 1]), make_float2(y[j], y[j + 1]));
       }
     }
   }
-  double x = (double)s.high + (double)s.low;
+}
+
+__device__ __forceinline__ Sum both(const Sums &s) {
+  Sum a, b;
+  a.high = s.high.x, a.low = s.low.x, b.high = s.high.y, b.low = s.low.y;
+  return neat(a) + neat(b);
+}
+
+// The sum over the lanes, in the same order in each.
+__device__ __forceinline__ Sum over_lanes(Sum a) {
 #pragma unroll
-  for (int d = 16; d > 0; d /= 2) x += __shfl_xor_sync(~0u, x, d);
-  return x;
+  for (int d = 1; d < 32; d *= 2) {
+    Sum x;
+    x.high = __shfl_xor_sync(~0u, a.high, d), x.low = __shfl_xor_sync(~0u, a.low, d);
+    a = a + x;
+  }
+  return a;
 }
 
 template <typename T> __device__ __forceinline__ int last_of(const Row<T> &row, int from, int to) {
   int last = -1;
   for (int v = from + (int)(threadIdx.x & 31); v < to; v += 32)
-    if (row(v) > 0.) last = v;
+    if (remaining(to_f32(row.p[v]), row.less ? to_f32(row.q[v]) : 0.f).high > 0.f) last = v;
   return __reduce_max_sync(~0u, last);
 }
 
-// The first token of the run at which `before` and the running sum pass `goal`; all of the run does.
-template <typename T> __device__ __forceinline__ int find(const Row<T> &row, int from, int to, double before, double goal) {
-  const int lane = threadIdx.x & 31, each = (to - from + 31) / 32;
-  const int v0 = min(to, from + lane * each), v1 = min(to, v0 + each);
-  double sum = 0.;
-#pragma unroll 8
-  for (int v = v0; v < v1; ++v) sum += row(v);
-  double upto = sum;
+// The first token of the groups from `from` on, up to `to`, at which `before` and the running sum pass `goal`, as they do; where rounding
+// hides that, the last that counts.
+template <typename T>
+__device__ __forceinline__ int find(const Row<T> &row, int64_t from, int64_t to, int vocab, Sum before, Sum goal) {
+  const int lane = threadIdx.x & 31;
+  int last = -1;
+#pragma unroll 1
+  for (int64_t v0 = from; v0 < to; v0 += 32 * kGroup) {
+    const int v = (int)min(v0 + lane * kGroup, (int64_t)vocab);
+    float p[kGroup], q[kGroup] = {};
+    load_ends(row.p, v, vocab, p);
+    if (row.less) load_ends(row.q, v, vocab, q);
+    Sum upto[kGroup], sum;
+    int mine = -1;  // the lane's last that counts
 #pragma unroll
-  for (int d = 1; d < 32; d *= 2) {
-    const double x = __shfl_up_sync(~0u, upto, d);
-    if (lane >= d) upto += x;
-  }
-  // (Where rounding hides the border, the last that counts.)
-  const uint32_t past = __ballot_sync(~0u, before + upto > goal && sum > 0.), some = __ballot_sync(~0u, sum > 0.);
-  const int from_lane = past ? __ffs(past) - 1 : 31 - __clz(some | 1u);
-  int found = -1;
-  if (lane == from_lane) {
-    double x = before + (upto - sum);
-#pragma unroll 8
-    for (int v = v0; v < v1; ++v) {
-      const double w = row(v);
-      if (w > 0. && !(x > goal)) x += w, found = v;
+    for (int i = 0; i < kGroup; ++i) {
+      const Sum w = remaining(p[i], q[i]);
+      if (w.high > 0.f) mine = i;
+      upto[i] = sum = sum + w;
     }
+    const Sum with = running(sum);
+    Sum start = up(with, 1);
+    start = lane == 0 ? before : before + start;
+    int passed = kGroup;
+#pragma unroll
+    for (int i = kGroup - 1; i >= 0; --i)
+      if (start + upto[i] > goal) passed = i;
+    // (the first that passes counts itself: its predecessor does not pass)
+    const uint32_t past = __ballot_sync(~0u, passed < kGroup && mine >= passed), some = __ballot_sync(~0u, mine >= 0);
+    if (past) {
+      const int from_one = __ffs(past) - 1;
+      return __shfl_sync(~0u, v + passed, from_one);
+    }
+    if (some) last = __shfl_sync(~0u, v + mine, 31 - __clz(some));
+    before = before + from_lane(with, 31);
   }
-  return __shfl_sync(~0u, found, from_lane);
+  return last;
 }
 
-template <typename T> __global__ void __launch_bounds__(kThreads) verify_kernel(const VerifyArgs a) {
-  __shared__ double totals[2][kMostCtas * kWarps];
+template <typename T> __global__ void __launch_bounds__(kThreads, 4) verify_kernel(const VerifyArgs a) {
+  __shared__ float2 totals[2][kMostCtas * kWarps];
   __shared__ int lasts[kMostCtas * kWarps];
-  __shared__ int stop, refused;
+  __shared__ int stop, refused, picked, empty;
+  __shared__ float2 bounds[2];
   const int rank = cluster_rank(), warp = threadIdx.x / 32, lane = threadIdx.x & 31, me = rank * kWarps + warp;
   const int64_t b = blockIdx.x / a.ctas;
   cluster_arrive();
@@ -164,58 +295,85 @@ template <typename T> __global__ void __launch_bounds__(kThreads) verify_kernel(
   }
   __syncthreads();
   Row<T> row{target + stop * a.tr, refused ? draft + stop * a.dr : nullptr, refused != 0};
-  const int from = min((int64_t)a.vocab, (int64_t)me * a.run), to = min((int64_t)a.vocab, (int64_t)from + a.run);
+  // Runs begin where the target's row is aligned: a few tokens early.
+  constexpr uintptr_t kWide = kGroup * sizeof(T);
+  const int shift = (int)((uintptr_t)row.p % kWide / sizeof(T)), run = kSubs * a.piece;
+  const int64_t begin = (int64_t)me * run;
+  const int from = (int)min((int64_t)a.vocab, max((int64_t)0, begin - shift)), to = (int)min((int64_t)a.vocab, begin + run - shift);
   cluster_wait();
 
-  // The running sums before and after each run; this lane knows those of 4 runs.
-  constexpr int EACH = kMostCtas * kWarps / 32;
-  double before = 0., goal = 0., all = 0.;
-  int chosen = -1;
   const float u = fmaxf(a.uniform[b * (a.drafts + 1) + a.drafts], 0.f);
+  Sums sums[kSubs];
   for (int pass = 0; pass < 2; ++pass) {
-    const double mine = run_sum(row, from, to);
-    if (lane < a.ctas) store_in_cta(&totals[pass][me], lane, mine);
+#pragma unroll
+    for (int i = 0; i < kSubs; ++i) sums[i] = Sums();
+    if (!row.less)
+      add_run<T, DRAFT_NONE>(row, begin, a.piece, a.vocab, shift, sums);
+    else if ((uintptr_t)(row.q - shift) % kWide == 0)
+      add_run<T, DRAFT_WIDE>(row, begin, a.piece, a.vocab, shift, sums);
+    else
+      add_run<T, DRAFT_NARROW>(row, begin, a.piece, a.vocab, shift, sums);
+    Sum mine = both(sums[0]);
+#pragma unroll
+    for (int i = 1; i < kSubs; ++i) mine = mine + both(sums[i]);
+    mine = over_lanes(mine);
+    if (lane < a.ctas) store_in_cta(&totals[pass][me], lane, make_float2(mine.high, mine.low));
     cluster_sync();
-    double upto[EACH], sum = 0.;
+    // One warp finds the run; this lane knows the running sums before and after EACH of them.
+    constexpr int EACH = kMostCtas * kWarps / 32;
+    if (warp == 0) {
+      Sum upto[EACH], sum;
 #pragma unroll
-    for (int i = 0; i < EACH; ++i) {
-      const int k = lane * EACH + i;
-      upto[i] = sum += k < a.ctas * kWarps ? totals[pass][k] : 0.;
-    }
-    double x = sum;
+      for (int i = 0; i < EACH; ++i) {
+        const int k = lane * EACH + i;
+        if (k < a.ctas * kWarps) {
+          Sum x;
+          x.high = totals[pass][k].x, x.low = totals[pass][k].y;
+          sum = sum + x;
+        }
+        upto[i] = sum;
+      }
+      const Sum with = running(sum);
+      Sum start = up(with, 1);
+      if (lane == 0) start = Sum();
 #pragma unroll
-    for (int d = 1; d < 32; d *= 2) {
-      const double y = __shfl_up_sync(~0u, x, d);
-      if (lane >= d) x += y;
-    }
-    const double base = __shfl_up_sync(~0u, x, 1);
-    const double start = lane == 0 ? 0. : base;
-    all = __shfl_sync(~0u, start + upto[EACH - 1], 31);
-    if (!(all > 0.) && row.less) {
-      row.less = false;  // nothing is left of the target: all of it
-      continue;
-    }
-    goal = (double)u * all;
-    int k = -1;
-    double low = 0.;
+      for (int i = 0; i < EACH; ++i) upto[i] = start + upto[i];
+      const Sum all = from_lane(upto[EACH - 1], 31), goal = all * u;
+      int k = -1;
+      Sum low;
 #pragma unroll
-    for (int i = EACH - 1; i >= 0; --i) {
-      const double lower = i == 0 ? start : start + upto[i - 1];
-      if (start + upto[i] > goal) k = lane * EACH + i, low = lower;
+      for (int i = EACH - 1; i >= 0; --i)
+        if (upto[i] > goal) k = lane * EACH + i, low = i == 0 ? start : upto[i - 1];
+      const uint32_t past = __ballot_sync(~0u, k >= 0);
+      if (lane == (past ? __ffs(past) - 1 : 0)) {
+        picked = past ? k : -1, empty = !(all.high > 0.f);
+        bounds[0] = make_float2(low.high, low.low), bounds[1] = make_float2(goal.high, goal.low);
+      }
     }
-    const uint32_t past = __ballot_sync(~0u, k >= 0);
-    if (past) {
-      chosen = __shfl_sync(~0u, k, __ffs(past) - 1);
-      before = __shfl_sync(~0u, low, __ffs(past) - 1);
-    }
-    break;
+    __syncthreads();
+    if (!empty || !row.less) break;
+    row.less = false;  // nothing is left of the target: all of it
+    __syncthreads();
   }
 
   const int64_t out = b * (a.drafts + 1);
-  if (chosen == me) {
-    const int token = find(row, from, to, before, goal);
+  if (picked == me) {
+    Sum sum, goal;
+    sum.high = bounds[0].x, sum.low = bounds[0].y, goal.high = bounds[1].x, goal.low = bounds[1].y;
+    // The piece in which that is; the last that has any where rounding hides it.
+    int piece = 0;
+    Sum start = sum;
+    bool found = false;
+#pragma unroll
+    for (int i = 0; i < kSubs; ++i) {
+      const Sum x = over_lanes(both(sums[i])), next = sum + x;
+      if (!found && x.high > 0.f) piece = i, start = sum, found = next > goal;
+      sum = next;
+    }
+    const int64_t first = begin + piece * a.piece - shift;
+    const int token = find(row, first, first + a.piece, a.vocab, start, goal);
     if (lane == 0) put_token(a, out + stop, token);
-  } else if (chosen < 0) {
+  } else if (picked < 0) {
     const int last = last_of(row, from, to);
     if (lane == 0) store_in_cta(&lasts[me], 0, last);
     cluster_sync();
@@ -266,7 +424,9 @@ extern "C" int gar_verify_drafts(const void *target, int64_t target_batch_stride
   a.ctas = 1;
   while (a.ctas < kMostCtas && (int64_t)batch * a.ctas < 152 * 4 && vocab > 2048 * a.ctas) a.ctas *= 2;
   const int warps = a.ctas * kWarps;
-  a.run = (int)((vocab + warps - 1) / warps + 31) / 32 * 32;
+// (the last tokens of a row that begins shifted are a group more)
+  const int64_t round = (int64_t)warps * kSubs * 32 * kGroup;
+  a.piece = (int)((vocab + kGroup - 1 + round - 1) / round) * 32 * kGroup;
   return with_float(dtype, [&](auto t) {
     using T = typename decltype(t)::type;
     return launch_clusters("gar_verify_drafts", verify_kernel<T>, (int64_t)batch * a.ctas, a.ctas, kThreads, stream, a);
