@@ -18,7 +18,7 @@
 namespace gar {
 namespace {
 
-constexpr int kThreads = 512, kWarps = kThreads / 32;
+constexpr int kThreads = 256, kWarps = kThreads / 32;
 constexpr int kMostCtas = 8;  // of a cluster
 
 struct EvictArgs {
@@ -33,6 +33,7 @@ struct EvictArgs {
   int each;        // rows of a lane
   int units;       // of a key row: what is copied at once
   int lanes;       // power of two: lanes that copy one row's keys and values
+  bool apart;      // rows are moved by a kernel of their own
 };
 
 // The order of floats as that of integers; 0: a NaN.
@@ -56,20 +57,81 @@ __device__ __forceinline__ Before count_before(const int *counts, int me, int wa
   return {__reduce_add_sync(~0u, x), __reduce_add_sync(~0u, y)};
 }
 
-// The place in the cache of a row of the sequence; false where its page is none.
-__device__ __forceinline__ bool place_of(const EvictArgs &a, int b, int head, int row, int64_t *at, int64_t *scale) {
-  const int p = (int)a.page((uint32_t)row), page = a.table[b * a.table_stride + p], in = row - p * a.c.page_size;
-  if ((unsigned)page >= (uint64_t)a.c.pages) {
+// Where a row of the sequence is: its page, and the row in it.
+struct Place {
+  int page, in;
+};
+__device__ __forceinline__ Place look_up(const EvictArgs &a, int b, int row) {
+  if (row < 0) return {0, -1};
+  const int p = (int)a.page((uint32_t)row);
+  return {a.table[b * a.table_stride + p], row - p * a.c.page_size};
+}
+// The place in the cache; false where there is none.
+__device__ __forceinline__ bool locate(const EvictArgs &a, int head, Place p, int64_t *at, int64_t *scale) {
+  *at = *scale = 0;
+  if (p.in < 0) return false;
+  if ((unsigned)p.page >= (uint64_t)a.c.pages) {
     if (a.c.status) atomicOr(a.c.status, GAR_KV_BAD_PAGE);
     return false;
   }
-  *at = page * a.c.page_stride + head * a.c.head_stride + in * a.c.token_stride;
-  *scale = page * a.c.scale_page_stride + head * a.c.scale_head_stride + in * a.c.scale_token_stride;
+  *at = p.page * a.c.page_stride + head * a.c.head_stride + p.in * a.c.token_stride;
+  *scale = p.page * a.c.scale_page_stride + head * a.c.scale_head_stride + p.in * a.c.scale_token_stride;
   return true;
 }
 
+// Moves some of the `count` rows of the lists behind `keep`: a warp the neighbouring ones from `first` on, then those `step` rows
+// further; a.lanes lanes to each, kRows of them on their way at a time.  OWN: the lists may end earlier, and what has been read of them is cleared.
+template <typename U, bool OWN>
+__device__ __forceinline__ void move_rows(const EvictArgs &a, int b, int head, const float *w, const int32_t *pos, float *out_w,
+                                          int32_t *out_p, int keep, int count, int first, int step) {
+  constexpr int kRows = 4;
+  const int sub = threadIdx.x & (a.lanes - 1), group = (threadIdx.x & 31) / a.lanes;
+  const bool scaled = a.c.k_scale != nullptr;
+  const int el = a.c.dtype == GAR_F32 ? 4 : a.c.dtype == GAR_I8 || a.c.dtype == GAR_E4M3 ? 1 : 2;
+  for (int base = first; base < count; base += step * kRows) {
+    const int i0 = base + group;
+    int to[kRows], from[kRows];
+#pragma unroll
+    for (int k = 0; k < kRows; ++k) {
+      const int i = i0 + k * step;
+      to[k] = i < count ? __ldcg(out_p + keep + i) : -1, from[k] = i < count ? __float_as_int(__ldcg(out_w + keep + i)) : -1;
+      if (OWN && to[k] < 0) from[k] = -1;
+    }
+    if (OWN && __all_sync(~0u, to[0] < 0)) break;  // past the lists' ends
+    int64_t at_to[kRows], at_from[kRows], scale_to[kRows], scale_from[kRows];
+    bool good[kRows];
+#pragma unroll
+    for (int k = 0; k < kRows; ++k) {
+      const Place x = look_up(a, b, to[k]), y = look_up(a, b, from[k]);
+      good[k] = locate(a, head, x, &at_to[k], &scale_to[k]);
+      good[k] = locate(a, head, y, &at_from[k], &scale_from[k]) && good[k];
+    }
+    for (int u = sub; u < 2 * a.units; u += a.lanes) {
+      char *const at = static_cast<char *>(u < a.units ? a.c.k : a.c.v) + (int64_t)(u < a.units ? u : u - a.units) * (int)sizeof(U);
+      U x[kRows];
+#pragma unroll
+      for (int k = 0; k < kRows; ++k)
+        if (good[k]) x[k] = *reinterpret_cast<const U *>(at + at_from[k] * el);
+#pragma unroll
+      for (int k = 0; k < kRows; ++k)
+        if (good[k]) *reinterpret_cast<U *>(at + at_to[k] * el) = x[k];
+    }
+    // A lane for each row's scales, weight and position.
+    if (OWN) __syncwarp();
+#pragma unroll
+    for (int k = 0; k < kRows; ++k)
+      if (k % a.lanes == sub) {
+        if (to[k] >= 0) {
+          if (scaled && good[k]) a.c.k_scale[scale_to[k]] = a.c.k_scale[scale_from[k]], a.c.v_scale[scale_to[k]] = a.c.v_scale[scale_from[k]];
+          out_w[to[k]] = w[from[k]], out_p[to[k]] = pos[from[k]];
+        }
+        if (OWN && to[k] >= 0) out_w[keep + i0 + k * step] = 0.f, out_p[keep + i0 + k * step] = -1;
+      }
+  }
+}
+
 // NK: keys that a lane holds in registers; 0: they are made anew each time.  U: what rows are copied in.
-template <int NK, typename U> __global__ void __launch_bounds__(kThreads, 2) evict_kernel(const EvictArgs a) {
+template <int NK, typename U> __global__ void __launch_bounds__(kThreads, 4) evict_kernel(const EvictArgs a) {
   constexpr int WARPS = kMostCtas * kWarps;
   __shared__ int histogram[4][256], largest[WARPS], counts[3][WARPS];
   __shared__ uint32_t found[4];
@@ -78,7 +140,14 @@ template <int NK, typename U> __global__ void __launch_bounds__(kThreads, 2) evi
   const int item = blockIdx.x / a.ctas, b = item / a.c.heads, head = item - b * a.c.heads, warps = a.ctas * kWarps;
   const int each = NK ? NK : a.each;
   for (int i = threadIdx.x; i < 4 * 256; i += kThreads) histogram[0][i] = 0;
-  cluster_arrive();
+  const bool alone = a.ctas == 1;
+  const auto sync = [&] {
+    if (alone)
+      __syncthreads();
+    else
+      cluster_sync();
+  };
+  sync();
   after_earlier_kernels();
 
   const float *const w = a.weights + (int64_t)item * a.rows;
@@ -93,9 +162,8 @@ template <int NK, typename U> __global__ void __launch_bounds__(kThreads, 2) evi
   const int keep = min(a.keep, n);
   if (head == 0 && rank == 0 && threadIdx.x == 0) a.out_lengths[b] = keep;
   const int row0 = me * each * 32 + lane;  // this lane's rows: 32 apart
-  cluster_wait();
 
-  int moved = 0;
+  int moved = 0, clear = keep;
   uint32_t stay[NK ? NK : 1] = {};         // (NK > 0) the rows' keys
   if (n > a.keep) {
     int newest = INT_MIN;
@@ -111,12 +179,16 @@ template <int NK, typename U> __global__ void __launch_bounds__(kThreads, 2) evi
       for (int j = 0; j < each; ++j)
         if (row0 + 32 * j < n) newest = max(newest, pos[row0 + 32 * j]);
     }
-    newest = __reduce_max_sync(~0u, newest);
-    if (lane < a.ctas) store_in_cta(&largest[me], lane, newest);
-    cluster_sync();
-    newest = INT_MIN;
-    for (int k = lane; k < warps; k += 32) newest = max(newest, largest[k]);
-    newest = __reduce_max_sync(~0u, newest);
+    if (a.recent > 0) {
+      newest = __reduce_max_sync(~0u, newest);
+      if (lane < a.ctas) store_in_cta(&largest[me], lane, newest);
+      sync();
+      newest = INT_MIN;
+      for (int k = lane; k < warps; k += 32) newest = max(newest, largest[k]);
+      newest = __reduce_max_sync(~0u, newest);
+    } else {
+      newest = INT_MAX;  // (no position is above it)
+    }
     const int64_t old = (int64_t)newest - a.recent;  // positions up to this one are not kept for being recent
     const auto make_key = [&](int row, float weight, int32_t position) {
       return row < a.first || position > old ? 0xffffffffu : order_of(weight);
@@ -137,9 +209,9 @@ template <int NK, typename U> __global__ void __launch_bounds__(kThreads, 2) evi
 
     // The keep-th largest key, 8 bits at a time; `need` rows of it are kept, `same` have it.
     uint32_t threshold = 0;
-    int need = a.keep, same = 0;
+    int need = a.keep, same = INT_MAX;
 #pragma unroll 1
-    for (int digit = 0; digit < 4; ++digit) {
+    for (int digit = 0; digit < 4 && need < same; ++digit) {
       const int shift = 24 - 8 * digit;
       const uint32_t above = digit == 0 ? 0 : ~0u << (shift + 8);
       each_row([&](int j, int, bool there) {
@@ -147,7 +219,7 @@ template <int NK, typename U> __global__ void __launch_bounds__(kThreads, 2) evi
         const uint32_t key = key_of(j);
         if (((key ^ threshold) & above) == 0) atomicAdd(&histogram[digit][key >> shift & 255], 1);
       });
-      cluster_sync();
+      sync();
       if (warp == 0) {
         // A lane for 8 values, the largest first.
         int count[8], sum = 0;
@@ -177,13 +249,15 @@ template <int NK, typename U> __global__ void __launch_bounds__(kThreads, 2) evi
       __syncthreads();
       threshold |= found[digit], need = left[digit], same = alike[digit];
     }
-    // Rows of that key: the lowest `need` stay.
+    // Rows of that key: the lowest `need` stay.  (After fewer than four counts all that begin with its bits do: no key of theirs is
+    // below it.)
     Before equal{0, same};
-    if (need < same) {
+    const bool all = need == same;
+    if (!all) {
       int mine = 0;
       each_row([&](int j, int, bool there) { mine += __popc(__ballot_sync(~0u, there && key_of(j) == threshold)); });
       if (lane < a.ctas) store_in_cta(&counts[0][me], lane, mine);
-      cluster_sync();
+      sync();
       equal = count_before(counts[0], me, warps);
     }
     // Which rows stay; the targets below `keep`, the sources from there on.
@@ -191,7 +265,7 @@ template <int NK, typename U> __global__ void __launch_bounds__(kThreads, 2) evi
     const auto stays = [&](int j, bool there) {
       const uint32_t key = there ? key_of(j) : 0;
       const uint32_t its = __ballot_sync(~0u, there && key == threshold);
-      const bool yes = there && (key > threshold || (key == threshold && seen + __popc(its & ((1u << lane) - 1)) < need));
+      const bool yes = there && (key > threshold || (all && key == threshold) || (key == threshold && seen + __popc(its & ((1u << lane) - 1)) < need));
       seen += __popc(its);
       return yes;
     };
@@ -201,7 +275,7 @@ template <int NK, typename U> __global__ void __launch_bounds__(kThreads, 2) evi
       sources += __popc(__ballot_sync(~0u, row >= keep && yes));
     });
     if (lane < a.ctas) store_in_cta(&counts[1][me], lane, targets), store_in_cta(&counts[2][me], lane, sources);
-    cluster_sync();
+    sync();
     const Before t = count_before(counts[1], me, warps), s = count_before(counts[2], me, warps);
     moved = t.all;
     targets = t.before, sources = s.before, seen = equal.before;
@@ -213,33 +287,34 @@ template <int NK, typename U> __global__ void __launch_bounds__(kThreads, 2) evi
       if (there && row < keep && yes) out_w[row] = w[row], out_p[row] = pos[row];
       targets += __popc(to), sources += __popc(from);
     });
-    cluster_sync();
+    sync();
 
-    // Row by row, from the lists.
-    const int sub = lane & (a.lanes - 1), groups = warps * (32 / a.lanes), scaled = a.c.k_scale != nullptr;
-    for (int i = me * (32 / a.lanes) + lane / a.lanes; i < moved; i += groups) {
-      const int to = __ldcg(out_p + keep + i), from = __float_as_int(__ldcg(out_w + keep + i));
-      int64_t at_to, at_from, scale_to, scale_from;
-      const bool good_to = place_of(a, b, head, to, &at_to, &scale_to), good_from = place_of(a, b, head, from, &at_from, &scale_from);
-      if (good_to && good_from) {
-        const int size = sizeof(U), el = a.c.dtype == GAR_F32 ? 4 : a.c.dtype == GAR_I8 || a.c.dtype == GAR_E4M3 ? 1 : 2;
-        for (int u = sub; u < 2 * a.units; u += a.lanes) {
-          char *const base = static_cast<char *>(u < a.units ? a.c.k : a.c.v) + (int64_t)(u < a.units ? u : u - a.units) * size;
-          *reinterpret_cast<U *>(base + at_to * el) = *reinterpret_cast<const U *>(base + at_from * el);
-        }
-        if (scaled && sub == 0) a.c.k_scale[scale_to] = a.c.k_scale[scale_from], a.c.v_scale[scale_to] = a.c.v_scale[scale_from];
-      }
-      if (sub == 0) out_w[to] = w[from], out_p[to] = pos[from];
+    if (a.apart) {
+      clear = keep + moved;  // (the lists are cleared as they are read, by the kernel that moves the rows; they end at a -1)
+    } else {
+      const int per = 32 / a.lanes;
+      move_rows<U, false>(a, b, head, w, pos, out_w, out_p, keep, moved, me * per, warps * per);
+      sync();
     }
-    cluster_sync();
   } else {
     for (int j = 0; j < each; ++j) {
       const int row = row0 + 32 * j;
       if (row < n) out_w[row] = w[row], out_p[row] = pos[row];
     }
   }
-  for (int64_t row = keep + (int64_t)rank * kThreads + threadIdx.x; row < a.rows; row += (int64_t)a.ctas * kThreads)
+  for (int64_t row = clear + (int64_t)rank * kThreads + threadIdx.x; row < a.rows; row += (int64_t)a.ctas * kThreads)
     out_w[row] = 0.f, out_p[row] = -1;
+}
+
+// The lists' rows, by `parts` CTAs for each item.
+template <typename U> __global__ void __launch_bounds__(kThreads, 4) move_kernel(const EvictArgs a, int parts) {
+  after_earlier_kernels();
+  const int item = blockIdx.x / parts, part = blockIdx.x - item * parts, b = item / a.c.heads, head = item - b * a.c.heads;
+  const int n = min(a.lengths[b], a.most_rows), per = 32 / a.lanes;
+  if (n <= a.keep) return;
+  const int64_t at = (int64_t)item * a.rows;
+  move_rows<U, true>(a, b, head, a.weights + at, a.positions + at, a.out_weights + at, a.out_positions + at, a.keep, n - a.keep,
+                     (part * kWarps + (int)threadIdx.x / 32) * per, parts * kWarps * per);
 }
 
 }  // namespace
@@ -277,7 +352,7 @@ extern "C" int gar_kv_evict(const gar_kv_cache *cache, const float *weights, con
   a.keep = keep, a.first = first, a.recent = recent;
   // CTAs of an item: enough to fill the GPU with 2048 rows each at least, and so many that the keys fit the registers.
   a.ctas = 1;
-  while (a.ctas < kMostCtas && ((items * a.ctas < 152 * 2 && a.most_rows > 2048 * a.ctas) || a.most_rows > 16 * kThreads * a.ctas))
+  while (a.ctas < kMostCtas && ((items * a.ctas < 152 * 4 && a.most_rows > 2048 * a.ctas) || a.most_rows > 16 * kThreads * a.ctas))
     a.ctas *= 2;
   const int lanes = a.ctas * kThreads;
   a.each = std::max(1, (a.most_rows + lanes - 1) / lanes);
@@ -291,8 +366,14 @@ extern "C" int gar_kv_evict(const gar_kv_cache *cache, const float *weights, con
     a.units = cache->dim * size / (int)sizeof(U);
     a.lanes = 1;
     while (a.lanes < 32 && a.lanes < 2 * a.units) a.lanes *= 2;
-    const auto kernel = a.each <= 4 ? evict_kernel<4, U> : a.each <= 16 ? evict_kernel<16, U> : evict_kernel<0, U>;
-    return launch_clusters("gar_kv_evict", kernel, items * a.ctas, a.ctas, kThreads, stream, a);
+    const auto kernel = a.each <= 8 ? evict_kernel<8, U> : a.each <= 16 ? evict_kernel<16, U> : evict_kernel<0, U>;
+    // Many rows are moved by a kernel of its own, all over the GPU.
+    const int64_t most = std::min(a.most_rows - keep, keep - first), per = kWarps * (32 / a.lanes) * 4;
+    a.apart = most > 256;
+    if (int rc = launch_clusters("gar_kv_evict", kernel, items * a.ctas, a.ctas, kThreads, stream, a)) return rc;
+    if (!a.apart) return (int)GAR_OK;
+    const int parts = (int)std::max<int64_t>(1, std::min<int64_t>((most + per - 1) / per, 152 * 4 / items));
+    return launch("gar_kv_evict", move_kernel<U>, dim3((unsigned)(items * parts)), kThreads, 0, stream, a, parts);
   };
   if (all % 16 == 0) return run(type_tag<uint4>{});
   if (all % 4 == 0) return run(type_tag<uint32_t>{});
