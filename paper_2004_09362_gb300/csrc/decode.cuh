@@ -42,6 +42,7 @@ struct DecodeArgs {
   int unit;                // rows of a unit of the line
   int slack;               // units of 192 KB
   int solo;                // tiles of an item that a warp takes whole
+  bool line;               // a line, whatever the batch (where parts need no join)
   int batch, q_heads, group, item_groups, item_heads;  // group: q_heads / kv_heads
   // Sequences that share their rows count as one: its query m of a cached head is query m % heads_each, of that head, of
   // its sequence m / heads_each (share: its sequences; 0: there is nothing to share).
@@ -128,7 +129,7 @@ struct Walk {
     for (int i = b0; i < b1; ++i) mine += span_of(a, n = a.lengths[i], unit).units;
     int total = __reduce_add_sync(~0u, mine);
     lead = min(a.slack, quotient(total, a.batch));
-    if (run <= 1 && a.batch * items <= ctas) {
+    if (!a.line && run <= 1 && a.batch * items <= ctas) {
       // The smallest parts that are no more than the CTAs, from an equal share on.  Units that are no more than the
       // CTAs are such parts already.
       const int share = total * items <= ctas ? 1 : quotient(total * items + ctas - 1, ctas);

@@ -4,8 +4,8 @@
 // cores as in decode attention, S^T = K Q^T with 16 rows of the cache by 8 queries, but nothing of a tile is needed twice, so
 // keys go from memory to the registers that multiply them: which channel sits at which place of the summed
 // dimension is free as long as keys and queries agree, so a lane's part of a row is whole 16-byte chunks (lane t of the
-// four that share a row has chunks t, t + 4, ...).  A warp has the next tile's keys and the pages of the one after that on
-// their way.  The rows of all sequences are shared out among the CTAs as in decode attention, by equal numbers.
+// four that share a row has chunks t, t + 4, ...).  A warp copies its rows to a ring of its own, two tiles and
+// more ahead.  The rows of all sequences are shared out among the CTAs as in decode attention, by equal numbers.
 //
 // 8-bit codes become f16 exactly, as do the queries that go with them: the head's largest is brought to 2^14, 32-bit ones in two
 // parts.  Keys of 32 bits are multiplied in 32 bits without tensor cores.
@@ -18,8 +18,8 @@
 namespace gar {
 namespace {
 
-constexpr int kThreads = 256, kWarps = kThreads / 32, kResident = 2;
-constexpr int kHeads = 64;  // queries whose parts lie in shared memory at a time
+constexpr int kThreads = 256, kWarps = kThreads / 32;
+constexpr int kHeads = 32;  // queries whose parts lie in shared memory at a time
 
 struct WeighArgs {
   DecodeArgs d;
@@ -38,10 +38,14 @@ __device__ __forceinline__ float weight_of(float score, float2 f) {
   return f.y == INFINITY ? 0.f : exp2_fast(fmaf(score, f.x, -f.y));
 }
 
-// Entries of rows that the sequences do not have, or not in their window.
+// The warps that weigh.
+__device__ __forceinline__ void sync_weighing() { asm volatile("bar.sync 1, %0;" ::"n"(kThreads) : "memory"); }
+
+// Entries of rows that the sequences do not have, or not in their window: by the CTA's last warp, beside the others.
 __device__ __forceinline__ void copy_rest(const WeighArgs &a) {
   if (!a.apart) return;
-  const int items = a.d.batch * a.d.c.heads, parts = max(1, (int)gridDim.x / items);
+  constexpr int N = 8;  // loads in flight
+  const int lane = threadIdx.x & 31, items = a.d.batch * a.d.c.heads, parts = max(1, (int)gridDim.x / items);
   for (int64_t i = blockIdx.x; i < (int64_t)items * parts; i += gridDim.x) {
     const int item = (int)(i / parts), part = (int)(i - (int64_t)item * parts);
     const int b = (int)a.d.items((uint32_t)item), h = item - b * a.d.c.heads;
@@ -49,12 +53,47 @@ __device__ __forceinline__ void copy_rest(const WeighArgs &a) {
     const float *const from = a.weights + b * a.wb + h * a.wh;
     float *const to = a.out + b * a.ob + h * a.oh;
     const int64_t rest = a.rows - (s.hi - s.lo), each = (rest + parts - 1) / parts, end = min(rest, (part + 1) * each);
-    for (int64_t k = part * each + threadIdx.x; k < end; k += kThreads) {
-      const int64_t n = k < s.lo ? k : k + (s.hi - s.lo);
-      to[n] = from[n];
+    for (int64_t k0 = part * each + lane; k0 < end; k0 += 32 * N) {
+      float x[N];
+#pragma unroll
+      for (int j = 0; j < N; ++j) {
+        const int64_t k = k0 + 32 * j;
+        x[j] = k < end ? from[k < s.lo ? k : k + (s.hi - s.lo)] : 0.f;
+      }
+#pragma unroll
+      for (int j = 0; j < N; ++j) {
+        const int64_t k = k0 + 32 * j;
+        if (k < end) to[k < s.lo ? k : k + (s.hi - s.lo)] = x[j];
+      }
     }
   }
 }
+
+// A CTA's walk over its segments, kept in shared memory: in the registers it cost the keys their places.
+struct Course {
+  Walk walk;
+  Segment segment;
+  int more;
+  __device__ __forceinline__ void start(const DecodeArgs &d) {
+    if (threadIdx.x < 32) {
+      Walk w;
+      w.start(d);
+      if (threadIdx.x == 0) walk = w;
+    }
+  }
+  // By all threads; the segment stays until the next call.
+  __device__ __forceinline__ bool next(const DecodeArgs &d) {
+    sync_weighing();
+    if (threadIdx.x == 0) {
+      Walk w = walk;
+      Segment s;
+      more = w.next(d, &s);
+      walk = w, segment = s;
+    }
+    sync_weighing();
+    return more != 0;
+  }
+};
 
 // Where a row's keys are and, over 8-bit caches, its scale; -1: on no page, or outside the segment.
 __device__ __forceinline__ int64_t key_at(const DecodeArgs &d, const Segment &g, int n, int64_t *scale) {
@@ -74,33 +113,95 @@ template <typename C, int KC, bool Q32> struct WeighShape {
   static constexpr int CH = 16 / sizeof(C);                    // channels of a chunk
   static constexpr int W4 = CH / 8;                            // 16-byte words of a chunk's queries
   static constexpr int PARTS = Q32 ? 2 : 1;
+  static constexpr int CHUNKS = 4 * KC, ROW = 64 * KC;         // of a row: chunks, bytes
+  static constexpr int kStage = 16 * ROW + 128;                // a tile's keys, 16 weights, 16 scales
+  static constexpr int kResident = KC <= 4 ? 2 : 1;            // CTAs of an SM
+  static constexpr int kStages = KC == 1 ? 8 : KC == 2 ? 6 : KC == 3 ? 4 : 3;
+  static constexpr int kRings = kWarps * kStages * kStage;
+  // Where chunk c of row r lies: rows of a multiple of 128 bytes twisted, so that the 8 lanes of a read meet all banks.
+  static __device__ __forceinline__ int place(int r, int c) { return KC % 2 == 0 ? c ^ (r & 1) * 4 : c; }
   // words: [group of 8 queries][part][chunk][W4][lane]
   static constexpr int kGroup = PARTS * KC * W4 * 32;
 };
 
-template <typename C, int KC, bool Q32> __global__ void __launch_bounds__(kThreads, kResident) weigh_mma(const WeighArgs a) {
+template <typename C, int KC, bool Q32> __global__ void __launch_bounds__(kThreads + 32, WeighShape<C, KC, Q32>::kResident) weigh_mma(const WeighArgs a) {
   using S = WeighShape<C, KC, Q32>;
   using T = typename operand<C>::type;
   constexpr bool Q8 = quantised<C>::value;
-  extern __shared__ uint4 queries[];
+  extern __shared__ __align__(16) char shared[];
+  constexpr int STEP = 16 * kWarps;
   __shared__ float2 factor[kHeads];
   __shared__ float down[kHeads];
   const DecodeArgs &d = a.d;
   const gar_kv_cache &c = d.c;
   const int warp = threadIdx.x / 32, lane = threadIdx.x & 31, g = lane / 4, t = lane & 3;
+  // The queries' parts are behind the warps' rings.
+  char *const rings = shared + warp * (S::kStages * S::kStage);
+  const uint32_t ring = (uint32_t)__cvta_generic_to_shared(rings);
+  uint4 *const queries = reinterpret_cast<uint4 *>(shared + S::kRings);
   after_earlier_kernels();
-  copy_rest(a);
-  Walk walk;
-  walk.start(d);
-  Segment seg;
-  while (walk.next(d, &seg)) {
+  if (warp == kWarps) return copy_rest(a);
+  __shared__ Course course;
+  course.start(d);
+  while (course.next(d)) {
+    const Segment &seg = course.segment;
     if (seg.lo >= seg.to) continue;
     const float *const w = a.weights + seg.b * a.wb + seg.kv_head * a.wh;
     float *const out = a.out + seg.b * a.ob + seg.kv_head * a.oh;
     for (int head0 = 0; head0 < d.group; head0 += kHeads) {
       const int heads = min(kHeads, d.group - head0), groups = (heads + 7) / 8;
       const int64_t q0 = seg.b * d.qb + (seg.head + head0) * d.qh;
-      __syncthreads();
+      const bool first = head0 == 0;
+      if (!first) sync_weighing();  // (what the queries before these have left in `out` is read)
+
+      // Rows are copied to the warp's ring, tiles ahead of the products.  Pages are looked up a tile before they are used, and
+      // checked only then.
+      const int lo = seg.lo, to = seg.to, kv_head = seg.kv_head;
+      const int32_t *const table = d.table + seg.b * d.table_stride;
+      const char *const keys = static_cast<const char *>(c.k) + kv_head * c.head_stride * (int)sizeof(C);
+      const float *const from = first ? w : out;
+      int page, in;  // of this lane's row (of 16) of the tile to be copied next
+      const auto look = [&](int n0) {
+        const int n = n0 + (lane & 15), p = (int)d.page((uint32_t)n);
+        in = n >= lo && n < to ? n - p * c.page_size : -1;
+        page = in >= 0 ? table[p] : 0;
+      };
+      const auto copy = [&](int n0, int stage) {
+        const uint32_t at = ring + stage * S::kStage;
+        bool there = in >= 0;
+        if (lane < 16) copy_async<4>(at + 16 * S::ROW + lane * 4, there ? from + n0 + lane : from, there);
+        if (there && (unsigned)page >= (uint64_t)c.pages) {
+          if (c.status) atomicOr(c.status, GAR_KV_BAD_PAGE);
+          there = false;
+        }
+        if (Q8 && lane < 16) {
+          const int64_t scale_at = there ? page * c.scale_page_stride + kv_head * c.scale_head_stride + in * c.scale_token_stride : 0;
+          copy_async<4>(at + 16 * S::ROW + 64 + lane * 4, c.k_scale + scale_at, there);
+        }
+        const int64_t row_at = there ? (page * c.page_stride + in * c.token_stride) * (int)sizeof(C) : -1;
+        look(n0 + STEP);
+#pragma unroll
+        for (int i = 0; i < 16 * S::CHUNKS / 32; ++i) {
+          const int x = i * 32 + lane, row = x / S::CHUNKS, chunk = x - row * S::CHUNKS;
+          const int64_t y = __shfl_sync(~0u, row_at, row);
+          const bool has = y >= 0 && chunk * S::CH < c.dim;
+          copy_async<16>(at + row * S::ROW + S::place(row, chunk) * 16, has ? keys + y + chunk * 16 : keys, has);
+        }
+        asm volatile("cp.async.commit_group;" ::: "memory");
+      };
+      int n0 = seg.from + 16 * warp, ahead = n0, in_stage = 0, out_stage = 0;
+      look(n0);
+      const auto pump = [&] {
+        if (ahead < to)
+          copy(ahead, in_stage);
+        else
+          asm volatile("cp.async.commit_group;" ::: "memory");
+        ahead += STEP;
+        if (++in_stage == S::kStages) in_stage = 0;
+      };
+#pragma unroll 1
+      for (int i = 0; i < S::kStages - 1; ++i) pump();
+      sync_weighing();
       for (int h = warp; h < 8 * groups; h += kWarps) {
         float up = 1.f, shrink = 1.f;
         if (Q8 && d.q_dtype != GAR_F16 && h < heads) {
@@ -115,7 +216,7 @@ template <typename C, int KC, bool Q32> __global__ void __launch_bounds__(kThrea
           down[h] = shrink;
         }
       }
-      __syncthreads();
+      sync_weighing();
       for (int i = threadIdx.x; i < groups * KC * S::W4 * 32; i += kThreads) {
         const int l = i & 31, rest = i / 32, x = rest % S::W4, k = rest / S::W4 % KC, ng = rest / S::W4 / KC;
         const int h = 8 * ng + l / 4, channel = ((l & 3) + 4 * k) * S::CH + 8 * x;
@@ -135,46 +236,24 @@ template <typename C, int KC, bool Q32> __global__ void __launch_bounds__(kThrea
         for (int p = 0; p < S::PARTS; ++p)
           queries[ng * S::kGroup + ((p * KC + k) * S::W4 + x) * 32 + l] = make_uint4(word[p][0], word[p][1], word[p][2], word[p][3]);
       }
-      __syncthreads();
-      const bool first = head0 == 0;
-
-      int64_t at[2], scale_at[2];
-      uint4 key[2][KC];
-      float key_scale[2], before[2];
-      const auto look = [&](int n0) {
-#pragma unroll
-        for (int r = 0; r < 2; ++r) at[r] = key_at(d, seg, n0 + g + 8 * r, &scale_at[r]);
-      };
-      const auto fetch = [&](int n0) {
-#pragma unroll
-        for (int r = 0; r < 2; ++r) {
-          const char *const p = static_cast<const char *>(c.k) + at[r] * (int)sizeof(C);
-#pragma unroll
-          for (int k = 0; k < KC; ++k) {
-            const int channel = (t + 4 * k) * S::CH;
-            key[r][k] = at[r] >= 0 && channel < c.dim ? __ldg(reinterpret_cast<const uint4 *>(p + (t + 4 * k) * 16)) : make_uint4(0, 0, 0, 0);
-          }
-          key_scale[r] = Q8 ? (at[r] >= 0 ? c.k_scale[scale_at[r]] : 0.f) : 1.f;
-          const int n = n0 + g + 8 * r;
-          before[r] = t == r && n >= seg.lo && n < seg.to ? (first ? w : out)[n] : 0.f;
-        }
-      };
-      constexpr int STEP = 16 * kWarps;
-      int n0 = seg.from + 16 * warp;
-      look(n0);
-      fetch(n0);
-      look(n0 + STEP);
-      for (; n0 < seg.to; n0 += STEP) {
+      sync_weighing();
+      for (; n0 < to; n0 += STEP) {
+        pump();
+        asm volatile("cp.async.wait_group %0;" ::"n"(S::kStages - 1) : "memory");
+        __syncwarp();
+        const char *const tile = rings + out_stage * S::kStage;
+        if (++out_stage == S::kStages) out_stage = 0;
         uint4 now[2][KC];
-        float scale[2], sum[2] = {before[0], before[1]}, p[2] = {0.f, 0.f};
+        float scale[2], sum[2], p[2] = {0.f, 0.f};
 #pragma unroll
         for (int r = 0; r < 2; ++r) {
-          scale[r] = key_scale[r];
+          const int row = g + 8 * r;
 #pragma unroll
-          for (int k = 0; k < KC; ++k) now[r][k] = key[r][k];
+          for (int k = 0; k < KC; ++k) now[r][k] = *reinterpret_cast<const uint4 *>(tile + row * S::ROW + S::place(row, t + 4 * k) * 16);
+          sum[r] = reinterpret_cast<const float *>(tile + 16 * S::ROW)[row];
+          scale[r] = Q8 ? reinterpret_cast<const float *>(tile + 16 * S::ROW)[16 + row] : 1.f;
         }
-        fetch(n0 + STEP);
-        look(n0 + 2 * STEP);
+        __syncwarp();  // (the stage may be copied to again)
         for (int ng = 0; ng < groups; ++ng) {
           float s[2][4] = {};
           const uint4 *const q = queries + ng * S::kGroup + lane;
@@ -213,7 +292,7 @@ template <typename C, int KC, bool Q32> __global__ void __launch_bounds__(kThrea
           p[r] += __shfl_xor_sync(~0u, p[r], 1);
           p[r] += __shfl_xor_sync(~0u, p[r], 2);
           const int n = n0 + g + 8 * r;
-          if (t == r && n >= seg.lo && n < seg.to) out[n] = sum[r] + p[r];
+          if (t == r && n >= lo && n < to) out[n] = sum[r] + p[r];
         }
       }
     }
@@ -221,7 +300,7 @@ template <typename C, int KC, bool Q32> __global__ void __launch_bounds__(kThrea
 }
 
 // Any types, strides and alignment; 32-bit keys.  A warp takes a row, a lane every 32nd of the groups of V channels.
-template <typename C, int V> __global__ void __launch_bounds__(kThreads) weigh_plain(const WeighArgs a) {
+template <typename C, int V> __global__ void __launch_bounds__(kThreads + 32) weigh_plain(const WeighArgs a) {
   extern __shared__ float query[];  // [heads][dim]
   __shared__ float2 factor[kHeads];
   const DecodeArgs &d = a.d;
@@ -231,24 +310,24 @@ template <typename C, int V> __global__ void __launch_bounds__(kThreads) weigh_p
   constexpr int ROWS = 4;                          // at a time
   const int warp = threadIdx.x / 32, lane = threadIdx.x & 31;
   after_earlier_kernels();
-  copy_rest(a);
-  Walk walk;
-  walk.start(d);
-  Segment seg;
-  while (walk.next(d, &seg)) {
+  if (warp == kWarps) return copy_rest(a);
+  __shared__ Course course;
+  course.start(d);
+  while (course.next(d)) {
+    const Segment &seg = course.segment;
     if (seg.lo >= seg.to) continue;
     const float *const w = a.weights + seg.b * a.wb + seg.kv_head * a.wh;
     float *const out = a.out + seg.b * a.ob + seg.kv_head * a.oh;
     for (int head0 = 0; head0 < d.group; head0 += kHeads) {
       const int heads = min(kHeads, d.group - head0);
       const int64_t q0 = seg.b * d.qb + (seg.head + head0) * d.qh;
-      __syncthreads();
+      sync_weighing();
       for (int i = threadIdx.x; i < heads * c.dim; i += kThreads) {
         const int h = i / c.dim;
         query[i] = load_q(d, q0 + h * d.qh + (i - h * c.dim));
       }
       for (int h = threadIdx.x; h < heads; h += kThreads) factor[h] = factor_of(a, seg.b, h, seg.head + head0 + h, 1.f);
-      __syncthreads();
+      sync_weighing();
       const float *const base = head0 == 0 ? w : out;
       for (int n0 = seg.lo + ROWS * warp; n0 < seg.to; n0 += ROWS * kWarps) {
         float key[ROWS][MOST][V], scale[ROWS];
@@ -301,13 +380,13 @@ template <typename C, int V> __global__ void __launch_bounds__(kThreads) weigh_p
 template <typename C, int KC, bool Q32> int launch_mma_weigh(const WeighArgs &a, int sms, gar_stream_t stream) {
   using S = WeighShape<C, KC, Q32>;
   constexpr auto kernel = weigh_mma<C, KC, Q32>;
-  const size_t shared = (size_t)((std::min(a.d.group, kHeads) + 7) / 8) * S::kGroup * 16;
+  const size_t shared = S::kRings + (size_t)((std::min(a.d.group, kHeads) + 7) / 8) * S::kGroup * 16;
   static DeviceSet allowed;
   const int e = once_for_device(allowed, a.d.device, [&] {
-    return (int)cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kHeads / 8 * S::kGroup * 16);
+    return (int)cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, S::kRings + kHeads / 8 * S::kGroup * 16);
   });
   if (e != 0) return cuda_fail((cudaError_t)e, "cudaFuncSetAttribute");
-  return launch("gar_kv_weigh", kernel, sms * kResident, kThreads, shared, stream, a);
+  return launch("gar_kv_weigh", kernel, sms * S::kResident, kThreads + 32, shared, stream, a);
 }
 
 template <typename C, bool Q32> int weigh(const WeighArgs &a, int sms, gar_stream_t stream) {
@@ -331,7 +410,7 @@ template <typename C, int V> int weigh_any(const WeighArgs &a, int sms, gar_stre
     return (int)cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kHeads * GAR_MAX_HEAD_DIM * 4);
   });
   if (e != 0) return cuda_fail((cudaError_t)e, "cudaFuncSetAttribute");
-  return launch("gar_kv_weigh", kernel, sms * kResident, kThreads, (size_t)std::min(a.d.group, kHeads) * a.d.c.dim * 4, stream, a);
+  return launch("gar_kv_weigh", kernel, sms * 2, kThreads + 32, (size_t)std::min(a.d.group, kHeads) * a.d.c.dim * 4, stream, a);
 }
 
 // Keys can be loaded 16 bytes at a time.
@@ -380,7 +459,7 @@ extern "C" int gar_kv_weigh(const gar_kv_cache *cache, const void *q, int64_t q_
   d.table = page_table, d.table_stride = table_stride, d.lengths = lengths;
   d.page = divide_by((uint32_t)cache->page_size), d.items = divide_by((uint32_t)cache->heads);
   d.most_rows = most_rows, d.batch = batch, d.q_heads = q_heads, d.window = window, d.unit = unit, d.device = dev;
-  d.group = d.item_heads = q_heads / cache->heads, d.item_groups = 1;
+  d.group = d.item_heads = q_heads / cache->heads, d.item_groups = 1, d.line = true;
   d.slack = std::max(1, 32768 / (64 * cache->dim * element_size(cache->dtype)));
   d.scale_log2 = (float)((double)scale * 1.4426950408889634);
   a.lse = lse, a.weights = weights, a.out = out, a.rows = rows, a.apart = out != weights;
