@@ -31,7 +31,8 @@ BUILD = os.path.join(ROOT, "_build")
 SOURCES = ["api.cpp", "plan.cpp", "codegen.cpp", "jit.cpp", "step_kernels.cu", "rope.cu", "cache.cu",
            "decode_api.cu", "decode_general.cu", "decode_mma_bf16.cu", "decode_mma_f16.cu", "decode_mma_i8.cu",
            "decode_mma_e4m3.cu", "decode_mma_f32.cu", "decode_mma_i8_f32.cu", "decode_mma_e4m3_f32.cu",
-           "prefix.cu", "prefix_mma.cu", "weigh.cu", "evict.cu", "verify.cu"]
+           "serve_mma_bf16.cu", "serve_mma_f16.cu", "serve_mma_i8.cu", "serve_mma_e4m3.cu", "serve_mma_f32.cu",
+           "serve_mma_i8_f32.cu", "serve_mma_e4m3_f32.cu", "prefix.cu", "prefix_mma.cu", "weigh.cu", "evict.cu", "verify.cu"]
 HEADERS = ["gar_internal.hpp", "gar_device.cuh", "decode.cuh", "decode_mma.cuh", "device_once.hpp", "cluster.cuh", "prefix.cuh", "tcgen05.cuh"]
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 

@@ -42,12 +42,7 @@ struct DecodeArgs {
   int unit;                // rows of a unit of the line
   int slack;               // units of 192 KB
   int solo;                // tiles of an item that a warp takes whole
-  bool line;               // a line, whatever the batch (where parts need no join)
   int batch, q_heads, group, item_groups, item_heads;  // group: q_heads / kv_heads
-  // Sequences that share their rows count as one: its query m of a cached head is query m % heads_each, of that head, of
-  // its sequence m / heads_each (share: its sequences; 0: there is nothing to share).
-  int share, heads_each;
-  Divide by_heads;         // by heads_each
   Divide items;            // by a sequence's items
   int q_dtype, out_dtype, window;
   bool out_wide;           // four neighbouring outputs can be stored at once
@@ -69,6 +64,20 @@ inline int unit_of(int64_t items, int most_rows) {
   return 0;
 }
 
+// What calls of a batch that shares rows, and others than decode attention, need beside that.  (A type of its own: the same kernels
+// with these questions in them took 206 us over the e4m3 batch above, then 220.)
+struct ServingArgs : DecodeArgs {
+  bool line;               // a line, whatever the batch (where parts need no join)
+  // Sequences that share their rows count as one: its query m of a cached head is query m % heads_each, of that head, of
+  // its sequence m / heads_each (share: its sequences; 0: there is nothing to share).
+  int share, heads_each;
+  Divide by_heads;         // by heads_each
+  // Rows that come before each sequence's own (or null): before_share sequences have one row of this table.
+  const int32_t *before_table, *before_lengths;
+  int64_t before_stride;
+  int before_share, before_most, own_most;
+};
+
 // x / d; a division in 32-bit floats, put right, where they hold x (the compiler's takes three times as long).
 __device__ __forceinline__ int quotient(int x, int d) {
   if (x >= 1 << 23) return x / d;
@@ -78,6 +87,32 @@ __device__ __forceinline__ int quotient(int x, int d) {
   const int rest = x - q * d;
   return rest >= d ? q + 1 : rest < 0 ? q - 1 : q;
 }
+
+// A length within what a table can hold.
+__device__ __forceinline__ int held(const DecodeArgs &a, int n, int most) {
+  if (n >= 0 && n <= most) return n;
+  if (a.c.status) atomicOr(a.c.status, GAR_KV_BAD_LENGTH);
+  return n < 0 ? 0 : most;
+}
+// The rows before a sequence's own, and all of its rows.
+__device__ __forceinline__ int before_of(const ServingArgs &a, int b) { return held(a, a.before_lengths[b / a.before_share], a.before_most); }
+__device__ __forceinline__ int length_of(const DecodeArgs &a, int b) { return a.lengths[b]; }
+__device__ __forceinline__ int length_of(const ServingArgs &a, int b) {
+  const int n = a.lengths[b];
+  return a.before_lengths == nullptr ? n : held(a, n, a.own_most) + before_of(a, b);
+}
+// The pages that have row n of a sequence, which becomes the row of those pages.
+__device__ __forceinline__ const int32_t *table_of(const DecodeArgs &a, int b, int &) { return a.table + b * a.table_stride; }
+__device__ __forceinline__ const int32_t *table_of(const ServingArgs &a, int b, int &n) {
+  if (a.before_lengths != nullptr) {
+    const int before = before_of(a, b);
+    if (n < before) return a.before_table + b / a.before_share * a.before_stride;
+    n -= before;
+  }
+  return a.table + b * a.table_stride;
+}
+__device__ __forceinline__ bool in_a_line(const DecodeArgs &) { return false; }
+__device__ __forceinline__ bool in_a_line(const ServingArgs &a) { return a.line; }
 
 struct Span {
   int units;
@@ -120,16 +155,16 @@ struct Walk {
 
   // By each warp on its own: a lane adds up a run of sequences, a scan over the lanes follows, and
   // the lane whose run holds the share's start looks it up.
-  __device__ __forceinline__ void start(const DecodeArgs &a) {
+  template <typename A> __device__ __forceinline__ void start(const A &a) {
     const int lane = threadIdx.x & 31, run = (a.batch + 31) / 32;
     const int b0 = min(a.batch, lane * run), b1 = min(a.batch, b0 + run);
     const int items = a.c.heads * a.item_groups, ctas = gridDim.x;
     unit = a.unit;
     int mine = 0, n = 0;
-    for (int i = b0; i < b1; ++i) mine += span_of(a, n = a.lengths[i], unit).units;
+    for (int i = b0; i < b1; ++i) mine += span_of(a, n = length_of(a, i), unit).units;
     int total = __reduce_add_sync(~0u, mine);
     lead = min(a.slack, quotient(total, a.batch));
-    if (!a.line && run <= 1 && a.batch * items <= ctas) {
+    if (!in_a_line(a) && run <= 1 && a.batch * items <= ctas) {
       // The smallest parts that are no more than the CTAs, from an equal share on.  Units that are no more than the
       // CTAs are such parts already.
       const int share = total * items <= ctas ? 1 : quotient(total * items + ctas - 1, ctas);
@@ -169,7 +204,7 @@ struct Walk {
     const bool here = pos >= before && pos < before + mine;
     if (here && run > 1)
       for (; i < b1; ++i) {
-        n = a.lengths[i];
+        n = length_of(a, i);
         const int units = (span_of(a, n, unit).units + lead) * items;
         if (pos < before + units) break;
         before += units;
@@ -182,16 +217,16 @@ struct Walk {
     first_segment = true;
   }
 
-  __device__ __forceinline__ void enter(const DecodeArgs &a, int sequence, int n) {
+  template <typename A> __device__ __forceinline__ void enter(const A &a, int sequence, int n) {
     b = sequence;
     s = span_of(a, n, unit);
     s.units += lead;
   }
 
-  __device__ __forceinline__ bool next(const DecodeArgs &a, Segment *g) {
+  template <typename A> __device__ __forceinline__ bool next(const A &a, Segment *g) {
     if (pos >= end) return false;
     if (!first_segment) {
-      if (++hh == a.c.heads * a.item_groups) hh = 0, enter(a, b + 1, a.lengths[b + 1]);
+      if (++hh == a.c.heads * a.item_groups) hh = 0, enter(a, b + 1, length_of(a, b + 1));
       item = pos;
     }
     const int u = pos - item, n = min(s.units - u, end - pos);
@@ -231,7 +266,7 @@ struct Notes {
   int begin, end, per, lead, unit;  // of the walk
   int next_item, at;                // the first item that is not noted yet, and where in the line it begins
 
-  __device__ __forceinline__ void start(const DecodeArgs &a) {
+  template <typename A> __device__ __forceinline__ void start(const A &a) {
     Walk w;
     w.start(a);
     begin = w.pos, end = w.end, per = w.per, lead = w.lead, unit = w.unit;
@@ -241,14 +276,14 @@ struct Notes {
   __device__ __forceinline__ bool more() const { return at < end && begin < end; }
 
   // Lane i < kNotes: the i-th of the next segments, or none (from > to).
-  __device__ __forceinline__ bool next(const DecodeArgs &a, Note *n) {
+  template <typename A> __device__ __forceinline__ bool next(const A &a, Note *n) {
     const int lane = threadIdx.x & 31, items = a.c.heads * a.item_groups;
     const int item = next_item + min(lane, kNotes - 1);
     n->b = (int)a.items((uint32_t)item);
     n->hh = item - n->b * items;
     Span s{};
     if (n->b < a.batch) {
-      s = span_of(a, a.lengths[n->b], unit);
+      s = span_of(a, length_of(a, n->b), unit);
       s.units += lead;
     }
     int upto = s.units;
@@ -317,7 +352,8 @@ __device__ __forceinline__ void store_out(const DecodeArgs &a, int64_t at, float
 }
 
 // Where the queries of head h of a segment are.
-__device__ __forceinline__ int64_t query_at(const DecodeArgs &a, const Segment &g, int h) {
+__device__ __forceinline__ int64_t query_at(const DecodeArgs &a, const Segment &g, int h) { return g.b * a.qb + (g.head + h) * a.qh; }
+__device__ __forceinline__ int64_t query_at(const ServingArgs &a, const Segment &g, int h) {
   if (a.share == 0) return g.b * a.qb + (g.head + h) * a.qh;
   const int m = g.head + h - g.kv_head * a.group, i = (int)a.by_heads((uint32_t)m);
   return ((int64_t)g.b * a.share + i) * a.qb + (g.kv_head * a.heads_each + (m - i * a.heads_each)) * a.qh;
@@ -480,13 +516,22 @@ __device__ __forceinline__ void join_parts(const DecodeArgs &a, const Segment &g
   group.sync();
 }
 
+// decode_mma_<cache>[_f32]: the cache's type, and 32-bit queries over 8 bits.
 int decode_general(const DecodeArgs &a, int sms, gar_stream_t stream);
 int decode_mma_bf16(const DecodeArgs &a, int sms, gar_stream_t stream);
 int decode_mma_f16(const DecodeArgs &a, int sms, gar_stream_t stream);
 int decode_mma_i8(const DecodeArgs &a, int sms, gar_stream_t stream);
 int decode_mma_e4m3(const DecodeArgs &a, int sms, gar_stream_t stream);
 int decode_mma_f32(const DecodeArgs &a, int sms, gar_stream_t stream);
-int decode_mma_i8_f32(const DecodeArgs &a, int sms, gar_stream_t stream);    // 32-bit queries
+int decode_mma_i8_f32(const DecodeArgs &a, int sms, gar_stream_t stream);
 int decode_mma_e4m3_f32(const DecodeArgs &a, int sms, gar_stream_t stream);
+int decode_general(const ServingArgs &a, int sms, gar_stream_t stream);
+int decode_mma_bf16(const ServingArgs &a, int sms, gar_stream_t stream);
+int decode_mma_f16(const ServingArgs &a, int sms, gar_stream_t stream);
+int decode_mma_i8(const ServingArgs &a, int sms, gar_stream_t stream);
+int decode_mma_e4m3(const ServingArgs &a, int sms, gar_stream_t stream);
+int decode_mma_f32(const ServingArgs &a, int sms, gar_stream_t stream);
+int decode_mma_i8_f32(const ServingArgs &a, int sms, gar_stream_t stream);
+int decode_mma_e4m3_f32(const ServingArgs &a, int sms, gar_stream_t stream);
 
 }  // namespace gar

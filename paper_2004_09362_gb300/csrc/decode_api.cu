@@ -84,6 +84,11 @@ constexpr int kManyQueries = 24;
 constexpr int kManyItems = 1024;  // blocks of queries at most: each has 132 KB of partial results
 int blocks_of(int rows) { return rows > 128 ? (rows + 255) / 256 : 1; }
 
+// Bytes of all sequences' rows, a shared one counted for each, up to which they are read for each sequence, mostly from the L2, in one
+// launch.  (That and the three launches that read a prefix once, 32/8 heads x 128 bf16: 5 x 425 rows, 9 MB, 11 us and 30; 5 x 4000, 82
+// MB, 20 and 32; 16 x 2000, 132 MB, 24 and 30; 64 x 500, 148 MB, 37 and 40; 120 x 1000 of 16/4 x 64 i8, 69 MB, 38 and 41.)
+constexpr double kReread = 128 << 20;
+
 bool many_queries(const gar_attn_plan &plan, int batch, int groups) {
   if (groups == 0 || plan.dim > 128) return false;
   const int rows = batch / groups * (plan.q_heads / plan.kv_heads);
@@ -99,9 +104,9 @@ size_t prefix_bytes(const gar_attn_plan &plan, int batch, int groups) {
 }
 
 // The arguments that follow from the plan, the cache and what a call has set.
-int complete(const gar_attn_plan *plan, const gar_kv_cache *cache, int table_width, float scale, DecodeArgs *a) {
+int complete(const gar_attn_plan *plan, const gar_kv_cache *cache, int64_t rows, float scale, DecodeArgs *a) {
   // Row numbers stay below 2^31 with room for a tile past the end.
-  const int most_rows = (int)std::min<int64_t>((int64_t)table_width * cache->page_size, 0x7fffffff - 65536);
+  const int most_rows = (int)std::min<int64_t>(rows, 0x7fffffff - 65536);
   const int unit = unit_of((int64_t)a->batch * plan->kv_heads * ((a->group + 7) / 8), most_rows);
   if (unit == 0) return refuse("too many sequences and heads for tables this wide");
   if (plan->ws == nullptr) {
@@ -130,15 +135,15 @@ int complete(const gar_attn_plan *plan, const gar_kv_cache *cache, int table_wid
   return GAR_OK;
 }
 
-int decode(const gar_attn_plan *plan, const DecodeArgs &a, gar_stream_t stream) {
+template <typename A> int decode(const gar_attn_plan *plan, const A &a, gar_stream_t stream) {
   if (!takes_mma(a.c, a.q, a.qb, a.qh, a.q_dtype)) return decode_general(a, plan->sms, stream);
   const bool q32 = a.q_dtype == GAR_F32;
   switch (a.c.dtype) {
     case GAR_F32: return decode_mma_f32(a, plan->sms, stream);
     case GAR_BF16: return decode_mma_bf16(a, plan->sms, stream);
     case GAR_F16: return decode_mma_f16(a, plan->sms, stream);
-    case GAR_I8: return (q32 ? decode_mma_i8_f32 : decode_mma_i8)(a, plan->sms, stream);
-    default: return (q32 ? decode_mma_e4m3_f32 : decode_mma_e4m3)(a, plan->sms, stream);
+    case GAR_I8: return q32 ? decode_mma_i8_f32(a, plan->sms, stream) : decode_mma_i8(a, plan->sms, stream);
+    default: return q32 ? decode_mma_e4m3_f32(a, plan->sms, stream) : decode_mma_e4m3(a, plan->sms, stream);
   }
 }
 
@@ -230,7 +235,7 @@ int gar_decode_attention(gar_attn_plan *plan, const gar_kv_cache *cache, const v
   a.table = page_table, a.table_stride = table_stride, a.lengths = lengths;
   a.batch = batch, a.q_dtype = q_dtype, a.out_dtype = out_dtype, a.window = window;
   a.group = plan->q_heads / plan->kv_heads;
-  if (int rc = complete(plan, cache, table_width, scale, &a)) return rc;
+  if (int rc = complete(plan, cache, (int64_t)table_width * cache->page_size, scale, &a)) return rc;
   return decode(plan, a, stream);
 }
 
@@ -272,9 +277,9 @@ int gar_prefix_attention(gar_attn_plan *plan, const gar_kv_cache *cache, const v
   }
   const size_t half = prefix_workspace(batch, heads, dim, static_cast<char *>(workspace), parts) / 2;
   // The parts' results: the sequences' own rows, and the prefixes with a group's queries as those of one sequence.
-  DecodeArgs a{};
-  a.q = q, a.qb = q_batch_stride, a.qh = q_head_stride, a.q_dtype = q_dtype, a.out_dtype = GAR_F32;
-  DecodeArgs own = a, prefix = a;
+  ServingArgs own{}, prefix{};
+  for (DecodeArgs *a : {static_cast<DecodeArgs *>(&own), static_cast<DecodeArgs *>(&prefix)})
+    a->q = q, a->qb = q_batch_stride, a->qh = q_head_stride, a->q_dtype = q_dtype, a->out_dtype = GAR_F32;
   const int64_t row = parts[0].row;
   own.out = parts[0].out, own.lse = parts[0].lse, own.ob = heads * row, own.oh = row;
   own.table = page_table, own.table_stride = table_stride, own.lengths = lengths;
@@ -283,8 +288,17 @@ int gar_prefix_attention(gar_attn_plan *plan, const gar_kv_cache *cache, const v
   prefix.table = prefix_table, prefix.table_stride = prefix_stride, prefix.lengths = prefix_lengths;
   prefix.batch = groups, prefix.group = share * group;
   prefix.share = share, prefix.heads_each = group, prefix.by_heads = divide_by((uint32_t)group);
-  if (int rc = complete(plan, cache, table_width, scale, &own)) return rc;
-  if (int rc = complete(plan, cache, prefix_width, scale, &prefix)) return rc;
+  const int64_t own_rows = (int64_t)table_width * cache->page_size, prefix_rows = (int64_t)prefix_width * cache->page_size;
+  if ((double)(own_rows + prefix_rows) * batch * cache->heads * dim * element_size(cache->dtype) * 2 <= kReread) {
+    // As sequences of their own, the prefix's rows first.
+    own.out = out, own.lse = lse, own.ob = out_batch_stride, own.oh = out_head_stride, own.out_dtype = out_dtype;
+    own.before_table = prefix_table, own.before_stride = prefix_stride, own.before_lengths = prefix_lengths;
+    own.before_share = share, own.before_most = (int)prefix_rows, own.own_most = (int)own_rows;
+    if (int rc = complete(plan, cache, own_rows + prefix_rows, scale, &own)) return rc;
+    return decode(plan, own, stream);
+  }
+  if (int rc = complete(plan, cache, own_rows, scale, &own)) return rc;
+  if (int rc = complete(plan, cache, prefix_rows, scale, &prefix)) return rc;
   JoinArgs j{};
   j.parts[0] = parts[0], j.parts[1] = parts[1];
   j.out = out, j.ob = out_batch_stride, j.oh = out_head_stride, j.out_dtype = out_dtype, j.lse = lse;
@@ -310,11 +324,11 @@ int gar_prefix_attention(gar_attn_plan *plan, const gar_kv_cache *cache, const v
     if (dim % 64 || p.box == 0 || !box_map(*cache, cache->k, p.box, false, &maps[0]) || !box_map(*cache, cache->v, p.box, false, &maps[1]))
       p.box = 0;
     if (int rc = prefix_mma(p, maps, stream)) return rc;
-    if (int rc = decode(plan, own, stream)) return rc;
+    if (int rc = decode(plan, static_cast<const DecodeArgs &>(own), stream)) return rc;
     return join_partials(p, j, stream);
   }
   if (int rc = decode(plan, prefix, stream)) return rc;
-  if (int rc = decode(plan, own, stream)) return rc;
+  if (int rc = decode(plan, static_cast<const DecodeArgs &>(own), stream)) return rc;
   return join_prefix(j, stream);
 }
 

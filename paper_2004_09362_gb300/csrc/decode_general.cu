@@ -18,7 +18,7 @@ constexpr int kWarps = 4, kThreads = 32 * kWarps;
 //
 // 16 sequences of up to 8192 rows, 32/8 heads x 100 channels bf16: 372 us (0.5 TB/s); the tensor cores'
 // kernel needs 43 us for 96 channels, this one 378.  7 sequences of up to 2000 rows, 6/6 x 80 f32: 21 us, that one 18.
-template <typename T, int J> __global__ void __launch_bounds__(kThreads) general_kernel(const DecodeArgs a) {
+template <typename T, int J, typename A> __global__ void __launch_bounds__(kThreads) general_kernel(const A a) {
   __shared__ JoinShared<kWarps> join;
   extern __shared__ __align__(16) float o_shared[];
   const gar_kv_cache &c = a.c;
@@ -47,8 +47,10 @@ template <typename T, int J> __global__ void __launch_bounds__(kThreads) general
       const int n = n0 + (lane & (kRows - 1));
       int64_t at = -1, at_scale = 0;
       if (n >= lo && n < g.to) {
-        const int p = (int)a.page(n), r = n - p * c.page_size;
-        const int page = a.table[g.b * a.table_stride + p];
+        int in = n;
+        const int32_t *const table = table_of(a, g.b, in);
+        const int p = (int)a.page(in), r = in - p * c.page_size;
+        const int page = table[p];
         if ((unsigned)page < (uint64_t)c.pages) {
           at = page * c.page_stride + g.kv_head * c.head_stride + r * c.token_stride;
           at_scale = page * c.scale_page_stride + g.kv_head * c.scale_head_stride + r * c.scale_token_stride;
@@ -125,20 +127,18 @@ template <typename T, int J> __global__ void __launch_bounds__(kThreads) general
   }
 }
 
-template <typename T, int J> int launch_general(DecodeArgs a, int sms, gar_stream_t stream) {
+template <typename T, int J, typename A> int launch_general(A a, int sms, gar_stream_t stream) {
   const size_t shared = sizeof(float) * kWarps * kHeads * J * 32;
   a.item_heads = std::min(a.group, kHeads);
   a.item_groups = (a.group + kHeads - 1) / kHeads;
-  return launch("gar_decode_attention", general_kernel<T, J>, sms * (J <= 4 ? 4 : 2), kThreads, shared, stream, a);
+  return launch("gar_decode_attention", general_kernel<T, J, A>, sms * (J <= 4 ? 4 : 2), kThreads, shared, stream, a);
 }
 
-template <typename T> int by_dim(const DecodeArgs &a, int sms, gar_stream_t stream) {
+template <typename T, typename A> int by_dim(const A &a, int sms, gar_stream_t stream) {
   return a.c.dim <= 64 ? launch_general<T, 2>(a, sms, stream) : a.c.dim <= 128 ? launch_general<T, 4>(a, sms, stream) : launch_general<T, 8>(a, sms, stream);
 }
 
-}  // namespace
-
-int decode_general(const DecodeArgs &a, int sms, gar_stream_t stream) {
+template <typename A> int by_type(const A &a, int sms, gar_stream_t stream) {
   switch (a.c.dtype) {
     case GAR_F32: return by_dim<float>(a, sms, stream);
     case GAR_BF16: return by_dim<__nv_bfloat16>(a, sms, stream);
@@ -147,5 +147,10 @@ int decode_general(const DecodeArgs &a, int sms, gar_stream_t stream) {
     default: return by_dim<e4m3>(a, sms, stream);
   }
 }
+
+}  // namespace
+
+int decode_general(const DecodeArgs &a, int sms, gar_stream_t stream) { return by_type(a, sms, stream); }
+int decode_general(const ServingArgs &a, int sms, gar_stream_t stream) { return by_type(a, sms, stream); }
 
 }  // namespace gar

@@ -231,9 +231,9 @@ template <int LINE> __device__ __forceinline__ int place(int r, int c) {
   return r * LINE + (LINE == 128 ? c ^ (r & 7) : c ^ (r / 2 & 3)) * 16;
 }
 
-template <typename C, int DP, int NG, bool BOXES, bool Q32>
+template <typename C, int DP, int NG, bool BOXES, bool Q32, typename A>
 __global__ void __launch_bounds__(32 * MmaShape<C, DP, NG>::kWarps, 1)
-    mma_kernel(const DecodeArgs a, const __grid_constant__ CUtensorMap k_map, const __grid_constant__ CUtensorMap v_map) {
+    mma_kernel(const A a, const __grid_constant__ CUtensorMap k_map, const __grid_constant__ CUtensorMap v_map) {
   using S = MmaShape<C, DP, NG>;
   using T = typename operand<C>::type;
   constexpr int EL = S::EL, KC = S::KC, VB = S::VB, LINE = S::LINE, PARTS = S::PARTS, KT = S::KT, SUBS = KT / 16;
@@ -324,8 +324,9 @@ __global__ void __launch_bounds__(32 * MmaShape<C, DP, NG>::kWarps, 1)
       there = n >= get.lo && n < get.to;
     }
     if (there) {
+      const int32_t *const table = table_of(a, get.b, n);
       const int p = (int)a.page(n);
-      x.page = a.table[get.b * a.table_stride + p], x.row = n - p * c.page_size;
+      x.page = table[p], x.row = n - p * c.page_size;
       if ((unsigned)x.page >= (uint64_t)c.pages) {
         x.page = -1;
         if (c.status) atomicOr(c.status, GAR_KV_BAD_PAGE);
@@ -816,7 +817,7 @@ __global__ void __launch_bounds__(32 * MmaShape<C, DP, NG>::kWarps, 1)
 // rows; false where it has none.
 bool box_map(const gar_kv_cache &c, void *base, int rows, bool all_lines, CUtensorMap *map);
 
-template <typename C, int DP, int NG, bool Q32> int launch_mma(DecodeArgs a, int sms, gar_stream_t stream) {
+template <typename C, int DP, int NG, bool Q32, typename A> int launch_mma(A a, int sms, gar_stream_t stream) {
   using S = MmaShape<C, DP, NG>;
   a.item_heads = std::min(a.group, 8 * NG);
   a.item_groups = (a.group + 8 * NG - 1) / (8 * NG);
@@ -827,7 +828,7 @@ template <typename C, int DP, int NG, bool Q32> int launch_mma(DecodeArgs a, int
   a.solo = std::min(64, std::max(4, (int)(2 * (int64_t)a.batch * a.c.heads * a.item_groups / sms)));
   CUtensorMap maps[2];
   const auto run = [&](auto boxes) {
-    constexpr auto kernel = mma_kernel<C, DP, NG, decltype(boxes)::value, Q32>;
+    constexpr auto kernel = mma_kernel<C, DP, NG, decltype(boxes)::value, Q32, A>;
     static DeviceSet allowed;
     const int e = once_for_device(allowed, a.device, [&] {
       return (int)cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, S::kShared);
@@ -835,14 +836,14 @@ template <typename C, int DP, int NG, bool Q32> int launch_mma(DecodeArgs a, int
     if (e != 0) return cuda_fail((cudaError_t)e, "cudaFuncSetAttribute");
     return launch("gar_decode_attention", kernel, sms, 32 * S::kWarps, S::kShared, stream, a, maps[0], maps[1]);
   };
-  if constexpr (S::kBoxes)
+  if constexpr (S::kBoxes && std::is_same<A, DecodeArgs>::value)
     if (a.c.dim == DP && a.c.page_size % S::KT == 0 && box_map(a.c, a.c.k, S::KT, true, &maps[0]) &&
         box_map(a.c, a.c.v, S::KT, true, &maps[1]))
       return run(std::true_type{});
   return run(std::false_type{});
 }
 
-template <typename C, bool Q32> int decode_mma(const DecodeArgs &a, int sms, gar_stream_t stream) {
+template <typename C, bool Q32, typename A> int decode_mma(const A &a, int sms, gar_stream_t stream) {
   // Sixteen heads at a time where there are more than eight (a row is read once for all; 256 channels' outputs do not fit the
   // registers).  64 x 16384, 64/4 x 128: bf16 202 us and 321 with eight at a time, i8 179 and 217, f32 573 and 761; 64 x 2000 bf16
   // 54 and 57, 8 x 60000, 16/1 x 128 39 and 38.  The slower of the two for one long sequence, 1 x 60000 36 and 22, 1 x 262143 55 and 42:

@@ -1,0 +1,8 @@
+// Attention of batches that share rows, on tensor cores: a cache of this type.
+#include <algorithm>
+
+#include "decode_mma.cuh"
+
+namespace gar {
+int decode_mma_f16(const ServingArgs &a, int sms, gar_stream_t stream) { return decode_mma<__half, false>(a, sms, stream); }
+}  // namespace gar

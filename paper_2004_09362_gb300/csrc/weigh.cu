@@ -22,7 +22,7 @@ constexpr int kThreads = 256, kWarps = kThreads / 32;
 constexpr int kHeads = 32;  // queries whose parts lie in shared memory at a time
 
 struct WeighArgs {
-  DecodeArgs d;
+  ServingArgs d;
   const float *lse, *weights;
   float *out;
   int64_t wb, wh, ob, oh, rows;
@@ -74,7 +74,7 @@ struct Course {
   Walk walk;
   Segment segment;
   int more;
-  __device__ __forceinline__ void start(const DecodeArgs &d) {
+  __device__ __forceinline__ void start(const ServingArgs &d) {
     if (threadIdx.x < 32) {
       Walk w;
       w.start(d);
@@ -82,7 +82,7 @@ struct Course {
     }
   }
   // By all threads; the segment stays until the next call.
-  __device__ __forceinline__ bool next(const DecodeArgs &d) {
+  __device__ __forceinline__ bool next(const ServingArgs &d) {
     sync_weighing();
     if (threadIdx.x == 0) {
       Walk w = walk;
@@ -132,7 +132,7 @@ template <typename C, int KC, bool Q32> __global__ void __launch_bounds__(kThrea
   constexpr int STEP = 16 * kWarps;
   __shared__ float2 factor[kHeads];
   __shared__ float down[kHeads];
-  const DecodeArgs &d = a.d;
+  const ServingArgs &d = a.d;
   const gar_kv_cache &c = d.c;
   const int warp = threadIdx.x / 32, lane = threadIdx.x & 31, g = lane / 4, t = lane & 3;
   // The queries' parts are behind the warps' rings.
@@ -303,7 +303,7 @@ template <typename C, int KC, bool Q32> __global__ void __launch_bounds__(kThrea
 template <typename C, int V> __global__ void __launch_bounds__(kThreads + 32) weigh_plain(const WeighArgs a) {
   extern __shared__ float query[];  // [heads][dim]
   __shared__ float2 factor[kHeads];
-  const DecodeArgs &d = a.d;
+  const ServingArgs &d = a.d;
   const gar_kv_cache &c = d.c;
   constexpr bool Q8 = quantised<C>::value;
   constexpr int MOST = GAR_MAX_HEAD_DIM / 32 / V;  // groups of channels of a lane
@@ -454,7 +454,7 @@ extern "C" int gar_kv_weigh(const gar_kv_cache *cache, const void *q, int64_t q_
   if (e == cudaSuccess) e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);
   if (e != cudaSuccess) return cuda_fail(e, "gar_kv_weigh");
   WeighArgs a{};
-  DecodeArgs &d = a.d;
+  ServingArgs &d = a.d;
   d.c = *cache, d.q = q, d.qb = q_batch_stride, d.qh = q_head_stride, d.q_dtype = q_dtype;
   d.table = page_table, d.table_stride = table_stride, d.lengths = lengths;
   d.page = divide_by((uint32_t)cache->page_size), d.items = divide_by((uint32_t)cache->heads);

@@ -96,13 +96,16 @@ def test_verify_refusals(bad, code):
 
 # ---------------------------------------------------------------------------- attention over shared prefixes
 
-def _prefix_case(prefixes, own, share, q_heads, kv_heads, dim, page_size, kind, dtype, seed=0, order="head", sharp=1.0, every=1):
+def _prefix_case(prefixes, own, share, q_heads, kv_heads, dim, page_size, kind, dtype, seed=0, order="head", sharp=1.0, every=1, wide=True):
     """(cache, prefix table and lengths, table and lengths, q, each sequence's keys and values in 64 bits)."""
     cache, table, lens, _, kvs = _attn_case(prefixes + own, q_heads, kv_heads, dim, page_size, kind, dtype, seed, order)
     groups = len(prefixes)
     q = _randn((len(own), q_heads, dim), dtype, seed + 7) * sharp
+    # (a table wide enough for so many rows that they are not read for each sequence)
+    pad = torch.full((groups, (1 << 22) // page_size if wide else 0), -1, dtype=torch.int32, device="cuda")
+    table = torch.cat([table[:groups], pad], 1), table[groups:]
     both = [tuple(torch.cat([kvs[b // share][i], kvs[groups + b][i]]) for i in (0, 1)) for b in range(0, len(own), every)]
-    return cache, table[:groups], lens[:groups], table[groups:], lens[groups:], q, both
+    return cache, table[0], lens[:groups], table[1], lens[groups:], q, both
 
 
 def _check_prefix(out, lse, q, both, scale, out_type):
@@ -138,12 +141,13 @@ OWN = [0, 1, 5, 16, 17, 33, 3, 0, 64, 65, 2, 130]
     (8, 2, 128, 16), (1, 1, 64, 1), (6, 6, 80, 5), (10, 2, 96, 24), (16, 1, 256, 32), (9, 1, 64, 48), (40, 2, 72, 7), (3, 3, 33, 4),
     (2, 1, 1, 3), (24, 8, 200, 48), (32, 4, 128, 64)])
 @pytest.mark.parametrize("share", [1, 3, 12])
-def test_prefix_attention(kind, dtype, q_heads, kv_heads, dim, page_size, share):
+@pytest.mark.parametrize("wide", [False, True])
+def test_prefix_attention(kind, dtype, q_heads, kv_heads, dim, page_size, share, wide):
     prefixes = [129, 0, 1, 300, 64, 127, 128, 2, 31, 33, 500, 16][:12 // share]
     if share == 12:
         prefixes = [777]
     order = "token" if page_size % 2 else "head"
-    cache, pt, pn, t, n, q, both = _prefix_case(prefixes, OWN, share, q_heads, kv_heads, dim, page_size, kind, dtype, order=order)
+    cache, pt, pn, t, n, q, both = _prefix_case(prefixes, OWN, share, q_heads, kv_heads, dim, page_size, kind, dtype, order=order, wide=wide)
     plan = gar.gar_attn_plan_create(q_heads, kv_heads, dim)
     out, lse = gar.gar_prefix_attention(plan, q, cache, pt, pn, t, n, lse=True)
     assert out.dtype == q.dtype
@@ -193,8 +197,9 @@ def test_prefix_attention_many_tiles_each(kind, dim, page_size, share, prefix):
 
 @pytest.mark.gpu
 @pytest.mark.parametrize("scale", [0.0, -0.1])
-def test_prefix_attention_scales(scale):
-    cache, pt, pn, t, n, q, both = _prefix_case([300], [b % 9 for b in range(40)], 40, 4, 2, 64, 16, "bf16", "bf16")
+@pytest.mark.parametrize("wide", [False, True])
+def test_prefix_attention_scales(scale, wide):
+    cache, pt, pn, t, n, q, both = _prefix_case([300], [b % 9 for b in range(40)], 40, 4, 2, 64, 16, "bf16", "bf16", wide=wide)
     plan = gar.gar_attn_plan_create(4, 2, 64)
     out, lse = gar.gar_prefix_attention(plan, q, cache, pt, pn, t, n, scale=scale, lse=True)
     _check_prefix(out, lse, q, both, scale, "bf16")
@@ -214,27 +219,29 @@ def test_prefix_attention_several_prefixes_of_many_queries(kind, dtype):
 
 @pytest.mark.gpu
 @pytest.mark.parametrize("kind,dtype,dim,share", [("bf16", "bf16", 128, 2), ("bf16", "bf16", 128, 64), ("f16", "f16", 64, 64), ("f32", "f32", 64, 64)])
-def test_prefix_attention_drafts_are_one_long_sequence(kind, dtype, dim, share):
+@pytest.mark.parametrize("wide", [False, True])
+def test_prefix_attention_drafts_are_one_long_sequence(kind, dtype, dim, share, wide):
     """Drafts over a context, their rows in pages of one table: each sees those before it."""
     cache, table, lens, _, kvs = _attn_case([1000, share], 8, 2, dim, 16, kind, dtype)
     q = _randn((share, 8, dim), dtype, 3)
     n = torch.arange(1, share + 1, dtype=torch.int32, device="cuda")
     plan = gar.gar_attn_plan_create(8, 2, dim)
-    out, lse = gar.gar_prefix_attention(plan, q, cache, table[:1], lens[:1], table[1:].expand(share, -1), n, lse=True)
+    prefix = torch.cat([table[:1], torch.full((1, 1 << 18 if wide else 1), -1, dtype=torch.int32, device="cuda")], 1)
+    out, lse = gar.gar_prefix_attention(plan, q, cache, prefix, lens[:1], table[1:].expand(share, -1), n, lse=True)
     both = [tuple(torch.cat([kvs[0][i], kvs[1][i][:b + 1]]) for i in (0, 1)) for b in range(share)]
     _check_prefix(out, lse, q, both, dim ** -0.5, dtype)
 
 
 @pytest.mark.gpu
-@pytest.mark.parametrize("share", [2, 64])
-def test_prefix_attention_bad_pages_and_lengths(share):
+@pytest.mark.parametrize("share,wide", [(2, False), (2, True), (64, False), (64, True)])
+def test_prefix_attention_bad_pages_and_lengths(share, wide):
     """A page that is none counts as rows of zeros, a length past the table as the longest."""
     dim, ps = 64, 16
     cache, table, lens, _, kvs = _attn_case([40] + [3] * share, 4, 2, dim, ps, "bf16", "bf16")
     q = _randn((share, 4, dim), "bf16", 3)
     plan = gar.gar_attn_plan_create(4, 2, dim)
     for bad in (-1, cache.pages, 2 ** 31 - 1):
-        broken = table.clone()
+        broken = torch.cat([table[:1], torch.full((1, 1 << 18 if wide else 1), -1, dtype=torch.int32, device="cuda")], 1)
         broken[0, 1] = bad
         out, lse = gar.gar_prefix_attention(plan, q, cache, broken[:1], lens[:1], table[1:], lens[1:], lse=True)
         both = []
@@ -253,6 +260,8 @@ def test_prefix_attention_bad_pages_and_lengths(share):
         n[0] = bad
         narrow = table[:1, :3].clone()
         narrow[0, 2] = narrow[0, 1]
+        if wide and bad < 0:
+            narrow = torch.cat([narrow, torch.full((1, 1 << 18), -1, dtype=torch.int32, device="cuda")], 1)
         out, lse = gar.gar_prefix_attention(plan, q, cache, narrow, n, table[1:], lens[1:], lse=True)
         with pytest.raises(gar.GarError) as e:
             gar.gar_kv_status(cache)
