@@ -132,7 +132,7 @@ template <typename T, int DP, bool PAIR> __global__ void __launch_bounds__(kThre
   constexpr int N = S::kStages, RING = PAIR ? N : N / 2, ROW = DP * 2, CHUNKS = ROW / 16;
   constexpr bool BF16 = std::is_same<T, __nv_bfloat16>::value;
   extern __shared__ char shared_from[];
-  __shared__ __align__(8) uint64_t full[N], empty[N], scores[2], weights[2][2], values[2], drained[2];
+  __shared__ __align__(8) uint64_t full[N], empty[N], scores[2][2], weights[2][2], values[2], drained[2];
   __shared__ uint32_t tensor_at;
   __shared__ int late_flag, copied[2];
   const uint32_t shared = (uint32_t)__cvta_generic_to_shared(shared_from) + 1023 & ~1023u;
@@ -146,7 +146,7 @@ template <typename T, int DP, bool PAIR> __global__ void __launch_bounds__(kThre
     late_flag = 0;
     for (int i = 0; i < N; ++i) init_barrier(at(full[i]), a.box > 0 ? 4 : 128), init_barrier(at(empty[i]), PAIR ? 2 : 1);
     for (int s = 0; s < 2; ++s) {
-      init_barrier(at(scores[s]), 1), init_barrier(at(values[s]), 1);
+      init_barrier(at(scores[s][0]), 1), init_barrier(at(scores[s][1]), 1), init_barrier(at(values[s]), 1);
       init_barrier(at(weights[s][0]), 4), init_barrier(at(weights[s][1]), 4);
       init_barrier(at(drained[s]), 1);
     }
@@ -185,58 +185,61 @@ template <typename T, int DP, bool PAIR> __global__ void __launch_bounds__(kThre
     // Issues the products of one stream.
     const int s = warp - kIssue;
     const uint32_t s_at = tensor + 256 * s, o_at = s_at + 128;
-    constexpr uint32_t scores_kind = product_of(BF16, kKeys, false), values_kind = product_of(BF16, DP, true);
+    constexpr uint32_t scores_kind = product_of(BF16, kKeys / 2, false), values_kind = product_of(BF16, DP, true);
     const uint32_t q_at = shared + (PAIR ? s * S::kTile : 0);
     const int stage0 = PAIR ? 0 : s * RING;
-    int done = 0, pos = 0;  // pos: the stream's next tile of keys or values
+    // done: halves of tiles whose values are added; pos: the stream's first tile of keys or values that is not done with.
+    int done = 0, pos = 0;
     bool good = true;
     while (next_part()) {
       asm volatile("bar.sync 2, 320;" ::: "memory");  // (the queries are there)
       if (lane == 0) {
         constexpr int STEP = PAIR ? 1 : 2;
-        const auto scores_of = [&](int j) {
-          const int k = stage0 + pos % RING;
-          if (j >= a.give_up || !wait_phase(at(full[k]), pos / RING & 1, late)) return false;
-          shared_for_mma();
-          tensor_after_sync();
-          const uint32_t k_at = ring + k * S::kTile;
-#pragma unroll
-          for (int i = 0; i < DP / 16; ++i) {
-            const uint32_t off = i / 4 * (kKeys * 128) + i % 4 * 32;
-            product(s_at, operand_k_major(q_at + off), operand_k_major(k_at + off), scores_kind, i > 0);
+        const int first = PAIR ? 0 : s, halves = part.tiles > first ? 2 * ((part.tiles - first + STEP - 1) / STEP) : 0;
+        // The scores of the part's i-th half of a tile: keys of tile i / 2, of which every second in the ring is one.
+        const auto scores_of = [&](int i) {
+          const int at_pos = pos + i / 2 * 2, k = stage0 + at_pos % RING;
+          if (i % 2 == 0) {
+            if (first + i / 2 * STEP >= a.give_up || !wait_phase(at(full[k]), at_pos / RING & 1, late)) return false;
+            shared_for_mma();
           }
-          commit(at(scores[s]));
-          commit(at(empty[k]));
-          ++pos;
+          tensor_after_sync();
+          const uint32_t k_at = ring + k * S::kTile + i % 2 * (kKeys / 2 * 128);
+#pragma unroll
+          for (int x = 0; x < DP / 16; ++x) {
+            const uint32_t off = x / 4 * (kKeys * 128) + x % 4 * 32;
+            product(s_at + i % 2 * (kKeys / 2), operand_k_major(q_at + off), operand_k_major(k_at + off), scores_kind, x > 0);
+          }
+          commit(at(scores[s][i % 2]));
+          if (i % 2) commit(at(empty[k]));
           return true;
         };
-        const int first = PAIR ? 0 : s;
-        if (good && first < part.tiles) good = scores_of(first);
-        for (int j = first; good && j < part.tiles; j += STEP) {
-          const int v = stage0 + pos % RING;
+        if (good && halves > 0) good = scores_of(0) && scores_of(1);
+        for (int i = 0; good && i < halves; ++i) {
+          const int at_pos = pos + i / 2 * 2 + 1, v = stage0 + at_pos % RING;
           const uint32_t v_at = ring + v * S::kTile;
-          good = wait_phase(at(full[v]), pos / RING & 1, late);
-          shared_for_mma();
-#pragma unroll
-          for (int half = 0; half < 2; ++half) {
-            good = good && wait_phase(at(weights[s][half]), done & 1, late);
-            if (!good) break;
-            tensor_after_sync();
-#pragma unroll
-            for (int i = half * (kKeys / 32); i < (half + 1) * (kKeys / 32); ++i) {
-              const uint32_t p_at = s_at + i / 2 * 32 + i % 2 * 8;
-              const uint64_t b = operand_mn_major(v_at + i * 2048, kKeys * 128);
-              product_tensor(o_at, p_at, b, values_kind, j > first || i > 0);
-              product_tensor(o_at, p_at + 16, b, values_kind, true);
-            }
+          if (i % 2 == 0) {
+            good = wait_phase(at(full[v]), at_pos / RING & 1, late);
+            shared_for_mma();
           }
+          good = good && wait_phase(at(weights[s][i % 2]), done / 2 & 1, late);
           if (!good) break;
+          tensor_after_sync();
+#pragma unroll
+          for (int x = 0; x < kKeys / 32; ++x) {
+            const int y = i % 2 * (kKeys / 32) + x;
+            const uint32_t p_at = s_at + y / 2 * 32 + y % 2 * 8;
+            const uint64_t b = operand_mn_major(v_at + y * 2048, kKeys * 128);
+            product_tensor(o_at, p_at, b, values_kind, i > 0 || x > 0);
+            product_tensor(o_at, p_at + 16, b, values_kind, true);
+          }
           commit(at(values[s]));
-          commit(at(empty[v]));
-          ++pos, ++done;
-          // The next scores go where these weights are: a thread's products run in the order that they are issued in.
-          if (j + STEP < part.tiles) good = scores_of(j + STEP);
+          if (i % 2) commit(at(empty[v]));
+          ++done;
+          // The next scores but one go where these weights are: a thread's products run in the order that they are issued in.
+          if (i + 2 < halves) good = scores_of(i + 2);
         }
+        pos += halves;
         if (!good) *late = 1;
       }
       __syncwarp();
@@ -380,43 +383,51 @@ template <typename T, int DP, bool PAIR> __global__ void __launch_bounds__(kThre
 
       const bool idle = (PAIR ? s * 128 : 0) + quarter * 32 >= many;  // no query in this warp
       float m = -INFINITY, l = 0.f;
-      bool first = true;
-      for (int j = PAIR ? 0 : s; good && j < part.tiles; j += PAIR ? 1 : 2) {
-        good = __all_sync(~0u, wait_phase(at(scores[s]), done & 1, late));
+      const int first_tile = PAIR ? 0 : s, step = PAIR ? 1 : 2;
+      const int halves = part.tiles > first_tile ? 2 * ((part.tiles - first_tile + step - 1) / step) : 0;
+#pragma unroll 1
+      for (int i = 0; good && i < halves; ++i) {
+        const uint32_t half_at = s_at + i % 2 * (kKeys / 2);
+        good = __all_sync(~0u, wait_phase(at(scores[s][i % 2]), done / 2 & 1, late));
         if (!good) break;
-        ++done;
         tensor_after_sync();
         if (!idle) {
-          const int n = part.rows - (part.from + j) * kKeys;  // rows of the tile that exist: n or all
-          uint32_t x[4][32];
-#pragma unroll
-          for (int c = 0; c < 4; ++c) tensor_load32(x[c], s_at + 32 * c);
+          const int n = part.rows - (part.from + first_tile + i / 2 * step) * kKeys - i % 2 * (kKeys / 2);  // rows that exist: n or all
+          uint32_t x[2][32];
+          tensor_load32(x[0], half_at);
+          tensor_load32(x[1], half_at + 32);
           wait_tensor_loads(x[0]);
+          loaded(x[1]);
+          if (n < kKeys / 2) {
 #pragma unroll
-          for (int c = 1; c < 4; ++c) loaded(x[c]);
-          if (n < kKeys) {
-#pragma unroll
-            for (int i = 0; i < kKeys; ++i)
-              if (i >= n) x[i / 32][i % 32] = 0xff800000u;  // -infinity: its weight is 0
+            for (int k = 0; k < kKeys / 2; ++k)
+              if (k >= n) x[k / 32][k % 32] = 0xff800000u;  // -infinity: its weight is 0
           }
           float tops[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
-          for (int i = 0; i < 32; i += 2)
+          for (int k = 0; k < 32; k += 4)
 #pragma unroll
-            for (int c = 0; c < 4; ++c) tops[c] = max3(tops[c], __uint_as_float(x[c][i]), __uint_as_float(x[c][i + 1]));
+            for (int c = 0; c < 4; ++c) {
+              const uint32_t *const y = &x[c / 2][k + c % 2 * 2];
+              tops[c] = max3(tops[c], __uint_as_float(y[0]), __uint_as_float(y[1]));
+            }
           const float top = fmaxf(max3(tops[0], tops[1], tops[2]), tops[3]) * a.scale_log2;
           const bool grown = top > m + Parts<T>::kLazy;
           if (__any_sync(~0u, grown)) {
             const float shrink = grown ? exp2_fast(m - top) : 1.f;  // (0 at first)
             if (grown) m = top;
             l *= shrink;
-            if (!first) {
+            if (i > 0) {
+              // (the values before these have been added; those before them had been when the scores were there)
+              good = __all_sync(~0u, wait_phase(at(values[s]), (done - 1) & 1, late));
+              if (!good) break;
+              tensor_after_sync();
 #pragma unroll 1
               for (int c = 0; c < DP; c += 8) {
                 uint32_t y[8];
                 tensor_load8(y, o_at + c);
 #pragma unroll
-                for (int i = 0; i < 8; ++i) y[i] = __float_as_uint(__uint_as_float(y[i]) * shrink);
+                for (int k = 0; k < 8; ++k) y[k] = __float_as_uint(__uint_as_float(y[k]) * shrink);
                 tensor_store8(o_at + c, y);
               }
             }
@@ -425,40 +436,34 @@ template <typename T, int DP, bool PAIR> __global__ void __launch_bounds__(kThre
           const float2 scale2 = make_float2(a.scale_log2, a.scale_log2), off2 = make_float2(off, off);
           float2 sum[2] = {};
 #pragma unroll
-          for (int c = 0; c < 4; ++c) {
+          for (int c = 0; c < 2; ++c) {
             uint32_t y[32];
 #pragma unroll
-            for (int i = 0; i < 32; i += 2) {
-              float2 p = fma2(make_float2(__uint_as_float(x[c][i]), __uint_as_float(x[c][i + 1])), scale2, off2);
+            for (int k = 0; k < 32; k += 2) {
+              float2 p = fma2(make_float2(__uint_as_float(x[c][k]), __uint_as_float(x[c][k + 1])), scale2, off2);
               p.x = exp2_fast(p.x), p.y = exp2_fast(p.y);
-              sum[i / 2 % 2] = add2(sum[i / 2 % 2], p);
-              split_weights(p, &y[i / 2], &y[16 + i / 2], T());
+              sum[k / 2 % 2] = add2(sum[k / 2 % 2], p);
+              split_weights(p, &y[k / 2], &y[16 + k / 2], T());
             }
-            tensor_store32(s_at + 32 * c, y);
-            if (c == 1) {  // half of the products can begin
-              wait_tensor_stores();
-              tensor_before_sync();
-              __syncwarp();
-              if (lane == 0) arrive(at(weights[s][0]));
-              __syncwarp();
-            }
+            tensor_store32(half_at + 32 * c, y);
           }
           l += (sum[0].x + sum[1].x) + (sum[0].y + sum[1].y);
           wait_tensor_stores();
         }
-        if (idle && lane == 0) arrive(at(weights[s][0]));
-        first = false;
+        ++done;
         tensor_before_sync();
         __syncwarp();
-        if (lane == 0) arrive(at(weights[s][1]));
+        if (lane == 0) arrive(at(weights[s][i % 2]));
         __syncwarp();
       }
+      const bool first = halves == 0;
       if (!good) continue;
       // This part's result, in units of one.
       constexpr float unit = Parts<T>::kUnit == 0.f ? 1.f : 1.f / 1024.f;
       const int64_t place = ((int64_t)blockIdx.x + part.item) * 2 + s;
       if (!first) {
-        good = __all_sync(~0u, wait_phase(at(values[s]), (done - 1) & 1, late));
+        // (a barrier tells a phase from the next only: the last but one first)
+        good = __all_sync(~0u, wait_phase(at(values[s]), (done - 2) & 1, late) && wait_phase(at(values[s]), (done - 1) & 1, late));
         if (!good) continue;
         tensor_after_sync();
       }
