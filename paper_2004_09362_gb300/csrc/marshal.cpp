@@ -573,6 +573,7 @@ PyObject *prefix_attention(PyObject *, PyObject *const *args, Py_ssize_t n, PyOb
     const Tensor &table = pages_of(a.at[5], q.size(0), "page_table"), &prefix = pages_of(a.at[3], -1, "prefix_table");
     const Tensor &prefix_lengths = integers(a.at[4], prefix.size(0), true, false, "prefix_lengths");
     const int batch = narrow(q.size(0), "the batch"), groups = narrow(prefix.size(0), "the number of prefixes");
+    if (batch > 0 && (groups == 0 || batch % groups)) bad("the batch must be a multiple of the prefixes");
     int shape[3];
     check(gar_attn_plan_shape(plan, &shape[0], &shape[1], &shape[2]), "gar_attn_plan_shape");
     if (q.size(1) != shape[0] || q.size(2) != shape[2])

@@ -119,10 +119,10 @@ template <typename T> struct Group<T, true> {
   uint32_t w[kGroup * sizeof(T) / 4];
   __device__ __forceinline__ void load(const T *p, bool there) {
     if constexpr (sizeof(T) == 4) {
-      const uint4 x = there ? __ldg(reinterpret_cast<const uint4 *>(p)) : make_uint4(0, 0, 0, 0);
+      const uint4 x = there ? *reinterpret_cast<const uint4 *>(p) : make_uint4(0, 0, 0, 0);
       w[0] = x.x, w[1] = x.y, w[2] = x.z, w[3] = x.w;
     } else {
-      const uint2 x = there ? __ldg(reinterpret_cast<const uint2 *>(p)) : make_uint2(0, 0);
+      const uint2 x = there ? *reinterpret_cast<const uint2 *>(p) : make_uint2(0, 0);
       w[0] = x.x, w[1] = x.y;
     }
   }

@@ -342,7 +342,7 @@ template <typename C, int V> __global__ void __launch_bounds__(kThreads + 32) we
             const int channel = (lane + 32 * m) * V;
             const bool there = at >= 0 && channel < c.dim;
             if constexpr (V == 4) {
-              const float4 x = there ? __ldg(reinterpret_cast<const float4 *>(k + channel)) : make_float4(0.f, 0.f, 0.f, 0.f);
+              const float4 x = there ? *reinterpret_cast<const float4 *>(k + channel) : make_float4(0.f, 0.f, 0.f, 0.f);
               key[r][m][0] = x.x, key[r][m][1] = x.y, key[r][m][2] = x.z, key[r][m][3] = x.w;
             } else {
               key[r][m][0] = there ? to_f32(k[channel]) : 0.f;
