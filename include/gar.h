@@ -488,7 +488,8 @@ GAR_API int gar_attn_plan_bytes(const gar_attn_plan *plan, size_t *workspace_byt
  * each stream. */
 GAR_API int gar_attn_plan_set_workspace(gar_attn_plan *plan, void *dev_ptr, size_t bytes);
 
-/* The waits for copies of gar_decode_attention (rows of 512 bytes and more; no counterpart in the paper): each is
+/* The waits for copies of gar_decode_attention (rows of 512 bytes and more) and gar_prefix_attention (a prefix of many queries; no
+ * counterpart in the paper of either): each is
  * bounded, some 0.1 s; one that runs out sets GAR_KV_TIMEOUT, and its warp leaves out the rest of its rows.  tile >= 0: waits
  * for a segment's tiles from that one on report that they ran out, which tests that path; negative: none do. */
 GAR_API int gar_attn_plan_debug_wait(gar_attn_plan *plan, int tile);
@@ -535,8 +536,10 @@ GAR_API int gar_prefix_attention_bytes(const gar_attn_plan *plan, int batch, int
  *   out = sum_n softmax_n(scale q.k_n) v_n,   lse = ln sum_n exp(scale q.k_n)
  * over both.  batch is a multiple of groups.  Drafted tokens are such sequences: the tokens of one context are a group,
  * their own rows the pages that they were written to, each length one more than the one before.
- * Pages, lengths, strides, dtypes, precision and what the status word says are as in gar_decode_attention;
- * prefix_lengths count in [0, prefix_width * page_size].
+ * Pages, lengths, strides, dtypes and what the status word says are as in gar_decode_attention;
+ * prefix_lengths count in [0, prefix_width * page_size].  So is precision, but where many queries share a prefix of 16 bits:
+ * weights over it are two parts that keep 2^-16 of the weight (bf16) or 2^-22 of it or 2^-34 of the largest, whichever is more (f16),
+ * and the tensor cores' sums of 16 tiles of 128 rows are off by 2^-15 at most.
  * workspace: 16-byte aligned, at least gar_prefix_attention_bytes, one for each call that may run at the same time
  * (what it held before does not matter).  The plan's own workspace is used too. */
 GAR_API int gar_prefix_attention(gar_attn_plan *plan, const gar_kv_cache *cache, const void *q, int64_t q_batch_stride,
@@ -567,7 +570,7 @@ GAR_API int gar_kv_weigh(const gar_kv_cache *cache, const void *q, int64_t q_bat
  * others by their weight, the largest first (a NaN counts as less than any number); of equal ones the lower row.  Rows
  * stay where they are as far as that goes: the i-th of the rows below `keep` that go is overwritten, keys, values
  * and scales, by the i-th of the rows from `keep` on that stay.  A row below `first` is never written, so a prefix
- * shared by sequences may lie there; no other page may be in two sequences' tables.
+ * shared by sequences may lie there; no other page may stand twice in the tables.
  * weights, positions: [batch][heads][rows], contiguous; out_weights and out_positions the same shape: entries of rows that
  * moved go with them, and rows past what is left hold 0 and -1, as new tokens find them.  out_lengths[b] =
  * min(lengths[b], keep).  The outputs overlap no input.  lengths count in [0, min(rows, table_width * page_size)]; what

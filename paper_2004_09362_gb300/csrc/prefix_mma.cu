@@ -1,18 +1,30 @@
 // Attention of many queries over a shared prefix, on the tensor cores' own memory.
 //
 // S = Q K^T of 128 queries (of all the sequences and query heads that read a cached head) by 128 cached rows, then
-// P = 2^(S - m) and O += P V: with fewer than some 300 queries for a cached row the rows' way from memory is what it takes, with more
-// the products.  A CTA keeps two streams of such tiles going, so that one's products run while the other's weights are computed: two
-// blocks of queries over the same rows (pair), or the even and the odd tiles of rows for one block.
+// P = 2^(S - m) and O += P V.  A CTA keeps two streams of such tiles going, so that one's products run while the other's weights are
+// computed: two blocks of queries over the same rows (pair), or the even and the odd tiles of rows for one block.
 //
-//  * 4 warps copy the rows, by cp.async since pages may be of any size, to a ring of tiles in shared memory.
-//  * A thread for each stream issues its products.  S and O are in tensor memory, 128 columns each.
+//  * 4 warps copy the rows to a ring of tiles in shared memory: boxes of pages by tensor copies where tiles are whole pages or pages
+//    whole tiles, cp.async for pages of any other size and for last tiles, whose rows past the end have to be zeros.
+//    (131072 rows, one block: 117 us with boxes of 64 rows, 131 with cp.async.  A lane's tensor copy takes some 190 clocks to issue.)
+//  * A thread for each stream issues its products.  S and O are in tensor memory, 128 columns each.  S is computed by halves of 64 rows, the
+//    next half's while the weights of one are computed (16384 rows x 1000 queries: 103 us, whole tiles 111).
 //  * 4 warps for each stream turn S to P, a query to a thread: no exchange between lanes.  P goes where S was, as two 16-bit parts
-//    (its sum is 17 bits or more), 16 columns each for 32 rows.
+//    (2^-16 of the weight; one part alone would be 2^-9, as much as the output's rounding, and took 98 us for 111), 16 columns each for
+//    32 rows.  These warps have 192 registers, the others 64: a half's scores fit them.
+//  * The tensor cores cut their sums off rather than round them: 2^-24 and more of the sum for each of 16 products a tile, all one way (parts
+//    of 1024 tiles came out 1.6e-3 short, of 54 tiles 3e-5).  So O holds 16 tiles at most, and is then added to the part's result in
+//    memory, rounded: 1.6e-5 is missing at most.  (8 tiles, by reductions in the L2: 0.8e-5, and 40 us more of 150.)
 //  * m is not the running maximum but a number within kLazy of it: O is rescaled only where the maximum passes m + kLazy.
 //
 // The tiles of all items are shared out among the CTAs as one line.  Each CTA leaves (m, l, O) for its part of
 // an item; the parts are joined in their order by the kernel after this.
+//
+// Bound, with few queries, by the rows' way from memory: 32 sequences of 32/8 heads x 128 bf16 over 131072 rows 115 us, 4.7 TB/s.  With many, 250
+// sequences over 16384 rows f16, 103 us: 0.66 PFLOP/s of S and P V, 0.99 counting both parts of P.  There a pair of tiles takes
+// 6200 clocks, of which its products take 4700 alone (3100 at the peak rate) and its weights 4400; leaving the exponentials, the
+// parts or the stores out changed little, so what remains is that products and weights hardly overlap.  The first 12 us of a
+// launch are the pages, the queries and the first copies, one after the other, and the instructions.
 #include <algorithm>
 #include <climits>
 
@@ -25,6 +37,7 @@ namespace {
 
 constexpr int kThreads = 32 * 16;  // at 128 registers; the weights' 8 warps take 64 of them from each thread of the others
 enum { kWeights = 0, kCopies = 8, kIssue = 12 };  // first warps of a part of the work
+constexpr int kSpan = 32;           // halves of tiles that the tensor cores add up
 constexpr int kCopyRows = 32;      // of a tile, copied by one warp
 
 template <typename T> struct Parts;
@@ -230,7 +243,7 @@ template <typename T, int DP, bool PAIR> __global__ void __launch_bounds__(kThre
             const int y = i % 2 * (kKeys / 32) + x;
             const uint32_t p_at = s_at + y / 2 * 32 + y % 2 * 8;
             const uint64_t b = operand_mn_major(v_at + y * 2048, kKeys * 128);
-            product_tensor(o_at, p_at, b, values_kind, i > 0 || x > 0);
+            product_tensor(o_at, p_at, b, values_kind, i % kSpan > 0 || x > 0);
             product_tensor(o_at, p_at + 16, b, values_kind, true);
           }
           commit(at(values[s]));
@@ -383,6 +396,30 @@ template <typename T, int DP, bool PAIR> __global__ void __launch_bounds__(kThre
 
       const bool idle = (PAIR ? s * 128 : 0) + quarter * 32 >= many;  // no query in this warp
       float m = -INFINITY, l = 0.f;
+      // The part's result, in units of one: what O holds comes to what it held before, which was relative to m_before.
+      constexpr float unit = Parts<T>::kUnit == 0.f ? 1.f : 1.f / 1024.f;
+      const int64_t place = ((int64_t)blockIdx.x + part.item) * 2 + s;
+      float4 *const result = reinterpret_cast<float4 *>(a.o) + place * (DP / 4 * 128) + row;
+      float m_before = -INFINITY;
+      bool fresh = true;
+      const auto add_up = [&] {
+        const float f = fresh ? 0.f : exp2_fast(m_before - offset_of(m));
+#pragma unroll 1
+        for (int c = 0; c < DP; c += 32) {
+          float4 *const to = result + c / 4 * 128;
+          float4 z[8];
+#pragma unroll
+          for (int i = 0; i < 8; ++i) z[i] = fresh ? make_float4(0.f, 0.f, 0.f, 0.f) : __ldcg(to + i * 128);
+          uint32_t x[32];
+          tensor_load32(x, o_at + c);
+          wait_tensor_loads(x);
+#pragma unroll
+          for (int i = 0; i < 8; ++i)
+            __stcg(to + i * 128, make_float4(fmaf(z[i].x, f, __uint_as_float(x[4 * i]) * unit), fmaf(z[i].y, f, __uint_as_float(x[4 * i + 1]) * unit),
+                                             fmaf(z[i].z, f, __uint_as_float(x[4 * i + 2]) * unit), fmaf(z[i].w, f, __uint_as_float(x[4 * i + 3]) * unit)));
+        }
+        fresh = false, m_before = m;
+      };
       const int first_tile = PAIR ? 0 : s, step = PAIR ? 1 : 2;
       const int halves = part.tiles > first_tile ? 2 * ((part.tiles - first_tile + step - 1) / step) : 0;
 #pragma unroll 1
@@ -391,6 +428,13 @@ template <typename T, int DP, bool PAIR> __global__ void __launch_bounds__(kThre
         good = __all_sync(~0u, wait_phase(at(scores[s][i % 2]), done / 2 & 1, late));
         if (!good) break;
         tensor_after_sync();
+        if (!idle && i > 0 && i % kSpan == 0) {
+          // (the values before these have been added; those before them had been when the scores were there)
+          good = __all_sync(~0u, wait_phase(at(values[s]), (done - 1) & 1, late));
+          if (!good) break;
+          tensor_after_sync();
+          add_up();
+        }
         if (!idle) {
           const int n = part.rows - (part.from + first_tile + i / 2 * step) * kKeys - i % 2 * (kKeys / 2);  // rows that exist: n or all
           uint32_t x[2][32];
@@ -417,8 +461,7 @@ template <typename T, int DP, bool PAIR> __global__ void __launch_bounds__(kThre
             const float shrink = grown ? exp2_fast(m - top) : 1.f;  // (0 at first)
             if (grown) m = top;
             l *= shrink;
-            if (i > 0) {
-              // (the values before these have been added; those before them had been when the scores were there)
+            if (i % kSpan > 0) {
               good = __all_sync(~0u, wait_phase(at(values[s]), (done - 1) & 1, late));
               if (!good) break;
               tensor_after_sync();
@@ -458,9 +501,6 @@ template <typename T, int DP, bool PAIR> __global__ void __launch_bounds__(kThre
       }
       const bool first = halves == 0;
       if (!good) continue;
-      // This part's result, in units of one.
-      constexpr float unit = Parts<T>::kUnit == 0.f ? 1.f : 1.f / 1024.f;
-      const int64_t place = ((int64_t)blockIdx.x + part.item) * 2 + s;
       if (!first) {
         // (a barrier tells a phase from the next only: the last but one first)
         good = __all_sync(~0u, wait_phase(at(values[s]), (done - 2) & 1, late) && wait_phase(at(values[s]), (done - 1) & 1, late));
@@ -469,19 +509,7 @@ template <typename T, int DP, bool PAIR> __global__ void __launch_bounds__(kThre
       }
       if (!idle) {
         a.ml[place * 128 + row] = make_float2(first ? -INFINITY : m, l * unit);
-        if (!first) {
-          float4 *const o = reinterpret_cast<float4 *>(a.o) + place * (DP / 4 * 128) + row;
-#pragma unroll 1
-          for (int c = 0; c < DP; c += 32) {
-            uint32_t x[32];
-            tensor_load32(x, o_at + c);
-            wait_tensor_loads(x);
-#pragma unroll
-            for (int i = 0; i < 32; i += 4)
-              o[(c + i) / 4 * 128] = make_float4(__uint_as_float(x[i]) * unit, __uint_as_float(x[i + 1]) * unit,
-                                                 __uint_as_float(x[i + 2]) * unit, __uint_as_float(x[i + 3]) * unit);
-          }
-        }
+        if (!first) add_up();
       }
       tensor_before_sync();
     }

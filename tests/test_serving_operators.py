@@ -196,6 +196,27 @@ def test_prefix_attention_many_tiles_each(kind, dim, page_size, share, prefix):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("kind", ["bf16", "f16"])
+def test_prefix_attention_holds_its_sums(kind):
+    """131072 rows of values that are all the same, a whole item to a CTA.  The tensor cores cut off less than 2^-23 of a sum for each
+    product; the sums of 16 tiles, of 16 products each, are held by them: 2^-15.  The weights' two parts 2^-16, and sums in 32 bits of
+    them, 64 to an addition chain, 32 chains of a tile's 4 and 2048 of a part: under 2^-16 if they are rounded."""
+    n, share, q_heads, heads, dim, ps = 131072, 76, 256, 8, 64, 128
+    pages = n // ps
+    k = _randn((pages, heads, ps, dim), kind, 1)
+    v = torch.full((pages, heads, ps, dim), 1.0 / 3, device="cuda").to(TORCH[kind])
+    cache, plan = gar.KVCache(k, v), gar.gar_attn_plan_create(q_heads, heads, dim)
+    table = torch.arange(pages, dtype=torch.int32, device="cuda")[None]
+    lens = torch.tensor([n], dtype=torch.int32, device="cuda")
+    none, zero = torch.zeros((share, 0), dtype=torch.int32, device="cuda"), torch.zeros(share, dtype=torch.int32, device="cuda")
+    q = _randn((share, q_heads, dim), kind, 2) * 0.2
+    out = torch.empty((share, q_heads, dim), device="cuda")
+    gar.gar_prefix_attention(plan, q, cache, table, lens, none, zero, out=out)
+    off = (out.double() / float(v[0, 0, 0, 0]) - 1).abs().max()
+    assert float(off) <= 2.0 ** -15 + 2.0 ** -16 + 2.0 ** -16, float(off)
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("scale", [0.0, -0.1])
 @pytest.mark.parametrize("wide", [False, True])
 def test_prefix_attention_scales(scale, wide):
