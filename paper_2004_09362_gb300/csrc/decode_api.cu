@@ -79,8 +79,10 @@ int check_groups(const gar_attn_plan *plan, int batch, int groups) {
   return GAR_OK;
 }
 
-// Queries of a cached head and a prefix from which on the prefix goes to the tensor cores' own memory, 128 at a time.
-constexpr int kManyQueries = 24;
+// Queries of a cached head and a prefix from which on the prefix goes to the tensor cores' own memory, 128 at a time: more than the
+// other kernel takes for one reading of the rows.  (The two, 8 cached heads x 128: 65536 rows bf16, 16 queries 96 us and 83, 24 95 and 118,
+// 64 96 and 220; 20000 rows f16, 16 queries 56 and 49, 24 54 and 59.)
+constexpr int kManyQueries = 17;
 constexpr int kManyItems = 1024;  // blocks of queries at most: each has 132 KB of partial results
 int blocks_of(int rows) { return rows > 128 ? (rows + 255) / 256 : 1; }
 

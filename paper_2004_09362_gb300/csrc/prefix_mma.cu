@@ -527,13 +527,14 @@ template <typename T, int DP, bool PAIR> __global__ void __launch_bounds__(kThre
   }
 }
 
-constexpr int kJoinThreads = 256, kJoinRows = 32, kJoinChannels = 32;
+constexpr int kJoinThreads = 256, kJoinRows = 32, kJoinChannels = 16;
 
-// Joins the parts of 32 queries of an item and their sequences' own rows' results, for 32 channels: a query to a lane, four
-// channels to a warp.
+// Joins the parts of 32 queries of an item and their sequences' own rows' results, for 16 channels: a query to a lane, four
+// channels of half the parts to a warp.
 template <int DP> __global__ void __launch_bounds__(kJoinThreads) join_kernel(const PrefixArgs a, const JoinArgs j) {
   extern __shared__ float factors[];  // [part][query]: what the part counts for
   __shared__ float tops[kJoinThreads / 32][32], sums[kJoinThreads / 32][32];
+  __shared__ float4 others[4][32];
   after_earlier_kernels();
   const int lane = threadIdx.x & 31, warp = threadIdx.x / 32, per_item = (a.pair ? 256 : 128) / kJoinRows;
   const int item = blockIdx.x / per_item, items = a.c.heads * a.blocks, g = item / items, in_group = item - g * items;
@@ -573,22 +574,28 @@ template <int DP> __global__ void __launch_bounds__(kJoinThreads) join_kernel(co
   for (int w = 0; w < kJoinThreads / 32; ++w) l += sums[w][lane];
   const float inverse = l == 0.f ? 0.f : 1.f / l;
   if (warp == 0 && blockIdx.y == 0 && there && j.lse) j.lse[own_at] = l == 0.f ? -INFINITY : (off + log2f(l)) * 0.693147180559945f;
-  const int d = blockIdx.y * kJoinChannels + warp * 4;
-  if (d >= j.dim) return;
+  const int quad = warp & 3, upper = warp / 4, d = blockIdx.y * kJoinChannels + quad * 4, half = (parts + 1) / 2;
   float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
-  if (!(own_weight == 0.f)) {
-    const float4 y = __ldcg(reinterpret_cast<const float4 *>(j.parts[0].out + own_at * j.parts[0].row + d));
-    x.x = own_weight * y.x, x.y = own_weight * y.y, x.z = own_weight * y.z, x.w = own_weight * y.w;
-  }
-  const float4 *const o = reinterpret_cast<const float4 *>(a.o) + ((((int64_t)first + item) * 2 + sub0) * (DP / 4) + d / 4) * 128 + in_sub;
+  if (d < j.dim) {
+    if (!upper && !(own_weight == 0.f)) {
+      const float4 y = __ldcg(reinterpret_cast<const float4 *>(j.parts[0].out + own_at * j.parts[0].row + d));
+      x.x = own_weight * y.x, x.y = own_weight * y.y, x.z = own_weight * y.z, x.w = own_weight * y.w;
+    }
+    const float4 *const o = reinterpret_cast<const float4 *>(a.o) + ((((int64_t)first + item) * 2 + sub0) * (DP / 4) + d / 4) * 128 + in_sub;
+    const int end = upper ? parts : half;
 #pragma unroll 8
-  for (int p = 0; p < parts; ++p) {
-    const float f = factors[p * 32 + lane];
-    const float4 y = __ldcg(o + (int64_t)p * step * (DP / 4 * 128));
-    // (a part without rows has left no o)
-    if (!(f == 0.f)) x.x += f * y.x, x.y += f * y.y, x.z += f * y.z, x.w += f * y.w;
+    for (int p = upper ? half : 0; p < end; ++p) {
+      const float f = factors[p * 32 + lane];
+      const float4 y = __ldcg(o + (int64_t)p * step * (DP / 4 * 128));
+      // (a part without rows has left no o)
+      if (!(f == 0.f)) x.x += f * y.x, x.y += f * y.y, x.z += f * y.z, x.w += f * y.w;
+    }
   }
-  if (!there) return;
+  if (upper) others[quad][lane] = x;
+  __syncthreads();
+  if (upper || d >= j.dim || !there) return;
+  const float4 y = others[quad][lane];
+  x.x += y.x, x.y += y.y, x.z += y.z, x.w += y.w;
   const float z[4] = {x.x * inverse, x.y * inverse, x.z * inverse, x.w * inverse};
   const int64_t at = b * j.ob + h * j.oh + d;
   if (j.out_dtype == GAR_F32) {

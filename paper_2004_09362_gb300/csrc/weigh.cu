@@ -1,11 +1,14 @@
 // The attention weights that cached rows gather: out[n] = weights[n] + sum_j exp(scale q_j.k_n - lse_j).
 //
 // Bound by memory: each key is read once for all the queries of its head, values not at all.  Scores are computed on tensor
-// cores as in decode attention, S^T = K Q^T with 16 rows of the cache by 8 queries, but nothing of a tile is needed twice, so
-// keys go from memory to the registers that multiply them: which channel sits at which place of the summed
+// cores as in decode attention, S^T = K Q^T with 16 rows of the cache by 8 queries: which channel sits at which place of the summed
 // dimension is free as long as keys and queries agree, so a lane's part of a row is whole 16-byte chunks (lane t of the
-// four that share a row has chunks t, t + 4, ...).  A warp copies its rows to a ring of its own, two tiles and
-// more ahead.  The rows of all sequences are shared out among the CTAs as in decode attention, by equal numbers.
+// four that share a row has chunks t, t + 4, ...).  A warp copies its rows to a ring of its own, two tiles and more ahead.  The rows of all
+// sequences are shared out among the CTAs as in decode attention, by equal numbers; entries of other rows are copied by a
+// warp of their own beside that.
+//
+// 24 x up to 8192 rows, 32/8 x 128 bf16: 49 us, 4.3 TB/s; 1 x 1021, 10/5 x 80 f16: 5 us.  What is missing to the copy rate are the ends of
+// segments, where a CTA has nothing on its way.
 //
 // 8-bit codes become f16 exactly, as do the queries that go with them: the head's largest is brought to 2^14, 32-bit ones in two
 // parts.  Keys of 32 bits are multiplied in 32 bits without tensor cores.
