@@ -134,7 +134,7 @@ __device__ __forceinline__ void move_rows(const EvictArgs &a, int b, int head, c
 // NK: keys that a lane holds in registers; 0: they are made anew each time.  U: what rows are copied in.
 template <int NK, typename U> __global__ void __launch_bounds__(kThreads, 4) evict_kernel(const EvictArgs a) {
   constexpr int WARPS = kMostCtas * kWarps;
-  __shared__ int histogram[4][256], largest[WARPS], counts[3][WARPS];
+  __shared__ int histogram[4][256], total[256], largest[WARPS], counts[3][WARPS];
   __shared__ uint32_t found[4];
   __shared__ int left[4], alike[4];
   const int rank = cluster_rank(), warp = threadIdx.x / 32, lane = threadIdx.x & 31, me = rank * kWarps + warp;
@@ -221,13 +221,23 @@ template <int NK, typename U> __global__ void __launch_bounds__(kThreads, 4) evi
         if (((key ^ threshold) & above) == 0) atomicAdd(&histogram[digit][key >> shift & 255], 1);
       });
       sync();
+      if (!alone) {
+        // The CTAs' counts, a value to a thread.  (By one warp, 64 reads of other CTAs' memory a lane, this took most of the time.)
+        static_assert(kThreads == 256, "a thread for each value");
+        int its[kMostCtas], sum = 0;
+#pragma unroll
+        for (int r = 0; r < kMostCtas; ++r) its[r] = r < a.ctas ? load_from_cta(&histogram[digit][threadIdx.x], r) : 0;
+#pragma unroll
+        for (int r = 0; r < kMostCtas; ++r) sum += its[r];
+        total[threadIdx.x] = sum;
+        __syncthreads();
+      }
       if (warp == 0) {
         // A lane for 8 values, the largest first.
         int count[8], sum = 0;
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-          count[i] = 0;
-          for (int r = 0; r < a.ctas; ++r) count[i] += load_from_cta(&histogram[digit][255 - 8 * lane - i], r);
+          count[i] = (alone ? histogram[digit] : total)[255 - 8 * lane - i];
           sum += count[i];
         }
         int upto = sum;

@@ -6,22 +6,22 @@
 //
 //  * 4 warps copy the rows to a ring of tiles in shared memory: boxes of pages by tensor copies where tiles are whole pages or pages
 //    whole tiles, cp.async for pages of any other size and for last tiles, whose rows past the end have to be zeros.
-//    (131072 rows, one block: 117 us with boxes of 64 rows, 131 with cp.async.  A lane's tensor copy takes some 190 clocks to issue.)
+//    (131072 rows, one block, when this was built: 117 us with boxes of 64 rows, 131 with cp.async.  A lane's tensor copy takes some 190 clocks to issue.)
 //  * A thread for each stream issues its products.  S and O are in tensor memory, 128 columns each.  S is computed by halves of 64 rows, the
-//    next half's while the weights of one are computed (16384 rows x 1000 queries: 103 us, whole tiles 111).
+//    next half's while the weights of one are computed (16384 rows x 1000 queries: 171 us a call, with whole tiles 180).
 //  * 4 warps for each stream turn S to P, a query to a thread: no exchange between lanes.  P goes where S was, as two 16-bit parts
-//    (2^-16 of the weight; one part alone would be 2^-9, as much as the output's rounding, and took 98 us for 111), 16 columns each for
+//    (2^-16 of the weight; one part alone would be 2^-9, as much as the output's rounding, and saved a tenth), 16 columns each for
 //    32 rows.  These warps have 192 registers, the others 64: a half's scores fit them.
 //  * The tensor cores cut their sums off rather than round them: 2^-24 and more of the sum for each of 16 products a tile, all one way (parts
 //    of 1024 tiles came out 1.6e-3 short, of 54 tiles 3e-5).  So O holds 16 tiles at most, and is then added to the part's result in
-//    memory, rounded: 1.6e-5 is missing at most.  (8 tiles, by reductions in the L2: 0.8e-5, and 40 us more of 150.)
+//    memory, rounded: less than 2^-15 is missing (2e-5 measured).  (8 tiles, by reductions in the L2: 1e-5, and 40 us more of 150.)
 //  * m is not the running maximum but a number within kLazy of it: O is rescaled only where the maximum passes m + kLazy.
 //
 // The tiles of all items are shared out among the CTAs as one line.  Each CTA leaves (m, l, O) for its part of
 // an item; the parts are joined in their order by the kernel after this.
 //
-// Bound, with few queries, by the rows' way from memory: 32 sequences of 32/8 heads x 128 bf16 over 131072 rows 115 us, 4.7 TB/s.  With many, 250
-// sequences over 16384 rows f16, 103 us: 0.66 PFLOP/s of S and P V, 0.99 counting both parts of P.  There a pair of tiles takes
+// Bound, with few queries, by the rows' way from memory: 32 sequences of 32/8 heads x 128 bf16 over 131072 rows 112 us, 4.8 TB/s.  With many, 250
+// sequences over 16384 rows f16, 105 us: 0.64 PFLOP/s of S and P V, 0.97 counting both parts of P.  There a pair of tiles takes
 // 6200 clocks, of which its products take 4700 alone (3100 at the peak rate) and its weights 4400; leaving the exponentials, the
 // parts or the stores out changed little, so what remains is that products and weights hardly overlap.  The first 12 us of a
 // launch are the pages, the queries and the first copies, one after the other, and the instructions.
