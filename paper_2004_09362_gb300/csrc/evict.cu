@@ -9,7 +9,7 @@
 // `keep` on.
 //
 // Bound by the chain of steps, each with a barrier of the CTA or cluster: 48 sequences of 1025 rows of 8 heads x 128 bf16, one row too many,
-// 17 us; 8 sequences of up to 16001 rows of 4 heads x 96 i8, cut to 4000, 55 us, 24 of them the moves.  The keys stay in registers between the
+// 13 us; 8 sequences of up to 16001 rows of 4 heads x 96 i8, cut to 4000, 39 us, 24 of them the moves.  The keys stay in registers between the
 // counts where they fit.
 #include <algorithm>
 #include <climits>
@@ -378,8 +378,8 @@ extern "C" int gar_kv_evict(const gar_kv_cache *cache, const float *weights, con
     a.lanes = 1;
     while (a.lanes < 32 && a.lanes < 2 * a.units) a.lanes *= 2;
     const auto kernel = a.each <= 8 ? evict_kernel<8, U> : a.each <= 16 ? evict_kernel<16, U> : evict_kernel<0, U>;
-    // Many rows are moved by a kernel of its own, all over the GPU.  (8 x up to 16001 rows cut to 4000, 4 heads x 96 i8: 55 us, by the
-    // clusters that chose them 70; a kernel more costs 2 us where there is one row to move.)
+    // Many rows are moved by a kernel of its own, all over the GPU.  (8 x up to 16001 rows cut to 4000, 4 heads x 96 i8: 55 us when this
+    // was built, by the clusters that chose them 70; a kernel more costs 2 us where there is one row to move.)
     const int64_t most = std::min(a.most_rows - keep, keep - first), per = kWarps * (32 / a.lanes) * 4;
     a.apart = most > 256;
     if (int rc = launch_clusters("gar_kv_evict", kernel, items * a.ctas, a.ctas, kThreads, stream, a)) return rc;
