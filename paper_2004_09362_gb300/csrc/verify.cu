@@ -15,7 +15,7 @@
 // exactly and added up beside it (Knuth's TwoSum).  64 bits are out of the question, this GPU does two such additions a clock and SM:
 // the warps' sums and scans alone took most of the time in 64 bits.
 //
-// 256 sequences, 131072 f32: 65 us, 4.1 TB/s; 57, 50021 bf16: 12 us; one, 32768 f32: 7 us, which is the chain of drafts, their
+// 256 sequences, 131072 f32: 67 us, 4.0 TB/s; 57, 50021 bf16: 12 us; one, 32768 f32: 7 us, which is the chain of drafts, their
 // probabilities, rows, sums and the token, each a round trip.
 #include <climits>
 
