@@ -223,8 +223,9 @@ template <typename T> __device__ __forceinline__ int last_of(const Row<T> &row, 
   return __reduce_max_sync(~0u, last);
 }
 
-// The first token of the groups from `from` on, up to `to`, at which `before` and the running sum pass `goal`, as they do; where rounding
-// hides that, the last that counts.
+// The first token that counts, of the groups from `from` on, up to `to`, at which `before` and the running sum pass `goal`, as they do; where
+// rounding hides that, the last that counts.  (A token that does not count passes where the one before it did.  But a lane's running sum
+// begins with one that was added up in another order than the lane's before it, so rounding may show that passing at the next token first.)
 template <typename T>
 __device__ __forceinline__ int find(const Row<T> &row, int64_t from, int64_t to, int vocab, Sum before, Sum goal) {
   const int lane = threadIdx.x & 31;
@@ -236,11 +237,13 @@ __device__ __forceinline__ int find(const Row<T> &row, int64_t from, int64_t to,
     load_ends(row.p, v, vocab, p);
     if (row.less) load_ends(row.q, v, vocab, q);
     Sum upto[kGroup], sum;
+    bool counts[kGroup];
     int mine = -1;  // the lane's last that counts
 #pragma unroll
     for (int i = 0; i < kGroup; ++i) {
       const Sum w = remaining(p[i], q[i]);
-      if (w.high > 0.f) mine = i;
+      counts[i] = w.high > 0.f;
+      if (counts[i]) mine = i;
       upto[i] = sum = sum + w;
     }
     const Sum with = running(sum);
@@ -249,9 +252,8 @@ __device__ __forceinline__ int find(const Row<T> &row, int64_t from, int64_t to,
     int passed = kGroup;
 #pragma unroll
     for (int i = kGroup - 1; i >= 0; --i)
-      if (start + upto[i] > goal) passed = i;
-    // (the first that passes counts itself: its predecessor does not pass)
-    const uint32_t past = __ballot_sync(~0u, passed < kGroup && mine >= passed), some = __ballot_sync(~0u, mine >= 0);
+      if (counts[i] && start + upto[i] > goal) passed = i;
+    const uint32_t past = __ballot_sync(~0u, passed < kGroup), some = __ballot_sync(~0u, mine >= 0);
     if (past) {
       const int from_one = __ffs(past) - 1;
       return __shfl_sync(~0u, v + passed, from_one);
@@ -326,12 +328,15 @@ template <typename T> __global__ void __launch_bounds__(kThreads, 4) verify_kern
     constexpr int EACH = kMostCtas * kWarps / 32;
     if (warp == 0) {
       Sum upto[EACH], sum;
+      bool counts[EACH];  // (as in find(): a run of nothing is not the one)
 #pragma unroll
       for (int i = 0; i < EACH; ++i) {
         const int k = lane * EACH + i;
+        counts[i] = false;
         if (k < a.ctas * kWarps) {
           Sum x;
           x.high = totals[pass][k].x, x.low = totals[pass][k].y;
+          counts[i] = x.high > 0.f;
           sum = sum + x;
         }
         upto[i] = sum;
@@ -346,7 +351,7 @@ template <typename T> __global__ void __launch_bounds__(kThreads, 4) verify_kern
       Sum low;
 #pragma unroll
       for (int i = EACH - 1; i >= 0; --i)
-        if (upto[i] > goal) k = lane * EACH + i, low = i == 0 ? start : upto[i - 1];
+        if (counts[i] && upto[i] > goal) k = lane * EACH + i, low = i == 0 ? start : upto[i - 1];
       const uint32_t past = __ballot_sync(~0u, k >= 0);
       if (lane == (past ? __ffs(past) - 1 : 0)) {
         picked = past ? k : -1, empty = !(all.high > 0.f);
