@@ -237,13 +237,11 @@ __device__ __forceinline__ int find(const Row<T> &row, int64_t from, int64_t to,
     load_ends(row.p, v, vocab, p);
     if (row.less) load_ends(row.q, v, vocab, q);
     Sum upto[kGroup], sum;
-    bool counts[kGroup];
-    int mine = -1;  // the lane's last that counts
+    uint32_t counts = 0;  // which of the lane's tokens count
 #pragma unroll
     for (int i = 0; i < kGroup; ++i) {
       const Sum w = remaining(p[i], q[i]);
-      counts[i] = w.high > 0.f;
-      if (counts[i]) mine = i;
+      if (w.high > 0.f) counts |= 1u << i;
       upto[i] = sum = sum + w;
     }
     const Sum with = running(sum);
@@ -252,13 +250,11 @@ __device__ __forceinline__ int find(const Row<T> &row, int64_t from, int64_t to,
     int passed = kGroup;
 #pragma unroll
     for (int i = kGroup - 1; i >= 0; --i)
-      if (counts[i] && start + upto[i] > goal) passed = i;
-    const uint32_t past = __ballot_sync(~0u, passed < kGroup), some = __ballot_sync(~0u, mine >= 0);
-    if (past) {
-      const int from_one = __ffs(past) - 1;
-      return __shfl_sync(~0u, v + passed, from_one);
-    }
-    if (some) last = __shfl_sync(~0u, v + mine, 31 - __clz(some));
+      if (start + upto[i] > goal) passed = i;
+    const uint32_t later = counts & ~0u << passed;
+    const uint32_t past = __ballot_sync(~0u, later != 0), some = __ballot_sync(~0u, counts != 0);
+    if (past) return __shfl_sync(~0u, v + __ffs(later) - 1, __ffs(past) - 1);
+    if (some) last = __shfl_sync(~0u, v + 31 - __clz(counts), 31 - __clz(some));
     before = before + from_lane(with, 31);
   }
   return last;
@@ -328,15 +324,12 @@ template <typename T> __global__ void __launch_bounds__(kThreads, 4) verify_kern
     constexpr int EACH = kMostCtas * kWarps / 32;
     if (warp == 0) {
       Sum upto[EACH], sum;
-      bool counts[EACH];  // (as in find(): a run of nothing is not the one)
 #pragma unroll
       for (int i = 0; i < EACH; ++i) {
         const int k = lane * EACH + i;
-        counts[i] = false;
         if (k < a.ctas * kWarps) {
           Sum x;
           x.high = totals[pass][k].x, x.low = totals[pass][k].y;
-          counts[i] = x.high > 0.f;
           sum = sum + x;
         }
         upto[i] = sum;
@@ -350,8 +343,10 @@ template <typename T> __global__ void __launch_bounds__(kThreads, 4) verify_kern
       int k = -1;
       Sum low;
 #pragma unroll
-      for (int i = EACH - 1; i >= 0; --i)
-        if (counts[i] && upto[i] > goal) k = lane * EACH + i, low = i == 0 ? start : upto[i - 1];
+      for (int i = EACH - 1; i >= 0; --i) {  // (a run that counts, as in find())
+        const int at = lane * EACH + i;
+        if (upto[i] > goal && at < a.ctas * kWarps && totals[pass][at].x > 0.f) k = at, low = i == 0 ? start : upto[i - 1];
+      }
       const uint32_t past = __ballot_sync(~0u, k >= 0);
       if (lane == (past ? __ffs(past) - 1 : 0)) {
         picked = past ? k : -1, empty = !(all.high > 0.f);
