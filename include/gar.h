@@ -590,7 +590,8 @@ GAR_API int gar_kv_evict(const gar_kv_cache *cache, const float *weights, const 
  * After the a drafts that stand comes one more token, drawn with u = uniform_drafts, the last: where a draft was refused from
  * r = max(p_a - q_a, 0), or from r = p_a where that is all zero; where there are no more drafts from r = p_a.  It is the
  * first v with r(0) + ... + r(v) > u (r(0) + ... + r(vocab - 1)), or, where there is none, the last with r(v) > 0, or -1.
- * Products are exact; sums are held in twice 32 bits, about 2^-45 of the sum.
+ * Products are exact; sums are held in twice 32 bits, those of many thousands of a lane's tokens in 64: off by about 2^-44 of the sum,
+ * whatever the vocabulary.
  * out_tokens: [batch][drafts + 1] of token_bytes: the drafts that stand, that token, then -1.  accepted: [batch], a.
  * All integers and uniform are contiguous; out_tokens may not overlap tokens. */
 GAR_API int gar_verify_drafts(const void *target, int64_t target_batch_stride, int64_t target_row_stride, const void *draft,

@@ -13,7 +13,9 @@
 // The token is a choice at a border between running sums, so these have to be better than 32 bits: after 131072 terms a sum in 32 bits
 // is off by more than a whole token's share.  All sums are held in twice 32 bits: the error of each addition is computed
 // exactly and added up beside it (Knuth's TwoSum).  64 bits are out of the question, this GPU does two such additions a clock and SM:
-// the warps' sums and scans alone took most of the time in 64 bits.
+// the warps' sums and scans alone took most of the time in 64 bits.  But the errors that are added up beside are rounded themselves, and
+// with very many they lose what they are there for (400 million numbers, half of them equal: 2^-24 of the sum).  So a lane of a longer run
+// adds up kRounds groups at a time, and those sums in 64 bits.
 //
 // 256 sequences, 131072 f32: 67 us, 4.0 TB/s; 57, 50021 bf16: 12 us; one, 32768 f32: 7 us, which is the chain of drafts, their
 // probabilities, rows, sums and the token, each a round trip.
@@ -28,6 +30,7 @@ constexpr int kThreads = 256, kWarps = kThreads / 32;
 constexpr int kMostCtas = 8;  // of a cluster
 constexpr int kSubs = 4;      // pieces of a warp's run
 constexpr int kGroup = 4;     // neighbouring tokens of a lane
+constexpr int kRounds = 64;   // sums are held in twice 32 bits over so many groups of a lane and piece
 
 struct VerifyArgs {
   const void *target, *draft;
@@ -167,13 +170,13 @@ __device__ __forceinline__ void add_pair(Sums &s, float2 p, float2 q) {
   s.high = t;
 }
 
-// A lane's part of the sums of a run's kSubs pieces.  Groups of tokens begin `shift` tokens early, where the target's row is
-// aligned.
+// A lane's part of the sums of tokens [at, end) of a run's kSubs pieces.  Groups of tokens begin `shift` tokens early, where the
+// target's row is aligned.
 template <typename T, int DRAFT>
-__device__ __forceinline__ void add_run(const Row<T> &row, int64_t from, int piece, int vocab, int shift, Sums (&s)[kSubs]) {
+__device__ __forceinline__ void add_run(const Row<T> &row, int64_t from, int piece, int vocab, int shift, int at, int end, Sums (&s)[kSubs]) {
   const int lane = threadIdx.x & 31;
 #pragma unroll 1
-  for (int k = lane * kGroup; k < piece; k += 32 * kGroup) {
+  for (int k = at + lane * kGroup; k < end; k += 32 * kGroup) {
     Group<T, true> p[kSubs];
     Group<T, DRAFT == DRAFT_WIDE> q[kSubs];
     int v[kSubs];
@@ -204,6 +207,12 @@ __device__ __forceinline__ Sum both(const Sums &s) {
   a.high = s.high.x, a.low = s.low.x, b.high = s.high.y, b.low = s.low.y;
   return neat(a) + neat(b);
 }
+__device__ __forceinline__ double in_64(Sum a) { return (double)a.high + a.low; }
+__device__ __forceinline__ Sum in_twice_32(double x) {
+  Sum a;
+  a.high = (float)x, a.low = (float)(x - a.high);
+  return a;
+}
 
 // The sum over the lanes, in the same order in each.
 __device__ __forceinline__ Sum over_lanes(Sum a) {
@@ -226,10 +235,13 @@ template <typename T> __device__ __forceinline__ int last_of(const Row<T> &row, 
 // The first token that counts, of the groups from `from` on, up to `to`, at which `before` and the running sum pass `goal`, as they do; where
 // rounding hides that, the last that counts.  (A token that does not count passes where the one before it did.  But a lane's running sum
 // begins with one that was added up in another order than the lane's before it, so rounding may show that passing at the next token first.)
-template <typename T>
+template <typename T, bool LONG>
 __device__ __forceinline__ int find(const Row<T> &row, int64_t from, int64_t to, int vocab, Sum before, Sum goal) {
   const int lane = threadIdx.x & 31;
   int last = -1;
+  double whole = LONG ? in_64(before) : 0.;
+  Sum part;  // (LONG) what has come to `before` since it was `whole`
+  int rounds = 0;
 #pragma unroll 1
   for (int64_t v0 = from; v0 < to; v0 += 32 * kGroup) {
     const int v = (int)min(v0 + lane * kGroup, (int64_t)vocab);
@@ -256,11 +268,16 @@ __device__ __forceinline__ int find(const Row<T> &row, int64_t from, int64_t to,
     if (past) return __shfl_sync(~0u, v + __ffs(later) - 1, __ffs(past) - 1);
     if (some) last = __shfl_sync(~0u, v + 31 - __clz(counts), 31 - __clz(some));
     before = before + from_lane(with, 31);
+    if constexpr (LONG) {
+      part = part + from_lane(with, 31);
+      if (++rounds % kRounds == 0) whole += in_64(part), before = in_twice_32(whole), part = Sum();
+    }
   }
   return last;
 }
 
-template <typename T> __global__ void __launch_bounds__(kThreads, 4) verify_kernel(const VerifyArgs a) {
+// LONG: pieces of more than kRounds groups a lane.
+template <typename T, bool LONG> __global__ void __launch_bounds__(kThreads, 4) verify_kernel(const VerifyArgs a) {
   __shared__ float2 totals[2][kMostCtas * kWarps];
   __shared__ int lasts[kMostCtas * kWarps];
   __shared__ int stop, refused, picked, empty;
@@ -304,19 +321,28 @@ template <typename T> __global__ void __launch_bounds__(kThreads, 4) verify_kern
   cluster_wait();
 
   const float u = fmaxf(a.uniform[b * (a.drafts + 1) + a.drafts], 0.f);
-  Sums sums[kSubs];
+  Sum pieces[kSubs];  // this lane's part
   for (int pass = 0; pass < 2; ++pass) {
+    double whole[LONG ? kSubs : 1] = {};
+    for (int at = 0;;) {
+      const int end = LONG ? min(a.piece, at + kRounds * 32 * kGroup) : a.piece;
+      Sums sums[kSubs];
+      if (!row.less)
+        add_run<T, DRAFT_NONE>(row, begin, a.piece, a.vocab, shift, at, end, sums);
+      else if ((uintptr_t)(row.q - shift) % kWide == 0)
+        add_run<T, DRAFT_WIDE>(row, begin, a.piece, a.vocab, shift, at, end, sums);
+      else
+        add_run<T, DRAFT_NARROW>(row, begin, a.piece, a.vocab, shift, at, end, sums);
 #pragma unroll
-    for (int i = 0; i < kSubs; ++i) sums[i] = Sums();
-    if (!row.less)
-      add_run<T, DRAFT_NONE>(row, begin, a.piece, a.vocab, shift, sums);
-    else if ((uintptr_t)(row.q - shift) % kWide == 0)
-      add_run<T, DRAFT_WIDE>(row, begin, a.piece, a.vocab, shift, sums);
-    else
-      add_run<T, DRAFT_NARROW>(row, begin, a.piece, a.vocab, shift, sums);
-    Sum mine = both(sums[0]);
+      for (int i = 0; i < kSubs; ++i) {
+        pieces[i] = both(sums[i]);
+        if constexpr (LONG) whole[i] += in_64(pieces[i]), pieces[i] = in_twice_32(whole[i]);
+      }
+      if (!LONG || (at = end) >= a.piece) break;
+    }
+    Sum mine = pieces[0];
 #pragma unroll
-    for (int i = 1; i < kSubs; ++i) mine = mine + both(sums[i]);
+    for (int i = 1; i < kSubs; ++i) mine = mine + pieces[i];
     mine = over_lanes(mine);
     if (lane < a.ctas) store_in_cta(&totals[pass][me], lane, make_float2(mine.high, mine.low));
     cluster_sync();
@@ -369,12 +395,12 @@ template <typename T> __global__ void __launch_bounds__(kThreads, 4) verify_kern
     bool found = false;
 #pragma unroll
     for (int i = 0; i < kSubs; ++i) {
-      const Sum x = over_lanes(both(sums[i])), next = sum + x;
+      const Sum x = over_lanes(pieces[i]), next = sum + x;
       if (!found && x.high > 0.f) piece = i, start = sum, found = next > goal;
       sum = next;
     }
     const int64_t first = begin + piece * a.piece - shift;
-    const int token = find(row, first, first + a.piece, a.vocab, start, goal);
+    const int token = find<T, LONG>(row, first, first + a.piece, a.vocab, start, goal);
     if (lane == 0) put_token(a, out + stop, token);
   } else if (picked < 0) {
     const int last = last_of(row, from, to);
@@ -433,6 +459,7 @@ extern "C" int gar_verify_drafts(const void *target, int64_t target_batch_stride
   a.piece = (int)((vocab + kGroup - 1 + round - 1) / round) * 32 * kGroup;
   return with_float(dtype, [&](auto t) {
     using T = typename decltype(t)::type;
-    return launch_clusters("gar_verify_drafts", verify_kernel<T>, (int64_t)batch * a.ctas, a.ctas, kThreads, stream, a);
+    const auto kernel = a.piece > kRounds * 32 * kGroup ? verify_kernel<T, true> : verify_kernel<T, false>;
+    return launch_clusters("gar_verify_drafts", kernel, (int64_t)batch * a.ctas, a.ctas, kThreads, stream, a);
   });
 }

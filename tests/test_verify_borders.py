@@ -1,7 +1,8 @@
-"""The verification of drafts where a token hangs on the last bits of running sums: borders next to tokens that cannot be drawn.
-What is right is computed in whole numbers.
+"""The verification of drafts where a token hangs on the last bits of running sums: borders next to tokens that cannot be drawn,
+and sums of very many probabilities.  What is right is computed in whole numbers.
 """
 
+import math
 import random
 from fractions import Fraction
 
@@ -9,6 +10,7 @@ import pytest
 import torch
 
 from paper_2004_09362_gb300 import gar
+from test_serving_operators import _verify_case, _verify_reference
 
 I64 = torch.int64
 
@@ -63,3 +65,64 @@ def test_a_token_that_cannot_be_drawn_is_never_drawn(vocab, batch, step, skipped
     # A sum of two is off by 2^-47 of it at most (the low part's rounding, once as it is added up and once as it is put right), of which
     # a border here is made of 16 in turn at most: sums in a lane and over lanes, runs and pieces, and the product.
     assert bad == 0 and far <= Fraction(1, 2 ** 43), (bad, float(far))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("vocab", [1_000_003, 100_000_007])
+def test_sums_of_many_probabilities(vocab):
+    """Dense probabilities, multiples of 2^-24, and numbers u that come within 2^-41.5 to 2^-40 of a border between two tokens."""
+    g = torch.Generator(device="cuda").manual_seed(3)
+    m = torch.randint(1, 1 << 24, (vocab,), generator=g, device="cuda")
+    upto = m.cumsum(0)
+    total = int(upto[-1])
+    j = torch.arange(1, 1 << 24, device="cuda")
+    low = j * (total & 0xffffff)
+    whole, part = j * (total >> 24) + (low >> 24), low & 0xffffff     # u times the sum, and its fraction in 2^-24
+    token = torch.searchsorted(upto, whole, right=True)
+    above, below = upto[token] - whole, whole - torch.where(token > 0, upto[(token - 1).clamp(min=0)], 0)
+    off = torch.minimum(above.double() - part.double() / 2 ** 24, below.double() + part.double() / 2 ** 24) / total
+    near = ((off >= 2.0 ** -41.5) & (off < 2.0 ** -40) & (token > 0) & (token < vocab - 1)).nonzero().flatten()
+    near = near[torch.linspace(0, near.numel() - 1, min(64, near.numel()), device="cuda").long()]
+    assert near.numel() >= 4
+    n = near.numel()
+    target = (m.float() / 2 ** 24)[None, None].expand(n, 1, vocab)
+    none = torch.zeros((n, 0), dtype=I64, device="cuda")
+    got, _ = gar.gar_verify_drafts(target, target[:, :0], none, (j[near].double() / 2 ** 24).float()[:, None])
+    wrong = (got[:, 0] != token[near]).sum()
+    assert int(wrong) == 0, (int(wrong), n)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("value", [8751087, 9007193, 8456019])
+def test_sums_of_many_equal_probabilities(value):
+    """Half of the tokens have one probability, half another: every addition of a lane rounds the same way."""
+    vocab, half, other = 400_000_000, 200_000_000, 1 << 22
+    target = torch.full((1, 1, vocab), value / 2 ** 24, device="cuda")
+    target[..., half:] = other / 2 ** 24
+    rng = random.Random(value)
+    j = [rng.randrange(1, 1 << 24) for _ in range(16)]
+    want = []
+    for i in j:
+        goal = i * (value + other) * half           # in 2^-24 of a value's step
+        head = value * half << 24
+        want.append(goal // (value << 24) if goal < head else half + (goal - head) // (other << 24))
+    u = torch.tensor([[i / 2 ** 24] for i in j], device="cuda")
+    none = torch.zeros((16, 0), dtype=I64, device="cuda")
+    got, _ = gar.gar_verify_drafts(target.expand(16, 1, vocab), target.expand(16, 1, vocab)[:, :0], none, u)
+    assert got[:, 0].tolist() == want, [a - b for a, b in zip(got[:, 0].tolist(), want)]
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
+def test_long_rows(dtype):
+    """Drafts over a vocabulary whose rows are summed part by part; nothing left of the target; rows aligned alike and not."""
+    vocab, n = 2_300_003, 4
+    target, draft, tokens, uniform = _verify_case(n, 2, vocab, dtype, seed=6)
+    draft[1] = target[1, :2] * 2
+    uniform[1, 0], uniform[2:, 0] = 0.9, 0.99
+    more = torch.full((n, 3, vocab + 5), math.nan, dtype=target.dtype, device="cuda")
+    more[..., 1:1 + vocab] = target
+    want, want_accepted = _verify_reference(target, draft, tokens, uniform)
+    for p in (target, more[..., 1:1 + vocab]):
+        got, accepted = gar.gar_verify_drafts(p, draft, tokens, uniform)
+        assert torch.equal(got.cpu(), want) and torch.equal(accepted.cpu(), want_accepted)
