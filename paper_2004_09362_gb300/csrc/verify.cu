@@ -30,6 +30,7 @@ constexpr int kThreads = 256, kWarps = kThreads / 32;
 constexpr int kMostCtas = 8;  // of a cluster
 constexpr int kSubs = 4;      // pieces of a warp's run
 constexpr int kGroup = 4;     // neighbouring tokens of a lane
+constexpr float kUnit = 0x1p64f;  // sums are compared in multiples of 1 / kUnit, see up_to_unit()
 constexpr int kRounds = 64;   // sums are held in twice 32 bits over so many groups of a lane and piece
 
 struct VerifyArgs {
@@ -53,6 +54,12 @@ struct Sum {
     high = t;
   }
 };
+// A sum of probabilities times kUnit, exactly.  The product with u rounds to 2^-149 at best, which is a whole probability of the smallest;
+// of 2^-149 times kUnit it is 2^-64, and no sum comes to 2^95 (2^30 tokens).
+__device__ __forceinline__ Sum up_to_unit(Sum a) {
+  a.high *= kUnit, a.low *= kUnit;
+  return a;
+}
 // The low part no more than a rounding error of the high one.
 __device__ __forceinline__ Sum neat(Sum a) {
   Sum s;
@@ -252,7 +259,7 @@ __device__ __forceinline__ int find(const Row<T> &row, int64_t from, int64_t to,
     uint32_t counts = 0;  // which of the lane's tokens count
 #pragma unroll
     for (int i = 0; i < kGroup; ++i) {
-      const Sum w = remaining(p[i], q[i]);
+      const Sum w = up_to_unit(remaining(p[i], q[i]));
       if (w.high > 0.f) counts |= 1u << i;
       upto[i] = sum = sum + w;
     }
@@ -335,7 +342,7 @@ template <typename T, bool LONG> __global__ void __launch_bounds__(kThreads, 4) 
         add_run<T, DRAFT_NARROW>(row, begin, a.piece, a.vocab, shift, at, end, sums);
 #pragma unroll
       for (int i = 0; i < kSubs; ++i) {
-        pieces[i] = both(sums[i]);
+        pieces[i] = up_to_unit(both(sums[i]));
         if constexpr (LONG) whole[i] += in_64(pieces[i]), pieces[i] = in_twice_32(whole[i]);
       }
       if (!LONG || (at = end) >= a.piece) break;

@@ -1,5 +1,5 @@
 """The verification of drafts where a token hangs on the last bits of running sums: borders next to tokens that cannot be drawn,
-and sums of very many probabilities.  What is right is computed in whole numbers.
+sums of very many probabilities, and sums of very small ones.  What is right is computed in whole numbers.
 """
 
 import math
@@ -126,3 +126,23 @@ def test_long_rows(dtype):
     for p in (target, more[..., 1:1 + vocab]):
         got, accepted = gar.gar_verify_drafts(p, draft, tokens, uniform)
         assert torch.equal(got.cpu(), want) and torch.equal(accepted.cpu(), want_accepted)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("drafts", [0, 1])
+def test_sums_of_the_smallest_numbers(drafts):
+    """Eight tokens of 2^-149 each, all that there is or all that is left over of a draft: each is drawn by an eighth of the numbers."""
+    vocab, n = 24, 64
+    target = torch.zeros(n, drafts + 1, vocab, dtype=torch.float64)
+    target[:, 0, 1::3] = 2.0 ** -149
+    draft = torch.zeros(n, drafts, vocab, dtype=torch.float64)
+    uniform = torch.zeros(n, drafts + 1)
+    if drafts:
+        target[:, 0, ::3] = 0.0625
+        draft[:, 0, ::3] = 0.0625
+        draft[:, 0, 2::3] = 0.0625               # the refused one: token 2
+    uniform[:, -1] = (torch.arange(n) + 0.5) / n
+    tokens = torch.full((n, drafts), 2, dtype=I64, device="cuda")
+    got, accepted = gar.gar_verify_drafts(target.float().cuda(), draft.float().cuda(), tokens, uniform.cuda())
+    assert bool((accepted == 0).all())
+    assert got[:, 0].tolist() == [3 * (i // 8) + 1 for i in range(n)]
