@@ -308,15 +308,15 @@ int gar_prefix_attention(gar_attn_plan *plan, const gar_kv_cache *cache, const v
   const int64_t several = 4 * element_size(out_dtype);
   j.wide = (uintptr_t)out % several == 0 && dim % 4 == 0 && out_batch_stride % 4 == 0 && out_head_stride % 4 == 0;
   const int rows = share * group, blocks = blocks_of(rows);
+  // (That way rows past the end have scores of -infinity, which a factor of zero would not leave so.)
   if (many_queries(*plan, batch, groups) && element_size(cache->dtype) == 2 && takes_mma(*cache, q, q_batch_stride, q_head_stride, q_dtype) &&
-      (int64_t)groups * plan->kv_heads * blocks * (prefix.most_rows / kKeys + 2) < 1 << 30) {
+      prefix.scale_log2 != 0.f && (int64_t)groups * plan->kv_heads * blocks * (prefix.most_rows / kKeys + 2) < 1 << 30) {
     PrefixArgs p{};
     p.c = *cache, p.q = q, p.qb = q_batch_stride, p.qh = q_head_stride;
     p.table = prefix_table, p.table_stride = prefix_stride, p.lengths = prefix_lengths;
     p.page = prefix.page, p.by_heads = prefix.by_heads, p.most_rows = prefix.most_rows;
     p.groups = groups, p.share = share, p.heads_each = group, p.rows = rows, p.blocks = blocks;
-    // (not zero: rows past the end have scores of -infinity)
-    p.scale_log2 = std::max(std::fabs(prefix.scale_log2), 1e-37f), p.negate = prefix.scale_log2 < 0.f ? 0x80008000u : 0u;
+    p.scale_log2 = std::fabs(prefix.scale_log2), p.negate = prefix.scale_log2 < 0.f ? 0x80008000u : 0u;
     p.ctas = plan->sms, p.device = plan->device, p.give_up = plan->give_up, p.pair = rows > 128;
     prefix_partials(groups * plan->kv_heads * blocks, dim, static_cast<char *>(workspace) + half, &p);
     // Boxes of 8 rows and more that tiles consist of.

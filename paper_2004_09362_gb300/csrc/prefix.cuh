@@ -23,7 +23,7 @@ struct PrefixArgs {
   Divide page, by_heads;   // by a page's rows; by heads_each
   int most_rows;           // of the cache that the table's width can hold
   int groups, share, heads_each, rows, blocks;
-  float scale_log2;        // of the scores, not negative: q is negated where it was
+  float scale_log2;        // of the scores, positive: q is negated where it was not
   uint32_t negate;         // bits of q that are turned over
   int ctas, device, give_up;
   int box;                 // rows of the boxes that a tile can be copied in, or 0
