@@ -526,8 +526,11 @@ GAR_API int gar_decode_attention(gar_attn_plan *plan, const gar_kv_cache *cache,
  * limited size, and which drafted tokens stand.  The conventions of the decoding operators
  * hold; the paper has no counterpart. */
 
-/* Bytes of the workspace of a gar_prefix_attention call of `batch` sequences in `groups` groups.  Host-only. */
+/* Bytes of the workspace of a gar_prefix_attention call of `batch` sequences in `groups` groups: enough whatever the cache and the
+ * tables, and what a call over this cache with tables of these widths needs, which may be much less, or 0.  Host-only. */
 GAR_API int gar_prefix_attention_bytes(const gar_attn_plan *plan, int batch, int groups, size_t *bytes);
+GAR_API int gar_prefix_attention_call_bytes(const gar_attn_plan *plan, const gar_kv_cache *cache, int batch, int groups,
+                                            int prefix_width, int table_width, size_t *bytes);
 
 /* Attention of one new token per sequence, as gar_decode_attention, where the sequences b of a group
  * g = b / (batch / groups) share the rows that come first: those of prefix_table[g], below prefix_lengths[g];
@@ -540,8 +543,8 @@ GAR_API int gar_prefix_attention_bytes(const gar_attn_plan *plan, int batch, int
  * prefix_lengths count in [0, prefix_width * page_size].  So is precision, but where many queries share a prefix of 16 bits:
  * weights over it are two parts that keep 2^-16 of the weight (bf16) or 2^-22 of it or 2^-34 of the largest, whichever is more (f16),
  * and the tensor cores' sums of 16 tiles of 128 rows are off by 2^-15 at most.
- * workspace: 16-byte aligned, at least gar_prefix_attention_bytes, one for each call that may run at the same time
- * (what it held before does not matter).  The plan's own workspace is used too. */
+ * workspace: 16-byte aligned, at least gar_prefix_attention_call_bytes (NULL where that is 0), one for each call that may run at the
+ * same time (what it held before does not matter).  The plan's own workspace is used too. */
 GAR_API int gar_prefix_attention(gar_attn_plan *plan, const gar_kv_cache *cache, const void *q, int64_t q_batch_stride,
                                  int64_t q_head_stride, int q_dtype, void *out, int64_t out_batch_stride,
                                  int64_t out_head_stride, int out_dtype, float *lse, const int32_t *prefix_table,

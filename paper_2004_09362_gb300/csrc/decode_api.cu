@@ -91,18 +91,29 @@ int blocks_of(int rows) { return rows > 128 ? (rows + 255) / 256 : 1; }
 // MB, 20 and 32; 16 x 2000, 132 MB, 24 and 30; 64 x 500, 148 MB, 37 and 40; 120 x 1000 of 16/4 x 64 i8, 69 MB, 38 and 41.)
 constexpr double kReread = 128 << 20;
 
+bool reads_again(const gar_kv_cache &c, int batch, int prefix_width, int table_width) {
+  return ((double)prefix_width + table_width) * c.page_size * batch * c.heads * c.dim * element_size(c.dtype) * 2 <= kReread;
+}
+
 bool many_queries(const gar_attn_plan &plan, int batch, int groups) {
   if (groups == 0 || plan.dim > 128) return false;
   const int rows = batch / groups * (plan.q_heads / plan.kv_heads);
   return rows >= kManyQueries && (int64_t)groups * plan.kv_heads * blocks_of(rows) <= kManyItems;
 }
 
-// Bytes of a call's workspace: the own rows' results, and the prefixes' as they come from either way.
+// Bytes of a call's workspace, whatever the cache and the tables: the own rows' results, and the prefixes' as they come from either way.
 size_t prefix_bytes(const gar_attn_plan &plan, int batch, int groups) {
   const size_t both = prefix_workspace(batch, plan.q_heads, plan.dim, nullptr, nullptr);
   if (!many_queries(plan, batch, groups)) return both;
   const int items = groups * plan.kv_heads * blocks_of(batch / groups * (plan.q_heads / plan.kv_heads));
   return std::max(both, both / 2 + prefix_partials(items, plan.dim, nullptr, nullptr));
+}
+
+// What a call over this cache and tables of these widths needs of that: nothing in one launch, and partial results of the tensor cores' own
+// memory (20 to 155 MB) with 16-bit rows only.
+size_t call_bytes(const gar_attn_plan &plan, const gar_kv_cache &c, int batch, int groups, int prefix_width, int table_width) {
+  if (batch == 0 || reads_again(c, batch, prefix_width, table_width)) return 0;
+  return element_size(c.dtype) == 2 ? prefix_bytes(plan, batch, groups) : prefix_workspace(batch, plan.q_heads, plan.dim, nullptr, nullptr);
 }
 
 // The arguments that follow from the plan, the cache and what a call has set.
@@ -248,6 +259,17 @@ int gar_prefix_attention_bytes(const gar_attn_plan *plan, int batch, int groups,
   return GAR_OK;
 }
 
+int gar_prefix_attention_call_bytes(const gar_attn_plan *plan, const gar_kv_cache *cache, int batch, int groups, int prefix_width,
+                                    int table_width, size_t *bytes) {
+  if (plan == nullptr || bytes == nullptr) return refuse("null plan or output");
+  if (int rc = check_cache(cache)) return rc;
+  if (cache->heads != plan->kv_heads || cache->dim != plan->dim) return refuse("the cache's heads or dim are not the plan's");
+  if (int rc = check_groups(plan, batch, groups)) return rc;
+  if (table_width < 0 || prefix_width < 0) return refuse("negative table_width or prefix_width");
+  *bytes = call_bytes(*plan, *cache, batch, groups, prefix_width, table_width);
+  return GAR_OK;
+}
+
 int gar_prefix_attention(gar_attn_plan *plan, const gar_kv_cache *cache, const void *q, int64_t q_batch_stride,
                          int64_t q_head_stride, int q_dtype, void *out, int64_t out_batch_stride, int64_t out_head_stride,
                          int out_dtype, float *lse, const int32_t *prefix_table, int64_t prefix_stride, int prefix_width,
@@ -273,8 +295,9 @@ int gar_prefix_attention(gar_attn_plan *plan, const gar_kv_cache *cache, const v
   }
   const int dim = plan->dim, heads = plan->q_heads, group = heads / plan->kv_heads, share = batch / groups;
   PrefixParts parts[2];
-  if (workspace == nullptr || workspace_bytes < prefix_bytes(*plan, batch, groups)) {
-    set_error("the workspace is smaller than gar_prefix_attention_bytes");
+  const size_t need = call_bytes(*plan, *cache, batch, groups, prefix_width, table_width);
+  if (need > 0 && (workspace == nullptr || workspace_bytes < need)) {
+    set_error("the workspace is smaller than gar_prefix_attention_call_bytes");
     return GAR_ENOWS;
   }
   const size_t half = prefix_workspace(batch, heads, dim, static_cast<char *>(workspace), parts) / 2;
@@ -291,7 +314,7 @@ int gar_prefix_attention(gar_attn_plan *plan, const gar_kv_cache *cache, const v
   prefix.batch = groups, prefix.group = share * group;
   prefix.share = share, prefix.heads_each = group, prefix.by_heads = divide_by((uint32_t)group);
   const int64_t own_rows = (int64_t)table_width * cache->page_size, prefix_rows = (int64_t)prefix_width * cache->page_size;
-  if ((double)(own_rows + prefix_rows) * batch * cache->heads * dim * element_size(cache->dtype) * 2 <= kReread) {
+  if (reads_again(*cache, batch, prefix_width, table_width)) {
     // As sequences of their own, the prefix's rows first.
     own.out = out, own.lse = lse, own.ob = out_batch_stride, own.oh = out_head_stride, own.out_dtype = out_dtype;
     own.before_table = prefix_table, own.before_stride = prefix_stride, own.before_lengths = prefix_lengths;

@@ -596,10 +596,12 @@ PyObject *prefix_attention(PyObject *, PyObject *const *args, Py_ssize_t n, PyOb
     refuse_graded({&q, &out, &lse});
     const Stream stream(a.at[10], device.check());
     size_t bytes = 0;
-    check(gar_prefix_attention_bytes(plan, batch, groups, &bytes), "gar_prefix_attention_bytes");
+    check(gar_prefix_attention_call_bytes(plan, cache, batch, groups, (int)prefix.size(1), (int)table.size(1), &bytes),
+          "gar_prefix_attention_call_bytes");
     use_workspace(a.at[0], a.at[1], stream);
     // (freed at the end: for what comes next on the stream)
-    const Tensor workspace = stream.empty({(int64_t)bytes}, at::kByte, q);
+    Tensor workspace;
+    if (bytes > 0) workspace = stream.empty({(int64_t)bytes}, at::kByte, q);
     if (!a.at[8]) out = stream.empty(q.sizes(), q.scalar_type(), q);
     if (wanted && !given) lse = stream.empty(q.sizes().slice(0, 2), at::kFloat, q);
     const double scale = a.at[7] ? number(a.at[7]) : 1.0 / std::sqrt((double)shape[2]);
@@ -609,7 +611,8 @@ PyObject *prefix_attention(PyObject *, PyObject *const *args, Py_ssize_t n, PyOb
                                static_cast<const int32_t *>(prefix.data_ptr()), prefix.stride(0), (int)prefix.size(1),
                                static_cast<const int32_t *>(prefix_lengths.data_ptr()), groups,
                                static_cast<const int32_t *>(table.data_ptr()), table.stride(0), (int)table.size(1),
-                               static_cast<const int32_t *>(lengths.data_ptr()), batch, (float)scale, workspace.data_ptr(), bytes,
+                               static_cast<const int32_t *>(lengths.data_ptr()), batch, (float)scale,
+                               bytes > 0 ? workspace.data_ptr() : nullptr, bytes,
                                stream.raw),
           "gar_prefix_attention");
     if (a.at[8]) changed(out);

@@ -52,7 +52,7 @@ EXPORTS = (
     "gar_plan_create_group", "gar_rope_frequencies", "gar_rope_table", "gar_rope", "gar_kv_write",
     "gar_kv_read", "gar_kv_status", "gar_attn_plan_create", "gar_attn_plan_destroy",
     "gar_attn_plan_shape", "gar_attn_plan_bytes", "gar_attn_plan_set_workspace", "gar_attn_plan_debug_wait", "gar_decode_attention",
-    "gar_prefix_attention_bytes", "gar_prefix_attention", "gar_kv_weigh", "gar_kv_evict", "gar_verify_drafts",
+    "gar_prefix_attention_bytes", "gar_prefix_attention_call_bytes", "gar_prefix_attention", "gar_kv_weigh", "gar_kv_evict", "gar_verify_drafts",
 )
 
 
@@ -131,6 +131,7 @@ def _load():
         "gar_decode_attention": (i32, [vp, P_(gar_kv_cache), vp, i64, i64, i32, vp, i64, i64, i32, vp, vp,
                                        i64, i32, vp, i32, f32, i32, vp]),
         "gar_prefix_attention_bytes": (i32, [vp, i32, i32, P_(sz)]),
+        "gar_prefix_attention_call_bytes": (i32, [vp, P_(gar_kv_cache), i32, i32, i32, i32, P_(sz)]),
         "gar_prefix_attention": (i32, [vp, P_(gar_kv_cache), vp, i64, i64, i32, vp, i64, i64, i32, vp, vp, i64, i32, vp,
                                        i32, vp, i64, i32, vp, i32, f32, vp, sz, vp]),
         "gar_kv_weigh": (i32, [P_(gar_kv_cache), vp, i64, i64, i32, i32, vp, vp, i64, i64, vp, i64, i64, i64, vp, i64, i32,
@@ -686,6 +687,14 @@ def gar_prefix_attention_bytes(plan: AttnPlan, batch: int, groups: int) -> int:
     n = ctypes.c_size_t()
     _check(_lib.gar_prefix_attention_bytes(plan.handle, _narrow(batch, "batch"), _narrow(groups, "groups"), ctypes.byref(n)),
            "gar_prefix_attention_bytes")
+    return n.value
+
+
+def gar_prefix_attention_call_bytes(plan: AttnPlan, cache: KVCache, batch: int, groups: int, prefix_width: int, table_width: int) -> int:
+    n = ctypes.c_size_t()
+    _check(_lib.gar_prefix_attention_call_bytes(plan.handle, ctypes.byref(cache._c), _narrow(batch, "batch"), _narrow(groups, "groups"),
+                                                _narrow(prefix_width, "prefix_width"), _narrow(table_width, "table_width"), ctypes.byref(n)),
+           "gar_prefix_attention_call_bytes")
     return n.value
 
 
