@@ -493,6 +493,12 @@ template <typename T, int DP, bool PAIR> __global__ void __launch_bounds__(kThre
           l += (sum[0].x + sum[1].x) + (sum[0].y + sum[1].y);
           wait_tensor_stores();
         }
+        if (i == halves - 1) {
+          // The last products but one.  They are waited for before this warp arrives, as the last cannot end until it does: a barrier tells whether
+          // the latest of its phases is the one asked for, and once the last has ended, a wait for the one before does not end.
+          good = __all_sync(~0u, wait_phase(at(values[s]), (done - 1) & 1, late));
+          if (!good) break;
+        }
         ++done;
         tensor_before_sync();
         __syncwarp();
@@ -502,8 +508,7 @@ template <typename T, int DP, bool PAIR> __global__ void __launch_bounds__(kThre
       const bool first = halves == 0;
       if (!good) continue;
       if (!first) {
-        // (a barrier tells a phase from the next only: the last but one first)
-        good = __all_sync(~0u, wait_phase(at(values[s]), (done - 2) & 1, late) && wait_phase(at(values[s]), (done - 1) & 1, late));
+        good = __all_sync(~0u, wait_phase(at(values[s]), (done - 1) & 1, late));
         if (!good) continue;
         tensor_after_sync();
       }

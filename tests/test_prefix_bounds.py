@@ -142,6 +142,24 @@ def test_every_half_tile_has_its_weight(kind, dim, page_size, order, share, q_he
     gar.gar_kv_status(cache)
 
 
+@pytest.mark.gpu
+@pytest.mark.parametrize("groups,share,q_heads,heads,dim,page_size,kind", [
+    (64, 8, 32, 8, 128, 16, "bf16"), (128, 5, 32, 8, 128, 16, "bf16"), (60, 20, 8, 8, 64, 64, "f16"), (40, 40, 32, 8, 128, 24, "f16"), (150, 17, 4, 4, 64, 128, "bf16")])
+def test_many_parts_to_a_cta(groups, share, q_heads, heads, dim, page_size, kind):
+    """Many prefixes of one to some dozen tiles: each CTA takes many parts, one after the other, and no wait runs out."""
+    prefixes = [max(0, int(2000 * ((g * 0.6180339887498949) % 1.0))) for g in range(groups)]
+    own = [1 + b % share for b in range(groups * share)]
+    cache, pt, pn, t, n, q, both = _prefix_case(prefixes, own, share, q_heads, heads, dim, page_size, kind, kind, every=53)
+    plan = gar.gar_attn_plan_create(q_heads, heads, dim)
+    out, lse = gar.gar_prefix_attention(plan, q, cache, pt, pn, t, n, lse=True)
+    gar.gar_kv_status(cache)
+    _check_prefix(out[::53], lse[::53], q[::53], both, dim ** -0.5, kind)
+    for _ in range(30):
+        again = gar.gar_prefix_attention(plan, q, cache, pt, pn, t, n, lse=True)
+        assert torch.equal(out, again[0]) and torch.equal(lse, again[1])
+    gar.gar_kv_status(cache)
+
+
 # ---------------------------------------------------------------------------- precision
 
 @pytest.mark.gpu
