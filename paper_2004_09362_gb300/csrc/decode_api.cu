@@ -83,7 +83,9 @@ int check_groups(const gar_attn_plan *plan, int batch, int groups) {
 // other kernel takes for one reading of the rows.  (The two, 8 cached heads x 128: 65536 rows bf16, 16 queries 96 us and 83, 24 95 and 118,
 // 64 96 and 220; 20000 rows f16, 16 queries 56 and 49, 24 54 and 59.)
 constexpr int kManyQueries = 17;
-constexpr int kManyItems = 1024;  // blocks of queries at most: each has 132 KB of partial results
+// Blocks of queries at most: each has 132 KB of partial results.  (With many prefixes there is not much to gain: 129 prefixes of up to 2000 rows, 20 queries,
+// 1032 blocks, 271 us the other way and 302 this, of up to 500 rows 186 and 203; 128 x 2000 264 and 293; 64 x 2000, 32 queries, 512 blocks, 177 both.)
+constexpr int kManyItems = 1024;
 int blocks_of(int rows) { return rows > 128 ? (rows + 255) / 256 : 1; }
 
 // Bytes of all sequences' rows, a shared one counted for each, up to which they are read for each sequence, mostly from the L2, in one

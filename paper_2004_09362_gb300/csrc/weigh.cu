@@ -118,7 +118,9 @@ template <typename C, int KC, bool Q32> struct WeighShape {
   static constexpr int PARTS = Q32 ? 2 : 1;
   static constexpr int CHUNKS = 4 * KC, ROW = 64 * KC;         // of a row: chunks, bytes
   static constexpr int kStage = 16 * ROW + 128;                // a tile's keys, 16 weights, 16 scales
-  static constexpr int kResident = KC <= 4 ? 2 : 1;            // CTAs of an SM
+  // CTAs of an SM, and tiles of a ring: two where their rings fit.  (24 x 8192, 32/8 heads x 128 bf16 49 us, by one CTA 59; i8 41 and 55; x 96 bf16 43 and 55.  Rings
+  // of half as many tiles 48, 41 and 42; of half as many again, which leaves one CTA for up to 192 bytes, 49, 58 and 57.)
+  static constexpr int kResident = KC <= 4 ? 2 : 1;
   static constexpr int kStages = KC == 1 ? 8 : KC == 2 ? 6 : KC == 3 ? 4 : 3;
   static constexpr int kRings = kWarps * kStages * kStage;
   // Where chunk c of row r lies: rows of a multiple of 128 bytes twisted, so that the 8 lanes of a read meet all banks.
@@ -463,6 +465,8 @@ extern "C" int gar_kv_weigh(const gar_kv_cache *cache, const void *q, int64_t q_
   d.page = divide_by((uint32_t)cache->page_size), d.items = divide_by((uint32_t)cache->heads);
   d.most_rows = most_rows, d.batch = batch, d.q_heads = q_heads, d.window = window, d.unit = unit, d.device = dev;
   d.group = d.item_heads = q_heads / cache->heads, d.item_groups = 1, d.line = true;
+  // What a segment costs beside its rows: the units of 64 rows that 32 KB of keys are.  (That, a quarter and four times as much: 24 x 8192, 32/8 x 128 bf16 49, 51 and 49 us; i8 41, 44 and 42; f32
+  // 239, 239 and 250; 128 x 500, 32/8 x 64 bf16 20, 28 and 20; 16 x 8192, 16/4 x 256 f16 35, 35 and 31.)
   d.slack = std::max(1, 32768 / (64 * cache->dim * element_size(cache->dtype)));
   d.scale_log2 = (float)((double)scale * 1.4426950408889634);
   a.lse = lse, a.weights = weights, a.out = out, a.rows = rows, a.apart = out != weights;
