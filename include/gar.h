@@ -541,7 +541,7 @@ GAR_API int gar_prefix_attention_call_bytes(const gar_attn_plan *plan, const gar
  * their own rows the pages that they were written to, each length one more than the one before.
  * Pages, lengths, strides, dtypes and what the status word says are as in gar_decode_attention;
  * prefix_lengths count in [0, prefix_width * page_size].  So is precision, but where many queries share a prefix of 16 bits:
- * weights over it are two parts that keep 2^-16 of the weight (bf16) or 2^-22 of it or 2^-34 of the largest, whichever is more (f16),
+ * weights over it are two parts that keep 2^-17 of the weight (bf16) or 2^-22 of it or 2^-34 of the largest, whichever is more (f16),
  * and the tensor cores' sums of 16 tiles of 128 rows are off by 2^-15 at most.
  * workspace: 16-byte aligned, at least gar_prefix_attention_call_bytes (NULL where that is 0), one for each call that may run at the
  * same time (what it held before does not matter).  The plan's own workspace is used too. */

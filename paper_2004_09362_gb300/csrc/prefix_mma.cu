@@ -10,7 +10,7 @@
 //  * A thread for each stream issues its products.  S and O are in tensor memory, 128 columns each.  S is computed by halves of 64 rows, the
 //    next half's while the weights of one are computed (16384 rows x 1000 queries: 171 us a call, with whole tiles 180).
 //  * 4 warps for each stream turn S to P, a query to a thread: no exchange between lanes.  P goes where S was, as two 16-bit parts
-//    (2^-16 of the weight; one part alone would be 2^-9, as much as the output's rounding, and saved a tenth), 16 columns each for
+//    (2^-17 of the weight in bf16; one part alone would be 2^-9, as much as the output's rounding, and saved a tenth), 16 columns each for
 //    32 rows.  These warps have 192 registers, the others 64: a half's scores fit them.
 //  * The tensor cores cut their sums off rather than round them: 2^-24 and more of the sum for each of 16 products a tile, all one way (parts
 //    of 1024 tiles came out 1.6e-3 short, of 54 tiles 3e-5).  So O holds 16 tiles at most, and is then added to the part's result in
@@ -49,11 +49,10 @@ template <> struct Parts<__half> {
   static constexpr float kLazy = 5.f, kUnit = 10.f;
 };
 
-// Two weights as a high and a low part each.  (bf16: the high part is cut off, the low one rounded: 2^-16 of the weight.)
+// Two weights as a high and a low part each, both rounded: the high one is off by 2^-9 of the weight (bf16), the low one by 2^-8 of that.
 __device__ __forceinline__ void split_weights(float2 p, uint32_t *hi, uint32_t *lo, __nv_bfloat16) {
-  const uint32_t x = __float_as_uint(p.x), y = __float_as_uint(p.y);
-  *hi = __byte_perm(x, y, 0x7632);
-  *lo = pack2(add2(p, make_float2(__uint_as_float(x & 0xffff0000u ^ 0x80000000u), __uint_as_float(y & 0xffff0000u ^ 0x80000000u))), __nv_bfloat16());
+  *hi = pack2(p, __nv_bfloat16());
+  *lo = pack2(fma2(unpack2(*hi, __nv_bfloat16()), make_float2(-1.f, -1.f), p), __nv_bfloat16());
 }
 __device__ __forceinline__ void split_weights(float2 p, uint32_t *hi, uint32_t *lo, __half) {
   *hi = pack2(p, __half());

@@ -22,11 +22,11 @@ def _bounds(out, lse, q, both, scale, kind, out_type):
     """Bounds.  A score, `dim` products in 32 bits (over 32-bit caches of two parts each, 2^-21; 8-bit ones of codes and queries, 2^-22, and a scale)
     and three roundings more, is off by e = (dim + 8) u + 2^-21 of scale sum|q||k|; the same counts for its difference to the maximum.  The weight has 2^-22 more;
     its parts keep 2^-21 (f32), 2^-22 of it and 2^-39 of the largest product of a weight and a scale (8 bits, f16), 2^-17 (bf16); on the tensor memory's
-    way 2^-16 (bf16) or 2^-22 and 2^-34 of the largest (f16), and sums of up to 16 tiles 2^-15 (here: one tile of 16 products of a truncation each,
+    way 2^-17 (bf16) or 2^-22 and 2^-34 of the largest (f16), and sums of up to 16 tiles 2^-15 (here: one tile of 16 products of a truncation each,
     2^-19).  32-bit sums over n rows: chains of n / 64 at most, rounded, and joins of lanes, warps and parts, n / 64 + 32 roundings.  The two
     parts' weights come from logarithms off by 2^-22 of themselves and 2^-22, and from exponentials, a sum and a quotient, 2^-21 together."""
     group = q.shape[1] // both[0][0].shape[1]
-    weight = {"f32": 2.0 ** -21, "bf16": 2.0 ** -16 + 2.0 ** -19, "f16": 2.0 ** -22 + 2.0 ** -19, "i8": 2.0 ** -22, "e4m3": 2.0 ** -22}[kind]
+    weight = {"f32": 2.0 ** -21, "bf16": 2.0 ** -17 + 2.0 ** -19, "f16": 2.0 ** -22 + 2.0 ** -19, "i8": 2.0 ** -22, "e4m3": 2.0 ** -22}[kind]
     least = {"f16": 2.0 ** -34}.get(kind, 2.0 ** -39)
     for b in range(q.shape[0]):
         k, v = (x.repeat_interleave(group, 1) for x in both[b])
@@ -174,6 +174,30 @@ def test_each_types_precision(kind, dtype, q_heads, kv_heads, dim, share, prefix
     out = torch.empty(q.shape, device="cuda")
     _, lse = gar.gar_prefix_attention(plan, q, cache, pt, pn, t, n, lse=True, out=out)
     _bounds(out, lse, q, both, dim ** -0.5, kind, "f32")
+    gar.gar_kv_status(cache)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("kind,wide", [("bf16", True), ("bf16", False), ("f16", True), ("f16", False)])
+def test_weights_come_out_as_their_parts_hold_them(kind, wide):
+    """Each row's value marks a channel of its own, so its weight comes out alone.  Scores are one product, exact, of 3 at most, times a rounded factor: 2^-20;
+    weights 2^-22, their parts 2^-17 (bf16) or 2^-22 (f16, and 2^-34 of the largest, 2^9 times the smallest), sums of weights and joins 2^-20."""
+    n, dim, share = 128, 128, 40
+    cache, pt, pn, t, lens, q, _ = _prefix_case([n], [0] * share, share, 8, 2, dim, 16, kind, kind, wide=wide)
+    at = torch.arange(n, device="cuda")
+    page = pt[0, at // 16].long()
+    mark = ((at * 37) % 192 - 96) / 32
+    cache.k.zero_()
+    cache.v.zero_()
+    cache.k[page, :, at % 16, 0] = mark.to(cache.k.dtype)[:, None]
+    cache.v[page, :, at % 16, at] = 1
+    q.zero_()
+    q[..., 0] = (1 - torch.arange(share, device="cuda") / 64).to(q.dtype)[:, None]
+    out = torch.empty(q.shape, device="cuda")
+    gar.gar_prefix_attention(gar.gar_attn_plan_create(8, 2, dim), q, cache, pt, pn, t, lens, scale=1.0, out=out)
+    want = torch.softmax(q[..., :1].double() * mark.double(), -1)
+    off = float(((out.double() - want).abs() / want).max())
+    assert off <= (2.0 ** -17 if kind == "bf16" else 2.0 ** -22 + 2.0 ** -25) + 2.0 ** -20 + 2.0 ** -22 + 2.0 ** -20, off
     gar.gar_kv_status(cache)
 
 
